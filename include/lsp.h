@@ -59,12 +59,16 @@ typedef enum {
     LSP_ERR_INDEX     = -6,  /* lsp_validate_projector found an index outside [0, r) */
     LSP_ERR_ALIGN     = -7,  /* a base pointer is not 16-byte aligned */
     LSP_ERR_SKEW      = -8,  /* lsp_plan_build: the columns of Q are used too unevenly for a plan; use lsp_compress */
-    LSP_ERR_TOO_LARGE = -9   /* lsp_compress_planned_static: the problem needs more than LSP_STATIC_SCRATCH_BYTES of scratch */
+    LSP_ERR_TOO_LARGE = -9,  /* lsp_compress_planned_static: the problem needs more than LSP_STATIC_SCRATCH_BYTES of scratch */
+    LSP_ERR_VALUE     = -10  /* a number is out of its range: a dropout not in [0, 1), a scale that is not finite, a negative eps */
 } lsp_status;
 
 #define LSP_MAX_R 2048       /* largest supported subspace size (the paper's largest setting) */
 #define LSP_MAX_D 64         /* largest supported number of entries per projector row */
 #define LSP_MAX_GROUP 16     /* most problems in one grouped call */
+#define LSP_MAX_HEAD_DIM 128 /* widest head of the attention calls */
+#define LSP_MAX_WIDTH 8192   /* longest row of the residual-norm calls */
+#define LSP_MAX_ROWS (1 << 22)   /* most rows of one residual-norm call */
 #define LSP_STATIC_SCRATCH_BYTES (24u << 20)   /* scratch held inside the library image, per GPU (lsp_compress_planned_static) */
 
 /* ------------------------------------------------------------------------------------------
@@ -366,6 +370,134 @@ size_t lsp_bias_gradient_workspace_bytes(int64_t m, int64_t n, int32_t r, int32_
  */
 int lsp_plan_refresh_values(void* plan, const float* P_val, const float* Q_val,
                             int64_t m, int64_t n, int32_t r, int32_t d, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * The operators of a training step that are no plain matrix products: what a transformer block
+ * does between its weights on the GPU ("forwardBackward", Alg. 1) and so what makes the weight
+ * gradients that compress takes.  They follow the rules above (device pointers, no allocation, no
+ * synchronisation, checks before the first HIP call).  Descriptors are HOST structures, read during
+ * the call only.
+ *
+ * Dropout.  A mask is a function of (seed, offset, place) and is never stored, so the backward pass
+ * makes the same one again.  Philox4x32 with 7 rounds (Salmon, Moraes, Dror and Shaw, "Parallel random
+ * numbers: as easy as 1, 2, 3", SC 2011) under the key (low half of seed, high half) turns a counter
+ * of four 32-bit words into eight 16-bit words, lower half of each output word first: one for each of
+ * eight elements that follow one another.  An element is dropped when its word is below
+ * t = round(65536 dropout) and otherwise scaled by 65536 / (65536 - t).  Counters: for an element of a
+ * matrix, (low half, high half of row * ceil(width / 8) + column / 8, 0, offset); for a probability,
+ * (key / 8, query, batch * heads + head, offset).  Calls whose masks have to be independent use
+ * different offsets (or seeds); dropout 0 keeps everything as it is.
+ *
+ * lsp_dropout:  y := drop(x), element by element; its backward pass is the same call on the gradient.
+ *   x, y   device, [rows][width] of `dtype`, rows one behind the other; y may be x; at most 2^31 blocks of eight
+ */
+int lsp_dropout(const void* x, void* y, int64_t rows, int64_t width, float dropout, uint64_t seed, uint32_t offset,
+                lsp_dtype dtype, void* stream);
+
+/* Attention:  O = drop(P) V,  P = softmax(scale Q K^T) over the keys that a query sees,
+ *             L = log of the sum of exp(scale q . k) over these keys (fp32, kept for the backward pass).
+ * Query i of batch b counts when i < q_lens[b], key j when j < k_lens[b] (lengths outside [0, q_len] and
+ * [0, k_len] are taken as the nearer end; NULL: all count).  Query i sees key j when both count and,
+ * if causal, j - k_lens[b] <= i - q_lens[b] (the last query sees every key).  A query that does not count
+ * or sees nothing has O = 0, L = -infinity and gets and gives no gradient; rows that do not count are
+ * not read (they may hold anything), but those of O, dQ, dK and dV are written (zeros).
+ * Query head h reads key head h / (heads / kv_heads).
+ *   Q, O, dO, dQ    device, [batch][q_len][heads][head_dim] of `dtype`; K, V, dK, dV  [batch][k_len][kv_heads][head_dim];
+ *                   each with the strides given (of batch, position and head, in elements; the last axis is
+ *                   contiguous), so views into a joint projection serve as they are.  Strides are multiples of
+ *                   16 bytes and a position's is below 8 MiB
+ *   L               device, [batch][heads][q_len] fp32
+ *   head_dim        a multiple of 8, at most LSP_MAX_HEAD_DIM;  scale > 0;  batch * heads * (q_len or k_len) below 2^27
+ * The products run on the matrix cores in `dtype` with fp32 accumulation (fp32: in fp32); scores, softmax
+ * statistics and sums are fp32; probabilities and the gradients of the scores are rounded to `dtype` as
+ * operands of the second products.  No atomics: results are the same bits from run to run.
+ * The backward pass computes the probabilities again from Q, K and L; it needs the same problem with O and L
+ * as the forward pass left them.  Non-finite elements of a row that counts reach the rows that see it, and may
+ * reach others.
+ * Workspaces: 16-byte aligned, as large as the queries say (0 bytes needed: may be NULL). */
+typedef struct {
+    const void*    Q;
+    const void*    K;
+    const void*    V;
+    void*          O;
+    float*         L;
+    const int32_t* q_lens;         /* device, [batch], or NULL */
+    const int32_t* k_lens;
+    int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];   /* batch, position, head */
+    int32_t batch, heads, kv_heads, q_len, k_len, head_dim;
+    int32_t causal;                /* 0 or 1 */
+    float   scale, dropout;
+    uint32_t offset;
+    uint64_t seed;
+} lsp_attention_problem;
+
+typedef struct {
+    const void* dO;
+    void*       dQ;
+    void*       dK;
+    void*       dV;
+    int64_t do_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];
+} lsp_attention_gradients;
+
+size_t lsp_attention_forward_workspace_bytes(const lsp_attention_problem* problem, lsp_dtype dtype);
+int    lsp_attention_forward(const lsp_attention_problem* problem, lsp_dtype dtype, void* workspace, size_t workspace_bytes, void* stream);
+size_t lsp_attention_backward_workspace_bytes(const lsp_attention_problem* problem, lsp_dtype dtype);
+int    lsp_attention_backward(const lsp_attention_problem* problem, const lsp_attention_gradients* gradients, lsp_dtype dtype,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* Between two blocks:  u = norm(f) (after a block),  y = residual_scale x + branch_scale gate * drop(u)
+ * (the residual stream),  h = norm(y) (before the next block), each row by itself:
+ *   LSP_NORM_NONE   norm(v) = v                        (weight and bias are ignored)
+ *   LSP_NORM_RMS    norm(v) = v / sqrt(mean(v^2) + eps) * weight [+ bias]
+ *   LSP_NORM_LAYER  norm(v) = (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) * weight [+ bias]
+ * All in fp32; y and h are rounded once each (h is made from the y before rounding).
+ *   x, f, y, h      device, [rows][width] of `dtype` with the row strides given (elements, at least width).  y may be x;
+ *                   h may be NULL, with pre = LSP_NORM_NONE
+ *   weights, biases, gate   device, [width] of `dtype`; NULL: ones, zeros, ones
+ *   stats           device, [4][rows] fp32, kept for the backward pass: mean of f, 1 / deviation of f, the same of y
+ * The backward pass takes the gradients of y (dy) and h (dh; NULL where h is) and gives those of x and f and,
+ * where asked for (not NULL), of the weights, biases and gate (fp32, [width], overwritten; sums over the rows in an
+ * order that does not change from run to run).  It needs x and f as the forward pass had them (so y must not
+ * be x then), and its stats.  dx may be dy. */
+typedef enum { LSP_NORM_NONE = 0, LSP_NORM_RMS = 1, LSP_NORM_LAYER = 2 } lsp_norm;
+
+typedef struct {
+    const void* x;
+    const void* f;
+    void*       y;
+    void*       h;
+    float*      stats;
+    const void* post_weight;       /* of the norm of f */
+    const void* post_bias;
+    const void* gate;
+    const void* pre_weight;        /* of the norm of y */
+    const void* pre_bias;
+    int64_t x_stride, f_stride, y_stride, h_stride;
+    int64_t rows;
+    int32_t width;
+    int32_t post, pre;             /* lsp_norm */
+    float   eps, residual_scale, branch_scale, dropout;
+    uint32_t offset;
+    uint64_t seed;
+} lsp_residual_norm_problem;
+
+typedef struct {
+    const void* dy;
+    const void* dh;
+    void*       dx;
+    void*       df;
+    float*      post_weight;
+    float*      post_bias;
+    float*      gate;
+    float*      pre_weight;
+    float*      pre_bias;
+    int64_t dy_stride, dh_stride, dx_stride, df_stride;
+} lsp_residual_norm_gradients;
+
+int    lsp_residual_norm_forward(const lsp_residual_norm_problem* problem, lsp_dtype dtype, void* stream);
+size_t lsp_residual_norm_backward_workspace_bytes(const lsp_residual_norm_problem* problem, lsp_dtype dtype);
+int    lsp_residual_norm_backward(const lsp_residual_norm_problem* problem, const lsp_residual_norm_gradients* gradients, lsp_dtype dtype,
+                                  void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------
  * Utilities.

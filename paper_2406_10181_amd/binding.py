@@ -24,6 +24,47 @@ class lsp_apply_item(ctypes.Structure):
                 ("Q_idx", ctypes.c_void_p), ("Q_val", ctypes.c_void_p), ("m", ctypes.c_int64), ("n", ctypes.c_int64)]
 
 
+_three = ctypes.c_int64 * 3
+
+
+class lsp_attention_problem(ctypes.Structure):
+    """What both attention calls take (field for field the C struct)."""
+    _fields_ = [("Q", ctypes.c_void_p), ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("O", ctypes.c_void_p), ("L", ctypes.c_void_p),
+                ("q_lens", ctypes.c_void_p), ("k_lens", ctypes.c_void_p),
+                ("q_stride", _three), ("k_stride", _three), ("v_stride", _three), ("o_stride", _three),
+                ("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("q_len", ctypes.c_int32),
+                ("k_len", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("dropout", ctypes.c_float), ("offset", ctypes.c_uint32), ("seed", ctypes.c_uint64)]
+
+
+class lsp_attention_gradients(ctypes.Structure):
+    """What lsp_attention_backward takes besides (field for field the C struct)."""
+    _fields_ = [("dO", ctypes.c_void_p), ("dQ", ctypes.c_void_p), ("dK", ctypes.c_void_p), ("dV", ctypes.c_void_p),
+                ("do_stride", _three), ("dq_stride", _three), ("dk_stride", _three), ("dv_stride", _three)]
+
+
+class lsp_residual_norm_problem(ctypes.Structure):
+    """What both residual-norm calls take (field for field the C struct)."""
+    _fields_ = [("x", ctypes.c_void_p), ("f", ctypes.c_void_p), ("y", ctypes.c_void_p), ("h", ctypes.c_void_p), ("stats", ctypes.c_void_p),
+                ("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p), ("gate", ctypes.c_void_p),
+                ("pre_weight", ctypes.c_void_p), ("pre_bias", ctypes.c_void_p),
+                ("x_stride", ctypes.c_int64), ("f_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64), ("h_stride", ctypes.c_int64),
+                ("rows", ctypes.c_int64), ("width", ctypes.c_int32), ("post", ctypes.c_int32), ("pre", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float), ("branch_scale", ctypes.c_float), ("dropout", ctypes.c_float),
+                ("offset", ctypes.c_uint32), ("seed", ctypes.c_uint64)]
+
+
+class lsp_residual_norm_gradients(ctypes.Structure):
+    """What lsp_residual_norm_backward takes besides (field for field the C struct)."""
+    _fields_ = [("dy", ctypes.c_void_p), ("dh", ctypes.c_void_p), ("dx", ctypes.c_void_p), ("df", ctypes.c_void_p),
+                ("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p), ("gate", ctypes.c_void_p),
+                ("pre_weight", ctypes.c_void_p), ("pre_bias", ctypes.c_void_p),
+                ("dy_stride", ctypes.c_int64), ("dh_stride", ctypes.c_int64), ("dx_stride", ctypes.c_int64), ("df_stride", ctypes.c_int64)]
+
+
+NORM_KIND = {"none": 0, "rms": 1, "layer": 2}
+
+
 class LspError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -107,6 +148,19 @@ def lib() -> ctypes.CDLL:
         L.lsp_hbm_probe_rmw.restype = ctypes.c_int
         L.lsp_validate_projector.argtypes = [vp, i64, i32, i32, vp, vp]
         L.lsp_validate_projector.restype = ctypes.c_int
+        L.lsp_dropout.argtypes = [vp, vp, i64, i64, ctypes.c_float, ctypes.c_uint64, ctypes.c_uint32, i32, vp]
+        L.lsp_dropout.restype = ctypes.c_int
+        for name in ("lsp_attention_forward_workspace_bytes", "lsp_attention_backward_workspace_bytes", "lsp_residual_norm_backward_workspace_bytes"):
+            getattr(L, name).argtypes = [vp, i32]
+            getattr(L, name).restype = sz
+        L.lsp_attention_forward.argtypes = [vp, i32, vp, sz, vp]
+        L.lsp_attention_forward.restype = ctypes.c_int
+        L.lsp_attention_backward.argtypes = [vp, vp, i32, vp, sz, vp]
+        L.lsp_attention_backward.restype = ctypes.c_int
+        L.lsp_residual_norm_forward.argtypes = [vp, i32, vp]
+        L.lsp_residual_norm_forward.restype = ctypes.c_int
+        L.lsp_residual_norm_backward.argtypes = [vp, vp, i32, vp, sz, vp]
+        L.lsp_residual_norm_backward.restype = ctypes.c_int
         L.lsp_strerror.argtypes = [ctypes.c_int]
         L.lsp_strerror.restype = ctypes.c_char_p
         L.lsp_last_hip_error.restype = ctypes.c_int
@@ -376,4 +430,123 @@ def lsp_validate_projector(idx, rows, d, r, flag, stream=None, check: bool = Fal
     rc = lib().lsp_validate_projector(_ptr(idx), rows, d, r, _ptr(flag), _stream(stream))
     if check:
         _check(rc, "lsp_validate_projector")
+    return rc
+
+
+def lsp_dropout(x, y, rows, width, dropout: float, seed: int, offset: int, dtype: int, stream=None, check: bool = True) -> int:
+    """y := drop(x); on a gradient, with the same numbers, its backward pass.  y may be x."""
+    rc = lib().lsp_dropout(_ptr(x), _ptr(y), rows, width, dropout, seed, offset, dtype, _stream(stream))
+    if check:
+        _check(rc, "lsp_dropout")
+    return rc
+
+
+def _strides(t):
+    """Strides of batch, position and head of a [batch][position][head][head_dim] tensor, whose last axis must be contiguous."""
+    b, s, h, d = t.stride()
+    if d != 1 and t.shape[3] != 1:
+        raise ValueError("the last axis of Q, K, V, O and their gradients must be contiguous")
+    return _three(b, s, h)
+
+
+def attention_problem(Q, K, V, O, L, *, q_lens=None, k_lens=None, scale: float, causal: bool = False, dropout: float = 0.0,
+                      seed: int = 0, offset: int = 0) -> lsp_attention_problem:
+    """The descriptor of an attention call from torch tensors: Q, O [batch][q_len][heads][head_dim] and K, V [batch][k_len][kv_heads][head_dim]
+    with any strides whose last is 1, L [batch][heads][q_len] fp32, q_lens and k_lens [batch] int32 or None.  The tensors are kept alive by
+    the caller."""
+    B, Sq, H, D = Q.shape
+    Sk, Hk = K.shape[1], K.shape[2]
+    if K.shape != (B, Sk, Hk, D) or V.shape != K.shape or O.shape != Q.shape or tuple(L.shape) != (B, H, Sq) or not L.is_contiguous():
+        raise ValueError("attention_problem: shapes do not belong together")
+    if not (K.dtype == V.dtype == O.dtype == Q.dtype):
+        raise ValueError("attention_problem: Q, K, V and O are of one type")
+    for lens in (q_lens, k_lens):
+        if lens is not None and (lens.element_size() != 4 or lens.is_floating_point() or lens.numel() != B or not lens.is_contiguous()):
+            raise ValueError("attention_problem: lengths are [batch] int32")
+    return lsp_attention_problem(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), L.data_ptr(), _ptr(q_lens), _ptr(k_lens),
+                                 _strides(Q), _strides(K), _strides(V), _strides(O), B, H, Hk, Sq, Sk, D, int(causal), scale, dropout,
+                                 offset, seed)
+
+
+def attention_gradients(dO, dQ, dK, dV) -> lsp_attention_gradients:
+    """The gradients' descriptor, from tensors shaped as O, Q, K and V."""
+    return lsp_attention_gradients(dO.data_ptr(), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), _strides(dO), _strides(dQ), _strides(dK), _strides(dV))
+
+
+def lsp_attention_forward_workspace_bytes(problem, dtype: int) -> int:
+    return lib().lsp_attention_forward_workspace_bytes(ctypes.byref(problem), dtype)
+
+
+def lsp_attention_backward_workspace_bytes(problem, dtype: int) -> int:
+    return lib().lsp_attention_backward_workspace_bytes(ctypes.byref(problem), dtype)
+
+
+def lsp_attention_forward(problem, dtype: int, workspace=None, workspace_bytes: int = 0, stream=None, check: bool = True) -> int:
+    """problem: from attention_problem()."""
+    rc = lib().lsp_attention_forward(ctypes.byref(problem) if problem is not None else None, dtype, _ptr(workspace), workspace_bytes, _stream(stream))
+    if check:
+        _check(rc, "lsp_attention_forward")
+    return rc
+
+
+def lsp_attention_backward(problem, gradients, dtype: int, workspace, workspace_bytes: int, stream=None, check: bool = True) -> int:
+    """gradients: from attention_gradients()."""
+    rc = lib().lsp_attention_backward(ctypes.byref(problem) if problem is not None else None, ctypes.byref(gradients) if gradients is not None else None,
+                                      dtype, _ptr(workspace), workspace_bytes, _stream(stream))
+    if check:
+        _check(rc, "lsp_attention_backward")
+    return rc
+
+
+def _row_stride(t) -> int:
+    if t is None:
+        return 0
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] != 1):
+        raise ValueError("rows of the residual-norm calls are [rows][width] tensors whose last axis is contiguous")
+    return t.stride(0)
+
+
+def residual_norm_problem(x, f, y, h, stats, *, post: str = "none", post_weight=None, post_bias=None, gate=None, pre: str = "none", pre_weight=None,
+                          pre_bias=None, eps: float = 1e-5, residual_scale: float = 1.0, branch_scale: float = 1.0, dropout: float = 0.0,
+                          seed: int = 0, offset: int = 0) -> lsp_residual_norm_problem:
+    """The descriptor of a residual-norm call from torch tensors: x, f, y, h [rows][width], stats [4][rows] fp32, weights, biases and gate
+    [width] (or None); post and pre are "none", "rms" or "layer".  The tensors are kept alive by the caller."""
+    rows, width = x.shape
+    for t in (f, y, h):
+        if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
+            raise ValueError("residual_norm_problem: x, f, y and h are of one shape and type")
+    for t in (post_weight, post_bias, gate, pre_weight, pre_bias):
+        if t is not None and (t.numel() != width or t.dtype != x.dtype or not t.is_contiguous()):
+            raise ValueError("residual_norm_problem: weights, biases and gate are [width], of the type of x")
+    if stats.numel() != 4 * rows or stats.element_size() != 4 or not stats.is_contiguous():
+        raise ValueError("residual_norm_problem: stats are [4][rows] fp32")
+    return lsp_residual_norm_problem(x.data_ptr(), f.data_ptr(), y.data_ptr(), _ptr(h), stats.data_ptr(), _ptr(post_weight), _ptr(post_bias), _ptr(gate),
+                                     _ptr(pre_weight), _ptr(pre_bias), _row_stride(x), _row_stride(f), _row_stride(y), _row_stride(h), rows, width,
+                                     NORM_KIND[post], NORM_KIND[pre], eps, residual_scale, branch_scale, dropout, offset, seed)
+
+
+def residual_norm_gradients(dy, dh, dx, df, *, post_weight=None, post_bias=None, gate=None, pre_weight=None, pre_bias=None) -> lsp_residual_norm_gradients:
+    """The gradients' descriptor: dy, dh (or None) arrive, dx and df are made, and the fp32 [width] gradients that are asked for."""
+    return lsp_residual_norm_gradients(dy.data_ptr(), _ptr(dh), dx.data_ptr(), df.data_ptr(), _ptr(post_weight), _ptr(post_bias), _ptr(gate),
+                                       _ptr(pre_weight), _ptr(pre_bias), _row_stride(dy), _row_stride(dh), _row_stride(dx), _row_stride(df))
+
+
+def lsp_residual_norm_forward(problem, dtype: int, stream=None, check: bool = True) -> int:
+    """problem: from residual_norm_problem()."""
+    rc = lib().lsp_residual_norm_forward(ctypes.byref(problem) if problem is not None else None, dtype, _stream(stream))
+    if check:
+        _check(rc, "lsp_residual_norm_forward")
+    return rc
+
+
+def lsp_residual_norm_backward_workspace_bytes(problem, dtype: int) -> int:
+    return lib().lsp_residual_norm_backward_workspace_bytes(ctypes.byref(problem), dtype)
+
+
+def lsp_residual_norm_backward(problem, gradients, dtype: int, workspace, workspace_bytes: int, stream=None, check: bool = True) -> int:
+    """gradients: from residual_norm_gradients()."""
+    rc = lib().lsp_residual_norm_backward(ctypes.byref(problem) if problem is not None else None, ctypes.byref(gradients) if gradients is not None else None,
+                                          dtype, _ptr(workspace), workspace_bytes, _stream(stream))
+    if check:
+        _check(rc, "lsp_residual_norm_backward")
     return rc

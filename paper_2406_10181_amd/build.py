@@ -16,7 +16,9 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "liblsp_hip.so")
 CALL_MODULE = os.path.join(PKG, "_call" + sysconfig.get_config_var("EXT_SUFFIX"))
 OBJDIR = os.path.join(PKG, "_build")
-SOURCES = ["compress_mm.hip", "compress_gq_bf16.hip", "compress_gq_f16.hip", "compress_gq_f32.hip", "plan_device.hip",
+SOURCES = ["attention_backward_bf16.hip", "attention_backward_f16.hip", "attention_backward_f32.hip",
+           "attention_forward_bf16.hip", "attention_forward_f16.hip", "attention_forward_f32.hip",
+           "residual_norm.hip", "dropout.hip", "operators.cpp", "compress_mm.hip", "compress_gq_bf16.hip", "compress_gq_f16.hip", "compress_gq_f32.hip", "plan_device.hip",
            "decompress_bf16.hip", "decompress_f16.hip", "decompress_f32.hip", "decompress_loose_bf16.hip", "decompress_loose_f16.hip", "decompress_loose_f32.hip", "decompress.hip",
            "compress.hip", "api.cpp", "plan.cpp", "reproject.hip", "dense.hip", "fitgrad.hip", "noalloc.hip", "probe.hip"]
 

@@ -384,6 +384,7 @@ const char* lsp_strerror(int code) {
         case LSP_ERR_SKEW:      return "projector columns used too unevenly for a plan (use lsp_compress)";
         case LSP_ERR_TOO_LARGE: return "problem needs more scratch than the library's static array holds (lsp_static_scratch_bytes); "
                                        "use the entry that takes a workspace";
+        case LSP_ERR_VALUE:     return "a number is out of its range (dropout in [0, 1), finite scales, eps >= 0)";
         default:                return "unknown lsp_status";
     }
 }

@@ -1,0 +1,254 @@
+// Arguments of the attention kernels, and the pieces they share: fragments of the matrix instructions and tiles in LDS.
+//
+// Everything is built on products of 32 x 32 tiles, C[m][n] += sum_k A[m][k] B[k][n], 16 values of k at a time
+// (v_mfma_f32_32x32x16 in 16 bits, eight v_mfma_f32_32x32x2 in fp32): lane l supplies eight A[l % 32][.] and eight B[.][l % 32],
+// and holds C[8 (i / 4) + 4 (l / 32) + i % 4][l % 32] in accumulator register i.  Which eight values of k a lane has is free as long
+// as A and B agree, and that is what joins one product to the next without moving anything between lanes: the lane's eight
+// registers 8 x .. 8 x + 7 of C are rows 16 x + {4 h + 0..3, 8 + 4 h + 0..3} (h = l / 32) of column l % 32, which is a B operand whose
+// k runs over these 16 rows; the A operand that meets it is read from LDS in the same order of k.  So the probabilities go from
+// the accumulators of one product into the operand of the next after nothing but a rounding.
+#pragma once
+
+#include "philox.h"
+
+namespace lsp {
+
+struct Strided { const void* p; int64_t batch, position, head; };      // strides in elements
+
+struct AttentionArgs {
+    Strided q, k, v, o, d_o, dq, dk, dv;
+    float*         L;                // [batch][heads][q_len]
+    float*         delta;            // [batch][heads][q_len]: dO . O; in the backward pass
+    uint32_t*      most;             // fp16 backward: bits of the largest norm of a row of dO and of V (atomic maxima)
+    float*         partial;          // forward with several splits: O of each, then (largest score, sum) of each row
+    const int32_t* q_lens;
+    const int32_t* k_lens;
+    int32_t batch, heads, kv_heads, group, q_len, k_len, head_dim, causal;
+    int32_t tiles;                   // row tiles of a head (or of a key head, where its query heads share the tiles)
+    int32_t rows;                    // rows of a head: q_len, or group * q_len where `packed`
+    int32_t packed;                  // rows are (query head of the group, query): few queries, all heads of a key head in one tile
+    int32_t splits, split_tiles;     // forward: parts of the keys, tiles of keys in each
+    float   scale, scale_log2;       // scale_log2 = scale * log2(e): probabilities are powers of two
+    Dropout drop;
+};
+
+hipError_t launch_attention_forward(const AttentionArgs& a, lsp_dtype dtype, hipStream_t st);
+hipError_t launch_attention_backward(const AttentionArgs& a, lsp_dtype dtype, hipStream_t st);
+// Splits of the keys in the forward pass and what that needs; fills the tiling fields of `a`.
+void plan_attention_forward(AttentionArgs& a, lsp_dtype dtype);
+size_t attention_partial_bytes(const AttentionArgs& a);
+
+constexpr int kRowsForward = 128;    // query rows of a workgroup: four waves of 32
+constexpr int kKeysBackward = 128;   // keys of a workgroup of the kernel that makes dK and dV
+
+// Keys (forward, dQ) or queries (dK, dV) of a tile in LDS
+template <typename D> constexpr int tile_rows() { return D::size == 2 ? 64 : 32; }
+constexpr int tile_rows_of(lsp_dtype t) { return t == LSP_F32 ? 32 : 64; }
+
+#if defined(__HIPCC__)
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+#define LSP_SHARED_AS __attribute__((address_space(3)))
+
+// Eight values of k of one lane
+template <typename D> struct Frag { u32x4 w; };
+template <> struct Frag<F32> { f32x8 w; };
+
+template <typename D> __device__ __forceinline__ f32x16 mma(const Frag<D>& a, const Frag<D>& b, f32x16 c) {
+    if constexpr (std::is_same<D, BF16>::value) {
+        bf16x8 x, y;
+        __builtin_memcpy(&x, &a.w, 16); __builtin_memcpy(&y, &b.w, 16);
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
+    } else if constexpr (std::is_same<D, F16>::value) {
+        f16x8 x, y;
+        __builtin_memcpy(&x, &a.w, 16); __builtin_memcpy(&y, &b.w, 16);
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, c, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w[j], b.w[j], c, 0, 0, 0);
+        return c;
+    }
+}
+
+__device__ __forceinline__ f32x16 zeros16() {
+    f32x16 z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+    return z;
+}
+
+// Registers 8 x .. 8 x + 7 of an accumulator as a B operand: rounded to the storage type, nearest even
+template <typename D> __device__ __forceinline__ Frag<D> to_frag(const f32x16& c, int x) {
+    Frag<D> f;
+    if constexpr (D::size == 4) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f.w[j] = c[8 * x + j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const f32x2 p = {c[8 * x + 2 * j], c[8 * x + 2 * j + 1]};
+            if constexpr (std::is_same<D, BF16>::value) { const bf16x2 r = __builtin_convertvector(p, bf16x2); uint32_t u; __builtin_memcpy(&u, &r, 4); f.w[j] = u; }
+            else { const f16x2 r = __builtin_convertvector(p, f16x2); uint32_t u; __builtin_memcpy(&u, &r, 4); f.w[j] = u; }
+        }
+    }
+    return f;
+}
+
+// The larger, and the sum, of a value of lane l and one of lane l ^ 32: the two lanes that share a column of C
+__device__ __forceinline__ float halves_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float halves_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A tile in LDS: rows of DP elements (head_dim, filled up with zeros to a multiple of 32) in units of 16 bytes.  A row has a power
+// of two of units, and unit c of row t lies at place c ^ swizzle(t), chosen so that neither way of reading meets a bank twice: the 16
+// lanes that read one unit of 16 consecutive rows (row_frag) hit 16 different groups of four banks, and so do the 32 lanes that read four
+// consecutive units of four consecutive rows (column_frag).
+template <typename D, int DP> struct Tile {
+    static constexpr int kUnitElems = 16 / D::size;
+    static constexpr int kUnits = DP / kUnitElems;                                        // in use
+    static constexpr int kPitch = kUnits <= 4 ? 4 : kUnits <= 8 ? 8 : kUnits <= 16 ? 16 : 32;
+    static constexpr int kRowBytes = kPitch * 16;
+    __device__ static __forceinline__ uint32_t swizzle(uint32_t t) {
+        if constexpr (D::size == 2) {
+            if constexpr (kPitch == 16) return (t & 3u) << 2 | ((t >> 2) & 3u);
+            else if constexpr (kPitch == 8) return ((t >> 1) & 1u) << 2 | ((t >> 2) & 3u);
+            else return (t >> 2) & 3u;
+        } else {
+            // fp32: columns are read one float a lane, rows t and t + 4 at a time
+            if constexpr (kPitch >= 16) return ((t >> 2) & 1u) << 3 | (t & 3u) | ((t >> 3) & 1u) << 2;
+            else return (t >> 1) & 7u;
+        }
+    }
+    __device__ static __forceinline__ uint32_t place(uint32_t row, uint32_t unit) { return row * kRowBytes + (unit ^ swizzle(row)) * 16u; }
+};
+
+__device__ __forceinline__ u32x4 lds_read16(uint32_t at) { return *(const LSP_SHARED_AS u32x4*)(uintptr_t)at; }
+__device__ __forceinline__ f32x4 lds_read16f(uint32_t at) { return *(const LSP_SHARED_AS f32x4*)(uintptr_t)at; }
+__device__ __forceinline__ float lds_read4f(uint32_t at) { return *(const LSP_SHARED_AS float*)(uintptr_t)at; }
+__device__ __forceinline__ void lds_write16(uint32_t at, u32x4 x) { *(LSP_SHARED_AS u32x4*)(uintptr_t)at = x; }
+
+// A operand whose rows are rows row0 + 0..31 of the tile and whose k are its columns 16 ks + 0..15 (lane half h: 8 h + 0..7)
+template <typename D, int DP> __device__ __forceinline__ Frag<D> row_frag(uint32_t tile, int row0, int ks, int lane) {
+    using T = Tile<D, DP>;
+    const uint32_t row = row0 + (lane & 31), h = (uint32_t)lane >> 5;
+    Frag<D> f;
+    if constexpr (D::size == 2) f.w = lds_read16(tile + T::place(row, 2 * ks + h));
+    else {
+        const f32x4 a = lds_read16f(tile + T::place(row, 4 * ks + 2 * h)), b = lds_read16f(tile + T::place(row, 4 * ks + 2 * h + 1));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { f.w[j] = a[j]; f.w[4 + j] = b[j]; }
+    }
+    return f;
+}
+
+// A operand whose rows are columns 32 ct + 0..31 of the tile and whose k are its rows row0 + 0..15, in the order that the accumulators
+// have them.  In 16 bits the transposing read does it: 16 lanes hold four rows of 16 columns, four columns each, and each gets one column of
+// the four rows.
+template <typename D, int DP> __device__ __forceinline__ Frag<D> column_frag(uint32_t tile, int row0, int ct, int lane) {
+    using T = Tile<D, DP>;
+    const uint32_t h = (uint32_t)lane >> 5;
+    Frag<D> f;
+    if constexpr (D::size == 2) {
+        const uint32_t unit = 4 * ct + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint32_t row = row0 + 8 * x + 4 * h + ((lane >> 2) & 3);
+            const s16x4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LSP_SHARED_AS s16x4*)(uintptr_t)(tile + T::place(row, unit) + (lane & 1) * 8u));
+            u32x2 u;
+            __builtin_memcpy(&u, &t, 8);
+            f.w[2 * x] = u[0]; f.w[2 * x + 1] = u[1];
+        }
+    } else {
+        const uint32_t unit = 8 * ct + ((lane & 31) >> 2);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t row = row0 + (j >> 2) * 8 + 4 * h + (j & 3);
+            f.w[j] = lds_read4f(tile + T::place(row, unit) + (lane & 3) * 4u);
+        }
+    }
+    return f;
+}
+
+typedef __amdgpu_buffer_rsrc_t Buffer;
+// A buffer of 2 GiB from p on; offsets from 2^31 on are out of it, and loads there give zeros
+__device__ __forceinline__ Buffer buffer_from(const void* p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x80000000u, 0x00027000);
+}
+template <typename D> __device__ __forceinline__ const uint8_t* at(const Strided& s, int64_t b, int64_t position, int64_t head) {
+    return static_cast<const uint8_t*>(s.p) + (b * s.batch + position * s.position + head * s.head) * D::size;
+}
+
+// ROWS rows of a tile on their way from memory to LDS: a thread holds kCount units.  Rows from `left` on and columns from head_dim on
+// are zeros and not read.
+template <typename D, int DP, int ROWS, int NT> struct Staged {
+    using T = Tile<D, DP>;
+    static constexpr int kTotal = ROWS * T::kUnits;
+    static constexpr int kCount = (kTotal + NT - 1) / NT;
+    u32x4 x[kCount];
+    __device__ __forceinline__ void load(const void* first_row, uint32_t row_bytes, int left, int head_dim, int tid) {
+        const Buffer b = buffer_from(first_row);
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            const int u = tid + i * NT, row = u / T::kUnits, unit = u % T::kUnits;
+            const bool there = row < left && unit * T::kUnitElems < head_dim && (kTotal % NT == 0 || u < kTotal);
+            const uint32_t off = there ? (uint32_t)row * row_bytes + (uint32_t)unit * 16u : 0x80000000u;
+            x[i] = __builtin_amdgcn_raw_buffer_load_b128(b, (int)off, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void store(uint32_t tile, int tid) const {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            const int u = tid + i * NT;
+            if (kTotal % NT == 0 || u < kTotal) lds_write16(tile + T::place(u / T::kUnits, u % T::kUnits), x[i]);
+        }
+    }
+};
+
+// Eight elements of row `row` (a pointer to it, or NULL: zeros) as a B operand: columns 16 ks + 8 h + 0..7
+template <typename D> __device__ __forceinline__ Frag<D> global_frag(const uint8_t* row, int ks, int head_dim, int lane) {
+    const int col = 16 * ks + 8 * (lane >> 5);
+    Frag<D> f;
+    if (row && col < head_dim) {
+        const uint8_t* p = row + col * D::size;
+        if constexpr (D::size == 2) f.w = *reinterpret_cast<const u32x4*>(p);
+        else {
+            const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { f.w[j] = a[j]; f.w[4 + j] = b[j]; }
+        }
+    } else {
+        __builtin_memset(&f, 0, sizeof(f));
+    }
+    return f;
+}
+
+// Four consecutive elements of an output row
+template <typename D> __device__ __forceinline__ void store_four(uint8_t* p, float a, float b, float c, float d) {
+    typename D::elem t[4] = {narrow<D>(a), narrow<D>(b), narrow<D>(c), narrow<D>(d)};
+    if constexpr (D::size == 2) { u32x2 w; __builtin_memcpy(&w, t, 8); *reinterpret_cast<u32x2*>(p) = w; }
+    else { u32x4 w; __builtin_memcpy(&w, t, 16); *reinterpret_cast<u32x4*>(p) = w; }
+}
+
+__device__ __forceinline__ int valid_length(const int32_t* lens, int b, int most) { return lens ? min(max(lens[b], 0), most) : most; }
+
+// Work item of a workgroup.  Workgroups go round the eight XCDs, each with an L2 of its own: a run of consecutive items is given to each XCD, so
+// that the workgroups that read the same keys share an L2.
+__device__ __forceinline__ uint32_t item_of_block(uint32_t block, uint32_t items) {
+    const uint32_t xcd = block & 7u, share = items >> 3, rest = items & 7u;
+    return xcd * share + min(xcd, rest) + (block >> 3);
+}
+#endif
+
+}  // namespace lsp

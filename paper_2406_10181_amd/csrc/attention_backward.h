@@ -1,0 +1,361 @@
+// The backward pass of attention.  The probabilities are made again from Q, K and the forward pass's L, tile by tile; no matrix of queries by
+// keys is ever in memory.  With delta_i = dO_i . O_i:
+//     P = exp(scale Q K^T - L),   dP = keep (dO V^T),   dS = P (dP - delta),
+//     dV = (keep P)^T dO,   dQ = scale dS K,   dK = scale dS^T Q    (the last two summed over the query heads of a key head).
+// Two kernels, each owner of what it writes, so that nothing is added by atomics and the result does not depend on timing: k_attention_dq
+// walks the keys for 128 queries, k_attention_dkv the queries for 128 keys.  Both make the scores, seven products instead of five.
+//
+// k_attention_dq has a query per lane, as the forward pass: S^T = K Q^T and dP^T = V dO^T give dS^T, the operand of dQ^T += K^T dS^T as it is.
+// k_attention_dkv has a key per lane: S = Q K^T and dP = dO V^T (keys and values of the lane in registers) give the operands P and dS of
+// dV^T += dO^T P and dK^T += Q^T dS; L and delta of the 16 queries of a lane come from LDS.
+//
+// fp16: gradients of scores can be far below what fp16 resolves, or above its range.  dP and delta are at most B = max |dO_i| max |V_j| keep, so
+// with the power of two g <= 1 / B the operand 2^14 P g (dP - delta) neither overflows nor loses more than values 2^-38 of B; P itself is
+// scaled by 2^14.  Powers of two change nothing else, and the sums are scaled back at the end.  bf16 and fp32 have the range of fp32.
+#pragma once
+
+#include "attention_forward.h"
+
+#if defined(__HIPCC__)
+namespace lsp {
+
+template <typename D> constexpr float kLiftLog2 = std::is_same<D, F16>::value ? 14.0f : 0.0f;
+template <typename D> constexpr float kLift = std::is_same<D, F16>::value ? 16384.0f : 1.0f;   // factor of the probabilities
+
+// g: a power of two, at most 1 / (the largest |dP|); 1 where that is no number
+template <typename D> __device__ __forceinline__ float score_factor(const AttentionArgs& a) {
+    if constexpr (!std::is_same<D, F16>::value) return 1.0f;
+    const float bound = __uint_as_float(a.most[0]) * __uint_as_float(a.most[1]) * a.drop.scale * 1.01f;
+    if (!(bound > 0.0f) || !(bound < INFINITY)) return 1.0f;
+    return __uint_as_float((uint32_t)min(max(254 - (int)(__float_as_uint(bound) >> 23) - 1, 1), 254) << 23);
+}
+
+// delta of every query that counts; fp16: the largest norms too.  16 lanes have a row, eight elements each.
+template <typename D>
+__global__ __launch_bounds__(256) void k_attention_delta(const AttentionArgs a, int64_t o_rows, int64_t v_rows) {
+    const int lane = threadIdx.x & 63, part = lane & 15, col = 8 * part;
+    int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    const bool values = row >= o_rows;                                                    // (whole workgroups: o_rows is rounded up to 16)
+    if (values) row -= o_rows;
+    const int len = values ? a.k_len : a.q_len, heads = values ? a.kv_heads : a.heads;
+    const bool there = row < (values ? v_rows : (int64_t)a.batch * a.heads * a.q_len);
+    const int64_t line = there ? row / len : 0;
+    const int i = there ? (int)(row - line * len) : 0, b = (int)(line / heads), head = (int)(line - (int64_t)b * heads);
+    const bool counts = there && i < valid_length(values ? a.k_lens : a.q_lens, b, len);
+    float dot = 0.0f, norm = 0.0f;
+    if (counts && col < a.head_dim) {
+        const uint8_t* p = at<D>(values ? a.v : a.d_o, b, i, head) + col * D::size;
+        const uint8_t* q = values ? p : at<D>(a.o, b, i, head) + col * D::size;
+        typename D::elem x[8], y[8];
+        __builtin_memcpy(x, __builtin_assume_aligned(p, 16), sizeof(x));
+        __builtin_memcpy(y, __builtin_assume_aligned(q, 16), sizeof(y));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { const float u = widen<D>(x[e]); dot = fmaf(u, widen<D>(y[e]), dot); norm = fmaf(u, u, norm); }
+    }
+#pragma unroll
+    for (int s = 1; s < 16; s <<= 1) { dot += __shfl_xor(dot, s); norm += __shfl_xor(norm, s); }
+    if (!values && counts && part == 0) a.delta[row] = dot;
+    if constexpr (std::is_same<D, F16>::value) {
+        norm = sqrtf(norm);
+#pragma unroll
+        for (int s = 16; s < 64; s <<= 1) norm = fmaxf(norm, __shfl_xor(norm, s));
+        if (lane == 0) atomicMax(&a.most[values ? 1 : 0], __float_as_uint(norm));         // (a maximum: the order does not matter)
+    }
+}
+
+template <typename D> __global__ void k_attention_clear(uint32_t* most) { if (threadIdx.x < 2) most[threadIdx.x] = 0; }
+
+template <typename D, int DP, bool DROP>
+__global__ __launch_bounds__(256) void k_attention_dq(const AttentionArgs a) {
+    using T = Tile<D, DP>;
+    constexpr int BN = tile_rows<D>(), NT = 256, kSteps = DP / 16, kTiles = BN / 32, kCols = DP / 32;
+    constexpr uint32_t kTileBytes = BN * T::kRowBytes;
+    extern __shared__ __align__(16) uint8_t smem[];
+    const uint32_t lds = (uint32_t)(uintptr_t)(LSP_SHARED_AS uint8_t*)smem;               // K | V, twice
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    const int tiles = (a.q_len + kRowsForward - 1) / kRowsForward;
+    uint32_t item = item_of_block(blockIdx.x, (uint32_t)a.batch * a.heads * tiles);
+    const int row_tile = tiles - 1 - (int)(item % tiles);
+    item /= tiles;
+    const int head = (int)(item % a.heads), b = (int)(item / a.heads), kv_head = head / a.group;
+    const int nq = valid_length(a.q_lens, b, a.q_len), nk = valid_length(a.k_lens, b, a.k_len), ahead = nk - nq;
+
+    const int first = row_tile * kRowsForward + wave * 32, qi = first + (lane & 31);
+    const bool counts = qi < nq;
+    const int limit = counts ? (a.causal ? min(nk, qi + ahead + 1) : nk) : 0;
+    const int last_row = min(row_tile * kRowsForward + kRowsForward, nq) - 1;
+    const int end = row_tile * kRowsForward >= nq ? 0 : a.causal ? min(nk, last_row + ahead + 1) : nk;
+    const int most = first >= nq ? 0 : a.causal ? min(nk, min(first + 31, nq - 1) + ahead + 1) : nk;
+    const int least = first + 31 >= nq ? 0 : a.causal ? min(nk, first + ahead + 1) : nk;
+
+    Frag<D> qf[kSteps], gf[kSteps];
+    {
+        const uint8_t* p = counts ? at<D>(a.q, b, qi, head) : nullptr;
+        const uint8_t* g = counts ? at<D>(a.d_o, b, qi, head) : nullptr;
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) { qf[ks] = global_frag<D>(p, ks, a.head_dim, lane); gf[ks] = global_frag<D>(g, ks, a.head_dim, lane); }
+    }
+    const float factor = score_factor<D>(a), keep = (DROP ? a.drop.scale : 1.0f) * factor;
+    float shift = 0.0f, delta = 0.0f;
+    if (counts) {
+        const int64_t line = ((int64_t)b * a.heads + head) * a.q_len + qi;
+        const float L = a.L[line];
+        shift = L == -INFINITY ? 0.0f : kLiftLog2<D> - L * 1.44269504f;
+        delta = a.delta[line] * factor;
+    }
+    const float c2 = a.scale_log2;
+    f32x16 dq[kCols];
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) dq[c] = zeros16();
+
+    const uint8_t* kp = at<D>(a.k, b, 0, kv_head);
+    const uint8_t* vp = at<D>(a.v, b, 0, kv_head);
+    const int64_t k_bytes = a.k.position * D::size, v_bytes = a.v.position * D::size;
+    Staged<D, DP, BN, NT> ks_, vs_;
+    if (end > 0) {
+        ks_.load(kp, (uint32_t)k_bytes, nk, a.head_dim, tid);
+        vs_.load(vp, (uint32_t)v_bytes, nk, a.head_dim, tid);
+        ks_.store(lds, tid);
+        vs_.store(lds + kTileBytes, tid);
+        __syncthreads();
+        uint32_t buf = lds;
+        for (int k0 = 0; k0 < end; k0 += BN) {
+            const bool more = k0 + BN < end;
+            if (more) {
+                ks_.load(kp + (k0 + BN) * k_bytes, (uint32_t)k_bytes, nk - k0 - BN, a.head_dim, tid);
+                vs_.load(vp + (k0 + BN) * v_bytes, (uint32_t)v_bytes, nk - k0 - BN, a.head_dim, tid);
+            }
+            if (k0 < most) {
+                const bool edge = k0 + BN > least;
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    f32x16 s = zeros16(), dp = zeros16();
+#pragma unroll
+                    for (int ks = 0; ks < kSteps; ++ks) s = mma<D>(row_frag<D, DP>(buf, 32 * t, ks, lane), qf[ks], s);
+#pragma unroll
+                    for (int ks = 0; ks < kSteps; ++ks) dp = mma<D>(row_frag<D, DP>(buf + kTileBytes, 32 * t, ks, lane), gf[ks], dp);
+                    if (edge)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] = k0 + 32 * t + 8 * (i >> 2) + 4 * h + (i & 3) < limit ? s[i] : -INFINITY;
+                    if constexpr (DROP) drop_keys(dp, k0 + 32 * t, qi, b * a.heads + head, a.drop, h);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float p = __builtin_amdgcn_exp2f(fmaf(s[i], c2, shift));
+                        s[i] = p * fmaf(dp[i], keep, -delta);
+                    }
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const Frag<D> ds = to_frag<D>(s, x);
+#pragma unroll
+                        for (int c = 0; c < kCols; ++c) dq[c] = mma<D>(column_frag<D, DP>(buf, 32 * t + 16 * x, c, lane), ds, dq[c]);
+                    }
+                }
+            }
+            buf = buf == lds ? lds + 2 * kTileBytes : lds;
+            if (more) {
+                ks_.store(buf, tid);
+                vs_.store(buf + kTileBytes, tid);
+            }
+            __syncthreads();
+        }
+    }
+    if (qi >= a.q_len) return;
+    const float back = a.scale / (factor * kLift<D>);
+    uint8_t* out = const_cast<uint8_t*>(at<D>(a.dq, b, qi, head));
+#pragma unroll
+    for (int c = 0; c < kCols; ++c)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int col = 32 * c + 8 * g + 4 * h;
+            if (col < a.head_dim) store_four<D>(out + col * D::size, dq[c][4 * g] * back, dq[c][4 * g + 1] * back, dq[c][4 * g + 2] * back, dq[c][4 * g + 3] * back);
+        }
+}
+
+template <typename D, int DP, bool DROP>
+__global__ __launch_bounds__(256) void k_attention_dkv(const AttentionArgs a) {
+    using T = Tile<D, DP>;
+    constexpr int BQ = tile_rows<D>(), NT = 256, kSteps = DP / 16, kTiles = BQ / 32, kCols = DP / 32;
+    constexpr uint32_t kTileBytes = BQ * T::kRowBytes, kBufBytes = 2 * kTileBytes + BQ * 8;
+    extern __shared__ __align__(16) uint8_t smem[];
+    const uint32_t lds = (uint32_t)(uintptr_t)(LSP_SHARED_AS uint8_t*)smem;               // Q | dO | L | delta, twice; bits of kept ones of each wave
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    const int tiles = (a.k_len + kKeysBackward - 1) / kKeysBackward;
+    uint32_t item = item_of_block(blockIdx.x, (uint32_t)a.batch * a.kv_heads * tiles);
+    const int key_tile = (int)(item % tiles);                                             // (causal: the first keys have the most queries)
+    item /= tiles;
+    const int kv_head = (int)(item % a.kv_heads), b = (int)(item / a.kv_heads);
+    const int nq = valid_length(a.q_lens, b, a.q_len), nk = valid_length(a.k_lens, b, a.k_len), ahead = nk - nq;
+
+    const int first = key_tile * kKeysBackward + wave * 32, key = first + (lane & 31);
+    const bool counts = key < nk;
+    // queries from key - ahead on see the key; the workgroup's tiles begin at a multiple of BQ
+    const int begin = a.causal ? max(0, key_tile * kKeysBackward - ahead) / BQ * BQ : 0;
+    const int end = key_tile * kKeysBackward < nk ? nq : 0;
+    const int from = a.causal ? max(0, first - ahead) : 0;                                // the wave's first query
+    const int all_from = a.causal ? first + 31 - ahead : 0;                               // from here on every key of the wave is seen
+    const int my_from = a.causal ? key - ahead : 0;
+
+    Frag<D> kf[kSteps], vf[kSteps];
+    {
+        const uint8_t* p = counts ? at<D>(a.k, b, key, kv_head) : nullptr;
+        const uint8_t* v = counts ? at<D>(a.v, b, key, kv_head) : nullptr;
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) { kf[ks] = global_frag<D>(p, ks, a.head_dim, lane); vf[ks] = global_frag<D>(v, ks, a.head_dim, lane); }
+    }
+    const float factor = score_factor<D>(a), keep = (DROP ? a.drop.scale : 1.0f) * factor, c2 = a.scale_log2;
+    f32x16 dk[kCols], dv[kCols];
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) { dk[c] = zeros16(); dv[c] = zeros16(); }
+
+    const int64_t q_bytes = a.q.position * D::size, g_bytes = a.d_o.position * D::size;
+    Staged<D, DP, BQ, NT> qs, gs;
+    float stat[2];                                                                        // threads below BQ: -L log2(e) and delta of a row
+    const auto load = [&](int q_head, int q0) {
+        qs.load(at<D>(a.q, b, q0, q_head), (uint32_t)q_bytes, nq - q0, a.head_dim, tid);
+        gs.load(at<D>(a.d_o, b, q0, q_head), (uint32_t)g_bytes, nq - q0, a.head_dim, tid);
+        if (tid < BQ) {
+            const int qi = q0 + tid;
+            const int64_t line = ((int64_t)b * a.heads + q_head) * a.q_len + qi;
+            const float L = qi < nq ? a.L[line] : -INFINITY;
+            stat[0] = L == -INFINITY ? -INFINITY : kLiftLog2<D> - L * 1.44269504f;        // a row that sees nothing has probabilities 2^-inf
+            stat[1] = L == -INFINITY ? 0.0f : a.delta[line] * factor;
+        }
+    };
+    const auto store = [&](uint32_t buf) {
+        qs.store(buf, tid);
+        gs.store(buf + kTileBytes, tid);
+        if (tid < BQ) {
+            *(LSP_SHARED_AS float*)(uintptr_t)(buf + 2 * kTileBytes + tid * 4) = stat[0];
+            *(LSP_SHARED_AS float*)(uintptr_t)(buf + 2 * kTileBytes + BQ * 4 + tid * 4) = stat[1];
+        }
+    };
+    if (begin < end) {
+        int q_head = kv_head * a.group, q0 = begin;
+        const int past = (kv_head + 1) * a.group;
+        load(q_head, q0);
+        store(lds);
+        __syncthreads();
+        uint32_t buf = lds;
+        while (q_head < past) {
+            int next_head = q_head, next_q0 = q0 + BQ;
+            if (next_q0 >= end) { next_q0 = begin; ++next_head; }
+            const bool more = next_head < past;
+            if (more) load(next_head, next_q0);
+            if (q0 + BQ > from && first < nk) {
+                const bool edge = q0 < all_from;
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    f32x16 s = zeros16(), dp = zeros16();
+#pragma unroll
+                    for (int ks = 0; ks < kSteps; ++ks) s = mma<D>(row_frag<D, DP>(buf, 32 * t, ks, lane), kf[ks], s);
+#pragma unroll
+                    for (int ks = 0; ks < kSteps; ++ks) dp = mma<D>(row_frag<D, DP>(buf + kTileBytes, 32 * t, ks, lane), vf[ks], dp);
+                    if (edge)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] = q0 + 32 * t + 8 * (i >> 2) + 4 * h + (i & 3) >= my_from ? s[i] : -INFINITY;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const f32x4 L = lds_read16f(buf + 2 * kTileBytes + (32 * t + 8 * g + 4 * h) * 4);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) s[4 * g + j] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + j], c2, L[j]));
+                    }
+                    f32x16 pd = s;
+                    if constexpr (DROP) {
+                        // eight lanes share a block of eight keys: of the 16 queries that they all have, each lane makes two; the bits go round by LDS
+                        const uint32_t bits = lds + 2 * kBufBytes + wave * 128 + (lane >> 3) * 16;
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            const int x = (lane & 7) + 8 * half;
+                            const u32x4 w = philox((uint32_t)key >> 3, q0 + 32 * t + 8 * (x >> 2) + 4 * h + (x & 3), b * a.heads + q_head, a.drop.offset, a.drop.key0, a.drop.key1);
+                            uint32_t kept = 0;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) kept |= (philox_word(w, e) < a.drop.limit ? 0u : 1u) << e;
+                            *(LSP_SHARED_AS uint8_t*)(uintptr_t)(bits + x) = (uint8_t)kept;
+                        }
+                        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                        __builtin_amdgcn_wave_barrier();
+                        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                        const u32x4 all = lds_read16(bits);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const bool kept = (all[i >> 2] >> (8 * (i & 3) + (lane & 7))) & 1u;
+                            pd[i] = kept ? s[i] : 0.0f;
+                            dp[i] = kept ? dp[i] : 0.0f;
+                        }
+                        __builtin_amdgcn_wave_barrier();
+                    }
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const f32x4 delta = lds_read16f(buf + 2 * kTileBytes + BQ * 4 + (32 * t + 8 * g + 4 * h) * 4);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) s[4 * g + j] *= fmaf(dp[4 * g + j], keep, -delta[j]);
+                    }
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const Frag<D> p = to_frag<D>(pd, x), ds = to_frag<D>(s, x);
+#pragma unroll
+                        for (int c = 0; c < kCols; ++c) {
+                            dv[c] = mma<D>(column_frag<D, DP>(buf + kTileBytes, 32 * t + 16 * x, c, lane), p, dv[c]);
+                            dk[c] = mma<D>(column_frag<D, DP>(buf, 32 * t + 16 * x, c, lane), ds, dk[c]);
+                        }
+                    }
+                }
+            }
+            buf = buf == lds ? lds + kBufBytes : lds;
+            if (more) store(buf);
+            __syncthreads();
+            q_head = next_head; q0 = next_q0;
+        }
+    }
+    if (key >= a.k_len) return;
+    const float back_v = counts ? (DROP ? a.drop.scale : 1.0f) / kLift<D> : 0.0f, back_k = counts ? a.scale / (factor * kLift<D>) : 0.0f;
+    uint8_t* out_k = const_cast<uint8_t*>(at<D>(a.dk, b, key, kv_head));
+    uint8_t* out_v = const_cast<uint8_t*>(at<D>(a.dv, b, key, kv_head));
+#pragma unroll
+    for (int c = 0; c < kCols; ++c)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int col = 32 * c + 8 * g + 4 * h;
+            if (col < a.head_dim) {
+                store_four<D>(out_k + col * D::size, counts ? dk[c][4 * g] * back_k : 0.0f, counts ? dk[c][4 * g + 1] * back_k : 0.0f,
+                              counts ? dk[c][4 * g + 2] * back_k : 0.0f, counts ? dk[c][4 * g + 3] * back_k : 0.0f);
+                store_four<D>(out_v + col * D::size, counts ? dv[c][4 * g] * back_v : 0.0f, counts ? dv[c][4 * g + 1] * back_v : 0.0f,
+                              counts ? dv[c][4 * g + 2] * back_v : 0.0f, counts ? dv[c][4 * g + 3] * back_v : 0.0f);
+            }
+        }
+}
+
+template <typename D, int DP, bool DROP> static hipError_t run_attention_backward(const AttentionArgs& a, hipStream_t st) {
+    constexpr size_t tile = (size_t)tile_rows<D>() * Tile<D, DP>::kRowBytes;
+    constexpr auto dkv = k_attention_dkv<D, DP, DROP>;
+    constexpr auto dq = k_attention_dq<D, DP, DROP>;
+    constexpr size_t lds_dkv = 4 * tile + 2 * 8 * tile_rows<D>() + 512, lds_dq = 4 * tile;
+    hipError_t e = allow_dynamic_lds<dkv, lds_dkv>();
+    if (e == hipSuccess) e = allow_dynamic_lds<dq, lds_dq>();
+    if (e != hipSuccess) return e;
+    const int64_t o_rows = ((int64_t)a.batch * a.heads * a.q_len + 15) / 16 * 16;
+    const int64_t v_rows = std::is_same<D, F16>::value ? (int64_t)a.batch * a.kv_heads * a.k_len : 0;
+    if (v_rows) {
+        hipLaunchKernelGGL(k_attention_clear<D>, dim3(1), dim3(64), 0, st, a.most);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(k_attention_delta<D>, dim3((unsigned)((o_rows + v_rows + 15) / 16)), dim3(256), 0, st, a, o_rows, v_rows);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const int64_t key_items = (int64_t)a.batch * a.kv_heads * ((a.k_len + kKeysBackward - 1) / kKeysBackward);
+    hipLaunchKernelGGL(dkv, dim3((unsigned)key_items), dim3(256), lds_dkv, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const int64_t query_items = (int64_t)a.batch * a.heads * ((a.q_len + kRowsForward - 1) / kRowsForward);
+    hipLaunchKernelGGL(dq, dim3((unsigned)query_items), dim3(256), lds_dq, st, a);
+    return hipGetLastError();
+}
+
+template <typename D> hipError_t attention_backward_of(const AttentionArgs& a, hipStream_t st) {
+    const bool drop = a.drop.limit != 0;
+    if (a.head_dim <= 32) return drop ? run_attention_backward<D, 32, true>(a, st) : run_attention_backward<D, 32, false>(a, st);
+    if (a.head_dim <= 64) return drop ? run_attention_backward<D, 64, true>(a, st) : run_attention_backward<D, 64, false>(a, st);
+    if (a.head_dim <= 96) return drop ? run_attention_backward<D, 96, true>(a, st) : run_attention_backward<D, 96, false>(a, st);
+    return drop ? run_attention_backward<D, 128, true>(a, st) : run_attention_backward<D, 128, false>(a, st);
+}
+
+}  // namespace lsp
+#endif

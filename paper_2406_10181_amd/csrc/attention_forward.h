@@ -1,0 +1,244 @@
+// The forward pass of attention: one pass over the keys with a running maximum and sum for each query.
+//
+// A workgroup has 128 query rows of a head, a wave 32 of them; tiles of keys and values go by in LDS, the next one on its way in registers
+// while the matrix cores work on the current.  The scores are made transposed, S^T = K Q^T: a lane then has all its scores (16 of every 32
+// keys; lane l ^ 32 has the others) of ONE query, so maxima and sums stay in the lane, and the accumulators are the operand of
+// O^T += V^T P^T as they are.
+//
+// The running maximum is moved only when a new one is larger by more than 8 in powers of two; until then probabilities are at most 2^8, and
+// neither their sum in fp32 nor their rounding minds, and the accumulators are left alone.
+#pragma once
+
+#include "attention.h"
+
+#if defined(__HIPCC__)
+namespace lsp {
+
+// Drops probabilities: registers i of `s` are keys key0 + 8 (i / 4) + 4 h + i % 4 of query q.  A block of eight keys belongs to two lanes (h = 0, 1), four words
+// each: of two blocks each lane makes one, and they swap the halves.
+__device__ __forceinline__ void drop_keys(f32x16& s, uint32_t key0, uint32_t q, uint32_t head, const Dropout& drop, int h) {
+#pragma unroll
+    for (int pair = 0; pair < 2; ++pair) {
+        const u32x4 w = philox((key0 >> 3) + 2 * pair + h, q, head, drop.offset, drop.key0, drop.key1);
+        const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+        const auto b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint32_t lo = a[x], hi = b[x];
+            const int i = 8 * pair + 4 * x;
+            s[i + 0] = (lo & 0xFFFFu) < drop.limit ? 0.0f : s[i + 0];
+            s[i + 1] = (lo >> 16) < drop.limit ? 0.0f : s[i + 1];
+            s[i + 2] = (hi & 0xFFFFu) < drop.limit ? 0.0f : s[i + 2];
+            s[i + 3] = (hi >> 16) < drop.limit ? 0.0f : s[i + 3];
+        }
+    }
+}
+
+template <typename D, int DP, bool DROP>
+__global__ __launch_bounds__(256) void k_attention_forward(const AttentionArgs a) {
+    using T = Tile<D, DP>;
+    constexpr int BN = tile_rows<D>(), NT = 256, kSteps = DP / 16, kTiles = BN / 32, kCols = DP / 32;
+    constexpr uint32_t kTileBytes = BN * T::kRowBytes;
+    extern __shared__ __align__(16) uint8_t smem[];
+    const uint32_t lds = (uint32_t)(uintptr_t)(LSP_SHARED_AS uint8_t*)smem;               // K | V, twice
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    // which rows, of which head, and which part of the keys
+    const uint32_t heads = a.packed ? a.kv_heads : a.heads, items = a.batch * heads * a.tiles * a.splits;
+    uint32_t item = item_of_block(blockIdx.x, items);
+    const int tile_r = (int)(item % a.tiles);
+    item /= a.tiles;
+    const int row_tile = a.tiles - 1 - tile_r;                                            // (causal: the longest first)
+    const int split = (int)(item % a.splits);
+    item /= a.splits;
+    const int head = (int)(item % heads), b = (int)(item / heads);
+    const int kv_head = a.packed ? head : head / a.group;
+    const int nq = valid_length(a.q_lens, b, a.q_len), nk = valid_length(a.k_lens, b, a.k_len);
+    const int ahead = nk - nq;                                                            // query i sees keys up to i + ahead
+
+    // this lane's row
+    const int row = row_tile * kRowsForward + wave * 32 + (lane & 31);
+    const int q_head = a.packed ? kv_head * a.group + row / a.q_len : head;
+    const int qi = a.packed ? row % a.q_len : row;
+    const bool counts = row < a.rows && qi < nq;
+    const int limit = counts ? (a.causal ? min(nk, qi + ahead + 1) : nk) : 0;             // it sees keys below
+    // the keys of the workgroup: below the largest limit, in this split
+    int most, least;                                                                      // of the wave
+    if (a.packed || !a.causal) { most = nk; least = a.causal ? min(nk, ahead + 1) : nk; }
+    else {
+        const int first = row_tile * kRowsForward + wave * 32;
+        most = min(nk, min(first + 31, nq - 1) + ahead + 1);
+        least = min(nk, first + ahead + 1);
+    }
+    const int last_row = min(row_tile * kRowsForward + kRowsForward, nq) - 1;
+    const int end_all = a.packed || !a.causal ? nk : min(nk, last_row + ahead + 1);
+    const int begin = split * a.split_tiles * BN;
+    const int end = min(end_all, begin + a.split_tiles * BN);
+    if (!a.packed && row_tile * kRowsForward >= nq) most = 0;
+
+    Frag<D> qf[kSteps];
+    {
+        const uint8_t* p = counts ? at<D>(a.q, b, qi, q_head) : nullptr;
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) qf[ks] = global_frag<D>(p, ks, a.head_dim, lane);
+    }
+    f32x16 o[kCols];
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) o[c] = zeros16();
+    float m = -INFINITY, l = 0.0f;                                                        // m: in the units of the scores; l: this lane's part
+    const float c2 = a.scale_log2, slack = 8.0f / c2;
+
+    const uint8_t* kp = at<D>(a.k, b, 0, kv_head);
+    const uint8_t* vp = at<D>(a.v, b, 0, kv_head);
+    const int64_t k_bytes = a.k.position * D::size, v_bytes = a.v.position * D::size;
+    Staged<D, DP, BN, NT> ks_, vs_;
+    const bool any = begin < end && (a.packed || row_tile * kRowsForward < nq);
+    if (any) {
+        ks_.load(kp + begin * k_bytes, (uint32_t)k_bytes, nk - begin, a.head_dim, tid);
+        vs_.load(vp + begin * v_bytes, (uint32_t)v_bytes, nk - begin, a.head_dim, tid);
+        ks_.store(lds, tid);
+        vs_.store(lds + kTileBytes, tid);
+        __syncthreads();
+        uint32_t buf = lds;
+        for (int k0 = begin; k0 < end; k0 += BN) {
+            const bool more = k0 + BN < end;
+            if (more) {
+                ks_.load(kp + (k0 + BN) * k_bytes, (uint32_t)k_bytes, nk - k0 - BN, a.head_dim, tid);
+                vs_.load(vp + (k0 + BN) * v_bytes, (uint32_t)v_bytes, nk - k0 - BN, a.head_dim, tid);
+            }
+            if (k0 < most) {
+                f32x16 s[kTiles];
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    s[t] = zeros16();
+#pragma unroll
+                    for (int ks = 0; ks < kSteps; ++ks) s[t] = mma<D>(row_frag<D, DP>(buf, 32 * t, ks, lane), qf[ks], s[t]);
+                }
+                if (k0 + BN > least || k0 + BN > nk || !__all(counts)) {
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[t][i] = k0 + 32 * t + 8 * (i >> 2) + 4 * h + (i & 3) < limit ? s[t][i] : -INFINITY;
+                }
+                float top = s[0][0];
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
+                top = halves_max(top);
+                if (__any(top > m + slack)) {
+                    const float m_new = fmaxf(m, top);
+                    const float keep = m_new == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - m_new) * c2);
+                    m = m_new;
+                    l *= keep;
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[c][i] *= keep;
+                }
+                const float shift = m == -INFINITY ? 0.0f : -m * c2;
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], c2, shift));
+                        l += s[t][i];
+                    }
+                    if constexpr (DROP) drop_keys(s[t], k0 + 32 * t, qi, b * a.heads + q_head, a.drop, h);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const Frag<D> p = to_frag<D>(s[t], x);
+#pragma unroll
+                        for (int c = 0; c < kCols; ++c) o[c] = mma<D>(column_frag<D, DP>(buf + kTileBytes, 32 * t + 16 * x, c, lane), p, o[c]);
+                    }
+                }
+            }
+            buf = buf == lds ? lds + 2 * kTileBytes : lds;
+            if (more) {
+                ks_.store(buf, tid);
+                vs_.store(buf + kTileBytes, tid);
+            }
+            __syncthreads();
+        }
+    }
+    l = halves_sum(l);
+    if (row >= a.rows) return;
+    if (a.splits > 1) {
+        // this part's sums as they are; k_attention_join puts the parts together
+        const int64_t lines = (int64_t)a.batch * a.heads * a.q_len;
+        const int64_t line = ((int64_t)b * a.heads + q_head) * a.q_len + qi;
+        float* out = a.partial + (split * lines + line) * a.head_dim;
+#pragma unroll
+        for (int c = 0; c < kCols; ++c)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int col = 32 * c + 8 * g + 4 * h;
+                if (col < a.head_dim) *reinterpret_cast<f32x4*>(out + col) = f32x4{o[c][4 * g], o[c][4 * g + 1], o[c][4 * g + 2], o[c][4 * g + 3]};
+            }
+        if (h == 0) *reinterpret_cast<f32x2*>(a.partial + a.splits * lines * a.head_dim + (split * lines + line) * 2) = f32x2{m, l};
+        return;
+    }
+    const float inv = l == 0.0f ? 0.0f : (DROP ? a.drop.scale : 1.0f) / l;
+    uint8_t* out = const_cast<uint8_t*>(at<D>(a.o, b, qi, q_head));
+#pragma unroll
+    for (int c = 0; c < kCols; ++c)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int col = 32 * c + 8 * g + 4 * h;
+            if (col < a.head_dim) store_four<D>(out + col * D::size, o[c][4 * g] * inv, o[c][4 * g + 1] * inv, o[c][4 * g + 2] * inv, o[c][4 * g + 3] * inv);
+        }
+    if (h == 0) a.L[((int64_t)b * a.heads + q_head) * a.q_len + qi] = l == 0.0f ? -INFINITY : m * a.scale + __logf(l);
+}
+
+// Joins the parts of a row: O = sum_s w_s O_s / sum_s w_s l_s with w_s = 2^(m_s - m).  A wave has a row, a lane two columns.
+template <typename D>
+__global__ __launch_bounds__(256) void k_attention_join(const AttentionArgs a) {
+    const int64_t lines = (int64_t)a.batch * a.heads * a.q_len;
+    const int64_t line = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (line >= lines) return;
+    const int lane = threadIdx.x & 63, col = 2 * lane;
+    const f32x2* ml = reinterpret_cast<const f32x2*>(a.partial + a.splits * lines * a.head_dim);
+    float m = -INFINITY;
+    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[s * lines + line][0]);
+    float l = 0.0f, x = 0.0f, y = 0.0f;
+    for (int s = 0; s < a.splits; ++s) {
+        const f32x2 part = ml[s * lines + line];
+        const float w = part[0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((part[0] - m) * a.scale_log2);
+        l += w * part[1];
+        if (col < a.head_dim) {
+            const f32x2 o = *reinterpret_cast<const f32x2*>(a.partial + (s * lines + line) * a.head_dim + col);
+            x += w * o[0]; y += w * o[1];
+        }
+    }
+    const float inv = l == 0.0f ? 0.0f : a.drop.scale / l;
+    const int64_t head_line = line / a.q_len;
+    const int qi = (int)(line - head_line * a.q_len), b = (int)(head_line / a.heads), head = (int)(head_line - (int64_t)b * a.heads);
+    if (col < a.head_dim) {
+        typename D::elem* out = reinterpret_cast<typename D::elem*>(const_cast<uint8_t*>(at<D>(a.o, b, qi, head))) + col;
+        out[0] = narrow<D>(x * inv); out[1] = narrow<D>(y * inv);
+    }
+    if (lane == 0) a.L[line] = l == 0.0f ? -INFINITY : m * a.scale + __logf(l);
+}
+
+template <typename D, int DP, bool DROP> static hipError_t run_attention_forward(const AttentionArgs& a, hipStream_t st) {
+    constexpr auto kern = k_attention_forward<D, DP, DROP>;
+    constexpr size_t lds = 4 * (size_t)tile_rows<D>() * Tile<D, DP>::kRowBytes;
+    hipError_t e = allow_dynamic_lds<kern, lds>();
+    if (e != hipSuccess) return e;
+    const int64_t items = (int64_t)a.batch * (a.packed ? a.kv_heads : a.heads) * a.tiles * a.splits;
+    hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(256), lds, st, a);
+    if ((e = hipGetLastError()) != hipSuccess || a.splits == 1) return e;
+    const int64_t lines = (int64_t)a.batch * a.heads * a.q_len;
+    hipLaunchKernelGGL(k_attention_join<D>, dim3((unsigned)((lines + 3) / 4)), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+template <typename D> hipError_t attention_forward_of(const AttentionArgs& a, hipStream_t st) {
+    const bool drop = a.drop.limit != 0;
+    if (a.head_dim <= 32) return drop ? run_attention_forward<D, 32, true>(a, st) : run_attention_forward<D, 32, false>(a, st);
+    if (a.head_dim <= 64) return drop ? run_attention_forward<D, 64, true>(a, st) : run_attention_forward<D, 64, false>(a, st);
+    if (a.head_dim <= 96) return drop ? run_attention_forward<D, 96, true>(a, st) : run_attention_forward<D, 96, false>(a, st);
+    return drop ? run_attention_forward<D, 128, true>(a, st) : run_attention_forward<D, 128, false>(a, st);
+}
+
+}  // namespace lsp
+#endif

@@ -1,0 +1,6 @@
+// The attention kernels of one storage type.
+#include "attention_forward.h"
+
+namespace lsp {
+template hipError_t attention_forward_of<F16>(const AttentionArgs& a, hipStream_t st);
+}

@@ -1,0 +1,237 @@
+// extern "C" entry points of the operators of a training step: attention, residual norm, dropout.  Argument checks, workspace carving, launches.
+#include <algorithm>
+#include <cmath>
+
+#include "attention.h"
+#include "residual_norm.h"
+
+namespace lsp {
+
+hipError_t launch_dropout(const void* x, void* y, int64_t rows, int64_t width, const Dropout& drop, lsp_dtype dtype, hipStream_t st);
+
+template <typename D> hipError_t attention_forward_of(const AttentionArgs& a, hipStream_t st);
+template <typename D> hipError_t attention_backward_of(const AttentionArgs& a, hipStream_t st);
+
+hipError_t launch_attention_forward(const AttentionArgs& a, lsp_dtype dtype, hipStream_t st) {
+    return dtype == LSP_F32 ? attention_forward_of<F32>(a, st) : dtype == LSP_F16 ? attention_forward_of<F16>(a, st) : attention_forward_of<BF16>(a, st);
+}
+hipError_t launch_attention_backward(const AttentionArgs& a, lsp_dtype dtype, hipStream_t st) {
+    return dtype == LSP_F32 ? attention_backward_of<F32>(a, st) : dtype == LSP_F16 ? attention_backward_of<F16>(a, st) : attention_backward_of<BF16>(a, st);
+}
+
+size_t attention_partial_bytes(const AttentionArgs& a) {
+    if (a.splits <= 1) return 0;
+    return align_up((size_t)a.splits * a.batch * a.heads * a.q_len * ((size_t)a.head_dim + 2) * sizeof(float), 256);
+}
+
+void plan_attention_forward(AttentionArgs& a, lsp_dtype dtype) {
+    // Few queries: the query heads that share a key head go into one tile of rows, so that keys and values are read once for all of them.
+    a.packed = a.group > 1 && (int64_t)a.group * a.q_len <= kRowsForward;
+    a.rows = a.packed ? a.group * a.q_len : a.q_len;
+    a.tiles = (a.rows + kRowsForward - 1) / kRowsForward;
+    // Few tiles of rows: the keys are split, as far as that gives each CU two workgroups and each of these four tiles of keys.
+    const int64_t row_tiles = (int64_t)a.batch * (a.packed ? a.kv_heads : a.heads) * a.tiles;
+    const int key_tiles = (a.k_len + tile_rows_of(dtype) - 1) / tile_rows_of(dtype);
+    int splits = (int)std::min<int64_t>(std::max<int64_t>(512 / row_tiles, 1), std::max(key_tiles / 4, 1));
+    a.split_tiles = (key_tiles + splits - 1) / splits;
+    a.splits = (key_tiles + a.split_tiles - 1) / a.split_tiles;
+}
+
+}  // namespace lsp
+
+namespace {
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool known(lsp_dtype t) { return t == LSP_F32 || t == LSP_F16 || t == LSP_BF16; }
+int elem_size(lsp_dtype t) { return t == LSP_F32 ? 4 : 2; }
+bool rate(float p) { return p >= 0.0f && p < 1.0f; }                       // (false for a NaN)
+int done(hipError_t e) { return e == hipSuccess ? LSP_OK : lsp::note_hip_error(e); }
+
+// One operand's strides: multiples of 16 bytes, positions less than 8 MiB apart (a tile is addressed with 32 bits), batches and heads anywhere
+// below 2^40 elements; what is written has a place of its own for every row.
+int check_strides(const int64_t (&s)[3], int64_t batch, int64_t positions, int64_t heads, int32_t dim, lsp_dtype t, bool written) {
+    const int64_t per = 16 / elem_size(t);
+    const int64_t count[3] = {batch, positions, heads};
+    for (int k = 0; k < 3; ++k) {
+        if (count[k] == 1) continue;                                      // (not used)
+        if (s[k] < 0 || s[k] > ((int64_t)1 << 40)) return LSP_ERR_SHAPE;
+        if (written && s[k] < dim) return LSP_ERR_SHAPE;
+        if (s[k] % per) return LSP_ERR_ALIGN;
+    }
+    if (positions > 1 && s[1] * elem_size(t) >= (8 << 20)) return LSP_ERR_SHAPE;
+    return LSP_OK;
+}
+
+lsp::Strided strided(const void* p, const int64_t (&s)[3], int64_t batch, int64_t positions, int64_t heads) {
+    return {p, batch > 1 ? s[0] : 0, positions > 1 ? s[1] : 0, heads > 1 ? s[2] : 0};
+}
+
+int check_attention_shape(const lsp_attention_problem* p, lsp_dtype t) {
+    if (!p) return LSP_ERR_NULL;
+    if (p->batch <= 0 || p->heads <= 0 || p->kv_heads <= 0 || p->q_len <= 0 || p->k_len <= 0 || p->head_dim <= 0) return LSP_ERR_SHAPE;
+    if (p->heads % p->kv_heads || p->head_dim % 8 || p->head_dim > LSP_MAX_HEAD_DIM) return LSP_ERR_SHAPE;
+    if (p->q_len > (1 << 30) || p->k_len > (1 << 30) || (p->causal != 0 && p->causal != 1)) return LSP_ERR_SHAPE;
+    // a launch has fewer than 2^32 threads: 16 for every row of dO and of V, where delta is made
+    if ((int64_t)p->batch * p->heads > (1 << 24) || (int64_t)p->batch * p->heads * std::max(p->q_len, p->k_len) >= ((int64_t)1 << 27)) return LSP_ERR_SHAPE;
+    if (!known(t)) return LSP_ERR_DTYPE;
+    return LSP_OK;
+}
+
+int check_attention(const lsp_attention_problem* p, lsp_dtype t) {
+    if (!p || !p->Q || !p->K || !p->V || !p->O || !p->L) return LSP_ERR_NULL;
+    int rc = check_attention_shape(p, t);
+    if (rc != LSP_OK) return rc;
+    if (!rate(p->dropout) || !(p->scale > 0.0f) || !std::isfinite(p->scale)) return LSP_ERR_VALUE;
+    if ((rc = check_strides(p->q_stride, p->batch, p->q_len, p->heads, p->head_dim, t, false)) != LSP_OK) return rc;
+    if ((rc = check_strides(p->k_stride, p->batch, p->k_len, p->kv_heads, p->head_dim, t, false)) != LSP_OK) return rc;
+    if ((rc = check_strides(p->v_stride, p->batch, p->k_len, p->kv_heads, p->head_dim, t, false)) != LSP_OK) return rc;
+    if ((rc = check_strides(p->o_stride, p->batch, p->q_len, p->heads, p->head_dim, t, true)) != LSP_OK) return rc;
+    if (!aligned16(p->Q) || !aligned16(p->K) || !aligned16(p->V) || !aligned16(p->O) || !aligned16(p->L)) return LSP_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(p->q_lens) | reinterpret_cast<uintptr_t>(p->k_lens)) & 3u) return LSP_ERR_ALIGN;
+    return LSP_OK;
+}
+
+lsp::AttentionArgs attention_args(const lsp_attention_problem* p) {
+    lsp::AttentionArgs a{};
+    a.q = strided(p->Q, p->q_stride, p->batch, p->q_len, p->heads);
+    a.k = strided(p->K, p->k_stride, p->batch, p->k_len, p->kv_heads);
+    a.v = strided(p->V, p->v_stride, p->batch, p->k_len, p->kv_heads);
+    a.o = strided(p->O, p->o_stride, p->batch, p->q_len, p->heads);
+    a.L = p->L;
+    a.q_lens = p->q_lens; a.k_lens = p->k_lens;
+    a.batch = p->batch; a.heads = p->heads; a.kv_heads = p->kv_heads; a.group = p->heads / p->kv_heads;
+    a.q_len = p->q_len; a.k_len = p->k_len; a.head_dim = p->head_dim; a.causal = p->causal;
+    a.scale = p->scale; a.scale_log2 = p->scale * 1.44269504088896341f;
+    a.drop = lsp::make_dropout(p->dropout, p->seed, p->offset);
+    return a;
+}
+
+size_t delta_bytes(const lsp_attention_problem* p) { return lsp::align_up((size_t)p->batch * p->heads * p->q_len * sizeof(float), 256); }
+
+bool norm_kind(int32_t k) { return k == LSP_NORM_NONE || k == LSP_NORM_RMS || k == LSP_NORM_LAYER; }
+
+int check_norm_shape(const lsp_residual_norm_problem* p, lsp_dtype t) {
+    if (!p) return LSP_ERR_NULL;
+    if (p->rows <= 0 || p->rows > LSP_MAX_ROWS || p->width <= 0 || p->width > LSP_MAX_WIDTH || !norm_kind(p->post) || !norm_kind(p->pre)) return LSP_ERR_SHAPE;
+    if (!known(t)) return LSP_ERR_DTYPE;
+    return LSP_OK;
+}
+
+int check_norm(const lsp_residual_norm_problem* p, lsp_dtype t) {
+    if (!p || !p->x || !p->f || !p->y || !p->stats || (!p->h && p->pre != LSP_NORM_NONE)) return LSP_ERR_NULL;
+    const int rc = check_norm_shape(p, t);
+    if (rc != LSP_OK) return rc;
+    if (!rate(p->dropout) || !std::isfinite(p->residual_scale) || !std::isfinite(p->branch_scale) || !(p->eps >= 0.0f) || !std::isfinite(p->eps)) return LSP_ERR_VALUE;
+    const int64_t most = (int64_t)1 << 40;
+    for (const int64_t s : {p->x_stride, p->f_stride, p->y_stride, p->h ? p->h_stride : p->width})
+        if (p->rows > 1 && (s < p->width || s > most)) return LSP_ERR_SHAPE;
+    for (const void* q : {p->x, p->f, static_cast<const void*>(p->y), static_cast<const void*>(p->h), static_cast<const void*>(p->stats), p->post_weight, p->post_bias, p->gate,
+                          p->pre_weight, p->pre_bias})
+        if (!aligned16(q)) return LSP_ERR_ALIGN;
+    return LSP_OK;
+}
+
+lsp::ResidualNormArgs norm_args(const lsp_residual_norm_problem* p) {
+    lsp::ResidualNormArgs a{};
+    a.x = p->x; a.f = p->f; a.y = p->y; a.h = p->h; a.stats = p->stats;
+    a.post_w = p->post_weight; a.post_b = p->post_bias; a.gate = p->gate; a.pre_w = p->pre_weight; a.pre_b = p->pre_bias;
+    a.x_stride = p->x_stride; a.f_stride = p->f_stride; a.y_stride = p->y_stride; a.h_stride = p->h_stride;
+    a.rows = p->rows; a.width = p->width; a.post = p->post; a.pre = p->pre;
+    a.eps = p->eps; a.residual_scale = p->residual_scale; a.branch_scale = p->branch_scale;
+    a.drop = lsp::make_dropout(p->dropout, p->seed, p->offset);
+    return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+int lsp_dropout(const void* x, void* y, int64_t rows, int64_t width, float dropout, uint64_t seed, uint32_t offset, lsp_dtype dtype, void* stream) {
+    if (!x || !y) return LSP_ERR_NULL;
+    if (rows <= 0 || width <= 0 || width > INT32_MAX - 7 || rows > ((int64_t)1 << 31) / ((width + 7) / 8)) return LSP_ERR_SHAPE;   // a thread for every block of eight
+    if (!known(dtype)) return LSP_ERR_DTYPE;
+    if (!rate(dropout)) return LSP_ERR_VALUE;
+    if (!aligned16(x) || !aligned16(y)) return LSP_ERR_ALIGN;
+    return done(lsp::launch_dropout(x, y, rows, width, lsp::make_dropout(dropout, seed, offset), dtype, static_cast<hipStream_t>(stream)));
+}
+
+size_t lsp_attention_forward_workspace_bytes(const lsp_attention_problem* p, lsp_dtype dtype) {
+    if (check_attention_shape(p, dtype) != LSP_OK) return 0;
+    lsp::AttentionArgs a = attention_args(p);
+    lsp::plan_attention_forward(a, dtype);
+    return lsp::attention_partial_bytes(a);
+}
+
+int lsp_attention_forward(const lsp_attention_problem* p, lsp_dtype dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = check_attention(p, dtype);
+    if (rc != LSP_OK) return rc;
+    lsp::AttentionArgs a = attention_args(p);
+    lsp::plan_attention_forward(a, dtype);
+    const size_t need = lsp::attention_partial_bytes(a);
+    if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return LSP_ERR_WORKSPACE;
+    a.partial = static_cast<float*>(workspace);
+    return done(lsp::launch_attention_forward(a, dtype, static_cast<hipStream_t>(stream)));
+}
+
+// delta | two maxima
+size_t lsp_attention_backward_workspace_bytes(const lsp_attention_problem* p, lsp_dtype dtype) {
+    if (check_attention_shape(p, dtype) != LSP_OK) return 0;
+    return delta_bytes(p) + 256;
+}
+
+int lsp_attention_backward(const lsp_attention_problem* p, const lsp_attention_gradients* g, lsp_dtype dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!p || !g || !g->dO || !g->dQ || !g->dK || !g->dV) return LSP_ERR_NULL;
+    int rc = check_attention(p, dtype);
+    if (rc != LSP_OK) return rc;
+    if ((rc = check_strides(g->do_stride, p->batch, p->q_len, p->heads, p->head_dim, dtype, false)) != LSP_OK) return rc;
+    if ((rc = check_strides(g->dq_stride, p->batch, p->q_len, p->heads, p->head_dim, dtype, true)) != LSP_OK) return rc;
+    if ((rc = check_strides(g->dk_stride, p->batch, p->k_len, p->kv_heads, p->head_dim, dtype, true)) != LSP_OK) return rc;
+    if ((rc = check_strides(g->dv_stride, p->batch, p->k_len, p->kv_heads, p->head_dim, dtype, true)) != LSP_OK) return rc;
+    if (!aligned16(g->dO) || !aligned16(g->dQ) || !aligned16(g->dK) || !aligned16(g->dV)) return LSP_ERR_ALIGN;
+    if (!workspace || workspace_bytes < lsp_attention_backward_workspace_bytes(p, dtype) || !aligned16(workspace)) return LSP_ERR_WORKSPACE;
+    lsp::AttentionArgs a = attention_args(p);
+    a.d_o = strided(g->dO, g->do_stride, p->batch, p->q_len, p->heads);
+    a.dq = strided(g->dQ, g->dq_stride, p->batch, p->q_len, p->heads);
+    a.dk = strided(g->dK, g->dk_stride, p->batch, p->k_len, p->kv_heads);
+    a.dv = strided(g->dV, g->dv_stride, p->batch, p->k_len, p->kv_heads);
+    a.delta = static_cast<float*>(workspace);
+    a.most = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + delta_bytes(p));
+    return done(lsp::launch_attention_backward(a, dtype, static_cast<hipStream_t>(stream)));
+}
+
+int lsp_residual_norm_forward(const lsp_residual_norm_problem* p, lsp_dtype dtype, void* stream) {
+    const int rc = check_norm(p, dtype);
+    if (rc != LSP_OK) return rc;
+    return done(lsp::launch_residual_norm_forward(norm_args(p), dtype, static_cast<hipStream_t>(stream)));
+}
+
+size_t lsp_residual_norm_backward_workspace_bytes(const lsp_residual_norm_problem* p, lsp_dtype dtype) {
+    if (check_norm_shape(p, dtype) != LSP_OK) return 0;
+    return lsp::residual_norm_partial_bytes(p->rows, p->width);
+}
+
+int lsp_residual_norm_backward(const lsp_residual_norm_problem* p, const lsp_residual_norm_gradients* g, lsp_dtype dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!p || !g || !g->dy || !g->dx || !g->df || (!g->dh && p->pre != LSP_NORM_NONE)) return LSP_ERR_NULL;
+    const int rc = check_norm(p, dtype);
+    if (rc != LSP_OK) return rc;
+    if (p->y == p->x) return LSP_ERR_SHAPE;                              // x is needed as it was
+    const int64_t most = (int64_t)1 << 40;
+    for (const int64_t s : {g->dy_stride, g->dx_stride, g->df_stride, g->dh ? g->dh_stride : p->width})
+        if (p->rows > 1 && (s < p->width || s > most)) return LSP_ERR_SHAPE;
+    for (const void* q : {g->dy, g->dh, static_cast<const void*>(g->dx), static_cast<const void*>(g->df)})
+        if (!aligned16(q)) return LSP_ERR_ALIGN;
+    for (const float* q : {g->post_weight, g->post_bias, g->gate, g->pre_weight, g->pre_bias})
+        if (!aligned16(q)) return LSP_ERR_ALIGN;
+    const size_t need = lsp_residual_norm_backward_workspace_bytes(p, dtype);
+    if (!workspace || workspace_bytes < need || !aligned16(workspace)) return LSP_ERR_WORKSPACE;
+    lsp::ResidualNormArgs a = norm_args(p);
+    a.dy = g->dy; a.dh = g->dh; a.dx = g->dx; a.df = g->df;
+    a.dy_stride = g->dy_stride; a.dh_stride = g->dh_stride; a.dx_stride = g->dx_stride; a.df_stride = g->df_stride;
+    a.grads[0] = g->pre_weight; a.grads[1] = g->pre_bias; a.grads[2] = g->gate; a.grads[3] = g->post_weight; a.grads[4] = g->post_bias;
+    if (p->pre == LSP_NORM_NONE && (g->pre_weight || g->pre_bias)) return LSP_ERR_SHAPE;      // a norm that is none has no weights
+    if (p->post == LSP_NORM_NONE && (g->post_weight || g->post_bias)) return LSP_ERR_SHAPE;
+    a.partial = static_cast<float*>(workspace);
+    return done(lsp::launch_residual_norm_backward(a, dtype, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"
