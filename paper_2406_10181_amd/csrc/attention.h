@@ -137,7 +137,6 @@ template <typename D, int DP> struct Tile {
 __device__ __forceinline__ u32x4 lds_read16(uint32_t at) { return *(const LSP_SHARED_AS u32x4*)(uintptr_t)at; }
 __device__ __forceinline__ f32x4 lds_read16f(uint32_t at) { return *(const LSP_SHARED_AS f32x4*)(uintptr_t)at; }
 __device__ __forceinline__ float lds_read4f(uint32_t at) { return *(const LSP_SHARED_AS float*)(uintptr_t)at; }
-__device__ __forceinline__ void lds_write16(uint32_t at, u32x4 x) { *(LSP_SHARED_AS u32x4*)(uintptr_t)at = x; }
 
 // A operand whose rows are rows row0 + 0..31 of the tile and whose k are its columns 16 ks + 0..15 (lane half h: 8 h + 0..7)
 template <typename D, int DP> __device__ __forceinline__ Frag<D> row_frag(uint32_t tile, int row0, int ks, int lane) {
@@ -190,28 +189,30 @@ template <typename D> __device__ __forceinline__ const uint8_t* at(const Strided
     return static_cast<const uint8_t*>(s.p) + (b * s.batch + position * s.position + head * s.head) * D::size;
 }
 
-// ROWS rows of a tile on their way from memory to LDS: a thread holds kCount units.  Rows from `left` on and columns from head_dim on
-// are zeros and not read.
-template <typename D, int DP, int ROWS, int NT> struct Staged {
+// ROWS rows of a tile, asked for straight into LDS: a wave's load fills 1 KiB of LDS in the order of its lanes, so a lane asks for the unit that
+// belongs at its place.  Rows from `left` on, columns from head_dim on and places that a row does not use lie out of the buffer: zeros, and not
+// read.  They have arrived when vmcnt says so.
+template <typename D, int DP, int ROWS, int NT> struct Fetch {
     using T = Tile<D, DP>;
-    static constexpr int kTotal = ROWS * T::kUnits;
-    static constexpr int kCount = (kTotal + NT - 1) / NT;
-    u32x4 x[kCount];
-    __device__ __forceinline__ void load(const void* first_row, uint32_t row_bytes, int left, int head_dim, int tid) {
+    static constexpr int kWaves = NT / 64, kRowsAtOnce = 64 / T::kPitch;                  // rows that a wave's load fills
+    static constexpr int kCount = ROWS / kRowsAtOnce / kWaves;
+    static_assert(kCount * kWaves * kRowsAtOnce == ROWS, "whole loads");
+    uint32_t off[kCount];                                                                 // of this lane, from the tile's first row on
+    int row0;
+    __device__ __forceinline__ void setup(uint32_t row_bytes, int head_dim, int wave, int lane) {
+        row0 = wave * kRowsAtOnce + lane / T::kPitch;
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            const uint32_t row = row0 + i * (kWaves * kRowsAtOnce), unit = (uint32_t)(lane % T::kPitch) ^ T::swizzle(row);
+            off[i] = (int)unit * T::kUnitElems < head_dim ? row * row_bytes + unit * 16u : 0x80000000u;
+        }
+    }
+    __device__ __forceinline__ void operator()(const void* first_row, int left, uint32_t tile, int wave) const {
         const Buffer b = buffer_from(first_row);
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
-            const int u = tid + i * NT, row = u / T::kUnits, unit = u % T::kUnits;
-            const bool there = row < left && unit * T::kUnitElems < head_dim && (kTotal % NT == 0 || u < kTotal);
-            const uint32_t off = there ? (uint32_t)row * row_bytes + (uint32_t)unit * 16u : 0x80000000u;
-            x[i] = __builtin_amdgcn_raw_buffer_load_b128(b, (int)off, 0, 0);
-        }
-    }
-    __device__ __forceinline__ void store(uint32_t tile, int tid) const {
-#pragma unroll
-        for (int i = 0; i < kCount; ++i) {
-            const int u = tid + i * NT;
-            if (kTotal % NT == 0 || u < kTotal) lds_write16(tile + T::place(u / T::kUnits, u % T::kUnits), x[i]);
+            const uint32_t o = row0 + i * (kWaves * kRowsAtOnce) < left ? off[i] : 0x80000000u;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (LSP_SHARED_AS void*)(uintptr_t)(tile + (i * kWaves + wave) * 1024u), 16, (int)o, 0, 0, 0);
         }
     }
 };

@@ -66,7 +66,7 @@ __global__ __launch_bounds__(256) void k_attention_delta(const AttentionArgs a, 
 template <typename D> __global__ void k_attention_clear(uint32_t* most) { if (threadIdx.x < 2) most[threadIdx.x] = 0; }
 
 template <typename D, int DP, bool DROP>
-__global__ __launch_bounds__(256) void k_attention_dq(const AttentionArgs a) {
+__global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_attention_dq(const AttentionArgs a) {
     using T = Tile<D, DP>;
     constexpr int BN = tile_rows<D>(), NT = 256, kSteps = DP / 16, kTiles = BN / 32, kCols = DP / 32;
     constexpr uint32_t kTileBytes = BN * T::kRowBytes;
@@ -111,19 +111,19 @@ __global__ __launch_bounds__(256) void k_attention_dq(const AttentionArgs a) {
     const uint8_t* kp = at<D>(a.k, b, 0, kv_head);
     const uint8_t* vp = at<D>(a.v, b, 0, kv_head);
     const int64_t k_bytes = a.k.position * D::size, v_bytes = a.v.position * D::size;
-    Staged<D, DP, BN, NT> ks_, vs_;
+    Fetch<D, DP, BN, NT> fetch_k, fetch_v;
+    fetch_k.setup((uint32_t)k_bytes, a.head_dim, wave, lane);
+    fetch_v.setup((uint32_t)v_bytes, a.head_dim, wave, lane);
     if (end > 0) {
-        ks_.load(kp, (uint32_t)k_bytes, nk, a.head_dim, tid);
-        vs_.load(vp, (uint32_t)v_bytes, nk, a.head_dim, tid);
-        ks_.store(lds, tid);
-        vs_.store(lds + kTileBytes, tid);
+        fetch_k(kp, nk, lds, wave);
+        fetch_v(vp, nk, lds + kTileBytes, wave);
         __syncthreads();
         uint32_t buf = lds;
         for (int k0 = 0; k0 < end; k0 += BN) {
-            const bool more = k0 + BN < end;
-            if (more) {
-                ks_.load(kp + (k0 + BN) * k_bytes, (uint32_t)k_bytes, nk - k0 - BN, a.head_dim, tid);
-                vs_.load(vp + (k0 + BN) * v_bytes, (uint32_t)v_bytes, nk - k0 - BN, a.head_dim, tid);
+            const uint32_t other = buf == lds ? lds + 2 * kTileBytes : lds;
+            if (k0 + BN < end) {
+                fetch_k(kp + (k0 + BN) * k_bytes, nk - k0 - BN, other, wave);
+                fetch_v(vp + (k0 + BN) * v_bytes, nk - k0 - BN, other + kTileBytes, wave);
             }
             if (k0 < most) {
                 const bool edge = k0 + BN > least;
@@ -151,11 +151,7 @@ __global__ __launch_bounds__(256) void k_attention_dq(const AttentionArgs a) {
                     }
                 }
             }
-            buf = buf == lds ? lds + 2 * kTileBytes : lds;
-            if (more) {
-                ks_.store(buf, tid);
-                vs_.store(buf + kTileBytes, tid);
-            }
+            buf = other;
             __syncthreads();
         }
     }
@@ -172,7 +168,7 @@ __global__ __launch_bounds__(256) void k_attention_dq(const AttentionArgs a) {
 }
 
 template <typename D, int DP, bool DROP>
-__global__ __launch_bounds__(256) void k_attention_dkv(const AttentionArgs a) {
+__global__ __launch_bounds__(256, (DP > (D::size == 4 ? 32 : 96) ? 1 : 2)) void k_attention_dkv(const AttentionArgs a) {
     using T = Tile<D, DP>;
     constexpr int BQ = tile_rows<D>(), NT = 256, kSteps = DP / 16, kTiles = BQ / 32, kCols = DP / 32;
     constexpr uint32_t kTileBytes = BQ * T::kRowBytes, kBufBytes = 2 * kTileBytes + BQ * 8;
@@ -208,11 +204,13 @@ __global__ __launch_bounds__(256) void k_attention_dkv(const AttentionArgs a) {
     for (int c = 0; c < kCols; ++c) { dk[c] = zeros16(); dv[c] = zeros16(); }
 
     const int64_t q_bytes = a.q.position * D::size, g_bytes = a.d_o.position * D::size;
-    Staged<D, DP, BQ, NT> qs, gs;
+    Fetch<D, DP, BQ, NT> fetch_q, fetch_g;
+    fetch_q.setup((uint32_t)q_bytes, a.head_dim, wave, lane);
+    fetch_g.setup((uint32_t)g_bytes, a.head_dim, wave, lane);
     float stat[2];                                                                        // threads below BQ: -L log2(e) and delta of a row
-    const auto load = [&](int q_head, int q0) {
-        qs.load(at<D>(a.q, b, q0, q_head), (uint32_t)q_bytes, nq - q0, a.head_dim, tid);
-        gs.load(at<D>(a.d_o, b, q0, q_head), (uint32_t)g_bytes, nq - q0, a.head_dim, tid);
+    const auto load = [&](int q_head, int q0, uint32_t buf) {
+        fetch_q(at<D>(a.q, b, q0, q_head), nq - q0, buf, wave);
+        fetch_g(at<D>(a.d_o, b, q0, q_head), nq - q0, buf + kTileBytes, wave);
         if (tid < BQ) {
             const int qi = q0 + tid;
             const int64_t line = ((int64_t)b * a.heads + q_head) * a.q_len + qi;
@@ -222,8 +220,6 @@ __global__ __launch_bounds__(256) void k_attention_dkv(const AttentionArgs a) {
         }
     };
     const auto store = [&](uint32_t buf) {
-        qs.store(buf, tid);
-        gs.store(buf + kTileBytes, tid);
         if (tid < BQ) {
             *(LSP_SHARED_AS float*)(uintptr_t)(buf + 2 * kTileBytes + tid * 4) = stat[0];
             *(LSP_SHARED_AS float*)(uintptr_t)(buf + 2 * kTileBytes + BQ * 4 + tid * 4) = stat[1];
@@ -232,7 +228,7 @@ __global__ __launch_bounds__(256) void k_attention_dkv(const AttentionArgs a) {
     if (begin < end) {
         int q_head = kv_head * a.group, q0 = begin;
         const int past = (kv_head + 1) * a.group;
-        load(q_head, q0);
+        load(q_head, q0, lds);
         store(lds);
         __syncthreads();
         uint32_t buf = lds;
@@ -240,10 +236,11 @@ __global__ __launch_bounds__(256) void k_attention_dkv(const AttentionArgs a) {
             int next_head = q_head, next_q0 = q0 + BQ;
             if (next_q0 >= end) { next_q0 = begin; ++next_head; }
             const bool more = next_head < past;
-            if (more) load(next_head, next_q0);
+            const uint32_t other = buf == lds ? lds + kBufBytes : lds;
+            if (more) load(next_head, next_q0, other);
             if (q0 + BQ > from && first < nk) {
                 const bool edge = q0 < all_from;
-#pragma unroll
+#pragma unroll 1
                 for (int t = 0; t < kTiles; ++t) {
                     f32x16 s = zeros16(), dp = zeros16();
 #pragma unroll
@@ -301,7 +298,7 @@ __global__ __launch_bounds__(256) void k_attention_dkv(const AttentionArgs a) {
                     }
                 }
             }
-            buf = buf == lds ? lds + kBufBytes : lds;
+            buf = other;
             if (more) store(buf);
             __syncthreads();
             q_head = next_head; q0 = next_q0;

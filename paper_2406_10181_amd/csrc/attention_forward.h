@@ -35,7 +35,7 @@ __device__ __forceinline__ void drop_keys(f32x16& s, uint32_t key0, uint32_t q, 
 }
 
 template <typename D, int DP, bool DROP>
-__global__ __launch_bounds__(256) void k_attention_forward(const AttentionArgs a) {
+__global__ __launch_bounds__(256, 2) void k_attention_forward(const AttentionArgs a) {
     using T = Tile<D, DP>;
     constexpr int BN = tile_rows<D>(), NT = 256, kSteps = DP / 16, kTiles = BN / 32, kCols = DP / 32;
     constexpr uint32_t kTileBytes = BN * T::kRowBytes;
@@ -90,20 +90,20 @@ __global__ __launch_bounds__(256) void k_attention_forward(const AttentionArgs a
     const uint8_t* kp = at<D>(a.k, b, 0, kv_head);
     const uint8_t* vp = at<D>(a.v, b, 0, kv_head);
     const int64_t k_bytes = a.k.position * D::size, v_bytes = a.v.position * D::size;
-    Staged<D, DP, BN, NT> ks_, vs_;
+    Fetch<D, DP, BN, NT> fetch_k, fetch_v;
+    fetch_k.setup((uint32_t)k_bytes, a.head_dim, wave, lane);
+    fetch_v.setup((uint32_t)v_bytes, a.head_dim, wave, lane);
     const bool any = begin < end && (a.packed || row_tile * kRowsForward < nq);
     if (any) {
-        ks_.load(kp + begin * k_bytes, (uint32_t)k_bytes, nk - begin, a.head_dim, tid);
-        vs_.load(vp + begin * v_bytes, (uint32_t)v_bytes, nk - begin, a.head_dim, tid);
-        ks_.store(lds, tid);
-        vs_.store(lds + kTileBytes, tid);
+        fetch_k(kp + begin * k_bytes, nk - begin, lds, wave);
+        fetch_v(vp + begin * v_bytes, nk - begin, lds + kTileBytes, wave);
         __syncthreads();
         uint32_t buf = lds;
         for (int k0 = begin; k0 < end; k0 += BN) {
-            const bool more = k0 + BN < end;
-            if (more) {
-                ks_.load(kp + (k0 + BN) * k_bytes, (uint32_t)k_bytes, nk - k0 - BN, a.head_dim, tid);
-                vs_.load(vp + (k0 + BN) * v_bytes, (uint32_t)v_bytes, nk - k0 - BN, a.head_dim, tid);
+            const uint32_t other = buf == lds ? lds + 2 * kTileBytes : lds;
+            if (k0 + BN < end) {
+                fetch_k(kp + (k0 + BN) * k_bytes, nk - k0 - BN, other, wave);
+                fetch_v(vp + (k0 + BN) * v_bytes, nk - k0 - BN, other + kTileBytes, wave);
             }
             if (k0 < most) {
                 f32x16 s[kTiles];
@@ -152,11 +152,7 @@ __global__ __launch_bounds__(256) void k_attention_forward(const AttentionArgs a
                     }
                 }
             }
-            buf = buf == lds ? lds + 2 * kTileBytes : lds;
-            if (more) {
-                ks_.store(buf, tid);
-                vs_.store(buf + kTileBytes, tid);
-            }
+            buf = other;
             __syncthreads();
         }
     }
