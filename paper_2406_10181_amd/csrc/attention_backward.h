@@ -167,10 +167,16 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
         }
 }
 
+// At head_dim 128 in 16 bits K and V of a wave's keys, dK, dV and the scores are more than the 256 registers that two waves a SIMD have: V stays in
+// LDS, and there is room for it with 32 queries at a time.
+template <typename D, int DP> constexpr bool values_in_lds() { return D::size == 2 && DP > 96; }
+template <typename D, int DP> constexpr int queries_at_once() { return values_in_lds<D, DP>() ? 32 : tile_rows<D>(); }
+
 template <typename D, int DP, bool DROP>
-__global__ __launch_bounds__(256, (DP > (D::size == 4 ? 32 : 96) ? 1 : 2)) void k_attention_dkv(const AttentionArgs a) {
+__global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_attention_dkv(const AttentionArgs a) {
     using T = Tile<D, DP>;
-    constexpr int BQ = tile_rows<D>(), NT = 256, kSteps = DP / 16, kTiles = BQ / 32, kCols = DP / 32;
+    constexpr bool kValuesInLds = values_in_lds<D, DP>();
+    constexpr int BQ = queries_at_once<D, DP>(), NT = 256, kSteps = DP / 16, kTiles = BQ / 32, kCols = DP / 32;
     constexpr uint32_t kTileBytes = BQ * T::kRowBytes, kBufBytes = 2 * kTileBytes + BQ * 8;
     extern __shared__ __align__(16) uint8_t smem[];
     const uint32_t lds = (uint32_t)(uintptr_t)(LSP_SHARED_AS uint8_t*)smem;               // Q | dO | L | delta, twice; bits of kept ones of each wave
@@ -191,12 +197,24 @@ __global__ __launch_bounds__(256, (DP > (D::size == 4 ? 32 : 96) ? 1 : 2)) void 
     const int all_from = a.causal ? first + 31 - ahead : 0;                               // from here on every key of the wave is seen
     const int my_from = a.causal ? key - ahead : 0;
 
-    Frag<D> kf[kSteps], vf[kSteps];
+    const uint32_t values = lds + 2 * kBufBytes + 512;                                    // V of the workgroup's keys
+    Frag<D> kf[kSteps], vf[kValuesInLds ? 1 : kSteps];
     {
         const uint8_t* p = counts ? at<D>(a.k, b, key, kv_head) : nullptr;
         const uint8_t* v = counts ? at<D>(a.v, b, key, kv_head) : nullptr;
 #pragma unroll
-        for (int ks = 0; ks < kSteps; ++ks) { kf[ks] = global_frag<D>(p, ks, a.head_dim, lane); vf[ks] = global_frag<D>(v, ks, a.head_dim, lane); }
+        for (int ks = 0; ks < kSteps; ++ks) {
+            kf[ks] = global_frag<D>(p, ks, a.head_dim, lane);
+            if constexpr (!kValuesInLds) vf[ks] = global_frag<D>(v, ks, a.head_dim, lane);
+        }
+    }
+    if constexpr (kValuesInLds) {
+        if (begin < end) {
+            const int64_t v_bytes = a.v.position * D::size;
+            Fetch<D, DP, kKeysBackward, NT> fetch_v;
+            fetch_v.setup((uint32_t)v_bytes, a.head_dim, wave, lane);
+            fetch_v(at<D>(a.v, b, key_tile * kKeysBackward, kv_head), nk - key_tile * kKeysBackward, values, wave);
+        }
     }
     const float factor = score_factor<D>(a), keep = (DROP ? a.drop.scale : 1.0f) * factor, c2 = a.scale_log2;
     f32x16 dk[kCols], dv[kCols];
@@ -246,7 +264,12 @@ __global__ __launch_bounds__(256, (DP > (D::size == 4 ? 32 : 96) ? 1 : 2)) void 
 #pragma unroll
                     for (int ks = 0; ks < kSteps; ++ks) s = mma<D>(row_frag<D, DP>(buf, 32 * t, ks, lane), kf[ks], s);
 #pragma unroll
-                    for (int ks = 0; ks < kSteps; ++ks) dp = mma<D>(row_frag<D, DP>(buf + kTileBytes, 32 * t, ks, lane), vf[ks], dp);
+                    for (int ks = 0; ks < kSteps; ++ks) {
+                        Frag<D> v;
+                        if constexpr (kValuesInLds) v = row_frag<D, DP>(values, 32 * wave, ks, lane);
+                        else v = vf[ks];
+                        dp = mma<D>(row_frag<D, DP>(buf + kTileBytes, 32 * t, ks, lane), v, dp);
+                    }
                     if (edge)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) s[i] = q0 + 32 * t + 8 * (i >> 2) + 4 * h + (i & 3) >= my_from ? s[i] : -INFINITY;
@@ -326,7 +349,8 @@ template <typename D, int DP, bool DROP> static hipError_t run_attention_backwar
     constexpr size_t tile = (size_t)tile_rows<D>() * Tile<D, DP>::kRowBytes;
     constexpr auto dkv = k_attention_dkv<D, DP, DROP>;
     constexpr auto dq = k_attention_dq<D, DP, DROP>;
-    constexpr size_t lds_dkv = 4 * tile + 2 * 8 * tile_rows<D>() + 512, lds_dq = 4 * tile;
+    constexpr size_t lds_dkv = queries_at_once<D, DP>() * (4 * Tile<D, DP>::kRowBytes + 16) + 512 + (values_in_lds<D, DP>() ? kKeysBackward * Tile<D, DP>::kRowBytes : 0);
+    constexpr size_t lds_dq = 4 * tile;
     hipError_t e = allow_dynamic_lds<dkv, lds_dkv>();
     if (e == hipSuccess) e = allow_dynamic_lds<dq, lds_dq>();
     if (e != hipSuccess) return e;
