@@ -111,74 +111,82 @@ __device__ __forceinline__ float halves_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// A tile in LDS: rows of DP elements (head_dim, filled up with zeros to a multiple of 32) in units of 16 bytes.  A row has a power
-// of two of units, and unit c of row t lies at place c ^ swizzle(t), chosen so that neither way of reading meets a bank twice: the 16
-// lanes that read one unit of 16 consecutive rows (row_frag) hit 16 different groups of four banks, and so do the 32 lanes that read four
-// consecutive units of four consecutive rows (column_frag).
+// A tile in LDS: rows of DP elements (head_dim, filled up with zeros to a multiple of 32) in units of 16 bytes, the units of eight rows together:
+// unit u of the rows 8 g .. 8 g + 7 makes a slab of 128 bytes.  Slabs of odd g change places in pairs, and rows 0..3 and 4..7 of a slab where bit 1 of u is
+// set, so that neither way of reading meets a bank twice: 16 lanes that read one unit of 16 rows (Reader::rows) hit 16 different groups of four banks, and so do
+// the 32 lanes that read four consecutive units of four rows (Reader::columns).  All that a lane adds to its own address for another row group, step or
+// column is then a constant of the instruction, and loads of whole 128-byte lines fill consecutive LDS.
 template <typename D, int DP> struct Tile {
     static constexpr int kUnitElems = 16 / D::size;
-    static constexpr int kUnits = DP / kUnitElems;                                        // in use
-    static constexpr int kPitch = kUnits <= 4 ? 4 : kUnits <= 8 ? 8 : kUnits <= 16 ? 16 : 32;
-    static constexpr int kRowBytes = kPitch * 16;
-    __device__ static __forceinline__ uint32_t swizzle(uint32_t t) {
-        if constexpr (D::size == 2) {
-            if constexpr (kPitch == 16) return (t & 3u) << 2 | ((t >> 2) & 3u);
-            else if constexpr (kPitch == 8) return ((t >> 1) & 1u) << 2 | ((t >> 2) & 3u);
-            else return (t >> 2) & 3u;
-        } else {
-            // fp32: columns are read one float a lane, rows t and t + 4 at a time
-            if constexpr (kPitch >= 16) return ((t >> 2) & 1u) << 3 | (t & 3u) | ((t >> 3) & 1u) << 2;
-            else return (t >> 1) & 7u;
-        }
+    static constexpr int kUnits = DP / kUnitElems;
+    static constexpr int kRowBytes = kUnits * 16;
+    __device__ static __forceinline__ uint32_t place(uint32_t row, uint32_t unit) {
+        const uint32_t g = row >> 3;
+        return g * (kUnits * 128) + (unit ^ (g & 1u)) * 128u + ((row & 7u) ^ (((unit >> 1) & 1u) << 2)) * 16u;
     }
-    __device__ static __forceinline__ uint32_t place(uint32_t row, uint32_t unit) { return row * kRowBytes + (unit ^ swizzle(row)) * 16u; }
+    // the other way round: which unit of which row is the p-th
+    __device__ static __forceinline__ void at_place(uint32_t p, uint32_t& row, uint32_t& unit) {
+        const uint32_t g = p / (8 * kUnits), rest = p % (8 * kUnits);
+        unit = (rest >> 3) ^ (g & 1u);
+        row = 8 * g + ((rest & 7u) ^ (((unit >> 1) & 1u) << 2));
+    }
 };
 
 __device__ __forceinline__ u32x4 lds_read16(uint32_t at) { return *(const LSP_SHARED_AS u32x4*)(uintptr_t)at; }
 __device__ __forceinline__ f32x4 lds_read16f(uint32_t at) { return *(const LSP_SHARED_AS f32x4*)(uintptr_t)at; }
+__device__ __forceinline__ void lds_write16(uint32_t at, u32x4 x) { *(LSP_SHARED_AS u32x4*)(uintptr_t)at = x; }
 __device__ __forceinline__ float lds_read4f(uint32_t at) { return *(const LSP_SHARED_AS float*)(uintptr_t)at; }
 
-// A operand whose rows are rows row0 + 0..31 of the tile and whose k are its columns 16 ks + 0..15 (lane half h: 8 h + 0..7)
-template <typename D, int DP> __device__ __forceinline__ Frag<D> row_frag(uint32_t tile, int row0, int ks, int lane) {
+// Where a lane reads in a tile: computed once, the rest are constants.
+template <typename D, int DP> struct Reader {
     using T = Tile<D, DP>;
-    const uint32_t row = row0 + (lane & 31), h = (uint32_t)lane >> 5;
-    Frag<D> f;
-    if constexpr (D::size == 2) f.w = lds_read16(tile + T::place(row, 2 * ks + h));
-    else {
-        const f32x4 a = lds_read16f(tile + T::place(row, 4 * ks + 2 * h)), b = lds_read16f(tile + T::place(row, 4 * ks + 2 * h + 1));
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { f.w[j] = a[j]; f.w[4 + j] = b[j]; }
-    }
-    return f;
-}
-
-// A operand whose rows are columns 32 ct + 0..31 of the tile and whose k are its rows row0 + 0..15, in the order that the accumulators
-// have them.  In 16 bits the transposing read does it: 16 lanes hold four rows of 16 columns, four columns each, and each gets one column of
-// the four rows.
-template <typename D, int DP> __device__ __forceinline__ Frag<D> column_frag(uint32_t tile, int row0, int ct, int lane) {
-    using T = Tile<D, DP>;
-    const uint32_t h = (uint32_t)lane >> 5;
-    Frag<D> f;
-    if constexpr (D::size == 2) {
-        const uint32_t unit = 4 * ct + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+    uint32_t row_at[2], column_at[2];
+    __device__ __forceinline__ explicit Reader(int lane) {
+        const uint32_t row = lane & 31, h = (uint32_t)lane >> 5;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            const uint32_t row = row0 + 8 * x + 4 * h + ((lane >> 2) & 3);
-            const s16x4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LSP_SHARED_AS s16x4*)(uintptr_t)(tile + T::place(row, unit) + (lane & 1) * 8u));
-            u32x2 u;
-            __builtin_memcpy(&u, &t, 8);
-            f.w[2 * x] = u[0]; f.w[2 * x + 1] = u[1];
-        }
-    } else {
-        const uint32_t unit = 8 * ct + ((lane & 31) >> 2);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t row = row0 + (j >> 2) * 8 + 4 * h + (j & 3);
-            f.w[j] = lds_read4f(tile + T::place(row, unit) + (lane & 3) * 4u);
+            if constexpr (D::size == 2) {
+                row_at[x] = T::place(row, 2 * x + h);                                     // even and odd steps
+                const uint32_t unit = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+                column_at[x] = T::place(8 * x + 4 * h + ((lane >> 2) & 3), unit) + (lane & 1) * 8u;
+            } else {
+                row_at[x] = T::place(row, 2 * h + x);                                     // the two units of a step
+                column_at[x] = T::place(8 * x + 4 * h, (lane & 31) >> 2) + (lane & 3) * 4u;
+            }
         }
     }
-    return f;
-}
+    // A (or B) operand whose rows (columns) are rows ROW0 + 0..31 of the tile and whose k are its columns 16 ks + 0..15 (lane half h: 8 h + 0..7)
+    __device__ __forceinline__ Frag<D> rows(uint32_t tile, int row0, int ks) const {
+        Frag<D> f;
+        const uint32_t t = tile + row0 / 8 * (T::kUnits * 128);
+        if constexpr (D::size == 2) f.w = lds_read16(row_at[ks & 1] + t + (ks >> 1) * 512);
+        else {
+            const f32x4 a = lds_read16f(row_at[0] + t + ks * 512), b = lds_read16f(row_at[1] + t + ks * 512);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { f.w[j] = a[j]; f.w[4 + j] = b[j]; }
+        }
+        return f;
+    }
+    // A operand whose rows are columns 32 ct + 0..31 of the tile and whose k are its rows ROW0 + 0..15, in the order that the accumulators have
+    // them.  In 16 bits the transposing read does it: 16 lanes hold four rows of 16 columns, four columns each, and each gets one column of the four rows.
+    __device__ __forceinline__ Frag<D> columns(uint32_t tile, int row0, int ct) const {
+        Frag<D> f;
+        const uint32_t t = tile + row0 / 8 * (T::kUnits * 128);
+        if constexpr (D::size == 2) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LSP_SHARED_AS s16x4*)(uintptr_t)(column_at[x] + t + ct * 512));
+                u32x2 u;
+                __builtin_memcpy(&u, &v, 8);
+                f.w[2 * x] = u[0]; f.w[2 * x + 1] = u[1];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f.w[j] = lds_read4f(column_at[j >> 2] + t + ct * 1024 + (j & 3) * 16);
+        }
+        return f;
+    }
+};
 
 typedef __amdgpu_buffer_rsrc_t Buffer;
 // A buffer of 2 GiB from p on; offsets from 2^31 on are out of it, and loads there give zeros
@@ -190,28 +198,29 @@ template <typename D> __device__ __forceinline__ const uint8_t* at(const Strided
 }
 
 // ROWS rows of a tile, asked for straight into LDS: a wave's load fills 1 KiB of LDS in the order of its lanes, so a lane asks for the unit that
-// belongs at its place.  Rows from `left` on, columns from head_dim on and places that a row does not use lie out of the buffer: zeros, and not
-// read.  They have arrived when vmcnt says so.
+// belongs at its place.  Rows from `left` on and columns from head_dim on lie out of the buffer: zeros, and not read.  They have arrived when vmcnt
+// says so.
 template <typename D, int DP, int ROWS, int NT> struct Fetch {
     using T = Tile<D, DP>;
-    static constexpr int kWaves = NT / 64, kRowsAtOnce = 64 / T::kPitch;                  // rows that a wave's load fills
-    static constexpr int kCount = ROWS / kRowsAtOnce / kWaves;
-    static_assert(kCount * kWaves * kRowsAtOnce == ROWS, "whole loads");
+    static constexpr int kWaves = NT / 64, kLoads = ROWS * T::kUnits / 64, kCount = (kLoads + kWaves - 1) / kWaves;
+    static_assert(ROWS * T::kUnits % 64 == 0, "whole loads");
     uint32_t off[kCount];                                                                 // of this lane, from the tile's first row on
-    int row0;
+    int row[kCount];
     __device__ __forceinline__ void setup(uint32_t row_bytes, int head_dim, int wave, int lane) {
-        row0 = wave * kRowsAtOnce + lane / T::kPitch;
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
-            const uint32_t row = row0 + i * (kWaves * kRowsAtOnce), unit = (uint32_t)(lane % T::kPitch) ^ T::swizzle(row);
-            off[i] = (int)unit * T::kUnitElems < head_dim ? row * row_bytes + unit * 16u : 0x80000000u;
+            uint32_t r, unit;
+            T::at_place((i * kWaves + wave) * 64 + lane, r, unit);
+            row[i] = (int)r;
+            off[i] = (int)unit * T::kUnitElems < head_dim ? r * row_bytes + unit * 16u : 0x80000000u;
         }
     }
     __device__ __forceinline__ void operator()(const void* first_row, int left, uint32_t tile, int wave) const {
         const Buffer b = buffer_from(first_row);
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
-            const uint32_t o = row0 + i * (kWaves * kRowsAtOnce) < left ? off[i] : 0x80000000u;
+            if (kLoads % kWaves && i * kWaves + wave >= kLoads) break;
+            const uint32_t o = row[i] < left ? off[i] : 0x80000000u;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (LSP_SHARED_AS void*)(uintptr_t)(tile + (i * kWaves + wave) * 1024u), 16, (int)o, 0, 0, 0);
         }
     }
@@ -243,6 +252,8 @@ template <typename D> __device__ __forceinline__ void store_four(uint8_t* p, flo
 }
 
 __device__ __forceinline__ int valid_length(const int32_t* lens, int b, int most) { return lens ? min(max(lens[b], 0), most) : most; }
+
+template <int I> using Const = std::integral_constant<int, I>;
 
 // Work item of a workgroup.  Workgroups go round the eight XCDs, each with an L2 of its own: a run of consecutive items is given to each XCD, so
 // that the workgroups that read the same keys share an L2.

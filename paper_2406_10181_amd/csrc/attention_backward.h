@@ -118,25 +118,26 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
         fetch_k(kp, nk, lds, wave);
         fetch_v(vp, nk, lds + kTileBytes, wave);
         __syncthreads();
-        uint32_t buf = lds;
-        for (int k0 = 0; k0 < end; k0 += BN) {
-            const uint32_t other = buf == lds ? lds + 2 * kTileBytes : lds;
+        const Reader<D, DP> read(lane);
+        const auto step = [&](auto which, int k0) {
+            const uint32_t buf = lds + which * 2 * kTileBytes, other = lds + (1 - which) * 2 * kTileBytes;
             if (k0 + BN < end) {
                 fetch_k(kp + (k0 + BN) * k_bytes, nk - k0 - BN, other, wave);
                 fetch_v(vp + (k0 + BN) * v_bytes, nk - k0 - BN, other + kTileBytes, wave);
             }
             if (k0 < most) {
                 const bool edge = k0 + BN > least;
+                const int seen = limit - k0 - 4 * h;
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t) {
                     f32x16 s = zeros16(), dp = zeros16();
 #pragma unroll
-                    for (int ks = 0; ks < kSteps; ++ks) s = mma<D>(row_frag<D, DP>(buf, 32 * t, ks, lane), qf[ks], s);
+                    for (int ks = 0; ks < kSteps; ++ks) s = mma<D>(read.rows(buf, 32 * t, ks), qf[ks], s);
 #pragma unroll
-                    for (int ks = 0; ks < kSteps; ++ks) dp = mma<D>(row_frag<D, DP>(buf + kTileBytes, 32 * t, ks, lane), gf[ks], dp);
+                    for (int ks = 0; ks < kSteps; ++ks) dp = mma<D>(read.rows(buf + kTileBytes, 32 * t, ks), gf[ks], dp);
                     if (edge)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = k0 + 32 * t + 8 * (i >> 2) + 4 * h + (i & 3) < limit ? s[i] : -INFINITY;
+                        for (int i = 0; i < 16; ++i) s[i] = 32 * t + 8 * (i >> 2) + (i & 3) < seen ? s[i] : -INFINITY;
                     if constexpr (DROP) drop_keys(dp, k0 + 32 * t, qi, b * a.heads + head, a.drop, h);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
@@ -147,12 +148,15 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
                     for (int x = 0; x < 2; ++x) {
                         const Frag<D> ds = to_frag<D>(s, x);
 #pragma unroll
-                        for (int c = 0; c < kCols; ++c) dq[c] = mma<D>(column_frag<D, DP>(buf, 32 * t + 16 * x, c, lane), ds, dq[c]);
+                        for (int c = 0; c < kCols; ++c) dq[c] = mma<D>(read.columns(buf, 32 * t + 16 * x, c), ds, dq[c]);
                     }
                 }
             }
-            buf = other;
             __syncthreads();
+        };
+        for (int k0 = 0; k0 < end; k0 += 2 * BN) {
+            step(Const<0>{}, k0);
+            if (k0 + BN < end) step(Const<1>{}, k0 + BN);
         }
     }
     if (qi >= a.q_len) return;
@@ -197,23 +201,16 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
     const int all_from = a.causal ? first + 31 - ahead : 0;                               // from here on every key of the wave is seen
     const int my_from = a.causal ? key - ahead : 0;
 
-    const uint32_t values = lds + 2 * kBufBytes + 512;                                    // V of the workgroup's keys
-    Frag<D> kf[kSteps], vf[kValuesInLds ? 1 : kSteps];
+    const uint32_t values = lds + 2 * kBufBytes + 512 + wave * (DP * 64) + lane * 16;     // V of the wave's keys, a lane's own operands
+    Frag<D> kf[kSteps], vf[kSteps];
     {
         const uint8_t* p = counts ? at<D>(a.k, b, key, kv_head) : nullptr;
         const uint8_t* v = counts ? at<D>(a.v, b, key, kv_head) : nullptr;
 #pragma unroll
         for (int ks = 0; ks < kSteps; ++ks) {
             kf[ks] = global_frag<D>(p, ks, a.head_dim, lane);
-            if constexpr (!kValuesInLds) vf[ks] = global_frag<D>(v, ks, a.head_dim, lane);
-        }
-    }
-    if constexpr (kValuesInLds) {
-        if (begin < end) {
-            const int64_t v_bytes = a.v.position * D::size;
-            Fetch<D, DP, kKeysBackward, NT> fetch_v;
-            fetch_v.setup((uint32_t)v_bytes, a.head_dim, wave, lane);
-            fetch_v(at<D>(a.v, b, key_tile * kKeysBackward, kv_head), nk - key_tile * kKeysBackward, values, wave);
+            vf[ks] = global_frag<D>(v, ks, a.head_dim, lane);
+            if constexpr (kValuesInLds) lds_write16(values + ks * 1024, vf[ks].w);
         }
     }
     const float factor = score_factor<D>(a), keep = (DROP ? a.drop.scale : 1.0f) * factor, c2 = a.scale_log2;
@@ -249,30 +246,31 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
         load(q_head, q0, lds);
         store(lds);
         __syncthreads();
-        uint32_t buf = lds;
-        while (q_head < past) {
+        const Reader<D, DP> read(lane);
+        const auto step = [&](auto which) {
+            const uint32_t buf = lds + which * kBufBytes, other = lds + (1 - which) * kBufBytes;
             int next_head = q_head, next_q0 = q0 + BQ;
             if (next_q0 >= end) { next_q0 = begin; ++next_head; }
             const bool more = next_head < past;
-            const uint32_t other = buf == lds ? lds + kBufBytes : lds;
             if (more) load(next_head, next_q0, other);
             if (q0 + BQ > from && first < nk) {
                 const bool edge = q0 < all_from;
+                const int hidden = my_from - q0 - 4 * h;
 #pragma unroll 1
                 for (int t = 0; t < kTiles; ++t) {
                     f32x16 s = zeros16(), dp = zeros16();
 #pragma unroll
-                    for (int ks = 0; ks < kSteps; ++ks) s = mma<D>(row_frag<D, DP>(buf, 32 * t, ks, lane), kf[ks], s);
+                    for (int ks = 0; ks < kSteps; ++ks) s = mma<D>(read.rows(buf, 32 * t, ks), kf[ks], s);
 #pragma unroll
                     for (int ks = 0; ks < kSteps; ++ks) {
                         Frag<D> v;
-                        if constexpr (kValuesInLds) v = row_frag<D, DP>(values, 32 * wave, ks, lane);
+                        if constexpr (kValuesInLds) v.w = lds_read16(values + ks * 1024);
                         else v = vf[ks];
-                        dp = mma<D>(row_frag<D, DP>(buf + kTileBytes, 32 * t, ks, lane), v, dp);
+                        dp = mma<D>(read.rows(buf + kTileBytes, 32 * t, ks), v, dp);
                     }
                     if (edge)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = q0 + 32 * t + 8 * (i >> 2) + 4 * h + (i & 3) >= my_from ? s[i] : -INFINITY;
+                        for (int i = 0; i < 16; ++i) s[i] = 32 * t + 8 * (i >> 2) + (i & 3) >= hidden ? s[i] : -INFINITY;
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
                         const f32x4 L = lds_read16f(buf + 2 * kTileBytes + (32 * t + 8 * g + 4 * h) * 4);
@@ -315,16 +313,19 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
                         const Frag<D> p = to_frag<D>(pd, x), ds = to_frag<D>(s, x);
 #pragma unroll
                         for (int c = 0; c < kCols; ++c) {
-                            dv[c] = mma<D>(column_frag<D, DP>(buf + kTileBytes, 32 * t + 16 * x, c, lane), p, dv[c]);
-                            dk[c] = mma<D>(column_frag<D, DP>(buf, 32 * t + 16 * x, c, lane), ds, dk[c]);
+                            dv[c] = mma<D>(read.columns(buf + kTileBytes, 32 * t + 16 * x, c), p, dv[c]);
+                            dk[c] = mma<D>(read.columns(buf, 32 * t + 16 * x, c), ds, dk[c]);
                         }
                     }
                 }
             }
-            buf = other;
-            if (more) store(buf);
+            if (more) store(other);
             __syncthreads();
             q_head = next_head; q0 = next_q0;
+        };
+        while (q_head < past) {
+            step(Const<0>{});
+            if (q_head < past) step(Const<1>{});
         }
     }
     if (key >= a.k_len) return;

@@ -94,13 +94,14 @@ __global__ __launch_bounds__(256, 2) void k_attention_forward(const AttentionArg
     fetch_k.setup((uint32_t)k_bytes, a.head_dim, wave, lane);
     fetch_v.setup((uint32_t)v_bytes, a.head_dim, wave, lane);
     const bool any = begin < end && (a.packed || row_tile * kRowsForward < nq);
+    const Reader<D, DP> read(lane);
+    const bool all_count = __all(counts);
     if (any) {
         fetch_k(kp + begin * k_bytes, nk - begin, lds, wave);
         fetch_v(vp + begin * v_bytes, nk - begin, lds + kTileBytes, wave);
         __syncthreads();
-        uint32_t buf = lds;
-        for (int k0 = begin; k0 < end; k0 += BN) {
-            const uint32_t other = buf == lds ? lds + 2 * kTileBytes : lds;
+        const auto step = [&](auto which, int k0) {                                       // which of the two buffers is a constant: so are all addresses but the lane's
+            const uint32_t buf = lds + which * 2 * kTileBytes, other = lds + (1 - which) * 2 * kTileBytes;
             if (k0 + BN < end) {
                 fetch_k(kp + (k0 + BN) * k_bytes, nk - k0 - BN, other, wave);
                 fetch_v(vp + (k0 + BN) * v_bytes, nk - k0 - BN, other + kTileBytes, wave);
@@ -111,13 +112,14 @@ __global__ __launch_bounds__(256, 2) void k_attention_forward(const AttentionArg
                 for (int t = 0; t < kTiles; ++t) {
                     s[t] = zeros16();
 #pragma unroll
-                    for (int ks = 0; ks < kSteps; ++ks) s[t] = mma<D>(row_frag<D, DP>(buf, 32 * t, ks, lane), qf[ks], s[t]);
+                    for (int ks = 0; ks < kSteps; ++ks) s[t] = mma<D>(read.rows(buf, 32 * t, ks), qf[ks], s[t]);
                 }
-                if (k0 + BN > least || k0 + BN > nk || !__all(counts)) {
+                if (k0 + BN > least || !all_count) {
+                    const int seen = limit - k0 - 4 * h;
 #pragma unroll
                     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[t][i] = k0 + 32 * t + 8 * (i >> 2) + 4 * h + (i & 3) < limit ? s[t][i] : -INFINITY;
+                        for (int i = 0; i < 16; ++i) s[t][i] = 32 * t + 8 * (i >> 2) + (i & 3) < seen ? s[t][i] : -INFINITY;
                 }
                 float top = s[0][0];
 #pragma unroll
@@ -148,12 +150,15 @@ __global__ __launch_bounds__(256, 2) void k_attention_forward(const AttentionArg
                     for (int x = 0; x < 2; ++x) {
                         const Frag<D> p = to_frag<D>(s[t], x);
 #pragma unroll
-                        for (int c = 0; c < kCols; ++c) o[c] = mma<D>(column_frag<D, DP>(buf + kTileBytes, 32 * t + 16 * x, c, lane), p, o[c]);
+                        for (int c = 0; c < kCols; ++c) o[c] = mma<D>(read.columns(buf + kTileBytes, 32 * t + 16 * x, c), p, o[c]);
                     }
                 }
             }
-            buf = other;
             __syncthreads();
+        };
+        for (int k0 = begin; k0 < end; k0 += 2 * BN) {
+            step(Const<0>{}, k0);
+            if (k0 + BN < end) step(Const<1>{}, k0 + BN);
         }
     }
     l = halves_sum(l);
