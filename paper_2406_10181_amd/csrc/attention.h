@@ -111,31 +111,44 @@ __device__ __forceinline__ float halves_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// A tile in LDS: rows of DP elements (head_dim, filled up with zeros to a multiple of 32) in units of 16 bytes, the units of eight rows together:
-// unit u of the rows 8 g .. 8 g + 7 makes a slab of 128 bytes.  Slabs of odd g change places in pairs, and rows 0..3 and 4..7 of a slab where bit 1 of u is
-// set, so that neither way of reading meets a bank twice: 16 lanes that read one unit of 16 rows (Reader::rows) hit 16 different groups of four banks, and so do
-// the 32 lanes that read four consecutive units of four rows (Reader::columns).  All that a lane adds to its own address for another row group, step or
-// column is then a constant of the instruction, and loads of whole 128-byte lines fill consecutive LDS.
+// A tile in LDS: rows of DP elements (head_dim, filled up with zeros to a multiple of 32) in units of 16 bytes, four of them (64 bytes of a row) side by side, and
+// the same four of four rows: slabs of 256 bytes.  Within the four the places are exchanged by the number of the row's four (xor), so that neither way of reading
+// meets a bank twice: 16 lanes that read one unit of 16 rows (Reader::rows) hit 16 different groups of four banks, and so do the 32 lanes that read four
+// consecutive units of four rows (Reader::columns).  All that a lane adds to its own address for other rows, steps or columns is then a constant of the
+// instruction.  And the loads that fill it, whose lanes go through LDS in order, find 64 bytes of a row in every four lanes: with rows or pairs of units next to
+// one another instead a load takes a cycle a lane (16 and 30 bytes a cycle and CU instead of 45).
 template <typename D, int DP> struct Tile {
     static constexpr int kUnitElems = 16 / D::size;
     static constexpr int kUnits = DP / kUnitElems;
     static constexpr int kRowBytes = kUnits * 16;
+    static_assert(kUnits % 4 == 0, "whole slabs");
     __device__ static __forceinline__ uint32_t place(uint32_t row, uint32_t unit) {
-        const uint32_t g = row >> 3;
-        return g * (kUnits * 128) + (unit ^ (g & 1u)) * 128u + ((row & 7u) ^ (((unit >> 1) & 1u) << 2)) * 16u;
+        return (row >> 2) * (kUnits * 64) + (unit >> 2) * 256u + (row & 3u) * 64u + ((unit ^ (row >> 2)) & 3u) * 16u;
     }
     // the other way round: which unit of which row is the p-th
     __device__ static __forceinline__ void at_place(uint32_t p, uint32_t& row, uint32_t& unit) {
-        const uint32_t g = p / (8 * kUnits), rest = p % (8 * kUnits);
-        unit = (rest >> 3) ^ (g & 1u);
-        row = 8 * g + ((rest & 7u) ^ (((unit >> 1) & 1u) << 2));
+        const uint32_t fours = (p >> 4) / (kUnits / 4);
+        row = 4 * fours + ((p >> 2) & 3u);
+        unit = 4 * ((p >> 4) % (kUnits / 4)) + ((p ^ fours) & 3u);
     }
 };
 
-__device__ __forceinline__ u32x4 lds_read16(uint32_t at) { return *(const LSP_SHARED_AS u32x4*)(uintptr_t)at; }
-__device__ __forceinline__ f32x4 lds_read16f(uint32_t at) { return *(const LSP_SHARED_AS f32x4*)(uintptr_t)at; }
-__device__ __forceinline__ void lds_write16(uint32_t at, u32x4 x) { *(LSP_SHARED_AS u32x4*)(uintptr_t)at = x; }
-__device__ __forceinline__ float lds_read4f(uint32_t at) { return *(const LSP_SHARED_AS float*)(uintptr_t)at; }
+// LDS by its bytes.  The kernels hand the buffer that is read and the one that is being filled to a step as __restrict pointers: that is how the compiler
+// knows that a read need not wait for the loads on their way into the other.
+typedef LSP_SHARED_AS uint8_t* Lds;
+template <typename V> __device__ __forceinline__ V lds_read(Lds at) { return *(const LSP_SHARED_AS V*)at; }
+template <typename V> __device__ __forceinline__ void lds_write(Lds at, V x) { *(LSP_SHARED_AS V*)at = x; }
+
+// All loads into LDS that this wave has asked for have arrived, and every wave has said so.
+__device__ __forceinline__ void arrived_for_all() {
+    __builtin_amdgcn_s_waitcnt(0x0F70);                               // vmcnt(0)
+    __syncthreads();
+}
+
+// Orders for the scheduler: so many matrix instructions, LDS reads, vector instructions next
+template <int N> __device__ __forceinline__ void then_matrix() { __builtin_amdgcn_sched_group_barrier(0x008, N, 0); }
+template <int N> __device__ __forceinline__ void then_reads() { __builtin_amdgcn_sched_group_barrier(0x100, N, 0); }
+template <int N> __device__ __forceinline__ void then_vector() { __builtin_amdgcn_sched_group_barrier(0x402, N, 0); }
 
 // Where a lane reads in a tile: computed once, the rest are constants.
 template <typename D, int DP> struct Reader {
@@ -156,12 +169,12 @@ template <typename D, int DP> struct Reader {
         }
     }
     // A (or B) operand whose rows (columns) are rows ROW0 + 0..31 of the tile and whose k are its columns 16 ks + 0..15 (lane half h: 8 h + 0..7)
-    __device__ __forceinline__ Frag<D> rows(uint32_t tile, int row0, int ks) const {
+    __device__ __forceinline__ Frag<D> rows(Lds tile, int row0, int ks) const {
         Frag<D> f;
-        const uint32_t t = tile + row0 / 8 * (T::kUnits * 128);
-        if constexpr (D::size == 2) f.w = lds_read16(row_at[ks & 1] + t + (ks >> 1) * 512);
+        const Lds t = tile + row0 / 4 * (T::kUnits * 64);
+        if constexpr (D::size == 2) f.w = lds_read<u32x4>(t + row_at[ks & 1] + (ks >> 1) * 256);
         else {
-            const f32x4 a = lds_read16f(row_at[0] + t + ks * 512), b = lds_read16f(row_at[1] + t + ks * 512);
+            const f32x4 a = lds_read<f32x4>(t + row_at[0] + ks * 256), b = lds_read<f32x4>(t + row_at[1] + ks * 256);
 #pragma unroll
             for (int j = 0; j < 4; ++j) { f.w[j] = a[j]; f.w[4 + j] = b[j]; }
         }
@@ -169,20 +182,20 @@ template <typename D, int DP> struct Reader {
     }
     // A operand whose rows are columns 32 ct + 0..31 of the tile and whose k are its rows ROW0 + 0..15, in the order that the accumulators have
     // them.  In 16 bits the transposing read does it: 16 lanes hold four rows of 16 columns, four columns each, and each gets one column of the four rows.
-    __device__ __forceinline__ Frag<D> columns(uint32_t tile, int row0, int ct) const {
+    __device__ __forceinline__ Frag<D> columns(Lds tile, int row0, int ct) const {
         Frag<D> f;
-        const uint32_t t = tile + row0 / 8 * (T::kUnits * 128);
+        const Lds t = tile + row0 / 4 * (T::kUnits * 64);
         if constexpr (D::size == 2) {
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LSP_SHARED_AS s16x4*)(uintptr_t)(column_at[x] + t + ct * 512));
+                const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LSP_SHARED_AS s16x4*)(t + column_at[x] + ct * 256));
                 u32x2 u;
                 __builtin_memcpy(&u, &v, 8);
                 f.w[2 * x] = u[0]; f.w[2 * x + 1] = u[1];
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f.w[j] = lds_read4f(column_at[j >> 2] + t + ct * 1024 + (j & 3) * 16);
+            for (int j = 0; j < 8; ++j) f.w[j] = lds_read<float>(t + column_at[j >> 2] + ct * 512 + (j & 3) * 64);
         }
         return f;
     }
@@ -215,13 +228,13 @@ template <typename D, int DP, int ROWS, int NT> struct Fetch {
             off[i] = (int)unit * T::kUnitElems < head_dim ? r * row_bytes + unit * 16u : 0x80000000u;
         }
     }
-    __device__ __forceinline__ void operator()(const void* first_row, int left, uint32_t tile, int wave) const {
+    __device__ __forceinline__ void operator()(const void* first_row, int left, Lds tile, int wave) const {
         const Buffer b = buffer_from(first_row);
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
             if (kLoads % kWaves && i * kWaves + wave >= kLoads) break;
             const uint32_t o = row[i] < left ? off[i] : 0x80000000u;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (LSP_SHARED_AS void*)(uintptr_t)(tile + (i * kWaves + wave) * 1024u), 16, (int)o, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (LSP_SHARED_AS void*)(tile + (i * kWaves + wave) * 1024u), 16, (int)o, 0, 0, 0);
         }
     }
 };
@@ -252,8 +265,6 @@ template <typename D> __device__ __forceinline__ void store_four(uint8_t* p, flo
 }
 
 __device__ __forceinline__ int valid_length(const int32_t* lens, int b, int most) { return lens ? min(max(lens[b], 0), most) : most; }
-
-template <int I> using Const = std::integral_constant<int, I>;
 
 // Work item of a workgroup.  Workgroups go round the eight XCDs, each with an L2 of its own: a run of consecutive items is given to each XCD, so
 // that the workgroups that read the same keys share an L2.

@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
     constexpr int BN = tile_rows<D>(), NT = 256, kSteps = DP / 16, kTiles = BN / 32, kCols = DP / 32;
     constexpr uint32_t kTileBytes = BN * T::kRowBytes;
     extern __shared__ __align__(16) uint8_t smem[];
-    const uint32_t lds = (uint32_t)(uintptr_t)(LSP_SHARED_AS uint8_t*)smem;               // K | V, twice
+    const Lds lds = (Lds)smem;                                                            // K | V, twice
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int tiles = (a.q_len + kRowsForward - 1) / kRowsForward;
     uint32_t item = item_of_block(blockIdx.x, (uint32_t)a.batch * a.heads * tiles);
@@ -117,10 +117,9 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
     if (end > 0) {
         fetch_k(kp, nk, lds, wave);
         fetch_v(vp, nk, lds + kTileBytes, wave);
-        __syncthreads();
+        arrived_for_all();
         const Reader<D, DP> read(lane);
-        const auto step = [&](auto which, int k0) {
-            const uint32_t buf = lds + which * 2 * kTileBytes, other = lds + (1 - which) * 2 * kTileBytes;
+        const auto step = [&](Lds __restrict buf, Lds __restrict other, int k0) {
             if (k0 + BN < end) {
                 fetch_k(kp + (k0 + BN) * k_bytes, nk - k0 - BN, other, wave);
                 fetch_v(vp + (k0 + BN) * v_bytes, nk - k0 - BN, other + kTileBytes, wave);
@@ -138,7 +137,10 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
                     if (edge)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) s[i] = 32 * t + 8 * (i >> 2) + (i & 3) < seen ? s[i] : -INFINITY;
-                    if constexpr (DROP) drop_keys(dp, k0 + 32 * t, qi, b * a.heads + head, a.drop, h);
+                    if constexpr (DROP) {
+                        drop_keys(dp, 0, k0 + 32 * t, qi, b * a.heads + head, a.drop, h);
+                        drop_keys(dp, 1, k0 + 32 * t, qi, b * a.heads + head, a.drop, h);
+                    }
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const float p = __builtin_amdgcn_exp2f(fmaf(s[i], c2, shift));
@@ -152,11 +154,11 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
                     }
                 }
             }
-            __syncthreads();
+            arrived_for_all();
         };
         for (int k0 = 0; k0 < end; k0 += 2 * BN) {
-            step(Const<0>{}, k0);
-            if (k0 + BN < end) step(Const<1>{}, k0 + BN);
+            step(lds, lds + 2 * kTileBytes, k0);
+            if (k0 + BN < end) step(lds + 2 * kTileBytes, lds, k0 + BN);
         }
     }
     if (qi >= a.q_len) return;
@@ -183,7 +185,7 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
     constexpr int BQ = queries_at_once<D, DP>(), NT = 256, kSteps = DP / 16, kTiles = BQ / 32, kCols = DP / 32;
     constexpr uint32_t kTileBytes = BQ * T::kRowBytes, kBufBytes = 2 * kTileBytes + BQ * 8;
     extern __shared__ __align__(16) uint8_t smem[];
-    const uint32_t lds = (uint32_t)(uintptr_t)(LSP_SHARED_AS uint8_t*)smem;               // Q | dO | L | delta, twice; bits of kept ones of each wave
+    const Lds lds = (Lds)smem;                                                            // Q | dO | L | delta, twice; bits of kept ones of each wave
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int tiles = (a.k_len + kKeysBackward - 1) / kKeysBackward;
     uint32_t item = item_of_block(blockIdx.x, (uint32_t)a.batch * a.kv_heads * tiles);
@@ -201,7 +203,7 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
     const int all_from = a.causal ? first + 31 - ahead : 0;                               // from here on every key of the wave is seen
     const int my_from = a.causal ? key - ahead : 0;
 
-    const uint32_t values = lds + 2 * kBufBytes + 512 + wave * (DP * 64) + lane * 16;     // V of the wave's keys, a lane's own operands
+    const Lds values = lds + 2 * kBufBytes + 512 + wave * (DP * 64) + lane * 16;     // V of the wave's keys, a lane's own operands
     Frag<D> kf[kSteps], vf[kSteps];
     {
         const uint8_t* p = counts ? at<D>(a.k, b, key, kv_head) : nullptr;
@@ -210,7 +212,7 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
         for (int ks = 0; ks < kSteps; ++ks) {
             kf[ks] = global_frag<D>(p, ks, a.head_dim, lane);
             vf[ks] = global_frag<D>(v, ks, a.head_dim, lane);
-            if constexpr (kValuesInLds) lds_write16(values + ks * 1024, vf[ks].w);
+            if constexpr (kValuesInLds) lds_write<u32x4>(values + ks * 1024, vf[ks].w);
         }
     }
     const float factor = score_factor<D>(a), keep = (DROP ? a.drop.scale : 1.0f) * factor, c2 = a.scale_log2;
@@ -223,7 +225,7 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
     fetch_q.setup((uint32_t)q_bytes, a.head_dim, wave, lane);
     fetch_g.setup((uint32_t)g_bytes, a.head_dim, wave, lane);
     float stat[2];                                                                        // threads below BQ: -L log2(e) and delta of a row
-    const auto load = [&](int q_head, int q0, uint32_t buf) {
+    const auto load = [&](int q_head, int q0, Lds buf) {
         fetch_q(at<D>(a.q, b, q0, q_head), nq - q0, buf, wave);
         fetch_g(at<D>(a.d_o, b, q0, q_head), nq - q0, buf + kTileBytes, wave);
         if (tid < BQ) {
@@ -234,10 +236,10 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
             stat[1] = L == -INFINITY ? 0.0f : a.delta[line] * factor;
         }
     };
-    const auto store = [&](uint32_t buf) {
+    const auto store = [&](Lds buf) {
         if (tid < BQ) {
-            *(LSP_SHARED_AS float*)(uintptr_t)(buf + 2 * kTileBytes + tid * 4) = stat[0];
-            *(LSP_SHARED_AS float*)(uintptr_t)(buf + 2 * kTileBytes + BQ * 4 + tid * 4) = stat[1];
+            lds_write<float>(buf + 2 * kTileBytes + tid * 4, stat[0]);
+            lds_write<float>(buf + 2 * kTileBytes + BQ * 4 + tid * 4, stat[1]);
         }
     };
     if (begin < end) {
@@ -245,10 +247,9 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
         const int past = (kv_head + 1) * a.group;
         load(q_head, q0, lds);
         store(lds);
-        __syncthreads();
+        arrived_for_all();
         const Reader<D, DP> read(lane);
-        const auto step = [&](auto which) {
-            const uint32_t buf = lds + which * kBufBytes, other = lds + (1 - which) * kBufBytes;
+        const auto step = [&](Lds __restrict buf, Lds __restrict other) {
             int next_head = q_head, next_q0 = q0 + BQ;
             if (next_q0 >= end) { next_q0 = begin; ++next_head; }
             const bool more = next_head < past;
@@ -264,7 +265,7 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
 #pragma unroll
                     for (int ks = 0; ks < kSteps; ++ks) {
                         Frag<D> v;
-                        if constexpr (kValuesInLds) v.w = lds_read16(values + ks * 1024);
+                        if constexpr (kValuesInLds) v.w = lds_read<u32x4>(values + ks * 1024);
                         else v = vf[ks];
                         dp = mma<D>(read.rows(buf + kTileBytes, 32 * t, ks), v, dp);
                     }
@@ -273,14 +274,14 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
                         for (int i = 0; i < 16; ++i) s[i] = 32 * t + 8 * (i >> 2) + (i & 3) >= hidden ? s[i] : -INFINITY;
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        const f32x4 L = lds_read16f(buf + 2 * kTileBytes + (32 * t + 8 * g + 4 * h) * 4);
+                        const f32x4 L = lds_read<f32x4>(buf + 2 * kTileBytes + (32 * t + 8 * g + 4 * h) * 4);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) s[4 * g + j] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + j], c2, L[j]));
                     }
                     f32x16 pd = s;
                     if constexpr (DROP) {
                         // eight lanes share a block of eight keys: of the 16 queries that they all have, each lane makes two; the bits go round by LDS
-                        const uint32_t bits = lds + 2 * kBufBytes + wave * 128 + (lane >> 3) * 16;
+                        const Lds bits = lds + 2 * kBufBytes + wave * 128 + (lane >> 3) * 16;
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
                             const int x = (lane & 7) + 8 * half;
@@ -288,12 +289,12 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
                             uint32_t kept = 0;
 #pragma unroll
                             for (int e = 0; e < 8; ++e) kept |= (philox_word(w, e) < a.drop.limit ? 0u : 1u) << e;
-                            *(LSP_SHARED_AS uint8_t*)(uintptr_t)(bits + x) = (uint8_t)kept;
+                            lds_write<uint8_t>(bits + x, (uint8_t)kept);
                         }
                         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
                         __builtin_amdgcn_wave_barrier();
                         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-                        const u32x4 all = lds_read16(bits);
+                        const u32x4 all = lds_read<u32x4>(bits);
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const bool kept = (all[i >> 2] >> (8 * (i & 3) + (lane & 7))) & 1u;
@@ -304,7 +305,7 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
                     }
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        const f32x4 delta = lds_read16f(buf + 2 * kTileBytes + BQ * 4 + (32 * t + 8 * g + 4 * h) * 4);
+                        const f32x4 delta = lds_read<f32x4>(buf + 2 * kTileBytes + BQ * 4 + (32 * t + 8 * g + 4 * h) * 4);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) s[4 * g + j] *= fmaf(dp[4 * g + j], keep, -delta[j]);
                     }
@@ -320,12 +321,12 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
                 }
             }
             if (more) store(other);
-            __syncthreads();
+            arrived_for_all();
             q_head = next_head; q0 = next_q0;
         };
         while (q_head < past) {
-            step(Const<0>{});
-            if (q_head < past) step(Const<1>{});
+            step(lds, lds + kBufBytes);
+            if (q_head < past) step(lds + kBufBytes, lds);
         }
     }
     if (key >= a.k_len) return;

@@ -14,11 +14,10 @@
 #if defined(__HIPCC__)
 namespace lsp {
 
-// Drops probabilities: registers i of `s` are keys key0 + 8 (i / 4) + 4 h + i % 4 of query q.  A block of eight keys belongs to two lanes (h = 0, 1), four words
-// each: of two blocks each lane makes one, and they swap the halves.
-__device__ __forceinline__ void drop_keys(f32x16& s, uint32_t key0, uint32_t q, uint32_t head, const Dropout& drop, int h) {
-#pragma unroll
-    for (int pair = 0; pair < 2; ++pair) {
+// Drops probabilities: registers i of `s` are keys key0 + 8 (i / 4) + 4 h + i % 4 of query q; those of `pair`, 8 of the 16.  A block of eight keys belongs to two
+// lanes (h = 0, 1), four words each: of two blocks each lane makes one, and they swap the halves.
+__device__ __forceinline__ void drop_keys(f32x16& s, int pair, uint32_t key0, uint32_t q, uint32_t head, const Dropout& drop, int h) {
+    {
         const u32x4 w = philox((key0 >> 3) + 2 * pair + h, q, head, drop.offset, drop.key0, drop.key1);
         const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
         const auto b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
@@ -35,12 +34,12 @@ __device__ __forceinline__ void drop_keys(f32x16& s, uint32_t key0, uint32_t q, 
 }
 
 template <typename D, int DP, bool DROP>
-__global__ __launch_bounds__(256, 2) void k_attention_forward(const AttentionArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_attention_forward(const AttentionArgs a) {
     using T = Tile<D, DP>;
     constexpr int BN = tile_rows<D>(), NT = 256, kSteps = DP / 16, kTiles = BN / 32, kCols = DP / 32;
     constexpr uint32_t kTileBytes = BN * T::kRowBytes;
     extern __shared__ __align__(16) uint8_t smem[];
-    const uint32_t lds = (uint32_t)(uintptr_t)(LSP_SHARED_AS uint8_t*)smem;               // K | V, twice
+    const Lds lds = (Lds)smem;                                                            // K | V, twice
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     // which rows, of which head, and which part of the keys
     const uint32_t heads = a.packed ? a.kv_heads : a.heads, items = a.batch * heads * a.tiles * a.splits;
@@ -99,9 +98,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_forward(const AttentionArg
     if (any) {
         fetch_k(kp + begin * k_bytes, nk - begin, lds, wave);
         fetch_v(vp + begin * v_bytes, nk - begin, lds + kTileBytes, wave);
-        __syncthreads();
-        const auto step = [&](auto which, int k0) {                                       // which of the two buffers is a constant: so are all addresses but the lane's
-            const uint32_t buf = lds + which * 2 * kTileBytes, other = lds + (1 - which) * 2 * kTileBytes;
+        arrived_for_all();
+        const auto step = [&](Lds __restrict buf, Lds __restrict other, int k0) {
             if (k0 + BN < end) {
                 fetch_k(kp + (k0 + BN) * k_bytes, nk - k0 - BN, other, wave);
                 fetch_v(vp + (k0 + BN) * v_bytes, nk - k0 - BN, other + kTileBytes, wave);
@@ -113,6 +111,15 @@ __global__ __launch_bounds__(256, 2) void k_attention_forward(const AttentionArg
                     s[t] = zeros16();
 #pragma unroll
                     for (int ks = 0; ks < kSteps; ++ks) s[t] = mma<D>(read.rows(buf, 32 * t, ks), qf[ks], s[t]);
+                }
+                Frag<D> vf[2][kCols];
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) vf[0][c] = read.columns(buf + kTileBytes, 0, c);
+                if constexpr (D::size == 2) {                                             // reads stay six ahead of their products
+                    then_reads<6>();
+#pragma unroll
+                    for (int i = 0; i < kTiles * kSteps - 6; ++i) { then_matrix<1>(); then_reads<1>(); }
+                    then_matrix<6>();
                 }
                 if (k0 + BN > least || !all_count) {
                     const int seen = limit - k0 - 4 * h;
@@ -138,27 +145,48 @@ __global__ __launch_bounds__(256, 2) void k_attention_forward(const AttentionArg
                         for (int i = 0; i < 16; ++i) o[c][i] *= keep;
                 }
                 const float shift = m == -INFINITY ? 0.0f : -m * c2;
+                const auto probabilities = [&](int x) {                                   // of keys 16 x .. 16 x + 15
+                    f32x16& w = s[x >> 1];
+                    float sum = 0.0f;
 #pragma unroll
-                for (int t = 0; t < kTiles; ++t) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], c2, shift));
-                        l += s[t][i];
+                    for (int j = 0; j < 8; ++j) {
+                        const int i = 8 * (x & 1) + j;
+                        w[i] = __builtin_amdgcn_exp2f(fmaf(w[i], c2, shift));
+                        sum += w[i];
                     }
-                    if constexpr (DROP) drop_keys(s[t], k0 + 32 * t, qi, b * a.heads + q_head, a.drop, h);
+                    l += sum;
+                    if constexpr (DROP) drop_keys(w, x & 1, k0 + 32 * (x >> 1), qi, b * a.heads + q_head, a.drop, h);
+                    return to_frag<D>(w, x & 1);
+                };
+                // the values of the next 16 keys are read, and their exponentials made, under the products of these
+                Frag<D> p = probabilities(0);
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const Frag<D> p = to_frag<D>(s[t], x);
+                for (int x = 0; x < kTiles * 2; ++x) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    Frag<D> next_p;
+                    if (x + 1 < kTiles * 2) {
 #pragma unroll
-                        for (int c = 0; c < kCols; ++c) o[c] = mma<D>(read.columns(buf + kTileBytes, 32 * t + 16 * x, c), p, o[c]);
+                        for (int c = 0; c < kCols; ++c) vf[(x + 1) & 1][c] = read.columns(buf + kTileBytes, 16 * (x + 1), c);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) o[c] = mma<D>(vf[x & 1][c], p, o[c]);
+                    if (x + 1 < kTiles * 2) {
+                        next_p = probabilities(x + 1);
+                        if constexpr (D::size == 2) {
+#pragma unroll
+                            for (int c = 0; c < kCols; ++c) { then_matrix<1>(); then_vector<28 / kCols>(); }
+                        }
+                    }
+                    p = next_p;
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            __syncthreads();
+            arrived_for_all();
         };
-        for (int k0 = begin; k0 < end; k0 += 2 * BN) {
-            step(Const<0>{}, k0);
-            if (k0 + BN < end) step(Const<1>{}, k0 + BN);
+        for (int k0 = begin; k0 < end; k0 += 2 * BN) {                                    // (by turns, so that the buffers are constants of the instructions)
+            step(lds, lds + 2 * kTileBytes, k0);
+            if (k0 + BN < end) step(lds + 2 * kTileBytes, lds, k0 + BN);
         }
     }
     l = halves_sum(l);
