@@ -20,7 +20,7 @@ struct AttentionArgs {
     float*         L;                // [batch][heads][q_len]
     float*         delta;            // [batch][heads][q_len]: dO . O; in the backward pass
     uint32_t*      most;             // fp16 backward: bits of the largest norm of a row of dO and of V (atomic maxima)
-    float*         partial;          // forward with several splits: O of each, then (largest score, sum) of each row
+    float*         partial;          // forward with several splits: O of each, then (largest score, sum) of each row; backward: parts of dK and dV, then of dQ
     const int32_t* q_lens;
     const int32_t* k_lens;
     int32_t batch, heads, kv_heads, group, q_len, k_len, head_dim, causal;
@@ -28,6 +28,7 @@ struct AttentionArgs {
     int32_t rows;                    // rows of a head: q_len, or group * q_len where `packed`
     int32_t packed;                  // rows are (query head of the group, query): few queries, all heads of a key head in one tile
     int32_t splits, split_tiles;     // forward: parts of the keys, tiles of keys in each
+    int32_t key_parts, query_parts;  // backward: workgroups that share 128 keys (parts of their queries), and 128 queries (parts of their keys)
     float   scale, scale_log2;       // scale_log2 = scale * log2(e): probabilities are powers of two
     Dropout drop;
 };
@@ -37,6 +38,8 @@ hipError_t launch_attention_backward(const AttentionArgs& a, lsp_dtype dtype, hi
 // Splits of the keys in the forward pass and what that needs; fills the tiling fields of `a`.
 void plan_attention_forward(AttentionArgs& a, lsp_dtype dtype);
 size_t attention_partial_bytes(const AttentionArgs& a);
+void plan_attention_backward(AttentionArgs& a, lsp_dtype dtype);
+size_t attention_backward_partial_bytes(const AttentionArgs& a);
 
 constexpr int kRowsForward = 128;    // query rows of a workgroup: four waves of 32
 constexpr int kKeysBackward = 128;   // keys of a workgroup of the kernel that makes dK and dV

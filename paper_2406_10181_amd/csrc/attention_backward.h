@@ -56,10 +56,17 @@ __global__ __launch_bounds__(256) void k_attention_delta(const AttentionArgs a, 
     for (int s = 1; s < 16; s <<= 1) { dot += __shfl_xor(dot, s); norm += __shfl_xor(norm, s); }
     if (!values && counts && part == 0) a.delta[row] = dot;
     if constexpr (std::is_same<D, F16>::value) {
-        norm = sqrtf(norm);
+        __shared__ float norms[4];
 #pragma unroll
         for (int s = 16; s < 64; s <<= 1) norm = fmaxf(norm, __shfl_xor(norm, s));
-        if (lane == 0) atomicMax(&a.most[values ? 1 : 0], __float_as_uint(norm));         // (a maximum: the order does not matter)
+        if (lane == 0) norms[threadIdx.x >> 6] = norm;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            // a maximum: the order does not matter, and few are larger than what is there already (a look costs less than an atomic that all wait for)
+            const uint32_t bits = __float_as_uint(sqrtf(fmaxf(fmaxf(norms[0], norms[1]), fmaxf(norms[2], norms[3]))));
+            uint32_t* most = &a.most[values ? 1 : 0];
+            if (bits > __hip_atomic_load(most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(most, bits);
+        }
     }
 }
 
@@ -74,9 +81,11 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
     const Lds lds = (Lds)smem;                                                            // K | V, twice
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int tiles = (a.q_len + kRowsForward - 1) / kRowsForward;
-    uint32_t item = item_of_block(blockIdx.x, (uint32_t)a.batch * a.heads * tiles);
+    uint32_t item = item_of_block(blockIdx.x, (uint32_t)a.batch * a.heads * tiles * a.query_parts);
     const int row_tile = tiles - 1 - (int)(item % tiles);
     item /= tiles;
+    const int part = (int)(item % a.query_parts);
+    item /= a.query_parts;
     const int head = (int)(item % a.heads), b = (int)(item / a.heads), kv_head = head / a.group;
     const int nq = valid_length(a.q_lens, b, a.q_len), nk = valid_length(a.k_lens, b, a.k_len), ahead = nk - nq;
 
@@ -84,7 +93,9 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
     const bool counts = qi < nq;
     const int limit = counts ? (a.causal ? min(nk, qi + ahead + 1) : nk) : 0;
     const int last_row = min(row_tile * kRowsForward + kRowsForward, nq) - 1;
-    const int end = row_tile * kRowsForward >= nq ? 0 : a.causal ? min(nk, last_row + ahead + 1) : nk;
+    const int end_all = row_tile * kRowsForward >= nq ? 0 : max(0, a.causal ? min(nk, last_row + ahead + 1) : nk);
+    const int tiles_k = (end_all + BN - 1) / BN;                                          // of which this part has an equal share
+    const int begin = tiles_k * part / a.query_parts * BN, end = min(end_all, tiles_k * (part + 1) / a.query_parts * BN);
     const int most = first >= nq ? 0 : a.causal ? min(nk, min(first + 31, nq - 1) + ahead + 1) : nk;
     const int least = first + 31 >= nq ? 0 : a.causal ? min(nk, first + ahead + 1) : nk;
 
@@ -114,9 +125,9 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
     Fetch<D, DP, BN, NT> fetch_k, fetch_v;
     fetch_k.setup((uint32_t)k_bytes, a.head_dim, wave, lane);
     fetch_v.setup((uint32_t)v_bytes, a.head_dim, wave, lane);
-    if (end > 0) {
-        fetch_k(kp, nk, lds, wave);
-        fetch_v(vp, nk, lds + kTileBytes, wave);
+    if (begin < end) {
+        fetch_k(kp + begin * k_bytes, nk - begin, lds, wave);
+        fetch_v(vp + begin * v_bytes, nk - begin, lds + kTileBytes, wave);
         arrived_for_all();
         const Reader<D, DP> read(lane);
         const auto step = [&](Lds __restrict buf, Lds __restrict other, int k0) {
@@ -156,21 +167,42 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
             }
             arrived_for_all();
         };
-        for (int k0 = 0; k0 < end; k0 += 2 * BN) {
+        for (int k0 = begin; k0 < end; k0 += 2 * BN) {
             step(lds, lds + 2 * kTileBytes, k0);
             if (k0 + BN < end) step(lds + 2 * kTileBytes, lds, k0 + BN);
         }
     }
     if (qi >= a.q_len) return;
     const float back = a.scale / (factor * kLift<D>);
+    const int64_t lines = (int64_t)a.batch * a.heads * a.q_len, line = ((int64_t)b * a.heads + head) * a.q_len + qi;
+    float* sums = a.partial + (part * lines + line) * a.head_dim;
     uint8_t* out = const_cast<uint8_t*>(at<D>(a.dq, b, qi, head));
 #pragma unroll
     for (int c = 0; c < kCols; ++c)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const int col = 32 * c + 8 * g + 4 * h;
-            if (col < a.head_dim) store_four<D>(out + col * D::size, dq[c][4 * g] * back, dq[c][4 * g + 1] * back, dq[c][4 * g + 2] * back, dq[c][4 * g + 3] * back);
+            const f32x4 v = {dq[c][4 * g] * back, dq[c][4 * g + 1] * back, dq[c][4 * g + 2] * back, dq[c][4 * g + 3] * back};
+            if (col < a.head_dim) {
+                if (a.query_parts > 1) *reinterpret_cast<f32x4*>(sums + col) = v;
+                else store_four<D>(out + col * D::size, v[0], v[1], v[2], v[3]);
+            }
         }
+}
+
+// Adds the parts of a gradient, in order: `lines` rows of (batch, head, position).  A thread has four columns.
+template <typename D>
+__global__ __launch_bounds__(256) void k_attention_add(const float* parts_at, Strided out, int parts, int batch, int heads, int len, int head_dim) {
+    const int64_t lines = (int64_t)batch * heads * len, quads = head_dim / 4;
+    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (n >= lines * quads) return;
+    const int64_t line = n / quads;
+    const int col = (int)(n - line * quads) * 4;
+    f32x4 sum = *reinterpret_cast<const f32x4*>(parts_at + line * head_dim + col);
+    for (int p = 1; p < parts; ++p) sum += *reinterpret_cast<const f32x4*>(parts_at + (p * lines + line) * head_dim + col);
+    const int64_t head_line = line / len;
+    const int i = (int)(line - head_line * len), b = (int)(head_line / heads), head = (int)(head_line - (int64_t)b * heads);
+    store_four<D>(const_cast<uint8_t*>(at<D>(out, b, i, head)) + col * D::size, sum[0], sum[1], sum[2], sum[3]);
 }
 
 // At head_dim 128 in 16 bits K and V of a wave's keys, dK, dV and the scores are more than the 256 registers that two waves a SIMD have: V stays in
@@ -188,9 +220,11 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
     const Lds lds = (Lds)smem;                                                            // Q | dO | L | delta, twice; bits of kept ones of each wave
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int tiles = (a.k_len + kKeysBackward - 1) / kKeysBackward;
-    uint32_t item = item_of_block(blockIdx.x, (uint32_t)a.batch * a.kv_heads * tiles);
+    uint32_t item = item_of_block(blockIdx.x, (uint32_t)a.batch * a.kv_heads * tiles * a.key_parts);
     const int key_tile = (int)(item % tiles);                                             // (causal: the first keys have the most queries)
     item /= tiles;
+    const int part = (int)(item % a.key_parts);
+    item /= a.key_parts;
     const int kv_head = (int)(item % a.kv_heads), b = (int)(item / a.kv_heads);
     const int nq = valid_length(a.q_lens, b, a.q_len), nk = valid_length(a.k_lens, b, a.k_len), ahead = nk - nq;
 
@@ -242,9 +276,12 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
             lds_write<float>(buf + 2 * kTileBytes + BQ * 4 + tid * 4, stat[1]);
         }
     };
-    if (begin < end) {
-        int q_head = kv_head * a.group, q0 = begin;
-        const int past = (kv_head + 1) * a.group;
+    // the steps are (query head of the group, tile of queries); this part has an equal share of them
+    const int tiles_q = begin < end ? (end - begin + BQ - 1) / BQ : 0;
+    const int step_from = (int)((int64_t)tiles_q * a.group * part / a.key_parts), step_past = (int)((int64_t)tiles_q * a.group * (part + 1) / a.key_parts);
+    if (step_from < step_past) {
+        int steps = step_past - step_from;
+        int q_head = kv_head * a.group + step_from / tiles_q, q0 = begin + step_from % tiles_q * BQ;
         load(q_head, q0, lds);
         store(lds);
         arrived_for_all();
@@ -252,7 +289,7 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
         const auto step = [&](Lds __restrict buf, Lds __restrict other) {
             int next_head = q_head, next_q0 = q0 + BQ;
             if (next_q0 >= end) { next_q0 = begin; ++next_head; }
-            const bool more = next_head < past;
+            const bool more = --steps > 0;
             if (more) load(next_head, next_q0, other);
             if (q0 + BQ > from && first < nk) {
                 const bool edge = q0 < all_from;
@@ -324,13 +361,15 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
             arrived_for_all();
             q_head = next_head; q0 = next_q0;
         };
-        while (q_head < past) {
+        while (steps > 0) {
             step(lds, lds + kBufBytes);
-            if (q_head < past) step(lds + kBufBytes, lds);
+            if (steps > 0) step(lds + kBufBytes, lds);
         }
     }
     if (key >= a.k_len) return;
     const float back_v = counts ? (DROP ? a.drop.scale : 1.0f) / kLift<D> : 0.0f, back_k = counts ? a.scale / (factor * kLift<D>) : 0.0f;
+    const int64_t lines = (int64_t)a.batch * a.kv_heads * a.k_len, line = ((int64_t)b * a.kv_heads + kv_head) * a.k_len + key;
+    float* sums = a.partial + (part * lines + line) * a.head_dim;                         // of dK; those of dV follow
     uint8_t* out_k = const_cast<uint8_t*>(at<D>(a.dk, b, key, kv_head));
     uint8_t* out_v = const_cast<uint8_t*>(at<D>(a.dv, b, key, kv_head));
 #pragma unroll
@@ -338,11 +377,17 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const int col = 32 * c + 8 * g + 4 * h;
+            f32x4 k, v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { k[j] = counts ? dk[c][4 * g + j] * back_k : 0.0f; v[j] = counts ? dv[c][4 * g + j] * back_v : 0.0f; }
             if (col < a.head_dim) {
-                store_four<D>(out_k + col * D::size, counts ? dk[c][4 * g] * back_k : 0.0f, counts ? dk[c][4 * g + 1] * back_k : 0.0f,
-                              counts ? dk[c][4 * g + 2] * back_k : 0.0f, counts ? dk[c][4 * g + 3] * back_k : 0.0f);
-                store_four<D>(out_v + col * D::size, counts ? dv[c][4 * g] * back_v : 0.0f, counts ? dv[c][4 * g + 1] * back_v : 0.0f,
-                              counts ? dv[c][4 * g + 2] * back_v : 0.0f, counts ? dv[c][4 * g + 3] * back_v : 0.0f);
+                if (a.key_parts > 1) {
+                    *reinterpret_cast<f32x4*>(sums + col) = k;
+                    *reinterpret_cast<f32x4*>(sums + a.key_parts * lines * a.head_dim + col) = v;
+                } else {
+                    store_four<D>(out_k + col * D::size, k[0], k[1], k[2], k[3]);
+                    store_four<D>(out_v + col * D::size, v[0], v[1], v[2], v[3]);
+                }
             }
         }
 }
@@ -364,12 +409,22 @@ template <typename D, int DP, bool DROP> static hipError_t run_attention_backwar
     }
     hipLaunchKernelGGL(k_attention_delta<D>, dim3((unsigned)((o_rows + v_rows + 15) / 16)), dim3(256), 0, st, a, o_rows, v_rows);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    const int64_t key_items = (int64_t)a.batch * a.kv_heads * ((a.k_len + kKeysBackward - 1) / kKeysBackward);
+    const auto add = [&](const float* from, const Strided& out, int parts, int heads, int len) {
+        const int64_t threads = (int64_t)a.batch * heads * len * (a.head_dim / 4);
+        hipLaunchKernelGGL(k_attention_add<D>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, from, out, parts, a.batch, heads, len, a.head_dim);
+        return hipGetLastError();
+    };
+    const int64_t key_items = (int64_t)a.batch * a.kv_heads * ((a.k_len + kKeysBackward - 1) / kKeysBackward) * a.key_parts;
     hipLaunchKernelGGL(dkv, dim3((unsigned)key_items), dim3(256), lds_dkv, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    const int64_t query_items = (int64_t)a.batch * a.heads * ((a.q_len + kRowsForward - 1) / kRowsForward);
+    if (a.key_parts > 1) {
+        if ((e = add(a.partial, a.dk, a.key_parts, a.kv_heads, a.k_len)) != hipSuccess) return e;
+        if ((e = add(a.partial + (int64_t)a.key_parts * a.batch * a.kv_heads * a.k_len * a.head_dim, a.dv, a.key_parts, a.kv_heads, a.k_len)) != hipSuccess) return e;
+    }
+    const int64_t query_items = (int64_t)a.batch * a.heads * ((a.q_len + kRowsForward - 1) / kRowsForward) * a.query_parts;
     hipLaunchKernelGGL(dq, dim3((unsigned)query_items), dim3(256), lds_dq, st, a);
-    return hipGetLastError();
+    if ((e = hipGetLastError()) != hipSuccess || a.query_parts == 1) return e;
+    return add(a.partial, a.dq, a.query_parts, a.heads, a.q_len);
 }
 
 template <typename D> hipError_t attention_backward_of(const AttentionArgs& a, hipStream_t st) {

@@ -37,6 +37,23 @@ void plan_attention_forward(AttentionArgs& a, lsp_dtype dtype) {
     a.splits = (key_tiles + a.split_tiles - 1) / a.split_tiles;
 }
 
+// Workgroups of the backward kernels that share a tile: as many as give each CU two, with four steps or more each.  What they add up goes through memory in
+// fp32, two more passes over the gradient a part.
+static int parts_for(int64_t tiles, int64_t steps) {
+    return (int)std::min<int64_t>({std::max<int64_t>(512 / tiles, 1), std::max<int64_t>(steps / 4, 1), 16});
+}
+void plan_attention_backward(AttentionArgs& a, lsp_dtype dtype) {
+    const int64_t key_tiles = (int64_t)a.batch * a.kv_heads * ((a.k_len + kKeysBackward - 1) / kKeysBackward);
+    const int64_t query_tiles = (int64_t)a.batch * a.heads * ((a.q_len + kRowsForward - 1) / kRowsForward);
+    a.key_parts = parts_for(key_tiles, (int64_t)a.group * ((a.q_len + tile_rows_of(dtype) - 1) / tile_rows_of(dtype)));
+    a.query_parts = parts_for(query_tiles, (a.k_len + tile_rows_of(dtype) - 1) / tile_rows_of(dtype));
+}
+size_t attention_backward_partial_bytes(const AttentionArgs& a) {
+    const size_t keys = a.key_parts > 1 ? (size_t)2 * a.key_parts * a.batch * a.kv_heads * a.k_len : 0;
+    const size_t queries = a.query_parts > 1 ? (size_t)a.query_parts * a.batch * a.heads * a.q_len : 0;
+    return align_up(std::max(keys, queries) * a.head_dim * sizeof(float), 256);              // one after the other in the same place
+}
+
 }  // namespace lsp
 
 namespace {
@@ -173,10 +190,12 @@ int lsp_attention_forward(const lsp_attention_problem* p, lsp_dtype dtype, void*
     return done(lsp::launch_attention_forward(a, dtype, static_cast<hipStream_t>(stream)));
 }
 
-// delta | two maxima
+// delta | two maxima | parts
 size_t lsp_attention_backward_workspace_bytes(const lsp_attention_problem* p, lsp_dtype dtype) {
     if (check_attention_shape(p, dtype) != LSP_OK) return 0;
-    return delta_bytes(p) + 256;
+    lsp::AttentionArgs a = attention_args(p);
+    lsp::plan_attention_backward(a, dtype);
+    return delta_bytes(p) + 256 + lsp::attention_backward_partial_bytes(a);
 }
 
 int lsp_attention_backward(const lsp_attention_problem* p, const lsp_attention_gradients* g, lsp_dtype dtype, void* workspace, size_t workspace_bytes, void* stream) {
@@ -196,6 +215,8 @@ int lsp_attention_backward(const lsp_attention_problem* p, const lsp_attention_g
     a.dv = strided(g->dV, g->dv_stride, p->batch, p->k_len, p->kv_heads);
     a.delta = static_cast<float*>(workspace);
     a.most = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + delta_bytes(p));
+    a.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + delta_bytes(p) + 256);
+    lsp::plan_attention_backward(a, dtype);
     return done(lsp::launch_attention_backward(a, dtype, static_cast<hipStream_t>(stream)));
 }
 
