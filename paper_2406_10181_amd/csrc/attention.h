@@ -213,6 +213,8 @@ template <typename D> __device__ __forceinline__ const uint8_t* at(const Strided
     return static_cast<const uint8_t*>(s.p) + (b * s.batch + position * s.position + head * s.head) * D::size;
 }
 
+constexpr uint32_t kNowhere = 0x80000000u;
+
 // ROWS rows of a tile, asked for straight into LDS: a wave's load fills 1 KiB of LDS in the order of its lanes, so a lane asks for the unit that
 // belongs at its place.  Rows from `left` on and columns from head_dim on lie out of the buffer: zeros, and not read.  They have arrived when vmcnt
 // says so.
@@ -228,7 +230,7 @@ template <typename D, int DP, int ROWS, int NT> struct Fetch {
             uint32_t r, unit;
             T::at_place((i * kWaves + wave) * 64 + lane, r, unit);
             row[i] = (int)r;
-            off[i] = (int)unit * T::kUnitElems < head_dim ? r * row_bytes + unit * 16u : 0x80000000u;
+            off[i] = (int)unit * T::kUnitElems < head_dim ? r * row_bytes + unit * 16u : kNowhere;
         }
     }
     __device__ __forceinline__ void operator()(const void* first_row, int left, Lds tile, int wave) const {
@@ -236,28 +238,54 @@ template <typename D, int DP, int ROWS, int NT> struct Fetch {
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
             if (kLoads % kWaves && i * kWaves + wave >= kLoads) break;
-            const uint32_t o = row[i] < left ? off[i] : 0x80000000u;
+            const uint32_t o = row[i] < left ? off[i] : kNowhere;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (LSP_SHARED_AS void*)(tile + (i * kWaves + wave) * 1024u), 16, (int)o, 0, 0, 0);
         }
     }
 };
 
-// Eight elements of row `row` (a pointer to it, or NULL: zeros) as a B operand: columns 16 ks + 8 h + 0..7
-template <typename D> __device__ __forceinline__ Frag<D> global_frag(const uint8_t* row, int ks, int head_dim, int lane) {
-    const int col = 16 * ks + 8 * (lane >> 5);
-    Frag<D> f;
-    if (row && col < head_dim) {
-        const uint8_t* p = row + col * D::size;
-        if constexpr (D::size == 2) f.w = *reinterpret_cast<const u32x4*>(p);
-        else {
-            const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 16);
+// The 32 rows of a wave on their way into 32 rows of LDS of its own, from where Reader::rows makes operands of them: a wave's loads find whole lines, where
+// each lane asking for its own row would take a cycle a lane.  `offset(r)`: bytes from the buffer's begin to row r of the 32, or kNowhere for a row of zeros.
+template <typename D, int DP, typename Offset> __device__ __forceinline__ void fetch_wave_rows(const Buffer& b, Lds at, int head_dim, int lane, Offset&& offset) {
+    using T = Tile<D, DP>;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { f.w[j] = a[j]; f.w[4 + j] = b[j]; }
-        }
-    } else {
-        __builtin_memset(&f, 0, sizeof(f));
+    for (int i = 0; i < T::kUnits / 2; ++i) {
+        uint32_t r, unit;
+        T::at_place(i * 64 + lane, r, unit);
+        const uint32_t o = (int)unit * T::kUnitElems < head_dim ? offset(r) : kNowhere;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (LSP_SHARED_AS void*)(at + i * 1024u), 16, (int)(o + unit * 16u), 0, 0, 0);
     }
-    return f;
+}
+
+// And the way back: a wave's results, columns 8 (i / 4) + 4 h + i % 4 of 32 c + .. in registers i of v[c] and rows across lanes, as rows of the storage type: through
+// 32 rows of LDS of its own, so that stores are of whole lines too.  `row(r)`: where row r of the 32 goes, or NULL.
+template <typename D, int DP, typename Row> __device__ __forceinline__ void store_wave_rows(const f32x16 (&v)[DP / 32], float factor, Lds at, int head_dim, int lane, Row&& row) {
+    using T = Tile<D, DP>;
+    const uint32_t mine = lane & 31, h = (uint32_t)lane >> 5;
+#pragma unroll
+    for (int c = 0; c < DP / 32; ++c)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float x[4] = {v[c][4 * g] * factor, v[c][4 * g + 1] * factor, v[c][4 * g + 2] * factor, v[c][4 * g + 3] * factor};
+            if constexpr (D::size == 4) lds_write<f32x4>(at + T::place(mine, 8 * c + 2 * g + h), f32x4{x[0], x[1], x[2], x[3]});
+            else {
+                u32x2 w;
+                w[0] = (uint32_t)narrow<D>(x[0]) | (uint32_t)narrow<D>(x[1]) << 16;
+                w[1] = (uint32_t)narrow<D>(x[2]) | (uint32_t)narrow<D>(x[3]) << 16;
+                lds_write<u32x2>(at + T::place(mine, 4 * c + g) + h * 8u, w);
+            }
+        }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int i = 0; i < T::kUnits / 2; ++i) {
+        uint32_t r, unit;
+        T::at_place(i * 64 + lane, r, unit);
+        const u32x4 w = lds_read<u32x4>(at + (i * 64 + lane) * 16);
+        uint8_t* p = row(r);
+        if (p && (int)unit * T::kUnitElems < head_dim) *reinterpret_cast<u32x4*>(p + unit * 16u) = w;
+    }
 }
 
 // Four consecutive elements of an output row
@@ -269,11 +297,19 @@ template <typename D> __device__ __forceinline__ void store_four(uint8_t* p, flo
 
 __device__ __forceinline__ int valid_length(const int32_t* lens, int b, int most) { return lens ? min(max(lens[b], 0), most) : most; }
 
-// Work item of a workgroup.  Workgroups go round the eight XCDs, each with an L2 of its own: a run of consecutive items is given to each XCD, so
-// that the workgroups that read the same keys share an L2.
-__device__ __forceinline__ uint32_t item_of_block(uint32_t block, uint32_t items) {
-    const uint32_t xcd = block & 7u, share = items >> 3, rest = items & 7u;
-    return xcd * share + min(xcd, rest) + (block >> 3);
+// What workgroup `block` does: a tile of a unit (a head, or a part of one).  Workgroups go round the eight XCDs, each with an L2 of its own: an XCD gets whole units, so
+// that the workgroups that read the same rows share an L2, and goes through them tile by tile: tile 0 of all its units first, the one with the most work.
+__device__ __forceinline__ void work_of_block(uint32_t block, uint32_t units, uint32_t tiles, int& unit, int& tile) {
+    const uint32_t xcd = block & 7u, nth = block >> 3;
+    if (units % 8u == 0) {
+        const uint32_t share = units / 8u;
+        tile = (int)(nth / share);
+        unit = (int)(xcd * share + nth % share);
+    } else {                                                                              // runs of (unit, tile)
+        const uint32_t items = units * tiles, share = items >> 3, rest = items & 7u, item = xcd * share + min(xcd, rest) + nth;
+        unit = (int)(item / tiles);
+        tile = (int)(item % tiles);
+    }
 }
 #endif
 

@@ -14,6 +14,8 @@
 // scaled by 2^14.  Powers of two change nothing else, and the sums are scaled back at the end.  bf16 and fp32 have the range of fp32.
 #pragma once
 
+#include <algorithm>
+
 #include "attention_forward.h"
 
 #if defined(__HIPCC__)
@@ -30,41 +32,51 @@ template <typename D> __device__ __forceinline__ float score_factor(const Attent
     return __uint_as_float((uint32_t)min(max(254 - (int)(__float_as_uint(bound) >> 23) - 1, 1), 254) << 23);
 }
 
-// delta of every query that counts; fp16: the largest norms too.  16 lanes have a row, eight elements each.
+// delta of every query that counts; fp16: the largest norms too, of rows of dO and of V.  16 lanes have a row, eight elements each; `blocks`: of 16 rows, of dO
+// and then of V, that the workgroups go through.
 template <typename D>
-__global__ __launch_bounds__(256) void k_attention_delta(const AttentionArgs a, int64_t o_rows, int64_t v_rows) {
+__global__ __launch_bounds__(256) void k_attention_delta(const AttentionArgs a, int64_t o_blocks, int64_t blocks) {
     const int lane = threadIdx.x & 63, part = lane & 15, col = 8 * part;
-    int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-    const bool values = row >= o_rows;                                                    // (whole workgroups: o_rows is rounded up to 16)
-    if (values) row -= o_rows;
-    const int len = values ? a.k_len : a.q_len, heads = values ? a.kv_heads : a.heads;
-    const bool there = row < (values ? v_rows : (int64_t)a.batch * a.heads * a.q_len);
-    const int64_t line = there ? row / len : 0;
-    const int i = there ? (int)(row - line * len) : 0, b = (int)(line / heads), head = (int)(line - (int64_t)b * heads);
-    const bool counts = there && i < valid_length(values ? a.k_lens : a.q_lens, b, len);
-    float dot = 0.0f, norm = 0.0f;
-    if (counts && col < a.head_dim) {
-        const uint8_t* p = at<D>(values ? a.v : a.d_o, b, i, head) + col * D::size;
-        const uint8_t* q = values ? p : at<D>(a.o, b, i, head) + col * D::size;
-        typename D::elem x[8], y[8];
-        __builtin_memcpy(x, __builtin_assume_aligned(p, 16), sizeof(x));
-        __builtin_memcpy(y, __builtin_assume_aligned(q, 16), sizeof(y));
+    float largest[2] = {0.0f, 0.0f};
+    for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
+        const bool values = block >= o_blocks;
+        const int len = values ? a.k_len : a.q_len, heads = values ? a.kv_heads : a.heads;
+        const int64_t row = (values ? block - o_blocks : block) * 16 + (threadIdx.x >> 4);
+        const bool there = row < (int64_t)a.batch * heads * len;
+        const int64_t line = there ? row / len : 0;
+        const int i = there ? (int)(row - line * len) : 0, b = (int)(line / heads), head = (int)(line - (int64_t)b * heads);
+        const bool counts = there && i < valid_length(values ? a.k_lens : a.q_lens, b, len);
+        float dot = 0.0f, norm = 0.0f;
+        if (counts && col < a.head_dim) {
+            const uint8_t* p = at<D>(values ? a.v : a.d_o, b, i, head) + col * D::size;
+            const uint8_t* q = values ? p : at<D>(a.o, b, i, head) + col * D::size;
+            typename D::elem x[8], y[8];
+            __builtin_memcpy(x, __builtin_assume_aligned(p, 16), sizeof(x));
+            __builtin_memcpy(y, __builtin_assume_aligned(q, 16), sizeof(y));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { const float u = widen<D>(x[e]); dot = fmaf(u, widen<D>(y[e]), dot); norm = fmaf(u, u, norm); }
+            for (int e = 0; e < 8; ++e) { const float u = widen<D>(x[e]); dot = fmaf(u, widen<D>(y[e]), dot); norm = fmaf(u, u, norm); }
+        }
+#pragma unroll
+        for (int s = 1; s < 16; s <<= 1) { dot += __shfl_xor(dot, s); norm += __shfl_xor(norm, s); }
+        if (!values && counts && part == 0) a.delta[row] = dot;
+        if (values) largest[1] = norm > largest[1] || norm != norm ? norm : largest[1];
+        else largest[0] = norm > largest[0] || norm != norm ? norm : largest[0];
     }
-#pragma unroll
-    for (int s = 1; s < 16; s <<= 1) { dot += __shfl_xor(dot, s); norm += __shfl_xor(norm, s); }
-    if (!values && counts && part == 0) a.delta[row] = dot;
     if constexpr (std::is_same<D, F16>::value) {
-        __shared__ float norms[4];
+        __shared__ uint32_t norms[2][4];                                                  // (bits of numbers that are not negative: their order, and a NaN above all)
 #pragma unroll
-        for (int s = 16; s < 64; s <<= 1) norm = fmaxf(norm, __shfl_xor(norm, s));
-        if (lane == 0) norms[threadIdx.x >> 6] = norm;
+        for (int which = 0; which < 2; ++which) {
+            uint32_t bits = __float_as_uint(sqrtf(largest[which])) & 0x7FFFFFFFu;
+#pragma unroll
+            for (int s = 16; s < 64; s <<= 1) bits = max(bits, (uint32_t)__shfl_xor((int)bits, s));
+            if (lane == 0) norms[which][threadIdx.x >> 6] = bits;
+        }
         __syncthreads();
-        if (threadIdx.x == 0) {
+        if (threadIdx.x < 2) {
+            const uint32_t* n = norms[threadIdx.x];
+            const uint32_t bits = max(max(n[0], n[1]), max(n[2], n[3]));
             // a maximum: the order does not matter, and few are larger than what is there already (a look costs less than an atomic that all wait for)
-            const uint32_t bits = __float_as_uint(sqrtf(fmaxf(fmaxf(norms[0], norms[1]), fmaxf(norms[2], norms[3]))));
-            uint32_t* most = &a.most[values ? 1 : 0];
+            uint32_t* most = &a.most[threadIdx.x];
             if (bits > __hip_atomic_load(most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(most, bits);
         }
     }
@@ -80,13 +92,11 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
     extern __shared__ __align__(16) uint8_t smem[];
     const Lds lds = (Lds)smem;                                                            // K | V, twice
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    int unit, tile;
     const int tiles = (a.q_len + kRowsForward - 1) / kRowsForward;
-    uint32_t item = item_of_block(blockIdx.x, (uint32_t)a.batch * a.heads * tiles * a.query_parts);
-    const int row_tile = tiles - 1 - (int)(item % tiles);
-    item /= tiles;
-    const int part = (int)(item % a.query_parts);
-    item /= a.query_parts;
-    const int head = (int)(item % a.heads), b = (int)(item / a.heads), kv_head = head / a.group;
+    work_of_block(blockIdx.x, (uint32_t)a.batch * a.heads * a.query_parts, tiles, unit, tile);
+    const int row_tile = tiles - 1 - tile;
+    const int part = unit % a.query_parts, head = unit / a.query_parts % a.heads, b = unit / a.query_parts / a.heads, kv_head = head / a.group;
     const int nq = valid_length(a.q_lens, b, a.q_len), nk = valid_length(a.k_lens, b, a.k_len), ahead = nk - nq;
 
     const int first = row_tile * kRowsForward + wave * 32, qi = first + (lane & 31);
@@ -99,13 +109,6 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
     const int most = first >= nq ? 0 : a.causal ? min(nk, min(first + 31, nq - 1) + ahead + 1) : nk;
     const int least = first + 31 >= nq ? 0 : a.causal ? min(nk, first + ahead + 1) : nk;
 
-    Frag<D> qf[kSteps], gf[kSteps];
-    {
-        const uint8_t* p = counts ? at<D>(a.q, b, qi, head) : nullptr;
-        const uint8_t* g = counts ? at<D>(a.d_o, b, qi, head) : nullptr;
-#pragma unroll
-        for (int ks = 0; ks < kSteps; ++ks) { qf[ks] = global_frag<D>(p, ks, a.head_dim, lane); gf[ks] = global_frag<D>(g, ks, a.head_dim, lane); }
-    }
     const float factor = score_factor<D>(a), keep = (DROP ? a.drop.scale : 1.0f) * factor;
     float shift = 0.0f, delta = 0.0f;
     if (counts) {
@@ -125,11 +128,31 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
     Fetch<D, DP, BN, NT> fetch_k, fetch_v;
     fetch_k.setup((uint32_t)k_bytes, a.head_dim, wave, lane);
     fetch_v.setup((uint32_t)v_bytes, a.head_dim, wave, lane);
+    const Reader<D, DP> read(lane);
     if (begin < end) {
+        // the wave's queries and their gradients come through the buffers (16 bits: each through half of them; fp32: one after the other)
+        Frag<D> qf[kSteps], gf[kSteps];
+        const Lds rows = lds + wave * 32 * T::kRowBytes, others = D::size == 2 ? rows + 2 * kTileBytes : rows;
+        const auto fetch_rows = [&](const Strided& from, Lds to) {
+            const uint32_t row_bytes = (uint32_t)(from.position * D::size);
+            fetch_wave_rows<D, DP>(buffer_from(at<D>(from, b, first, head)), to, a.head_dim, lane, [&](uint32_t r) { return first + (int)r < nq ? r * row_bytes : kNowhere; });
+        };
+        fetch_rows(a.q, rows);
+        if constexpr (D::size == 2) fetch_rows(a.d_o, others);
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) qf[ks] = read.rows(rows, 0, ks);
+        if constexpr (D::size == 4) {
+            __builtin_amdgcn_s_waitcnt(0xC07F);                                           // (lgkmcnt(0): what was there has been read)
+            fetch_rows(a.d_o, others);
+            __builtin_amdgcn_s_waitcnt(0x0F70);
+        }
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) gf[ks] = read.rows(others, 0, ks);
+        __syncthreads();
         fetch_k(kp + begin * k_bytes, nk - begin, lds, wave);
         fetch_v(vp + begin * v_bytes, nk - begin, lds + kTileBytes, wave);
         arrived_for_all();
-        const Reader<D, DP> read(lane);
         const auto step = [&](Lds __restrict buf, Lds __restrict other, int k0) {
             if (k0 + BN < end) {
                 fetch_k(kp + (k0 + BN) * k_bytes, nk - k0 - BN, other, wave);
@@ -172,22 +195,22 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
             if (k0 + BN < end) step(lds + 2 * kTileBytes, lds, k0 + BN);
         }
     }
-    if (qi >= a.q_len) return;
     const float back = a.scale / (factor * kLift<D>);
-    const int64_t lines = (int64_t)a.batch * a.heads * a.q_len, line = ((int64_t)b * a.heads + head) * a.q_len + qi;
-    float* sums = a.partial + (part * lines + line) * a.head_dim;
-    uint8_t* out = const_cast<uint8_t*>(at<D>(a.dq, b, qi, head));
+    if (a.query_parts > 1) {
+        if (qi >= a.q_len) return;
+        const int64_t lines = (int64_t)a.batch * a.heads * a.q_len, line = ((int64_t)b * a.heads + head) * a.q_len + qi;
+        float* sums = a.partial + (part * lines + line) * a.head_dim;
 #pragma unroll
-    for (int c = 0; c < kCols; ++c)
+        for (int c = 0; c < kCols; ++c)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int col = 32 * c + 8 * g + 4 * h;
-            const f32x4 v = {dq[c][4 * g] * back, dq[c][4 * g + 1] * back, dq[c][4 * g + 2] * back, dq[c][4 * g + 3] * back};
-            if (col < a.head_dim) {
-                if (a.query_parts > 1) *reinterpret_cast<f32x4*>(sums + col) = v;
-                else store_four<D>(out + col * D::size, v[0], v[1], v[2], v[3]);
+            for (int g = 0; g < 4; ++g) {
+                const int col = 32 * c + 8 * g + 4 * h;
+                if (col < a.head_dim) *reinterpret_cast<f32x4*>(sums + col) = f32x4{dq[c][4 * g] * back, dq[c][4 * g + 1] * back, dq[c][4 * g + 2] * back, dq[c][4 * g + 3] * back};
             }
-        }
+        return;
+    }
+    store_wave_rows<D, DP>(dq, back, lds + wave * 32 * T::kRowBytes, a.head_dim, lane,
+                           [&](uint32_t r) -> uint8_t* { return first + (int)r < a.q_len ? const_cast<uint8_t*>(at<D>(a.dq, b, first + (int)r, head)) : nullptr; });
 }
 
 // Adds the parts of a gradient, in order: `lines` rows of (batch, head, position).  A thread has four columns.
@@ -219,13 +242,9 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
     extern __shared__ __align__(16) uint8_t smem[];
     const Lds lds = (Lds)smem;                                                            // Q | dO | L | delta, twice; bits of kept ones of each wave
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
-    const int tiles = (a.k_len + kKeysBackward - 1) / kKeysBackward;
-    uint32_t item = item_of_block(blockIdx.x, (uint32_t)a.batch * a.kv_heads * tiles * a.key_parts);
-    const int key_tile = (int)(item % tiles);                                             // (causal: the first keys have the most queries)
-    item /= tiles;
-    const int part = (int)(item % a.key_parts);
-    item /= a.key_parts;
-    const int kv_head = (int)(item % a.kv_heads), b = (int)(item / a.kv_heads);
+    int unit, key_tile;                                                                   // (causal: the first keys have the most queries)
+    work_of_block(blockIdx.x, (uint32_t)a.batch * a.kv_heads * a.key_parts, (a.k_len + kKeysBackward - 1) / kKeysBackward, unit, key_tile);
+    const int part = unit % a.key_parts, kv_head = unit / a.key_parts % a.kv_heads, b = unit / a.key_parts / a.kv_heads;
     const int nq = valid_length(a.q_lens, b, a.q_len), nk = valid_length(a.k_lens, b, a.k_len), ahead = nk - nq;
 
     const int first = key_tile * kKeysBackward + wave * 32, key = first + (lane & 31);
@@ -237,18 +256,6 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
     const int all_from = a.causal ? first + 31 - ahead : 0;                               // from here on every key of the wave is seen
     const int my_from = a.causal ? key - ahead : 0;
 
-    const Lds values = lds + 2 * kBufBytes + 512 + wave * (DP * 64) + lane * 16;     // V of the wave's keys, a lane's own operands
-    Frag<D> kf[kSteps], vf[kSteps];
-    {
-        const uint8_t* p = counts ? at<D>(a.k, b, key, kv_head) : nullptr;
-        const uint8_t* v = counts ? at<D>(a.v, b, key, kv_head) : nullptr;
-#pragma unroll
-        for (int ks = 0; ks < kSteps; ++ks) {
-            kf[ks] = global_frag<D>(p, ks, a.head_dim, lane);
-            vf[ks] = global_frag<D>(v, ks, a.head_dim, lane);
-            if constexpr (kValuesInLds) lds_write<u32x4>(values + ks * 1024, vf[ks].w);
-        }
-    }
     const float factor = score_factor<D>(a), keep = (DROP ? a.drop.scale : 1.0f) * factor, c2 = a.scale_log2;
     f32x16 dk[kCols], dv[kCols];
 #pragma unroll
@@ -280,12 +287,34 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
     const int tiles_q = begin < end ? (end - begin + BQ - 1) / BQ : 0;
     const int step_from = (int)((int64_t)tiles_q * a.group * part / a.key_parts), step_past = (int)((int64_t)tiles_q * a.group * (part + 1) / a.key_parts);
     if (step_from < step_past) {
+        // keys and values of the wave come through the buffers (V stays where it came to, if it stays in LDS; fp32: one after the other)
+        const Reader<D, DP> read(lane);
+        const Lds rows = lds + wave * 32 * T::kRowBytes;
+        const Lds values = kValuesInLds ? rows + 2 * kBufBytes + 512 : D::size == 2 ? rows + kKeysBackward * T::kRowBytes : rows;
+        Frag<D> kf[kSteps], vf[kValuesInLds ? 1 : kSteps];
+        const auto fetch_rows = [&](const Strided& from, Lds to) {
+            const uint32_t row_bytes = (uint32_t)(from.position * D::size);
+            fetch_wave_rows<D, DP>(buffer_from(at<D>(from, b, first, kv_head)), to, a.head_dim, lane, [&](uint32_t r) { return first + (int)r < nk ? r * row_bytes : kNowhere; });
+        };
+        fetch_rows(a.k, rows);
+        if constexpr (D::size == 2) fetch_rows(a.v, values);
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) kf[ks] = read.rows(rows, 0, ks);
+        if constexpr (D::size == 4) {
+            __builtin_amdgcn_s_waitcnt(0xC07F);                                           // (lgkmcnt(0): what was there has been read)
+            fetch_rows(a.v, values);
+            __builtin_amdgcn_s_waitcnt(0x0F70);
+        }
+        if constexpr (!kValuesInLds)
+#pragma unroll
+            for (int ks = 0; ks < kSteps; ++ks) vf[ks] = read.rows(values, 0, ks);
+        __syncthreads();
         int steps = step_past - step_from;
         int q_head = kv_head * a.group + step_from / tiles_q, q0 = begin + step_from % tiles_q * BQ;
         load(q_head, q0, lds);
         store(lds);
         arrived_for_all();
-        const Reader<D, DP> read(lane);
         const auto step = [&](Lds __restrict buf, Lds __restrict other) {
             int next_head = q_head, next_q0 = q0 + BQ;
             if (next_q0 >= end) { next_q0 = begin; ++next_head; }
@@ -302,7 +331,7 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
 #pragma unroll
                     for (int ks = 0; ks < kSteps; ++ks) {
                         Frag<D> v;
-                        if constexpr (kValuesInLds) v.w = lds_read<u32x4>(values + ks * 1024);
+                        if constexpr (kValuesInLds) v = read.rows(values, 0, ks);
                         else v = vf[ks];
                         dp = mma<D>(read.rows(buf + kTileBytes, 32 * t, ks), v, dp);
                     }
@@ -366,30 +395,31 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
             if (steps > 0) step(lds + kBufBytes, lds);
         }
     }
-    if (key >= a.k_len) return;
-    const float back_v = counts ? (DROP ? a.drop.scale : 1.0f) / kLift<D> : 0.0f, back_k = counts ? a.scale / (factor * kLift<D>) : 0.0f;
-    const int64_t lines = (int64_t)a.batch * a.kv_heads * a.k_len, line = ((int64_t)b * a.kv_heads + kv_head) * a.k_len + key;
-    float* sums = a.partial + (part * lines + line) * a.head_dim;                         // of dK; those of dV follow
-    uint8_t* out_k = const_cast<uint8_t*>(at<D>(a.dk, b, key, kv_head));
-    uint8_t* out_v = const_cast<uint8_t*>(at<D>(a.dv, b, key, kv_head));
+    const float back_v = (DROP ? a.drop.scale : 1.0f) / kLift<D>, back_k = a.scale / (factor * kLift<D>);
+    if (!counts)                                                                          // (its scores were those of a row of zeros)
 #pragma unroll
-    for (int c = 0; c < kCols; ++c)
+        for (int c = 0; c < kCols; ++c) { dk[c] = zeros16(); dv[c] = zeros16(); }
+    if (a.key_parts > 1) {
+        if (key >= a.k_len) return;
+        const int64_t lines = (int64_t)a.batch * a.kv_heads * a.k_len, line = ((int64_t)b * a.kv_heads + kv_head) * a.k_len + key;
+        float* sums = a.partial + (part * lines + line) * a.head_dim;                     // of dK; those of dV follow
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int col = 32 * c + 8 * g + 4 * h;
-            f32x4 k, v;
+        for (int c = 0; c < kCols; ++c)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { k[j] = counts ? dk[c][4 * g + j] * back_k : 0.0f; v[j] = counts ? dv[c][4 * g + j] * back_v : 0.0f; }
-            if (col < a.head_dim) {
-                if (a.key_parts > 1) {
-                    *reinterpret_cast<f32x4*>(sums + col) = k;
-                    *reinterpret_cast<f32x4*>(sums + a.key_parts * lines * a.head_dim + col) = v;
-                } else {
-                    store_four<D>(out_k + col * D::size, k[0], k[1], k[2], k[3]);
-                    store_four<D>(out_v + col * D::size, v[0], v[1], v[2], v[3]);
-                }
+            for (int g = 0; g < 4; ++g) {
+                const int col = 32 * c + 8 * g + 4 * h;
+                if (col >= a.head_dim) continue;
+                *reinterpret_cast<f32x4*>(sums + col) = f32x4{dk[c][4 * g] * back_k, dk[c][4 * g + 1] * back_k, dk[c][4 * g + 2] * back_k, dk[c][4 * g + 3] * back_k};
+                *reinterpret_cast<f32x4*>(sums + a.key_parts * lines * a.head_dim + col) = f32x4{dv[c][4 * g] * back_v, dv[c][4 * g + 1] * back_v, dv[c][4 * g + 2] * back_v, dv[c][4 * g + 3] * back_v};
             }
-        }
+        return;
+    }
+    const Lds room = lds + wave * 32 * T::kRowBytes;
+    store_wave_rows<D, DP>(dk, back_k, room, a.head_dim, lane,
+                           [&](uint32_t r) -> uint8_t* { return first + (int)r < a.k_len ? const_cast<uint8_t*>(at<D>(a.dk, b, first + (int)r, kv_head)) : nullptr; });
+    __builtin_amdgcn_wave_barrier();
+    store_wave_rows<D, DP>(dv, back_v, room, a.head_dim, lane,
+                           [&](uint32_t r) -> uint8_t* { return first + (int)r < a.k_len ? const_cast<uint8_t*>(at<D>(a.dv, b, first + (int)r, kv_head)) : nullptr; });
 }
 
 template <typename D, int DP, bool DROP> static hipError_t run_attention_backward(const AttentionArgs& a, hipStream_t st) {
@@ -401,13 +431,15 @@ template <typename D, int DP, bool DROP> static hipError_t run_attention_backwar
     hipError_t e = allow_dynamic_lds<dkv, lds_dkv>();
     if (e == hipSuccess) e = allow_dynamic_lds<dq, lds_dq>();
     if (e != hipSuccess) return e;
-    const int64_t o_rows = ((int64_t)a.batch * a.heads * a.q_len + 15) / 16 * 16;
-    const int64_t v_rows = std::is_same<D, F16>::value ? (int64_t)a.batch * a.kv_heads * a.k_len : 0;
-    if (v_rows) {
+    const bool norms = std::is_same<D, F16>::value;
+    const int64_t o_blocks = ((int64_t)a.batch * a.heads * a.q_len + 15) / 16;
+    const int64_t blocks = o_blocks + (norms ? ((int64_t)a.batch * a.kv_heads * a.k_len + 15) / 16 : 0);
+    if (norms) {
         hipLaunchKernelGGL(k_attention_clear<D>, dim3(1), dim3(64), 0, st, a.most);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(k_attention_delta<D>, dim3((unsigned)((o_rows + v_rows + 15) / 16)), dim3(256), 0, st, a, o_rows, v_rows);
+    // (norms: few workgroups, each of which ends with an atomic)
+    hipLaunchKernelGGL(k_attention_delta<D>, dim3((unsigned)(norms ? std::min<int64_t>(blocks, 512) : blocks)), dim3(256), 0, st, a, o_blocks, blocks);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const auto add = [&](const float* from, const Strided& out, int parts, int heads, int len) {
         const int64_t threads = (int64_t)a.batch * heads * len * (a.head_dim / 4);

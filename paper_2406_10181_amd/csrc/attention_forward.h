@@ -42,14 +42,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const Lds lds = (Lds)smem;                                                            // K | V, twice
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     // which rows, of which head, and which part of the keys
-    const uint32_t heads = a.packed ? a.kv_heads : a.heads, items = a.batch * heads * a.tiles * a.splits;
-    uint32_t item = item_of_block(blockIdx.x, items);
-    const int tile_r = (int)(item % a.tiles);
-    item /= a.tiles;
-    const int row_tile = a.tiles - 1 - tile_r;                                            // (causal: the longest first)
-    const int split = (int)(item % a.splits);
-    item /= a.splits;
-    const int head = (int)(item % heads), b = (int)(item / heads);
+    const int heads = a.packed ? a.kv_heads : a.heads;
+    int unit, tile;
+    work_of_block(blockIdx.x, (uint32_t)a.batch * heads * a.splits, a.tiles, unit, tile);
+    const int row_tile = a.tiles - 1 - tile;                                              // (causal: the longest first)
+    const int split = unit % a.splits, head = unit / a.splits % heads, b = unit / a.splits / heads;
     const int kv_head = a.packed ? head : head / a.group;
     const int nq = valid_length(a.q_lens, b, a.q_len), nk = valid_length(a.k_lens, b, a.k_len);
     const int ahead = nk - nq;                                                            // query i sees keys up to i + ahead
@@ -74,12 +71,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int end = min(end_all, begin + a.split_tiles * BN);
     if (!a.packed && row_tile * kRowsForward >= nq) most = 0;
 
-    Frag<D> qf[kSteps];
-    {
-        const uint8_t* p = counts ? at<D>(a.q, b, qi, q_head) : nullptr;
-#pragma unroll
-        for (int ks = 0; ks < kSteps; ++ks) qf[ks] = global_frag<D>(p, ks, a.head_dim, lane);
-    }
     f32x16 o[kCols];
 #pragma unroll
     for (int c = 0; c < kCols; ++c) o[c] = zeros16();
@@ -96,8 +87,30 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const Reader<D, DP> read(lane);
     const bool all_count = __all(counts);
     if (any) {
-        fetch_k(kp + begin * k_bytes, nk - begin, lds, wave);
-        fetch_v(vp + begin * v_bytes, nk - begin, lds + kTileBytes, wave);
+        // the wave's queries come through the second buffer while the first keys are on their way into the first (fp32: through both, before them)
+        const Lds rows = lds + (D::size == 2 ? 2 * kTileBytes : 0) + wave * 32 * T::kRowBytes;
+        const int wave_row = row_tile * kRowsForward + wave * 32;
+        const uint32_t q_bytes = (uint32_t)(a.q.position * D::size);
+        const Buffer q = buffer_from(at<D>(a.q, b, a.packed ? 0 : wave_row, a.packed ? kv_head * a.group : head));
+        fetch_wave_rows<D, DP>(q, rows, a.head_dim, lane, [&](uint32_t r) {
+            if (!a.packed) return wave_row + (int)r < nq ? r * q_bytes : kNowhere;
+            const uint32_t n = wave_row + r, of_group = n / a.q_len, i = n - of_group * a.q_len;
+            return (int)n < a.rows && (int)i < nq ? of_group * (uint32_t)(a.q.head * D::size) + i * q_bytes : kNowhere;
+        });
+        if constexpr (D::size == 4) arrived_for_all();
+        else {
+            fetch_k(kp + begin * k_bytes, nk - begin, lds, wave);
+            fetch_v(vp + begin * v_bytes, nk - begin, lds + kTileBytes, wave);
+            __builtin_amdgcn_s_waitcnt(0x0F70);
+        }
+        Frag<D> qf[kSteps];
+#pragma unroll
+        for (int ks = 0; ks < kSteps; ++ks) qf[ks] = read.rows(rows, 0, ks);
+        if constexpr (D::size == 4) {
+            __syncthreads();
+            fetch_k(kp + begin * k_bytes, nk - begin, lds, wave);
+            fetch_v(vp + begin * v_bytes, nk - begin, lds + kTileBytes, wave);
+        }
         arrived_for_all();
         const auto step = [&](Lds __restrict buf, Lds __restrict other, int k0) {
             if (k0 + BN < end) {
@@ -190,9 +203,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         }
     }
     l = halves_sum(l);
-    if (row >= a.rows) return;
     if (a.splits > 1) {
         // this part's sums as they are; k_attention_join puts the parts together
+        if (row >= a.rows) return;
         const int64_t lines = (int64_t)a.batch * a.heads * a.q_len;
         const int64_t line = ((int64_t)b * a.heads + q_head) * a.q_len + qi;
         float* out = a.partial + (split * lines + line) * a.head_dim;
@@ -207,15 +220,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         return;
     }
     const float inv = l == 0.0f ? 0.0f : (DROP ? a.drop.scale : 1.0f) / l;
-    uint8_t* out = const_cast<uint8_t*>(at<D>(a.o, b, qi, q_head));
-#pragma unroll
-    for (int c = 0; c < kCols; ++c)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int col = 32 * c + 8 * g + 4 * h;
-            if (col < a.head_dim) store_four<D>(out + col * D::size, o[c][4 * g] * inv, o[c][4 * g + 1] * inv, o[c][4 * g + 2] * inv, o[c][4 * g + 3] * inv);
-        }
-    if (h == 0) a.L[((int64_t)b * a.heads + q_head) * a.q_len + qi] = l == 0.0f ? -INFINITY : m * a.scale + __logf(l);
+    const int wave_row = row_tile * kRowsForward + wave * 32;
+    store_wave_rows<D, DP>(o, inv, lds + wave * 32 * T::kRowBytes, a.head_dim, lane, [&](uint32_t r) -> uint8_t* {
+        const int n = wave_row + (int)r;
+        if (n >= a.rows) return nullptr;
+        return const_cast<uint8_t*>(a.packed ? at<D>(a.o, b, n % a.q_len, kv_head * a.group + n / a.q_len) : at<D>(a.o, b, n, head));
+    });
+    if (h == 0 && row < a.rows) a.L[((int64_t)b * a.heads + q_head) * a.q_len + qi] = l == 0.0f ? -INFINITY : m * a.scale + __logf(l);
 }
 
 // Joins the parts of a row: O = sum_s w_s O_s / sum_s w_s l_s with w_s = 2^(m_s - m).  A wave has a row, a lane two columns.

@@ -26,7 +26,8 @@ size_t attention_partial_bytes(const AttentionArgs& a) {
 
 void plan_attention_forward(AttentionArgs& a, lsp_dtype dtype) {
     // Few queries: the query heads that share a key head go into one tile of rows, so that keys and values are read once for all of them.
-    a.packed = a.group > 1 && (int64_t)a.group * a.q_len <= kRowsForward;
+    // (Its rows are addressed with 32 bits from the first head's first row.)
+    a.packed = a.group > 1 && (int64_t)a.group * a.q_len <= kRowsForward && ((int64_t)a.group * a.q.head + (int64_t)a.q_len * a.q.position) * 4 < ((int64_t)1 << 31);
     a.rows = a.packed ? a.group * a.q_len : a.q_len;
     a.tiles = (a.rows + kRowsForward - 1) / kRowsForward;
     // Few tiles of rows: the keys are split, as far as that gives each CU two workgroups and each of these four tiles of keys.

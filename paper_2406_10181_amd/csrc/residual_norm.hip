@@ -26,9 +26,7 @@ template <int TPR, int N> struct RowSum {
     int turn = 0;
     __device__ __forceinline__ void operator()(float (&v)[N]) {
 #pragma unroll
-        for (int s = 1; s < 64; s <<= 1)
-#pragma unroll
-            for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], s);
+        for (int k = 0; k < N; ++k) v[k] = wave_sum(v[k]);
         if constexpr (TPR > 64) {
             constexpr int kWaves = TPR / 64;
             const int lane = threadIdx.x & 63, wave = (threadIdx.x % TPR) >> 6;
@@ -153,143 +151,146 @@ __global__ __launch_bounds__(TPR * GROUPS) void k_residual_norm(const ResidualNo
     }
 }
 
-template <typename D, int TPR, int NV, int GROUPS, bool DROP>
-__global__ __launch_bounds__(TPR * GROUPS) void k_residual_norm_back(const ResidualNormArgs a) {
+// A thread has eight columns, TPR threads a row and GROUPS rows a workgroup; the row after this one is on its way while this one's sums wait for one another, and the
+// weights stay in registers.  BIAS: a norm has a bias, or the gradient of one is asked for.
+template <typename D, int TPR, int GROUPS, bool DROP, bool BIAS>
+__global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const ResidualNormArgs a) {
     using elem = typename D::elem;
-    __shared__ float scratch[GROUPS][2 * 2 * (TPR / 64)];
-    const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
-    const int width = a.width;
+    constexpr int kSumFloats = GROUPS * 4 * (TPR / 64);
+    __shared__ float scratch[GROUPS > 1 ? (GROUPS - 1) * TPR * 8 : kSumFloats];           // RowSum's, and at the end the other groups' sums over rows
+    const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR), t = threadIdx.x % TPR, col = t * 8;
+    const int width = a.width, left = width - col;
     const float per = 1.0f / (float)width;
-    RowSum<TPR, 2> sum{scratch[group]};
-    float acc[kGrads][NV][8];
+    RowSum<TPR, 2> sum{scratch + group * 4 * (TPR / 64)};
+    const bool post = a.post != LSP_NORM_NONE, pre = a.pre != LSP_NORM_NONE;
+    const auto vector = [&](const void* p, float otherwise) {
+        if (p) return load_packed<D>(static_cast<const elem*>(p) + col, left);
+        Packed<D> r;
+#pragma unroll
+        for (int k = 0; k < 2 * D::size; ++k)
+            r.w[k] = D::size == 4 ? __float_as_uint(otherwise) : (uint32_t)narrow<D>(otherwise) * 0x10001u;
+        return r;
+    };
+    Packed<D> wf_ = vector(post ? a.post_w : nullptr, 1.0f), bf_ = vector(BIAS && post ? a.post_b : nullptr, 0.0f), g_ = vector(a.gate, 1.0f), wy_ = vector(pre ? a.pre_w : nullptr, 1.0f);
+    float acc[kGrads][8];
 #pragma unroll
     for (int k = 0; k < kGrads; ++k)
 #pragma unroll
-        for (int n = 0; n < NV; ++n)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) acc[k][n][e] = 0.0f;
-    const int64_t step = (int64_t)gridDim.x * GROUPS;
-    for (int64_t base = (int64_t)blockIdx.x * GROUPS; base < a.rows; base += step) {
+        for (int e = 0; e < 8; ++e) acc[k][e] = 0.0f;
+    Packed<D> xp, fp, dyp, dhp;
+    float mean_f, rstd_f, mean_y, rstd_y;
+    const auto load_first = [&](int64_t row) {
+        const elem* x = static_cast<const elem*>(a.x) + row * a.x_stride + col;
+        const elem* f = static_cast<const elem*>(a.f) + row * a.f_stride + col;
+        const elem* dh = a.dh ? static_cast<const elem*>(a.dh) + row * a.dh_stride + col : x;
+        if (left >= 8) { xp = load_whole<D>(x); fp = load_whole<D>(f); dhp = load_whole<D>(dh); }
+        else { xp = load_part<D>(x, left); fp = load_part<D>(f, left); dhp = load_part<D>(dh, left); }
+    };
+    const auto load_dy = [&](int64_t row) { dyp = load_packed<D>(static_cast<const elem*>(a.dy) + row * a.dy_stride + col, left); };
+    const int64_t step = (int64_t)gridDim.x * GROUPS, first = (int64_t)blockIdx.x * GROUPS;
+    const auto mine_of = [&](int64_t base) { return base + group < a.rows ? base + group : a.rows - 1; };   // (every thread goes to every barrier)
+    load_first(mine_of(first));
+    load_dy(mine_of(first));
+    for (int64_t base = first; base < a.rows; base += step) {
         const bool mine = base + group < a.rows;
-        const int64_t row = mine ? base + group : a.rows - 1;
-        const elem* x = static_cast<const elem*>(a.x) + row * a.x_stride;
-        const elem* f = static_cast<const elem*>(a.f) + row * a.f_stride;
-        const elem* dy = static_cast<const elem*>(a.dy) + row * a.dy_stride;
-        const elem* dh = a.dh ? static_cast<const elem*>(a.dh) + row * a.dh_stride : nullptr;
-        Eight xv[NV], fv[NV], dyv[NV], dhv[NV];
+        const int64_t row = mine_of(base);
+        const int64_t next = mine_of(base + step < a.rows ? base + step : base);
+        mean_f = a.stats[row]; rstd_f = a.stats[a.rows + row]; mean_y = a.stats[2 * a.rows + row]; rstd_y = a.stats[3 * a.rows + row];
+        // (the vectors stay packed: widened once, before the loop, they would take twice the registers)
 #pragma unroll
-        for (int n = 0; n < NV; ++n) {
-            const int col = (t + n * TPR) * 8;
-            xv[n] = load_eight<D>(x + col, width - col);
-            fv[n] = load_eight<D>(f + col, width - col);
-            dyv[n] = load_eight<D>(dy + col, width - col);
-            if (dh) dhv[n] = load_eight<D>(dh + col, width - col);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e) dhv[n].x[e] = 0.0f;
+        for (int k = 0; k < 2 * D::size; ++k) {
+            asm volatile("" : "+v"(wf_.w[k]), "+v"(g_.w[k]), "+v"(wy_.w[k]));
+            if constexpr (BIAS) asm volatile("" : "+v"(bf_.w[k]));
         }
-        const float mean_f = a.stats[row], rstd_f = a.stats[a.rows + row], mean_y = a.stats[2 * a.rows + row], rstd_y = a.stats[3 * a.rows + row];
-        float s[2] = {0.0f, 0.0f};
-        // xv: y^, dhv: the gradient of y^;  fv: f^
-        uint32_t kept[NV];
+        // y^ and f^, and the gradient of y^
+        uint32_t kept = 0xFFu;
+        if constexpr (DROP) {
+            const uint64_t at = (uint64_t)row * (uint64_t)((width + 7) >> 3) + (uint64_t)t;
+            const u32x4 w = philox((uint32_t)at, (uint32_t)(at >> 32), 0, a.drop.offset, a.drop.key0, a.drop.key1);
+            kept = 0;
 #pragma unroll
-        for (int n = 0; n < NV; ++n) {
-            const int col = (t + n * TPR) * 8;
-            Eight u;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { fv[n].x[e] = col + e < width ? (fv[n].x[e] - mean_f) * rstd_f : 0.0f; u.x[e] = fv[n].x[e]; }
-            if (a.post != LSP_NORM_NONE) {
-                const Eight w = vector_eight<D>(a.post_w, col, width, 1.0f), b = vector_eight<D>(a.post_b, col, width, 0.0f);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u.x[e] = fmaf(u.x[e], w.x[e], b.x[e]);
-            }
-            kept[n] = 0xFFu;
-            if constexpr (DROP) {
-                const uint64_t at = (uint64_t)row * (uint64_t)((width + 7) >> 3) + (uint64_t)(col >> 3);
-                const u32x4 w = philox((uint32_t)at, (uint32_t)(at >> 32), 0, a.drop.offset, a.drop.key0, a.drop.key1);
-                kept[n] = 0;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) kept[n] |= (philox_word(w, e) < a.drop.limit ? 0u : 1u) << e;
-            }
-            const Eight g = vector_eight<D>(a.gate, col, width, 1.0f), wp = vector_eight<D>(a.pre != LSP_NORM_NONE ? a.pre_w : nullptr, col, width, 1.0f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float keep = !DROP ? 1.0f : (kept[n] >> e) & 1u ? a.drop.scale : 0.0f;
-                const float kept_u = keep == 0.0f ? 0.0f : keep * u.x[e];                 // (what is dropped may be infinite)
-                const float y = fmaf(a.branch_scale * g.x[e], kept_u, a.residual_scale * xv[n].x[e]);
-                const float hat = col + e < width ? (y - mean_y) * rstd_y : 0.0f;
-                const float d = dhv[n].x[e];
-                if (mine) { acc[0][n][e] = fmaf(d, hat, acc[0][n][e]); acc[1][n][e] += d; }
-                const float de = d * wp.x[e];
-                xv[n].x[e] = hat;
-                dhv[n].x[e] = de;
-                s[0] = fmaf(de, hat, s[0]);
-                s[1] += de;
-            }
+            for (int e = 0; e < 8; ++e) kept |= (philox_word(w, e) < a.drop.limit ? 0u : 1u) << e;
         }
-        if (a.pre != LSP_NORM_NONE) sum(s);
+        float fhat[8], yhat[8], de[8], s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (e == 4) __builtin_amdgcn_sched_barrier(0);                                // (four at a time: eight would take registers for speed that nothing waits for)
+            const bool in = e < left;
+            const float wf = element<D>(wf_, e), bf = (BIAS ? element<D>(bf_, e) : 0.0f), g = element<D>(g_, e), wy = element<D>(wy_, e);
+            fhat[e] = in ? (element<D>(fp, e) - mean_f) * rstd_f : 0.0f;
+            const float u = !DROP ? fmaf(fhat[e], wf, bf) : (kept >> e) & 1u ? a.drop.scale * fmaf(fhat[e], wf, bf) : 0.0f;   // (what is dropped may be infinite)
+            const float y = fmaf(a.branch_scale * g, u, a.residual_scale * element<D>(xp, e));
+            yhat[e] = in ? (y - mean_y) * rstd_y : 0.0f;
+            const float d = a.dh ? element<D>(dhp, e) : 0.0f;
+            if (mine) {
+                acc[0][e] = fmaf(d, yhat[e], acc[0][e]);
+                if constexpr (BIAS) acc[1][e] += d;
+            }
+            de[e] = d * wy;
+            s[0] = fmaf(de[e], yhat[e], s[0]);
+            s[1] += de[e];
+        }
+        load_first(next);                                                                 // (where what they held is used up)
+        if (pre) sum(s);
         float s1 = s[0] * per, s0 = a.pre == LSP_NORM_LAYER ? s[1] * per : 0.0f;
         s[0] = s[1] = 0.0f;
+        Eight out;
 #pragma unroll
-        for (int n = 0; n < NV; ++n) {
-            const int col = (t + n * TPR) * 8;
-            Eight out;
-            const Eight g = vector_eight<D>(a.gate, col, width, 1.0f);
-            const Eight w = vector_eight<D>(a.post != LSP_NORM_NONE ? a.post_w : nullptr, col, width, 1.0f), b = vector_eight<D>(a.post != LSP_NORM_NONE ? a.post_b : nullptr, col, width, 0.0f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float total = dyv[n].x[e] + (a.pre == LSP_NORM_NONE ? dhv[n].x[e] : rstd_y * (dhv[n].x[e] - s0 - xv[n].x[e] * s1));
-                out.x[e] = a.residual_scale * total;
-                const float keep = !DROP ? 1.0f : (kept[n] >> e) & 1u ? a.drop.scale : 0.0f;
-                const float branch = a.branch_scale * total * keep, u = keep == 0.0f ? 0.0f : fmaf(fv[n].x[e], w.x[e], b.x[e]);
-                const float du = branch * g.x[e];
-                if (mine) {
-                    acc[2][n][e] = fmaf(branch, u, acc[2][n][e]);
-                    acc[3][n][e] = fmaf(du, fv[n].x[e], acc[3][n][e]);
-                    acc[4][n][e] += du;
-                }
-                const float de = col + e < width ? du * w.x[e] : 0.0f;
-                dyv[n].x[e] = de;
-                s[0] = fmaf(de, fv[n].x[e], s[0]);
-                s[1] += de;
+        for (int e = 0; e < 8; ++e) {
+            if (e == 4) __builtin_amdgcn_sched_barrier(0);
+            const float wf = element<D>(wf_, e), bf = (BIAS ? element<D>(bf_, e) : 0.0f), g = element<D>(g_, e);
+            const float total = element<D>(dyp, e) + (pre ? rstd_y * (de[e] - s0 - yhat[e] * s1) : de[e]);
+            out.x[e] = a.residual_scale * total;
+            const bool keep = !DROP || ((kept >> e) & 1u);
+            const float branch = keep ? a.branch_scale * total * (DROP ? a.drop.scale : 1.0f) : 0.0f, u = keep ? fmaf(fhat[e], wf, bf) : 0.0f;
+            const float du = branch * g;
+            if (mine) {
+                acc[2][e] = fmaf(branch, u, acc[2][e]);
+                acc[3][e] = fmaf(du, fhat[e], acc[3][e]);
+                if constexpr (BIAS) acc[4][e] += du;
             }
-            if (mine) store_eight<D>(static_cast<elem*>(a.dx) + row * a.dx_stride + col, out, width - col);
+            de[e] = e < left ? du * wf : 0.0f;
+            s[0] = fmaf(de[e], fhat[e], s[0]);
+            s[1] += de[e];
         }
-        if (a.post != LSP_NORM_NONE) sum(s);
+        if (mine) store_eight<D>(static_cast<elem*>(a.dx) + row * a.dx_stride + col, out, left);
+        load_dy(next);
+        if (post) sum(s);
         s1 = s[0] * per; s0 = a.post == LSP_NORM_LAYER ? s[1] * per : 0.0f;
 #pragma unroll
-        for (int n = 0; n < NV; ++n) {
-            const int col = (t + n * TPR) * 8;
-            Eight out;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) out.x[e] = a.post == LSP_NORM_NONE ? dyv[n].x[e] : rstd_f * (dyv[n].x[e] - s0 - fv[n].x[e] * s1);
-            if (mine) store_eight<D>(static_cast<elem*>(a.df) + row * a.df_stride + col, out, width - col);
-        }
+        for (int e = 0; e < 8; ++e) out.x[e] = post ? rstd_f * (de[e] - s0 - fhat[e] * s1) : de[e];
+        if (mine) store_eight<D>(static_cast<elem*>(a.df) + row * a.df_stride + col, out, left);
     }
-    // this row group's part of the sums over rows
-    const int64_t part = (int64_t)blockIdx.x * GROUPS + group, parts = (int64_t)gridDim.x * GROUPS;
+    // the workgroup's part of the sums over rows
     int slot = 0;
 #pragma unroll
     for (int k = 0; k < kGrads; ++k) {
         if (!a.grads[k]) continue;
-        float* out = a.partial + ((int64_t)slot * parts + part) * width;
-        ++slot;
+        Eight v;
 #pragma unroll
-        for (int n = 0; n < NV; ++n) {
-            const int col = (t + n * TPR) * 8;
-            Eight v;
+        for (int e = 0; e < 8; ++e) v.x[e] = acc[k][e];
+        if constexpr (GROUPS > 1) {
+            __syncthreads();                                                              // (scratch is free)
+            if (group > 0)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v.x[e] = acc[k][n][e];
-            store_eight<F32>(out + col, v, width - col);
+                for (int e = 0; e < 8; ++e) scratch[((group - 1) * 8 + e) * TPR + t] = v.x[e];
+            __syncthreads();
+            if (group == 0)
+#pragma unroll
+                for (int o = 0; o < GROUPS - 1; ++o)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v.x[e] += scratch[(o * 8 + e) * TPR + t];
         }
+        if (group == 0) store_eight<F32>(a.partial + ((int64_t)slot * gridDim.x + blockIdx.x) * width + col, v, left);
+        ++slot;
     }
 }
 
-// Adds the parts: a workgroup has 64 columns of one sum, its four waves take turns at the parts.
-__global__ __launch_bounds__(256) void k_residual_norm_sums(const ResidualNormArgs a, int64_t parts) {
-    __shared__ float add[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int col = blockIdx.x * 64 + lane;
+// Adds the parts: a workgroup has 32 columns of one sum, its 32 rows of threads take turns at the parts.
+__global__ __launch_bounds__(1024) void k_residual_norm_sums(const ResidualNormArgs a, int parts) {
+    __shared__ float add[32][33];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int col = blockIdx.x * 32 + x;
     float* out = nullptr;
     int slot = 0;
 #pragma unroll
@@ -298,21 +299,27 @@ __global__ __launch_bounds__(256) void k_residual_norm_sums(const ResidualNormAr
     const float* p = a.partial + (int64_t)blockIdx.y * parts * a.width;
     float s = 0.0f;
     if (col < a.width)
-        for (int64_t r = wave; r < parts; r += 4) s += p[r * a.width + col];
-    add[wave][lane] = s;
+        for (int r = y; r < parts; r += 32) s += p[(int64_t)r * a.width + col];
+    add[y][x] = s;
     __syncthreads();
-    if (wave == 0 && col < a.width) out[col] = (add[0][lane] + add[1][lane]) + (add[2][lane] + add[3][lane]);
+    if (y == 0 && col < a.width) {
+        s = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 32; ++r) s += add[r][x];
+        out[col] = s;
+    }
 }
 
-// Rows that a workgroup has at a time, by their width
-static int groups_of(int width) { return width <= 1024 ? 4 : width <= 4096 ? 2 : 1; }
-
+// Backward: threads of a row, and rows that a workgroup has at a time, by their width.  One workgroup a CU: its registers hold no second one of 512 threads, and fewer
+// workgroups leave fewer parts to add (4096 x 4096, bf16: 48 + 5 us; twice as many workgroups 53 + 7; two a CU at 128 registers, with spills, 91).
+static int row_threads(int width) { return width <= 512 ? 64 : width <= 1024 ? 128 : width <= 2048 ? 256 : width <= 4096 ? 512 : 1024; }
+static int row_groups(int width) { return width <= 512 ? 8 : width <= 1024 ? 4 : width <= 2048 ? 2 : 1; }
 static int64_t workgroups_of(int64_t rows, int32_t width) {
-    const int64_t all = (rows + groups_of(width) - 1) / groups_of(width);
+    const int64_t all = (rows + row_groups(width) - 1) / row_groups(width);
     return all < 256 ? all : 256;
 }
 size_t residual_norm_partial_bytes(int64_t rows, int32_t width) {
-    return align_up((size_t)workgroups_of(rows, width) * groups_of(width) * kGrads * (size_t)width * sizeof(float), 256);
+    return align_up((size_t)workgroups_of(rows, width) * kGrads * (size_t)width * sizeof(float), 256);
 }
 
 template <typename D, int TPR, int NV, int GROUPS> static hipError_t run_forward(const ResidualNormArgs& a, hipStream_t st) {
@@ -321,32 +328,42 @@ template <typename D, int TPR, int NV, int GROUPS> static hipError_t run_forward
     else hipLaunchKernelGGL((k_residual_norm<D, TPR, NV, GROUPS, false>), grid, block, 0, st, a);
     return hipGetLastError();
 }
-template <typename D, int TPR, int NV, int GROUPS> static hipError_t run_backward(const ResidualNormArgs& a, hipStream_t st) {
+template <typename D, int TPR, int GROUPS> static hipError_t run_backward(const ResidualNormArgs& a, hipStream_t st) {
     const int64_t workgroups = workgroups_of(a.rows, a.width);
-    if (a.drop.limit) hipLaunchKernelGGL((k_residual_norm_back<D, TPR, NV, GROUPS, true>), dim3((unsigned)workgroups), dim3(TPR * GROUPS), 0, st, a);
-    else hipLaunchKernelGGL((k_residual_norm_back<D, TPR, NV, GROUPS, false>), dim3((unsigned)workgroups), dim3(TPR * GROUPS), 0, st, a);
+    const bool bias = (a.post != LSP_NORM_NONE && a.post_b) || a.grads[1] || a.grads[4];
+    const dim3 grid((unsigned)workgroups), block(TPR * GROUPS);
+    if (a.drop.limit && bias) hipLaunchKernelGGL((k_residual_norm_back<D, TPR, GROUPS, true, true>), grid, block, 0, st, a);
+    else if (a.drop.limit) hipLaunchKernelGGL((k_residual_norm_back<D, TPR, GROUPS, true, false>), grid, block, 0, st, a);
+    else if (bias) hipLaunchKernelGGL((k_residual_norm_back<D, TPR, GROUPS, false, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_residual_norm_back<D, TPR, GROUPS, false, false>), grid, block, 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     int sums = 0;
     for (float* g : a.grads) sums += g != nullptr;
     if (!sums) return hipSuccess;
-    hipLaunchKernelGGL(k_residual_norm_sums, dim3((unsigned)((a.width + 63) / 64), (unsigned)sums), dim3(256), 0, st, a, workgroups * GROUPS);
+    hipLaunchKernelGGL(k_residual_norm_sums, dim3((unsigned)((a.width + 31) / 32), (unsigned)sums), dim3(1024), 0, st, a, (int)workgroups);
     return hipGetLastError();
 }
 
+// Forward: a row has as few idle threads as the variants allow (2999 columns in 128 threads of 24 columns 24 us, in 256 threads of 16 columns 30: 3001 rows, fp16,
+// dropout); beyond 4096 columns two units a thread in 512 threads (16384 rows of 8192, bf16: 198 us; one unit in 1024 threads 215, four in 256 threads 241).
 template <typename D> static hipError_t forward_of(const ResidualNormArgs& a, hipStream_t st) {
-    if (a.width <= 512) return run_forward<D, 64, 1, 4>(a, st);
-    if (a.width <= 1024) return run_forward<D, 64, 2, 4>(a, st);
-    if (a.width <= 2048) return run_forward<D, 256, 1, 2>(a, st);
-    if (a.width <= 4096) return run_forward<D, 256, 2, 2>(a, st);
+    if (a.width <= 64 * 8) return run_forward<D, 64, 1, 4>(a, st);
+    if (a.width <= 64 * 16) return run_forward<D, 64, 2, 4>(a, st);
+    if (a.width <= 64 * 24) return run_forward<D, 64, 3, 4>(a, st);
+    if (a.width <= 256 * 8) return run_forward<D, 256, 1, 2>(a, st);
+    if (a.width <= 128 * 24) return run_forward<D, 128, 3, 2>(a, st);
+    if (a.width <= 256 * 16) return run_forward<D, 256, 2, 2>(a, st);
     return run_forward<D, 512, 2, 1>(a, st);
 }
 template <typename D> static hipError_t backward_of(const ResidualNormArgs& a, hipStream_t st) {
-    if (a.width <= 512) return run_backward<D, 64, 1, 4>(a, st);
-    if (a.width <= 1024) return run_backward<D, 64, 2, 4>(a, st);
-    if (a.width <= 2048) return run_backward<D, 256, 1, 2>(a, st);
-    if (a.width <= 4096) return run_backward<D, 256, 2, 2>(a, st);
-    return run_backward<D, 512, 2, 1>(a, st);
+    switch (row_threads(a.width)) {
+        case 64:  return run_backward<D, 64, 8>(a, st);
+        case 128: return run_backward<D, 128, 4>(a, st);
+        case 256: return run_backward<D, 256, 2>(a, st);
+        case 512: return run_backward<D, 512, 1>(a, st);
+        default:  return run_backward<D, 1024, 1>(a, st);
+    }
 }
 
 hipError_t launch_residual_norm_forward(const ResidualNormArgs& a, lsp_dtype dtype, hipStream_t st) {
