@@ -19,8 +19,8 @@ struct AttentionArgs {
     Strided q, k, v, o, d_o, dq, dk, dv;
     float*         L;                // [batch][heads][q_len]
     float*         delta;            // [batch][heads][q_len]: dO . O; in the backward pass
-    uint32_t*      most;             // fp16 backward: bits of the largest norm of a row of dO and of V (atomic maxima)
-    float*         partial;          // forward with several splits: O of each, then (largest score, sum) of each row; backward: parts of dK and dV, then of dQ
+    float*         norms;            // fp16 backward: [2][kNormSlots], squares of the largest norm of a row of dO and of V that a workgroup met
+    float*         partial;          // forward with several splits: O of each, then (largest score, sum) of each row; backward: parts of dK, of dV, of dQ
     const int32_t* q_lens;
     const int32_t* k_lens;
     int32_t batch, heads, kv_heads, group, q_len, k_len, head_dim, causal;
@@ -28,6 +28,7 @@ struct AttentionArgs {
     int32_t rows;                    // rows of a head: q_len, or group * q_len where `packed`
     int32_t packed;                  // rows are (query head of the group, query): few queries, all heads of a key head in one tile
     int32_t splits, split_tiles;     // forward: parts of the keys, tiles of keys in each
+    int32_t norm_slots;              // fp16 backward: slots in use
     int32_t key_parts, query_parts;  // backward: workgroups that share 128 keys (parts of their queries), and 128 queries (parts of their keys)
     float   scale, scale_log2;       // scale_log2 = scale * log2(e): probabilities are powers of two
     Dropout drop;
@@ -42,6 +43,7 @@ void plan_attention_backward(AttentionArgs& a, lsp_dtype dtype);
 size_t attention_backward_partial_bytes(const AttentionArgs& a);
 
 constexpr int kRowsForward = 128;    // query rows of a workgroup: four waves of 32
+constexpr int kNormSlots = 1024;
 constexpr int kKeysBackward = 128;   // keys of a workgroup of the kernel that makes dK and dV
 
 // Keys (forward, dQ) or queries (dK, dV) of a tile in LDS
@@ -243,6 +245,22 @@ template <typename D, int DP, int ROWS, int NT> struct Fetch {
         }
     }
 };
+
+// fp32: operands straight from the lane's own row (a pointer to it, or NULL: zeros), columns 16 ks + 8 h + 0..7.  There the matrix instructions take so long that the
+// way through LDS (below) only adds its latency: 37 instead of 41 us for the three passes of 8 heads of 64 x 64 x 64.
+__device__ __forceinline__ Frag<F32> global_frag(const uint8_t* row, int ks, int head_dim, int lane) {
+    const int col = 16 * ks + 8 * (lane >> 5);
+    Frag<F32> f;
+    if (row && col < head_dim) {
+        const f32x4 a = *reinterpret_cast<const f32x4*>(row + col * 4), b = *reinterpret_cast<const f32x4*>(row + col * 4 + 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { f.w[j] = a[j]; f.w[4 + j] = b[j]; }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f.w[j] = 0.0f;
+    }
+    return f;
+}
 
 // The 32 rows of a wave on their way into 32 rows of LDS of its own, from where Reader::rows makes operands of them: a wave's loads find whole lines, where
 // each lane asking for its own row would take a cycle a lane.  `offset(r)`: bytes from the buffer's begin to row r of the 32, or kNowhere for a row of zeros.

@@ -2,11 +2,11 @@
 // keys is ever in memory.  With delta_i = dO_i . O_i:
 //     P = exp(scale Q K^T - L),   dP = keep (dO V^T),   dS = P (dP - delta),
 //     dV = (keep P)^T dO,   dQ = scale dS K,   dK = scale dS^T Q    (the last two summed over the query heads of a key head).
-// Two kernels, each owner of what it writes, so that nothing is added by atomics and the result does not depend on timing: k_attention_dq
+// Two kernels, each owner of what it writes, so that nothing is added by atomics and the result does not depend on timing: attention_dq
 // walks the keys for 128 queries, k_attention_dkv the queries for 128 keys.  Both make the scores, seven products instead of five.
 //
-// k_attention_dq has a query per lane, as the forward pass: S^T = K Q^T and dP^T = V dO^T give dS^T, the operand of dQ^T += K^T dS^T as it is.
-// k_attention_dkv has a key per lane: S = Q K^T and dP = dO V^T (keys and values of the lane in registers) give the operands P and dS of
+// attention_dq has a query per lane, as the forward pass: S^T = K Q^T and dP^T = V dO^T give dS^T, the operand of dQ^T += K^T dS^T as it is.
+// attention_dkv has a key per lane: S = Q K^T and dP = dO V^T (keys and values of the lane in registers) give the operands P and dS of
 // dV^T += dO^T P and dK^T += Q^T dS; L and delta of the 16 queries of a lane come from LDS.
 //
 // fp16: gradients of scores can be far below what fp16 resolves, or above its range.  dP and delta are at most B = max |dO_i| max |V_j| keep, so
@@ -21,19 +21,34 @@
 #if defined(__HIPCC__)
 namespace lsp {
 
+// The larger of two numbers, or the NaN if one is
+__device__ __forceinline__ float larger(float x, float y) { return !(y <= x) ? y : x; }
+
 template <typename D> constexpr float kLiftLog2 = std::is_same<D, F16>::value ? 14.0f : 0.0f;
 template <typename D> constexpr float kLift = std::is_same<D, F16>::value ? 16384.0f : 1.0f;   // factor of the probabilities
 
 // g: a power of two, at most 1 / (the largest |dP|); 1 where that is no number
-template <typename D> __device__ __forceinline__ float score_factor(const AttentionArgs& a) {
+template <typename D> __device__ __forceinline__ float score_factor(const AttentionArgs& a, int lane) {
     if constexpr (!std::is_same<D, F16>::value) return 1.0f;
-    const float bound = __uint_as_float(a.most[0]) * __uint_as_float(a.most[1]) * a.drop.scale * 1.01f;
+    float largest[2] = {0.0f, 0.0f};
+    for (int i = 4 * lane; i < a.norm_slots; i += 256)
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(a.norms + which * kNormSlots + i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (i + j < a.norm_slots) largest[which] = larger(largest[which], v[j]);
+        }
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1)
+#pragma unroll
+        for (int which = 0; which < 2; ++which) largest[which] = larger(largest[which], __shfl_xor(largest[which], s));
+    const float bound = sqrtf(largest[0]) * sqrtf(largest[1]) * a.drop.scale * 1.01f;
     if (!(bound > 0.0f) || !(bound < INFINITY)) return 1.0f;
     return __uint_as_float((uint32_t)min(max(254 - (int)(__float_as_uint(bound) >> 23) - 1, 1), 254) << 23);
 }
 
 // delta of every query that counts; fp16: the largest norms too, of rows of dO and of V.  16 lanes have a row, eight elements each; `blocks`: of 16 rows, of dO
-// and then of V, that the workgroups go through.
+// and then of V, that the workgroups go through.  (What the workgroups of fp16 find they leave side by side: an atomic that all of them wait for took longer than the rest.)
 template <typename D>
 __global__ __launch_bounds__(256) void k_attention_delta(const AttentionArgs a, int64_t o_blocks, int64_t blocks) {
     const int lane = threadIdx.x & 63, part = lane & 15, col = 8 * part;
@@ -43,8 +58,8 @@ __global__ __launch_bounds__(256) void k_attention_delta(const AttentionArgs a, 
         const int len = values ? a.k_len : a.q_len, heads = values ? a.kv_heads : a.heads;
         const int64_t row = (values ? block - o_blocks : block) * 16 + (threadIdx.x >> 4);
         const bool there = row < (int64_t)a.batch * heads * len;
-        const int64_t line = there ? row / len : 0;
-        const int i = there ? (int)(row - line * len) : 0, b = (int)(line / heads), head = (int)(line - (int64_t)b * heads);
+        const uint32_t line = there ? (uint32_t)row / (uint32_t)len : 0u;                 // (there are fewer than 2^27 rows)
+        const int i = there ? (int)((uint32_t)row - line * (uint32_t)len) : 0, b = (int)(line / (uint32_t)heads), head = (int)(line - (uint32_t)(b * heads));
         const bool counts = there && i < valid_length(values ? a.k_lens : a.q_lens, b, len);
         float dot = 0.0f, norm = 0.0f;
         if (counts && col < a.head_dim) {
@@ -59,42 +74,40 @@ __global__ __launch_bounds__(256) void k_attention_delta(const AttentionArgs a, 
 #pragma unroll
         for (int s = 1; s < 16; s <<= 1) { dot += __shfl_xor(dot, s); norm += __shfl_xor(norm, s); }
         if (!values && counts && part == 0) a.delta[row] = dot;
-        if (values) largest[1] = norm > largest[1] || norm != norm ? norm : largest[1];
-        else largest[0] = norm > largest[0] || norm != norm ? norm : largest[0];
+        if (values) largest[1] = larger(largest[1], norm);
+        else largest[0] = larger(largest[0], norm);
     }
     if constexpr (std::is_same<D, F16>::value) {
-        __shared__ uint32_t norms[2][4];                                                  // (bits of numbers that are not negative: their order, and a NaN above all)
+        __shared__ float found[2][4];
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            uint32_t bits = __float_as_uint(sqrtf(largest[which])) & 0x7FFFFFFFu;
 #pragma unroll
-            for (int s = 16; s < 64; s <<= 1) bits = max(bits, (uint32_t)__shfl_xor((int)bits, s));
-            if (lane == 0) norms[which][threadIdx.x >> 6] = bits;
+            for (int s = 16; s < 64; s <<= 1) largest[which] = larger(largest[which], __shfl_xor(largest[which], s));
+            if (lane == 0) found[which][threadIdx.x >> 6] = largest[which];
         }
         __syncthreads();
         if (threadIdx.x < 2) {
-            const uint32_t* n = norms[threadIdx.x];
-            const uint32_t bits = max(max(n[0], n[1]), max(n[2], n[3]));
-            // a maximum: the order does not matter, and few are larger than what is there already (a look costs less than an atomic that all wait for)
-            uint32_t* most = &a.most[threadIdx.x];
-            if (bits > __hip_atomic_load(most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(most, bits);
+            const float* n = found[threadIdx.x];
+            a.norms[threadIdx.x * kNormSlots + blockIdx.x] = larger(larger(n[0], n[1]), larger(n[2], n[3]));
         }
     }
 }
 
-template <typename D> __global__ void k_attention_clear(uint32_t* most) { if (threadIdx.x < 2) most[threadIdx.x] = 0; }
+// Where the parts of dQ begin: behind those of dK and dV
+__host__ __device__ static inline float* query_partial(const AttentionArgs& a) {
+    return a.partial + (a.key_parts > 1 ? (int64_t)2 * a.key_parts * a.batch * a.kv_heads * a.k_len * a.head_dim : 0);
+}
 
 template <typename D, int DP, bool DROP>
-__global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_attention_dq(const AttentionArgs a) {
+__device__ __forceinline__ void attention_dq(const AttentionArgs& a, uint32_t block, uint8_t* smem) {
     using T = Tile<D, DP>;
     constexpr int BN = tile_rows<D>(), NT = 256, kSteps = DP / 16, kTiles = BN / 32, kCols = DP / 32;
     constexpr uint32_t kTileBytes = BN * T::kRowBytes;
-    extern __shared__ __align__(16) uint8_t smem[];
     const Lds lds = (Lds)smem;                                                            // K | V, twice
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     int unit, tile;
     const int tiles = (a.q_len + kRowsForward - 1) / kRowsForward;
-    work_of_block(blockIdx.x, (uint32_t)a.batch * a.heads * a.query_parts, tiles, unit, tile);
+    work_of_block(block, (uint32_t)a.batch * a.heads * a.query_parts, tiles, unit, tile);
     const int row_tile = tiles - 1 - tile;
     const int part = unit % a.query_parts, head = unit / a.query_parts % a.heads, b = unit / a.query_parts / a.heads, kv_head = head / a.group;
     const int nq = valid_length(a.q_lens, b, a.q_len), nk = valid_length(a.k_lens, b, a.k_len), ahead = nk - nq;
@@ -109,7 +122,7 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
     const int most = first >= nq ? 0 : a.causal ? min(nk, min(first + 31, nq - 1) + ahead + 1) : nk;
     const int least = first + 31 >= nq ? 0 : a.causal ? min(nk, first + ahead + 1) : nk;
 
-    const float factor = score_factor<D>(a), keep = (DROP ? a.drop.scale : 1.0f) * factor;
+    const float factor = score_factor<D>(a, lane), keep = (DROP ? a.drop.scale : 1.0f) * factor;
     float shift = 0.0f, delta = 0.0f;
     if (counts) {
         const int64_t line = ((int64_t)b * a.heads + head) * a.q_len + qi;
@@ -130,26 +143,26 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
     fetch_v.setup((uint32_t)v_bytes, a.head_dim, wave, lane);
     const Reader<D, DP> read(lane);
     if (begin < end) {
-        // the wave's queries and their gradients come through the buffers (16 bits: each through half of them; fp32: one after the other)
         Frag<D> qf[kSteps], gf[kSteps];
-        const Lds rows = lds + wave * 32 * T::kRowBytes, others = D::size == 2 ? rows + 2 * kTileBytes : rows;
-        const auto fetch_rows = [&](const Strided& from, Lds to) {
-            const uint32_t row_bytes = (uint32_t)(from.position * D::size);
-            fetch_wave_rows<D, DP>(buffer_from(at<D>(from, b, first, head)), to, a.head_dim, lane, [&](uint32_t r) { return first + (int)r < nq ? r * row_bytes : kNowhere; });
-        };
-        fetch_rows(a.q, rows);
-        if constexpr (D::size == 2) fetch_rows(a.d_o, others);
-        __builtin_amdgcn_s_waitcnt(0x0F70);
-#pragma unroll
-        for (int ks = 0; ks < kSteps; ++ks) qf[ks] = read.rows(rows, 0, ks);
         if constexpr (D::size == 4) {
-            __builtin_amdgcn_s_waitcnt(0xC07F);                                           // (lgkmcnt(0): what was there has been read)
+            const uint8_t* p = counts ? at<D>(a.q, b, qi, head) : nullptr;
+            const uint8_t* g = counts ? at<D>(a.d_o, b, qi, head) : nullptr;
+#pragma unroll
+            for (int ks = 0; ks < kSteps; ++ks) { qf[ks] = global_frag(p, ks, a.head_dim, lane); gf[ks] = global_frag(g, ks, a.head_dim, lane); }
+        } else {
+            // the wave's queries and their gradients come through the buffers, each through half of them
+            const Lds rows = lds + wave * 32 * T::kRowBytes, others = rows + 2 * kTileBytes;
+            const auto fetch_rows = [&](const Strided& from, Lds to) {
+                const uint32_t row_bytes = (uint32_t)(from.position * D::size);
+                fetch_wave_rows<D, DP>(buffer_from(at<D>(from, b, first, head)), to, a.head_dim, lane, [&](uint32_t r) { return first + (int)r < nq ? r * row_bytes : kNowhere; });
+            };
+            fetch_rows(a.q, rows);
             fetch_rows(a.d_o, others);
             __builtin_amdgcn_s_waitcnt(0x0F70);
-        }
 #pragma unroll
-        for (int ks = 0; ks < kSteps; ++ks) gf[ks] = read.rows(others, 0, ks);
-        __syncthreads();
+            for (int ks = 0; ks < kSteps; ++ks) { qf[ks] = read.rows(rows, 0, ks); gf[ks] = read.rows(others, 0, ks); }
+            __syncthreads();
+        }
         fetch_k(kp + begin * k_bytes, nk - begin, lds, wave);
         fetch_v(vp + begin * v_bytes, nk - begin, lds + kTileBytes, wave);
         arrived_for_all();
@@ -168,6 +181,12 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
                     for (int ks = 0; ks < kSteps; ++ks) s = mma<D>(read.rows(buf, 32 * t, ks), qf[ks], s);
 #pragma unroll
                     for (int ks = 0; ks < kSteps; ++ks) dp = mma<D>(read.rows(buf + kTileBytes, 32 * t, ks), gf[ks], dp);
+                    if constexpr (D::size == 2) {                                         // reads stay six ahead of their products
+                        then_reads<6>();
+#pragma unroll
+                        for (int i = 0; i < 2 * kSteps - 6; ++i) { then_matrix<1>(); then_reads<1>(); }
+                        then_matrix<6>();
+                    }
                     if (edge)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) s[i] = 32 * t + 8 * (i >> 2) + (i & 3) < seen ? s[i] : -INFINITY;
@@ -199,7 +218,7 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 64 ? 1 : 2)) void k_atte
     if (a.query_parts > 1) {
         if (qi >= a.q_len) return;
         const int64_t lines = (int64_t)a.batch * a.heads * a.q_len, line = ((int64_t)b * a.heads + head) * a.q_len + qi;
-        float* sums = a.partial + (part * lines + line) * a.head_dim;
+        float* sums = query_partial(a) + (part * lines + line) * a.head_dim;
 #pragma unroll
         for (int c = 0; c < kCols; ++c)
 #pragma unroll
@@ -234,16 +253,15 @@ template <typename D, int DP> constexpr bool values_in_lds() { return D::size ==
 template <typename D, int DP> constexpr int queries_at_once() { return values_in_lds<D, DP>() ? 32 : tile_rows<D>(); }
 
 template <typename D, int DP, bool DROP>
-__global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_attention_dkv(const AttentionArgs a) {
+__device__ __forceinline__ void attention_dkv(const AttentionArgs& a, uint32_t block, uint8_t* smem) {
     using T = Tile<D, DP>;
     constexpr bool kValuesInLds = values_in_lds<D, DP>();
     constexpr int BQ = queries_at_once<D, DP>(), NT = 256, kSteps = DP / 16, kTiles = BQ / 32, kCols = DP / 32;
     constexpr uint32_t kTileBytes = BQ * T::kRowBytes, kBufBytes = 2 * kTileBytes + BQ * 8;
-    extern __shared__ __align__(16) uint8_t smem[];
     const Lds lds = (Lds)smem;                                                            // Q | dO | L | delta, twice; bits of kept ones of each wave
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     int unit, key_tile;                                                                   // (causal: the first keys have the most queries)
-    work_of_block(blockIdx.x, (uint32_t)a.batch * a.kv_heads * a.key_parts, (a.k_len + kKeysBackward - 1) / kKeysBackward, unit, key_tile);
+    work_of_block(block, (uint32_t)a.batch * a.kv_heads * a.key_parts, (a.k_len + kKeysBackward - 1) / kKeysBackward, unit, key_tile);
     const int part = unit % a.key_parts, kv_head = unit / a.key_parts % a.kv_heads, b = unit / a.key_parts / a.kv_heads;
     const int nq = valid_length(a.q_lens, b, a.q_len), nk = valid_length(a.k_lens, b, a.k_len), ahead = nk - nq;
 
@@ -256,7 +274,7 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
     const int all_from = a.causal ? first + 31 - ahead : 0;                               // from here on every key of the wave is seen
     const int my_from = a.causal ? key - ahead : 0;
 
-    const float factor = score_factor<D>(a), keep = (DROP ? a.drop.scale : 1.0f) * factor, c2 = a.scale_log2;
+    const float factor = score_factor<D>(a, lane), keep = (DROP ? a.drop.scale : 1.0f) * factor, c2 = a.scale_log2;
     f32x16 dk[kCols], dv[kCols];
 #pragma unroll
     for (int c = 0; c < kCols; ++c) { dk[c] = zeros16(); dv[c] = zeros16(); }
@@ -287,29 +305,31 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
     const int tiles_q = begin < end ? (end - begin + BQ - 1) / BQ : 0;
     const int step_from = (int)((int64_t)tiles_q * a.group * part / a.key_parts), step_past = (int)((int64_t)tiles_q * a.group * (part + 1) / a.key_parts);
     if (step_from < step_past) {
-        // keys and values of the wave come through the buffers (V stays where it came to, if it stays in LDS; fp32: one after the other)
         const Reader<D, DP> read(lane);
-        const Lds rows = lds + wave * 32 * T::kRowBytes;
-        const Lds values = kValuesInLds ? rows + 2 * kBufBytes + 512 : D::size == 2 ? rows + kKeysBackward * T::kRowBytes : rows;
         Frag<D> kf[kSteps], vf[kValuesInLds ? 1 : kSteps];
-        const auto fetch_rows = [&](const Strided& from, Lds to) {
-            const uint32_t row_bytes = (uint32_t)(from.position * D::size);
-            fetch_wave_rows<D, DP>(buffer_from(at<D>(from, b, first, kv_head)), to, a.head_dim, lane, [&](uint32_t r) { return first + (int)r < nk ? r * row_bytes : kNowhere; });
-        };
-        fetch_rows(a.k, rows);
-        if constexpr (D::size == 2) fetch_rows(a.v, values);
-        __builtin_amdgcn_s_waitcnt(0x0F70);
-#pragma unroll
-        for (int ks = 0; ks < kSteps; ++ks) kf[ks] = read.rows(rows, 0, ks);
+        const Lds rows = lds + wave * 32 * T::kRowBytes;
+        const Lds values = kValuesInLds ? rows + 2 * kBufBytes + 512 : rows + kKeysBackward * T::kRowBytes;
         if constexpr (D::size == 4) {
-            __builtin_amdgcn_s_waitcnt(0xC07F);                                           // (lgkmcnt(0): what was there has been read)
+            const uint8_t* p = counts ? at<D>(a.k, b, key, kv_head) : nullptr;
+            const uint8_t* v = counts ? at<D>(a.v, b, key, kv_head) : nullptr;
+#pragma unroll
+            for (int ks = 0; ks < kSteps; ++ks) { kf[ks] = global_frag(p, ks, a.head_dim, lane); vf[ks] = global_frag(v, ks, a.head_dim, lane); }
+        } else {
+            // keys and values of the wave come through the buffers (V stays where it came to, if it stays in LDS)
+            const auto fetch_rows = [&](const Strided& from, Lds to) {
+                const uint32_t row_bytes = (uint32_t)(from.position * D::size);
+                fetch_wave_rows<D, DP>(buffer_from(at<D>(from, b, first, kv_head)), to, a.head_dim, lane, [&](uint32_t r) { return first + (int)r < nk ? r * row_bytes : kNowhere; });
+            };
+            fetch_rows(a.k, rows);
             fetch_rows(a.v, values);
             __builtin_amdgcn_s_waitcnt(0x0F70);
-        }
-        if constexpr (!kValuesInLds)
 #pragma unroll
-            for (int ks = 0; ks < kSteps; ++ks) vf[ks] = read.rows(values, 0, ks);
-        __syncthreads();
+            for (int ks = 0; ks < kSteps; ++ks) {
+                kf[ks] = read.rows(rows, 0, ks);
+                if constexpr (!kValuesInLds) vf[ks] = read.rows(values, 0, ks);
+            }
+            __syncthreads();
+        }
         int steps = step_past - step_from;
         int q_head = kv_head * a.group + step_from / tiles_q, q0 = begin + step_from % tiles_q * BQ;
         load(q_head, q0, lds);
@@ -422,41 +442,42 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
                            [&](uint32_t r) -> uint8_t* { return first + (int)r < a.k_len ? const_cast<uint8_t*>(at<D>(a.dv, b, first + (int)r, kv_head)) : nullptr; });
 }
 
-template <typename D, int DP, bool DROP> static hipError_t run_attention_backward(const AttentionArgs& a, hipStream_t st) {
-    constexpr size_t tile = (size_t)tile_rows<D>() * Tile<D, DP>::kRowBytes;
-    constexpr auto dkv = k_attention_dkv<D, DP, DROP>;
-    constexpr auto dq = k_attention_dq<D, DP, DROP>;
+// Both in one launch, dK and dV first: neither waits for the other, and the last workgroups of the one leave no CU idle.
+template <typename D, int DP, bool DROP>
+__global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_attention_backward(const AttentionArgs a, uint32_t key_items) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    if (blockIdx.x < key_items) attention_dkv<D, DP, DROP>(a, blockIdx.x, smem);
+    else attention_dq<D, DP, DROP>(a, blockIdx.x - key_items, smem);
+}
+
+template <typename D, int DP, bool DROP> static hipError_t run_attention_backward(AttentionArgs a, hipStream_t st) {
+    constexpr auto kern = k_attention_backward<D, DP, DROP>;
     constexpr size_t lds_dkv = queries_at_once<D, DP>() * (4 * Tile<D, DP>::kRowBytes + 16) + 512 + (values_in_lds<D, DP>() ? kKeysBackward * Tile<D, DP>::kRowBytes : 0);
-    constexpr size_t lds_dq = 4 * tile;
-    hipError_t e = allow_dynamic_lds<dkv, lds_dkv>();
-    if (e == hipSuccess) e = allow_dynamic_lds<dq, lds_dq>();
+    constexpr size_t lds_dq = 4 * (size_t)tile_rows<D>() * Tile<D, DP>::kRowBytes;
+    constexpr size_t lds = lds_dkv > lds_dq ? lds_dkv : lds_dq;
+    hipError_t e = allow_dynamic_lds<kern, lds>();
     if (e != hipSuccess) return e;
     const bool norms = std::is_same<D, F16>::value;
     const int64_t o_blocks = ((int64_t)a.batch * a.heads * a.q_len + 15) / 16;
     const int64_t blocks = o_blocks + (norms ? ((int64_t)a.batch * a.kv_heads * a.k_len + 15) / 16 : 0);
-    if (norms) {
-        hipLaunchKernelGGL(k_attention_clear<D>, dim3(1), dim3(64), 0, st, a.most);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    // (norms: few workgroups, each of which ends with an atomic)
-    hipLaunchKernelGGL(k_attention_delta<D>, dim3((unsigned)(norms ? std::min<int64_t>(blocks, 512) : blocks)), dim3(256), 0, st, a, o_blocks, blocks);
+    const int64_t grid = norms ? std::min<int64_t>(blocks, kNormSlots) : blocks;
+    a.norm_slots = (int32_t)grid;
+    hipLaunchKernelGGL(k_attention_delta<D>, dim3((unsigned)grid), dim3(256), 0, st, a, o_blocks, blocks);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const int64_t key_items = (int64_t)a.batch * a.kv_heads * ((a.k_len + kKeysBackward - 1) / kKeysBackward) * a.key_parts;
+    const int64_t query_items = (int64_t)a.batch * a.heads * ((a.q_len + kRowsForward - 1) / kRowsForward) * a.query_parts;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(key_items + query_items)), dim3(256), lds, st, a, (uint32_t)key_items);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const auto add = [&](const float* from, const Strided& out, int parts, int heads, int len) {
         const int64_t threads = (int64_t)a.batch * heads * len * (a.head_dim / 4);
         hipLaunchKernelGGL(k_attention_add<D>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, from, out, parts, a.batch, heads, len, a.head_dim);
         return hipGetLastError();
     };
-    const int64_t key_items = (int64_t)a.batch * a.kv_heads * ((a.k_len + kKeysBackward - 1) / kKeysBackward) * a.key_parts;
-    hipLaunchKernelGGL(dkv, dim3((unsigned)key_items), dim3(256), lds_dkv, st, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
     if (a.key_parts > 1) {
         if ((e = add(a.partial, a.dk, a.key_parts, a.kv_heads, a.k_len)) != hipSuccess) return e;
         if ((e = add(a.partial + (int64_t)a.key_parts * a.batch * a.kv_heads * a.k_len * a.head_dim, a.dv, a.key_parts, a.kv_heads, a.k_len)) != hipSuccess) return e;
     }
-    const int64_t query_items = (int64_t)a.batch * a.heads * ((a.q_len + kRowsForward - 1) / kRowsForward) * a.query_parts;
-    hipLaunchKernelGGL(dq, dim3((unsigned)query_items), dim3(256), lds_dq, st, a);
-    if ((e = hipGetLastError()) != hipSuccess || a.query_parts == 1) return e;
-    return add(a.partial, a.dq, a.query_parts, a.heads, a.q_len);
+    return a.query_parts > 1 ? add(query_partial(a), a.dq, a.query_parts, a.heads, a.q_len) : hipSuccess;
 }
 
 template <typename D> hipError_t attention_backward_of(const AttentionArgs& a, hipStream_t st) {

@@ -87,29 +87,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const Reader<D, DP> read(lane);
     const bool all_count = __all(counts);
     if (any) {
-        // the wave's queries come through the second buffer while the first keys are on their way into the first (fp32: through both, before them)
-        const Lds rows = lds + (D::size == 2 ? 2 * kTileBytes : 0) + wave * 32 * T::kRowBytes;
-        const int wave_row = row_tile * kRowsForward + wave * 32;
-        const uint32_t q_bytes = (uint32_t)(a.q.position * D::size);
-        const Buffer q = buffer_from(at<D>(a.q, b, a.packed ? 0 : wave_row, a.packed ? kv_head * a.group : head));
-        fetch_wave_rows<D, DP>(q, rows, a.head_dim, lane, [&](uint32_t r) {
-            if (!a.packed) return wave_row + (int)r < nq ? r * q_bytes : kNowhere;
-            const uint32_t n = wave_row + r, of_group = n / a.q_len, i = n - of_group * a.q_len;
-            return (int)n < a.rows && (int)i < nq ? of_group * (uint32_t)(a.q.head * D::size) + i * q_bytes : kNowhere;
-        });
-        if constexpr (D::size == 4) arrived_for_all();
-        else {
-            fetch_k(kp + begin * k_bytes, nk - begin, lds, wave);
-            fetch_v(vp + begin * v_bytes, nk - begin, lds + kTileBytes, wave);
-            __builtin_amdgcn_s_waitcnt(0x0F70);
-        }
+        fetch_k(kp + begin * k_bytes, nk - begin, lds, wave);
+        fetch_v(vp + begin * v_bytes, nk - begin, lds + kTileBytes, wave);
         Frag<D> qf[kSteps];
-#pragma unroll
-        for (int ks = 0; ks < kSteps; ++ks) qf[ks] = read.rows(rows, 0, ks);
         if constexpr (D::size == 4) {
-            __syncthreads();
-            fetch_k(kp + begin * k_bytes, nk - begin, lds, wave);
-            fetch_v(vp + begin * v_bytes, nk - begin, lds + kTileBytes, wave);
+            const uint8_t* p = counts ? at<D>(a.q, b, qi, q_head) : nullptr;
+#pragma unroll
+            for (int ks = 0; ks < kSteps; ++ks) qf[ks] = global_frag(p, ks, a.head_dim, lane);
+        } else {
+            // the wave's queries come through the second buffer while the first keys are on their way into the first
+            const Lds rows = lds + 2 * kTileBytes + wave * 32 * T::kRowBytes;
+            const int wave_row = row_tile * kRowsForward + wave * 32;
+            const uint32_t q_bytes = (uint32_t)(a.q.position * D::size);
+            const Buffer q = buffer_from(at<D>(a.q, b, a.packed ? 0 : wave_row, a.packed ? kv_head * a.group : head));
+            fetch_wave_rows<D, DP>(q, rows, a.head_dim, lane, [&](uint32_t r) {
+                if (!a.packed) return wave_row + (int)r < nq ? r * q_bytes : kNowhere;
+                const uint32_t n = wave_row + r, of_group = n / a.q_len, i = n - of_group * a.q_len;
+                return (int)n < a.rows && (int)i < nq ? of_group * (uint32_t)(a.q.head * D::size) + i * q_bytes : kNowhere;
+            });
+            __builtin_amdgcn_s_waitcnt(0x0F70);
+#pragma unroll
+            for (int ks = 0; ks < kSteps; ++ks) qf[ks] = read.rows(rows, 0, ks);
         }
         arrived_for_all();
         const auto step = [&](Lds __restrict buf, Lds __restrict other, int k0) {

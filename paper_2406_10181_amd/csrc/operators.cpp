@@ -52,7 +52,7 @@ void plan_attention_backward(AttentionArgs& a, lsp_dtype dtype) {
 size_t attention_backward_partial_bytes(const AttentionArgs& a) {
     const size_t keys = a.key_parts > 1 ? (size_t)2 * a.key_parts * a.batch * a.kv_heads * a.k_len : 0;
     const size_t queries = a.query_parts > 1 ? (size_t)a.query_parts * a.batch * a.heads * a.q_len : 0;
-    return align_up(std::max(keys, queries) * a.head_dim * sizeof(float), 256);              // one after the other in the same place
+    return align_up((keys + queries) * a.head_dim * sizeof(float), 256);
 }
 
 }  // namespace lsp
@@ -124,6 +124,7 @@ lsp::AttentionArgs attention_args(const lsp_attention_problem* p) {
     return a;
 }
 
+constexpr size_t kNormBytes = 2 * lsp::kNormSlots * sizeof(float);
 size_t delta_bytes(const lsp_attention_problem* p) { return lsp::align_up((size_t)p->batch * p->heads * p->q_len * sizeof(float), 256); }
 
 bool norm_kind(int32_t k) { return k == LSP_NORM_NONE || k == LSP_NORM_RMS || k == LSP_NORM_LAYER; }
@@ -191,12 +192,12 @@ int lsp_attention_forward(const lsp_attention_problem* p, lsp_dtype dtype, void*
     return done(lsp::launch_attention_forward(a, dtype, static_cast<hipStream_t>(stream)));
 }
 
-// delta | two maxima | parts
+// delta | norms | parts
 size_t lsp_attention_backward_workspace_bytes(const lsp_attention_problem* p, lsp_dtype dtype) {
     if (check_attention_shape(p, dtype) != LSP_OK) return 0;
     lsp::AttentionArgs a = attention_args(p);
     lsp::plan_attention_backward(a, dtype);
-    return delta_bytes(p) + 256 + lsp::attention_backward_partial_bytes(a);
+    return delta_bytes(p) + kNormBytes + lsp::attention_backward_partial_bytes(a);
 }
 
 int lsp_attention_backward(const lsp_attention_problem* p, const lsp_attention_gradients* g, lsp_dtype dtype, void* workspace, size_t workspace_bytes, void* stream) {
@@ -215,8 +216,8 @@ int lsp_attention_backward(const lsp_attention_problem* p, const lsp_attention_g
     a.dk = strided(g->dK, g->dk_stride, p->batch, p->k_len, p->kv_heads);
     a.dv = strided(g->dV, g->dv_stride, p->batch, p->k_len, p->kv_heads);
     a.delta = static_cast<float*>(workspace);
-    a.most = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + delta_bytes(p));
-    a.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + delta_bytes(p) + 256);
+    a.norms = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + delta_bytes(p));
+    a.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + delta_bytes(p) + kNormBytes);
     lsp::plan_attention_backward(a, dtype);
     return done(lsp::launch_attention_backward(a, dtype, static_cast<hipStream_t>(stream)));
 }
