@@ -433,44 +433,56 @@ def lsp_validate_projector(idx, rows, d, r, flag, stream=None, check: bool = Fal
     return rc
 
 
+# ------------------------------------------------------------------ the operators of a training step
+_operators = None
+
+
+def _operator_calls():
+    """The call module with the training operators bound."""
+    global _operators
+    if _operators is None:
+        L, module = lib(), _bound()
+        module.bind_operators(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            L.lsp_dropout, L.lsp_attention_forward, L.lsp_attention_backward, L.lsp_residual_norm_forward, L.lsp_residual_norm_backward)))
+        _operators = module
+    return _operators
+
+
+def _at(descriptor) -> Optional[int]:
+    return None if descriptor is None else ctypes.addressof(descriptor)
+
+
 def lsp_dropout(x, y, rows, width, dropout: float, seed: int, offset: int, dtype: int, stream=None, check: bool = True) -> int:
     """y := drop(x); on a gradient, with the same numbers, its backward pass.  y may be x."""
-    rc = lib().lsp_dropout(_ptr(x), _ptr(y), rows, width, dropout, seed, offset, dtype, _stream(stream))
-    if check:
+    rc = (_operators or _operator_calls()).dropout(x, y, rows, width, dropout, seed, offset, dtype, stream)
+    if check and rc:
         _check(rc, "lsp_dropout")
     return rc
 
 
-def _strides(t):
-    """Strides of batch, position and head of a [batch][position][head][head_dim] tensor, whose last axis must be contiguous."""
-    b, s, h, d = t.stride()
-    if d != 1 and t.shape[3] != 1:
-        raise ValueError("the last axis of Q, K, V, O and their gradients must be contiguous")
-    return _three(b, s, h)
+def _int32(lens, what):
+    if lens is not None and (lens.element_size() != 4 or lens.is_floating_point()):
+        raise ValueError(f"{what}: lengths are int32")
+    return lens
 
 
 def attention_problem(Q, K, V, O, L, *, q_lens=None, k_lens=None, scale: float, causal: bool = False, dropout: float = 0.0,
                       seed: int = 0, offset: int = 0) -> lsp_attention_problem:
     """The descriptor of an attention call from torch tensors: Q, O [batch][q_len][heads][head_dim] and K, V [batch][k_len][kv_heads][head_dim]
-    with any strides whose last is 1, L [batch][heads][q_len] fp32, q_lens and k_lens [batch] int32 or None.  The tensors are kept alive by
-    the caller."""
-    B, Sq, H, D = Q.shape
-    Sk, Hk = K.shape[1], K.shape[2]
-    if K.shape != (B, Sk, Hk, D) or V.shape != K.shape or O.shape != Q.shape or tuple(L.shape) != (B, H, Sq) or not L.is_contiguous():
-        raise ValueError("attention_problem: shapes do not belong together")
-    if not (K.dtype == V.dtype == O.dtype == Q.dtype):
-        raise ValueError("attention_problem: Q, K, V and O are of one type")
-    for lens in (q_lens, k_lens):
-        if lens is not None and (lens.element_size() != 4 or lens.is_floating_point() or lens.numel() != B or not lens.is_contiguous()):
-            raise ValueError("attention_problem: lengths are [batch] int32")
-    return lsp_attention_problem(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), L.data_ptr(), _ptr(q_lens), _ptr(k_lens),
-                                 _strides(Q), _strides(K), _strides(V), _strides(O), B, H, Hk, Sq, Sk, D, int(causal), scale, dropout,
-                                 offset, seed)
+    with any strides whose last is 1, L [batch][heads][q_len] fp32, q_lens and k_lens [batch] int32 or None.  Tensors that do not belong
+    together are a ValueError.  They are kept alive by the caller."""
+    p = lsp_attention_problem()
+    if q_lens is not None or k_lens is not None:
+        _int32(q_lens, "attention_problem"), _int32(k_lens, "attention_problem")
+    (_operators or _operator_calls()).attention_problem(ctypes.addressof(p), Q, K, V, O, L, q_lens, k_lens, scale, causal, dropout, seed, offset)
+    return p
 
 
 def attention_gradients(dO, dQ, dK, dV) -> lsp_attention_gradients:
     """The gradients' descriptor, from tensors shaped as O, Q, K and V."""
-    return lsp_attention_gradients(dO.data_ptr(), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), _strides(dO), _strides(dQ), _strides(dK), _strides(dV))
+    g = lsp_attention_gradients()
+    (_operators or _operator_calls()).attention_gradients(ctypes.addressof(g), dO, dQ, dK, dV)
+    return g
 
 
 def lsp_attention_forward_workspace_bytes(problem, dtype: int) -> int:
@@ -483,58 +495,43 @@ def lsp_attention_backward_workspace_bytes(problem, dtype: int) -> int:
 
 def lsp_attention_forward(problem, dtype: int, workspace=None, workspace_bytes: int = 0, stream=None, check: bool = True) -> int:
     """problem: from attention_problem()."""
-    rc = lib().lsp_attention_forward(ctypes.byref(problem) if problem is not None else None, dtype, _ptr(workspace), workspace_bytes, _stream(stream))
-    if check:
+    rc = (_operators or _operator_calls()).attention_forward(_at(problem), dtype, workspace, workspace_bytes, stream)
+    if check and rc:
         _check(rc, "lsp_attention_forward")
     return rc
 
 
 def lsp_attention_backward(problem, gradients, dtype: int, workspace, workspace_bytes: int, stream=None, check: bool = True) -> int:
     """gradients: from attention_gradients()."""
-    rc = lib().lsp_attention_backward(ctypes.byref(problem) if problem is not None else None, ctypes.byref(gradients) if gradients is not None else None,
-                                      dtype, _ptr(workspace), workspace_bytes, _stream(stream))
-    if check:
+    rc = (_operators or _operator_calls()).attention_backward(_at(problem), _at(gradients), dtype, workspace, workspace_bytes, stream)
+    if check and rc:
         _check(rc, "lsp_attention_backward")
     return rc
-
-
-def _row_stride(t) -> int:
-    if t is None:
-        return 0
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] != 1):
-        raise ValueError("rows of the residual-norm calls are [rows][width] tensors whose last axis is contiguous")
-    return t.stride(0)
 
 
 def residual_norm_problem(x, f, y, h, stats, *, post: str = "none", post_weight=None, post_bias=None, gate=None, pre: str = "none", pre_weight=None,
                           pre_bias=None, eps: float = 1e-5, residual_scale: float = 1.0, branch_scale: float = 1.0, dropout: float = 0.0,
                           seed: int = 0, offset: int = 0) -> lsp_residual_norm_problem:
-    """The descriptor of a residual-norm call from torch tensors: x, f, y, h [rows][width], stats [4][rows] fp32, weights, biases and gate
-    [width] (or None); post and pre are "none", "rms" or "layer".  The tensors are kept alive by the caller."""
-    rows, width = x.shape
-    for t in (f, y, h):
-        if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
-            raise ValueError("residual_norm_problem: x, f, y and h are of one shape and type")
-    for t in (post_weight, post_bias, gate, pre_weight, pre_bias):
-        if t is not None and (t.numel() != width or t.dtype != x.dtype or not t.is_contiguous()):
-            raise ValueError("residual_norm_problem: weights, biases and gate are [width], of the type of x")
-    if stats.numel() != 4 * rows or stats.element_size() != 4 or not stats.is_contiguous():
-        raise ValueError("residual_norm_problem: stats are [4][rows] fp32")
-    return lsp_residual_norm_problem(x.data_ptr(), f.data_ptr(), y.data_ptr(), _ptr(h), stats.data_ptr(), _ptr(post_weight), _ptr(post_bias), _ptr(gate),
-                                     _ptr(pre_weight), _ptr(pre_bias), _row_stride(x), _row_stride(f), _row_stride(y), _row_stride(h), rows, width,
-                                     NORM_KIND[post], NORM_KIND[pre], eps, residual_scale, branch_scale, dropout, offset, seed)
+    """The descriptor of a residual-norm call from torch tensors: x, f, y, h [rows][width] (h may be None), stats [4][rows] fp32, weights, biases and
+    gate [width] (or None); post and pre are "none", "rms" or "layer".  Tensors that do not belong together are a ValueError.  They are kept
+    alive by the caller."""
+    p = lsp_residual_norm_problem()
+    (_operators or _operator_calls()).residual_norm_problem(ctypes.addressof(p), x, f, y, h, stats, post_weight, post_bias, gate, pre_weight, pre_bias, NORM_KIND[post],
+                                                            NORM_KIND[pre], eps, residual_scale, branch_scale, dropout, seed, offset)
+    return p
 
 
 def residual_norm_gradients(dy, dh, dx, df, *, post_weight=None, post_bias=None, gate=None, pre_weight=None, pre_bias=None) -> lsp_residual_norm_gradients:
     """The gradients' descriptor: dy, dh (or None) arrive, dx and df are made, and the fp32 [width] gradients that are asked for."""
-    return lsp_residual_norm_gradients(dy.data_ptr(), _ptr(dh), dx.data_ptr(), df.data_ptr(), _ptr(post_weight), _ptr(post_bias), _ptr(gate),
-                                       _ptr(pre_weight), _ptr(pre_bias), _row_stride(dy), _row_stride(dh), _row_stride(dx), _row_stride(df))
+    g = lsp_residual_norm_gradients()
+    (_operators or _operator_calls()).residual_norm_gradients(ctypes.addressof(g), dy, dh, dx, df, post_weight, post_bias, gate, pre_weight, pre_bias)
+    return g
 
 
 def lsp_residual_norm_forward(problem, dtype: int, stream=None, check: bool = True) -> int:
     """problem: from residual_norm_problem()."""
-    rc = lib().lsp_residual_norm_forward(ctypes.byref(problem) if problem is not None else None, dtype, _stream(stream))
-    if check:
+    rc = (_operators or _operator_calls()).residual_norm_forward(_at(problem), dtype, stream)
+    if check and rc:
         _check(rc, "lsp_residual_norm_forward")
     return rc
 
@@ -545,8 +542,7 @@ def lsp_residual_norm_backward_workspace_bytes(problem, dtype: int) -> int:
 
 def lsp_residual_norm_backward(problem, gradients, dtype: int, workspace, workspace_bytes: int, stream=None, check: bool = True) -> int:
     """gradients: from residual_norm_gradients()."""
-    rc = lib().lsp_residual_norm_backward(ctypes.byref(problem) if problem is not None else None, ctypes.byref(gradients) if gradients is not None else None,
-                                          dtype, _ptr(workspace), workspace_bytes, _stream(stream))
-    if check:
+    rc = (_operators or _operator_calls()).residual_norm_backward(_at(problem), _at(gradients), dtype, workspace, workspace_bytes, stream)
+    if check and rc:
         _check(rc, "lsp_residual_norm_backward")
     return rc
