@@ -24,10 +24,12 @@ struct AttentionArgs {
     const int32_t* q_lens;
     const int32_t* k_lens;
     int32_t batch, heads, kv_heads, group, q_len, k_len, head_dim, causal;
+    int32_t waves;                   // of a forward workgroup: 4 or 8, each with 32 rows
     int32_t tiles;                   // row tiles of a head (or of a key head, where its query heads share the tiles)
     int32_t rows;                    // rows of a head: q_len, or group * q_len where `packed`
     int32_t packed;                  // rows are (query head of the group, query): few queries, all heads of a key head in one tile
-    int32_t splits, split_tiles;     // forward: parts of the keys, tiles of keys in each
+    int32_t few;                     // forward: at most 32 rows, the kernel for these
+    int32_t splits, split_tiles;     // forward: parts of the keys (at most 64), tiles of keys in each
     int32_t norm_slots;              // fp16 backward: slots in use
     int32_t key_parts, query_parts;  // backward: workgroups that share 128 keys (parts of their queries), and 128 queries (parts of their keys)
     float   scale, scale_log2;       // scale_log2 = scale * log2(e): probabilities are powers of two
@@ -42,9 +44,9 @@ size_t attention_partial_bytes(const AttentionArgs& a);
 void plan_attention_backward(AttentionArgs& a, lsp_dtype dtype);
 size_t attention_backward_partial_bytes(const AttentionArgs& a);
 
-constexpr int kRowsForward = 128;    // query rows of a workgroup: four waves of 32
+constexpr int kWaveRows = 32;        // query rows (or keys, where dK and dV are made) of a wave
+constexpr int kBackwardRows = 4 * kWaveRows;
 constexpr int kNormSlots = 1024;
-constexpr int kKeysBackward = 128;   // keys of a workgroup of the kernel that makes dK and dV
 
 // Keys (forward, dQ) or queries (dK, dV) of a tile in LDS
 template <typename D> constexpr int tile_rows() { return D::size == 2 ? 64 : 32; }

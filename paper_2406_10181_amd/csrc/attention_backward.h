@@ -101,22 +101,23 @@ __host__ __device__ static inline float* query_partial(const AttentionArgs& a) {
 template <typename D, int DP, bool DROP>
 __device__ __forceinline__ void attention_dq(const AttentionArgs& a, uint32_t block, uint8_t* smem) {
     using T = Tile<D, DP>;
+    constexpr int kRows = kBackwardRows;
     constexpr int BN = tile_rows<D>(), NT = 256, kSteps = DP / 16, kTiles = BN / 32, kCols = DP / 32;
     constexpr uint32_t kTileBytes = BN * T::kRowBytes;
     const Lds lds = (Lds)smem;                                                            // K | V, twice
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     int unit, tile;
-    const int tiles = (a.q_len + kRowsForward - 1) / kRowsForward;
+    const int tiles = (a.q_len + kRows - 1) / kRows;
     work_of_block(block, (uint32_t)a.batch * a.heads * a.query_parts, tiles, unit, tile);
     const int row_tile = tiles - 1 - tile;
     const int part = unit % a.query_parts, head = unit / a.query_parts % a.heads, b = unit / a.query_parts / a.heads, kv_head = head / a.group;
     const int nq = valid_length(a.q_lens, b, a.q_len), nk = valid_length(a.k_lens, b, a.k_len), ahead = nk - nq;
 
-    const int first = row_tile * kRowsForward + wave * 32, qi = first + (lane & 31);
+    const int first = row_tile * kRows + wave * 32, qi = first + (lane & 31);
     const bool counts = qi < nq;
     const int limit = counts ? (a.causal ? min(nk, qi + ahead + 1) : nk) : 0;
-    const int last_row = min(row_tile * kRowsForward + kRowsForward, nq) - 1;
-    const int end_all = row_tile * kRowsForward >= nq ? 0 : max(0, a.causal ? min(nk, last_row + ahead + 1) : nk);
+    const int last_row = min(row_tile * kRows + kRows, nq) - 1;
+    const int end_all = row_tile * kRows >= nq ? 0 : max(0, a.causal ? min(nk, last_row + ahead + 1) : nk);
     const int tiles_k = (end_all + BN - 1) / BN;                                          // of which this part has an equal share
     const int begin = tiles_k * part / a.query_parts * BN, end = min(end_all, tiles_k * (part + 1) / a.query_parts * BN);
     const int most = first >= nq ? 0 : a.causal ? min(nk, min(first + 31, nq - 1) + ahead + 1) : nk;
@@ -151,7 +152,7 @@ __device__ __forceinline__ void attention_dq(const AttentionArgs& a, uint32_t bl
             for (int ks = 0; ks < kSteps; ++ks) { qf[ks] = global_frag(p, ks, a.head_dim, lane); gf[ks] = global_frag(g, ks, a.head_dim, lane); }
         } else {
             // the wave's queries and their gradients come through the buffers, each through half of them
-            const Lds rows = lds + wave * 32 * T::kRowBytes, others = rows + 2 * kTileBytes;
+            const Lds rows = lds + wave * 32 * T::kRowBytes, others = rows + kRows * T::kRowBytes;
             const auto fetch_rows = [&](const Strided& from, Lds to) {
                 const uint32_t row_bytes = (uint32_t)(from.position * D::size);
                 fetch_wave_rows<D, DP>(buffer_from(at<D>(from, b, first, head)), to, a.head_dim, lane, [&](uint32_t r) { return first + (int)r < nq ? r * row_bytes : kNowhere; });
@@ -252,24 +253,41 @@ __global__ __launch_bounds__(256) void k_attention_add(const float* parts_at, St
 template <typename D, int DP> constexpr bool values_in_lds() { return D::size == 2 && DP > 96; }
 template <typename D, int DP> constexpr int queries_at_once() { return values_in_lds<D, DP>() ? 32 : tile_rows<D>(); }
 
+// LDS of attention_dkv: two buffers, where K (and V) come through before and the results go through after; the bits; V
+template <typename D, int DP> constexpr uint32_t dkv_bits_at() {
+    constexpr uint32_t row = Tile<D, DP>::kRowBytes, buffers = 2 * queries_at_once<D, DP>() * (2 * row + 8);
+    constexpr uint32_t rows = kBackwardRows * row * (values_in_lds<D, DP>() || D::size == 4 ? 1 : 2);
+    return buffers > rows ? buffers : rows;
+}
+template <typename D, int DP> constexpr uint32_t dkv_lds() {
+    return dkv_bits_at<D, DP>() + 512 + (values_in_lds<D, DP>() ? kBackwardRows * Tile<D, DP>::kRowBytes : 0);
+}
+// and of attention_dq: two buffers, where Q and dO come through before
+template <typename D, int DP> constexpr uint32_t dq_lds() {
+    constexpr uint32_t tiles = 4 * tile_rows<D>(), rows = kBackwardRows * (D::size == 2 ? 2 : 1);
+    return (tiles > rows ? tiles : rows) * Tile<D, DP>::kRowBytes;
+}
+
 template <typename D, int DP, bool DROP>
 __device__ __forceinline__ void attention_dkv(const AttentionArgs& a, uint32_t block, uint8_t* smem) {
     using T = Tile<D, DP>;
     constexpr bool kValuesInLds = values_in_lds<D, DP>();
+    constexpr int kKeys = kBackwardRows;
     constexpr int BQ = queries_at_once<D, DP>(), NT = 256, kSteps = DP / 16, kTiles = BQ / 32, kCols = DP / 32;
     constexpr uint32_t kTileBytes = BQ * T::kRowBytes, kBufBytes = 2 * kTileBytes + BQ * 8;
+    constexpr uint32_t kBits = dkv_bits_at<D, DP>();                               // where the bits of dropout lie; V, if it stays, behind them
     const Lds lds = (Lds)smem;                                                            // Q | dO | L | delta, twice; bits of kept ones of each wave
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     int unit, key_tile;                                                                   // (causal: the first keys have the most queries)
-    work_of_block(block, (uint32_t)a.batch * a.kv_heads * a.key_parts, (a.k_len + kKeysBackward - 1) / kKeysBackward, unit, key_tile);
+    work_of_block(block, (uint32_t)a.batch * a.kv_heads * a.key_parts, (a.k_len + kKeys - 1) / kKeys, unit, key_tile);
     const int part = unit % a.key_parts, kv_head = unit / a.key_parts % a.kv_heads, b = unit / a.key_parts / a.kv_heads;
     const int nq = valid_length(a.q_lens, b, a.q_len), nk = valid_length(a.k_lens, b, a.k_len), ahead = nk - nq;
 
-    const int first = key_tile * kKeysBackward + wave * 32, key = first + (lane & 31);
+    const int first = key_tile * kKeys + wave * 32, key = first + (lane & 31);
     const bool counts = key < nk;
     // queries from key - ahead on see the key; the workgroup's tiles begin at a multiple of BQ
-    const int begin = a.causal ? max(0, key_tile * kKeysBackward - ahead) / BQ * BQ : 0;
-    const int end = key_tile * kKeysBackward < nk ? nq : 0;
+    const int begin = a.causal ? max(0, key_tile * kKeys - ahead) / BQ * BQ : 0;
+    const int end = key_tile * kKeys < nk ? nq : 0;
     const int from = a.causal ? max(0, first - ahead) : 0;                                // the wave's first query
     const int all_from = a.causal ? first + 31 - ahead : 0;                               // from here on every key of the wave is seen
     const int my_from = a.causal ? key - ahead : 0;
@@ -308,7 +326,7 @@ __device__ __forceinline__ void attention_dkv(const AttentionArgs& a, uint32_t b
         const Reader<D, DP> read(lane);
         Frag<D> kf[kSteps], vf[kValuesInLds ? 1 : kSteps];
         const Lds rows = lds + wave * 32 * T::kRowBytes;
-        const Lds values = kValuesInLds ? rows + 2 * kBufBytes + 512 : rows + kKeysBackward * T::kRowBytes;
+        const Lds values = kValuesInLds ? rows + kBits + 512 : rows + kKeys * T::kRowBytes;
         if constexpr (D::size == 4) {
             const uint8_t* p = counts ? at<D>(a.k, b, key, kv_head) : nullptr;
             const uint8_t* v = counts ? at<D>(a.v, b, key, kv_head) : nullptr;
@@ -367,7 +385,7 @@ __device__ __forceinline__ void attention_dkv(const AttentionArgs& a, uint32_t b
                     f32x16 pd = s;
                     if constexpr (DROP) {
                         // eight lanes share a block of eight keys: of the 16 queries that they all have, each lane makes two; the bits go round by LDS
-                        const Lds bits = lds + 2 * kBufBytes + wave * 128 + (lane >> 3) * 16;
+                        const Lds bits = lds + kBits + wave * 128 + (lane >> 3) * 16;
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
                             const int x = (lane & 7) + 8 * half;
@@ -452,9 +470,8 @@ __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_atte
 
 template <typename D, int DP, bool DROP> static hipError_t run_attention_backward(AttentionArgs a, hipStream_t st) {
     constexpr auto kern = k_attention_backward<D, DP, DROP>;
-    constexpr size_t lds_dkv = queries_at_once<D, DP>() * (4 * Tile<D, DP>::kRowBytes + 16) + 512 + (values_in_lds<D, DP>() ? kKeysBackward * Tile<D, DP>::kRowBytes : 0);
-    constexpr size_t lds_dq = 4 * (size_t)tile_rows<D>() * Tile<D, DP>::kRowBytes;
-    constexpr size_t lds = lds_dkv > lds_dq ? lds_dkv : lds_dq;
+    constexpr int kRows = kBackwardRows;
+    constexpr size_t lds = dkv_lds<D, DP>() > dq_lds<D, DP>() ? dkv_lds<D, DP>() : dq_lds<D, DP>();
     hipError_t e = allow_dynamic_lds<kern, lds>();
     if (e != hipSuccess) return e;
     const bool norms = std::is_same<D, F16>::value;
@@ -464,8 +481,8 @@ template <typename D, int DP, bool DROP> static hipError_t run_attention_backwar
     a.norm_slots = (int32_t)grid;
     hipLaunchKernelGGL(k_attention_delta<D>, dim3((unsigned)grid), dim3(256), 0, st, a, o_blocks, blocks);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    const int64_t key_items = (int64_t)a.batch * a.kv_heads * ((a.k_len + kKeysBackward - 1) / kKeysBackward) * a.key_parts;
-    const int64_t query_items = (int64_t)a.batch * a.heads * ((a.q_len + kRowsForward - 1) / kRowsForward) * a.query_parts;
+    const int64_t key_items = (int64_t)a.batch * a.kv_heads * ((a.k_len + kRows - 1) / kRows) * a.key_parts;
+    const int64_t query_items = (int64_t)a.batch * a.heads * ((a.q_len + kRows - 1) / kRows) * a.query_parts;
     hipLaunchKernelGGL(kern, dim3((unsigned)(key_items + query_items)), dim3(256), lds, st, a, (uint32_t)key_items);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     const auto add = [&](const float* from, const Strided& out, int parts, int heads, int len) {
@@ -480,12 +497,12 @@ template <typename D, int DP, bool DROP> static hipError_t run_attention_backwar
     return a.query_parts > 1 ? add(query_partial(a), a.dq, a.query_parts, a.heads, a.q_len) : hipSuccess;
 }
 
+template <typename D, int DP> static hipError_t run_attention_backward(const AttentionArgs& a, hipStream_t st) {
+    return a.drop.limit ? run_attention_backward<D, DP, true>(a, st) : run_attention_backward<D, DP, false>(a, st);
+}
 template <typename D> hipError_t attention_backward_of(const AttentionArgs& a, hipStream_t st) {
-    const bool drop = a.drop.limit != 0;
-    if (a.head_dim <= 32) return drop ? run_attention_backward<D, 32, true>(a, st) : run_attention_backward<D, 32, false>(a, st);
-    if (a.head_dim <= 64) return drop ? run_attention_backward<D, 64, true>(a, st) : run_attention_backward<D, 64, false>(a, st);
-    if (a.head_dim <= 96) return drop ? run_attention_backward<D, 96, true>(a, st) : run_attention_backward<D, 96, false>(a, st);
-    return drop ? run_attention_backward<D, 128, true>(a, st) : run_attention_backward<D, 128, false>(a, st);
+    return a.head_dim <= 32 ? run_attention_backward<D, 32>(a, st) : a.head_dim <= 64 ? run_attention_backward<D, 64>(a, st)
+         : a.head_dim <= 96 ? run_attention_backward<D, 96>(a, st) : run_attention_backward<D, 128>(a, st);
 }
 
 }  // namespace lsp

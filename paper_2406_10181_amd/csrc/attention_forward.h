@@ -1,6 +1,6 @@
 // The forward pass of attention: one pass over the keys with a running maximum and sum for each query.
 //
-// A workgroup has 128 query rows of a head, a wave 32 of them; tiles of keys and values go by in LDS, the next one on its way in registers
+// A workgroup has 128 or 256 query rows of a head, a wave 32 of them; tiles of keys and values go by in LDS, the next one on its way in registers
 // while the matrix cores work on the current.  The scores are made transposed, S^T = K Q^T: a lane then has all its scores (16 of every 32
 // keys; lane l ^ 32 has the others) of ONE query, so maxima and sums stay in the lane, and the accumulators are the operand of
 // O^T += V^T P^T as they are.
@@ -9,7 +9,7 @@
 // neither their sum in fp32 nor their rounding minds, and the accumulators are left alone.
 #pragma once
 
-#include "attention.h"
+#include "attention_few.h"
 
 #if defined(__HIPCC__)
 namespace lsp {
@@ -33,10 +33,11 @@ __device__ __forceinline__ void drop_keys(f32x16& s, int pair, uint32_t key0, ui
     }
 }
 
-template <typename D, int DP, bool DROP>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_attention_forward(const AttentionArgs a) {
+template <typename D, int DP, bool DROP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_attention_forward(const AttentionArgs a) {
     using T = Tile<D, DP>;
-    constexpr int BN = tile_rows<D>(), NT = 256, kSteps = DP / 16, kTiles = BN / 32, kCols = DP / 32;
+    constexpr int kRows = WAVES * kWaveRows;
+    constexpr int BN = tile_rows<D>(), NT = 64 * WAVES, kSteps = DP / 16, kTiles = BN / 32, kCols = DP / 32;
     constexpr uint32_t kTileBytes = BN * T::kRowBytes;
     extern __shared__ __align__(16) uint8_t smem[];
     const Lds lds = (Lds)smem;                                                            // K | V, twice
@@ -52,7 +53,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int ahead = nk - nq;                                                            // query i sees keys up to i + ahead
 
     // this lane's row
-    const int row = row_tile * kRowsForward + wave * 32 + (lane & 31);
+    const int row = row_tile * kRows + wave * 32 + (lane & 31);
     const int q_head = a.packed ? kv_head * a.group + row / a.q_len : head;
     const int qi = a.packed ? row % a.q_len : row;
     const bool counts = row < a.rows && qi < nq;
@@ -61,15 +62,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     int most, least;                                                                      // of the wave
     if (a.packed || !a.causal) { most = nk; least = a.causal ? min(nk, ahead + 1) : nk; }
     else {
-        const int first = row_tile * kRowsForward + wave * 32;
+        const int first = row_tile * kRows + wave * 32;
         most = min(nk, min(first + 31, nq - 1) + ahead + 1);
         least = min(nk, first + ahead + 1);
     }
-    const int last_row = min(row_tile * kRowsForward + kRowsForward, nq) - 1;
+    const int last_row = min(row_tile * kRows + kRows, nq) - 1;
     const int end_all = a.packed || !a.causal ? nk : min(nk, last_row + ahead + 1);
     const int begin = split * a.split_tiles * BN;
     const int end = min(end_all, begin + a.split_tiles * BN);
-    if (!a.packed && row_tile * kRowsForward >= nq) most = 0;
+    if (!a.packed && row_tile * kRows >= nq) most = 0;
 
     f32x16 o[kCols];
 #pragma unroll
@@ -83,21 +84,22 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     Fetch<D, DP, BN, NT> fetch_k, fetch_v;
     fetch_k.setup((uint32_t)k_bytes, a.head_dim, wave, lane);
     fetch_v.setup((uint32_t)v_bytes, a.head_dim, wave, lane);
-    const bool any = begin < end && (a.packed || row_tile * kRowsForward < nq);
+    const bool any = begin < end && (a.packed || row_tile * kRows < nq);
     const Reader<D, DP> read(lane);
     const bool all_count = __all(counts);
     if (any) {
-        fetch_k(kp + begin * k_bytes, nk - begin, lds, wave);
-        fetch_v(vp + begin * v_bytes, nk - begin, lds + kTileBytes, wave);
         Frag<D> qf[kSteps];
         if constexpr (D::size == 4) {
             const uint8_t* p = counts ? at<D>(a.q, b, qi, q_head) : nullptr;
 #pragma unroll
             for (int ks = 0; ks < kSteps; ++ks) qf[ks] = global_frag(p, ks, a.head_dim, lane);
-        } else {
+        }
+        fetch_k(kp + begin * k_bytes, nk - begin, lds, wave);
+        fetch_v(vp + begin * v_bytes, nk - begin, lds + kTileBytes, wave);
+        if constexpr (D::size == 2) {
             // the wave's queries come through the second buffer while the first keys are on their way into the first
             const Lds rows = lds + 2 * kTileBytes + wave * 32 * T::kRowBytes;
-            const int wave_row = row_tile * kRowsForward + wave * 32;
+            const int wave_row = row_tile * kRows + wave * 32;
             const uint32_t q_bytes = (uint32_t)(a.q.position * D::size);
             const Buffer q = buffer_from(at<D>(a.q, b, a.packed ? 0 : wave_row, a.packed ? kv_head * a.group : head));
             fetch_wave_rows<D, DP>(q, rows, a.head_dim, lane, [&](uint32_t r) {
@@ -218,7 +220,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         return;
     }
     const float inv = l == 0.0f ? 0.0f : (DROP ? a.drop.scale : 1.0f) / l;
-    const int wave_row = row_tile * kRowsForward + wave * 32;
+    const int wave_row = row_tile * kRows + wave * 32;
     store_wave_rows<D, DP>(o, inv, lds + wave * 32 * T::kRowBytes, a.head_dim, lane, [&](uint32_t r) -> uint8_t* {
         const int n = wave_row + (int)r;
         if (n >= a.rows) return nullptr;
@@ -227,24 +229,31 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     if (h == 0 && row < a.rows) a.L[((int64_t)b * a.heads + q_head) * a.q_len + qi] = l == 0.0f ? -INFINITY : m * a.scale + __logf(l);
 }
 
-// Joins the parts of a row: O = sum_s w_s O_s / sum_s w_s l_s with w_s = 2^(m_s - m).  A wave has a row, a lane two columns.
+// Joins the parts of a row: O = sum_s w_s O_s / sum_s w_s l_s with w_s = 2^(m_s - m).  A wave has a row: its lanes have a part's (m, l) each, and then two columns.
 template <typename D>
 __global__ __launch_bounds__(256) void k_attention_join(const AttentionArgs a) {
     const int64_t lines = (int64_t)a.batch * a.heads * a.q_len;
-    const int64_t line = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t line = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (line >= lines) return;
     const int lane = threadIdx.x & 63, col = 2 * lane;
     const f32x2* ml = reinterpret_cast<const f32x2*>(a.partial + a.splits * lines * a.head_dim);
-    float m = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[s * lines + line][0]);
-    float l = 0.0f, x = 0.0f, y = 0.0f;
-    for (int s = 0; s < a.splits; ++s) {
-        const f32x2 part = ml[s * lines + line];
-        const float w = part[0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((part[0] - m) * a.scale_log2);
-        l += w * part[1];
-        if (col < a.head_dim) {
-            const f32x2 o = *reinterpret_cast<const f32x2*>(a.partial + (s * lines + line) * a.head_dim + col);
-            x += w * o[0]; y += w * o[1];
+    const f32x2 part = lane < a.splits ? ml[lane * lines + line] : f32x2{-INFINITY, 0.0f};       // (there are at most 64 parts)
+    float m = part[0];
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
+    const float w = part[0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((part[0] - m) * a.scale_log2);
+    float l = w * part[1], x = 0.0f, y = 0.0f;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) l += __shfl_xor(l, s);
+    const float* o = a.partial + line * a.head_dim + min(col, a.head_dim - 2);
+    for (int s = 0; s < a.splits; s += 4) {                                               // (a part past the last has no weight)
+        f32x2 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const f32x2*>(o + min(s + k, a.splits - 1) * lines * a.head_dim);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float f = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), min(s + k, 63)));
+            x = s + k < a.splits ? fmaf(f, v[k][0], x) : x; y = s + k < a.splits ? fmaf(f, v[k][1], y) : y;
         }
     }
     const float inv = l == 0.0f ? 0.0f : a.drop.scale / l;
@@ -257,25 +266,38 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttentionArgs a) {
     if (lane == 0) a.L[line] = l == 0.0f ? -INFINITY : m * a.scale + __logf(l);
 }
 
-template <typename D, int DP, bool DROP> static hipError_t run_attention_forward(const AttentionArgs& a, hipStream_t st) {
-    constexpr auto kern = k_attention_forward<D, DP, DROP>;
-    constexpr size_t lds = 4 * (size_t)tile_rows<D>() * Tile<D, DP>::kRowBytes;
-    hipError_t e = allow_dynamic_lds<kern, lds>();
-    if (e != hipSuccess) return e;
-    const int64_t items = (int64_t)a.batch * (a.packed ? a.kv_heads : a.heads) * a.tiles * a.splits;
-    hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(256), lds, st, a);
-    if ((e = hipGetLastError()) != hipSuccess || a.splits == 1) return e;
+template <typename D> static hipError_t run_attention_join(const AttentionArgs& a, hipStream_t st) {
     const int64_t lines = (int64_t)a.batch * a.heads * a.q_len;
     hipLaunchKernelGGL(k_attention_join<D>, dim3((unsigned)((lines + 3) / 4)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
+template <typename D, int DP, bool DROP, int WAVES> static hipError_t run_attention_forward(const AttentionArgs& a, hipStream_t st) {
+    constexpr auto kern = k_attention_forward<D, DP, DROP, WAVES>;
+    // two buffers of keys and values; the second is where the queries come through, and the results go through all of it
+    constexpr size_t tiles = 4 * (size_t)tile_rows<D>(), rows = D::size == 2 ? tiles / 2 + WAVES * kWaveRows : WAVES * kWaveRows;
+    constexpr size_t lds = (tiles > rows ? tiles : rows) * Tile<D, DP>::kRowBytes;
+    hipError_t e = allow_dynamic_lds<kern, lds>();
+    if (e != hipSuccess) return e;
+    const int64_t items = (int64_t)a.batch * (a.packed ? a.kv_heads : a.heads) * a.tiles * a.splits;
+    hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(64 * WAVES), lds, st, a);
+    return hipGetLastError();
+}
+
+template <typename D, int DP, int WAVES> static hipError_t run_attention_forward(const AttentionArgs& a, hipStream_t st) {
+    return a.drop.limit ? run_attention_forward<D, DP, true, WAVES>(a, st) : run_attention_forward<D, DP, false, WAVES>(a, st);
+}
+template <typename D, int WAVES> static hipError_t run_attention_forward(const AttentionArgs& a, hipStream_t st) {
+    return a.head_dim <= 32 ? run_attention_forward<D, 32, WAVES>(a, st) : a.head_dim <= 64 ? run_attention_forward<D, 64, WAVES>(a, st)
+         : a.head_dim <= 96 ? run_attention_forward<D, 96, WAVES>(a, st) : run_attention_forward<D, 128, WAVES>(a, st);
+}
 template <typename D> hipError_t attention_forward_of(const AttentionArgs& a, hipStream_t st) {
-    const bool drop = a.drop.limit != 0;
-    if (a.head_dim <= 32) return drop ? run_attention_forward<D, 32, true>(a, st) : run_attention_forward<D, 32, false>(a, st);
-    if (a.head_dim <= 64) return drop ? run_attention_forward<D, 64, true>(a, st) : run_attention_forward<D, 64, false>(a, st);
-    if (a.head_dim <= 96) return drop ? run_attention_forward<D, 96, true>(a, st) : run_attention_forward<D, 96, false>(a, st);
-    return drop ? run_attention_forward<D, 128, true>(a, st) : run_attention_forward<D, 128, false>(a, st);
+    hipError_t e;
+    if constexpr (D::size == 2) e = a.few ? run_attention_few<D>(a, st)
+                                  : a.waves == 8 ? (a.head_dim <= 96 ? run_attention_forward<D, 96, 8>(a, st) : run_attention_forward<D, 128, 8>(a, st))
+                                                 : run_attention_forward<D, 4>(a, st);
+    else e = run_attention_forward<D, 4>(a, st);
+    return e != hipSuccess || a.splits == 1 ? e : run_attention_join<D>(a, st);
 }
 
 }  // namespace lsp

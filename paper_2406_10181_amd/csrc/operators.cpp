@@ -24,28 +24,38 @@ size_t attention_partial_bytes(const AttentionArgs& a) {
     return align_up((size_t)a.splits * a.batch * a.heads * a.q_len * ((size_t)a.head_dim + 2) * sizeof(float), 256);
 }
 
+// Eight waves a workgroup for wide heads and long texts, where that leaves every CU a workgroup: a tile of keys serves twice the queries.  16 heads of 128, one text of
+// 8192, bf16: 266 us, with four waves 282; 32 heads, four texts of 1024: 51.5 both; 16 heads of 64, eight texts of 2048: 187 and 179; padded texts of 777: 39 and 29.
+static int waves_for(int64_t units, int64_t rows, int64_t keys, int head_dim, lsp_dtype dtype) {
+    return dtype != LSP_F32 && head_dim > 64 && keys >= 2048 && units * ((rows + 8 * kWaveRows - 1) / (8 * kWaveRows)) >= 256 ? 8 : 4;
+}
+
 void plan_attention_forward(AttentionArgs& a, lsp_dtype dtype) {
     // Few queries: the query heads that share a key head go into one tile of rows, so that keys and values are read once for all of them.
     // (Its rows are addressed with 32 bits from the first head's first row.)
-    a.packed = a.group > 1 && (int64_t)a.group * a.q_len <= kRowsForward && ((int64_t)a.group * a.q.head + (int64_t)a.q_len * a.q.position) * 4 < ((int64_t)1 << 31);
+    a.packed = a.group > 1 && (int64_t)a.group * a.q_len <= 4 * kWaveRows && ((int64_t)a.group * a.q.head + (int64_t)a.q_len * a.q.position) * 4 < ((int64_t)1 << 31);
     a.rows = a.packed ? a.group * a.q_len : a.q_len;
-    a.tiles = (a.rows + kRowsForward - 1) / kRowsForward;
-    // Few tiles of rows: the keys are split, as far as that gives each CU two workgroups and each of these four tiles of keys.
-    const int64_t row_tiles = (int64_t)a.batch * (a.packed ? a.kv_heads : a.heads) * a.tiles;
-    const int key_tiles = (a.k_len + tile_rows_of(dtype) - 1) / tile_rows_of(dtype);
-    int splits = (int)std::min<int64_t>(std::max<int64_t>(512 / row_tiles, 1), std::max(key_tiles / 4, 1));
+    const int64_t units = (int64_t)a.batch * (a.packed ? a.kv_heads : a.heads);
+    a.few = dtype != LSP_F32 && a.rows <= 32 && a.drop.limit == 0;
+    a.waves = a.packed ? 4 : waves_for(units, a.rows, a.k_len, a.head_dim, dtype);
+    a.tiles = a.few ? 1 : (int)((a.rows + a.waves * kWaveRows - 1) / (a.waves * kWaveRows));
+    // Few tiles of rows: the keys are split, as far as that gives each CU two workgroups (few queries: four) and each of these four tiles of keys (two a wave).
+    const int tile = a.few ? 32 : tile_rows_of(dtype);
+    const int64_t row_tiles = units * a.tiles;
+    const int key_tiles = (a.k_len + tile - 1) / tile;
+    const int splits = a.waves == 8 ? 1 : (int)std::min<int64_t>({std::max<int64_t>((a.few ? 1024 : 512) / row_tiles, 1), std::max(key_tiles / (a.few ? 8 : 4), 1), 64});
     a.split_tiles = (key_tiles + splits - 1) / splits;
     a.splits = (key_tiles + a.split_tiles - 1) / a.split_tiles;
 }
 
-// Workgroups of the backward kernels that share a tile: as many as give each CU two, with four steps or more each.  What they add up goes through memory in
+// Workgroups of the backward pass that share a tile: as many as give each CU two, with four steps or more each.  What they add up goes through memory in
 // fp32, two more passes over the gradient a part.
 static int parts_for(int64_t tiles, int64_t steps) {
     return (int)std::min<int64_t>({std::max<int64_t>(512 / tiles, 1), std::max<int64_t>(steps / 4, 1), 16});
 }
 void plan_attention_backward(AttentionArgs& a, lsp_dtype dtype) {
-    const int64_t key_tiles = (int64_t)a.batch * a.kv_heads * ((a.k_len + kKeysBackward - 1) / kKeysBackward);
-    const int64_t query_tiles = (int64_t)a.batch * a.heads * ((a.q_len + kRowsForward - 1) / kRowsForward);
+    const int64_t key_tiles = (int64_t)a.batch * a.kv_heads * ((a.k_len + kBackwardRows - 1) / kBackwardRows);
+    const int64_t query_tiles = (int64_t)a.batch * a.heads * ((a.q_len + kBackwardRows - 1) / kBackwardRows);
     a.key_parts = parts_for(key_tiles, (int64_t)a.group * ((a.q_len + tile_rows_of(dtype) - 1) / tile_rows_of(dtype)));
     a.query_parts = parts_for(query_tiles, (a.k_len + tile_rows_of(dtype) - 1) / tile_rows_of(dtype));
 }
