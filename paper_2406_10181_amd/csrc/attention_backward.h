@@ -233,19 +233,24 @@ __device__ __forceinline__ void attention_dq(const AttentionArgs& a, uint32_t bl
                            [&](uint32_t r) -> uint8_t* { return first + (int)r < a.q_len ? const_cast<uint8_t*>(at<D>(a.dq, b, first + (int)r, head)) : nullptr; });
 }
 
-// Adds the parts of a gradient, in order: `lines` rows of (batch, head, position).  A thread has four columns.
+// Adds the parts of gradients, in order: `heads` x `len` rows of every batch each.  A thread has four columns, blockIdx.y is the gradient.
+struct GradientParts { const float* from; Strided out; int32_t parts, heads, len; };
+struct AddArgs { GradientParts g[3]; int32_t batch, head_dim; };
 template <typename D>
-__global__ __launch_bounds__(256) void k_attention_add(const float* parts_at, Strided out, int parts, int batch, int heads, int len, int head_dim) {
-    const int64_t lines = (int64_t)batch * heads * len, quads = head_dim / 4;
+__global__ __launch_bounds__(256) void k_attention_add(const AddArgs a) {
+    const GradientParts& g = a.g[blockIdx.y];
+    const int64_t lines = (int64_t)a.batch * g.heads * g.len;
+    const int quads = a.head_dim / 4;
     const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (n >= lines * quads) return;
     const int64_t line = n / quads;
     const int col = (int)(n - line * quads) * 4;
-    f32x4 sum = *reinterpret_cast<const f32x4*>(parts_at + line * head_dim + col);
-    for (int p = 1; p < parts; ++p) sum += *reinterpret_cast<const f32x4*>(parts_at + (p * lines + line) * head_dim + col);
-    const int64_t head_line = line / len;
-    const int i = (int)(line - head_line * len), b = (int)(head_line / heads), head = (int)(head_line - (int64_t)b * heads);
-    store_four<D>(const_cast<uint8_t*>(at<D>(out, b, i, head)) + col * D::size, sum[0], sum[1], sum[2], sum[3]);
+    const float* from = g.from + line * a.head_dim + col;
+    f32x4 sum = *reinterpret_cast<const f32x4*>(from);
+    for (int p = 1; p < g.parts; ++p) sum += *reinterpret_cast<const f32x4*>(from + p * lines * a.head_dim);
+    const int64_t head_line = line / g.len;
+    const int i = (int)(line - head_line * g.len), b = (int)(head_line / g.heads), head = (int)(head_line - (int64_t)b * g.heads);
+    store_four<D>(const_cast<uint8_t*>(at<D>(g.out, b, i, head)) + col * D::size, sum[0], sum[1], sum[2], sum[3]);
 }
 
 // At head_dim 128 in 16 bits K and V of a wave's keys, dK, dV and the scores are more than the 256 registers that two waves a SIMD have: V stays in
@@ -460,7 +465,8 @@ __device__ __forceinline__ void attention_dkv(const AttentionArgs& a, uint32_t b
                            [&](uint32_t r) -> uint8_t* { return first + (int)r < a.k_len ? const_cast<uint8_t*>(at<D>(a.dv, b, first + (int)r, kv_head)) : nullptr; });
 }
 
-// Both in one launch, dK and dV first: neither waits for the other, and the last workgroups of the one leave no CU idle.
+// Both kinds in one launch, dK and dV first: neither waits for the other, and the last workgroups of the one leave no CU idle.  (In turns, with the longest of both
+// kinds first, what is read is shared less: 178 instead of 150 us for four texts of 1024 with 32 heads of 128.)
 template <typename D, int DP, bool DROP>
 __global__ __launch_bounds__(256, (D::size == 4 && DP > 32 ? 1 : 2)) void k_attention_backward(const AttentionArgs a, uint32_t key_items) {
     extern __shared__ __align__(16) uint8_t smem[];
@@ -485,16 +491,22 @@ template <typename D, int DP, bool DROP> static hipError_t run_attention_backwar
     const int64_t query_items = (int64_t)a.batch * a.heads * ((a.q_len + kRows - 1) / kRows) * a.query_parts;
     hipLaunchKernelGGL(kern, dim3((unsigned)(key_items + query_items)), dim3(256), lds, st, a, (uint32_t)key_items);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    const auto add = [&](const float* from, const Strided& out, int parts, int heads, int len) {
-        const int64_t threads = (int64_t)a.batch * heads * len * (a.head_dim / 4);
-        hipLaunchKernelGGL(k_attention_add<D>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, from, out, parts, a.batch, heads, len, a.head_dim);
-        return hipGetLastError();
+    AddArgs add{};
+    add.batch = a.batch; add.head_dim = a.head_dim;
+    int gradients = 0;
+    int64_t rows = 0;
+    const auto also = [&](const float* from, const Strided& out, int parts, int heads, int len) {
+        add.g[gradients++] = {from, out, parts, heads, len};
+        rows = std::max(rows, (int64_t)a.batch * heads * len);
     };
     if (a.key_parts > 1) {
-        if ((e = add(a.partial, a.dk, a.key_parts, a.kv_heads, a.k_len)) != hipSuccess) return e;
-        if ((e = add(a.partial + (int64_t)a.key_parts * a.batch * a.kv_heads * a.k_len * a.head_dim, a.dv, a.key_parts, a.kv_heads, a.k_len)) != hipSuccess) return e;
+        also(a.partial, a.dk, a.key_parts, a.kv_heads, a.k_len);
+        also(a.partial + (int64_t)a.key_parts * a.batch * a.kv_heads * a.k_len * a.head_dim, a.dv, a.key_parts, a.kv_heads, a.k_len);
     }
-    return a.query_parts > 1 ? add(query_partial(a), a.dq, a.query_parts, a.heads, a.q_len) : hipSuccess;
+    if (a.query_parts > 1) also(query_partial(a), a.dq, a.query_parts, a.heads, a.q_len);
+    if (!gradients) return hipSuccess;
+    hipLaunchKernelGGL(k_attention_add<D>, dim3((unsigned)((rows * (a.head_dim / 4) + 255) / 256), (unsigned)gradients), dim3(256), 0, st, add);
+    return hipGetLastError();
 }
 
 template <typename D, int DP> static hipError_t run_attention_backward(const AttentionArgs& a, hipStream_t st) {

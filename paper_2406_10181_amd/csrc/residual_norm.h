@@ -13,7 +13,7 @@ struct ResidualNormArgs {
     float* grads[5];                                     // of pre_w, pre_b, gate, post_w, post_b; NULL: not asked for
     int64_t x_stride, f_stride, y_stride, h_stride, dy_stride, dh_stride, dx_stride, df_stride;
     int64_t rows;
-    int32_t width, post, pre;
+    int32_t width, post, pre, many;                      // many: backward, see many_rows()
     float   eps, residual_scale, branch_scale;
     Dropout drop;
 };

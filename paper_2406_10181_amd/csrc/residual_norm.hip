@@ -269,6 +269,11 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
         Eight v;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v.x[e] = acc[k][e];
+        if (GROUPS > 1 && !a.many) {                                                      // (few rows: every group's part by itself, the adding is short)
+            store_eight<F32>(a.partial + (((int64_t)slot * gridDim.x + blockIdx.x) * GROUPS + group) * width + col, v, left);
+            ++slot;
+            continue;
+        }
         if constexpr (GROUPS > 1) {
             __syncthreads();                                                              // (scratch is free)
             if (group > 0)
@@ -318,8 +323,11 @@ static int64_t workgroups_of(int64_t rows, int32_t width) {
     const int64_t all = (rows + row_groups(width) - 1) / row_groups(width);
     return all < 256 ? all : 256;
 }
+// Whether a workgroup adds its groups' sums before it leaves them: where it has rows enough to pay for the barriers
+static bool many_rows(int64_t rows, int32_t width) { return rows > 4 * workgroups_of(rows, width) * row_groups(width); }
+static int64_t parts_of(int64_t rows, int32_t width) { return workgroups_of(rows, width) * (many_rows(rows, width) ? 1 : row_groups(width)); }
 size_t residual_norm_partial_bytes(int64_t rows, int32_t width) {
-    return align_up((size_t)workgroups_of(rows, width) * kGrads * (size_t)width * sizeof(float), 256);
+    return align_up((size_t)parts_of(rows, width) * kGrads * (size_t)width * sizeof(float), 256);
 }
 
 template <typename D, int TPR, int NV, int GROUPS> static hipError_t run_forward(const ResidualNormArgs& a, hipStream_t st) {
@@ -328,8 +336,9 @@ template <typename D, int TPR, int NV, int GROUPS> static hipError_t run_forward
     else hipLaunchKernelGGL((k_residual_norm<D, TPR, NV, GROUPS, false>), grid, block, 0, st, a);
     return hipGetLastError();
 }
-template <typename D, int TPR, int GROUPS> static hipError_t run_backward(const ResidualNormArgs& a, hipStream_t st) {
+template <typename D, int TPR, int GROUPS> static hipError_t run_backward(ResidualNormArgs a, hipStream_t st) {
     const int64_t workgroups = workgroups_of(a.rows, a.width);
+    a.many = many_rows(a.rows, a.width);
     const bool bias = (a.post != LSP_NORM_NONE && a.post_b) || a.grads[1] || a.grads[4];
     const dim3 grid((unsigned)workgroups), block(TPR * GROUPS);
     if (a.drop.limit && bias) hipLaunchKernelGGL((k_residual_norm_back<D, TPR, GROUPS, true, true>), grid, block, 0, st, a);
@@ -341,7 +350,7 @@ template <typename D, int TPR, int GROUPS> static hipError_t run_backward(const 
     int sums = 0;
     for (float* g : a.grads) sums += g != nullptr;
     if (!sums) return hipSuccess;
-    hipLaunchKernelGGL(k_residual_norm_sums, dim3((unsigned)((a.width + 31) / 32), (unsigned)sums), dim3(1024), 0, st, a, (int)workgroups);
+    hipLaunchKernelGGL(k_residual_norm_sums, dim3((unsigned)((a.width + 31) / 32), (unsigned)sums), dim3(1024), 0, st, a, (int)parts_of(a.rows, a.width));
     return hipGetLastError();
 }
 
