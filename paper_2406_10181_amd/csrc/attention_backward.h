@@ -182,6 +182,9 @@ __device__ __forceinline__ void attention_dq(const AttentionArgs& a, uint32_t bl
                     for (int ks = 0; ks < kSteps; ++ks) s = mma<D>(read.rows(buf, 32 * t, ks), qf[ks], s);
 #pragma unroll
                     for (int ks = 0; ks < kSteps; ++ks) dp = mma<D>(read.rows(buf + kTileBytes, 32 * t, ks), gf[ks], dp);
+                    Frag<D> kc[2][kCols];
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) kc[0][c] = read.columns(buf, 32 * t, c);
                     if constexpr (D::size == 2) {                                         // reads stay six ahead of their products
                         then_reads<6>();
 #pragma unroll
@@ -191,21 +194,27 @@ __device__ __forceinline__ void attention_dq(const AttentionArgs& a, uint32_t bl
                     if (edge)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) s[i] = 32 * t + 8 * (i >> 2) + (i & 3) < seen ? s[i] : -INFINITY;
-                    if constexpr (DROP) {
-                        drop_keys(dp, 0, k0 + 32 * t, qi, b * a.heads + head, a.drop, h);
-                        drop_keys(dp, 1, k0 + 32 * t, qi, b * a.heads + head, a.drop, h);
-                    }
+                    const auto gradients = [&](int x) {                                   // of the scores of 16 keys
+                        if constexpr (DROP) drop_keys(dp, x, k0 + 32 * t, qi, b * a.heads + head, a.drop, h);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float p = __builtin_amdgcn_exp2f(fmaf(s[i], c2, shift));
-                        s[i] = p * fmaf(dp[i], keep, -delta);
-                    }
+                        for (int i = 8 * x; i < 8 * x + 8; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, shift)) * fmaf(dp[i], keep, -delta);
+                        return to_frag<D>(s, x);
+                    };
+                    // the other 16 keys' columns are read, and their gradients made, under the products of these
+                    const Frag<D> ds0 = gradients(0);
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const Frag<D> ds = to_frag<D>(s, x);
+                    for (int c = 0; c < kCols; ++c) kc[1][c] = read.columns(buf, 32 * t + 16, c);
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int c = 0; c < kCols; ++c) dq[c] = mma<D>(read.columns(buf, 32 * t + 16 * x, c), ds, dq[c]);
-                    }
+                    for (int c = 0; c < kCols; ++c) dq[c] = mma<D>(kc[0][c], ds0, dq[c]);
+                    const Frag<D> ds1 = gradients(1);
+                    if constexpr (D::size == 2)
+#pragma unroll
+                        for (int c = 0; c < kCols; ++c) { then_matrix<1>(); then_vector<36 / kCols>(); }
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) dq[c] = mma<D>(kc[1][c], ds1, dq[c]);
                 }
             }
             arrived_for_all();
@@ -378,16 +387,20 @@ __device__ __forceinline__ void attention_dkv(const AttentionArgs& a, uint32_t b
                         else v = vf[ks];
                         dp = mma<D>(read.rows(buf + kTileBytes, 32 * t, ks), v, dp);
                     }
+                    // columns of dO and of Q by turns, 16 queries each; each is read under the products of the one before
+                    Frag<D> gc[kCols], qc[kCols];
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) gc[c] = read.columns(buf + kTileBytes, 32 * t, c);
+                    if constexpr (D::size == 2) {                                         // reads stay six ahead of their products
+                        then_reads<6>();
+#pragma unroll
+                        for (int i = 0; i < 2 * kSteps - 6; ++i) { then_matrix<1>(); then_reads<1>(); }
+                        then_matrix<6>();
+                    }
                     if (edge)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) s[i] = 32 * t + 8 * (i >> 2) + (i & 3) >= hidden ? s[i] : -INFINITY;
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const f32x4 L = lds_read<f32x4>(buf + 2 * kTileBytes + (32 * t + 8 * g + 4 * h) * 4);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) s[4 * g + j] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + j], c2, L[j]));
-                    }
-                    f32x16 pd = s;
+                    u32x4 kept = {0, 0, 0, 0};
                     if constexpr (DROP) {
                         // eight lanes share a block of eight keys: of the 16 queries that they all have, each lane makes two; the bits go round by LDS
                         const Lds bits = lds + kBits + wave * 128 + (lane >> 3) * 16;
@@ -395,36 +408,69 @@ __device__ __forceinline__ void attention_dkv(const AttentionArgs& a, uint32_t b
                         for (int half = 0; half < 2; ++half) {
                             const int x = (lane & 7) + 8 * half;
                             const u32x4 w = philox((uint32_t)key >> 3, q0 + 32 * t + 8 * (x >> 2) + 4 * h + (x & 3), b * a.heads + q_head, a.drop.offset, a.drop.key0, a.drop.key1);
-                            uint32_t kept = 0;
+                            uint32_t byte = 0;
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) kept |= (philox_word(w, e) < a.drop.limit ? 0u : 1u) << e;
-                            lds_write<uint8_t>(bits + x, (uint8_t)kept);
+                            for (int e = 0; e < 8; ++e) byte |= (philox_word(w, e) < a.drop.limit ? 0u : 1u) << e;
+                            lds_write<uint8_t>(bits + x, (uint8_t)byte);
                         }
                         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
                         __builtin_amdgcn_wave_barrier();
                         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-                        const u32x4 all = lds_read<u32x4>(bits);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const bool kept = (all[i >> 2] >> (8 * (i & 3) + (lane & 7))) & 1u;
-                            pd[i] = kept ? s[i] : 0.0f;
-                            dp[i] = kept ? dp[i] : 0.0f;
-                        }
+                        kept = lds_read<u32x4>(bits) >> (uint32_t)(lane & 7);
                         __builtin_amdgcn_wave_barrier();
                     }
+                    const auto probabilities = [&](int x) {                               // of 16 queries
+                        f32x16 pd;
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const f32x4 delta = lds_read<f32x4>(buf + 2 * kTileBytes + BQ * 4 + (32 * t + 8 * g + 4 * h) * 4);
+                        for (int g = 2 * x; g < 2 * x + 2; ++g) {
+                            const f32x4 L = lds_read<f32x4>(buf + 2 * kTileBytes + (32 * t + 8 * g + 4 * h) * 4);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) s[4 * g + j] *= fmaf(dp[4 * g + j], keep, -delta[j]);
-                    }
+                            for (int j = 0; j < 4; ++j) {
+                                const int i = 4 * g + j;
+                                s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, L[j]));
+                                pd[i] = DROP && !(kept[g] >> (8 * j) & 1u) ? 0.0f : s[i];
+                            }
+                        }
+                        return to_frag<D>(pd, x);
+                    };
+                    const auto gradients = [&](int x) {
+#pragma unroll
+                        for (int g = 2 * x; g < 2 * x + 2; ++g) {
+                            const f32x4 delta = lds_read<f32x4>(buf + 2 * kTileBytes + BQ * 4 + (32 * t + 8 * g + 4 * h) * 4);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const int i = 4 * g + j;
+                                s[i] *= fmaf(DROP && !(kept[g] >> (8 * j) & 1u) ? 0.0f : dp[i], keep, -delta[j]);
+                            }
+                        }
+                        return to_frag<D>(s, x);
+                    };
+                    Frag<D> p = probabilities(0);
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const Frag<D> p = to_frag<D>(pd, x), ds = to_frag<D>(s, x);
+                        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int c = 0; c < kCols; ++c) {
-                            dv[c] = mma<D>(read.columns(buf + kTileBytes, 32 * t + 16 * x, c), p, dv[c]);
-                            dk[c] = mma<D>(read.columns(buf, 32 * t + 16 * x, c), ds, dk[c]);
+                        for (int c = 0; c < kCols; ++c) qc[c] = read.columns(buf, 32 * t + 16 * x, c);
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int c = 0; c < kCols; ++c) dv[c] = mma<D>(gc[c], p, dv[c]);
+                        const Frag<D> ds = gradients(x);
+                        if constexpr (D::size == 2)
+#pragma unroll
+                            for (int c = 0; c < kCols; ++c) { then_matrix<1>(); then_vector<20 / kCols>(); }
+                        __builtin_amdgcn_sched_barrier(0);
+                        if (x == 0) {
+#pragma unroll
+                            for (int c = 0; c < kCols; ++c) gc[c] = read.columns(buf + kTileBytes, 32 * t + 16, c);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+#pragma unroll
+                        for (int c = 0; c < kCols; ++c) dk[c] = mma<D>(qc[c], ds, dk[c]);
+                        if (x == 0) {
+                            p = probabilities(1);
+                            if constexpr (D::size == 2)
+#pragma unroll
+                                for (int c = 0; c < kCols; ++c) { then_matrix<1>(); then_vector<20 / kCols>(); }
                         }
                     }
                 }
