@@ -151,142 +151,175 @@ __global__ __launch_bounds__(TPR * GROUPS) void k_residual_norm(const ResidualNo
     }
 }
 
-// A thread has eight columns, TPR threads a row and GROUPS rows a workgroup; the row after this one is on its way while this one's sums wait for one another, and the
+// A thread has NV units of eight columns, TPR threads a row and GROUPS rows a workgroup; the row after this one is on its way while this one's sums wait for one another, and the
 // weights stay in registers.  BIAS: a norm has a bias, or the gradient of one is asked for.
-template <typename D, int TPR, int GROUPS, bool DROP, bool BIAS>
+template <typename D, int TPR, int NV, int GROUPS, bool DROP, bool BIAS>
 __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const ResidualNormArgs a) {
     using elem = typename D::elem;
     constexpr int kSumFloats = GROUPS * 4 * (TPR / 64);
     __shared__ float scratch[GROUPS > 1 ? (GROUPS - 1) * TPR * 8 : kSumFloats];           // RowSum's, and at the end the other groups' sums over rows
-    const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR), t = threadIdx.x % TPR, col = t * 8;
-    const int width = a.width, left = width - col;
+    const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR), t = threadIdx.x % TPR;
+    const int width = a.width;
+    const auto col_of = [&](int n) { return (t + n * TPR) * 8; };
+    const auto left_of = [&](int n) { return width - col_of(n); };
     const float per = 1.0f / (float)width;
     RowSum<TPR, 2> sum{scratch + group * 4 * (TPR / 64)};
     const bool post = a.post != LSP_NORM_NONE, pre = a.pre != LSP_NORM_NONE;
-    const auto vector = [&](const void* p, float otherwise) {
-        if (p) return load_packed<D>(static_cast<const elem*>(p) + col, left);
+    const auto vector = [&](const void* p, float otherwise, int n) {
+        if (p) return load_packed<D>(static_cast<const elem*>(p) + col_of(n), left_of(n));
         Packed<D> r;
 #pragma unroll
         for (int k = 0; k < 2 * D::size; ++k)
             r.w[k] = D::size == 4 ? __float_as_uint(otherwise) : (uint32_t)narrow<D>(otherwise) * 0x10001u;
         return r;
     };
-    Packed<D> wf_ = vector(post ? a.post_w : nullptr, 1.0f), bf_ = vector(BIAS && post ? a.post_b : nullptr, 0.0f), g_ = vector(a.gate, 1.0f), wy_ = vector(pre ? a.pre_w : nullptr, 1.0f);
-    float acc[kGrads][8];
+    Packed<D> wf_[NV], bf_[NV], g_[NV], wy_[NV];
 #pragma unroll
-    for (int k = 0; k < kGrads; ++k)
+    for (int n = 0; n < NV; ++n) {
+        wf_[n] = vector(post ? a.post_w : nullptr, 1.0f, n); bf_[n] = vector(BIAS && post ? a.post_b : nullptr, 0.0f, n);
+        g_[n] = vector(a.gate, 1.0f, n); wy_[n] = vector(pre ? a.pre_w : nullptr, 1.0f, n);
+    }
+    // The vectors stay packed: what is made of them before the loop, or in one half of a row for the other, would take twice the registers.
+    const auto afresh = [&] {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[k][e] = 0.0f;
-    Packed<D> xp, fp, dyp, dhp;
-    float mean_f, rstd_f, mean_y, rstd_y;
-    const auto load_first = [&](int64_t row) {
-        const elem* x = static_cast<const elem*>(a.x) + row * a.x_stride + col;
-        const elem* f = static_cast<const elem*>(a.f) + row * a.f_stride + col;
-        const elem* dh = a.dh ? static_cast<const elem*>(a.dh) + row * a.dh_stride + col : x;
-        if (left >= 8) { xp = load_whole<D>(x); fp = load_whole<D>(f); dhp = load_whole<D>(dh); }
-        else { xp = load_part<D>(x, left); fp = load_part<D>(f, left); dhp = load_part<D>(dh, left); }
-    };
-    const auto load_dy = [&](int64_t row) { dyp = load_packed<D>(static_cast<const elem*>(a.dy) + row * a.dy_stride + col, left); };
-    const int64_t step = (int64_t)gridDim.x * GROUPS, first = (int64_t)blockIdx.x * GROUPS;
-    const auto mine_of = [&](int64_t base) { return base + group < a.rows ? base + group : a.rows - 1; };   // (every thread goes to every barrier)
-    load_first(mine_of(first));
-    load_dy(mine_of(first));
-    for (int64_t base = first; base < a.rows; base += step) {
-        const bool mine = base + group < a.rows;
-        const int64_t row = mine_of(base);
-        const int64_t next = mine_of(base + step < a.rows ? base + step : base);
-        mean_f = a.stats[row]; rstd_f = a.stats[a.rows + row]; mean_y = a.stats[2 * a.rows + row]; rstd_y = a.stats[3 * a.rows + row];
-        // (the vectors stay packed: widened once, before the loop, they would take twice the registers)
+        for (int n = 0; n < NV; ++n)
 #pragma unroll
-        for (int k = 0; k < 2 * D::size; ++k) {
-            asm volatile("" : "+v"(wf_.w[k]), "+v"(g_.w[k]), "+v"(wy_.w[k]));
-            if constexpr (BIAS) asm volatile("" : "+v"(bf_.w[k]));
-        }
-        // y^ and f^, and the gradient of y^
-        uint32_t kept = 0xFFu;
-        if constexpr (DROP) {
-            const uint64_t at = (uint64_t)row * (uint64_t)((width + 7) >> 3) + (uint64_t)t;
-            const u32x4 w = philox((uint32_t)at, (uint32_t)(at >> 32), 0, a.drop.offset, a.drop.key0, a.drop.key1);
-            kept = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) kept |= (philox_word(w, e) < a.drop.limit ? 0u : 1u) << e;
-        }
-        float fhat[8], yhat[8], de[8], s[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (e == 4) __builtin_amdgcn_sched_barrier(0);                                // (four at a time: eight would take registers for speed that nothing waits for)
-            const bool in = e < left;
-            const float wf = element<D>(wf_, e), bf = (BIAS ? element<D>(bf_, e) : 0.0f), g = element<D>(g_, e), wy = element<D>(wy_, e);
-            fhat[e] = in ? (element<D>(fp, e) - mean_f) * rstd_f : 0.0f;
-            const float u = !DROP ? fmaf(fhat[e], wf, bf) : (kept >> e) & 1u ? a.drop.scale * fmaf(fhat[e], wf, bf) : 0.0f;   // (what is dropped may be infinite)
-            const float y = fmaf(a.branch_scale * g, u, a.residual_scale * element<D>(xp, e));
-            yhat[e] = in ? (y - mean_y) * rstd_y : 0.0f;
-            const float d = a.dh ? element<D>(dhp, e) : 0.0f;
-            if (mine) {
-                acc[0][e] = fmaf(d, yhat[e], acc[0][e]);
-                if constexpr (BIAS) acc[1][e] += d;
+            for (int k = 0; k < 2 * D::size; ++k) {
+                asm volatile("" : "+v"(wf_[n].w[k]), "+v"(g_[n].w[k]), "+v"(wy_[n].w[k]));
+                if constexpr (BIAS) asm volatile("" : "+v"(bf_[n].w[k]));
             }
-            de[e] = d * wy;
-            s[0] = fmaf(de[e], yhat[e], s[0]);
-            s[1] += de[e];
+    };
+    float acc[NV][kGrads][8];
+#pragma unroll
+    for (int n = 0; n < NV; ++n)
+#pragma unroll
+        for (int k = 0; k < kGrads; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[n][k][e] = 0.0f;
+    Packed<D> xp[NV], fp[NV], dyp[NV], dhp[NV];
+    float mean_f, rstd_f, mean_y, rstd_y;
+    // A group without a row (every thread goes to every barrier) has the last row with gradients of zeros: it adds zeros, and stores nothing.
+    const auto load_first = [&](int64_t base) {
+        const int64_t row = base + group < a.rows ? base + group : a.rows - 1;
+        const elem* x = static_cast<const elem*>(a.x) + row * a.x_stride;
+        const elem* f = static_cast<const elem*>(a.f) + row * a.f_stride;
+        const elem* dh = a.dh ? static_cast<const elem*>(a.dh) + row * a.dh_stride : x;
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+            const int col = col_of(n), left = base + group < a.rows ? left_of(n) : 0;     // (zeros where the group has no row: its sums then get zeros)
+            if (left >= 8) { xp[n] = load_whole<D>(x + col); fp[n] = load_whole<D>(f + col); }
+            else { xp[n] = load_part<D>(x + col, left); fp[n] = load_part<D>(f + col, left); }
+            dhp[n] = load_packed<D>(dh + col, a.dh ? left : 0);
+        }
+    };
+    const auto load_dy = [&](int64_t base) {
+        const int64_t row = base + group < a.rows ? base + group : a.rows - 1;
+#pragma unroll
+        for (int n = 0; n < NV; ++n) dyp[n] = load_packed<D>(static_cast<const elem*>(a.dy) + row * a.dy_stride + col_of(n), base + group < a.rows ? left_of(n) : 0);
+    };
+    const int64_t step = (int64_t)gridDim.x * GROUPS, first = (int64_t)blockIdx.x * GROUPS;
+    load_first(first);
+    load_dy(first);
+    for (int64_t base = first; base < a.rows; base += step) {
+        const bool mine = GROUPS == 1 || base + group < a.rows;
+        const int64_t row = base + group < a.rows ? base + group : a.rows - 1, next = base + step < a.rows ? base + step : base;
+        mean_f = a.stats[row]; rstd_f = a.stats[a.rows + row]; mean_y = a.stats[2 * a.rows + row]; rstd_y = a.stats[3 * a.rows + row];
+        afresh();
+        // y^ and f^, and the gradient of y^
+        uint32_t kept[NV];
+        float fhat[NV][8], yhat[NV][8], de[NV][8], s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+            kept[n] = 0xFFu;
+            if constexpr (DROP) {
+                const uint64_t at = (uint64_t)row * (uint64_t)((width + 7) >> 3) + (uint64_t)(t + n * TPR);
+                const u32x4 w = philox((uint32_t)at, (uint32_t)(at >> 32), 0, a.drop.offset, a.drop.key0, a.drop.key1);
+                kept[n] = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) kept[n] |= (philox_word(w, e) < a.drop.limit ? 0u : 1u) << e;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);                        // (four at a time: eight would take registers for speed that nothing waits for)
+                const bool in = e < left_of(n);
+                const float wf = element<D>(wf_[n], e), bf = (BIAS ? element<D>(bf_[n], e) : 0.0f), g = element<D>(g_[n], e), wy = element<D>(wy_[n], e);
+                fhat[n][e] = in ? (element<D>(fp[n], e) - mean_f) * rstd_f : 0.0f;
+                const float u = !DROP ? fmaf(fhat[n][e], wf, bf) : (kept[n] >> e) & 1u ? a.drop.scale * fmaf(fhat[n][e], wf, bf) : 0.0f;   // (what is dropped may be infinite)
+                const float y = fmaf(a.branch_scale * g, u, a.residual_scale * element<D>(xp[n], e));
+                yhat[n][e] = in ? (y - mean_y) * rstd_y : 0.0f;
+                const float d = element<D>(dhp[n], e);
+                acc[n][0][e] = fmaf(d, yhat[n][e], acc[n][0][e]);
+                if constexpr (BIAS) acc[n][1][e] += d;
+                de[n][e] = d * wy;
+                s[0] = fmaf(de[n][e], yhat[n][e], s[0]);
+                s[1] += de[n][e];
+            }
         }
         load_first(next);                                                                 // (where what they held is used up)
         if (pre) sum(s);
         float s1 = s[0] * per, s0 = a.pre == LSP_NORM_LAYER ? s[1] * per : 0.0f;
         s[0] = s[1] = 0.0f;
-        Eight out;
+        afresh();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (e == 4) __builtin_amdgcn_sched_barrier(0);
-            const float wf = element<D>(wf_, e), bf = (BIAS ? element<D>(bf_, e) : 0.0f), g = element<D>(g_, e);
-            const float total = element<D>(dyp, e) + (pre ? rstd_y * (de[e] - s0 - yhat[e] * s1) : de[e]);
-            out.x[e] = a.residual_scale * total;
-            const bool keep = !DROP || ((kept >> e) & 1u);
-            const float branch = keep ? a.branch_scale * total * (DROP ? a.drop.scale : 1.0f) : 0.0f, u = keep ? fmaf(fhat[e], wf, bf) : 0.0f;
-            const float du = branch * g;
-            if (mine) {
-                acc[2][e] = fmaf(branch, u, acc[2][e]);
-                acc[3][e] = fmaf(du, fhat[e], acc[3][e]);
-                if constexpr (BIAS) acc[4][e] += du;
+        for (int n = 0; n < NV; ++n) {
+            Eight out;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                const float wf = element<D>(wf_[n], e), bf = (BIAS ? element<D>(bf_[n], e) : 0.0f), g = element<D>(g_[n], e);
+                const float total = element<D>(dyp[n], e) + (pre ? rstd_y * (de[n][e] - s0 - yhat[n][e] * s1) : de[n][e]);
+                out.x[e] = a.residual_scale * total;
+                const bool keep = !DROP || ((kept[n] >> e) & 1u);
+                const float branch = keep ? a.branch_scale * total * (DROP ? a.drop.scale : 1.0f) : 0.0f, u = keep ? fmaf(fhat[n][e], wf, bf) : 0.0f;
+                const float du = branch * g;
+                acc[n][2][e] = fmaf(branch, u, acc[n][2][e]);
+                acc[n][3][e] = fmaf(du, fhat[n][e], acc[n][3][e]);
+                if constexpr (BIAS) acc[n][4][e] += du;
+                de[n][e] = e < left_of(n) ? du * wf : 0.0f;
+                s[0] = fmaf(de[n][e], fhat[n][e], s[0]);
+                s[1] += de[n][e];
             }
-            de[e] = e < left ? du * wf : 0.0f;
-            s[0] = fmaf(de[e], fhat[e], s[0]);
-            s[1] += de[e];
+            if (mine) store_eight<D>(static_cast<elem*>(a.dx) + row * a.dx_stride + col_of(n), out, left_of(n));
         }
-        if (mine) store_eight<D>(static_cast<elem*>(a.dx) + row * a.dx_stride + col, out, left);
         load_dy(next);
         if (post) sum(s);
         s1 = s[0] * per; s0 = a.post == LSP_NORM_LAYER ? s[1] * per : 0.0f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) out.x[e] = post ? rstd_f * (de[e] - s0 - fhat[e] * s1) : de[e];
-        if (mine) store_eight<D>(static_cast<elem*>(a.df) + row * a.df_stride + col, out, left);
+        for (int n = 0; n < NV; ++n) {
+            Eight out;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) out.x[e] = post ? rstd_f * (de[n][e] - s0 - fhat[n][e] * s1) : de[n][e];
+            if (mine) store_eight<D>(static_cast<elem*>(a.df) + row * a.df_stride + col_of(n), out, left_of(n));
+        }
     }
     // the workgroup's part of the sums over rows
     int slot = 0;
 #pragma unroll
     for (int k = 0; k < kGrads; ++k) {
         if (!a.grads[k]) continue;
-        Eight v;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v.x[e] = acc[k][e];
-        if (GROUPS > 1 && !a.many) {                                                      // (few rows: every group's part by itself, the adding is short)
-            store_eight<F32>(a.partial + (((int64_t)slot * gridDim.x + blockIdx.x) * GROUPS + group) * width + col, v, left);
-            ++slot;
-            continue;
+        for (int n = 0; n < NV; ++n) {
+            Eight v;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v.x[e] = acc[n][k][e];
+            if (GROUPS > 1 && !a.many) {                                                  // (few rows: every group's part by itself, the adding is short)
+                store_eight<F32>(a.partial + (((int64_t)slot * gridDim.x + blockIdx.x) * GROUPS + group) * width + col_of(n), v, left_of(n));
+                continue;
+            }
+            if constexpr (GROUPS > 1) {
+                __syncthreads();                                                          // (scratch is free)
+                if (group > 0)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) scratch[((group - 1) * 8 + e) * TPR + t] = v.x[e];
+                __syncthreads();
+                if (group == 0)
+#pragma unroll
+                    for (int o = 0; o < GROUPS - 1; ++o)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v.x[e] += scratch[(o * 8 + e) * TPR + t];
+            }
+            if (group == 0) store_eight<F32>(a.partial + ((int64_t)slot * gridDim.x + blockIdx.x) * width + col_of(n), v, left_of(n));
         }
-        if constexpr (GROUPS > 1) {
-            __syncthreads();                                                              // (scratch is free)
-            if (group > 0)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) scratch[((group - 1) * 8 + e) * TPR + t] = v.x[e];
-            __syncthreads();
-            if (group == 0)
-#pragma unroll
-                for (int o = 0; o < GROUPS - 1; ++o)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v.x[e] += scratch[(o * 8 + e) * TPR + t];
-        }
-        if (group == 0) store_eight<F32>(a.partial + ((int64_t)slot * gridDim.x + blockIdx.x) * width + col, v, left);
         ++slot;
     }
 }
@@ -316,8 +349,9 @@ __global__ __launch_bounds__(1024) void k_residual_norm_sums(const ResidualNormA
 }
 
 // Backward: threads of a row, and rows that a workgroup has at a time, by their width.  One workgroup a CU: its registers hold no second one of 512 threads, and fewer
-// workgroups leave fewer parts to add (4096 x 4096, bf16: 48 + 5 us; twice as many workgroups 53 + 7; two a CU at 128 registers, with spills, 91).
-static int row_threads(int width) { return width <= 512 ? 64 : width <= 1024 ? 128 : width <= 2048 ? 256 : width <= 4096 ? 512 : 1024; }
+// workgroups leave fewer parts to add (4096 x 4096, bf16: 48 + 5 us; twice as many workgroups 53 + 7; two a CU at 128 registers, with spills, 91).  Beyond 4096 columns
+// two units a thread, which spill some (4096 x 8192, fp16: 119 us; one unit in 1024 threads has half the registers a thread and spills more: 252).
+static int row_threads(int width) { return width <= 512 ? 64 : width <= 1024 ? 128 : width <= 2048 ? 256 : 512; }
 static int row_groups(int width) { return width <= 512 ? 8 : width <= 1024 ? 4 : width <= 2048 ? 2 : 1; }
 static int64_t workgroups_of(int64_t rows, int32_t width) {
     const int64_t all = (rows + row_groups(width) - 1) / row_groups(width);
@@ -336,15 +370,15 @@ template <typename D, int TPR, int NV, int GROUPS> static hipError_t run_forward
     else hipLaunchKernelGGL((k_residual_norm<D, TPR, NV, GROUPS, false>), grid, block, 0, st, a);
     return hipGetLastError();
 }
-template <typename D, int TPR, int GROUPS> static hipError_t run_backward(ResidualNormArgs a, hipStream_t st) {
+template <typename D, int TPR, int NV, int GROUPS> static hipError_t run_backward(ResidualNormArgs a, hipStream_t st) {
     const int64_t workgroups = workgroups_of(a.rows, a.width);
     a.many = many_rows(a.rows, a.width);
     const bool bias = (a.post != LSP_NORM_NONE && a.post_b) || a.grads[1] || a.grads[4];
     const dim3 grid((unsigned)workgroups), block(TPR * GROUPS);
-    if (a.drop.limit && bias) hipLaunchKernelGGL((k_residual_norm_back<D, TPR, GROUPS, true, true>), grid, block, 0, st, a);
-    else if (a.drop.limit) hipLaunchKernelGGL((k_residual_norm_back<D, TPR, GROUPS, true, false>), grid, block, 0, st, a);
-    else if (bias) hipLaunchKernelGGL((k_residual_norm_back<D, TPR, GROUPS, false, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((k_residual_norm_back<D, TPR, GROUPS, false, false>), grid, block, 0, st, a);
+    if (a.drop.limit && bias) hipLaunchKernelGGL((k_residual_norm_back<D, TPR, NV, GROUPS, true, true>), grid, block, 0, st, a);
+    else if (a.drop.limit) hipLaunchKernelGGL((k_residual_norm_back<D, TPR, NV, GROUPS, true, false>), grid, block, 0, st, a);
+    else if (bias) hipLaunchKernelGGL((k_residual_norm_back<D, TPR, NV, GROUPS, false, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_residual_norm_back<D, TPR, NV, GROUPS, false, false>), grid, block, 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     int sums = 0;
@@ -367,11 +401,10 @@ template <typename D> static hipError_t forward_of(const ResidualNormArgs& a, hi
 }
 template <typename D> static hipError_t backward_of(const ResidualNormArgs& a, hipStream_t st) {
     switch (row_threads(a.width)) {
-        case 64:  return run_backward<D, 64, 8>(a, st);
-        case 128: return run_backward<D, 128, 4>(a, st);
-        case 256: return run_backward<D, 256, 2>(a, st);
-        case 512: return run_backward<D, 512, 1>(a, st);
-        default:  return run_backward<D, 1024, 1>(a, st);
+        case 64:  return run_backward<D, 64, 1, 8>(a, st);
+        case 128: return run_backward<D, 128, 1, 4>(a, st);
+        case 256: return run_backward<D, 256, 1, 2>(a, st);
+        default:  return a.width <= 4096 ? run_backward<D, 512, 1, 1>(a, st) : run_backward<D, 512, 2, 1>(a, st);
     }
 }
 
