@@ -151,43 +151,57 @@ __global__ __launch_bounds__(TPR * GROUPS) void k_residual_norm(const ResidualNo
     }
 }
 
-// A thread has NV units of eight columns, TPR threads a row and GROUPS rows a workgroup; the row after this one is on its way while this one's sums wait for one another, and the
-// weights stay in registers.  BIAS: a norm has a bias, or the gradient of one is asked for.
+// A thread has NV units of eight columns, TPR threads a row and GROUPS rows a workgroup.  With one workgroup a CU, what is on the way is what its rows ask for, so the rows of the
+// next two steps are (one step ahead, 16384 x 2048 took 115 us, with two 90; wide rows, NV = 2, have registers for one).  Beside memory the instructions count, some 60 an
+// element: weights stay in registers, in fp32, and what can be folded into a factor of the row is (4096 x 4096: 47 to 42 us, 3001 x 3000 with biases 49 to 37).
+// BIAS: a norm has a bias, or the gradient of one is asked for.
 template <typename D, int TPR, int NV, int GROUPS, bool DROP, bool BIAS>
 __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const ResidualNormArgs a) {
     using elem = typename D::elem;
-    constexpr int kSumFloats = GROUPS * 4 * (TPR / 64);
+    constexpr int kSumFloats = GROUPS * 4 * (TPR / 64), AHEAD = NV == 1 ? 2 : 1;
     __shared__ float scratch[GROUPS > 1 ? (GROUPS - 1) * TPR * 8 : kSumFloats];           // RowSum's, and at the end the other groups' sums over rows
     const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR), t = threadIdx.x % TPR;
     const int width = a.width;
-    const auto col_of = [&](int n) { return (t + n * TPR) * 8; };
-    const auto left_of = [&](int n) { return width - col_of(n); };
-    const float per = 1.0f / (float)width;
+    // The last thread of a row has the row's last eight columns, of which the first `others` are the thread's before it: there its weights are zeros, so they add nothing to any
+    // sum, and they are not stored.  (A block put together from smaller loads waits for them at once, and every thread of the row for it: 2999 columns took 8 us longer than 3000, now 3.)
+    const auto col_of = [&](int n) { return min((t + n * TPR) * 8, width - 8); };
+    const auto others = [&](int n) { return min((t + n * TPR) * 8 - col_of(n), 8); };
+    const bool whole = width >= 8, dy_whole = whole && a.dx != a.dy;                      // (in place: a neighbour may have stored already)
+    const float per = 1.0f / (float)width, scale_u = DROP ? a.branch_scale * a.drop.scale : a.branch_scale;
     RowSum<TPR, 2> sum{scratch + group * 4 * (TPR / 64)};
     const bool post = a.post != LSP_NORM_NONE, pre = a.pre != LSP_NORM_NONE;
-    const auto vector = [&](const void* p, float otherwise, int n) {
-        if (p) return load_packed<D>(static_cast<const elem*>(p) + col_of(n), left_of(n));
-        Packed<D> r;
+    // Weights in fp32 while they have the registers for it (NV = 1), else packed: what is made of them in one half of a row for the other would take more.
+    constexpr bool HELD = NV == 1;
+    struct Vector { Packed<D> packed; float value[8]; };
+    Vector wf_[NV], bf_[NV], g_[NV], wy_[NV];
+    const auto vector = [&](Vector& v, const void* p, float otherwise, bool zeros, int n) {
+        const int first = zeros ? others(n) : 0;
+        Eight r;
+        if (p) r = widen_eight<D>(load_ending<D>(static_cast<const elem*>(p) + col_of(n), others(n), whole));
 #pragma unroll
-        for (int k = 0; k < 2 * D::size; ++k)
-            r.w[k] = D::size == 4 ? __float_as_uint(otherwise) : (uint32_t)narrow<D>(otherwise) * 0x10001u;
-        return r;
+        for (int e = 0; e < 8; ++e) v.value[e] = e < first ? 0.0f : p ? r.x[e] : otherwise;
+        if constexpr (!HELD) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r.x[e] = v.value[e];
+            v.packed = narrow_eight<D>(r);
+        }
     };
-    Packed<D> wf_[NV], bf_[NV], g_[NV], wy_[NV];
+    const auto of = [&](const Vector& v, int e) { return HELD ? v.value[e] : element<D>(v.packed, e); };
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
-        wf_[n] = vector(post ? a.post_w : nullptr, 1.0f, n); bf_[n] = vector(BIAS && post ? a.post_b : nullptr, 0.0f, n);
-        g_[n] = vector(a.gate, 1.0f, n); wy_[n] = vector(pre ? a.pre_w : nullptr, 1.0f, n);
+        vector(wf_[n], post ? a.post_w : nullptr, 1.0f, false, n); vector(bf_[n], BIAS && post ? a.post_b : nullptr, 0.0f, false, n);
+        vector(g_[n], a.gate, 1.0f, true, n); vector(wy_[n], pre ? a.pre_w : nullptr, 1.0f, true, n);
     }
-    // The vectors stay packed: what is made of them before the loop, or in one half of a row for the other, would take twice the registers.
     const auto afresh = [&] {
+        if constexpr (!HELD) {
 #pragma unroll
-        for (int n = 0; n < NV; ++n)
+            for (int n = 0; n < NV; ++n)
 #pragma unroll
-            for (int k = 0; k < 2 * D::size; ++k) {
-                asm volatile("" : "+v"(wf_[n].w[k]), "+v"(g_[n].w[k]), "+v"(wy_[n].w[k]));
-                if constexpr (BIAS) asm volatile("" : "+v"(bf_[n].w[k]));
-            }
+                for (int k = 0; k < 2 * D::size; ++k) {
+                    asm volatile("" : "+v"(wf_[n].packed.w[k]), "+v"(g_[n].packed.w[k]), "+v"(wy_[n].packed.w[k]));
+                    if constexpr (BIAS) asm volatile("" : "+v"(bf_[n].packed.w[k]));
+                }
+        }
     };
     float acc[NV][kGrads][8];
 #pragma unroll
@@ -196,58 +210,65 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
         for (int k = 0; k < kGrads; ++k)
 #pragma unroll
             for (int e = 0; e < 8; ++e) acc[n][k][e] = 0.0f;
-    Packed<D> xp[NV], fp[NV], dyp[NV], dhp[NV];
-    float mean_f, rstd_f, mean_y, rstd_y;
+    // What belongs to a row is asked for AHEAD rows before.
+    struct Row { Packed<D> x[NV], f[NV], dy[NV], dh[NV]; float stats[4]; };
+    Row rows_[AHEAD];
+    uint32_t lane0 = 0;                                                                   // (statistics come into vector registers, as the rest does: a scalar load would be waited for with LDS)
+    asm volatile("" : "+v"(lane0));
     // A group without a row (every thread goes to every barrier) has the last row with gradients of zeros: it adds zeros, and stores nothing.
-    const auto load_first = [&](int64_t base) {
+    const auto load_first = [&](Row& r, int64_t base) {
         const int64_t row = base + group < a.rows ? base + group : a.rows - 1;
         const elem* x = static_cast<const elem*>(a.x) + row * a.x_stride;
         const elem* f = static_cast<const elem*>(a.f) + row * a.f_stride;
         const elem* dh = a.dh ? static_cast<const elem*>(a.dh) + row * a.dh_stride : x;
 #pragma unroll
+        for (int k = 0; k < 4; ++k) r.stats[k] = (a.stats + k * a.rows + row)[lane0];
+#pragma unroll
         for (int n = 0; n < NV; ++n) {
-            const int col = col_of(n), left = base + group < a.rows ? left_of(n) : 0;     // (zeros where the group has no row: its sums then get zeros)
-            if (left >= 8) { xp[n] = load_whole<D>(x + col); fp[n] = load_whole<D>(f + col); }
-            else { xp[n] = load_part<D>(x + col, left); fp[n] = load_part<D>(f + col, left); }
-            dhp[n] = load_packed<D>(dh + col, a.dh ? left : 0);
+            const int col = col_of(n), first = base + group < a.rows ? others(n) : 8;     // (zeros where the group has no row: its sums then get zeros)
+            r.x[n] = load_ending<D>(x + col, first, whole);
+            r.f[n] = load_ending<D>(f + col, first, whole);
+            r.dh[n] = load_ending<D>(dh + col, a.dh ? first : 8, whole);
         }
     };
-    const auto load_dy = [&](int64_t base) {
+    const auto load_dy = [&](Row& r, int64_t base) {
         const int64_t row = base + group < a.rows ? base + group : a.rows - 1;
 #pragma unroll
-        for (int n = 0; n < NV; ++n) dyp[n] = load_packed<D>(static_cast<const elem*>(a.dy) + row * a.dy_stride + col_of(n), base + group < a.rows ? left_of(n) : 0);
+        for (int n = 0; n < NV; ++n) r.dy[n] = load_ending<D>(static_cast<const elem*>(a.dy) + row * a.dy_stride + col_of(n), base + group < a.rows ? others(n) : 8, dy_whole);
     };
     const int64_t step = (int64_t)gridDim.x * GROUPS, first = (int64_t)blockIdx.x * GROUPS;
-    load_first(first);
-    load_dy(first);
-    for (int64_t base = first; base < a.rows; base += step) {
+    const auto one_row = [&](Row& r, int64_t base) {
         const bool mine = GROUPS == 1 || base + group < a.rows;
-        const int64_t row = base + group < a.rows ? base + group : a.rows - 1, next = base + step < a.rows ? base + step : base;
-        mean_f = a.stats[row]; rstd_f = a.stats[a.rows + row]; mean_y = a.stats[2 * a.rows + row]; rstd_y = a.stats[3 * a.rows + row];
+        const int64_t row = base + group < a.rows ? base + group : a.rows - 1, next = base + AHEAD * step;
+        const float mean_f = r.stats[0], rstd_f = r.stats[1], mean_y = r.stats[2], rstd_y = r.stats[3];
         afresh();
         // y^ and f^, and the gradient of y^
-        uint32_t kept[NV];
+        bool kept[NV][8];
         float fhat[NV][8], yhat[NV][8], de[NV][8], s[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
-            kept[n] = 0xFFu;
             if constexpr (DROP) {
                 const uint64_t at = (uint64_t)row * (uint64_t)((width + 7) >> 3) + (uint64_t)(t + n * TPR);
                 const u32x4 w = philox((uint32_t)at, (uint32_t)(at >> 32), 0, a.drop.offset, a.drop.key0, a.drop.key1);
-                kept[n] = 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) kept[n] |= (philox_word(w, e) < a.drop.limit ? 0u : 1u) << e;
+                for (int e = 0; e < 8; ++e) kept[n][e] = philox_word(w, e) >= a.drop.limit;
+                if (others(n)) {                                                          // (the block's words belong to the last columns)
+                    uint32_t bits = 0;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) bits |= (kept[n][e] ? 1u : 0u) << e;
+                    bits <<= others(n);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) kept[n][e] = bits >> e & 1u;
+                }
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);                        // (four at a time: eight would take registers for speed that nothing waits for)
-                const bool in = e < left_of(n);
-                const float wf = element<D>(wf_[n], e), bf = (BIAS ? element<D>(bf_[n], e) : 0.0f), g = element<D>(g_[n], e), wy = element<D>(wy_[n], e);
-                fhat[n][e] = in ? (element<D>(fp[n], e) - mean_f) * rstd_f : 0.0f;
-                const float u = !DROP ? fmaf(fhat[n][e], wf, bf) : (kept[n] >> e) & 1u ? a.drop.scale * fmaf(fhat[n][e], wf, bf) : 0.0f;   // (what is dropped may be infinite)
-                const float y = fmaf(a.branch_scale * g, u, a.residual_scale * element<D>(xp[n], e));
-                yhat[n][e] = in ? (y - mean_y) * rstd_y : 0.0f;
-                const float d = element<D>(dhp[n], e);
+                const float wf = of(wf_[n], e), bf = BIAS ? of(bf_[n], e) : 0.0f, gate = of(g_[n], e), wy = of(wy_[n], e);
+                fhat[n][e] = (element<D>(r.f[n], e) - mean_f) * rstd_f;
+                const float u = !DROP ? fmaf(fhat[n][e], wf, bf) : kept[n][e] ? fmaf(fhat[n][e], wf, bf) : 0.0f;   // (what is dropped may be infinite)
+                yhat[n][e] = fmaf(scale_u * gate, u, fmaf(a.residual_scale, element<D>(r.x[n], e), -mean_y)) * rstd_y;
+                const float d = element<D>(r.dh[n], e);
                 acc[n][0][e] = fmaf(d, yhat[n][e], acc[n][0][e]);
                 if constexpr (BIAS) acc[n][1][e] += d;
                 de[n][e] = d * wy;
@@ -255,9 +276,9 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
                 s[1] += de[n][e];
             }
         }
-        load_first(next);                                                                 // (where what they held is used up)
+        load_first(r, next);                                                              // (where what they held is used up)
         if (pre) sum(s);
-        float s1 = s[0] * per, s0 = a.pre == LSP_NORM_LAYER ? s[1] * per : 0.0f;
+        float s1 = pre ? s[0] * per * rstd_y : 0.0f, s0 = a.pre == LSP_NORM_LAYER ? s[1] * per * rstd_y : 0.0f;
         s[0] = s[1] = 0.0f;
         afresh();
 #pragma unroll
@@ -266,31 +287,37 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-                const float wf = element<D>(wf_[n], e), bf = (BIAS ? element<D>(bf_[n], e) : 0.0f), g = element<D>(g_[n], e);
-                const float total = element<D>(dyp[n], e) + (pre ? rstd_y * (de[n][e] - s0 - yhat[n][e] * s1) : de[n][e]);
+                const float wf = of(wf_[n], e), bf = BIAS ? of(bf_[n], e) : 0.0f, gate = of(g_[n], e);
+                const float dy = element<D>(r.dy[n], e), total = pre ? fmaf(de[n][e], rstd_y, dy - s0) - yhat[n][e] * s1 : dy + de[n][e];
                 out.x[e] = a.residual_scale * total;
-                const bool keep = !DROP || ((kept[n] >> e) & 1u);
-                const float branch = keep ? a.branch_scale * total * (DROP ? a.drop.scale : 1.0f) : 0.0f, u = keep ? fmaf(fhat[n][e], wf, bf) : 0.0f;
-                const float du = branch * g;
+                const float branch = !DROP || kept[n][e] ? total : 0.0f, u = !DROP || kept[n][e] ? fmaf(fhat[n][e], wf, bf) : 0.0f;
+                const float du = branch * (scale_u * gate);
                 acc[n][2][e] = fmaf(branch, u, acc[n][2][e]);
                 acc[n][3][e] = fmaf(du, fhat[n][e], acc[n][3][e]);
                 if constexpr (BIAS) acc[n][4][e] += du;
-                de[n][e] = e < left_of(n) ? du * wf : 0.0f;
+                de[n][e] = du * wf;
                 s[0] = fmaf(de[n][e], fhat[n][e], s[0]);
                 s[1] += de[n][e];
             }
-            if (mine) store_eight<D>(static_cast<elem*>(a.dx) + row * a.dx_stride + col_of(n), out, left_of(n));
+            if (mine) store_ending<D>(static_cast<elem*>(a.dx) + row * a.dx_stride + col_of(n), out, others(n));
         }
-        load_dy(next);
+        load_dy(r, next);
         if (post) sum(s);
-        s1 = s[0] * per; s0 = a.post == LSP_NORM_LAYER ? s[1] * per : 0.0f;
+        s1 = s[0] * per * rstd_f; s0 = a.post == LSP_NORM_LAYER ? s[1] * per * rstd_f : 0.0f;
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
             Eight out;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) out.x[e] = post ? rstd_f * (de[n][e] - s0 - fhat[n][e] * s1) : de[n][e];
-            if (mine) store_eight<D>(static_cast<elem*>(a.df) + row * a.df_stride + col_of(n), out, left_of(n));
+            for (int e = 0; e < 8; ++e) out.x[e] = post ? fmaf(de[n][e], rstd_f, -s0) - fhat[n][e] * s1 : de[n][e];
+            if (mine) store_ending<D>(static_cast<elem*>(a.df) + row * a.df_stride + col_of(n), out, others(n));
         }
+    };
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) { load_first(rows_[k], first + k * step); load_dy(rows_[k], first + k * step); }
+    for (int64_t base = first; base < a.rows; base += AHEAD * step) {
+        one_row(rows_[0], base);
+        if constexpr (AHEAD > 1)
+            if (base + step < a.rows) one_row(rows_[1], base + step);
     }
     // the workgroup's part of the sums over rows
     int slot = 0;
@@ -301,9 +328,9 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
         for (int n = 0; n < NV; ++n) {
             Eight v;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v.x[e] = acc[n][k][e];
+            for (int e = 0; e < 8; ++e) v.x[e] = acc[n][k][e] * (k == 2 ? scale_u : 1.0f);
             if (GROUPS > 1 && !a.many) {                                                  // (few rows: every group's part by itself, the adding is short)
-                store_eight<F32>(a.partial + (((int64_t)slot * gridDim.x + blockIdx.x) * GROUPS + group) * width + col_of(n), v, left_of(n));
+                store_ending<F32>(a.partial + (((int64_t)slot * gridDim.x + blockIdx.x) * GROUPS + group) * width + col_of(n), v, others(n));
                 continue;
             }
             if constexpr (GROUPS > 1) {
@@ -318,7 +345,7 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
 #pragma unroll
                         for (int e = 0; e < 8; ++e) v.x[e] += scratch[(o * 8 + e) * TPR + t];
             }
-            if (group == 0) store_eight<F32>(a.partial + ((int64_t)slot * gridDim.x + blockIdx.x) * width + col_of(n), v, left_of(n));
+            if (group == 0) store_ending<F32>(a.partial + ((int64_t)slot * gridDim.x + blockIdx.x) * width + col_of(n), v, others(n));
         }
         ++slot;
     }
@@ -349,8 +376,9 @@ __global__ __launch_bounds__(1024) void k_residual_norm_sums(const ResidualNormA
 }
 
 // Backward: threads of a row, and rows that a workgroup has at a time, by their width.  One workgroup a CU: its registers hold no second one of 512 threads, and fewer
-// workgroups leave fewer parts to add (4096 x 4096, bf16: 48 + 5 us; twice as many workgroups 53 + 7; two a CU at 128 registers, with spills, 91).  Beyond 4096 columns
-// two units a thread, which spill some (4096 x 8192, fp16: 119 us; one unit in 1024 threads has half the registers a thread and spills more: 252).
+// workgroups leave fewer parts to add (4096 x 4096, bf16, 201 MB: 39 us, 5.1 TB/s, and 5 to add the parts; in a form that took 48 + 5, twice as many workgroups took 53 + 7
+// and two a CU at 128 registers, with spills, 91).  Beyond 4096 columns two units a thread, which spill some (4096 x 8192, fp16: 101 us; one unit in 1024 threads has half the
+// registers a thread and spills more: 252).
 static int row_threads(int width) { return width <= 512 ? 64 : width <= 1024 ? 128 : width <= 2048 ? 256 : 512; }
 static int row_groups(int width) { return width <= 512 ? 8 : width <= 1024 ? 4 : width <= 2048 ? 2 : 1; }
 static int64_t workgroups_of(int64_t rows, int32_t width) {

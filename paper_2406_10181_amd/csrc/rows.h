@@ -78,6 +78,24 @@ template <typename D> __device__ __forceinline__ Eight load_eight(const typename
     return widen_eight<D>(load_packed<D>(p, left));
 }
 
+// Eight elements at p of which the first `first` belong to somebody else.  They are read with the others where that may be (`whole`, the same for all), so that nothing is
+// put together from parts before it is needed, and otherwise are zeros; first = 8: zeros.
+template <typename D> __device__ __forceinline__ Packed<D> load_ending(const typename D::elem* p, int first, bool whole) {
+    Packed<D> r;
+#pragma unroll
+    for (int k = 0; k < 2 * D::size; ++k) r.w[k] = 0;
+    if (first == 0 || (whole && first < 8)) r = load_whole<D>(p);
+    else if (!whole) {
+#pragma unroll
+        for (int e = 1; e < 8; ++e) {
+            if (e < first) continue;
+            if constexpr (D::size == 4) r.w[e] = __float_as_uint(p[e]);
+            else r.w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+        }
+    }
+    return r;
+}
+
 // Sum over a wave, in every lane.  Sums of 16 lanes and then of the four sixteens by moves between lanes that need no LDS.
 template <int CTRL, int ROWS> __device__ __forceinline__ float plus_lane(float x) {
     return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, ROWS, 0xF, false));
@@ -88,7 +106,7 @@ __device__ __forceinline__ float wave_sum(float x) {
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 
-template <typename D> __device__ __forceinline__ void store_eight(typename D::elem* p, const Eight& r, int left) {
+template <typename D> __device__ __forceinline__ Packed<D> narrow_eight(const Eight& r) {
     Packed<D> o;
     if constexpr (D::size == 4) {
 #pragma unroll
@@ -97,15 +115,30 @@ template <typename D> __device__ __forceinline__ void store_eight(typename D::el
 #pragma unroll
         for (int k = 0; k < 4; ++k) o.w[k] = (uint32_t)narrow<D>(r.x[2 * k]) | (uint32_t)narrow<D>(r.x[2 * k + 1]) << 16;
     }
-    if (left >= 8) {
-        if constexpr (D::size == 2) {
-            *reinterpret_cast<u32x4_any2*>(p) = u32x4{o.w[0], o.w[1], o.w[2], o.w[3]};
-        } else {
-            *reinterpret_cast<u32x4_any4*>(p) = u32x4{o.w[0], o.w[1], o.w[2], o.w[3]};
-            *reinterpret_cast<u32x4_any4*>(p + 4) = u32x4{o.w[4], o.w[5], o.w[6], o.w[7]};
-        }
-        return;
+    return o;
+}
+template <typename D> __device__ __forceinline__ void store_whole(typename D::elem* p, const Packed<D>& o) {
+    if constexpr (D::size == 2) {
+        *reinterpret_cast<u32x4_any2*>(p) = u32x4{o.w[0], o.w[1], o.w[2], o.w[3]};
+    } else {
+        *reinterpret_cast<u32x4_any4*>(p) = u32x4{o.w[0], o.w[1], o.w[2], o.w[3]};
+        *reinterpret_cast<u32x4_any4*>(p + 4) = u32x4{o.w[4], o.w[5], o.w[6], o.w[7]};
     }
+}
+// Eight elements but the first `first`
+template <typename D> __device__ __forceinline__ void store_ending(typename D::elem* p, const Eight& r, int first) {
+    const Packed<D> o = narrow_eight<D>(r);
+    if (first == 0) { store_whole<D>(p, o); return; }
+#pragma unroll
+    for (int e = 1; e < 8; ++e) {
+        if (e < first) continue;
+        if constexpr (D::size == 4) p[e] = __uint_as_float(o.w[e]);
+        else p[e] = (uint16_t)(o.w[e >> 1] >> (16 * (e & 1)));
+    }
+}
+template <typename D> __device__ __forceinline__ void store_eight(typename D::elem* p, const Eight& r, int left) {
+    const Packed<D> o = narrow_eight<D>(r);
+    if (left >= 8) { store_whole<D>(p, o); return; }
     const int n = max(left, 0);
     const bool four = n & 4, two = n & 2;
     if constexpr (D::size == 2) {
