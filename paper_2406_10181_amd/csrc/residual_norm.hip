@@ -47,8 +47,27 @@ template <int TPR, int N> struct RowSum {
     }
 };
 
+// Columns of a thread: eight from `col` on.  The last thread of a row has the row's last eight, of which the first `others` are the thread's before it (and all eight, where the
+// row has ended): they count in no sum and are not stored.  A block put together from smaller loads would wait for them at once, and every thread of the row for it (backward,
+// 3001 rows: 2999 columns took 8 us longer than 3000, so 3).
+struct Columns { int col, others; };
+__device__ __forceinline__ Columns columns_of(int unit, int width) {
+    const int col = min(unit * 8, width - 8);
+    return {col, min(unit * 8 - col, 8)};
+}
+
+// Which of a thread's eight elements are kept, as bits
+__device__ __forceinline__ uint32_t kept_bits(int64_t row, int unit, int others, int width, const Dropout& drop) {
+    const uint64_t n = (uint64_t)row * (uint64_t)((width + 7) >> 3) + (uint64_t)unit;
+    const u32x4 w = philox((uint32_t)n, (uint32_t)(n >> 32), 0, drop.offset, drop.key0, drop.key1);
+    uint32_t bits = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bits |= (philox_word(w, e) >= drop.limit ? 1u : 0u) << e;
+    return bits << others;                                                                // (the block's words belong to the last columns)
+}
+
 // mean and 1 / deviation of a row, by kind; v becomes (v - mean) / deviation
-template <int TPR, int NV> __device__ __forceinline__ void normalise(Eight (&v)[NV], int kind, int width, float eps, int lane_col, RowSum<TPR, 1>& sum, float& mean, float& rstd) {
+template <int TPR, int NV> __device__ __forceinline__ void normalise(Eight (&v)[NV], const Columns (&c)[NV], int kind, int width, float eps, RowSum<TPR, 1>& sum, float& mean, float& rstd) {
     mean = 0.0f; rstd = 1.0f;
     if (kind == LSP_NORM_NONE) return;
     const float per = 1.0f / (float)width;
@@ -57,21 +76,19 @@ template <int TPR, int NV> __device__ __forceinline__ void normalise(Eight (&v)[
 #pragma unroll
         for (int n = 0; n < NV; ++n)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[0] += v[n].x[e];                                // (columns from width on are zeros)
+            for (int e = 0; e < 8; ++e) s[0] += v[n].x[e];                                // (others' columns are zeros)
         sum(s);
         mean = s[0] * per;
     }
     float s[1] = {0.0f};
 #pragma unroll
-    for (int n = 0; n < NV; ++n) {
-        const int col = lane_col + n * TPR * 8;
+    for (int n = 0; n < NV; ++n)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float t = col + e < width ? v[n].x[e] - mean : 0.0f;
+            const float t = e >= c[n].others ? v[n].x[e] - mean : 0.0f;
             s[0] = fmaf(t, t, s[0]);
             v[n].x[e] = t;
         }
-    }
     sum(s);
     rstd = 1.0f / sqrtf(s[0] * per + eps);
 #pragma unroll
@@ -80,21 +97,13 @@ template <int TPR, int NV> __device__ __forceinline__ void normalise(Eight (&v)[
         for (int e = 0; e < 8; ++e) v[n].x[e] *= rstd;
 }
 
-template <typename D> __device__ __forceinline__ Eight vector_eight(const void* p, int col, int width, float otherwise) {
-    if (!p) {
-        Eight r;
+// A weight's or bias' columns, or `otherwise` where it has none
+template <typename D> __device__ __forceinline__ Packed<D> vector_packed(const void* p, const Columns& c, bool whole, float otherwise) {
+    if (p) return load_ending<D>(static_cast<const typename D::elem*>(p) + c.col, c.others, whole);
+    Eight r;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r.x[e] = otherwise;
-        return r;
-    }
-    return load_eight<D>(static_cast<const typename D::elem*>(p) + col, width - col);
-}
-
-template <typename D> __device__ __forceinline__ void drop_eight(Eight& v, int64_t row, int col, int width, const Dropout& drop) {
-    const uint64_t n = (uint64_t)row * (uint64_t)((width + 7) >> 3) + (uint64_t)(col >> 3);
-    const u32x4 w = philox((uint32_t)n, (uint32_t)(n >> 32), 0, drop.offset, drop.key0, drop.key1);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v.x[e] = philox_word(w, e) < drop.limit ? 0.0f : v.x[e] * drop.scale;
+    for (int e = 0; e < 8; ++e) r.x[e] = otherwise;
+    return narrow_eight<D>(r);
 }
 
 template <typename D, int TPR, int NV, int GROUPS, bool DROP>
@@ -109,40 +118,53 @@ __global__ __launch_bounds__(TPR * GROUPS) void k_residual_norm(const ResidualNo
     RowSum<TPR, 1> sum{scratch[group]};
     const elem* x = static_cast<const elem*>(a.x) + row * a.x_stride;
     const elem* f = static_cast<const elem*>(a.f) + row * a.f_stride;
+    const bool whole = width >= 8, x_whole = whole && a.y != a.x;                         // (in place: a neighbour may have stored already)
+    Columns c[NV];
     Eight xv[NV], fv[NV];
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
-        const int col = (t + n * TPR) * 8;
-        xv[n] = load_eight<D>(x + col, width - col);
-        fv[n] = load_eight<D>(f + col, width - col);
+        c[n] = columns_of(t + n * TPR, width);
+        xv[n] = widen_eight<D>(load_ending<D>(x + c[n].col, c[n].others, x_whole));
+        fv[n] = widen_eight<D>(load_ending<D>(f + c[n].col, c[n].others, whole));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) fv[n].x[e] = e >= c[n].others ? fv[n].x[e] : 0.0f;
     }
-    float mean_f, rstd_f, mean_y, rstd_y;
-    normalise<TPR, NV>(fv, a.post, width, a.eps, t * 8, sum, mean_f, rstd_f);
+    // What the row is multiplied with is asked for before the sums that come first (4096 x 4096, layer norms with biases and dropout, fp16: 31 to 26 us).
+    Packed<D> w[NV], b[NV], g[NV];
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
-        const int col = (t + n * TPR) * 8;
-        if (a.post != LSP_NORM_NONE) {
-            const Eight w = vector_eight<D>(a.post_w, col, width, 1.0f), b = vector_eight<D>(a.post_b, col, width, 0.0f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) fv[n].x[e] = fmaf(fv[n].x[e], w.x[e], b.x[e]);
-        }
-        if constexpr (DROP) drop_eight<D>(fv[n], row, col, width, a.drop);
-        const Eight g = vector_eight<D>(a.gate, col, width, 1.0f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) xv[n].x[e] = col + e < width ? fmaf(a.branch_scale * g.x[e], fv[n].x[e], a.residual_scale * xv[n].x[e]) : 0.0f;
-        if (mine) store_eight<D>(static_cast<elem*>(a.y) + row * a.y_stride + col, xv[n], width - col);
+        w[n] = vector_packed<D>(a.post != LSP_NORM_NONE ? a.post_w : nullptr, c[n], whole, 1.0f);
+        b[n] = vector_packed<D>(a.post != LSP_NORM_NONE ? a.post_b : nullptr, c[n], whole, 0.0f);
+        g[n] = vector_packed<D>(a.gate, c[n], whole, 1.0f);
     }
-    normalise<TPR, NV>(xv, a.pre, width, a.eps, t * 8, sum, mean_y, rstd_y);
+    float mean_f, rstd_f, mean_y, rstd_y;
+    normalise<TPR, NV>(fv, c, a.post, width, a.eps, sum, mean_f, rstd_f);
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+        if (a.post != LSP_NORM_NONE) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) fv[n].x[e] = fmaf(fv[n].x[e], element<D>(w[n], e), element<D>(b[n], e));
+        }
+        if constexpr (DROP) {
+            const uint32_t kept = kept_bits(row, t + n * TPR, c[n].others, width, a.drop);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) fv[n].x[e] = kept >> e & 1u ? fv[n].x[e] * a.drop.scale : 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) xv[n].x[e] = e >= c[n].others ? fmaf(a.branch_scale * element<D>(g[n], e), fv[n].x[e], a.residual_scale * xv[n].x[e]) : 0.0f;
+        if (mine) store_ending<D>(static_cast<elem*>(a.y) + row * a.y_stride + c[n].col, xv[n], c[n].others);
+        w[n] = vector_packed<D>(a.pre != LSP_NORM_NONE ? a.pre_w : nullptr, c[n], whole, 1.0f);
+        b[n] = vector_packed<D>(a.pre != LSP_NORM_NONE ? a.pre_b : nullptr, c[n], whole, 0.0f);
+    }
+    normalise<TPR, NV>(xv, c, a.pre, width, a.eps, sum, mean_y, rstd_y);
     if (mine && a.h) {
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
-            const int col = (t + n * TPR) * 8;
             if (a.pre != LSP_NORM_NONE) {
-                const Eight w = vector_eight<D>(a.pre_w, col, width, 1.0f), b = vector_eight<D>(a.pre_b, col, width, 0.0f);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) xv[n].x[e] = fmaf(xv[n].x[e], w.x[e], b.x[e]);
+                for (int e = 0; e < 8; ++e) xv[n].x[e] = fmaf(xv[n].x[e], element<D>(w[n], e), element<D>(b[n], e));
             }
-            store_eight<D>(static_cast<elem*>(a.h) + row * a.h_stride + col, xv[n], width - col);
+            store_ending<D>(static_cast<elem*>(a.h) + row * a.h_stride + c[n].col, xv[n], c[n].others);
         }
     }
     if (mine && t == 0) {
@@ -162,10 +184,9 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
     __shared__ float scratch[GROUPS > 1 ? (GROUPS - 1) * TPR * 8 : kSumFloats];           // RowSum's, and at the end the other groups' sums over rows
     const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR), t = threadIdx.x % TPR;
     const int width = a.width;
-    // The last thread of a row has the row's last eight columns, of which the first `others` are the thread's before it: there its weights are zeros, so they add nothing to any
-    // sum, and they are not stored.  (A block put together from smaller loads waits for them at once, and every thread of the row for it: 2999 columns took 8 us longer than 3000, now 3.)
-    const auto col_of = [&](int n) { return min((t + n * TPR) * 8, width - 8); };
-    const auto others = [&](int n) { return min((t + n * TPR) * 8 - col_of(n), 8); };
+    Columns c[NV];
+#pragma unroll
+    for (int n = 0; n < NV; ++n) c[n] = columns_of(t + n * TPR, width);
     const bool whole = width >= 8, dy_whole = whole && a.dx != a.dy;                      // (in place: a neighbour may have stored already)
     const float per = 1.0f / (float)width, scale_u = DROP ? a.branch_scale * a.drop.scale : a.branch_scale;
     RowSum<TPR, 2> sum{scratch + group * 4 * (TPR / 64)};
@@ -174,10 +195,11 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
     constexpr bool HELD = NV == 1;
     struct Vector { Packed<D> packed; float value[8]; };
     Vector wf_[NV], bf_[NV], g_[NV], wy_[NV];
+    // (Zeros for others' columns: they add nothing to any sum.)
     const auto vector = [&](Vector& v, const void* p, float otherwise, bool zeros, int n) {
-        const int first = zeros ? others(n) : 0;
+        const int first = zeros ? c[n].others : 0;
         Eight r;
-        if (p) r = widen_eight<D>(load_ending<D>(static_cast<const elem*>(p) + col_of(n), others(n), whole));
+        if (p) r = widen_eight<D>(load_ending<D>(static_cast<const elem*>(p) + c[n].col, c[n].others, whole));
 #pragma unroll
         for (int e = 0; e < 8; ++e) v.value[e] = e < first ? 0.0f : p ? r.x[e] : otherwise;
         if constexpr (!HELD) {
@@ -225,7 +247,7 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
         for (int k = 0; k < 4; ++k) r.stats[k] = (a.stats + k * a.rows + row)[lane0];
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
-            const int col = col_of(n), first = base + group < a.rows ? others(n) : 8;     // (zeros where the group has no row: its sums then get zeros)
+            const int col = c[n].col, first = base + group < a.rows ? c[n].others : 8;     // (zeros where the group has no row: its sums then get zeros)
             r.x[n] = load_ending<D>(x + col, first, whole);
             r.f[n] = load_ending<D>(f + col, first, whole);
             r.dh[n] = load_ending<D>(dh + col, a.dh ? first : 8, whole);
@@ -234,7 +256,7 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
     const auto load_dy = [&](Row& r, int64_t base) {
         const int64_t row = base + group < a.rows ? base + group : a.rows - 1;
 #pragma unroll
-        for (int n = 0; n < NV; ++n) r.dy[n] = load_ending<D>(static_cast<const elem*>(a.dy) + row * a.dy_stride + col_of(n), base + group < a.rows ? others(n) : 8, dy_whole);
+        for (int n = 0; n < NV; ++n) r.dy[n] = load_ending<D>(static_cast<const elem*>(a.dy) + row * a.dy_stride + c[n].col, base + group < a.rows ? c[n].others : 8, dy_whole);
     };
     const int64_t step = (int64_t)gridDim.x * GROUPS, first = (int64_t)blockIdx.x * GROUPS;
     const auto one_row = [&](Row& r, int64_t base) {
@@ -243,30 +265,17 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
         const float mean_f = r.stats[0], rstd_f = r.stats[1], mean_y = r.stats[2], rstd_y = r.stats[3];
         afresh();
         // y^ and f^, and the gradient of y^
-        bool kept[NV][8];
+        uint32_t kept[NV];
         float fhat[NV][8], yhat[NV][8], de[NV][8], s[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
-            if constexpr (DROP) {
-                const uint64_t at = (uint64_t)row * (uint64_t)((width + 7) >> 3) + (uint64_t)(t + n * TPR);
-                const u32x4 w = philox((uint32_t)at, (uint32_t)(at >> 32), 0, a.drop.offset, a.drop.key0, a.drop.key1);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) kept[n][e] = philox_word(w, e) >= a.drop.limit;
-                if (others(n)) {                                                          // (the block's words belong to the last columns)
-                    uint32_t bits = 0;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) bits |= (kept[n][e] ? 1u : 0u) << e;
-                    bits <<= others(n);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) kept[n][e] = bits >> e & 1u;
-                }
-            }
+            if constexpr (DROP) kept[n] = kept_bits(row, t + n * TPR, c[n].others, width, a.drop);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);                        // (four at a time: eight would take registers for speed that nothing waits for)
                 const float wf = of(wf_[n], e), bf = BIAS ? of(bf_[n], e) : 0.0f, gate = of(g_[n], e), wy = of(wy_[n], e);
                 fhat[n][e] = (element<D>(r.f[n], e) - mean_f) * rstd_f;
-                const float u = !DROP ? fmaf(fhat[n][e], wf, bf) : kept[n][e] ? fmaf(fhat[n][e], wf, bf) : 0.0f;   // (what is dropped may be infinite)
+                const float u = !DROP ? fmaf(fhat[n][e], wf, bf) : (kept[n] >> e & 1u) ? fmaf(fhat[n][e], wf, bf) : 0.0f;   // (what is dropped may be infinite)
                 yhat[n][e] = fmaf(scale_u * gate, u, fmaf(a.residual_scale, element<D>(r.x[n], e), -mean_y)) * rstd_y;
                 const float d = element<D>(r.dh[n], e);
                 acc[n][0][e] = fmaf(d, yhat[n][e], acc[n][0][e]);
@@ -290,7 +299,7 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
                 const float wf = of(wf_[n], e), bf = BIAS ? of(bf_[n], e) : 0.0f, gate = of(g_[n], e);
                 const float dy = element<D>(r.dy[n], e), total = pre ? fmaf(de[n][e], rstd_y, dy - s0) - yhat[n][e] * s1 : dy + de[n][e];
                 out.x[e] = a.residual_scale * total;
-                const float branch = !DROP || kept[n][e] ? total : 0.0f, u = !DROP || kept[n][e] ? fmaf(fhat[n][e], wf, bf) : 0.0f;
+                const float branch = !DROP || (kept[n] >> e & 1u) ? total : 0.0f, u = !DROP || (kept[n] >> e & 1u) ? fmaf(fhat[n][e], wf, bf) : 0.0f;
                 const float du = branch * (scale_u * gate);
                 acc[n][2][e] = fmaf(branch, u, acc[n][2][e]);
                 acc[n][3][e] = fmaf(du, fhat[n][e], acc[n][3][e]);
@@ -299,7 +308,7 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
                 s[0] = fmaf(de[n][e], fhat[n][e], s[0]);
                 s[1] += de[n][e];
             }
-            if (mine) store_ending<D>(static_cast<elem*>(a.dx) + row * a.dx_stride + col_of(n), out, others(n));
+            if (mine) store_ending<D>(static_cast<elem*>(a.dx) + row * a.dx_stride + c[n].col, out, c[n].others);
         }
         load_dy(r, next);
         if (post) sum(s);
@@ -309,7 +318,7 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
             Eight out;
 #pragma unroll
             for (int e = 0; e < 8; ++e) out.x[e] = post ? fmaf(de[n][e], rstd_f, -s0) - fhat[n][e] * s1 : de[n][e];
-            if (mine) store_ending<D>(static_cast<elem*>(a.df) + row * a.df_stride + col_of(n), out, others(n));
+            if (mine) store_ending<D>(static_cast<elem*>(a.df) + row * a.df_stride + c[n].col, out, c[n].others);
         }
     };
 #pragma unroll
@@ -330,7 +339,7 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
 #pragma unroll
             for (int e = 0; e < 8; ++e) v.x[e] = acc[n][k][e] * (k == 2 ? scale_u : 1.0f);
             if (GROUPS > 1 && !a.many) {                                                  // (few rows: every group's part by itself, the adding is short)
-                store_ending<F32>(a.partial + (((int64_t)slot * gridDim.x + blockIdx.x) * GROUPS + group) * width + col_of(n), v, others(n));
+                store_ending<F32>(a.partial + (((int64_t)slot * gridDim.x + blockIdx.x) * GROUPS + group) * width + c[n].col, v, c[n].others);
                 continue;
             }
             if constexpr (GROUPS > 1) {
@@ -345,7 +354,7 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
 #pragma unroll
                         for (int e = 0; e < 8; ++e) v.x[e] += scratch[(o * 8 + e) * TPR + t];
             }
-            if (group == 0) store_ending<F32>(a.partial + ((int64_t)slot * gridDim.x + blockIdx.x) * width + col_of(n), v, others(n));
+            if (group == 0) store_ending<F32>(a.partial + ((int64_t)slot * gridDim.x + blockIdx.x) * width + c[n].col, v, c[n].others);
         }
         ++slot;
     }
