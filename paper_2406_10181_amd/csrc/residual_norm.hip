@@ -425,8 +425,8 @@ template <typename D, int TPR, int NV, int GROUPS> static hipError_t run_backwar
     return hipGetLastError();
 }
 
-// Forward: a row has as few idle threads as the variants allow (2999 columns in 128 threads of 24 columns 24 us, in 256 threads of 16 columns 30: 3001 rows, fp16,
-// dropout); beyond 4096 columns two units a thread in 512 threads (16384 rows of 8192, bf16: 198 us; one unit in 1024 threads 215, four in 256 threads 241).
+// Forward: a row has as few idle threads as the variants allow (2999 columns in 128 threads of 24 columns 21.3 us, in 256 threads of 16 columns 22.8: 3001 rows, fp16,
+// dropout); beyond 4096 columns two units a thread in 512 threads (16384 rows of 8192, bf16, 1074 MB: 188 us, 5.7 TB/s; one unit in 1024 threads 307, four in 256 threads 189).
 template <typename D> static hipError_t forward_of(const ResidualNormArgs& a, hipStream_t st) {
     if (a.width <= 64 * 8) return run_forward<D, 64, 1, 4>(a, st);
     if (a.width <= 64 * 16) return run_forward<D, 64, 2, 4>(a, st);
