@@ -30,6 +30,24 @@ static int waves_for(int64_t units, int64_t rows, int64_t keys, int head_dim, ls
     return dtype != LSP_F32 && head_dim > 64 && keys >= 2048 && units * ((rows + 8 * kWaveRows - 1) / (8 * kWaveRows)) >= 256 ? 8 : 4;
 }
 
+// In how many parts the steps of a tile are done, by workgroups of their own: what takes the least time by a rough account.  A step takes a workgroup that has a CU for itself about
+// step_us; a part's sums (`bytes` for all tiles) are written and read again, at 5 bytes a ps, and are added by a launch of its own, 4 us.  No more parts than give each CU two workgroups.
+static int parts_for(int64_t tiles, int64_t steps, double step_us, int64_t bytes) {
+    const int64_t most = std::min<int64_t>({512 / std::max<int64_t>(tiles, 1), steps, 16});
+    int best = 1;
+    double least = (double)steps * step_us;
+    for (int p = 2; p <= most; ++p) {
+        const double us = (double)((steps + p - 1) / p) * step_us + 4.0 + p * (0.25 + 2.0 * (double)bytes / 5e6);
+        if (us < least) { least = us; best = p; }
+    }
+    return best;
+}
+// of a wave's 32 rows and one tile of the others, `products` of them; 16 bits: 64 a tile, fp32: 32
+static double step_us(const AttentionArgs& a, lsp_dtype dtype, int products) {
+    const int dim = (a.head_dim + 31) / 32 * 32;
+    return products * dim * (dtype == LSP_F32 ? 1.0 / 64 : 1.0 / 256) * (a.drop.limit ? 1.5 : 1.0);
+}
+
 void plan_attention_forward(AttentionArgs& a, lsp_dtype dtype) {
     // Few queries: the query heads that share a key head go into one tile of rows, so that keys and values are read once for all of them.
     // (Its rows are addressed with 32 bits from the first head's first row.)
@@ -39,25 +57,22 @@ void plan_attention_forward(AttentionArgs& a, lsp_dtype dtype) {
     a.few = dtype != LSP_F32 && a.rows <= 32 && a.drop.limit == 0;
     a.waves = a.packed ? 4 : waves_for(units, a.rows, a.k_len, a.head_dim, dtype);
     a.tiles = a.few ? 1 : (int)((a.rows + a.waves * kWaveRows - 1) / (a.waves * kWaveRows));
-    // Few tiles of rows: the keys are split, as far as that gives each CU two workgroups (few queries: four) and each of these four tiles of keys (two a wave).
+    // Few tiles of rows: the keys are split.  (Few queries: as far as that gives each CU four workgroups, and each of these two tiles of keys a wave.)
     const int tile = a.few ? 32 : tile_rows_of(dtype);
     const int64_t row_tiles = units * a.tiles;
     const int key_tiles = (a.k_len + tile - 1) / tile;
-    const int splits = a.waves == 8 ? 1 : (int)std::min<int64_t>({std::max<int64_t>((a.few ? 1024 : 512) / row_tiles, 1), std::max(key_tiles / (a.few ? 8 : 4), 1), 64});
+    const int splits = a.few ? (int)std::min<int64_t>({std::max<int64_t>(1024 / row_tiles, 1), std::max(key_tiles / 8, 1), 64})
+                     : a.waves == 8 ? 1 : parts_for(row_tiles, key_tiles, step_us(a, dtype, 2), units * a.rows * a.head_dim * 4);
     a.split_tiles = (key_tiles + splits - 1) / splits;
     a.splits = (key_tiles + a.split_tiles - 1) / a.split_tiles;
 }
 
-// Workgroups of the backward pass that share a tile: as many as give each CU two, with four steps or more each.  What they add up goes through memory in
-// fp32, two more passes over the gradient a part.
-static int parts_for(int64_t tiles, int64_t steps) {
-    return (int)std::min<int64_t>({std::max<int64_t>(512 / tiles, 1), std::max<int64_t>(steps / 4, 1), 16});
-}
 void plan_attention_backward(AttentionArgs& a, lsp_dtype dtype) {
     const int64_t key_tiles = (int64_t)a.batch * a.kv_heads * ((a.k_len + kBackwardRows - 1) / kBackwardRows);
     const int64_t query_tiles = (int64_t)a.batch * a.heads * ((a.q_len + kBackwardRows - 1) / kBackwardRows);
-    a.key_parts = parts_for(key_tiles, (int64_t)a.group * ((a.q_len + tile_rows_of(dtype) - 1) / tile_rows_of(dtype)));
-    a.query_parts = parts_for(query_tiles, (a.k_len + tile_rows_of(dtype) - 1) / tile_rows_of(dtype));
+    const int64_t q_steps = (a.q_len + tile_rows_of(dtype) - 1) / tile_rows_of(dtype), k_steps = (a.k_len + tile_rows_of(dtype) - 1) / tile_rows_of(dtype);
+    a.key_parts = parts_for(key_tiles, a.group * q_steps, step_us(a, dtype, 4), (int64_t)8 * a.batch * a.kv_heads * a.k_len * a.head_dim);
+    a.query_parts = parts_for(query_tiles, k_steps, step_us(a, dtype, 3), (int64_t)4 * a.batch * a.heads * a.q_len * a.head_dim);
 }
 size_t attention_backward_partial_bytes(const AttentionArgs& a) {
     const size_t keys = a.key_parts > 1 ? (size_t)2 * a.key_parts * a.batch * a.kv_heads * a.k_len : 0;
