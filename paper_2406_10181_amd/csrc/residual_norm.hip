@@ -191,40 +191,48 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
     const float per = 1.0f / (float)width, scale_u = DROP ? a.branch_scale * a.drop.scale : a.branch_scale;
     RowSum<TPR, 2> sum{scratch + group * 4 * (TPR / 64)};
     const bool post = a.post != LSP_NORM_NONE, pre = a.pre != LSP_NORM_NONE;
-    // Weights in fp32 while they have the registers for it (NV = 1), else packed: what is made of them in one half of a row for the other would take more.
+    // Weights stay in registers, in fp32, while these have room (NV = 1), else in LDS as they came, where each thread reads what it wrote, a unit at a time; as packed registers
+    // they made others spill (4096 x 8192, fp32: 253 us, so 165; with layer norms, biases and dropout 669, so 509; the same in fp16 244, so 197).
     constexpr bool HELD = NV == 1;
-    struct Vector { Packed<D> packed; float value[8]; };
-    Vector wf_[NV], bf_[NV], g_[NV], wy_[NV];
-    // (Zeros for others' columns: they add nothing to any sum.)
-    const auto vector = [&](Vector& v, const void* p, float otherwise, bool zeros, int n) {
-        const int first = zeros ? c[n].others : 0;
+    constexpr int kPieces = D::size / 2;                                                  // of 16 bytes, of eight elements
+    __shared__ u32x4 kept_weights[HELD ? 1 : 4 * NV * kPieces * TPR];
+    float held[HELD ? 4 : 1][8];
+    const auto vector = [&](int which, const void* p, float otherwise, bool zeros, int n) {
+        const int first = zeros ? c[n].others : 0;                                        // (zeros for others' columns: they add nothing to any sum)
         Eight r;
         if (p) r = widen_eight<D>(load_ending<D>(static_cast<const elem*>(p) + c[n].col, c[n].others, whole));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v.value[e] = e < first ? 0.0f : p ? r.x[e] : otherwise;
-        if constexpr (!HELD) {
+        for (int e = 0; e < 8; ++e) r.x[e] = e < first ? 0.0f : p ? r.x[e] : otherwise;
+        if constexpr (HELD) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) r.x[e] = v.value[e];
-            v.packed = narrow_eight<D>(r);
+            for (int e = 0; e < 8; ++e) held[which][e] = r.x[e];
+        } else {
+            const Packed<D> v = narrow_eight<D>(r);
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) kept_weights[((which * NV + n) * kPieces + k) * TPR + t] = u32x4{v.w[4 * k], v.w[4 * k + 1], v.w[4 * k + 2], v.w[4 * k + 3]};
         }
     };
-    const auto of = [&](const Vector& v, int e) { return HELD ? v.value[e] : element<D>(v.packed, e); };
+    enum { WF, BF, G, WY };
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
-        vector(wf_[n], post ? a.post_w : nullptr, 1.0f, false, n); vector(bf_[n], BIAS && post ? a.post_b : nullptr, 0.0f, false, n);
-        vector(g_[n], a.gate, 1.0f, true, n); vector(wy_[n], pre ? a.pre_w : nullptr, 1.0f, true, n);
+        vector(WF, post ? a.post_w : nullptr, 1.0f, false, n); if (BIAS) vector(BF, post ? a.post_b : nullptr, 0.0f, false, n);
+        vector(G, a.gate, 1.0f, true, n); vector(WY, pre ? a.pre_w : nullptr, 1.0f, true, n);
     }
-    const auto afresh = [&] {
-        if constexpr (!HELD) {
+    struct Weights { Packed<D> v[HELD ? 1 : 4]; };
+    const auto weights_of = [&](Weights& w, int n, bool all) {                            // for the next eight columns
+        if constexpr (!HELD)
 #pragma unroll
-            for (int n = 0; n < NV; ++n)
+            for (int which = 0; which < 4; ++which) {
+                if ((which == BF && !BIAS) || (which == WY && !all)) continue;
 #pragma unroll
-                for (int k = 0; k < 2 * D::size; ++k) {
-                    asm volatile("" : "+v"(wf_[n].packed.w[k]), "+v"(g_[n].packed.w[k]), "+v"(wy_[n].packed.w[k]));
-                    if constexpr (BIAS) asm volatile("" : "+v"(bf_[n].packed.w[k]));
+                for (int k = 0; k < kPieces; ++k) {
+                    const u32x4 v = kept_weights[((which * NV + n) * kPieces + k) * TPR + t];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w.v[which].w[4 * k + i] = v[i];
                 }
-        }
+            }
     };
+    const auto of = [&](const Weights& w, int which, int e) { if constexpr (HELD) return held[which][e]; else return element<D>(w.v[which], e); };
     float acc[NV][kGrads][8];
 #pragma unroll
     for (int n = 0; n < NV; ++n)
@@ -263,17 +271,18 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
         const bool mine = GROUPS == 1 || base + group < a.rows;
         const int64_t row = base + group < a.rows ? base + group : a.rows - 1, next = base + AHEAD * step;
         const float mean_f = r.stats[0], rstd_f = r.stats[1], mean_y = r.stats[2], rstd_y = r.stats[3];
-        afresh();
         // y^ and f^, and the gradient of y^
         uint32_t kept[NV];
         float fhat[NV][8], yhat[NV][8], de[NV][8], s[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
             if constexpr (DROP) kept[n] = kept_bits(row, t + n * TPR, c[n].others, width, a.drop);
+            Weights w;
+            weights_of(w, n, true);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);                        // (four at a time: eight would take registers for speed that nothing waits for)
-                const float wf = of(wf_[n], e), bf = BIAS ? of(bf_[n], e) : 0.0f, gate = of(g_[n], e), wy = of(wy_[n], e);
+                const float wf = of(w, WF, e), bf = BIAS ? of(w, BF, e) : 0.0f, gate = of(w, G, e), wy = of(w, WY, e);
                 fhat[n][e] = (element<D>(r.f[n], e) - mean_f) * rstd_f;
                 const float u = !DROP ? fmaf(fhat[n][e], wf, bf) : (kept[n] >> e & 1u) ? fmaf(fhat[n][e], wf, bf) : 0.0f;   // (what is dropped may be infinite)
                 yhat[n][e] = fmaf(scale_u * gate, u, fmaf(a.residual_scale, element<D>(r.x[n], e), -mean_y)) * rstd_y;
@@ -289,14 +298,15 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
         if (pre) sum(s);
         float s1 = pre ? s[0] * per * rstd_y : 0.0f, s0 = a.pre == LSP_NORM_LAYER ? s[1] * per * rstd_y : 0.0f;
         s[0] = s[1] = 0.0f;
-        afresh();
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
             Eight out;
+            Weights w;
+            weights_of(w, n, false);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-                const float wf = of(wf_[n], e), bf = BIAS ? of(bf_[n], e) : 0.0f, gate = of(g_[n], e);
+                const float wf = of(w, WF, e), bf = BIAS ? of(w, BF, e) : 0.0f, gate = of(w, G, e);
                 const float dy = element<D>(r.dy[n], e), total = pre ? fmaf(de[n][e], rstd_y, dy - s0) - yhat[n][e] * s1 : dy + de[n][e];
                 out.x[e] = a.residual_scale * total;
                 const float branch = !DROP || (kept[n] >> e & 1u) ? total : 0.0f, u = !DROP || (kept[n] >> e & 1u) ? fmaf(fhat[n][e], wf, bf) : 0.0f;
@@ -373,7 +383,14 @@ __global__ __launch_bounds__(1024) void k_residual_norm_sums(const ResidualNormA
     const float* p = a.partial + (int64_t)blockIdx.y * parts * a.width;
     float s = 0.0f;
     if (col < a.width)
-        for (int r = y; r < parts; r += 32) s += p[(int64_t)r * a.width + col];
+#pragma unroll 1
+        for (int r = y; r < parts; r += 32 * 8) {                                         // (eight on the way at a time)
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = r + 32 * k < parts ? p[(int64_t)(r + 32 * k) * a.width + col] : 0.0f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += v[k];
+        }
     add[y][x] = s;
     __syncthreads();
     if (y == 0 && col < a.width) {
@@ -386,8 +403,8 @@ __global__ __launch_bounds__(1024) void k_residual_norm_sums(const ResidualNormA
 
 // Backward: threads of a row, and rows that a workgroup has at a time, by their width.  One workgroup a CU: its registers hold no second one of 512 threads, and fewer
 // workgroups leave fewer parts to add (4096 x 4096, bf16, 201 MB: 39 us, 5.1 TB/s, and 5 to add the parts; in a form that took 48 + 5, twice as many workgroups took 53 + 7
-// and two a CU at 128 registers, with spills, 91).  Beyond 4096 columns two units a thread, which spill some (4096 x 8192, fp16: 101 us; one unit in 1024 threads has half the
-// registers a thread and spills more: 252).
+// and two a CU at 128 registers, with spills, 91).  Beyond 4096 columns two units a thread: 4096 x 8192, fp16
+// 83 us (403 MB, 4.9 TB/s), fp32 165; with biases, whose sums spill, 197 and 509.  (One unit in 1024 threads has half the registers a thread: 252 in fp16 without biases.)
 static int row_threads(int width) { return width <= 512 ? 64 : width <= 1024 ? 128 : width <= 2048 ? 256 : 512; }
 static int row_groups(int width) { return width <= 512 ? 8 : width <= 1024 ? 4 : width <= 2048 ? 2 : 1; }
 static int64_t workgroups_of(int64_t rows, int32_t width) {
