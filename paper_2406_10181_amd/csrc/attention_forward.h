@@ -1,12 +1,17 @@
 // The forward pass of attention: one pass over the keys with a running maximum and sum for each query.
 //
-// A workgroup has 128 or 256 query rows of a head, a wave 32 of them; tiles of keys and values go by in LDS, the next one on its way in registers
-// while the matrix cores work on the current.  The scores are made transposed, S^T = K Q^T: a lane then has all its scores (16 of every 32
+// A workgroup has 128 or 256 query rows of a head, a wave 32 of them; tiles of keys and values go by in LDS, the next one on its way straight to its
+// other half while the matrix cores work on the current.  The scores are made transposed, S^T = K Q^T: a lane then has all its scores (16 of every 32
 // keys; lane l ^ 32 has the others) of ONE query, so maxima and sums stay in the lane, and the accumulators are the operand of
 // O^T += V^T P^T as they are.
 //
 // The running maximum is moved only when a new one is larger by more than 8 in powers of two; until then probabilities are at most 2^8, and
-// neither their sum in fp32 nor their rounding minds, and the accumulators are left alone.
+// neither their sum in fp32 nor their rounding minds, and the accumulators are left alone.  Probabilities are rounded to the storage type as operands of
+// the second product, half a unit in the last place of each beside the result's own rounding; their sums, and L, are made before that.
+//
+// Heads of 128: bound by the matrix cores (one text of 8192, 16 heads, causal, bf16: 270 to 300 us, 275 GFLOP, 0.9 to 1.0 PFLOP/s; four of 1024, 32 heads: 52 us, 34 GFLOP).
+// Heads of 64: by exponentials and what else a score takes outside the matrix cores, a quarter-rate instruction and four others for 256 operations of theirs (16 heads, eight texts
+// of 2048, fp16: 180 us, 137 GFLOP, 0.76 PFLOP/s; the vector units are busy 83 % of the time, the matrix cores 48 %).
 #pragma once
 
 #include "attention_few.h"
@@ -229,7 +234,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2
     if (h == 0 && row < a.rows) a.L[((int64_t)b * a.heads + q_head) * a.q_len + qi] = l == 0.0f ? -INFINITY : m * a.scale + __logf(l);
 }
 
-// Joins the parts of a row: O = sum_s w_s O_s / sum_s w_s l_s with w_s = 2^(m_s - m).  A wave has a row: its lanes have a part's (m, l) each, and then two columns.
+// Joins the parts of a row: O = sum_s w_s O_s / sum_s w_s l_s with w_s = 2^(m_s - m).  Bound by memory, and where parts are few by its launch (4 us).  A wave has a row: its lanes have a part's (m, l) each, and then two columns.
 template <typename D>
 __global__ __launch_bounds__(256) void k_attention_join(const AttentionArgs a) {
     const int64_t lines = (int64_t)a.batch * a.heads * a.q_len;

@@ -31,7 +31,7 @@ static int waves_for(int64_t units, int64_t rows, int64_t keys, int head_dim, ls
 }
 
 // In how many parts the steps of a tile are done, by workgroups of their own: what takes the least time by a rough account.  A step takes a workgroup that has a CU for itself about
-// step_us; a part's sums (`bytes` for all tiles) are written and read again, at 5 bytes a ps, and are added by a launch of its own, 4 us.  No more parts than give each CU two workgroups.
+// step_us; a part's sums (`bytes` for all tiles) are written and read again, at 5 TB/s, and are added by a launch of its own, 4 us.  No more parts than give each CU two workgroups.
 static int parts_for(int64_t tiles, int64_t steps, double step_us, int64_t bytes) {
     const int64_t most = std::min<int64_t>({512 / std::max<int64_t>(tiles, 1), steps, 16});
     int best = 1;
