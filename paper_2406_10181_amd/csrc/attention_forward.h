@@ -11,7 +11,7 @@
 //
 // Heads of 128: bound by the matrix cores (one text of 8192, 16 heads, causal, bf16: 270 to 300 us, 275 GFLOP, 0.9 to 1.0 PFLOP/s; four of 1024, 32 heads: 52 us, 34 GFLOP).
 // Heads of 64: by exponentials and what else a score takes outside the matrix cores, a quarter-rate instruction and four others for 256 operations of theirs (16 heads, eight texts
-// of 2048, fp16: 180 us, 137 GFLOP, 0.76 PFLOP/s; the vector units are busy 83 % of the time, the matrix cores 48 %).
+// of 2048, fp16: 182 us, 137 GFLOP, 0.76 PFLOP/s; the vector units issue 70 % of the time, the matrix cores work 40 %).
 #pragma once
 
 #include "attention_few.h"
@@ -38,8 +38,10 @@ __device__ __forceinline__ void drop_keys(f32x16& s, int pair, uint32_t key0, ui
     }
 }
 
+// Two waves a SIMD at heads of 128, three below: one waits or takes exponentials while the others multiply (eight texts of 2048, 16 heads of 64, fp16: 182 us, with two 188; heads of 96
+// 236 and 242; 1073 queries and 2456 keys, heads of 32, 98 and 105; causal texts of 1024, heads of 64, 20 both, with four waves 27: all tiles at once, whatever their length).
 template <typename D, int DP, bool DROP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_attention_forward(const AttentionArgs a) {
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, DP <= 96 ? 3 : 2))) void k_attention_forward(const AttentionArgs a) {
     using T = Tile<D, DP>;
     constexpr int kRows = WAVES * kWaveRows;
     constexpr int BN = tile_rows<D>(), NT = 64 * WAVES, kSteps = DP / 16, kTiles = BN / 32, kCols = DP / 32;

@@ -4,7 +4,9 @@
 // A thread takes eight elements that follow one another in a row: one call of the generator, one load and one store of 16 (or, in
 // fp32, 32) bytes.  Rows need not be a multiple of anything: each begins a new block of eight, so that the mask of a row does not
 // depend on how the others lie; where rows begin off the 16-byte steps the loads are unaligned ones, and the last block of a row
-// goes element by element.
+// goes in pieces of four, two and one.
+//
+// Bound by memory: 4096 x 11008 bf16, 180 MB, 30 us, 6.0 TB/s; the generator's 28 products of 32 bits for eight elements hide behind it.
 //
 // Bound by memory: 4096 x 11008 bf16, 180 MB, 30 us, 6.0 TB/s (the generator's 28 products of 32 bits for eight elements hide behind it).
 #include "philox.h"
