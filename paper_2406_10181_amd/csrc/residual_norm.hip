@@ -12,7 +12,8 @@
 // f, in fp32: nothing of the row is stored but its four statistics.  A workgroup goes through many rows and keeps its part of the sums over
 // rows in registers; the parts are added by a second kernel in a fixed order, so the results do not depend on timing.
 //
-// Both are bound by memory: forward reads x and f and writes y and h, backward reads x, f, dy, dh and writes dx, df, each once.
+// Both are bound by memory, and nearly as much by the vector units: forward reads x and f and writes y and h (4096 x 4096, bf16, 134 MB: 23.6 us, 5.7 TB/s), backward reads x, f,
+// dy, dh and writes dx, df (201 MB: 39 us, 5.1 TB/s), each once.
 #include "residual_norm.h"
 #include "rows.h"
 
@@ -66,29 +67,38 @@ __device__ __forceinline__ uint32_t kept_bits(int64_t row, int unit, int others,
     return bits << others;                                                                // (the block's words belong to the last columns)
 }
 
-// mean and 1 / deviation of a row, by kind; v becomes (v - mean) / deviation
+// mean and 1 / deviation of a row, by kind; v becomes (v - mean) / deviation.  (Others' columns are set apart by branches that waves without such skip, not by selects for every element.)
 template <int TPR, int NV> __device__ __forceinline__ void normalise(Eight (&v)[NV], const Columns (&c)[NV], int kind, int width, float eps, RowSum<TPR, 1>& sum, float& mean, float& rstd) {
     mean = 0.0f; rstd = 1.0f;
     if (kind == LSP_NORM_NONE) return;
     const float per = 1.0f / (float)width;
+    const auto others_are_zero = [&] {
+#pragma unroll
+        for (int n = 0; n < NV; ++n)
+            if (c[n].others)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[n].x[e] = e >= c[n].others ? v[n].x[e] : 0.0f;
+    };
+    others_are_zero();
     if (kind == LSP_NORM_LAYER) {
         float s[1] = {0.0f};
 #pragma unroll
         for (int n = 0; n < NV; ++n)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[0] += v[n].x[e];                                // (others' columns are zeros)
+            for (int e = 0; e < 8; ++e) s[0] += v[n].x[e];
         sum(s);
         mean = s[0] * per;
+#pragma unroll
+        for (int n = 0; n < NV; ++n)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[n].x[e] -= mean;
+        others_are_zero();
     }
     float s[1] = {0.0f};
 #pragma unroll
     for (int n = 0; n < NV; ++n)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float t = e >= c[n].others ? v[n].x[e] - mean : 0.0f;
-            s[0] = fmaf(t, t, s[0]);
-            v[n].x[e] = t;
-        }
+        for (int e = 0; e < 8; ++e) s[0] = fmaf(v[n].x[e], v[n].x[e], s[0]);
     sum(s);
     rstd = 1.0f / sqrtf(s[0] * per + eps);
 #pragma unroll
@@ -97,13 +107,19 @@ template <int TPR, int NV> __device__ __forceinline__ void normalise(Eight (&v)[
         for (int e = 0; e < 8; ++e) v[n].x[e] *= rstd;
 }
 
-// A weight's or bias' columns, or `otherwise` where it has none
-template <typename D> __device__ __forceinline__ Packed<D> vector_packed(const void* p, const Columns& c, bool whole, float otherwise) {
-    if (p) return load_ending<D>(static_cast<const typename D::elem*>(p) + c.col, c.others, whole);
-    Eight r;
+// v := v w + b, with ones and zeros where these are not there
+template <typename D> __device__ __forceinline__ void weigh(Eight& v, const Packed<D>& w, const Packed<D>& b, bool weight, bool bias) {
+    if (weight)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r.x[e] = otherwise;
-    return narrow_eight<D>(r);
+        for (int e = 0; e < 8; ++e) v.x[e] *= element<D>(w, e);
+    if (bias)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v.x[e] += element<D>(b, e);
+}
+
+// A weight's or bias' columns, if it has some
+template <typename D> __device__ __forceinline__ void ask_for(Packed<D>& v, const void* p, const Columns& c, bool whole) {
+    if (p) v = load_ending<D>(static_cast<const typename D::elem*>(p) + c.col, c.others, whole);
 }
 
 template <typename D, int TPR, int NV, int GROUPS, bool DROP>
@@ -126,44 +142,39 @@ __global__ __launch_bounds__(TPR * GROUPS) void k_residual_norm(const ResidualNo
         c[n] = columns_of(t + n * TPR, width);
         xv[n] = widen_eight<D>(load_ending<D>(x + c[n].col, c[n].others, x_whole));
         fv[n] = widen_eight<D>(load_ending<D>(f + c[n].col, c[n].others, whole));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) fv[n].x[e] = e >= c[n].others ? fv[n].x[e] : 0.0f;
     }
     // What the row is multiplied with is asked for before the sums that come first (4096 x 4096, layer norms with biases and dropout, fp16: 31 to 26 us).
+    const bool post = a.post != LSP_NORM_NONE, pre = a.pre != LSP_NORM_NONE;
+    const void *post_w = post ? a.post_w : nullptr, *post_b = post ? a.post_b : nullptr, *pre_w = pre ? a.pre_w : nullptr, *pre_b = pre ? a.pre_b : nullptr;
     Packed<D> w[NV], b[NV], g[NV];
 #pragma unroll
-    for (int n = 0; n < NV; ++n) {
-        w[n] = vector_packed<D>(a.post != LSP_NORM_NONE ? a.post_w : nullptr, c[n], whole, 1.0f);
-        b[n] = vector_packed<D>(a.post != LSP_NORM_NONE ? a.post_b : nullptr, c[n], whole, 0.0f);
-        g[n] = vector_packed<D>(a.gate, c[n], whole, 1.0f);
-    }
+    for (int n = 0; n < NV; ++n) { ask_for<D>(w[n], post_w, c[n], whole); ask_for<D>(b[n], post_b, c[n], whole); ask_for<D>(g[n], a.gate, c[n], whole); }
     float mean_f, rstd_f, mean_y, rstd_y;
     normalise<TPR, NV>(fv, c, a.post, width, a.eps, sum, mean_f, rstd_f);
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
-        if (a.post != LSP_NORM_NONE) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) fv[n].x[e] = fmaf(fv[n].x[e], element<D>(w[n], e), element<D>(b[n], e));
-        }
+        weigh<D>(fv[n], w[n], b[n], post_w, post_b);
+        float scale = a.branch_scale;
         if constexpr (DROP) {
             const uint32_t kept = kept_bits(row, t + n * TPR, c[n].others, width, a.drop);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) fv[n].x[e] = kept >> e & 1u ? fv[n].x[e] * a.drop.scale : 0.0f;
+            for (int e = 0; e < 8; ++e) fv[n].x[e] = kept >> e & 1u ? fv[n].x[e] : 0.0f;
+            scale *= a.drop.scale;
         }
+        if (a.gate)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) xv[n].x[e] = e >= c[n].others ? fmaf(a.branch_scale * element<D>(g[n], e), fv[n].x[e], a.residual_scale * xv[n].x[e]) : 0.0f;
+            for (int e = 0; e < 8; ++e) fv[n].x[e] *= element<D>(g[n], e);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) xv[n].x[e] = fmaf(scale, fv[n].x[e], a.residual_scale * xv[n].x[e]);
         if (mine) store_ending<D>(static_cast<elem*>(a.y) + row * a.y_stride + c[n].col, xv[n], c[n].others);
-        w[n] = vector_packed<D>(a.pre != LSP_NORM_NONE ? a.pre_w : nullptr, c[n], whole, 1.0f);
-        b[n] = vector_packed<D>(a.pre != LSP_NORM_NONE ? a.pre_b : nullptr, c[n], whole, 0.0f);
+        ask_for<D>(w[n], pre_w, c[n], whole);
+        ask_for<D>(b[n], pre_b, c[n], whole);
     }
     normalise<TPR, NV>(xv, c, a.pre, width, a.eps, sum, mean_y, rstd_y);
     if (mine && a.h) {
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
-            if (a.pre != LSP_NORM_NONE) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) xv[n].x[e] = fmaf(xv[n].x[e], element<D>(w[n], e), element<D>(b[n], e));
-            }
+            weigh<D>(xv[n], w[n], b[n], pre_w, pre_b);
             store_ending<D>(static_cast<elem*>(a.h) + row * a.h_stride + c[n].col, xv[n], c[n].others);
         }
     }
@@ -442,8 +453,9 @@ template <typename D, int TPR, int NV, int GROUPS> static hipError_t run_backwar
     return hipGetLastError();
 }
 
-// Forward: a row has as few idle threads as the variants allow (2999 columns in 128 threads of 24 columns 21.3 us, in 256 threads of 16 columns 22.8: 3001 rows, fp16,
-// dropout); beyond 4096 columns two units a thread in 512 threads (16384 rows of 8192, bf16, 1074 MB: 188 us, 5.7 TB/s; one unit in 1024 threads 307, four in 256 threads 189).
+// Forward: a row has as few idle threads as the variants allow (3001 rows of 2999, fp16, dropout, 72 MB: 20.6 us, 3.5 TB/s; when this took 21.3, 256 threads of 16 columns in place of
+// 128 of 24 took 22.8); beyond 4096 columns two units a thread in 512 threads (16384 rows of 8192, bf16, 1074 MB: 184 us, 5.8 TB/s; when this took 188, one unit in 1024 threads took
+// 307, four in 256 threads 189).  Beside memory the vector units count: 45 instructions an element were all of their time, some 30 are left.
 template <typename D> static hipError_t forward_of(const ResidualNormArgs& a, hipStream_t st) {
     if (a.width <= 64 * 8) return run_forward<D, 64, 1, 4>(a, st);
     if (a.width <= 64 * 16) return run_forward<D, 64, 2, 4>(a, st);
