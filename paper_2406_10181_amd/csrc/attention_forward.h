@@ -75,8 +75,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, D
     }
     const int last_row = min(row_tile * kRows + kRows, nq) - 1;
     const int end_all = a.packed || !a.causal ? nk : min(nk, last_row + ahead + 1);
-    const int begin = split * a.split_tiles * BN;
-    const int end = min(end_all, begin + a.split_tiles * BN);
+    const int tiles_k = (max(end_all, 0) + BN - 1) / BN;                                  // of which this part has an equal share
+    const int begin = tiles_k * split / a.splits * BN, end = min(end_all, tiles_k * (split + 1) / a.splits * BN);
     if (!a.packed && row_tile * kRows >= nq) most = 0;
 
     f32x16 o[kCols];
