@@ -31,11 +31,12 @@ static int waves_for(int64_t units, int64_t rows, int64_t keys, int head_dim, ls
 }
 
 // In how many parts the steps of a tile are done, by workgroups of their own: what takes the least time by a rough account.  A step takes a workgroup that has a CU for itself about
-// step_us; a part's sums (`bytes` for all tiles) are written and read again, at 5 TB/s, and are added by a launch of its own, 4 us.  No more parts than give each CU two workgroups.
+// step_us; a part's sums (`bytes` for all tiles) are written and read again, at 5 TB/s, and are added by a launch of its own, 4 us.  No more parts than run at once: two
+// workgroups a CU, in the backward pass of fp32 beyond heads of 32 one (4 texts of 512, 8 heads of 64: 129 us, with parts for two 143; 2 of 1024, 16 heads of 128: 441 and 461).
 // Against parts of four steps or more, as many as give each CU two workgroups, forward and backward kernels: fp32, one text of 469, 2 heads of 128, 97 us, so 62; bf16, three texts of
 // 407, 1 head of 128, 41 and 35; fp16, two texts of 1000, 8 heads of 64, 64 and 57; one text of 1464, 8 heads of 128, 104 and 102; but bf16, one text of 4691, 2 heads, 130 and 133.
-static int parts_for(int64_t tiles, int64_t steps, double step_us, int64_t bytes) {
-    const int64_t most = std::min<int64_t>({512 / std::max<int64_t>(tiles, 1), steps, 16});
+static int parts_for(int64_t tiles, int64_t steps, double step_us, int64_t bytes, int at_once = 512) {
+    const int64_t most = std::min<int64_t>({at_once / std::max<int64_t>(tiles, 1), steps, 16});
     int best = 1;
     double least = (double)steps * step_us;
     for (int p = 2; p <= most; ++p) {
@@ -73,8 +74,9 @@ void plan_attention_backward(AttentionArgs& a, lsp_dtype dtype) {
     const int64_t key_tiles = (int64_t)a.batch * a.kv_heads * ((a.k_len + kBackwardRows - 1) / kBackwardRows);
     const int64_t query_tiles = (int64_t)a.batch * a.heads * ((a.q_len + kBackwardRows - 1) / kBackwardRows);
     const int64_t q_steps = (a.q_len + tile_rows_of(dtype) - 1) / tile_rows_of(dtype), k_steps = (a.k_len + tile_rows_of(dtype) - 1) / tile_rows_of(dtype);
-    a.key_parts = parts_for(key_tiles, a.group * q_steps, step_us(a, dtype, 4), (int64_t)8 * a.batch * a.kv_heads * a.k_len * a.head_dim);
-    a.query_parts = parts_for(query_tiles, k_steps, step_us(a, dtype, 3), (int64_t)4 * a.batch * a.heads * a.q_len * a.head_dim);
+    const int at_once = dtype == LSP_F32 && a.head_dim > 32 ? 256 : 512;
+    a.key_parts = parts_for(key_tiles, a.group * q_steps, step_us(a, dtype, 4), (int64_t)8 * a.batch * a.kv_heads * a.k_len * a.head_dim, at_once);
+    a.query_parts = parts_for(query_tiles, k_steps, step_us(a, dtype, 3), (int64_t)4 * a.batch * a.heads * a.q_len * a.head_dim, at_once);
 }
 size_t attention_backward_partial_bytes(const AttentionArgs& a) {
     const size_t keys = a.key_parts > 1 ? (size_t)2 * a.key_parts * a.batch * a.kv_heads * a.k_len : 0;
