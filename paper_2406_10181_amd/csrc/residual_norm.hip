@@ -20,6 +20,7 @@
 namespace lsp {
 
 constexpr int kGrads = 5;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // Sums of N values over the TPR threads of a row, in all of them.  `scratch`: this row group's, two sets that take turns.
 template <int TPR, int N> struct RowSum {
@@ -251,6 +252,17 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
         for (int k = 0; k < kGrads; ++k)
 #pragma unroll
             for (int e = 0; e < 8; ++e) acc[n][k][e] = 0.0f;
+    // The biases' sums of wide rows in 16 bits are in LDS too, where each thread adds to its own.
+    constexpr bool SUMS_IN_LDS = BIAS && !HELD && D::size == 2;
+    __shared__ f32x4 bias_sums[SUMS_IN_LDS ? 2 * NV * 2 * TPR : 1];
+    const auto bias_sum = [&](int which, int n, int half) -> f32x4& { return bias_sums[((which * NV + n) * 2 + half) * TPR + t]; };
+    if constexpr (SUMS_IN_LDS)
+#pragma unroll
+        for (int k = 0; k < 4 * NV; ++k) bias_sums[k * TPR + t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const auto add_to_bias = [&](int which, int n, const float (&v)[8]) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) bias_sum(which, n, half) += f32x4{v[4 * half], v[4 * half + 1], v[4 * half + 2], v[4 * half + 3]};
+    };
     // What belongs to a row is asked for AHEAD rows before.
     struct Row { Packed<D> x[NV], f[NV], dy[NV], dh[NV]; float stats[4]; };
     Row rows_[AHEAD];
@@ -290,6 +302,7 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
             if constexpr (DROP) kept[n] = kept_bits(row, t + n * TPR, c[n].others, width, a.drop);
             Weights w;
             weights_of(w, n, true);
+            float to_bias[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);                        // (four at a time: eight would take registers for speed that nothing waits for)
@@ -299,11 +312,13 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
                 yhat[n][e] = fmaf(scale_u * gate, u, fmaf(a.residual_scale, element<D>(r.x[n], e), -mean_y)) * rstd_y;
                 const float d = element<D>(r.dh[n], e);
                 acc[n][0][e] = fmaf(d, yhat[n][e], acc[n][0][e]);
-                if constexpr (BIAS) acc[n][1][e] += d;
+                if constexpr (SUMS_IN_LDS) to_bias[e] = d;
+                else if constexpr (BIAS) acc[n][1][e] += d;
                 de[n][e] = d * wy;
                 s[0] = fmaf(de[n][e], yhat[n][e], s[0]);
                 s[1] += de[n][e];
             }
+            if constexpr (SUMS_IN_LDS) add_to_bias(0, n, to_bias);
         }
         load_first(r, next);                                                              // (where what they held is used up)
         if (pre) sum(s);
@@ -314,6 +329,7 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
             Eight out;
             Weights w;
             weights_of(w, n, false);
+            float to_bias[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
@@ -324,11 +340,13 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
                 const float du = branch * (scale_u * gate);
                 acc[n][2][e] = fmaf(branch, u, acc[n][2][e]);
                 acc[n][3][e] = fmaf(du, fhat[n][e], acc[n][3][e]);
-                if constexpr (BIAS) acc[n][4][e] += du;
+                if constexpr (SUMS_IN_LDS) to_bias[e] = du;
+                else if constexpr (BIAS) acc[n][4][e] += du;
                 de[n][e] = du * wf;
                 s[0] = fmaf(de[n][e], fhat[n][e], s[0]);
                 s[1] += de[n][e];
             }
+            if constexpr (SUMS_IN_LDS) add_to_bias(1, n, to_bias);
             if (mine) store_ending<D>(static_cast<elem*>(a.dx) + row * a.dx_stride + c[n].col, out, c[n].others);
         }
         load_dy(r, next);
@@ -358,7 +376,7 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
         for (int n = 0; n < NV; ++n) {
             Eight v;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v.x[e] = acc[n][k][e] * (k == 2 ? scale_u : 1.0f);
+            for (int e = 0; e < 8; ++e) v.x[e] = (SUMS_IN_LDS && (k == 1 || k == 4) ? bias_sum(k == 4, n, e >> 2)[e & 3] : acc[n][k][e]) * (k == 2 ? scale_u : 1.0f);
             if (GROUPS > 1 && !a.many) {                                                  // (few rows: every group's part by itself, the adding is short)
                 store_ending<F32>(a.partial + (((int64_t)slot * gridDim.x + blockIdx.x) * GROUPS + group) * width + c[n].col, v, c[n].others);
                 continue;
