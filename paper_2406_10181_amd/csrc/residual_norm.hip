@@ -204,38 +204,45 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
     RowSum<TPR, 2> sum{scratch + group * 4 * (TPR / 64)};
     const bool post = a.post != LSP_NORM_NONE, pre = a.pre != LSP_NORM_NONE;
     // Weights stay in registers, in fp32, while these have room (NV = 1), else in LDS as they came, where each thread reads what it wrote, a unit at a time; as packed registers
-    // they made others spill (4096 x 8192, fp32: 253 us, so 165; with layer norms, biases and dropout 669, so 509; the same in fp16 244, so 197).
+    // they made others spill (4096 x 8192, fp32: 253 us, so 165).
     constexpr bool HELD = NV == 1;
     constexpr int kPieces = D::size / 2;                                                  // of 16 bytes, of eight elements
-    __shared__ u32x4 kept_weights[HELD ? 1 : 4 * NV * kPieces * TPR];
+    enum { WF, G, BF, WY };
+    constexpr int kInLds = BIAS && D::size == 4 ? 2 : 4;                                  // (LDS has not room for all; the others are read again, from the caches)
+    __shared__ u32x4 kept_weights[HELD ? 1 : kInLds * NV * kPieces * TPR];
     float held[HELD ? 4 : 1][8];
-    const auto vector = [&](int which, const void* p, float otherwise, bool zeros, int n) {
-        const int first = zeros ? c[n].others : 0;                                        // (zeros for others' columns: they add nothing to any sum)
+    const auto vector = [&](int which, int n) {
+        const void* p = which == WF ? (post ? a.post_w : nullptr) : which == BF ? (post ? a.post_b : nullptr) : which == G ? a.gate : pre ? a.pre_w : nullptr;
+        const float otherwise = which == BF ? 0.0f : 1.0f;
+        const int first = which == G || which == WY ? c[n].others : 0;                    // (zeros for others' columns: they add nothing to any sum)
         Eight r;
         if (p) r = widen_eight<D>(load_ending<D>(static_cast<const elem*>(p) + c[n].col, c[n].others, whole));
 #pragma unroll
         for (int e = 0; e < 8; ++e) r.x[e] = e < first ? 0.0f : p ? r.x[e] : otherwise;
-        if constexpr (HELD) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) held[which][e] = r.x[e];
-        } else {
-            const Packed<D> v = narrow_eight<D>(r);
-#pragma unroll
-            for (int k = 0; k < kPieces; ++k) kept_weights[((which * NV + n) * kPieces + k) * TPR + t] = u32x4{v.w[4 * k], v.w[4 * k + 1], v.w[4 * k + 2], v.w[4 * k + 3]};
-        }
+        return r;
     };
-    enum { WF, BF, G, WY };
 #pragma unroll
-    for (int n = 0; n < NV; ++n) {
-        vector(WF, post ? a.post_w : nullptr, 1.0f, false, n); if (BIAS) vector(BF, post ? a.post_b : nullptr, 0.0f, false, n);
-        vector(G, a.gate, 1.0f, true, n); vector(WY, pre ? a.pre_w : nullptr, 1.0f, true, n);
-    }
+    for (int n = 0; n < NV; ++n)
+#pragma unroll
+        for (int which = 0; which < (HELD ? 4 : kInLds); ++which) {
+            if (which == BF && !BIAS) continue;
+            const Eight r = vector(which, n);
+            if constexpr (HELD) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) held[which][e] = r.x[e];
+            } else {
+                const Packed<D> v = narrow_eight<D>(r);
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) kept_weights[((which * NV + n) * kPieces + k) * TPR + t] = u32x4{v.w[4 * k], v.w[4 * k + 1], v.w[4 * k + 2], v.w[4 * k + 3]};
+            }
+        }
     struct Weights { Packed<D> v[HELD ? 1 : 4]; };
     const auto weights_of = [&](Weights& w, int n, bool all) {                            // for the next eight columns
         if constexpr (!HELD)
 #pragma unroll
             for (int which = 0; which < 4; ++which) {
                 if ((which == BF && !BIAS) || (which == WY && !all)) continue;
+                if (which >= kInLds) { w.v[which] = narrow_eight<D>(vector(which, n)); continue; }
 #pragma unroll
                 for (int k = 0; k < kPieces; ++k) {
                     const u32x4 v = kept_weights[((which * NV + n) * kPieces + k) * TPR + t];
@@ -252,8 +259,8 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
         for (int k = 0; k < kGrads; ++k)
 #pragma unroll
             for (int e = 0; e < 8; ++e) acc[n][k][e] = 0.0f;
-    // The biases' sums of wide rows in 16 bits are in LDS too, where each thread adds to its own.
-    constexpr bool SUMS_IN_LDS = BIAS && !HELD && D::size == 2;
+    // The biases' sums of wide rows are in LDS too, where each thread adds to its own (4096 x 8192, layer norms with dropout: fp16 98 us, in registers, which spill, 196; fp32 286 and 509).
+    constexpr bool SUMS_IN_LDS = BIAS && !HELD;
     __shared__ f32x4 bias_sums[SUMS_IN_LDS ? 2 * NV * 2 * TPR : 1];
     const auto bias_sum = [&](int which, int n, int half) -> f32x4& { return bias_sums[((which * NV + n) * 2 + half) * TPR + t]; };
     if constexpr (SUMS_IN_LDS)
@@ -433,7 +440,7 @@ __global__ __launch_bounds__(1024) void k_residual_norm_sums(const ResidualNormA
 // Backward: threads of a row, and rows that a workgroup has at a time, by their width.  One workgroup a CU: its registers hold no second one of 512 threads, and fewer
 // workgroups leave fewer parts to add (4096 x 4096, bf16, 201 MB: 39 us, 5.1 TB/s, and 5 to add the parts; in a form that took 48 + 5, twice as many workgroups took 53 + 7
 // and two a CU at 128 registers, with spills, 91).  Beyond 4096 columns two units a thread: 4096 x 8192, fp16
-// 83 us (403 MB, 4.9 TB/s), fp32 165; with biases, whose sums spill, 197 and 509.  (One unit in 1024 threads has half the registers a thread: 252 in fp16 without biases.)
+// 83 us (403 MB, 4.9 TB/s), with biases 98; fp32 165 and, with some spills, 286.  (One unit in 1024 threads has half the registers a thread: 252 in fp16 without biases.)
 static int row_threads(int width) { return width <= 512 ? 64 : width <= 1024 ? 128 : width <= 2048 ? 256 : 512; }
 static int row_groups(int width) { return width <= 512 ? 8 : width <= 1024 ? 4 : width <= 2048 ? 2 : 1; }
 static int64_t workgroups_of(int64_t rows, int32_t width) {
