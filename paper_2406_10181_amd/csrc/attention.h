@@ -64,6 +64,14 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 #define LSP_SHARED_AS __attribute__((address_space(3)))
 
+// Forward: the running maximum stays until a new one is larger by more than 2^kLagLog2, and its own probability counts as 2^kTopLog2, in the operands as in their sums, so that
+// the factor leaves with the division and only L has to take it back.  fp16 has normal numbers down to 2^-14 only: with 2^11 at the top probabilities keep all their digits down to
+// 2^-25 of the largest and some down to 2^-35, and with a lag of 2^4 none is above 2^15.  (With 1 at the top one of 2^-23 was up to a quarter off, and where one key has nearly all the
+// weight and no value the others' are all there is.)  bf16 and fp32 have the range.
+template <typename D> constexpr float kTopLog2 = std::is_same<D, F16>::value ? 11.0f : 0.0f;
+template <typename D> constexpr float kTop = std::is_same<D, F16>::value ? 2048.0f : 1.0f;
+template <typename D> constexpr float kLagLog2 = std::is_same<D, F16>::value ? 4.0f : 8.0f;
+
 // Eight values of k of one lane
 template <typename D> struct Frag { u32x4 w; };
 template <> struct Frag<F32> { f32x8 w; };

@@ -47,7 +47,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
     for (int c = 0; c < kCols; ++c) o[c] = zeros16();
     float m = -INFINITY, l = 0.0f;
-    const float c2 = a.scale_log2, slack = 8.0f / c2;
+    const float c2 = a.scale_log2, slack = kLagLog2<D> / c2;
     const Reader<D, DP> read(lane);
     const uint8_t* kp = at<D>(a.k, b, 0, kv_head);
     const uint8_t* vp = at<D>(a.v, b, 0, kv_head);
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[c][i] *= keep;
             }
-            const float shift = m == -INFINITY ? 0.0f : -m * c2;
+            const float shift = m == -INFINITY ? 0.0f : fmaf(-m, c2, kTopLog2<D>);
 #pragma unroll
             for (int i = 0; i < 16; ++i) { s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, shift)); l += s[i]; }
             // the values of this step have arrived when no more is on the way than the next one's keys and values
@@ -143,7 +143,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         } else {
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
             store_four<D>(const_cast<uint8_t*>(at<D>(a.o, b, ri, rq_head)) + col * D::size, v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-            if (col == 0) a.L[line] = sum == 0.0f ? -INFINITY : top * a.scale + __logf(sum);
+            if (col == 0) a.L[line] = sum == 0.0f ? -INFINITY : top * a.scale + __logf(sum * (1.0f / kTop<D>));
         }
     }
 }

@@ -5,9 +5,10 @@
 // keys; lane l ^ 32 has the others) of ONE query, so maxima and sums stay in the lane, and the accumulators are the operand of
 // O^T += V^T P^T as they are.
 //
-// The running maximum is moved only when a new one is larger by more than 8 in powers of two; until then probabilities are at most 2^8, and
+// The running maximum is moved only when a new one is larger by more than 2^8 (fp16: 2^4); until then probabilities are at most that much above its own, which
 // neither their sum in fp32 nor their rounding minds, and the accumulators are left alone.  Probabilities are rounded to the storage type as operands of
-// the second product, half a unit in the last place of each beside the result's own rounding; their sums, and L, are made before that.
+// the second product, half a unit in the last place of each beside the result's own rounding (fp16: of those down to 2^-25 of the largest, see kTopLog2); their
+// sums, and L, are made before that.
 //
 // Heads of 128: bound by the matrix cores (one text of 8192, 16 heads, causal, bf16: 270 to 300 us, 275 GFLOP, 0.9 to 1.0 PFLOP/s; four of 1024, 32 heads: 52 us, 34 GFLOP).
 // Heads of 64: by exponentials and what else a score takes outside the matrix cores, a quarter-rate instruction and four others for 256 operations of theirs (16 heads, eight texts
@@ -88,7 +89,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, D
 #pragma unroll
     for (int c = 0; c < kCols; ++c) o[c] = zeros16();
     float m = -INFINITY, l = 0.0f;                                                        // m: in the units of the scores; l: this lane's part
-    const float c2 = a.scale_log2, slack = 8.0f / c2;
+    const float c2 = a.scale_log2, slack = kLagLog2<D> / c2;
 
     const uint8_t* kp = at<D>(a.k, b, 0, kv_head);
     const uint8_t* vp = at<D>(a.v, b, 0, kv_head);
@@ -169,7 +170,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, D
 #pragma unroll
                         for (int i = 0; i < 16; ++i) o[c][i] *= keep;
                 }
-                const float shift = m == -INFINITY ? 0.0f : -m * c2;
+                const float shift = m == -INFINITY ? 0.0f : fmaf(-m, c2, kTopLog2<D>);
                 const auto probabilities = [&](int x) {                                   // of keys 16 x .. 16 x + 15
                     f32x16& w = s[x >> 1];
                     float sum = 0.0f;
@@ -238,7 +239,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, D
         if (n >= a.rows) return nullptr;
         return const_cast<uint8_t*>(a.packed ? at<D>(a.o, b, n % a.q_len, kv_head * a.group + n / a.q_len) : at<D>(a.o, b, n, head));
     });
-    if (h == 0 && row < a.rows) a.L[((int64_t)b * a.heads + q_head) * a.q_len + qi] = l == 0.0f ? -INFINITY : m * a.scale + __logf(l);
+    if (h == 0 && row < a.rows) a.L[((int64_t)b * a.heads + q_head) * a.q_len + qi] = l == 0.0f ? -INFINITY : m * a.scale + __logf(l * (1.0f / kTop<D>));
 }
 
 // Joins the parts of a row: O = sum_s w_s O_s / sum_s w_s l_s with w_s = 2^(m_s - m).  Bound by memory, and where parts are few by its launch (4 us).  A wave has a row: its lanes have a part's (m, l) each, and then two columns.
@@ -275,7 +276,7 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttentionArgs a) {
         typename D::elem* out = reinterpret_cast<typename D::elem*>(const_cast<uint8_t*>(at<D>(a.o, b, qi, head))) + col;
         out[0] = narrow<D>(x * inv); out[1] = narrow<D>(y * inv);
     }
-    if (lane == 0) a.L[line] = l == 0.0f ? -INFINITY : m * a.scale + __logf(l);
+    if (lane == 0) a.L[line] = l == 0.0f ? -INFINITY : m * a.scale + __logf(l * (1.0f / kTop<D>));
 }
 
 template <typename D> static hipError_t run_attention_join(const AttentionArgs& a, hipStream_t st) {
