@@ -30,6 +30,7 @@ decltype(&lsp_residual_norm_backward) g_norm_backward;
 PyObject* g_shape;
 PyObject* g_stride;
 PyObject* g_dtype;
+PyObject* g_types[3];         // torch's types, in the order of lsp_dtype; from the first descriptor on
 
 // Converts one argument after another, to what ctypes makes of it; the first failure leaves a Python exception and ok = false.
 struct Args {
@@ -199,6 +200,21 @@ PyObject* refuse(const char* text) {
     return nullptr;
 }
 
+bool know_types() {
+    if (g_types[0]) return true;
+    PyObject* torch = PyImport_ImportModule("torch");
+    if (!torch) return false;
+    const char* names[3] = {"float32", "float16", "bfloat16"};
+    for (int i = 2; i >= 0; --i) if (!(g_types[i] = PyObject_GetAttrString(torch, names[i]))) break;
+    Py_DECREF(torch);
+    return g_types[0] != nullptr;
+}
+// An lsp_dtype, or -1
+int type_code(const PyObject* dtype) {
+    for (int i = 0; i < 3; ++i) if (dtype == g_types[i]) return i;
+    return -1;
+}
+
 float number(PyObject* x, bool& ok) {
     const double v = PyFloat_AsDouble(x);
     if (v == -1.0 && PyErr_Occurred()) ok = false;
@@ -211,13 +227,14 @@ PyObject* attention_problem(PyObject*, PyObject* const* args, Py_ssize_t nargs) 
     const char* what = "attention_problem";
     Args head(args);
     auto* p = static_cast<lsp_attention_problem*>(head.pointer());
-    if (!head.ok) return nullptr;
+    if (!head.ok || !know_types()) return nullptr;
     Tensor q, k, v, o, l;
     if (!q.read(args[1], 4, what) || !k.read(args[2], 4, what) || !v.read(args[3], 4, what) || !o.read(args[4], 4, what) || !l.read(args[5], 3, what)) return nullptr;
     if (!k.same_shape(v) || !q.same_shape(o) || k.shape[0] != q.shape[0] || k.shape[3] != q.shape[3] || l.shape[0] != q.shape[0] || l.shape[1] != q.shape[2] ||
         l.shape[2] != q.shape[1] || (l.shape[1] != 1 && l.stride[1] != l.shape[2]) || (l.shape[0] != 1 && l.stride[0] != l.shape[1] * l.shape[2]))
         return refuse("attention_problem: Q, O [batch][q_len][heads][head_dim], K, V [batch][k_len][kv_heads][head_dim] and a contiguous L [batch][heads][q_len] are wanted");
-    if (k.dtype != q.dtype || v.dtype != q.dtype || o.dtype != q.dtype) return refuse("attention_problem: Q, K, V and O are of one type");
+    if (type_code(q.dtype) < 0 || k.dtype != q.dtype || v.dtype != q.dtype || o.dtype != q.dtype) return refuse("attention_problem: Q, K, V and O are of one type, float32, float16 or bfloat16");
+    if (type_code(l.dtype) != LSP_F32) return refuse("attention_problem: L is float32");
     void* lens[2] = {nullptr, nullptr};
     for (int i = 0; i < 2; ++i) {
         if (args[6 + i] == Py_None) continue;
@@ -246,22 +263,23 @@ PyObject* attention_gradients(PyObject*, PyObject* const* args, Py_ssize_t nargs
     if (!count_is(nargs, 5)) return nullptr;
     Args head(args);
     auto* p = static_cast<lsp_attention_gradients*>(head.pointer());
-    if (!head.ok) return nullptr;
+    if (!head.ok || !know_types()) return nullptr;
     Tensor t[4];
     for (int i = 0; i < 4; ++i) if (!t[i].read(args[1 + i], 4, "attention_gradients")) return nullptr;
     if (!t[0].same_shape(t[1]) || !t[2].same_shape(t[3])) return refuse("attention_gradients: dO and dQ, and dK and dV, are of one shape");
+    for (const Tensor& x : t) if (type_code(x.dtype) < 0 || x.dtype != t[0].dtype) return refuse("attention_gradients: dO, dQ, dK and dV are of one type, float32, float16 or bfloat16");
     *p = lsp_attention_gradients{t[0].data, t[1].data, t[2].data, t[3].data, {t[0].stride[0], t[0].stride[1], t[0].stride[2]}, {t[1].stride[0], t[1].stride[1], t[1].stride[2]},
                                  {t[2].stride[0], t[2].stride[1], t[2].stride[2]}, {t[3].stride[0], t[3].stride[1], t[3].stride[2]}};
     Py_RETURN_NONE;
 }
 
-// A [width] vector of type `dtype` (NULL: any), or None
-bool vector(PyObject* t, int64_t width, PyObject* dtype, void*& to, const char* what) {
+// A [width] vector of type `dtype`, or None
+bool vector(PyObject* t, int64_t width, const PyObject* dtype, void*& to, const char* what) {
     to = nullptr;
     if (t == Py_None) return true;
     Tensor v;
     if (!v.read(t, 1, what)) return false;
-    if (v.shape[0] != width || (dtype && v.dtype != dtype)) { PyErr_Format(PyExc_ValueError, "%s: weights, biases and gate are [width], of the type of x", what); return false; }
+    if (v.shape[0] != width || v.dtype != dtype) { PyErr_Format(PyExc_ValueError, "%s: weights, biases and gate are [width], of the type of x, and their gradients float32", what); return false; }
     to = v.data;
     return true;
 }
@@ -272,12 +290,13 @@ PyObject* residual_norm_problem(PyObject*, PyObject* const* args, Py_ssize_t nar
     const char* what = "residual_norm_problem";
     Args head(args);
     auto* p = static_cast<lsp_residual_norm_problem*>(head.pointer());
-    if (!head.ok) return nullptr;
+    if (!head.ok || !know_types()) return nullptr;
     Tensor x, f, y, h, stats;
     if (!x.read(args[1], 2, what) || !f.read(args[2], 2, what) || !y.read(args[3], 2, what) || (args[4] != Py_None && !h.read(args[4], 2, what)) || !stats.read(args[5], 2, what)) return nullptr;
-    if (!f.same_shape(x) || !y.same_shape(x) || f.dtype != x.dtype || y.dtype != x.dtype || (h.data && (!h.same_shape(x) || h.dtype != x.dtype)))
-        return refuse("residual_norm_problem: x, f, y and h are of one shape and type");
-    if (stats.shape[0] != 4 || stats.shape[1] != x.shape[0] || stats.stride[0] != stats.shape[1]) return refuse("residual_norm_problem: stats are [4][rows]");
+    if (type_code(x.dtype) < 0 || !f.same_shape(x) || !y.same_shape(x) || f.dtype != x.dtype || y.dtype != x.dtype || (h.dtype && (!h.same_shape(x) || h.dtype != x.dtype)))
+        return refuse("residual_norm_problem: x, f, y and h are of one shape and type, float32, float16 or bfloat16");
+    if (type_code(stats.dtype) != LSP_F32 || stats.shape[0] != 4 || stats.shape[1] != x.shape[0] || stats.stride[0] != stats.shape[1])
+        return refuse("residual_norm_problem: stats are [4][rows], float32");
     void* v[5];
     for (int i = 0; i < 5; ++i) if (!vector(args[6 + i], x.shape[1], x.dtype, v[i], what)) return nullptr;
     Args kinds(args + 11), tail(args + 17);
@@ -299,12 +318,14 @@ PyObject* residual_norm_gradients(PyObject*, PyObject* const* args, Py_ssize_t n
     const char* what = "residual_norm_gradients";
     Args head(args);
     auto* p = static_cast<lsp_residual_norm_gradients*>(head.pointer());
-    if (!head.ok) return nullptr;
+    if (!head.ok || !know_types()) return nullptr;
     Tensor t[4];
     for (int i = 0; i < 4; ++i) if ((i != 1 || args[2] != Py_None) && !t[i].read(args[1 + i], 2, what)) return nullptr;
-    for (int i = 1; i < 4; ++i) if (t[i].data && !t[i].same_shape(t[0])) return refuse("residual_norm_gradients: dy, dh, dx and df are of one shape");
+    for (int i = 0; i < 4; ++i)
+        if (t[i].dtype && (!t[i].same_shape(t[0]) || t[i].dtype != t[0].dtype || type_code(t[i].dtype) < 0))
+            return refuse("residual_norm_gradients: dy, dh, dx and df are of one shape and type, float32, float16 or bfloat16");
     void* v[5];
-    for (int i = 0; i < 5; ++i) if (!vector(args[5 + i], t[0].shape[1], nullptr, v[i], what)) return nullptr;
+    for (int i = 0; i < 5; ++i) if (!vector(args[5 + i], t[0].shape[1], g_types[LSP_F32], v[i], what)) return nullptr;
     *p = lsp_residual_norm_gradients{t[0].data, t[1].data, t[2].data, t[3].data, static_cast<float*>(v[0]), static_cast<float*>(v[1]), static_cast<float*>(v[2]), static_cast<float*>(v[3]),
                                      static_cast<float*>(v[4]), t[0].stride[0], t[1].stride[0], t[2].stride[0], t[3].stride[0]};
     Py_RETURN_NONE;
