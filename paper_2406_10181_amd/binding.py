@@ -62,6 +62,26 @@ class lsp_residual_norm_gradients(ctypes.Structure):
                 ("dy_stride", ctypes.c_int64), ("dh_stride", ctypes.c_int64), ("dx_stride", ctypes.c_int64), ("df_stride", ctypes.c_int64)]
 
 
+# What attention_problem() and its like return: behind the C struct's fields what the call compares with its other arguments (field for field what the call module fills).
+_four = ctypes.c_int64 * 4
+
+
+class _AttentionOfTensors(lsp_attention_problem):
+    _fields_ = [("dtype", ctypes.c_int32)]
+
+
+class _AttentionGradientsOfTensors(lsp_attention_gradients):
+    _fields_ = [("q_shape", _four), ("k_shape", _four), ("dtype", ctypes.c_int32)]
+
+
+class _ResidualNormOfTensors(lsp_residual_norm_problem):
+    _fields_ = [("dtype", ctypes.c_int32)]
+
+
+class _ResidualNormGradientsOfTensors(lsp_residual_norm_gradients):
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
 NORM_KIND = {"none": 0, "rms": 1, "layer": 2}
 
 
@@ -443,13 +463,11 @@ def _operator_calls():
     if _operators is None:
         L, module = lib(), _bound()
         module.bind_operators(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
-            L.lsp_dropout, L.lsp_attention_forward, L.lsp_attention_backward, L.lsp_residual_norm_forward, L.lsp_residual_norm_backward)))
+            L.lsp_dropout, L.lsp_attention_forward, L.lsp_attention_backward, L.lsp_residual_norm_forward, L.lsp_residual_norm_backward)),
+            lsp_attention_problem, lsp_attention_gradients, lsp_residual_norm_problem, lsp_residual_norm_gradients,
+            _AttentionOfTensors, _AttentionGradientsOfTensors, _ResidualNormOfTensors, _ResidualNormGradientsOfTensors)
         _operators = module
     return _operators
-
-
-def _at(descriptor) -> Optional[int]:
-    return None if descriptor is None else ctypes.addressof(descriptor)
 
 
 def lsp_dropout(x, y, rows, width, dropout: float, seed: int, offset: int, dtype: int, stream=None, check: bool = True) -> int:
@@ -471,7 +489,7 @@ def attention_problem(Q, K, V, O, L, *, q_lens=None, k_lens=None, scale: float, 
     """The descriptor of an attention call from torch tensors: Q, O [batch][q_len][heads][head_dim] and K, V [batch][k_len][kv_heads][head_dim]
     with any strides whose last is 1, L [batch][heads][q_len] fp32, q_lens and k_lens [batch] int32 or None.  Tensors that do not belong
     together are a ValueError.  They are kept alive by the caller."""
-    p = lsp_attention_problem()
+    p = _AttentionOfTensors()
     if q_lens is not None or k_lens is not None:
         _int32(q_lens, "attention_problem"), _int32(k_lens, "attention_problem")
     (_operators or _operator_calls()).attention_problem(ctypes.addressof(p), Q, K, V, O, L, q_lens, k_lens, scale, causal, dropout, seed, offset)
@@ -480,7 +498,7 @@ def attention_problem(Q, K, V, O, L, *, q_lens=None, k_lens=None, scale: float, 
 
 def attention_gradients(dO, dQ, dK, dV) -> lsp_attention_gradients:
     """The gradients' descriptor, from tensors shaped as O, Q, K and V."""
-    g = lsp_attention_gradients()
+    g = _AttentionGradientsOfTensors()
     (_operators or _operator_calls()).attention_gradients(ctypes.addressof(g), dO, dQ, dK, dV)
     return g
 
@@ -494,16 +512,16 @@ def lsp_attention_backward_workspace_bytes(problem, dtype: int) -> int:
 
 
 def lsp_attention_forward(problem, dtype: int, workspace=None, workspace_bytes: int = 0, stream=None, check: bool = True) -> int:
-    """problem: from attention_problem()."""
-    rc = (_operators or _operator_calls()).attention_forward(_at(problem), dtype, workspace, workspace_bytes, stream)
+    """problem: from attention_problem(), of tensors of `dtype` (else a ValueError)."""
+    rc = (_operators or _operator_calls()).attention_forward(problem, dtype, workspace, workspace_bytes, stream)
     if check and rc:
         _check(rc, "lsp_attention_forward")
     return rc
 
 
 def lsp_attention_backward(problem, gradients, dtype: int, workspace, workspace_bytes: int, stream=None, check: bool = True) -> int:
-    """gradients: from attention_gradients()."""
-    rc = (_operators or _operator_calls()).attention_backward(_at(problem), _at(gradients), dtype, workspace, workspace_bytes, stream)
+    """gradients: from attention_gradients(), shaped as the problem's tensors and of `dtype`, as these (else a ValueError)."""
+    rc = (_operators or _operator_calls()).attention_backward(problem, gradients, dtype, workspace, workspace_bytes, stream)
     if check and rc:
         _check(rc, "lsp_attention_backward")
     return rc
@@ -515,7 +533,7 @@ def residual_norm_problem(x, f, y, h, stats, *, post: str = "none", post_weight=
     """The descriptor of a residual-norm call from torch tensors: x, f, y, h [rows][width] (h may be None), stats [4][rows] fp32, weights, biases and
     gate [width] (or None); post and pre are "none", "rms" or "layer".  Tensors that do not belong together are a ValueError.  They are kept
     alive by the caller."""
-    p = lsp_residual_norm_problem()
+    p = _ResidualNormOfTensors()
     (_operators or _operator_calls()).residual_norm_problem(ctypes.addressof(p), x, f, y, h, stats, post_weight, post_bias, gate, pre_weight, pre_bias, NORM_KIND[post],
                                                             NORM_KIND[pre], eps, residual_scale, branch_scale, dropout, seed, offset)
     return p
@@ -523,14 +541,14 @@ def residual_norm_problem(x, f, y, h, stats, *, post: str = "none", post_weight=
 
 def residual_norm_gradients(dy, dh, dx, df, *, post_weight=None, post_bias=None, gate=None, pre_weight=None, pre_bias=None) -> lsp_residual_norm_gradients:
     """The gradients' descriptor: dy, dh (or None) arrive, dx and df are made, and the fp32 [width] gradients that are asked for."""
-    g = lsp_residual_norm_gradients()
+    g = _ResidualNormGradientsOfTensors()
     (_operators or _operator_calls()).residual_norm_gradients(ctypes.addressof(g), dy, dh, dx, df, post_weight, post_bias, gate, pre_weight, pre_bias)
     return g
 
 
 def lsp_residual_norm_forward(problem, dtype: int, stream=None, check: bool = True) -> int:
-    """problem: from residual_norm_problem()."""
-    rc = (_operators or _operator_calls()).residual_norm_forward(_at(problem), dtype, stream)
+    """problem: from residual_norm_problem(), of tensors of `dtype` (else a ValueError)."""
+    rc = (_operators or _operator_calls()).residual_norm_forward(problem, dtype, stream)
     if check and rc:
         _check(rc, "lsp_residual_norm_forward")
     return rc
@@ -541,8 +559,8 @@ def lsp_residual_norm_backward_workspace_bytes(problem, dtype: int) -> int:
 
 
 def lsp_residual_norm_backward(problem, gradients, dtype: int, workspace, workspace_bytes: int, stream=None, check: bool = True) -> int:
-    """gradients: from residual_norm_gradients()."""
-    rc = (_operators or _operator_calls()).residual_norm_backward(_at(problem), _at(gradients), dtype, workspace, workspace_bytes, stream)
+    """gradients: from residual_norm_gradients(), shaped as the problem's tensors and of `dtype`, as these (else a ValueError)."""
+    rc = (_operators or _operator_calls()).residual_norm_backward(problem, gradients, dtype, workspace, workspace_bytes, stream)
     if check and rc:
         _check(rc, "lsp_residual_norm_backward")
     return rc

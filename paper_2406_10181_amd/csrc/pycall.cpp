@@ -221,12 +221,26 @@ float number(PyObject* x, bool& ok) {
     return (float)v;
 }
 
-// (address of the lsp_attention_problem, Q, K, V, O, L, q_lens, k_lens, scale, causal, dropout, seed, offset)
+// What a descriptor made here remembers beside the C structure, so that the call can compare it with its other arguments: the binding's objects have these
+// fields behind the structure's own.
+struct AttentionOfTensors { lsp_attention_problem p; int32_t dtype; };
+struct AttentionGradientsOfTensors { lsp_attention_gradients g; int64_t q_shape[4], k_shape[4]; int32_t dtype; };
+struct ResidualNormOfTensors { lsp_residual_norm_problem p; int32_t dtype; };
+struct ResidualNormGradientsOfTensors { lsp_residual_norm_gradients g; int64_t rows, width; int32_t dtype; };
+
+bool matches(const AttentionOfTensors& a, const AttentionGradientsOfTensors& b) {
+    const int64_t q[4] = {a.p.batch, a.p.q_len, a.p.heads, a.p.head_dim}, k[4] = {a.p.batch, a.p.k_len, a.p.kv_heads, a.p.head_dim};
+    for (int i = 0; i < 4; ++i) if (q[i] != b.q_shape[i] || k[i] != b.k_shape[i]) return false;
+    return true;
+}
+bool matches(const ResidualNormOfTensors& a, const ResidualNormGradientsOfTensors& b) { return a.p.rows == b.rows && a.p.width == b.width; }
+
+// (address of the binding's attention_problem, Q, K, V, O, L, q_lens, k_lens, scale, causal, dropout, seed, offset)
 PyObject* attention_problem(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!count_is(nargs, 13)) return nullptr;
     const char* what = "attention_problem";
     Args head(args);
-    auto* p = static_cast<lsp_attention_problem*>(head.pointer());
+    auto* d = static_cast<AttentionOfTensors*>(head.pointer());
     if (!head.ok || !know_types()) return nullptr;
     Tensor q, k, v, o, l;
     if (!q.read(args[1], 4, what) || !k.read(args[2], 4, what) || !v.read(args[3], 4, what) || !o.read(args[4], 4, what) || !l.read(args[5], 3, what)) return nullptr;
@@ -252,23 +266,26 @@ PyObject* attention_problem(PyObject*, PyObject* const* args, Py_ssize_t nargs) 
     const uint64_t seed = tail.integer();
     const uint32_t offset = (uint32_t)tail.integer();
     if (!tail.ok || PyErr_Occurred()) return nullptr;
-    *p = lsp_attention_problem{q.data, k.data, v.data, o.data, static_cast<float*>(l.data), static_cast<const int32_t*>(lens[0]), static_cast<const int32_t*>(lens[1]),
+    d->dtype = type_code(q.dtype);
+    d->p = lsp_attention_problem{q.data, k.data, v.data, o.data, static_cast<float*>(l.data), static_cast<const int32_t*>(lens[0]), static_cast<const int32_t*>(lens[1]),
                                {q.stride[0], q.stride[1], q.stride[2]}, {k.stride[0], k.stride[1], k.stride[2]}, {v.stride[0], v.stride[1], v.stride[2]}, {o.stride[0], o.stride[1], o.stride[2]},
                                (int32_t)q.shape[0], (int32_t)q.shape[2], (int32_t)k.shape[2], (int32_t)q.shape[1], (int32_t)k.shape[1], (int32_t)q.shape[3], causal, scale, dropout, offset, seed};
     Py_RETURN_NONE;
 }
 
-// (address of the lsp_attention_gradients, dO, dQ, dK, dV)
+// (address of the binding's attention_gradients, dO, dQ, dK, dV)
 PyObject* attention_gradients(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!count_is(nargs, 5)) return nullptr;
     Args head(args);
-    auto* p = static_cast<lsp_attention_gradients*>(head.pointer());
+    auto* d = static_cast<AttentionGradientsOfTensors*>(head.pointer());
     if (!head.ok || !know_types()) return nullptr;
     Tensor t[4];
     for (int i = 0; i < 4; ++i) if (!t[i].read(args[1 + i], 4, "attention_gradients")) return nullptr;
     if (!t[0].same_shape(t[1]) || !t[2].same_shape(t[3])) return refuse("attention_gradients: dO and dQ, and dK and dV, are of one shape");
     for (const Tensor& x : t) if (type_code(x.dtype) < 0 || x.dtype != t[0].dtype) return refuse("attention_gradients: dO, dQ, dK and dV are of one type, float32, float16 or bfloat16");
-    *p = lsp_attention_gradients{t[0].data, t[1].data, t[2].data, t[3].data, {t[0].stride[0], t[0].stride[1], t[0].stride[2]}, {t[1].stride[0], t[1].stride[1], t[1].stride[2]},
+    for (int i = 0; i < 4; ++i) { d->q_shape[i] = t[1].shape[i]; d->k_shape[i] = t[2].shape[i]; }
+    d->dtype = type_code(t[0].dtype);
+    d->g = lsp_attention_gradients{t[0].data, t[1].data, t[2].data, t[3].data, {t[0].stride[0], t[0].stride[1], t[0].stride[2]}, {t[1].stride[0], t[1].stride[1], t[1].stride[2]},
                                  {t[2].stride[0], t[2].stride[1], t[2].stride[2]}, {t[3].stride[0], t[3].stride[1], t[3].stride[2]}};
     Py_RETURN_NONE;
 }
@@ -284,12 +301,12 @@ bool vector(PyObject* t, int64_t width, const PyObject* dtype, void*& to, const 
     return true;
 }
 
-// (address of the lsp_residual_norm_problem, x, f, y, h, stats, post_weight, post_bias, gate, pre_weight, pre_bias, post, pre, eps, residual_scale, branch_scale, dropout, seed, offset)
+// (address of the binding's residual_norm_problem, x, f, y, h, stats, post_weight, post_bias, gate, pre_weight, pre_bias, post, pre, eps, residual_scale, branch_scale, dropout, seed, offset)
 PyObject* residual_norm_problem(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!count_is(nargs, 19)) return nullptr;
     const char* what = "residual_norm_problem";
     Args head(args);
-    auto* p = static_cast<lsp_residual_norm_problem*>(head.pointer());
+    auto* d = static_cast<ResidualNormOfTensors*>(head.pointer());
     if (!head.ok || !know_types()) return nullptr;
     Tensor x, f, y, h, stats;
     if (!x.read(args[1], 2, what) || !f.read(args[2], 2, what) || !y.read(args[3], 2, what) || (args[4] != Py_None && !h.read(args[4], 2, what)) || !stats.read(args[5], 2, what)) return nullptr;
@@ -307,17 +324,18 @@ PyObject* residual_norm_problem(PyObject*, PyObject* const* args, Py_ssize_t nar
     const uint64_t seed = tail.integer();
     const uint32_t offset = (uint32_t)tail.integer();
     if (!ok || !tail.ok) return nullptr;
-    *p = lsp_residual_norm_problem{x.data, f.data, y.data, h.data, static_cast<float*>(stats.data), v[0], v[1], v[2], v[3], v[4], x.stride[0], f.stride[0], y.stride[0], h.stride[0],
+    d->dtype = type_code(x.dtype);
+    d->p = lsp_residual_norm_problem{x.data, f.data, y.data, h.data, static_cast<float*>(stats.data), v[0], v[1], v[2], v[3], v[4], x.stride[0], f.stride[0], y.stride[0], h.stride[0],
                                    x.shape[0], (int32_t)(x.shape[1] > INT32_MAX ? 0 : x.shape[1]), post, pre, n[0], n[1], n[2], n[3], offset, seed};
     Py_RETURN_NONE;
 }
 
-// (address of the lsp_residual_norm_gradients, dy, dh, dx, df, post_weight, post_bias, gate, pre_weight, pre_bias)
+// (address of the binding's residual_norm_gradients, dy, dh, dx, df, post_weight, post_bias, gate, pre_weight, pre_bias)
 PyObject* residual_norm_gradients(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!count_is(nargs, 10)) return nullptr;
     const char* what = "residual_norm_gradients";
     Args head(args);
-    auto* p = static_cast<lsp_residual_norm_gradients*>(head.pointer());
+    auto* d = static_cast<ResidualNormGradientsOfTensors*>(head.pointer());
     if (!head.ok || !know_types()) return nullptr;
     Tensor t[4];
     for (int i = 0; i < 4; ++i) if ((i != 1 || args[2] != Py_None) && !t[i].read(args[1 + i], 2, what)) return nullptr;
@@ -326,7 +344,8 @@ PyObject* residual_norm_gradients(PyObject*, PyObject* const* args, Py_ssize_t n
             return refuse("residual_norm_gradients: dy, dh, dx and df are of one shape and type, float32, float16 or bfloat16");
     void* v[5];
     for (int i = 0; i < 5; ++i) if (!vector(args[5 + i], t[0].shape[1], g_types[LSP_F32], v[i], what)) return nullptr;
-    *p = lsp_residual_norm_gradients{t[0].data, t[1].data, t[2].data, t[3].data, static_cast<float*>(v[0]), static_cast<float*>(v[1]), static_cast<float*>(v[2]), static_cast<float*>(v[3]),
+    d->rows = t[0].shape[0]; d->width = t[0].shape[1]; d->dtype = type_code(t[0].dtype);
+    d->g = lsp_residual_norm_gradients{t[0].data, t[1].data, t[2].data, t[3].data, static_cast<float*>(v[0]), static_cast<float*>(v[1]), static_cast<float*>(v[2]), static_cast<float*>(v[3]),
                                      static_cast<float*>(v[4]), t[0].stride[0], t[1].stride[0], t[2].stride[0], t[3].stride[0]};
     Py_RETURN_NONE;
 }
@@ -348,51 +367,103 @@ PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     return without_gil([&] { return g_dropout(x, y, rows, width, p, seed, offset, static_cast<lsp_dtype>(dtype), st); });
 }
 
+// The binding's classes of descriptors: those of the C structures and, derived from these, those that are made of tensors
+enum Kind { ATTENTION, ATTENTION_GRADIENTS, RESIDUAL_NORM, RESIDUAL_NORM_GRADIENTS };
+PyTypeObject* g_base[4];
+PyTypeObject* g_of_tensors[4];
+
+// A descriptor as it is given, made by hand or of tensors; None: NULL
+template <Kind KIND, typename Base, typename OfTensors> struct Given {
+    const Base* p = nullptr;
+    const OfTensors* of_tensors = nullptr;
+    bool take(PyObject* x) {
+        if (x == Py_None) return true;
+        if (!PyObject_TypeCheck(x, g_base[KIND])) { PyErr_Format(PyExc_TypeError, "a descriptor of class %s is wanted", g_base[KIND]->tp_name); return false; }
+        Py_buffer v;
+        if (PyObject_GetBuffer(x, &v, PyBUF_SIMPLE) < 0) return false;
+        p = static_cast<const Base*>(v.buf);
+        if (PyObject_TypeCheck(x, g_of_tensors[KIND])) of_tensors = static_cast<const OfTensors*>(v.buf);
+        PyBuffer_Release(&v);                          // (the object stays the caller's during the call)
+        return true;
+    }
+    bool is_of(int32_t dtype) const {
+        if (!of_tensors || of_tensors->dtype == dtype) return true;
+        refuse("the descriptor's tensors are of another type than the call's");
+        return false;
+    }
+};
+using GivenAttention = Given<ATTENTION, lsp_attention_problem, AttentionOfTensors>;
+using GivenAttentionGradients = Given<ATTENTION_GRADIENTS, lsp_attention_gradients, AttentionGradientsOfTensors>;
+using GivenResidualNorm = Given<RESIDUAL_NORM, lsp_residual_norm_problem, ResidualNormOfTensors>;
+using GivenResidualNormGradients = Given<RESIDUAL_NORM_GRADIENTS, lsp_residual_norm_gradients, ResidualNormGradientsOfTensors>;
+
+// (problem, dtype, ...)
+template <typename P> bool problem_of(Args& a, P& p, int32_t& dtype) {
+    if (!p.take(*a.a++)) return false;
+    dtype = a.int32();
+    return a.ok && p.is_of(dtype);
+}
+
 // (problem, dtype, workspace, workspace_bytes, stream)
 PyObject* attention_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!count_is(nargs, 5)) return nullptr;
     Args a(args);
-    const auto* p = static_cast<const lsp_attention_problem*>(a.pointer());
-    const int32_t dtype = a.int32();
+    GivenAttention p;
+    int32_t dtype;
+    if (!problem_of(a, p, dtype)) return nullptr;
     void* ws = a.pointer();
     const size_t bytes = a.integer();
     void* st = a.stream();
     if (!a.ok) return nullptr;
-    return without_gil([&] { return g_attention_forward(p, static_cast<lsp_dtype>(dtype), ws, bytes, st); });
+    return without_gil([&] { return g_attention_forward(p.p, static_cast<lsp_dtype>(dtype), ws, bytes, st); });
 }
 // (problem, gradients, dtype, workspace, workspace_bytes, stream)
 template <typename Problem, typename Gradients, typename Entry> PyObject* backward(Entry entry, PyObject* const* args, Py_ssize_t nargs) {
     if (!count_is(nargs, 6)) return nullptr;
     Args a(args);
-    const auto* p = static_cast<const Problem*>(a.pointer());
-    const auto* g = static_cast<const Gradients*>(a.pointer());
+    Problem p;
+    Gradients g;
+    if (!p.take(*a.a++) || !g.take(*a.a++)) return nullptr;
     const int32_t dtype = a.int32();
     void* ws = a.pointer();
     const size_t bytes = a.integer();
     void* st = a.stream();
-    if (!a.ok) return nullptr;
-    return without_gil([&] { return entry(p, g, static_cast<lsp_dtype>(dtype), ws, bytes, st); });
+    if (!a.ok || !p.is_of(dtype) || !g.is_of(dtype)) return nullptr;
+    if (p.of_tensors && g.of_tensors && !matches(*p.of_tensors, *g.of_tensors)) return refuse("the gradients are of other shapes than the problem's tensors");
+    return without_gil([&] { return entry(p.p, g.p, static_cast<lsp_dtype>(dtype), ws, bytes, st); });
 }
-PyObject* attention_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return backward<lsp_attention_problem, lsp_attention_gradients>(g_attention_backward, args, nargs); }
-PyObject* residual_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return backward<lsp_residual_norm_problem, lsp_residual_norm_gradients>(g_norm_backward, args, nargs); }
+PyObject* attention_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    return backward<GivenAttention, GivenAttentionGradients>(g_attention_backward, args, nargs);
+}
+PyObject* residual_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    return backward<GivenResidualNorm, GivenResidualNormGradients>(g_norm_backward, args, nargs);
+}
 // (problem, dtype, stream)
 PyObject* residual_norm_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (!count_is(nargs, 3)) return nullptr;
     Args a(args);
-    const auto* p = static_cast<const lsp_residual_norm_problem*>(a.pointer());
-    const int32_t dtype = a.int32();
+    GivenResidualNorm p;
+    int32_t dtype;
+    if (!problem_of(a, p, dtype)) return nullptr;
     void* st = a.stream();
     if (!a.ok) return nullptr;
-    return without_gil([&] { return g_norm_forward(p, static_cast<lsp_dtype>(dtype), st); });
+    return without_gil([&] { return g_norm_forward(p.p, static_cast<lsp_dtype>(dtype), st); });
 }
 
-// (addresses of lsp_dropout, lsp_attention_forward, lsp_attention_backward, lsp_residual_norm_forward, lsp_residual_norm_backward)
+// (addresses of lsp_dropout, lsp_attention_forward, lsp_attention_backward, lsp_residual_norm_forward, lsp_residual_norm_backward; the classes of the four C structures, in
+// the order of Kind, and those of descriptors made of tensors)
 PyObject* bind_operators(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-    if (!count_is(nargs, 5)) return nullptr;
+    if (!count_is(nargs, 13)) return nullptr;
     Args a(args);
     void* p[5];
     for (void*& x : p) x = a.pointer();
     if (!a.ok) return nullptr;
+    for (int i = 5; i < 13; ++i) if (!PyType_Check(args[i])) return refuse("bind_operators: classes are wanted");
+    for (int i = 0; i < 4; ++i) {
+        Py_INCREF(args[5 + i]); Py_INCREF(args[9 + i]);                    // (kept as long as the module is)
+        g_base[i] = reinterpret_cast<PyTypeObject*>(args[5 + i]);
+        g_of_tensors[i] = reinterpret_cast<PyTypeObject*>(args[9 + i]);
+    }
     g_dropout = reinterpret_cast<decltype(g_dropout)>(p[0]);
     g_attention_forward = reinterpret_cast<decltype(g_attention_forward)>(p[1]);
     g_attention_backward = reinterpret_cast<decltype(g_attention_backward)>(p[2]);

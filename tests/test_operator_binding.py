@@ -62,3 +62,69 @@ def test_types_without_a_kernel(other):
     for make in (lambda: _attention(other), lambda: _norm(other), lambda: _gradients(other, other, other, other), lambda: _norm_gradients(other, other, other, other)):
         with pytest.raises(ValueError):
             make()
+
+
+CODE = {F32: 0, F16: 1, BF16: 2}
+FAKE, ROOM = 0x1000, 1 << 30                 # never followed: these calls fail before any HIP call
+
+
+def _attention_back(problem, gradients, dtype=2):
+    return L.lsp_attention_backward(problem, gradients, dtype, FAKE, ROOM, None, check=False)
+
+
+def _norm_back(problem, gradients, dtype=2):
+    return L.lsp_residual_norm_backward(problem, gradients, dtype, FAKE, ROOM, None, check=False)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_the_calls_type_is_the_tensors(dtype):
+    p, n = _attention(dtype), _norm(dtype)
+    for code in {0, 1, 2, 3} - {CODE[dtype]}:
+        with pytest.raises(ValueError):
+            L.lsp_attention_forward(p, code, FAKE, ROOM, None, check=False)
+        with pytest.raises(ValueError):
+            _attention_back(p, _gradients(dtype, dtype, dtype, dtype), code)
+        with pytest.raises(ValueError):
+            L.lsp_residual_norm_forward(n, code, None, check=False)
+        with pytest.raises(ValueError):
+            _norm_back(n, _norm_gradients(dtype, dtype, dtype, dtype), code)
+
+
+@pytest.mark.parametrize("other", [F32, F16])
+def test_gradients_are_of_the_problems_type(other):
+    with pytest.raises(ValueError):
+        _attention_back(_attention(BF16), _gradients(other, other, other, other))
+    with pytest.raises(ValueError):
+        _norm_back(_norm(BF16), _norm_gradients(other, other, other, other))
+
+
+@pytest.mark.parametrize("q,k", [((2, 4, 4, 16), (2, 7, 2, 16)), ((2, 5, 4, 16), (2, 6, 2, 16)), ((1, 5, 4, 16), (1, 7, 2, 16)), ((2, 5, 2, 16), (2, 7, 2, 16)), ((2, 5, 4, 16), (2, 7, 1, 16)),
+                                 ((2, 5, 4, 8), (2, 7, 2, 8)), ((2, 5, 4, 24), (2, 7, 2, 24)), ((2, 5, 4, 16), (1, 7, 2, 16))])
+def test_gradients_have_the_problems_shapes(q, k):
+    a, b = torch.zeros(q, dtype=BF16), torch.zeros(k, dtype=BF16)
+    with pytest.raises(ValueError):
+        _attention_back(_attention(), L.attention_gradients(a, a, b, b))
+
+
+@pytest.mark.parametrize("shape", [(2, 8), (4, 8), (3, 7), (3, 16)])
+def test_norm_gradients_have_the_problems_shape(shape):
+    t = torch.zeros(shape, dtype=BF16)
+    with pytest.raises(ValueError):
+        _norm_back(_norm(), L.residual_norm_gradients(t, t, t, t))
+
+
+def test_descriptors_of_another_kind():
+    a, g, n, m = _attention(), _gradients(), _norm(), _norm_gradients()
+    for call in (lambda: L.lsp_attention_forward(n, 2, FAKE, ROOM, None, check=False), lambda: L.lsp_residual_norm_forward(a, 2, None, check=False),
+                 lambda: _attention_back(a, m), lambda: _attention_back(g, g), lambda: _norm_back(n, g), lambda: _norm_back(m, m)):
+        with pytest.raises(TypeError):
+            call()
+
+
+def test_descriptors_keep_what_they_were_made_of():
+    """Fields may be changed between calls (offsets are); what is compared is what the structure says then."""
+    p = _attention()
+    p.offset = 7
+    p.k_len = 6
+    with pytest.raises(ValueError):
+        _attention_back(p, _gradients())
