@@ -30,6 +30,7 @@ decltype(&lsp_residual_norm_backward) g_norm_backward;
 PyObject* g_shape;
 PyObject* g_stride;
 PyObject* g_dtype;
+PyObject* g_get_device;
 PyObject* g_types[3];         // torch's types, in the order of lsp_dtype; from the first descriptor on
 
 // Converts one argument after another, to what ctypes makes of it; the first failure leaves a Python exception and ok = false.
@@ -195,6 +196,15 @@ struct Tensor {
     bool same_shape(const Tensor& o) const { return shape[0] == o.shape[0] && shape[1] == o.shape[1] && shape[2] == o.shape[2] && shape[3] == o.shape[3]; }
 };
 
+// The device that a tensor is on, -1: the host; false with a Python exception set
+bool device_of(PyObject* t, long& device) {
+    PyObject* where = PyObject_CallMethodNoArgs(t, g_get_device);
+    if (!where) return false;
+    device = PyLong_AsLong(where);
+    Py_DECREF(where);
+    return !PyErr_Occurred();
+}
+
 PyObject* refuse(const char* text) {
     PyErr_SetString(PyExc_ValueError, text);
     return nullptr;
@@ -255,6 +265,9 @@ PyObject* attention_problem(PyObject*, PyObject* const* args, Py_ssize_t nargs) 
         Tensor n;
         if (!n.read(args[6 + i], 1, what)) return nullptr;
         if (n.shape[0] != q.shape[0]) return refuse("attention_problem: lengths are [batch]");
+        long there, here;                              // (the one operand that a program may well have on the host, where the kernels must not read it)
+        if (!device_of(args[6 + i], there) || !device_of(args[1], here)) return nullptr;
+        if (there != here) return refuse("attention_problem: lengths are on the device of the other tensors");
         lens[i] = n.data;
     }
     Args tail(args + 9);
@@ -497,6 +510,7 @@ PyMODINIT_FUNC PyInit__call(void) {
     g_shape = PyUnicode_InternFromString("shape");
     g_stride = PyUnicode_InternFromString("stride");
     g_dtype = PyUnicode_InternFromString("dtype");
+    g_get_device = PyUnicode_InternFromString("get_device");
     PyObject* ctypes = PyImport_ImportModule("ctypes");
     if (!ctypes) return nullptr;
     g_argument_error = PyObject_GetAttrString(ctypes, "ArgumentError");

@@ -128,3 +128,25 @@ def test_descriptors_keep_what_they_were_made_of():
     p.k_len = 6
     with pytest.raises(ValueError):
         _attention_back(p, _gradients())
+
+
+def test_lengths_are_where_the_other_tensors_are():
+    """Lists of lengths begin on the host; the kernels would follow the address there."""
+    q, logs = torch.zeros(2, 5, 4, 16), torch.zeros(2, 4, 5)
+
+    class Elsewhere:
+        """Lengths that say of themselves that they are on device 0."""
+        def __init__(self):
+            self.t = torch.ones(2, dtype=torch.int32)
+
+        def __getattr__(self, name):
+            return getattr(self.t, name)
+
+        def get_device(self):
+            return 0
+
+    ok = torch.ones(2, dtype=torch.int32)
+    L.attention_problem(q, q, q, q, logs, scale=1.0, q_lens=ok, k_lens=ok)
+    for lens in (dict(q_lens=Elsewhere()), dict(k_lens=Elsewhere()), dict(q_lens=ok, k_lens=Elsewhere())):
+        with pytest.raises(ValueError):
+            L.attention_problem(q, q, q, q, logs, scale=1.0, **lens)
