@@ -225,6 +225,9 @@ int type_code(const PyObject* dtype) {
     return -1;
 }
 
+// A size as the C structures have it; 0, which the library refuses, where it has no room there
+int32_t size32(int64_t n) { return n > INT32_MAX ? 0 : (int32_t)n; }
+
 float number(PyObject* x, bool& ok) {
     const double v = PyFloat_AsDouble(x);
     if (v == -1.0 && PyErr_Occurred()) ok = false;
@@ -282,7 +285,7 @@ PyObject* attention_problem(PyObject*, PyObject* const* args, Py_ssize_t nargs) 
     d->dtype = type_code(q.dtype);
     d->p = lsp_attention_problem{q.data, k.data, v.data, o.data, static_cast<float*>(l.data), static_cast<const int32_t*>(lens[0]), static_cast<const int32_t*>(lens[1]),
                                {q.stride[0], q.stride[1], q.stride[2]}, {k.stride[0], k.stride[1], k.stride[2]}, {v.stride[0], v.stride[1], v.stride[2]}, {o.stride[0], o.stride[1], o.stride[2]},
-                               (int32_t)q.shape[0], (int32_t)q.shape[2], (int32_t)k.shape[2], (int32_t)q.shape[1], (int32_t)k.shape[1], (int32_t)q.shape[3], causal, scale, dropout, offset, seed};
+                               size32(q.shape[0]), size32(q.shape[2]), size32(k.shape[2]), size32(q.shape[1]), size32(k.shape[1]), size32(q.shape[3]), causal, scale, dropout, offset, seed};
     Py_RETURN_NONE;
 }
 
@@ -339,7 +342,7 @@ PyObject* residual_norm_problem(PyObject*, PyObject* const* args, Py_ssize_t nar
     if (!ok || !tail.ok) return nullptr;
     d->dtype = type_code(x.dtype);
     d->p = lsp_residual_norm_problem{x.data, f.data, y.data, h.data, static_cast<float*>(stats.data), v[0], v[1], v[2], v[3], v[4], x.stride[0], f.stride[0], y.stride[0], h.stride[0],
-                                   x.shape[0], (int32_t)(x.shape[1] > INT32_MAX ? 0 : x.shape[1]), post, pre, n[0], n[1], n[2], n[3], offset, seed};
+                                   x.shape[0], size32(x.shape[1]), post, pre, n[0], n[1], n[2], n[3], offset, seed};
     Py_RETURN_NONE;
 }
 

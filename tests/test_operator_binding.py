@@ -150,3 +150,10 @@ def test_lengths_are_where_the_other_tensors_are():
     for lens in (dict(q_lens=Elsewhere()), dict(k_lens=Elsewhere()), dict(q_lens=ok, k_lens=Elsewhere())):
         with pytest.raises(ValueError):
             L.attention_problem(q, q, q, q, logs, scale=1.0, **lens)
+
+
+def test_sizes_beyond_32_bits_are_refused():
+    """Views that repeat one position 2^32 + 2 times: not two positions."""
+    q, k, logs = torch.zeros(1, 2, 1, 16), torch.zeros(1, 1, 1, 16).expand(1, (1 << 32) + 2, 1, 16), torch.zeros(1, 1, 2)
+    p = L.attention_problem(q, k, k, q, logs, scale=1.0)
+    assert L.lsp_attention_forward(p, 0, FAKE, ROOM, None, check=False) == -2
