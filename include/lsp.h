@@ -408,6 +408,7 @@ int lsp_dropout(const void* x, void* y, int64_t rows, int64_t width, float dropo
  *                   16 bytes and a position's is below 8 MiB
  *   L               device, [batch][heads][q_len] fp32
  *   head_dim        a multiple of 8, at most LSP_MAX_HEAD_DIM;  scale > 0;  batch * heads * (q_len or k_len) below 2^27
+ *   and, tiles of 128 positions counted up, batch * heads * tiles(q_len) below 2^24 (backward: together with batch * kv_heads * tiles(k_len))
  * The products run on the matrix cores in `dtype` with fp32 accumulation (fp32: in fp32); scores, softmax
  * statistics and sums are fp32; probabilities and the gradients of the scores are rounded to `dtype` as
  * operands of the second products.  No atomics: results are the same bits from run to run.

@@ -1,0 +1,54 @@
+"""CPU-only: problems at the border of what the training operators' launches hold; refused before any HIP call."""
+import ctypes
+
+import pytest
+
+from test_operator_refusals import FAKE, attention, gradients
+import paper_2406_10181_amd as L
+
+THREE = ctypes.c_int64 * 3
+BIG = 1 << 40
+
+
+def _forward(p, dtype=2):
+    return L.lsp_attention_forward(p, dtype, FAKE, BIG, None, check=False)
+
+
+def _backward(p, g, dtype=2):
+    return L.lsp_attention_backward(p, g, dtype, FAKE, BIG, None, check=False)
+
+
+def _tokens(batch, q_len=1, k_len=1, heads=1):
+    """Short texts of one head, rows one behind the other."""
+    strides = lambda length: THREE(length * heads * 8, heads * 8, 8)
+    q, k = strides(q_len), strides(k_len)
+    p = attention(batch=batch, heads=heads, kv_heads=heads, q_len=q_len, k_len=k_len, head_dim=8, q_stride=q, k_stride=k, v_stride=k, o_stride=q)
+    return p, gradients(do_stride=q, dq_stride=q, dk_stride=k, dv_stride=k)
+
+
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+def test_forward_launches_have_fewer_than_2_to_32_threads(dtype):
+    """256 threads for every text and head."""
+    for p in (_tokens(1 << 24)[0], _tokens(1 << 23, heads=2)[0], _tokens(1 << 24, 7, 3)[0]):
+        assert _forward(p, dtype) == -2
+        assert L.lsp_attention_forward_workspace_bytes(p, dtype) == 0
+
+
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+@pytest.mark.parametrize("q_len,k_len", [(1, 1), (15, 1), (1, 15), (15, 15)])
+def test_backward_launches_have_fewer_than_2_to_32_threads(dtype, q_len, k_len):
+    """Twice as many: workgroups for queries and for keys are of one launch."""
+    for batch in (1 << 23, (1 << 23) + 1):
+        p, g = _tokens(batch, q_len, k_len)
+        assert L.lsp_attention_backward_workspace_bytes(p, dtype) == 0
+        assert _backward(p, g, dtype) == -2
+    p, g = _tokens((1 << 23) - 1, q_len, k_len)
+    assert L.lsp_attention_backward_workspace_bytes(p, dtype) > 0
+
+
+def test_shared_key_heads_count_once():
+    q, k = THREE(32, 32, 8), THREE(8, 8, 8)
+    p = attention(batch=3 << 20, heads=4, kv_heads=1, q_len=1, k_len=1, head_dim=8, q_stride=q, k_stride=k, v_stride=k, o_stride=q)
+    assert L.lsp_attention_backward_workspace_bytes(p, 2) > 0             # 12 * 2^20 + 3 * 2^20
+    p.batch = 1 << 22
+    assert L.lsp_attention_backward_workspace_bytes(p, 2) == 0            # 16 * 2^20 + 4 * 2^20
