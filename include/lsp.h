@@ -408,7 +408,8 @@ int lsp_dropout(const void* x, void* y, int64_t rows, int64_t width, float dropo
  *                   16 bytes and a position's is below 8 MiB
  *   L               device, [batch][heads][q_len] fp32
  *   head_dim        a multiple of 8, at most LSP_MAX_HEAD_DIM;  scale > 0;  batch * heads * (q_len or k_len) below 2^27
- *   and, tiles of 128 positions counted up, batch * heads * tiles(q_len) below 2^24 (backward: together with batch * kv_heads * tiles(k_len))
+ *   and no launch of 2^24 workgroups or more: batch * heads * ceil(q_len / 128) below 2^24 (forward: batch * kv_heads, where the query heads of
+ *   a key head have 128 rows or fewer together; backward: together with batch * kv_heads * ceil(k_len / 128))
  * The products run on the matrix cores in `dtype` with fp32 accumulation (fp32: in fp32); scores, softmax
  * statistics and sums are fp32; probabilities and the gradients of the scores are rounded to `dtype` as
  * operands of the second products.  No atomics: results are the same bits from run to run.

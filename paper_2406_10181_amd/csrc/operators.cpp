@@ -113,26 +113,16 @@ lsp::Strided strided(const void* p, const int64_t (&s)[3], int64_t batch, int64_
     return {p, batch > 1 ? s[0] : 0, positions > 1 ? s[1] : 0, heads > 1 ? s[2] : 0};
 }
 
-constexpr int64_t kMostWorkgroups = (int64_t)1 << 24;                      // of 256 threads
-int64_t tiles_of(int64_t positions) { return (positions + lsp::kBackwardRows - 1) / lsp::kBackwardRows; }
-int64_t row_tiles(const lsp_attention_problem* p) { return (int64_t)p->batch * p->heads * tiles_of(p->q_len); }
-int64_t key_tiles(const lsp_attention_problem* p) { return (int64_t)p->batch * p->kv_heads * tiles_of(p->k_len); }
-
 int check_attention_shape(const lsp_attention_problem* p, lsp_dtype t) {
     if (!p) return LSP_ERR_NULL;
     if (p->batch <= 0 || p->heads <= 0 || p->kv_heads <= 0 || p->q_len <= 0 || p->k_len <= 0 || p->head_dim <= 0) return LSP_ERR_SHAPE;
     if (p->heads % p->kv_heads || p->head_dim % 8 || p->head_dim > LSP_MAX_HEAD_DIM) return LSP_ERR_SHAPE;
     if (p->q_len > (1 << 30) || p->k_len > (1 << 30) || (p->causal != 0 && p->causal != 1)) return LSP_ERR_SHAPE;
-    // A launch has fewer than 2^32 threads: 16 for every row of dO and of V, where delta is made, and 256 for every 128 queries of a head (and every 128 keys, see
-    // check_backward_launch).  Parts of a tile, and workgroups of 512, are for few tiles and long texts.
-    if ((int64_t)p->batch * p->heads >= (1 << 24) || (int64_t)p->batch * p->heads * std::max(p->q_len, p->k_len) >= ((int64_t)1 << 27)) return LSP_ERR_SHAPE;
-    if (row_tiles(p) >= kMostWorkgroups) return LSP_ERR_SHAPE;
+    // a launch has fewer than 2^32 threads: 16 for every row of dO and of V, where delta is made (the others: launches())
+    if ((int64_t)p->batch * p->heads > (1 << 24) || (int64_t)p->batch * p->heads * std::max(p->q_len, p->k_len) >= ((int64_t)1 << 27)) return LSP_ERR_SHAPE;
     if (!known(t)) return LSP_ERR_DTYPE;
     return LSP_OK;
 }
-
-// The backward pass has both kinds of workgroups in one launch
-int check_backward_launch(const lsp_attention_problem* p) { return row_tiles(p) + key_tiles(p) < kMostWorkgroups ? LSP_OK : LSP_ERR_SHAPE; }
 
 int check_attention(const lsp_attention_problem* p, lsp_dtype t) {
     if (!p || !p->Q || !p->K || !p->V || !p->O || !p->L) return LSP_ERR_NULL;
@@ -161,6 +151,15 @@ lsp::AttentionArgs attention_args(const lsp_attention_problem* p) {
     a.scale = p->scale; a.scale_log2 = p->scale * 1.44269504088896341f;
     a.drop = lsp::make_dropout(p->dropout, p->seed, p->offset);
     return a;
+}
+
+// Whether the workgroups of the plan have fewer than 2^32 threads; the backward pass has those for queries and those for keys in one launch.
+bool launches_forward(const lsp::AttentionArgs& a) {
+    return (int64_t)a.batch * (a.packed ? a.kv_heads : a.heads) * a.tiles * a.splits * a.waves * 64 < ((int64_t)1 << 32);
+}
+bool launches_backward(const lsp::AttentionArgs& a) {
+    const auto tiles = [](int64_t positions) { return (positions + lsp::kBackwardRows - 1) / lsp::kBackwardRows; };
+    return (a.batch * (int64_t)a.heads * tiles(a.q_len) * a.query_parts + a.batch * (int64_t)a.kv_heads * tiles(a.k_len) * a.key_parts) * 256 < ((int64_t)1 << 32);
 }
 
 constexpr size_t kNormBytes = 2 * lsp::kNormSlots * sizeof(float);
@@ -217,7 +216,7 @@ size_t lsp_attention_forward_workspace_bytes(const lsp_attention_problem* p, lsp
     if (check_attention_shape(p, dtype) != LSP_OK) return 0;
     lsp::AttentionArgs a = attention_args(p);
     lsp::plan_attention_forward(a, dtype);
-    return lsp::attention_partial_bytes(a);
+    return launches_forward(a) ? lsp::attention_partial_bytes(a) : 0;
 }
 
 int lsp_attention_forward(const lsp_attention_problem* p, lsp_dtype dtype, void* workspace, size_t workspace_bytes, void* stream) {
@@ -225,6 +224,7 @@ int lsp_attention_forward(const lsp_attention_problem* p, lsp_dtype dtype, void*
     if (rc != LSP_OK) return rc;
     lsp::AttentionArgs a = attention_args(p);
     lsp::plan_attention_forward(a, dtype);
+    if (!launches_forward(a)) return LSP_ERR_SHAPE;
     const size_t need = lsp::attention_partial_bytes(a);
     if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return LSP_ERR_WORKSPACE;
     a.partial = static_cast<float*>(workspace);
@@ -233,22 +233,24 @@ int lsp_attention_forward(const lsp_attention_problem* p, lsp_dtype dtype, void*
 
 // delta | norms | parts
 size_t lsp_attention_backward_workspace_bytes(const lsp_attention_problem* p, lsp_dtype dtype) {
-    if (check_attention_shape(p, dtype) != LSP_OK || check_backward_launch(p) != LSP_OK) return 0;
+    if (check_attention_shape(p, dtype) != LSP_OK) return 0;
     lsp::AttentionArgs a = attention_args(p);
     lsp::plan_attention_backward(a, dtype);
-    return delta_bytes(p) + kNormBytes + lsp::attention_backward_partial_bytes(a);
+    return launches_backward(a) ? delta_bytes(p) + kNormBytes + lsp::attention_backward_partial_bytes(a) : 0;
 }
 
 int lsp_attention_backward(const lsp_attention_problem* p, const lsp_attention_gradients* g, lsp_dtype dtype, void* workspace, size_t workspace_bytes, void* stream) {
     if (!p || !g || !g->dO || !g->dQ || !g->dK || !g->dV) return LSP_ERR_NULL;
     int rc = check_attention(p, dtype);
-    if (rc != LSP_OK || (rc = check_backward_launch(p)) != LSP_OK) return rc;
+    if (rc != LSP_OK) return rc;
     if ((rc = check_strides(g->do_stride, p->batch, p->q_len, p->heads, p->head_dim, dtype, false)) != LSP_OK) return rc;
     if ((rc = check_strides(g->dq_stride, p->batch, p->q_len, p->heads, p->head_dim, dtype, true)) != LSP_OK) return rc;
     if ((rc = check_strides(g->dk_stride, p->batch, p->k_len, p->kv_heads, p->head_dim, dtype, true)) != LSP_OK) return rc;
     if ((rc = check_strides(g->dv_stride, p->batch, p->k_len, p->kv_heads, p->head_dim, dtype, true)) != LSP_OK) return rc;
     if (!aligned16(g->dO) || !aligned16(g->dQ) || !aligned16(g->dK) || !aligned16(g->dV)) return LSP_ERR_ALIGN;
-    if (!workspace || workspace_bytes < lsp_attention_backward_workspace_bytes(p, dtype) || !aligned16(workspace)) return LSP_ERR_WORKSPACE;
+    const size_t need = lsp_attention_backward_workspace_bytes(p, dtype);
+    if (!need) return LSP_ERR_SHAPE;                                      // (a launch too large)
+    if (!workspace || workspace_bytes < need || !aligned16(workspace)) return LSP_ERR_WORKSPACE;
     lsp::AttentionArgs a = attention_args(p);
     a.d_o = strided(g->dO, g->do_stride, p->batch, p->q_len, p->heads);
     a.dq = strided(g->dQ, g->dq_stride, p->batch, p->q_len, p->heads);

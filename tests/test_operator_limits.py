@@ -52,3 +52,11 @@ def test_shared_key_heads_count_once():
     assert L.lsp_attention_backward_workspace_bytes(p, 2) > 0             # 12 * 2^20 + 3 * 2^20
     p.batch = 1 << 22
     assert L.lsp_attention_backward_workspace_bytes(p, 2) == 0            # 16 * 2^20 + 4 * 2^20
+
+
+def test_parts_of_the_keys_keep_their_workspace():
+    """Few texts, long caches: the limit counts the parts too, and they are few."""
+    q, k = THREE(128, 128, 8), THREE(8192 * 8, 8, 8)
+    p = attention(batch=4, heads=16, kv_heads=1, q_len=1, k_len=8192, head_dim=8, q_stride=q, k_stride=k, v_stride=k, o_stride=q)
+    need = L.lsp_attention_forward_workspace_bytes(p, 2)
+    assert need > 0 and L.lsp_attention_forward(p, 2, FAKE, need - 1, None, check=False) == -4
