@@ -405,7 +405,8 @@ int lsp_dropout(const void* x, void* y, int64_t rows, int64_t width, float dropo
  *   Q, O, dO, dQ    device, [batch][q_len][heads][head_dim] of `dtype`; K, V, dK, dV  [batch][k_len][kv_heads][head_dim];
  *                   each with the strides given (of batch, position and head, in elements; the last axis is
  *                   contiguous), so views into a joint projection serve as they are.  Strides are multiples of
- *                   16 bytes and a position's is below 8 MiB
+ *                   16 bytes and a position's is below 8 MiB.  In O, dQ, dK and dV every row has a place of its own: the stride of an
+ *                   axis is at least what the axes of smaller strides span; and none of them overlaps another operand
  *   L               device, [batch][heads][q_len] fp32
  *   head_dim        a multiple of 8, at most LSP_MAX_HEAD_DIM;  scale > 0;  batch * heads * (q_len or k_len) below 2^27
  *   and no launch of 2^24 workgroups or more: batch * heads * ceil(q_len / 128) below 2^24 (forward: batch * kv_heads, where the query heads of
