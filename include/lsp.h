@@ -454,14 +454,15 @@ int    lsp_attention_backward(const lsp_attention_problem* problem, const lsp_at
  *   LSP_NORM_RMS    norm(v) = v / sqrt(mean(v^2) + eps) * weight [+ bias]
  *   LSP_NORM_LAYER  norm(v) = (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) * weight [+ bias]
  * All in fp32; y and h are rounded once each (h is made from the y before rounding).
- *   x, f, y, h      device, [rows][width] of `dtype` with the row strides given (elements, at least width).  y may be x;
- *                   h may be NULL, with pre = LSP_NORM_NONE
+ *   x, f, y, h      device, [rows][width] of `dtype` with the row strides given (elements, at least width).  y and h may each be x or
+ *                   f, row on row, or one the other (h stays); h may be NULL, with pre = LSP_NORM_NONE
  *   weights, biases, gate   device, [width] of `dtype`; NULL: ones, zeros, ones
  *   stats           device, [4][rows] fp32, kept for the backward pass: mean of f, 1 / deviation of f, the same of y
  * The backward pass takes the gradients of y (dy) and h (dh; NULL where h is) and gives those of x and f and,
  * where asked for (not NULL), of the weights, biases and gate (fp32, [width], overwritten; sums over the rows in an
- * order that does not change from run to run).  It needs x and f as the forward pass had them (so y must not
- * be x then), and its stats.  dx may be dy. */
+ * order that does not change from run to run).  It needs x and f as the forward pass had them (so neither y nor h
+ * may be one of them then), and its stats.  dx and df may each be dy, dh, x or f, row on row, or one the other (df stays).
+ * Otherwise what is written overlaps nothing else. */
 typedef enum { LSP_NORM_NONE = 0, LSP_NORM_RMS = 1, LSP_NORM_LAYER = 2 } lsp_norm;
 
 typedef struct {

@@ -187,6 +187,9 @@ int check_norm_shape(const lsp_residual_norm_problem* p, lsp_dtype t) {
     return LSP_OK;
 }
 
+// Whether an output over an input lies on it row by row
+bool on_it(const void* in, int64_t in_stride, const void* out, int64_t out_stride, int64_t rows) { return in != out || rows == 1 || in_stride == out_stride; }
+
 int check_norm(const lsp_residual_norm_problem* p, lsp_dtype t) {
     if (!p || !p->x || !p->f || !p->y || !p->stats || (!p->h && p->pre != LSP_NORM_NONE)) return LSP_ERR_NULL;
     const int rc = check_norm_shape(p, t);
@@ -198,6 +201,9 @@ int check_norm(const lsp_residual_norm_problem* p, lsp_dtype t) {
     for (const void* q : {p->x, p->f, static_cast<const void*>(p->y), static_cast<const void*>(p->h), static_cast<const void*>(p->stats), p->post_weight, p->post_bias, p->gate,
                           p->pre_weight, p->pre_bias})
         if (!aligned16(q)) return LSP_ERR_ALIGN;
+    if (!on_it(p->x, p->x_stride, p->y, p->y_stride, p->rows) || !on_it(p->f, p->f_stride, p->y, p->y_stride, p->rows)) return LSP_ERR_SHAPE;
+    if (p->h && (!on_it(p->x, p->x_stride, p->h, p->h_stride, p->rows) || !on_it(p->f, p->f_stride, p->h, p->h_stride, p->rows) || !on_it(p->y, p->y_stride, p->h, p->h_stride, p->rows)))
+        return LSP_ERR_SHAPE;
     return LSP_OK;
 }
 
@@ -299,8 +305,13 @@ int lsp_residual_norm_backward(const lsp_residual_norm_problem* p, const lsp_res
         if (!aligned16(q)) return LSP_ERR_ALIGN;
     for (const float* q : {g->post_weight, g->post_bias, g->gate, g->pre_weight, g->pre_bias})
         if (!aligned16(q)) return LSP_ERR_ALIGN;
+    const struct { const void* at; int64_t stride; } in[4] = {{p->x, p->x_stride}, {p->f, p->f_stride}, {g->dy, g->dy_stride}, {g->dh, g->dh_stride}};
+    for (const auto& i : in)
+        if (!on_it(i.at, i.stride, g->dx, g->dx_stride, p->rows) || !on_it(i.at, i.stride, g->df, g->df_stride, p->rows)) return LSP_ERR_SHAPE;
+    if (!on_it(g->dx, g->dx_stride, g->df, g->df_stride, p->rows)) return LSP_ERR_SHAPE;
     const size_t need = lsp_residual_norm_backward_workspace_bytes(p, dtype);
     if (!workspace || workspace_bytes < need || !aligned16(workspace)) return LSP_ERR_WORKSPACE;
+    if (p->y == p->f || (p->h && (p->h == p->x || p->h == p->f))) return LSP_ERR_SHAPE;      // as are x and f
     lsp::ResidualNormArgs a = norm_args(p);
     a.dy = g->dy; a.dh = g->dh; a.dx = g->dx; a.df = g->df;
     a.dy_stride = g->dy_stride; a.dh_stride = g->dh_stride; a.dx_stride = g->dx_stride; a.df_stride = g->df_stride;

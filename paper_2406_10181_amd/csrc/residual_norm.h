@@ -14,6 +14,7 @@ struct ResidualNormArgs {
     int64_t x_stride, f_stride, y_stride, h_stride, dy_stride, dh_stride, dx_stride, df_stride;
     int64_t rows;
     int32_t width, post, pre, many;                      // many: backward, see many_rows()
+    int32_t whole, whole_too;                            // see may_read_whole()
     float   eps, residual_scale, branch_scale;
     Dropout drop;
 };

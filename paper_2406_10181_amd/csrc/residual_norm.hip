@@ -135,7 +135,7 @@ __global__ __launch_bounds__(TPR * GROUPS) void k_residual_norm(const ResidualNo
     RowSum<TPR, 1> sum{scratch[group]};
     const elem* x = static_cast<const elem*>(a.x) + row * a.x_stride;
     const elem* f = static_cast<const elem*>(a.f) + row * a.f_stride;
-    const bool whole = width >= 8, x_whole = whole && a.y != a.x;                         // (in place: a neighbour may have stored already)
+    const bool whole = a.whole, x_whole = a.whole_too;
     Columns c[NV];
     Eight xv[NV], fv[NV];
 #pragma unroll
@@ -199,7 +199,7 @@ __global__ __launch_bounds__(TPR * GROUPS, 2) void k_residual_norm_back(const Re
     Columns c[NV];
 #pragma unroll
     for (int n = 0; n < NV; ++n) c[n] = columns_of(t + n * TPR, width);
-    const bool whole = width >= 8, dy_whole = whole && a.dx != a.dy;                      // (in place: a neighbour may have stored already)
+    const bool whole = a.whole, dy_whole = a.whole_too;
     const float per = 1.0f / (float)width, scale_u = DROP ? a.branch_scale * a.drop.scale : a.branch_scale;
     RowSum<TPR, 2> sum{scratch + group * 4 * (TPR / 64)};
     const bool post = a.post != LSP_NORM_NONE, pre = a.pre != LSP_NORM_NONE;
@@ -454,7 +454,17 @@ size_t residual_norm_partial_bytes(int64_t rows, int32_t width) {
     return align_up((size_t)parts_of(rows, width) * kGrads * (size_t)width * sizeof(float), 256);
 }
 
-template <typename D, int TPR, int NV, int GROUPS> static hipError_t run_forward(const ResidualNormArgs& a, hipStream_t st) {
+// Whether a row's last thread may read eight columns whole: no output lies on what it reads, where a neighbour may have stored already.  Forward: f (and the weights), and x;
+// backward: x, f, dh (and the weights), and dy.
+template <int N> static bool may_read_whole(const ResidualNormArgs& a, const void* const (&read)[N], const void* out, const void* out_too) {
+    bool apart = a.width >= 8;
+    for (const void* p : read) apart = apart && p != out && p != out_too;
+    return apart;
+}
+
+template <typename D, int TPR, int NV, int GROUPS> static hipError_t run_forward(ResidualNormArgs a, hipStream_t st) {
+    a.whole = may_read_whole(a, {a.f}, a.y, a.h);
+    a.whole_too = may_read_whole(a, {a.x}, a.y, a.h);
     const dim3 grid((unsigned)((a.rows + GROUPS - 1) / GROUPS)), block(TPR * GROUPS);
     if (a.drop.limit) hipLaunchKernelGGL((k_residual_norm<D, TPR, NV, GROUPS, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((k_residual_norm<D, TPR, NV, GROUPS, false>), grid, block, 0, st, a);
@@ -463,6 +473,8 @@ template <typename D, int TPR, int NV, int GROUPS> static hipError_t run_forward
 template <typename D, int TPR, int NV, int GROUPS> static hipError_t run_backward(ResidualNormArgs a, hipStream_t st) {
     const int64_t workgroups = workgroups_of(a.rows, a.width);
     a.many = many_rows(a.rows, a.width);
+    a.whole = may_read_whole(a, {a.x, a.f, a.dh}, a.dx, a.df);
+    a.whole_too = may_read_whole(a, {a.dy}, a.dx, a.df);
     const bool bias = (a.post != LSP_NORM_NONE && a.post_b) || a.grads[1] || a.grads[4];
     const dim3 grid((unsigned)workgroups), block(TPR * GROUPS);
     if (a.drop.limit && bias) hipLaunchKernelGGL((k_residual_norm_back<D, TPR, NV, GROUPS, true, true>), grid, block, 0, st, a);
