@@ -47,7 +47,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
     for (int c = 0; c < kCols; ++c) o[c] = zeros16();
     float m = -INFINITY, l = 0.0f;
-    const float c2 = a.scale_log2, slack = kLagLog2<D> / c2;
+    const float c2 = a.scale_log2, slack = fminf(kLagLog2<D> / c2, 3e38f);    // (finite: the first maximum is above -infinity and it)
     const Reader<D, DP> read(lane);
     const uint8_t* kp = at<D>(a.k, b, 0, kv_head);
     const uint8_t* vp = at<D>(a.v, b, 0, kv_head);

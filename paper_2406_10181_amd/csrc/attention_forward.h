@@ -89,7 +89,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, D
 #pragma unroll
     for (int c = 0; c < kCols; ++c) o[c] = zeros16();
     float m = -INFINITY, l = 0.0f;                                                        // m: in the units of the scores; l: this lane's part
-    const float c2 = a.scale_log2, slack = kLagLog2<D> / c2;
+    const float c2 = a.scale_log2, slack = fminf(kLagLog2<D> / c2, 3e38f);    // (finite: the first maximum is above -infinity and it)
 
     const uint8_t* kp = at<D>(a.k, b, 0, kv_head);
     const uint8_t* vp = at<D>(a.v, b, 0, kv_head);
