@@ -408,7 +408,7 @@ int lsp_dropout(const void* x, void* y, int64_t rows, int64_t width, float dropo
  *                   16 bytes and a position's is below 8 MiB.  In O, dQ, dK and dV every row has a place of its own: the stride of an
  *                   axis is at least what the axes of smaller strides span; and none of them overlaps another operand
  *   L               device, [batch][heads][q_len] fp32
- *   head_dim        a multiple of 8, at most LSP_MAX_HEAD_DIM;  scale > 0;  batch * heads * (q_len or k_len) below 2^27
+ *   head_dim        a multiple of 8, at most LSP_MAX_HEAD_DIM;  scale > 0, at most 2^127;  batch * heads * (q_len or k_len) below 2^27
  *   and no launch of 2^24 workgroups or more: batch * heads * ceil(q_len / 128) below 2^24 (forward: batch * kv_heads, where the query heads of
  *   a key head have 128 rows or fewer together; backward: together with batch * kv_heads * ceil(k_len / 128))
  * The products run on the matrix cores in `dtype` with fp32 accumulation (fp32: in fp32); scores, softmax

@@ -88,6 +88,8 @@ size_t attention_backward_partial_bytes(const AttentionArgs& a) {
 
 namespace {
 
+constexpr float kLog2e = 1.44269504088896341f;
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool known(lsp_dtype t) { return t == LSP_F32 || t == LSP_F16 || t == LSP_BF16; }
 int elem_size(lsp_dtype t) { return t == LSP_F32 ? 4 : 2; }
@@ -141,7 +143,7 @@ int check_attention(const lsp_attention_problem* p, lsp_dtype t) {
     if (!p || !p->Q || !p->K || !p->V || !p->O || !p->L) return LSP_ERR_NULL;
     int rc = check_attention_shape(p, t);
     if (rc != LSP_OK) return rc;
-    if (!rate(p->dropout) || !(p->scale > 0.0f) || !std::isfinite(p->scale)) return LSP_ERR_VALUE;
+    if (!rate(p->dropout) || !(p->scale > 0.0f) || !std::isfinite(p->scale * kLog2e)) return LSP_ERR_VALUE;
     if ((rc = check_strides(p->q_stride, p->batch, p->q_len, p->heads, p->head_dim, t, false)) != LSP_OK) return rc;
     if ((rc = check_strides(p->k_stride, p->batch, p->k_len, p->kv_heads, p->head_dim, t, false)) != LSP_OK) return rc;
     if ((rc = check_strides(p->v_stride, p->batch, p->k_len, p->kv_heads, p->head_dim, t, false)) != LSP_OK) return rc;
@@ -161,7 +163,7 @@ lsp::AttentionArgs attention_args(const lsp_attention_problem* p) {
     a.q_lens = p->q_lens; a.k_lens = p->k_lens;
     a.batch = p->batch; a.heads = p->heads; a.kv_heads = p->kv_heads; a.group = p->heads / p->kv_heads;
     a.q_len = p->q_len; a.k_len = p->k_len; a.head_dim = p->head_dim; a.causal = p->causal;
-    a.scale = p->scale; a.scale_log2 = p->scale * 1.44269504088896341f;
+    a.scale = p->scale; a.scale_log2 = p->scale * kLog2e;
     a.drop = lsp::make_dropout(p->dropout, p->seed, p->offset);
     return a;
 }

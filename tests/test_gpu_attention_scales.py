@@ -2,7 +2,9 @@
 import pytest
 
 import operator_reference as ref
+import paper_2406_10181_amd as L
 from test_gpu_attention import Call, _against_reference, _check, _problem
+from test_operator_refusals import FAKE, attention, gradients
 
 
 @pytest.mark.gpu
@@ -24,3 +26,11 @@ def test_the_largest_scales(dtype):
     got = Call(dtype, Q, K, V, scale=scale).run()
     f = [t.double().numpy() for t in (Q, K, V)]
     _check(got, ref.attention(*f, dtype=dtype, scale=scale, causal=False), (dtype, scale))
+
+
+@pytest.mark.parametrize("scale", [2.4e38, 3.4e38])
+def test_scales_whose_powers_of_two_are_out_of_range(scale):
+    """CPU: the kernels take powers of two, of scale * log2(e)."""
+    p = attention(scale=scale)
+    assert L.lsp_attention_forward(p, 2, FAKE, 1 << 30, None, check=False) == -10
+    assert L.lsp_attention_backward(p, gradients(), 2, FAKE, 1 << 30, None, check=False) == -10
