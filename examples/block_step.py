@@ -28,7 +28,6 @@ class Block:
         assert heads % kv_heads == 0 and head_dim % 8 == 0
         self.batch, self.length, self.heads, self.kv_heads, self.head_dim, self.dropout, self.seed = batch, length, heads, kv_heads, head_dim, dropout, seed
         self.rows, self.width, self.hidden, self.dtype, self.code = batch * length, heads * head_dim, hidden, dtype, lsp.DTYPE_CODE[dtype]
-        self.stream = torch.cuda.current_stream()
         g = torch.Generator().manual_seed(seed)
         new = lambda *shape: torch.empty(*shape, dtype=DTYPE[dtype], device="cuda")
         joint = (heads + 2 * kv_heads) * head_dim
@@ -48,6 +47,11 @@ class Block:
         self.da, self.df, self.dh = (new(self.rows, self.width) for _ in range(3))
         self.k_lens = torch.full((batch,), length, dtype=torch.int32, device="cuda")
         self._describe()
+
+    @property
+    def stream(self):
+        """The stream of torch's products, whichever it is at the call."""
+        return torch.cuda.current_stream()
 
     def heads_of(self, joint):
         """Views of a joint projection [rows][...] as Q, K and V with heads."""
