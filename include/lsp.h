@@ -413,7 +413,9 @@ int lsp_dropout(const void* x, void* y, int64_t rows, int64_t width, float dropo
  *   a key head have 128 rows or fewer together; backward: together with batch * kv_heads * ceil(k_len / 128))
  * The products run on the matrix cores in `dtype` with fp32 accumulation (fp32: in fp32); scores, softmax
  * statistics and sums are fp32; probabilities and the gradients of the scores are rounded to `dtype` as
- * operands of the second products.  No atomics: results are the same bits from run to run.
+ * operands of the second products, and dO . O is made of O as it is stored.  So in 16 bits O and dV are 1.3 to 1.4
+ * times, dQ and dK 1.5 times as far from the exact ones as these rounded once; fp32 has no such roundings.  No
+ * atomics: results are the same bits from run to run.
  * The backward pass computes the probabilities again from Q, K and L; it needs the same problem with O and L
  * as the forward pass left them.  Non-finite elements of a row that counts reach the rows that see it, and may
  * reach others.

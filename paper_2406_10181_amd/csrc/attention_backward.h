@@ -20,7 +20,7 @@
 // the exact ones as results rounded once: 0.0025 of their norm in bf16, 0.0003 in fp16.
 //
 // Bound by the matrix cores, at the clock that they leave.  Four texts of 1024, 32 heads of 128, causal, bf16: 145 us, 120 GFLOP of seven products, 0.83 PFLOP/s (0.93 with what
-// the diagonal tiles make in vain); one of 8192, 16 heads: 840 to 915 us, 962 GFLOP, 1.05 to 1.15 PFLOP/s (a product of 8192 x 8192 matrices reaches 1.24).
+// the diagonal tiles make in vain); one of 8192, 16 heads: 800 to 915 us, 962 GFLOP, 1.05 to 1.2 PFLOP/s (a product of 8192 x 8192 matrices reaches 1.24 to 1.28).
 #pragma once
 
 #include <algorithm>

@@ -10,9 +10,9 @@
 // the second product, half a unit in the last place of each beside the result's own rounding (fp16: of those down to 2^-25 of the largest, see kTopLog2); their
 // sums, and L, are made before that.
 //
-// Heads of 128: bound by the matrix cores (one text of 8192, 16 heads, causal, bf16: 270 to 300 us, 275 GFLOP, 0.9 to 1.0 PFLOP/s; four of 1024, 32 heads: 52 us, 34 GFLOP).
+// Heads of 128: bound by the matrix cores (one text of 8192, 16 heads, causal, bf16: 255 to 300 us, 275 GFLOP, 0.9 to 1.1 PFLOP/s; four of 1024, 32 heads: 52 us, 34 GFLOP).
 // Heads of 64: by exponentials and what else a score takes outside the matrix cores, a quarter-rate instruction and four others for 256 operations of theirs (16 heads, eight texts
-// of 2048, fp16: 182 us, 137 GFLOP, 0.76 PFLOP/s; the vector units issue 70 % of the time, the matrix cores work 40 %).
+// of 2048, fp16: 167 to 182 us, 137 GFLOP, 0.76 to 0.82 PFLOP/s; the vector units issue 70 % of the time, the matrix cores work 40 %).
 #pragma once
 
 #include "attention_few.h"

@@ -6,8 +6,6 @@
 // depend on how the others lie; where rows begin off the 16-byte steps the loads are unaligned ones, and the last block of a row
 // goes in pieces of four, two and one.
 //
-// Bound by memory: 4096 x 11008 bf16, 180 MB, 30 us, 6.0 TB/s; the generator's 28 products of 32 bits for eight elements hide behind it.
-//
 // Bound by memory: 4096 x 11008 bf16, 180 MB, 30 us, 6.0 TB/s (the generator's 28 products of 32 bits for eight elements hide behind it).
 #include "philox.h"
 #include "rows.h"

@@ -164,7 +164,8 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 }
 
 // The training operators.  Their descriptors are C structures that the binding has as ctypes objects; here they are filled from torch tensors (7.7 us for the
-// residual norm's in Python, 1.4 here), with the checks that only the tensors allow: shapes and types that belong together, contiguous last axes.
+// residual norm's in Python, 3.7 here with three vectors; attention's 4.2, with lengths 4.5), with the checks that only the tensors allow: shapes, types and devices that belong
+// together, contiguous last axes.
 
 // What a tensor says of itself; false with a Python exception set
 struct Tensor {
