@@ -60,7 +60,7 @@ typedef enum {
     LSP_ERR_ALIGN     = -7,  /* a base pointer is not 16-byte aligned */
     LSP_ERR_SKEW      = -8,  /* lsp_plan_build: the columns of Q are used too unevenly for a plan; use lsp_compress */
     LSP_ERR_TOO_LARGE = -9,  /* lsp_compress_planned_static: the problem needs more than LSP_STATIC_SCRATCH_BYTES of scratch */
-    LSP_ERR_VALUE     = -10  /* a number is out of its range: a dropout not in [0, 1), a scale that is not finite, a negative eps */
+    LSP_ERR_VALUE     = -10  /* a number is out of its range: a dropout, a beta or a smoothing not in [0, 1), a scale that is not finite, a negative eps */
 } lsp_status;
 
 #define LSP_MAX_R 2048       /* largest supported subspace size (the paper's largest setting) */
@@ -69,6 +69,7 @@ typedef enum {
 #define LSP_MAX_HEAD_DIM 128 /* widest head of the attention calls */
 #define LSP_MAX_WIDTH 8192   /* longest row of the residual-norm calls */
 #define LSP_MAX_ROWS (1 << 22)   /* most rows of one residual-norm call */
+#define LSP_MAX_TENSORS (1 << 16)    /* most tensors of one optimizer step */
 #define LSP_STATIC_SCRATCH_BYTES (24u << 20)   /* scratch held inside the library image, per GPU (lsp_compress_planned_static) */
 
 /* ------------------------------------------------------------------------------------------
@@ -504,6 +505,142 @@ int    lsp_residual_norm_forward(const lsp_residual_norm_problem* problem, lsp_d
 size_t lsp_residual_norm_backward_workspace_bytes(const lsp_residual_norm_problem* problem, lsp_dtype dtype);
 int    lsp_residual_norm_backward(const lsp_residual_norm_problem* problem, const lsp_residual_norm_gradients* gradients, lsp_dtype dtype,
                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rotary positions with norms of the heads, between the joint projection and attention:
+ *   Qr = rotate(norm(Q)),  Kr = rotate(norm(K)),  and, where it is asked for, Vr = V,
+ * each head of each token by itself.  norm: lsp_norm over the head_dim elements of a head, with weight [+ bias] as below (LSP_NORM_NONE: not
+ * read).  rotate: pair j < rotated / 2 of a head turns by the angle position * frequencies[j],
+ *   (a, b) -> (a cos - b sin, a sin + b cos);   elements from `rotated` on stay.
+ * A pair is elements (j, rotated / 2 + j) or, with neighbours = 1, (2 j, 2 j + 1).  Angles are computed in fp64 (a far position keeps all
+ * digits), their sines, the norms and the turning in fp32; the result is rounded once.
+ * Token i of text b counts when i < lens[b] (lengths outside [0, length] are taken as the nearer end; NULL: all count).  Its position is
+ * positions[b][i] or, where that is NULL, starts[b] + i (starts NULL: i).  Its key goes to place starts[b] + i of the text's `cache` places in Kr, and its
+ * value there in Vr, so that the caches that lsp_attention_forward reads are filled by the call that turns the keys (cache = length and starts =
+ * NULL: tensors like K).  Tokens that do not count are not read, and their rows not written; nor are places outside [0, cache).
+ *   Q, Qr, dQr, dQ  device, [batch][length][heads][head_dim] of `dtype`; K, V, dK  [batch][length][kv_heads][head_dim];
+ *   Kr, Vr, dKr     [batch][cache][kv_heads][head_dim]; each with strides as in attention (multiples of 16 bytes, a position's below 8 MiB; in what
+ *                   is written every row has a place of its own).  V and Vr may be NULL, both.
+ *   Qr may be Q and, where starts is NULL, Kr may be K and Vr V, row on row.  Otherwise what is written overlaps nothing else.
+ *   q_weight, k_weight, q_bias, k_bias   device, [head_dim] of `dtype`; NULL: ones, zeros
+ *   frequencies     device, [rotated / 2] fp32, radians a position; NULL only where rotated = 0
+ *   head_dim, rotated   multiples of 8, rotated <= head_dim <= LSP_MAX_HEAD_DIM;  batch * length * (heads + 2 kv_heads) below 2^31
+ * The backward pass gives dQ and dK from dQr and dKr (of tokens that do not count zeros, without reading anything; a key whose place is outside the
+ * cache has gradient zero) and, where asked for (not NULL), the gradients of weights and biases (fp32, [head_dim], overwritten; sums over tokens and
+ * heads in an order that does not change from run to run).  It needs Q and K as the forward pass had them where there is a norm (so Qr and Kr may
+ * not be on them then).  dQ may be dQr or Q, row on row, and, where starts is NULL, dK may be dKr or K. */
+typedef struct {
+    const void*    Q;
+    const void*    K;
+    const void*    V;
+    void*          Qr;
+    void*          Kr;
+    void*          Vr;
+    const void*    q_weight;
+    const void*    k_weight;
+    const void*    q_bias;
+    const void*    k_bias;
+    const float*   frequencies;
+    const int32_t* positions;      /* device, [batch][length], or NULL */
+    const int32_t* starts;         /* device, [batch], or NULL */
+    const int32_t* lens;
+    int64_t q_stride[3], k_stride[3], v_stride[3], qr_stride[3], kr_stride[3], vr_stride[3];   /* batch, position, head */
+    int32_t batch, length, cache, heads, kv_heads, head_dim, rotated;
+    int32_t neighbours;            /* 0 or 1 */
+    int32_t norm;                  /* lsp_norm */
+    float   eps;
+} lsp_rotary_problem;
+
+typedef struct {
+    const void* dQr;
+    const void* dKr;
+    void*       dQ;
+    void*       dK;
+    float*      q_weight;
+    float*      k_weight;
+    float*      q_bias;
+    float*      k_bias;
+    int64_t dqr_stride[3], dkr_stride[3], dq_stride[3], dk_stride[3];
+} lsp_rotary_gradients;
+
+int    lsp_rotary_forward(const lsp_rotary_problem* problem, lsp_dtype dtype, void* stream);
+size_t lsp_rotary_backward_workspace_bytes(const lsp_rotary_problem* problem, lsp_dtype dtype);
+int    lsp_rotary_backward(const lsp_rotary_problem* problem, const lsp_rotary_gradients* gradients, lsp_dtype dtype,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Softmax cross entropy over a vocabulary, from the last hidden states:  z = H W^T (never stored),
+ *   L = log(sum over the vocabulary of exp(z)),
+ *   losses = L - (1 - smoothing) z[target] - smoothing mean(z) + z_loss L^2,  row by row.
+ * A row whose target is outside [0, vocab) does not count: it is not read, its loss and L are 0, and it gets and gives no gradient.
+ *   H        device, [rows][width] of `dtype`;  W  [vocab][width]; with row strides (elements), multiples of 16 bytes below 8 MiB
+ *   targets  device, [rows] int64
+ *   losses   device, [rows] fp32;  logs: the same for L, or NULL
+ *   width    a multiple of 8, at most 2^16;  rows at most LSP_MAX_ROWS;  vocab at most 2^20;  0 <= smoothing < 1;  0 <= z_loss <= 1
+ * lsp_cross_entropy_backward gives losses and logs too (it needs no forward call before it), and the gradients of
+ *   scale * sum over the rows of weights * losses
+ * with respect to H (dH, rows that do not count: zeros) and W (dW), overwritten; either may be NULL.  weights: device, [rows] fp32, or NULL: ones (of rows that
+ * do not count not used); scale is finite.
+ * The products run on the matrix cores in `dtype` with fp32 accumulation (fp32: in fp32).  Rows are taken in blocks; for a block the
+ * exponentials are kept in `dtype`, each relative to the largest of its row in a piece of the vocabulary, and become the gradient of z in place: two roundings
+ * in 16 bits before the second products, the largest gradient of a row being computed without them (a target's).  No atomics that add: results are the same
+ * bits from run to run.  A logit that is not finite reaches its row's loss and dH, and all of dW.
+ * Workspaces: 16-byte aligned, as large as the queries say; a bounded size however many rows there are. */
+typedef struct {
+    const void*    H;
+    const void*    W;
+    const int64_t* targets;
+    float*         losses;
+    float*         logs;
+    int64_t h_stride, w_stride;
+    int64_t rows;
+    int32_t width, vocab;
+    float   smoothing, z_loss;
+} lsp_cross_entropy_problem;
+
+typedef struct {
+    void*        dH;
+    void*        dW;
+    const float* weights;
+    int64_t dh_stride, dw_stride;
+    float   scale;
+} lsp_cross_entropy_gradients;
+
+size_t lsp_cross_entropy_forward_workspace_bytes(const lsp_cross_entropy_problem* problem, lsp_dtype dtype);
+int    lsp_cross_entropy_forward(const lsp_cross_entropy_problem* problem, lsp_dtype dtype, void* workspace, size_t workspace_bytes, void* stream);
+size_t lsp_cross_entropy_backward_workspace_bytes(const lsp_cross_entropy_problem* problem, lsp_dtype dtype);
+int    lsp_cross_entropy_backward(const lsp_cross_entropy_problem* problem, const lsp_cross_entropy_gradients* gradients, lsp_dtype dtype,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* One step of AdamW (Loshchilov and Hutter, "Decoupled weight decay regularization", ICLR 2019) over many tensors, for the parameters that have no projector:
+ *   g = grad_scale grad,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   param -= rate * rate_factor * (decay param + (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)),   all in fp32, in place.
+ * Each tensor has its own types, decay and factor of the rate.  Where there is a master (fp32), it is what is updated, and param becomes it rounded; otherwise
+ * param itself is read and rounded once.
+ * LSP_STATE_F32: m and v are fp32.  LSP_STATE_8BIT: bytes; 256 elements that follow one another (the last ones of a tensor: fewer) share an fp32 scale.  m is e4m3 (4 bits
+ * of exponent, 3 of mantissa, largest 448) times m_scale; v is without sign, 5 bits of exponent and 3 of mantissa: code 0 is 0 and code c otherwise
+ * 2^((c >> 3) - 31) * (1 + (c & 7) / 8) (largest 1.875), times v_scale.  The step takes m and v before they are rounded (to nearest, ties to even; a v
+ * that is not 0 never becomes 0, so that no small v makes a large step); a scale is the block's largest magnitude over 448 or 1.875.  State that is all zeros,
+ * codes and scales, is where training begins.  A gradient that is not finite spoils its element and, in 8 bits, can spoil its block's states.
+ *   items       HOST array of `count` descriptors, 1 <= count <= LSP_MAX_TENSORS, read during the call only; no tensor twice, no overlaps
+ *   step        number of this step, from 1 on (a captured call repeats it);  0 <= beta < 1, eps >= 0
+ *   grad_scale  device, one fp32 (of clipping, or of a scaled loss), or NULL: 1.  Where it is not finite the step does nothing
+ * At most 2^35 elements a call, all tensors padded to 2048. */
+typedef enum { LSP_STATE_F32 = 0, LSP_STATE_8BIT = 1 } lsp_state;
+
+typedef struct {
+    void*       param;             /* device, [elements] of `dtype` */
+    const void* grad;              /* device, [elements] of `grad_dtype` */
+    void*       m;                 /* device, [elements] fp32, or bytes */
+    void*       v;
+    float*      m_scale;           /* device, [ceil(elements / 256)]; LSP_STATE_8BIT only */
+    float*      v_scale;
+    float*      master;            /* device, [elements] fp32, or NULL */
+    int64_t     elements;
+    float       rate_factor, decay;
+    int32_t     dtype, grad_dtype; /* lsp_dtype */
+} lsp_adamw_item;
+
+int lsp_adamw(const lsp_adamw_item* items, int32_t count, lsp_state states, double rate, double beta1, double beta2, double eps, int64_t step,
+              const float* grad_scale, void* stream);
 
 /* ------------------------------------------------------------------------------------------
  * Utilities.

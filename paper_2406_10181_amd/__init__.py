@@ -1,7 +1,8 @@
 """MI355X (gfx950) library for the GPU hot path of LSP-Offload: compress S = P^T G Q and
 decompress-and-apply W <- W - P S Q^T with (d,r)-sparse ELL projectors (Alg. 1 / Alg. 3, Def. 1),
 and the estimation bias of Def. 2 built from the two.  Beside them the operators of a training step that are no plain
-matrix products: attention with its backward pass, the norms and the gated residual between two blocks, and dropout.
+matrix products: attention with its backward pass, the norms and the gated residual between two blocks, dropout, the rotation of queries and
+keys by position with the norms of their heads, the cross entropy over a vocabulary with its gradients, and AdamW for what has no projector.
 
 This package is a thin binding: it marshals torch device pointers into the C ABI declared in
 ``include/lsp.h``.  Every step of the path runs in the HIP kernels of ``liblsp_hip.so``; there is
@@ -21,4 +22,8 @@ from .binding import (  # noqa: F401
     lsp_attention_forward, lsp_attention_forward_workspace_bytes, lsp_attention_backward, lsp_attention_backward_workspace_bytes,
     lsp_residual_norm_problem, lsp_residual_norm_gradients, residual_norm_problem, residual_norm_gradients,
     lsp_residual_norm_forward, lsp_residual_norm_backward, lsp_residual_norm_backward_workspace_bytes,
+    lsp_rotary_problem, lsp_rotary_gradients, rotary_problem, rotary_gradients, lsp_rotary_forward, lsp_rotary_backward, lsp_rotary_backward_workspace_bytes,
+    lsp_cross_entropy_problem, lsp_cross_entropy_gradients, cross_entropy_problem, cross_entropy_gradients, lsp_cross_entropy_forward,
+    lsp_cross_entropy_forward_workspace_bytes, lsp_cross_entropy_backward, lsp_cross_entropy_backward_workspace_bytes,
+    lsp_adamw_item, AdamwItems, adamw_items, lsp_adamw,
 )

@@ -62,6 +62,36 @@ class lsp_residual_norm_gradients(ctypes.Structure):
                 ("dy_stride", ctypes.c_int64), ("dh_stride", ctypes.c_int64), ("dx_stride", ctypes.c_int64), ("df_stride", ctypes.c_int64)]
 
 
+class lsp_rotary_problem(ctypes.Structure):
+    """What both rotary calls take (field for field the C struct)."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("Q", "K", "V", "Qr", "Kr", "Vr", "q_weight", "k_weight", "q_bias", "k_bias", "frequencies", "positions", "starts", "lens")] + \
+               [(n, _three) for n in ("q_stride", "k_stride", "v_stride", "qr_stride", "kr_stride", "vr_stride")] + \
+               [(n, ctypes.c_int32) for n in ("batch", "length", "cache", "heads", "kv_heads", "head_dim", "rotated", "neighbours", "norm")] + [("eps", ctypes.c_float)]
+
+
+class lsp_rotary_gradients(ctypes.Structure):
+    """What lsp_rotary_backward takes besides (field for field the C struct)."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dQr", "dKr", "dQ", "dK", "q_weight", "k_weight", "q_bias", "k_bias")] + \
+               [(n, _three) for n in ("dqr_stride", "dkr_stride", "dq_stride", "dk_stride")]
+
+
+class lsp_cross_entropy_problem(ctypes.Structure):
+    """What both cross-entropy calls take (field for field the C struct)."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("H", "W", "targets", "losses", "logs")] + [(n, ctypes.c_int64) for n in ("h_stride", "w_stride", "rows")] + \
+               [("width", ctypes.c_int32), ("vocab", ctypes.c_int32), ("smoothing", ctypes.c_float), ("z_loss", ctypes.c_float)]
+
+
+class lsp_cross_entropy_gradients(ctypes.Structure):
+    """What lsp_cross_entropy_backward takes besides (field for field the C struct)."""
+    _fields_ = [("dH", ctypes.c_void_p), ("dW", ctypes.c_void_p), ("weights", ctypes.c_void_p), ("dh_stride", ctypes.c_int64), ("dw_stride", ctypes.c_int64), ("scale", ctypes.c_float)]
+
+
+class lsp_adamw_item(ctypes.Structure):
+    """One tensor of lsp_adamw (field for field the C struct)."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "m", "v", "m_scale", "v_scale", "master")] + \
+               [("elements", ctypes.c_int64), ("rate_factor", ctypes.c_float), ("decay", ctypes.c_float), ("dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32)]
+
+
 # What attention_problem() and its like return: behind the C struct's fields what the call compares with its other arguments (field for field what the call module fills).
 _four = ctypes.c_int64 * 4
 
@@ -80,6 +110,22 @@ class _ResidualNormOfTensors(lsp_residual_norm_problem):
 
 class _ResidualNormGradientsOfTensors(lsp_residual_norm_gradients):
     _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class _RotaryOfTensors(lsp_rotary_problem):
+    _fields_ = [("dtype", ctypes.c_int32)]
+
+
+class _RotaryGradientsOfTensors(lsp_rotary_gradients):
+    _fields_ = [("q_shape", _four), ("k_shape", _four), ("kr_shape", _four), ("dtype", ctypes.c_int32)]
+
+
+class _CrossEntropyOfTensors(lsp_cross_entropy_problem):
+    _fields_ = [("dtype", ctypes.c_int32)]
+
+
+class _CrossEntropyGradientsOfTensors(lsp_cross_entropy_gradients):
+    _fields_ = [("h_shape", ctypes.c_int64 * 2), ("w_shape", ctypes.c_int64 * 2), ("weights_count", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
 
 NORM_KIND = {"none": 0, "rms": 1, "layer": 2}
@@ -170,7 +216,8 @@ def lib() -> ctypes.CDLL:
         L.lsp_validate_projector.restype = ctypes.c_int
         L.lsp_dropout.argtypes = [vp, vp, i64, i64, ctypes.c_float, ctypes.c_uint64, ctypes.c_uint32, i32, vp]
         L.lsp_dropout.restype = ctypes.c_int
-        for name in ("lsp_attention_forward_workspace_bytes", "lsp_attention_backward_workspace_bytes", "lsp_residual_norm_backward_workspace_bytes"):
+        for name in ("lsp_attention_forward_workspace_bytes", "lsp_attention_backward_workspace_bytes", "lsp_residual_norm_backward_workspace_bytes",
+                     "lsp_rotary_backward_workspace_bytes", "lsp_cross_entropy_forward_workspace_bytes", "lsp_cross_entropy_backward_workspace_bytes"):
             getattr(L, name).argtypes = [vp, i32]
             getattr(L, name).restype = sz
         L.lsp_attention_forward.argtypes = [vp, i32, vp, sz, vp]
@@ -181,6 +228,13 @@ def lib() -> ctypes.CDLL:
         L.lsp_residual_norm_forward.restype = ctypes.c_int
         L.lsp_residual_norm_backward.argtypes = [vp, vp, i32, vp, sz, vp]
         L.lsp_residual_norm_backward.restype = ctypes.c_int
+        for name, forward in (("lsp_rotary", [vp, i32, vp]), ("lsp_cross_entropy", [vp, i32, vp, sz, vp])):
+            getattr(L, name + "_forward").argtypes = forward
+            getattr(L, name + "_forward").restype = ctypes.c_int
+            getattr(L, name + "_backward").argtypes = [vp, vp, i32, vp, sz, vp]
+            getattr(L, name + "_backward").restype = ctypes.c_int
+        L.lsp_adamw.argtypes = [vp, i32, i32] + [ctypes.c_double] * 4 + [i64, vp, vp]
+        L.lsp_adamw.restype = ctypes.c_int
         L.lsp_strerror.argtypes = [ctypes.c_int]
         L.lsp_strerror.restype = ctypes.c_char_p
         L.lsp_last_hip_error.restype = ctypes.c_int
@@ -463,9 +517,12 @@ def _operator_calls():
     if _operators is None:
         L, module = lib(), _bound()
         module.bind_operators(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
-            L.lsp_dropout, L.lsp_attention_forward, L.lsp_attention_backward, L.lsp_residual_norm_forward, L.lsp_residual_norm_backward)),
-            lsp_attention_problem, lsp_attention_gradients, lsp_residual_norm_problem, lsp_residual_norm_gradients,
-            _AttentionOfTensors, _AttentionGradientsOfTensors, _ResidualNormOfTensors, _ResidualNormGradientsOfTensors)
+            L.lsp_dropout, L.lsp_attention_forward, L.lsp_attention_backward, L.lsp_residual_norm_forward, L.lsp_residual_norm_backward, L.lsp_rotary_forward,
+            L.lsp_rotary_backward, L.lsp_cross_entropy_forward, L.lsp_cross_entropy_backward)),
+            lsp_attention_problem, lsp_attention_gradients, lsp_residual_norm_problem, lsp_residual_norm_gradients, lsp_rotary_problem, lsp_rotary_gradients,
+            lsp_cross_entropy_problem, lsp_cross_entropy_gradients,
+            _AttentionOfTensors, _AttentionGradientsOfTensors, _ResidualNormOfTensors, _ResidualNormGradientsOfTensors, _RotaryOfTensors, _RotaryGradientsOfTensors,
+            _CrossEntropyOfTensors, _CrossEntropyGradientsOfTensors)
         _operators = module
     return _operators
 
@@ -563,4 +620,142 @@ def lsp_residual_norm_backward(problem, gradients, dtype: int, workspace, worksp
     rc = (_operators or _operator_calls()).residual_norm_backward(problem, gradients, dtype, workspace, workspace_bytes, stream)
     if check and rc:
         _check(rc, "lsp_residual_norm_backward")
+    return rc
+
+
+def rotary_problem(Q, K, Qr, Kr, *, V=None, Vr=None, frequencies=None, neighbours: bool = False, positions=None, starts=None, lens=None, norm: str = "none",
+                   q_weight=None, k_weight=None, q_bias=None, k_bias=None, eps: float = 1e-5) -> lsp_rotary_problem:
+    """The descriptor of a rotary call from torch tensors: Q, Qr [batch][length][heads][head_dim], K and V [batch][length][kv_heads][head_dim], Kr and Vr
+    [batch][cache][kv_heads][head_dim] with any strides whose last is 1; frequencies [rotated / 2] fp32 (None: nothing turns), positions [batch][length], starts
+    and lens [batch] int32 or None; norm is "none", "rms" or "layer".  Tensors that do not belong together are a ValueError.  They are kept alive by the caller."""
+    p = _RotaryOfTensors()
+    (_operators or _operator_calls()).rotary_problem(ctypes.addressof(p), Q, K, V, Qr, Kr, Vr, q_weight, k_weight, q_bias, k_bias, frequencies, positions, starts, lens,
+                                                     neighbours, NORM_KIND[norm], eps)
+    return p
+
+
+def rotary_gradients(dQr, dKr, dQ, dK, *, q_weight=None, k_weight=None, q_bias=None, k_bias=None) -> lsp_rotary_gradients:
+    """The gradients' descriptor: dQr and dKr, shaped as Qr and Kr, arrive; dQ and dK, shaped as Q and K, are made, and the fp32 [head_dim] gradients that are asked for."""
+    g = _RotaryGradientsOfTensors()
+    (_operators or _operator_calls()).rotary_gradients(ctypes.addressof(g), dQr, dKr, dQ, dK, q_weight, k_weight, q_bias, k_bias)
+    return g
+
+
+def lsp_rotary_forward(problem, dtype: int, stream=None, check: bool = True) -> int:
+    """problem: from rotary_problem(), of tensors of `dtype` (else a ValueError)."""
+    rc = (_operators or _operator_calls()).rotary_forward(problem, dtype, stream)
+    if check and rc:
+        _check(rc, "lsp_rotary_forward")
+    return rc
+
+
+def lsp_rotary_backward_workspace_bytes(problem, dtype: int) -> int:
+    return lib().lsp_rotary_backward_workspace_bytes(ctypes.byref(problem), dtype)
+
+
+def lsp_rotary_backward(problem, gradients, dtype: int, workspace=None, workspace_bytes: int = 0, stream=None, check: bool = True) -> int:
+    """gradients: from rotary_gradients(), shaped as the problem's tensors and of `dtype`, as these (else a ValueError)."""
+    rc = (_operators or _operator_calls()).rotary_backward(problem, gradients, dtype, workspace, workspace_bytes, stream)
+    if check and rc:
+        _check(rc, "lsp_rotary_backward")
+    return rc
+
+
+def cross_entropy_problem(H, W, targets, losses, *, logs=None, smoothing: float = 0.0, z_loss: float = 0.0) -> lsp_cross_entropy_problem:
+    """The descriptor of a cross-entropy call from torch tensors: H [rows][width], W [vocab][width], targets [rows] int64 (outside the vocabulary: the row does not count),
+    losses and logs [rows] fp32.  Tensors that do not belong together are a ValueError.  They are kept alive by the caller."""
+    p = _CrossEntropyOfTensors()
+    (_operators or _operator_calls()).cross_entropy_problem(ctypes.addressof(p), H, W, targets, losses, logs, smoothing, z_loss)
+    return p
+
+
+def cross_entropy_gradients(dH, dW, *, weights=None, scale: float = 1.0) -> lsp_cross_entropy_gradients:
+    """The gradients' descriptor: dH and dW, shaped as H and W (one may be None), of scale * sum(weights * losses); weights [rows] fp32 or None."""
+    g = _CrossEntropyGradientsOfTensors()
+    (_operators or _operator_calls()).cross_entropy_gradients(ctypes.addressof(g), dH, dW, weights, scale)
+    return g
+
+
+def lsp_cross_entropy_forward_workspace_bytes(problem, dtype: int) -> int:
+    return lib().lsp_cross_entropy_forward_workspace_bytes(ctypes.byref(problem), dtype)
+
+
+def lsp_cross_entropy_backward_workspace_bytes(problem, dtype: int) -> int:
+    return lib().lsp_cross_entropy_backward_workspace_bytes(ctypes.byref(problem), dtype)
+
+
+def lsp_cross_entropy_forward(problem, dtype: int, workspace, workspace_bytes: int, stream=None, check: bool = True) -> int:
+    """problem: from cross_entropy_problem(), of tensors of `dtype` (else a ValueError).  The losses alone."""
+    rc = (_operators or _operator_calls()).cross_entropy_forward(problem, dtype, workspace, workspace_bytes, stream)
+    if check and rc:
+        _check(rc, "lsp_cross_entropy_forward")
+    return rc
+
+
+def lsp_cross_entropy_backward(problem, gradients, dtype: int, workspace, workspace_bytes: int, stream=None, check: bool = True) -> int:
+    """The losses and their gradients, in one call; gradients: from cross_entropy_gradients(), shaped as the problem's tensors and of `dtype`, as these (else a ValueError)."""
+    rc = (_operators or _operator_calls()).cross_entropy_backward(problem, gradients, dtype, workspace, workspace_bytes, stream)
+    if check and rc:
+        _check(rc, "lsp_cross_entropy_backward")
+    return rc
+
+
+STATE_KIND = {"f32": 0, "8bit": 1}
+
+
+class AdamwItems:
+    """HOST array of lsp_adamw_item (`array`) with what the call needs to know of all of them."""
+
+    def __init__(self, array, states: str):
+        self.array, self.states = array, states
+
+
+def adamw_items(tensors) -> AdamwItems:
+    """What lsp_adamw updates, from a list of dicts: param and grad, m and v (both float32, or both of one byte an element: states in 8 bits, with m_scale and v_scale, float32,
+    one for 256 elements), optionally master (float32), rate_factor (1) and decay (0).  Tensors are contiguous, of one size and on one device; others are a
+    ValueError.  They are kept alive by the caller, and the array serves as long as they are where they are."""
+    import torch
+    code = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+    array, kinds, devices, seen = (lsp_adamw_item * len(tensors))(), set(), set(), set()
+
+    def need(ok, what):
+        if not ok:
+            raise ValueError(f"adamw_items: {what}")
+
+    need(len(tensors) > 0, "tensors are wanted")
+    for k, t in enumerate(tensors):
+        need(not set(t) - {"param", "grad", "m", "v", "m_scale", "v_scale", "master", "rate_factor", "decay"}, "unknown names")
+        param, grad, m, v, master = t["param"], t["grad"], t["m"], t["v"], t.get("master")
+        bits8 = m.element_size() == 1
+        kinds.add("8bit" if bits8 else "f32")
+        need(param.dtype in code and grad.dtype in code, "param and grad are float32, float16 or bfloat16")
+        need(m.element_size() == v.element_size() and (bits8 or m.dtype == v.dtype == torch.float32), "m and v are both float32 or both of one byte an element")
+        need(master is None or master.dtype == torch.float32, "master is float32")
+        n = param.numel()
+        need(n > 0 and all(x is None or x.numel() == n for x in (grad, m, v, master)), "param, grad, m, v and master are of one size")
+        scales = [t.get("m_scale"), t.get("v_scale")]
+        if bits8:
+            need(all(x is not None and x.dtype == torch.float32 and x.numel() == (n + 255) // 256 for x in scales), "m_scale and v_scale are float32, one for 256 elements")
+        else:
+            need(scales == [None, None], "scales belong to states in 8 bits")
+        there = [x for x in (param, grad, m, v, master, *scales) if x is not None]
+        need(all(x.is_contiguous() for x in there), "tensors are contiguous")
+        devices.update(x.get_device() for x in there)
+        written = [x.data_ptr() for x in there if x is not grad]
+        need(not seen & set(written) and len(set(written)) == len(written), "a tensor appears twice")
+        seen.update(written)
+        array[k] = lsp_adamw_item(param.data_ptr(), grad.data_ptr(), m.data_ptr(), v.data_ptr(), *(None if x is None else x.data_ptr() for x in (*scales, master)), n,
+                                  t.get("rate_factor", 1.0), t.get("decay", 0.0), code[param.dtype], code[grad.dtype])
+    need(len(kinds) == 1, "states are all in fp32 or all in 8 bits")
+    need(len(devices) == 1, "the tensors are on one device")
+    return AdamwItems(array, kinds.pop())
+
+
+def lsp_adamw(items: AdamwItems, *, rate: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step: int, grad_scale=None, stream=None, check: bool = True) -> int:
+    """items: from adamw_items(); step counts from 1; grad_scale: one float32 on the device, or None."""
+    if grad_scale is not None and hasattr(grad_scale, "numel") and (grad_scale.numel() != 1 or grad_scale.element_size() != 4 or not grad_scale.is_floating_point()):
+        raise ValueError("lsp_adamw: grad_scale is one float32")
+    rc = lib().lsp_adamw(items.array, len(items.array), STATE_KIND[items.states], rate, beta1, beta2, eps, step, _ptr(grad_scale), _stream(stream))
+    if check and rc:
+        _check(rc, "lsp_adamw")
     return rc

@@ -18,6 +18,7 @@ CALL_MODULE = os.path.join(PKG, "_call" + sysconfig.get_config_var("EXT_SUFFIX")
 OBJDIR = os.path.join(PKG, "_build")
 SOURCES = ["attention_backward_bf16.hip", "attention_backward_f16.hip", "attention_backward_f32.hip",
            "attention_forward_bf16.hip", "attention_forward_f16.hip", "attention_forward_f32.hip",
+           "cross_entropy_bf16.hip", "cross_entropy_f16.hip", "cross_entropy_f32.hip", "rotary.hip", "cross_entropy.hip", "adamw.hip", "training.cpp",
            "residual_norm.hip", "dropout.hip", "operators.cpp", "compress_mm.hip", "compress_gq_bf16.hip", "compress_gq_f16.hip", "compress_gq_f32.hip", "plan_device.hip",
            "decompress_bf16.hip", "decompress_f16.hip", "decompress_f32.hip", "decompress_loose_bf16.hip", "decompress_loose_f16.hip", "decompress_loose_f32.hip", "decompress.hip",
            "compress.hip", "api.cpp", "plan.cpp", "reproject.hip", "dense.hip", "fitgrad.hip", "noalloc.hip", "probe.hip"]

@@ -1,0 +1,254 @@
+// Arguments of the cross-entropy kernels, and the kernels with products in them (instantiated for each type in cross_entropy_{bf16,f16,f32}.hip; the others are in
+// cross_entropy.hip).
+//
+// A block of rows goes through six kernels.  k_loss_pack copies the rows of H that count, one behind the other, so that rows that do not count cost nothing and are not
+// read.  k_loss_logits multiplies W by them; z[v][row] is in registers with the row across lanes and a piece of the vocabulary (a wave's part of the tile)
+// in the lane's registers, so that a piece's maximum and sum of exponentials take no LDS.  The exponentials, relative to the piece's maximum, are stored in the storage type: whatever
+// the size of z they keep its digits, where z itself in 16 bits would be off by a hundredth of a unit and p by a percent.  k_loss_rows makes the rows' L and losses of
+// the pieces; k_loss_dz turns the exponentials into the gradient of z in place; k_loss_dh and k_loss_dw multiply that by W and by H.
+//
+// 6 rows width vocab operations in all: keeping 16 bits an exponential, 2 bytes written, read, written and read twice, costs less than a second product
+// would.  The blocks are as large as kLossBytes allows, and where there are several, dW is added up in fp32.
+#pragma once
+
+#include "matmul.h"
+
+namespace lsp {
+
+constexpr size_t kLossBytes = (size_t)1 << 30;    // of exponentials, at most (but for one tile of rows)
+
+struct LossArgs {
+    const void *H, *W;
+    const int64_t* targets;
+    const float* weights;
+    float *losses, *logs;
+    void *dH, *dW;
+    int64_t h_stride, w_stride, dh_stride, dw_stride;
+    int64_t rows;
+    int32_t width, vocab;
+    float smoothing, z_loss, scale;
+    // workspace
+    int32_t* count;              // [4]: rows that count; bits of the largest gradient factor; two of padding
+    int32_t* index;              // [rows]: which they are
+    uint8_t* packed;             // [block_rows][width] of the storage type: the block's rows
+    int32_t* target;             // [block_rows]
+    float *top, *sum, *plain;    // [pieces][block_rows]: a piece's maximum, sum of exponentials, sum of z (with smoothing only)
+    float *hit;                  // [block_rows]: z[target]
+    float *log_sum;              // [block_rows]: L
+    float *factor;               // [block_rows]: scale * weight
+    uint8_t* e;                  // [block_rows][padded]
+    float* dh_parts;             // [dh_splits][block_rows][width], where there are several
+    float* dw_sum;               // [vocab][width], where there are several blocks of rows and dW is not fp32
+    // plan
+    int32_t block_rows, padded;  // multiples of 256
+    int32_t blocks, block;       // blocks of rows, and which this is
+    int32_t pieces, piece;       // pieces of the vocabulary, of so many
+    int32_t tile[3];             // 256, 128 or 64: of the logits, dH, dW
+    int32_t dh_splits;
+    int32_t train;
+};
+
+void plan_loss(LossArgs& a, lsp_dtype dtype);
+size_t loss_workspace(LossArgs& a, lsp_dtype dtype, uint8_t* base);     // the bytes; places the pieces where base is not NULL
+hipError_t launch_loss(LossArgs& a, lsp_dtype dtype, hipStream_t st);
+
+template <typename D> hipError_t launch_loss_logits(const LossArgs& a, hipStream_t st);
+template <typename D> hipError_t launch_loss_dh(const LossArgs& a, hipStream_t st);
+template <typename D> hipError_t launch_loss_dw(const LossArgs& a, hipStream_t st);
+
+#if defined(__HIPCC__)
+constexpr float kLossLog2e = 1.44269504088896341f;
+// fp16: an exponential counts as 2^15 at the top, so that what is 2^-29 of the largest still has all its digits
+template <typename D> constexpr float kLossTop = std::is_same<D, F16>::value ? 32768.0f : 1.0f;
+
+// Rows of this block that count
+__device__ __forceinline__ int rows_of_block(const LossArgs& a) {
+    return min(max(*as_const<int32_t>(a.count) - a.block * a.block_rows, 0), a.block_rows);
+}
+// fp16: what the gradient of z is multiplied by, a power of two that brings the largest that it can be to 2^14; the products of it are divided by that
+template <typename D> __device__ __forceinline__ float gradient_scale(const LossArgs& a) {
+    if constexpr (!std::is_same<D, F16>::value) return 1.0f;
+    const uint32_t largest = as_const<uint32_t>(a.count)[1];                              // an fp32 number's bits
+    const int exponent = min(max((int)(largest >> 23) - 127, -100), 100);
+    return largest == 0 || largest >= 0x7F800000u ? 1.0f : __uint_as_float((uint32_t)(127 + 13 - exponent) << 23);
+}
+
+template <typename D, int TILE> struct LossTiles;
+template <typename D> struct LossTiles<D, 256> { static constexpr int M = 256, N = 256, WM = 2, WN = 4; };
+template <typename D> struct LossTiles<D, 128> { static constexpr int M = 128, N = 128, WM = 2, WN = 2; };
+template <typename D> struct LossTiles<D, 64> { static constexpr int M = 64, N = 64, WM = 2, WN = 2; };
+template <typename D, int TILE, bool A_ACROSS, bool B_ACROSS>
+using LossProduct = Product<D, LossTiles<D, TILE>::M, LossTiles<D, TILE>::N, LossTiles<D, TILE>::WM, LossTiles<D, TILE>::WN, A_ACROSS, B_ACROSS>;
+
+// z[v][row] = W[v] . H[row]
+template <typename D, int TILE>
+__global__ __launch_bounds__((LossProduct<D, TILE, false, false>::kThreads)) void k_loss_logits(LossArgs a) {
+    using P = LossProduct<D, TILE, false, false>;
+    extern __shared__ uint8_t lds_bytes[];
+    const Lds lds = (Lds)lds_bytes;
+    const int rows = rows_of_block(a);
+    const uint32_t tiles_m = a.padded / P::BM, tiles_n = (rows + P::BN - 1) / P::BN, item = item_of_block(blockIdx.x, tiles_m * tiles_n);
+    if (item == tiles_m * tiles_n) return;
+    uint32_t tm, tn;
+    tile_of_item(item, tiles_m, tiles_n, tm, tn);
+    const int v0 = tm * P::BM, r0 = tn * P::BN;
+    const int64_t w_bytes = a.w_stride * D::size, h_bytes = (int64_t)a.width * D::size;
+    P p;
+    p.run({static_cast<const uint8_t*>(a.W) + v0 * w_bytes, w_bytes}, {a.packed + r0 * h_bytes, h_bytes}, a.width, max(a.vocab - v0, 0), P::BN, lds);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM, h = lane >> 5;
+    const int first = v0 + wm * 32 * P::MI;                                               // of the wave's piece
+    const int64_t piece = first / (32 * P::MI);
+#pragma unroll
+    for (int j = 0; j < P::NI; ++j) {
+        const int row = r0 + 32 * (wn * P::NI + j) + (lane & 31);
+        const int target = a.target[row];
+        float top = -INFINITY, plain = 0.0f;
+#pragma unroll
+        for (int i = 0; i < P::MI; ++i)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                const int v = first + 32 * i + 8 * (x / 4) + 4 * h + x % 4;
+                const float z = p.acc[j][i][x];
+                if (v == target) a.hit[row] = z;
+                if (v < a.vocab) { top = fmaxf(top, z); plain += z; }
+            }
+        top = halves_max(top);
+        const float from = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < P::MI; ++i)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                const int v = first + 32 * i + 8 * (x / 4) + 4 * h + x % 4;
+                const float e = v < a.vocab ? __builtin_amdgcn_exp2f((p.acc[j][i][x] - from) * kLossLog2e) : 0.0f;
+                sum += e;
+                p.acc[j][i][x] = e;
+            }
+        sum = halves_sum(sum);
+        if (h == 0) { a.top[piece * a.block_rows + row] = top; a.sum[piece * a.block_rows + row] = sum; }
+        if (a.smoothing > 0.0f) {
+            plain = halves_sum(plain);
+            if (h == 0) a.plain[piece * a.block_rows + row] = plain;
+        }
+    }
+    if (!a.train) return;
+    const Lds own = lds + wave * (32 * 32 * P::MI * D::size);
+#pragma unroll
+    for (int j = 0; j < P::NI; ++j) {
+        const int row0 = r0 + 32 * (wn * P::NI + j);
+        store_wave_rows<D, 32 * P::MI>(p.acc[j], kLossTop<D>, own, 32 * P::MI, lane, [&](uint32_t r) { return a.e + ((int64_t)(row0 + (int)r) * a.padded + first) * D::size; });
+    }
+}
+
+// dH[row][d] = sum over v of dz[row][v] W[v][d]; with several parts of the vocabulary each has its sum in fp32
+template <typename D, int TILE>
+__global__ __launch_bounds__((LossProduct<D, TILE, true, false>::kThreads)) void k_loss_dh(LossArgs a) {
+    using P = LossProduct<D, TILE, true, false>;
+    extern __shared__ uint8_t lds_bytes[];
+    const Lds lds = (Lds)lds_bytes;
+    const int rows = rows_of_block(a);
+    const uint32_t tiles_m = (a.width + P::BM - 1) / P::BM, tiles_n = (rows + P::BN - 1) / P::BN, items = tiles_m * tiles_n * a.dh_splits, item = item_of_block(blockIdx.x, items);
+    if (item == items) return;
+    const uint32_t split = item / (tiles_m * tiles_n);
+    uint32_t tm, tn;
+    tile_of_item(item - split * tiles_m * tiles_n, tiles_m, tiles_n, tm, tn);
+    const int d0 = tm * P::BM, r0 = tn * P::BN, steps = (a.vocab + P::BK - 1) / P::BK, share = (steps + a.dh_splits - 1) / a.dh_splits;
+    const int v0 = min((int)split * share * P::BK, a.vocab), v1 = min(v0 + share * P::BK, a.vocab);
+    const int64_t w_bytes = a.w_stride * D::size, e_bytes = (int64_t)a.padded * D::size;
+    P p;
+    p.run({static_cast<const uint8_t*>(a.W) + v0 * w_bytes + (int64_t)d0 * D::size, w_bytes}, {a.e + r0 * e_bytes + (int64_t)v0 * D::size, e_bytes}, v1 - v0, a.width - d0, P::BN, lds);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM;
+    const int first = d0 + wm * 32 * P::MI, left = a.width - first;
+    const float factor = 1.0f / gradient_scale<D>(a);
+#pragma unroll
+    for (int j = 0; j < P::NI; ++j) {
+        const int row0 = r0 + 32 * (wn * P::NI + j);
+        if (a.dh_splits > 1) {
+            float* const to = a.dh_parts + (int64_t)split * a.block_rows * a.width + first;
+            store_wave_rows<F32, 32 * P::MI>(p.acc[j], factor, lds + wave * (32 * 32 * P::MI * 4), left, lane,
+                                             [&](uint32_t r) { return reinterpret_cast<uint8_t*>(to + (int64_t)(row0 + (int)r) * a.width); });
+        } else {
+            store_wave_rows<D, 32 * P::MI>(p.acc[j], factor, lds + wave * (32 * 32 * P::MI * D::size), left, lane, [&](uint32_t r) -> uint8_t* {
+                const int row = row0 + (int)r;
+                return row < rows ? static_cast<uint8_t*>(a.dH) + (a.index[a.block * a.block_rows + row] * a.dh_stride + first) * D::size : nullptr;
+            });
+        }
+    }
+}
+
+// dW[v][d] = sum over the rows of dz[row][v] H[row][d]
+template <typename D, int TILE>
+__global__ __launch_bounds__((LossProduct<D, TILE, true, true>::kThreads)) void k_loss_dw(LossArgs a) {
+    using P = LossProduct<D, TILE, true, true>;
+    extern __shared__ uint8_t lds_bytes[];
+    const Lds lds = (Lds)lds_bytes;
+    const int rows = rows_of_block(a);
+    const uint32_t tiles_m = (a.width + P::BM - 1) / P::BM, tiles_n = (a.vocab + P::BN - 1) / P::BN, item = item_of_block(blockIdx.x, tiles_m * tiles_n);
+    if (item == tiles_m * tiles_n) return;
+    uint32_t tm, tn;
+    tile_of_item(item, tiles_m, tiles_n, tm, tn);
+    const int d0 = tm * P::BM, v0 = tn * P::BN;
+    const int64_t h_bytes = (int64_t)a.width * D::size, e_bytes = (int64_t)a.padded * D::size;
+    P p;
+    // (up to whole steps: the rows behind those that count are zeros in both)
+    p.run({a.packed + (int64_t)d0 * D::size, h_bytes}, {a.e + (int64_t)v0 * D::size, e_bytes}, (rows + P::BK - 1) / P::BK * P::BK, a.width - d0, P::BN, lds);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM;
+    const int first = d0 + wm * 32 * P::MI, left = a.width - first;
+    const float factor = 1.0f / gradient_scale<D>(a);
+#pragma unroll
+    for (int j = 0; j < P::NI; ++j) {
+        const int row0 = v0 + 32 * (wn * P::NI + j);
+        if (a.blocks > 1) {
+            // the sum so far is added in registers: a lane has four d that follow one another
+            float* const so_far = D::size == 4 ? static_cast<float*>(a.dW) : a.dw_sum;
+            const int64_t stride = D::size == 4 ? a.dw_stride : a.width;
+            const int v = row0 + (lane & 31);
+#pragma unroll
+            for (int i = 0; i < P::MI; ++i)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int d = first + 32 * i + 8 * g + 4 * (lane >> 5);
+                    f32x4 x = {p.acc[j][i][4 * g] * factor, p.acc[j][i][4 * g + 1] * factor, p.acc[j][i][4 * g + 2] * factor, p.acc[j][i][4 * g + 3] * factor};
+                    if (v < a.vocab && d < a.width) {
+                        f32x4* const at = reinterpret_cast<f32x4*>(so_far + v * stride + d);
+                        if (a.block > 0) x += *at;
+                        if (D::size == 4 || a.block + 1 < a.blocks) *at = x;
+                        else store_four<D>(static_cast<uint8_t*>(a.dW) + (v * a.dw_stride + d) * D::size, x[0], x[1], x[2], x[3]);
+                    }
+                }
+        } else {
+            store_wave_rows<D, 32 * P::MI>(p.acc[j], factor, lds + wave * (32 * 32 * P::MI * D::size), left, lane, [&](uint32_t r) -> uint8_t* {
+                const int v = row0 + (int)r;
+                return v < a.vocab ? static_cast<uint8_t*>(a.dW) + (v * a.dw_stride + first) * D::size : nullptr;
+            });
+        }
+    }
+}
+
+template <typename P, auto Kernel> static inline hipError_t launch_tiles(const LossArgs& a, uint32_t tiles, hipStream_t st) {
+    const hipError_t e = allow_dynamic_lds<Kernel, P::kLds>();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(Kernel, dim3(tiles), dim3(P::kThreads), P::kLds, st, a);
+    return hipGetLastError();
+}
+template <typename D, int TILE> static inline hipError_t launch_logits_of(const LossArgs& a, hipStream_t st) {
+    return launch_tiles<LossProduct<D, TILE, false, false>, &k_loss_logits<D, TILE>>(a, (uint32_t)(a.padded / TILE * (a.block_rows / TILE)), st);
+}
+template <typename D, int TILE> static inline hipError_t launch_dh_of(const LossArgs& a, hipStream_t st) {
+    return launch_tiles<LossProduct<D, TILE, true, false>, &k_loss_dh<D, TILE>>(a, (uint32_t)((a.width + TILE - 1) / TILE * (a.block_rows / TILE) * a.dh_splits), st);
+}
+template <typename D, int TILE> static inline hipError_t launch_dw_of(const LossArgs& a, hipStream_t st) {
+    return launch_tiles<LossProduct<D, TILE, true, true>, &k_loss_dw<D, TILE>>(a, (uint32_t)((a.width + TILE - 1) / TILE * ((a.vocab + TILE - 1) / TILE)), st);
+}
+template <typename D> hipError_t launch_loss_logits(const LossArgs& a, hipStream_t st) {
+    return a.tile[0] == 256 ? launch_logits_of<D, 256>(a, st) : a.tile[0] == 128 ? launch_logits_of<D, 128>(a, st) : launch_logits_of<D, 64>(a, st);
+}
+template <typename D> hipError_t launch_loss_dh(const LossArgs& a, hipStream_t st) {
+    return a.tile[1] == 256 ? launch_dh_of<D, 256>(a, st) : a.tile[1] == 128 ? launch_dh_of<D, 128>(a, st) : launch_dh_of<D, 64>(a, st);
+}
+template <typename D> hipError_t launch_loss_dw(const LossArgs& a, hipStream_t st) {
+    return a.tile[2] == 256 ? launch_dw_of<D, 256>(a, st) : a.tile[2] == 128 ? launch_dw_of<D, 128>(a, st) : launch_dw_of<D, 64>(a, st);
+}
+#endif
+
+}  // namespace lsp

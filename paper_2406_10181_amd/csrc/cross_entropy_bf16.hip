@@ -1,0 +1,8 @@
+// The cross entropy's products in bf16.
+#include "cross_entropy.h"
+
+namespace lsp {
+template hipError_t launch_loss_logits<BF16>(const LossArgs& a, hipStream_t st);
+template hipError_t launch_loss_dh<BF16>(const LossArgs& a, hipStream_t st);
+template hipError_t launch_loss_dw<BF16>(const LossArgs& a, hipStream_t st);
+}  // namespace lsp

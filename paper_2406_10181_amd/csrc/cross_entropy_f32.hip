@@ -1,0 +1,8 @@
+// The cross entropy's products in f32.
+#include "cross_entropy.h"
+
+namespace lsp {
+template hipError_t launch_loss_logits<F32>(const LossArgs& a, hipStream_t st);
+template hipError_t launch_loss_dh<F32>(const LossArgs& a, hipStream_t st);
+template hipError_t launch_loss_dw<F32>(const LossArgs& a, hipStream_t st);
+}  // namespace lsp

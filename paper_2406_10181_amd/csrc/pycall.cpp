@@ -26,12 +26,18 @@ decltype(&lsp_attention_forward) g_attention_forward;
 decltype(&lsp_attention_backward) g_attention_backward;
 decltype(&lsp_residual_norm_forward) g_norm_forward;
 decltype(&lsp_residual_norm_backward) g_norm_backward;
+decltype(&lsp_rotary_forward) g_rotary_forward;
+decltype(&lsp_rotary_backward) g_rotary_backward;
+decltype(&lsp_cross_entropy_forward) g_loss_forward;
+decltype(&lsp_cross_entropy_backward) g_loss_backward;
 
 PyObject* g_shape;
 PyObject* g_stride;
 PyObject* g_dtype;
 PyObject* g_get_device;
 PyObject* g_types[3];         // torch's types, in the order of lsp_dtype; from the first descriptor on
+PyObject* g_int32;
+PyObject* g_int64;
 
 // Converts one argument after another, to what ctypes makes of it; the first failure leaves a Python exception and ok = false.
 struct Args {
@@ -216,7 +222,10 @@ bool know_types() {
     PyObject* torch = PyImport_ImportModule("torch");
     if (!torch) return false;
     const char* names[3] = {"float32", "float16", "bfloat16"};
-    for (int i = 2; i >= 0; --i) if (!(g_types[i] = PyObject_GetAttrString(torch, names[i]))) break;
+    if (!g_int32) g_int32 = PyObject_GetAttrString(torch, "int32");
+    if (!g_int64) g_int64 = PyObject_GetAttrString(torch, "int64");
+    if (g_int32 && g_int64)
+        for (int i = 2; i >= 0; --i) if (!(g_types[i] = PyObject_GetAttrString(torch, names[i]))) break;
     Py_DECREF(torch);
     return g_types[0] != nullptr;
 }
@@ -241,6 +250,10 @@ struct AttentionOfTensors { lsp_attention_problem p; int32_t dtype; };
 struct AttentionGradientsOfTensors { lsp_attention_gradients g; int64_t q_shape[4], k_shape[4]; int32_t dtype; };
 struct ResidualNormOfTensors { lsp_residual_norm_problem p; int32_t dtype; };
 struct ResidualNormGradientsOfTensors { lsp_residual_norm_gradients g; int64_t rows, width; int32_t dtype; };
+struct RotaryOfTensors { lsp_rotary_problem p; int32_t dtype; };
+struct RotaryGradientsOfTensors { lsp_rotary_gradients g; int64_t q_shape[4], k_shape[4], kr_shape[4]; int32_t dtype; };
+struct CrossEntropyOfTensors { lsp_cross_entropy_problem p; int32_t dtype; };
+struct CrossEntropyGradientsOfTensors { lsp_cross_entropy_gradients g; int64_t h_shape[2], w_shape[2], weights; int32_t dtype; };
 
 bool matches(const AttentionOfTensors& a, const AttentionGradientsOfTensors& b) {
     const int64_t q[4] = {a.p.batch, a.p.q_len, a.p.heads, a.p.head_dim}, k[4] = {a.p.batch, a.p.k_len, a.p.kv_heads, a.p.head_dim};
@@ -248,6 +261,15 @@ bool matches(const AttentionOfTensors& a, const AttentionGradientsOfTensors& b) 
     return true;
 }
 bool matches(const ResidualNormOfTensors& a, const ResidualNormGradientsOfTensors& b) { return a.p.rows == b.rows && a.p.width == b.width; }
+bool matches(const RotaryOfTensors& a, const RotaryGradientsOfTensors& b) {
+    const int64_t q[4] = {a.p.batch, a.p.length, a.p.heads, a.p.head_dim}, k[4] = {a.p.batch, a.p.length, a.p.kv_heads, a.p.head_dim}, kr[4] = {a.p.batch, a.p.cache, a.p.kv_heads, a.p.head_dim};
+    for (int i = 0; i < 4; ++i) if (q[i] != b.q_shape[i] || k[i] != b.k_shape[i] || kr[i] != b.kr_shape[i]) return false;
+    return true;
+}
+bool matches(const CrossEntropyOfTensors& a, const CrossEntropyGradientsOfTensors& b) {      // (-1: not there)
+    const bool h = b.h_shape[0] < 0 || (b.h_shape[0] == a.p.rows && b.h_shape[1] == a.p.width), w = b.w_shape[0] < 0 || (b.w_shape[0] == a.p.vocab && b.w_shape[1] == a.p.width);
+    return h && w && (b.weights < 0 || b.weights == a.p.rows);
+}
 
 // (address of the binding's attention_problem, Q, K, V, O, L, q_lens, k_lens, scale, causal, dropout, seed, offset)
 PyObject* attention_problem(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
@@ -384,10 +406,160 @@ PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     return without_gil([&] { return g_dropout(x, y, rows, width, p, seed, offset, static_cast<lsp_dtype>(dtype), st); });
 }
 
+// Whether tensors (None: passed over) are on one device; false with a Python exception set
+bool on_one_device(PyObject* const* t, int count, const char* what) {
+    long first = 0;
+    bool any = false;
+    for (int i = 0; i < count; ++i) {
+        if (t[i] == Py_None) continue;
+        long d;
+        if (!device_of(t[i], d)) return false;
+        if (any && d != first) { PyErr_Format(PyExc_ValueError, "%s: the tensors are on one device", what); return false; }
+        first = d;
+        any = true;
+    }
+    return true;
+}
+// A contiguous tensor of integers of one type, or None
+bool whole_numbers(PyObject* t, int dims, const int64_t* shape, const PyObject* dtype, void*& to, const char* what) {
+    to = nullptr;
+    if (t == Py_None) return true;
+    Tensor x;
+    if (!x.read(t, dims, what)) return false;
+    bool ok = x.dtype == dtype;
+    for (int i = 0; ok && i < dims; ++i) ok = x.shape[i] == shape[i];
+    if (ok && dims == 2) ok = x.shape[0] == 1 || x.stride[0] == x.shape[1];
+    if (!ok) { PyErr_Format(PyExc_ValueError, "%s: positions [batch][length], starts and lens [batch] are int32, targets [rows] int64, all contiguous", what); return false; }
+    to = x.data;
+    return true;
+}
+
+// (address of the binding's rotary_problem, Q, K, V, Qr, Kr, Vr, q_weight, k_weight, q_bias, k_bias, frequencies, positions, starts, lens, neighbours, norm, eps)
+PyObject* rotary_problem(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    if (!count_is(nargs, 18)) return nullptr;
+    const char* what = "rotary_problem";
+    Args head(args);
+    auto* d = static_cast<RotaryOfTensors*>(head.pointer());
+    if (!head.ok || !know_types()) return nullptr;
+    Tensor t[6];                                       // Q, K, V, Qr, Kr, Vr
+    for (int i = 0; i < 6; ++i) if ((args[1 + i] != Py_None || i % 3 != 2) && !t[i].read(args[1 + i], 4, what)) return nullptr;
+    const Tensor &q = t[0], &k = t[1], &v = t[2], &qr = t[3], &kr = t[4], &vr = t[5];
+    if (!qr.same_shape(q) || k.shape[0] != q.shape[0] || k.shape[1] != q.shape[1] || k.shape[3] != q.shape[3] || kr.shape[0] != k.shape[0] || kr.shape[2] != k.shape[2] ||
+        kr.shape[3] != k.shape[3] || !v.dtype != !vr.dtype || (v.dtype && (!v.same_shape(k) || !vr.same_shape(kr))))
+        return refuse("rotary_problem: Q, Qr [batch][length][heads][head_dim], K [batch][length][kv_heads][head_dim], Kr [batch][cache][kv_heads][head_dim] and, both or neither, V like K and Vr like Kr are wanted");
+    for (const Tensor& x : t) if (x.dtype && (x.dtype != q.dtype || type_code(x.dtype) < 0)) return refuse("rotary_problem: all of Q, K, V, Qr, Kr and Vr are of one type, float32, float16 or bfloat16");
+    void* w[4];
+    for (int i = 0; i < 4; ++i) if (!vector(args[7 + i], q.shape[3], q.dtype, w[i], what)) return nullptr;
+    Tensor f;
+    if (args[11] != Py_None) {
+        if (!f.read(args[11], 1, what)) return nullptr;
+        if (type_code(f.dtype) != LSP_F32) return refuse("rotary_problem: frequencies are [rotated / 2], float32");
+    }
+    void* n[3];
+    const int64_t tokens[2] = {q.shape[0], q.shape[1]};
+    for (int i = 0; i < 3; ++i) if (!whole_numbers(args[12 + i], i == 0 ? 2 : 1, tokens, g_int32, n[i], what)) return nullptr;
+    if (!on_one_device(args + 1, 14, what)) return nullptr;
+    Args tail(args + 15);
+    const int32_t neighbours = PyObject_IsTrue(*tail.a++), norm = tail.int32();
+    bool ok = tail.ok;
+    const float eps = number(args[17], ok);
+    if (!ok || PyErr_Occurred()) return nullptr;
+    d->dtype = type_code(q.dtype);
+    d->p = lsp_rotary_problem{q.data, k.data, v.data, qr.data, kr.data, vr.data, w[0], w[1], w[2], w[3], static_cast<const float*>(f.data), static_cast<const int32_t*>(n[0]),
+                              static_cast<const int32_t*>(n[1]), static_cast<const int32_t*>(n[2]),
+                              {q.stride[0], q.stride[1], q.stride[2]}, {k.stride[0], k.stride[1], k.stride[2]}, {v.stride[0], v.stride[1], v.stride[2]},
+                              {qr.stride[0], qr.stride[1], qr.stride[2]}, {kr.stride[0], kr.stride[1], kr.stride[2]}, {vr.stride[0], vr.stride[1], vr.stride[2]},
+                              size32(q.shape[0]), size32(q.shape[1]), size32(kr.shape[1]), size32(q.shape[2]), size32(k.shape[2]), size32(q.shape[3]),
+                              f.shape[0] > INT32_MAX / 2 ? -1 : 2 * (int32_t)f.shape[0], neighbours, norm, eps};
+    Py_RETURN_NONE;
+}
+
+// (address of the binding's rotary_gradients, dQr, dKr, dQ, dK, q_weight, k_weight, q_bias, k_bias)
+PyObject* rotary_gradients(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    if (!count_is(nargs, 9)) return nullptr;
+    const char* what = "rotary_gradients";
+    Args head(args);
+    auto* d = static_cast<RotaryGradientsOfTensors*>(head.pointer());
+    if (!head.ok || !know_types()) return nullptr;
+    Tensor t[4];
+    for (int i = 0; i < 4; ++i) if (!t[i].read(args[1 + i], 4, what)) return nullptr;
+    if (!t[0].same_shape(t[2])) return refuse("rotary_gradients: dQr and dQ are of one shape");
+    for (const Tensor& x : t) if (type_code(x.dtype) < 0 || x.dtype != t[0].dtype) return refuse("rotary_gradients: dQr, dKr, dQ and dK are of one type, float32, float16 or bfloat16");
+    void* w[4];
+    for (int i = 0; i < 4; ++i) if (!vector(args[5 + i], t[0].shape[3], g_types[LSP_F32], w[i], what)) return nullptr;
+    if (!on_one_device(args + 1, 8, what)) return nullptr;
+    for (int i = 0; i < 4; ++i) { d->q_shape[i] = t[2].shape[i]; d->k_shape[i] = t[3].shape[i]; d->kr_shape[i] = t[1].shape[i]; }
+    d->dtype = type_code(t[0].dtype);
+    d->g = lsp_rotary_gradients{t[0].data, t[1].data, t[2].data, t[3].data, static_cast<float*>(w[0]), static_cast<float*>(w[1]), static_cast<float*>(w[2]), static_cast<float*>(w[3]),
+                                {t[0].stride[0], t[0].stride[1], t[0].stride[2]}, {t[1].stride[0], t[1].stride[1], t[1].stride[2]},
+                                {t[2].stride[0], t[2].stride[1], t[2].stride[2]}, {t[3].stride[0], t[3].stride[1], t[3].stride[2]}};
+    Py_RETURN_NONE;
+}
+
+// A contiguous [count] vector in float32, or None
+bool floats(PyObject* t, int64_t count, float*& to, const char* what) {
+    to = nullptr;
+    if (t == Py_None) return true;
+    Tensor x;
+    if (!x.read(t, 1, what)) return false;
+    if (type_code(x.dtype) != LSP_F32 || (count >= 0 && x.shape[0] != count)) { PyErr_Format(PyExc_ValueError, "%s: losses, logs and weights are [rows], float32", what); return false; }
+    to = static_cast<float*>(x.data);
+    return true;
+}
+
+// (address of the binding's cross_entropy_problem, H, W, targets, losses, logs, smoothing, z_loss)
+PyObject* cross_entropy_problem(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    if (!count_is(nargs, 8)) return nullptr;
+    const char* what = "cross_entropy_problem";
+    Args head(args);
+    auto* d = static_cast<CrossEntropyOfTensors*>(head.pointer());
+    if (!head.ok || !know_types()) return nullptr;
+    Tensor h, w;
+    if (!h.read(args[1], 2, what) || !w.read(args[2], 2, what)) return nullptr;
+    if (h.shape[1] != w.shape[1] || h.dtype != w.dtype || type_code(h.dtype) < 0) return refuse("cross_entropy_problem: H [rows][width] and W [vocab][width] of one type, float32, float16 or bfloat16, are wanted");
+    void* targets;
+    float *losses, *logs;
+    if (args[3] == Py_None || args[4] == Py_None) return refuse("cross_entropy_problem: targets and losses are wanted");
+    if (!whole_numbers(args[3], 1, h.shape, g_int64, targets, what) || !floats(args[4], h.shape[0], losses, what) || !floats(args[5], h.shape[0], logs, what)) return nullptr;
+    if (!on_one_device(args + 1, 5, what)) return nullptr;
+    bool ok = true;
+    const float smoothing = number(args[6], ok), z_loss = number(args[7], ok);
+    if (!ok) return nullptr;
+    d->dtype = type_code(h.dtype);
+    d->p = lsp_cross_entropy_problem{h.data, w.data, static_cast<const int64_t*>(targets), losses, logs, h.stride[0], w.stride[0], h.shape[0], size32(h.shape[1]), size32(w.shape[0]), smoothing, z_loss};
+    Py_RETURN_NONE;
+}
+
+// (address of the binding's cross_entropy_gradients, dH, dW, weights, scale)
+PyObject* cross_entropy_gradients(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    if (!count_is(nargs, 5)) return nullptr;
+    const char* what = "cross_entropy_gradients";
+    Args head(args);
+    auto* d = static_cast<CrossEntropyGradientsOfTensors*>(head.pointer());
+    if (!head.ok || !know_types()) return nullptr;
+    Tensor t[2];
+    for (int i = 0; i < 2; ++i) if (args[1 + i] != Py_None && !t[i].read(args[1 + i], 2, what)) return nullptr;
+    const PyObject* dtype = t[0].dtype ? t[0].dtype : t[1].dtype;
+    if (!dtype) return refuse("cross_entropy_gradients: dH, dW or both are wanted");
+    for (const Tensor& x : t) if (x.dtype && (x.dtype != dtype || type_code(x.dtype) < 0)) return refuse("cross_entropy_gradients: dH and dW are of one type, float32, float16 or bfloat16");
+    float* weights;
+    Tensor n;
+    if (args[3] != Py_None && !n.read(args[3], 1, what)) return nullptr;
+    if (!floats(args[3], -1, weights, what) || !on_one_device(args + 1, 3, what)) return nullptr;
+    bool ok = true;
+    const float scale = number(args[4], ok);
+    if (!ok) return nullptr;
+    for (int i = 0; i < 2; ++i) { d->h_shape[i] = t[0].dtype ? t[0].shape[i] : -1; d->w_shape[i] = t[1].dtype ? t[1].shape[i] : -1; }
+    d->weights = weights ? n.shape[0] : -1;
+    d->dtype = type_code(dtype);
+    d->g = lsp_cross_entropy_gradients{t[0].data, t[1].data, weights, t[0].stride[0], t[1].stride[0], scale};
+    Py_RETURN_NONE;
+}
+
 // The binding's classes of descriptors: those of the C structures and, derived from these, those that are made of tensors
-enum Kind { ATTENTION, ATTENTION_GRADIENTS, RESIDUAL_NORM, RESIDUAL_NORM_GRADIENTS };
-PyTypeObject* g_base[4];
-PyTypeObject* g_of_tensors[4];
+enum Kind { ATTENTION, ATTENTION_GRADIENTS, RESIDUAL_NORM, RESIDUAL_NORM_GRADIENTS, ROTARY, ROTARY_GRADIENTS, CROSS_ENTROPY, CROSS_ENTROPY_GRADIENTS, KINDS };
+PyTypeObject* g_base[KINDS];
+PyTypeObject* g_of_tensors[KINDS];
 
 // A descriptor as it is given, made by hand or of tensors; None: NULL
 template <Kind KIND, typename Base, typename OfTensors> struct Given {
@@ -413,6 +585,10 @@ using GivenAttention = Given<ATTENTION, lsp_attention_problem, AttentionOfTensor
 using GivenAttentionGradients = Given<ATTENTION_GRADIENTS, lsp_attention_gradients, AttentionGradientsOfTensors>;
 using GivenResidualNorm = Given<RESIDUAL_NORM, lsp_residual_norm_problem, ResidualNormOfTensors>;
 using GivenResidualNormGradients = Given<RESIDUAL_NORM_GRADIENTS, lsp_residual_norm_gradients, ResidualNormGradientsOfTensors>;
+using GivenRotary = Given<ROTARY, lsp_rotary_problem, RotaryOfTensors>;
+using GivenRotaryGradients = Given<ROTARY_GRADIENTS, lsp_rotary_gradients, RotaryGradientsOfTensors>;
+using GivenCrossEntropy = Given<CROSS_ENTROPY, lsp_cross_entropy_problem, CrossEntropyOfTensors>;
+using GivenCrossEntropyGradients = Given<CROSS_ENTROPY_GRADIENTS, lsp_cross_entropy_gradients, CrossEntropyGradientsOfTensors>;
 
 // (problem, dtype, ...)
 template <typename P> bool problem_of(Args& a, P& p, int32_t& dtype) {
@@ -422,18 +598,20 @@ template <typename P> bool problem_of(Args& a, P& p, int32_t& dtype) {
 }
 
 // (problem, dtype, workspace, workspace_bytes, stream)
-PyObject* attention_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+template <typename Problem, typename Entry> PyObject* forward(Entry entry, PyObject* const* args, Py_ssize_t nargs) {
     if (!count_is(nargs, 5)) return nullptr;
     Args a(args);
-    GivenAttention p;
+    Problem p;
     int32_t dtype;
     if (!problem_of(a, p, dtype)) return nullptr;
     void* ws = a.pointer();
     const size_t bytes = a.integer();
     void* st = a.stream();
     if (!a.ok) return nullptr;
-    return without_gil([&] { return g_attention_forward(p.p, static_cast<lsp_dtype>(dtype), ws, bytes, st); });
+    return without_gil([&] { return entry(p.p, static_cast<lsp_dtype>(dtype), ws, bytes, st); });
 }
+PyObject* attention_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return forward<GivenAttention>(g_attention_forward, args, nargs); }
+PyObject* cross_entropy_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return forward<GivenCrossEntropy>(g_loss_forward, args, nargs); }
 // (problem, gradients, dtype, workspace, workspace_bytes, stream)
 template <typename Problem, typename Gradients, typename Entry> PyObject* backward(Entry entry, PyObject* const* args, Py_ssize_t nargs) {
     if (!count_is(nargs, 6)) return nullptr;
@@ -455,37 +633,48 @@ PyObject* attention_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs)
 PyObject* residual_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     return backward<GivenResidualNorm, GivenResidualNormGradients>(g_norm_backward, args, nargs);
 }
+PyObject* rotary_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return backward<GivenRotary, GivenRotaryGradients>(g_rotary_backward, args, nargs); }
+PyObject* cross_entropy_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    return backward<GivenCrossEntropy, GivenCrossEntropyGradients>(g_loss_backward, args, nargs);
+}
 // (problem, dtype, stream)
-PyObject* residual_norm_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+template <typename Problem, typename Entry> PyObject* forward_alone(Entry entry, PyObject* const* args, Py_ssize_t nargs) {
     if (!count_is(nargs, 3)) return nullptr;
     Args a(args);
-    GivenResidualNorm p;
+    Problem p;
     int32_t dtype;
     if (!problem_of(a, p, dtype)) return nullptr;
     void* st = a.stream();
     if (!a.ok) return nullptr;
-    return without_gil([&] { return g_norm_forward(p.p, static_cast<lsp_dtype>(dtype), st); });
+    return without_gil([&] { return entry(p.p, static_cast<lsp_dtype>(dtype), st); });
 }
+PyObject* residual_norm_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return forward_alone<GivenResidualNorm>(g_norm_forward, args, nargs); }
+PyObject* rotary_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return forward_alone<GivenRotary>(g_rotary_forward, args, nargs); }
 
-// (addresses of lsp_dropout, lsp_attention_forward, lsp_attention_backward, lsp_residual_norm_forward, lsp_residual_norm_backward; the classes of the four C structures, in
-// the order of Kind, and those of descriptors made of tensors)
+// (addresses of lsp_dropout, lsp_attention_forward, lsp_attention_backward, lsp_residual_norm_forward, lsp_residual_norm_backward, lsp_rotary_forward, lsp_rotary_backward,
+// lsp_cross_entropy_forward, lsp_cross_entropy_backward; the classes of the C structures, in the order of Kind, and those of descriptors made of tensors)
 PyObject* bind_operators(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-    if (!count_is(nargs, 13)) return nullptr;
+    constexpr int kCalls = 9;
+    if (!count_is(nargs, kCalls + 2 * KINDS)) return nullptr;
     Args a(args);
-    void* p[5];
+    void* p[kCalls];
     for (void*& x : p) x = a.pointer();
     if (!a.ok) return nullptr;
-    for (int i = 5; i < 13; ++i) if (!PyType_Check(args[i])) return refuse("bind_operators: classes are wanted");
-    for (int i = 0; i < 4; ++i) {
-        Py_INCREF(args[5 + i]); Py_INCREF(args[9 + i]);                    // (kept as long as the module is)
-        g_base[i] = reinterpret_cast<PyTypeObject*>(args[5 + i]);
-        g_of_tensors[i] = reinterpret_cast<PyTypeObject*>(args[9 + i]);
+    for (int i = kCalls; i < kCalls + 2 * KINDS; ++i) if (!PyType_Check(args[i])) return refuse("bind_operators: classes are wanted");
+    for (int i = 0; i < KINDS; ++i) {
+        Py_INCREF(args[kCalls + i]); Py_INCREF(args[kCalls + KINDS + i]);  // (kept as long as the module is)
+        g_base[i] = reinterpret_cast<PyTypeObject*>(args[kCalls + i]);
+        g_of_tensors[i] = reinterpret_cast<PyTypeObject*>(args[kCalls + KINDS + i]);
     }
     g_dropout = reinterpret_cast<decltype(g_dropout)>(p[0]);
     g_attention_forward = reinterpret_cast<decltype(g_attention_forward)>(p[1]);
     g_attention_backward = reinterpret_cast<decltype(g_attention_backward)>(p[2]);
     g_norm_forward = reinterpret_cast<decltype(g_norm_forward)>(p[3]);
     g_norm_backward = reinterpret_cast<decltype(g_norm_backward)>(p[4]);
+    g_rotary_forward = reinterpret_cast<decltype(g_rotary_forward)>(p[5]);
+    g_rotary_backward = reinterpret_cast<decltype(g_rotary_backward)>(p[6]);
+    g_loss_forward = reinterpret_cast<decltype(g_loss_forward)>(p[7]);
+    g_loss_backward = reinterpret_cast<decltype(g_loss_backward)>(p[8]);
     Py_RETURN_NONE;
 }
 
@@ -500,6 +689,9 @@ PyMethodDef g_methods[] = {
     method<residual_norm_problem>("residual_norm_problem"), method<residual_norm_gradients>("residual_norm_gradients"),
     method<dropout>("dropout"), method<attention_forward>("attention_forward"), method<attention_backward>("attention_backward"),
     method<residual_norm_forward>("residual_norm_forward"), method<residual_norm_backward>("residual_norm_backward"),
+    method<rotary_problem>("rotary_problem"), method<rotary_gradients>("rotary_gradients"), method<rotary_forward>("rotary_forward"), method<rotary_backward>("rotary_backward"),
+    method<cross_entropy_problem>("cross_entropy_problem"), method<cross_entropy_gradients>("cross_entropy_gradients"),
+    method<cross_entropy_forward>("cross_entropy_forward"), method<cross_entropy_backward>("cross_entropy_backward"),
     method<bind_operators>("bind_operators"), {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_call", "Argument marshalling of the per-step entry points.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,214 @@
+"""lsp_cross_entropy_forward and lsp_cross_entropy_backward against the definition in 64 bits, through the C ABI."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2406_10181_amd as L
+import training_reference as ref
+
+pytestmark = pytest.mark.gpu
+DTYPE = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def room(n):
+    return torch.full((n + 256,), 255, dtype=torch.uint8, device="cuda")     # (what lies there is not used: NaN as a float)
+
+
+class Case:
+    def __init__(self, dtype, rows, width, vocab, smoothing=0.0, z_loss=0.0, left_out=0.0, weights=True, scale=1.0, seed=0, reach=1.0, pad=0):
+        g = torch.Generator().manual_seed(seed)
+        t = DTYPE[dtype]
+        self.__dict__.update(dtype=dtype, code=L.DTYPE_CODE[dtype], smoothing=smoothing, z_loss=z_loss, scale=scale)
+        W = torch.randn(vocab, width, generator=g) / width ** 0.5
+        self.targets = torch.randint(0, vocab, (rows,), generator=g)
+        H = (reach * (torch.randn(rows, width, generator=g) + 4 * torch.rand(rows, 1, generator=g) * W[self.targets])).to(t)
+        self.targets[torch.rand(rows, generator=g) < left_out] = -100
+        self.H, self.W = torch.zeros(rows, width + pad, dtype=t)[:, :width], torch.zeros(vocab, width + pad, dtype=t)[:, :width]
+        self.H.copy_(H), self.W.copy_(W.to(t))
+        self.weights = (0.5 + torch.rand(rows, generator=g)) / rows if weights else None
+        for k in ("H", "W", "targets", "weights"):                           # (strides as they are)
+            x = getattr(self, k)
+            if x is not None:
+                y = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device="cuda")
+                y.copy_(x)
+                setattr(self, k, y)
+        new = lambda x: torch.full_like(x, 7.0)
+        self.losses, self.logs = (torch.full((rows,), 7.0, device="cuda") for _ in range(2))
+        self.dH, self.dW = new(self.H), new(self.W)
+
+    def problem(self):
+        return L.cross_entropy_problem(self.H, self.W, self.targets, self.losses, logs=self.logs, smoothing=self.smoothing, z_loss=self.z_loss)
+
+    def forward(self):
+        p = self.problem()
+        n = L.lsp_cross_entropy_forward_workspace_bytes(p, self.code)
+        L.lsp_cross_entropy_forward(p, self.code, room(n), n, torch.cuda.current_stream())
+
+    def backward(self, dH=True, dW=True):
+        p = self.problem()
+        n = L.lsp_cross_entropy_backward_workspace_bytes(p, self.code)
+        ws = room(n)
+        L.lsp_cross_entropy_backward(p, L.cross_entropy_gradients(self.dH if dH else None, self.dW if dW else None, weights=self.weights, scale=self.scale), self.code, ws, n,
+                                     torch.cuda.current_stream())
+        assert bool((ws[n:] == 255).all()), "written behind the workspace"
+
+    def check(self, names=("losses", "logs", "dH", "dW")):
+        want = ref.cross_entropy(f64(self.H), f64(self.W), self.targets.cpu().numpy(), smoothing=self.smoothing, z_loss=self.z_loss, weights=None if self.weights is None else f64(self.weights),
+                                 scale=self.scale, dtype=self.dtype)
+        for k in names:
+            value, bound = want[k]
+            got = f64(getattr(self, k))
+            off = np.abs(got - value)
+            assert np.all(off <= bound), f"{k}: {np.nanmax(off / np.maximum(bound, 1e-300)):.2f} times its bound ({np.isnan(got).sum()} NaN)"
+
+
+SHAPES = [
+    # dtype, rows, width, vocab, more
+    ("f32", 64, 256, 1000, dict()),
+    ("f32", 1, 8, 1, dict()),
+    ("bf16", 1, 8, 7, dict(smoothing=0.1)),
+    ("f16", 1, 64, 300, dict(z_loss=1e-2)),
+    ("bf16", 17, 40, 513, dict(smoothing=0.2, z_loss=1e-3, left_out=0.3)),
+    ("f16", 257, 72, 255, dict(left_out=0.5)),
+    ("f32", 130, 24, 2049, dict(smoothing=0.1, z_loss=1e-4, left_out=0.2, pad=8)),
+    ("bf16", 300, 264, 4099, dict(pad=64)),
+    ("f16", 333, 1000, 1500, dict(smoothing=0.1, left_out=0.4, weights=False, scale=1 / 333)),
+    ("bf16", 700, 512, 3001, dict(weights=False)),
+    ("f32", 515, 136, 700, dict(weights=False, scale=-3.0)),
+    ("bf16", 2100, 64, 300, dict(left_out=0.1)),
+]
+
+
+@pytest.mark.parametrize("dtype,rows,width,vocab,more", SHAPES)
+def test_losses_and_gradients(dtype, rows, width, vocab, more):
+    c = Case(dtype, rows, width, vocab, **more)
+    c.forward()
+    c.check(("losses", "logs"))
+    before = c.losses.clone(), c.logs.clone()
+    c.losses.fill_(7.0), c.logs.fill_(7.0)
+    c.backward()
+    c.check()
+    assert torch.equal(before[0], c.losses) and torch.equal(before[1], c.logs)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_the_tiles_of_large_problems(dtype):
+    """Products of 256 x 256 tiles and of 128 x 128, ragged on every side."""
+    c = Case(dtype, 1500, 520, 9001, left_out=0.15)
+    c.backward()
+    c.check()
+    c = Case(dtype, 520, 2056, 4100)
+    c.backward()
+    c.check()
+
+
+def test_rows_that_do_not_count_are_not_read():
+    c = Case("bf16", 90, 64, 500, seed=2)
+    c.targets[::3] = torch.tensor([-1, 500, -2 ** 63, 2 ** 62, 2 ** 32], device="cuda").repeat(6)
+    out = c.targets.ge(500) | c.targets.lt(0)
+    kept = c.H.clone()
+    c.H[out] = float("nan")
+    c.weights[out] = float("nan")
+    c.backward()
+    assert not c.losses[out].any() and not c.logs[out].any() and not c.dH[out].any()
+    c.H, c.weights = kept, torch.where(out, 0.0, c.weights)
+    c.check()
+
+
+def test_no_row_counts():
+    c = Case("f16", 40, 64, 500, left_out=1.1)
+    c.backward()
+    assert not c.losses.any() and not c.dH.any() and not c.dW.any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_wide_logits(dtype):
+    """Logits of some hundreds: most probabilities underflow, some rows have one word with all of it."""
+    c = Case(dtype, 100, 64, 800, reach=40.0, seed=4)
+    c.backward()
+    c.check()
+
+
+def test_one_gradient_alone():
+    c = Case("bf16", 200, 128, 900, seed=5)
+    c.backward()
+    both = c.dH.clone(), c.dW.clone()
+    c.dH.fill_(7.0), c.dW.fill_(7.0)
+    c.backward(dW=False)
+    assert torch.equal(c.dH, both[0]) and bool((c.dW == 7.0).all())
+    c.dH.fill_(7.0)
+    c.backward(dH=False)
+    assert torch.equal(c.dW, both[1]) and bool((c.dH == 7.0).all())
+
+
+def test_the_same_bits_from_run_to_run():
+    c = Case("f16", 600, 256, 5000, left_out=0.2, seed=6)
+    c.backward()
+    first = [x.clone() for x in (c.losses, c.dH, c.dW)]
+    for _ in range(3):
+        c.dH.fill_(7.0), c.dW.fill_(7.0)
+        c.backward()
+        assert all(torch.equal(a, b) for a, b in zip(first, (c.losses, c.dH, c.dW)))
+
+
+def test_a_word_that_is_nan_stays_in_its_row_and_in_dw():
+    c = Case("bf16", 50, 64, 300, seed=7)
+    want = Case("bf16", 50, 64, 300, seed=7)
+    want.backward()
+    c.H[20, 5] = float("nan")
+    c.backward()
+    rest = torch.arange(50, device="cuda") != 20
+    assert torch.isnan(c.losses[20]) and torch.isnan(c.dH[20]).all()
+    assert torch.equal(c.losses[rest], want.losses[rest]) and torch.equal(c.dH[rest], want.dH[rest])
+
+
+def test_a_captured_call_repeats_with_other_rows():
+    """The rows that count are found on the device: a replay finds those that count then."""
+    c = Case("bf16", 300, 128, 1000, seed=8)
+    p = c.problem()
+    n = L.lsp_cross_entropy_backward_workspace_bytes(p, c.code)
+    ws = room(n)
+    g = L.cross_entropy_gradients(c.dH, c.dW, weights=c.weights)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        L.lsp_cross_entropy_backward(p, g, c.code, ws, n, torch.cuda.current_stream())
+    for k in range(4):
+        gen = torch.Generator().manual_seed(k)
+        targets = torch.randint(0, 1000, (300,), generator=gen)
+        targets[torch.rand(300, generator=gen) < 0.3 * k] = -100
+        c.targets.copy_(targets)
+        c.H.copy_(torch.randn(c.H.shape, generator=gen))
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        c.check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_blocks_of_rows(dtype):
+    """More rows than one block of exponentials holds: dW is a sum over blocks."""
+    vocab = 400000 if dtype == "bf16" else 200000                            # 1 GiB is 1280 rows of these
+    c = Case(dtype, 2900, 8, vocab, left_out=0.2, seed=9)
+    c.backward()
+    H, W, t, g = c.H.double(), c.W.double(), c.targets, c.weights.double()
+    rows = ((t >= 0) & (t < vocab)).nonzero().squeeze(1)
+    dH, dW, losses = torch.zeros_like(H), torch.zeros_like(W), torch.zeros(2900, dtype=torch.float64, device="cuda")
+    for some in rows.split(256):
+        z = H[some].mm(W.t().contiguous())
+        lse = torch.logsumexp(z, 1)
+        losses[some] = lse - z[torch.arange(len(some)), t[some]]
+        d = torch.exp(z - lse[:, None])
+        d[torch.arange(len(some)), t[some]] -= 1.0
+        d *= g[some, None]
+        dH[some] = d.mm(W)
+        dW += d.t().contiguous().mm(H[some])
+    # norms of the errors: fp32 sums of this many terms of random signs; 16 bits: two roundings of every probability (one of them of all), then the result's
+    u = ref.U[dtype]
+    for got, want in ((c.losses, losses), (c.dH, dH), (c.dW, dW)):
+        rel = float((got.double() - want).norm() / want.norm())
+        assert rel <= (2e-5 if dtype == "f32" or got is c.losses else 3 * u), rel
