@@ -15,6 +15,7 @@ struct AdamwGroup {
     AdamwStep      step;
     const float*   grad_scale;
     int64_t        pad;
+    double         one_minus_beta1, beta1, one_minus_beta2, beta2;      // states in 8 bits
     uint32_t       first[kMaxItems];               // workgroup that each tensor begins with; past the last tensor UINT32_MAX
     lsp_adamw_item item[kMaxItems];
 };

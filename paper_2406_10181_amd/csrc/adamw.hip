@@ -9,13 +9,19 @@
 
 namespace lsp {
 
-// The largest of 32 lanes, in all of them.  (row_ror by 8, 4, 2, 1 in the sixteens, then the two halves of 32.)  fmaxf passes over a NaN.
-template <int CTRL> __device__ __forceinline__ float max_lane(float x) {
-    return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, false)));
+// The largest of 32 lanes' numbers in fp64, none of them negative, in all of them: as integers, first the upper halves, then the lower halves of those that have the largest.
+// (Lane + 8, 4, 2, 1 of the sixteen, then the other sixteen.)
+__device__ __forceinline__ uint32_t top_of_32(uint32_t x) {
+    const auto step = [&](int y) { x = max(x, (uint32_t)y); };
+    step(__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xF, 0xF, false)); step(__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xF, 0xF, false));
+    step(__builtin_amdgcn_update_dpp(0, (int)x, 0x122, 0xF, 0xF, false)); step(__builtin_amdgcn_update_dpp(0, (int)x, 0x121, 0xF, 0xF, false));
+    step(__builtin_amdgcn_ds_swizzle((int)x, 0x401F));
+    return x;
 }
-__device__ __forceinline__ float max_of_32(float x) {
-    x = max_lane<0x128>(x); x = max_lane<0x124>(x); x = max_lane<0x122>(x); x = max_lane<0x121>(x);
-    return fmaxf(x, __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(x), 0x401F)));              // lane ^ 16
+__device__ __forceinline__ double max_of_32(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t high = top_of_32((uint32_t)(u >> 32)), low = top_of_32((uint32_t)(u >> 32) == high ? (uint32_t)u : 0u);
+    return __builtin_bit_cast(double, (uint64_t)high << 32 | low);
 }
 
 __device__ __forceinline__ Eight load_any(const void* p, int64_t at, int left, int dtype) {
@@ -33,65 +39,67 @@ __device__ __forceinline__ void store_any(void* p, int64_t at, const Eight& x, i
 // Eight bytes, of which `left` there are
 __device__ __forceinline__ u32x2 load_codes(const uint8_t* p, int left) {
     if (left >= 8) return *reinterpret_cast<const u32x2*>(p);
-    u32x2 w = {0, 0};
-    for (int e = 0; e < left; ++e) w[e >> 2] |= (uint32_t)p[e] << (8 * (e & 3));
-    return w;
+    uint32_t a = 0, b = 0;
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+        if (e < left) (e < 4 ? a : b) |= (uint32_t)p[e] << (8 * (e & 3));
+    return u32x2{a, b};
 }
 __device__ __forceinline__ void store_codes(uint8_t* p, u32x2 w, int left) {
     if (left >= 8) { *reinterpret_cast<u32x2*>(p) = w; return; }
-    for (int e = 0; e < left; ++e) p[e] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+        if (e < left) p[e] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
 }
 
-// e4m3 and back: the conversions of the vector unit, to nearest even; what is above 448 (a quotient's last bit) is 448
-__device__ __forceinline__ Eight widen_m(u32x2 w, float scale) {
-    Eight r;
+// States in 8 bits are computed in fp64 up to their rounding, so that what lies near the border between two codes gets the one that the formulas say.  (A product in fp64 takes the
+// vector unit no longer than one in fp32.)
+struct EightWide { double x[8]; };
+
+// e4m3 and back: the conversions of the vector unit, to nearest even; a quotient above 448, by a last bit, is 448
+__device__ __forceinline__ EightWide widen_m(u32x2 w, float scale) {
+    EightWide r;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], true);
-        r.x[4 * k] = a[0] * scale; r.x[4 * k + 1] = a[1] * scale; r.x[4 * k + 2] = b[0] * scale; r.x[4 * k + 3] = b[1] * scale;
+        r.x[4 * k] = a[0]; r.x[4 * k + 1] = a[1]; r.x[4 * k + 2] = b[0]; r.x[4 * k + 3] = b[1];
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.x[e] *= (double)scale;
     return r;
 }
-__device__ __forceinline__ float within(float x) { return x != x ? x : fminf(fmaxf(x, -448.0f), 448.0f); }
-__device__ __forceinline__ u32x2 narrow_m(const Eight& x) {
+__device__ __forceinline__ float within(double x) {
+    const float y = (float)x;
+    return y != y ? y : fminf(fmaxf(y, -448.0f), 448.0f);
+}
+__device__ __forceinline__ u32x2 narrow_m(const EightWide& x, double inverse) {
     u32x2 w;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        int c = __builtin_amdgcn_cvt_pk_fp8_f32(within(x.x[4 * k]), within(x.x[4 * k + 1]), 0, false);
-        c = __builtin_amdgcn_cvt_pk_fp8_f32(within(x.x[4 * k + 2]), within(x.x[4 * k + 3]), c, true);
+        int c = __builtin_amdgcn_cvt_pk_fp8_f32(within(x.x[4 * k] * inverse), within(x.x[4 * k + 1] * inverse), 0, false);
+        c = __builtin_amdgcn_cvt_pk_fp8_f32(within(x.x[4 * k + 2] * inverse), within(x.x[4 * k + 3] * inverse), c, true);
         w[k] = (uint32_t)c;
     }
     return w;
 }
 // v's codes are the upper bits of an fp32 number without its sign: five of exponent (2^-31 .. 1) and three of mantissa
 constexpr uint32_t kLowest = (127 - 31) << 3;
-__device__ __forceinline__ Eight widen_v(u32x2 w, float scale) {
-    Eight r;
+__device__ __forceinline__ EightWide widen_v(u32x2 w, float scale) {
+    EightWide r;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const uint32_t c = (w[e >> 2] >> (8 * (e & 3))) & 0xFFu;
-        r.x[e] = c ? __uint_as_float((c + kLowest) << 20) * scale : 0.0f;
+        r.x[e] = (double)(c ? __uint_as_float((c + kLowest) << 20) : 0.0f) * (double)scale;
     }
     return r;
 }
-
-// One over a scale and its block's numbers are taken as 2^120 times as large where they are tiny, so that neither is infinite or loses digits
-struct Quotient {
-    float up, inverse;
-    __device__ __forceinline__ Quotient(float largest, float top) {
-        up = largest < 0x1p-90f ? 0x1p120f : 1.0f;
-        inverse = largest > 0.0f ? top / (largest * up) : 0.0f;
-    }
-    __device__ __forceinline__ float operator()(float x) const { return (x * up) * inverse; }
-};
-
-__device__ __forceinline__ u32x2 narrow_v(const Eight& x, const Quotient& q) {
+__device__ __forceinline__ u32x2 narrow_v(const EightWide& x, double inverse) {
     u32x2 w = {0, 0};
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const uint32_t u = __float_as_uint(q(x.x[e]));
+        const uint32_t u = __float_as_uint((float)(x.x[e] * inverse));
         const int c = (int)((u + 0x7FFFFu + ((u >> 20) & 1u)) >> 20) - (int)kLowest;
-        w[e >> 2] |= (x.x[e] > 0.0f ? (uint32_t)min(max(c, 1), 255) : 0u) << (8 * (e & 3));
+        w[e >> 2] |= (x.x[e] > 0.0 ? (uint32_t)min(max(c, 1), 255) : 0u) << (8 * (e & 3));
     }
     return w;
 }
@@ -115,50 +123,55 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw(AdamwGroup unused) {
     float* const master = global_pointer(item.master);
     const int dtype = item.dtype, grad_dtype = item.grad_dtype;
     const float rate = step.rate * item.rate_factor, decay = item.decay;
-    Eight p, d, m, v;
+    const auto update = [&](float p, float m, float v) {
+        const float by = m * step.inv_c1 / (sqrtf(v * step.inv_c2) + step.eps);
+        return fmaf(-rate, fmaf(decay, p, by), p);
+    };
+    const auto load_param = [&] { return master ? load_eight<F32>(master + at, left) : load_any(param, at, left, dtype); };
+    const auto store_param = [&](const Eight& p) {
+        if (master) store_eight<F32>(master + at, p, left);
+        store_any(param, at, p, left, dtype);
+    };
     if constexpr (BITS8) {
-        const int64_t of_scale = left > 0 ? at / kAdamwBlock : 0;
-        const float ms = global_pointer(item.m_scale)[of_scale], vs = global_pointer(item.v_scale)[of_scale];
-        const u32x2 mw = load_codes(static_cast<const uint8_t*>(global_pointer(item.m)) + at, left), vw = load_codes(static_cast<const uint8_t*>(global_pointer(item.v)) + at, left);
-        d = load_any(grad, at, left, grad_dtype);
-        p = master ? load_eight<F32>(master + at, left) : load_any(param, at, left, dtype);
-        m = widen_m(mw, ms); v = widen_v(vw, vs);
-    } else {
-        m = load_eight<F32>(static_cast<const float*>(global_pointer(item.m)) + at, left);
-        v = load_eight<F32>(static_cast<const float*>(global_pointer(item.v)) + at, left);
-        d = load_any(grad, at, left, grad_dtype);
-        p = master ? load_eight<F32>(master + at, left) : load_any(param, at, left, dtype);
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float x = d.x[e] * grad_scale;
-        m.x[e] = fmaf(step.beta1, m.x[e], step.one_minus_beta1 * x);
-        v.x[e] = fmaf(step.beta2, v.x[e], step.one_minus_beta2 * x * x);
-        const float by = m.x[e] * step.inv_c1 / (sqrtf(v.x[e] * step.inv_c2) + step.eps);
-        p.x[e] = fmaf(-rate, fmaf(decay, p.x[e], by), p.x[e]);
-    }
-    if (master) store_eight<F32>(master + at, p, left);
-    store_any(param, at, p, left, dtype);
-    if constexpr (BITS8) {
-        float largest_m = 0.0f, largest_v = 0.0f;
+        uint8_t* const m_at = static_cast<uint8_t*>(global_pointer(item.m)) + at;
+        uint8_t* const v_at = static_cast<uint8_t*>(global_pointer(item.v)) + at;
+        float* const m_scale = global_pointer(item.m_scale) + (left > 0 ? at / kAdamwBlock : 0);
+        float* const v_scale = global_pointer(item.v_scale) + (left > 0 ? at / kAdamwBlock : 0);
+        const float ms = *m_scale, vs = *v_scale;
+        const u32x2 mw = load_codes(m_at, left), vw = load_codes(v_at, left);
+        const Eight d = load_any(grad, at, left, grad_dtype);
+        Eight p = load_param();
+        EightWide m = widen_m(mw, ms), v = widen_v(vw, vs);
+        double top_m = 0.0, top_v = 0.0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            if (e >= left) { m.x[e] = 0.0f; v.x[e] = 0.0f; }
-            largest_m = fmaxf(largest_m, fabsf(m.x[e])); largest_v = fmaxf(largest_v, v.x[e]);
+            const double x = (double)d.x[e] * (double)grad_scale;
+            m.x[e] = g->beta1 * m.x[e] + g->one_minus_beta1 * x;
+            v.x[e] = g->beta2 * v.x[e] + g->one_minus_beta2 * x * x;
+            p.x[e] = update(p.x[e], (float)m.x[e], (float)v.x[e]);
+            if (e < left) { top_m = fmax(top_m, fabs(m.x[e])); top_v = fmax(top_v, v.x[e]); }            // (past a NaN)
         }
-        largest_m = max_of_32(largest_m); largest_v = max_of_32(largest_v);
-        const Quotient qm(largest_m, 448.0f), qv(largest_v, 1.875f);
-        if ((threadIdx.x & 31) == 0 && left > 0) {
-            global_pointer(item.m_scale)[at / kAdamwBlock] = largest_m / 448.0f;
-            global_pointer(item.v_scale)[at / kAdamwBlock] = largest_v / 1.875f;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) m.x[e] = qm(m.x[e]);
-        store_codes(static_cast<uint8_t*>(global_pointer(item.m)) + at, narrow_m(m), left);
-        store_codes(static_cast<uint8_t*>(global_pointer(item.v)) + at, narrow_v(v, qv), left);
+        store_param(p);
+        top_m = max_of_32(top_m); top_v = max_of_32(top_v);
+        if ((threadIdx.x & 31) == 0 && left > 0) { *m_scale = (float)(top_m / 448.0); *v_scale = (float)(top_v / 1.875); }
+        store_codes(m_at, narrow_m(m, top_m > 0.0 ? 448.0 / top_m : 0.0), left);
+        store_codes(v_at, narrow_v(v, top_v > 0.0 ? 1.875 / top_v : 0.0), left);
     } else {
-        store_eight<F32>(static_cast<float*>(global_pointer(item.m)) + at, m, left);
-        store_eight<F32>(static_cast<float*>(global_pointer(item.v)) + at, v, left);
+        float* const m_at = static_cast<float*>(global_pointer(item.m)) + at;
+        float* const v_at = static_cast<float*>(global_pointer(item.v)) + at;
+        Eight m = load_eight<F32>(m_at, left), v = load_eight<F32>(v_at, left);
+        const Eight d = load_any(grad, at, left, grad_dtype);
+        Eight p = load_param();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = d.x[e] * grad_scale;
+            m.x[e] = fmaf(step.beta1, m.x[e], step.one_minus_beta1 * x);
+            v.x[e] = fmaf(step.beta2, v.x[e], step.one_minus_beta2 * x * x);
+            p.x[e] = update(p.x[e], m.x[e], v.x[e]);
+        }
+        store_param(p);
+        store_eight<F32>(m_at, m, left);
+        store_eight<F32>(v_at, v, left);
     }
 }
 

@@ -95,41 +95,49 @@ __global__ __launch_bounds__((LossProduct<D, TILE, false, false>::kThreads)) voi
     const int64_t w_bytes = a.w_stride * D::size, h_bytes = (int64_t)a.width * D::size;
     P p;
     p.run({static_cast<const uint8_t*>(a.W) + v0 * w_bytes, w_bytes}, {a.packed + r0 * h_bytes, h_bytes}, a.width, max(a.vocab - v0, 0), P::BN, lds);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM, h = lane >> 5;
     const int first = v0 + wm * 32 * P::MI;                                               // of the wave's piece
     const int64_t piece = first / (32 * P::MI);
 #pragma unroll
     for (int j = 0; j < P::NI; ++j) {
         const int row = r0 + 32 * (wn * P::NI + j) + (lane & 31);
-        const int target = a.target[row];
-        float top = -INFINITY, plain = 0.0f;
+        const int want = a.target[row] - first - 4 * h;                                   // (a lane has v = first + 4 h + these)
+        float hit = 0.0f, plain = 0.0f;
 #pragma unroll
         for (int i = 0; i < P::MI; ++i)
 #pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                const int v = first + 32 * i + 8 * (x / 4) + 4 * h + x % 4;
-                const float z = p.acc[j][i][x];
-                if (v == target) a.hit[row] = z;
-                if (v < a.vocab) { top = fmaxf(top, z); plain += z; }
-            }
-        top = halves_max(top);
-        const float from = top == -INFINITY ? 0.0f : top;
-        float sum = 0.0f;
+            for (int x = 0; x < 16; ++x) hit = want == 32 * i + 8 * (x / 4) + x % 4 ? p.acc[j][i][x] : hit;
+        if (want >= 0 && want < 32 * P::MI && !(want & 4)) a.hit[row] = hit;
+        if (a.smoothing > 0.0f) {                                                         // (z behind the vocabulary is 0)
 #pragma unroll
-        for (int i = 0; i < P::MI; ++i)
+            for (int i = 0; i < P::MI; ++i)
 #pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                const int v = first + 32 * i + 8 * (x / 4) + 4 * h + x % 4;
-                const float e = v < a.vocab ? __builtin_amdgcn_exp2f((p.acc[j][i][x] - from) * kLossLog2e) : 0.0f;
-                sum += e;
-                p.acc[j][i][x] = e;
-            }
-        sum = halves_sum(sum);
-        if (h == 0) { a.top[piece * a.block_rows + row] = top; a.sum[piece * a.block_rows + row] = sum; }
-        if (a.smoothing > 0.0f) {
+                for (int x = 0; x < 16; ++x) plain += p.acc[j][i][x];
             plain = halves_sum(plain);
             if (h == 0) a.plain[piece * a.block_rows + row] = plain;
         }
+        if (first + 32 * P::MI > a.vocab) {
+#pragma unroll
+            for (int i = 0; i < P::MI; ++i)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) p.acc[j][i][x] = first + 4 * h + 32 * i + 8 * (x / 4) + x % 4 < a.vocab ? p.acc[j][i][x] : -INFINITY;
+        }
+        float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < P::MI; ++i)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) top = fmaxf(top, p.acc[j][i][x]);
+        top = halves_max(top);
+        const float from = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int i = 0; i < P::MI; ++i)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                p.acc[j][i][x] = __builtin_amdgcn_exp2f((p.acc[j][i][x] - from) * kLossLog2e);
+                sum += p.acc[j][i][x];
+            }
+        sum = halves_sum(sum);
+        if (h == 0) { a.top[piece * a.block_rows + row] = top; a.sum[piece * a.block_rows + row] = sum; }
     }
     if (!a.train) return;
     const Lds own = lds + wave * (32 * 32 * P::MI * D::size);
@@ -157,7 +165,7 @@ __global__ __launch_bounds__((LossProduct<D, TILE, true, false>::kThreads)) void
     const int64_t w_bytes = a.w_stride * D::size, e_bytes = (int64_t)a.padded * D::size;
     P p;
     p.run({static_cast<const uint8_t*>(a.W) + v0 * w_bytes + (int64_t)d0 * D::size, w_bytes}, {a.e + r0 * e_bytes + (int64_t)v0 * D::size, e_bytes}, v1 - v0, a.width - d0, P::BN, lds);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM;
     const int first = d0 + wm * 32 * P::MI, left = a.width - first;
     const float factor = 1.0f / gradient_scale<D>(a);
 #pragma unroll
@@ -192,7 +200,7 @@ __global__ __launch_bounds__((LossProduct<D, TILE, true, true>::kThreads)) void 
     P p;
     // (up to whole steps: the rows behind those that count are zeros in both)
     p.run({a.packed + (int64_t)d0 * D::size, h_bytes}, {a.e + (int64_t)v0 * D::size, e_bytes}, (rows + P::BK - 1) / P::BK * P::BK, a.width - d0, P::BN, lds);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM;
     const int first = d0 + wm * 32 * P::MI, left = a.width - first;
     const float factor = 1.0f / gradient_scale<D>(a);
 #pragma unroll

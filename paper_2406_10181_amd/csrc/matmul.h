@@ -22,46 +22,48 @@ template <typename D, int N, int BK, int WAVES, bool ACROSS> struct OperandTile 
     static constexpr int kLoads = kBytes / 1024, kCount = (kLoads + WAVES - 1) / WAVES;
     static_assert(kBytes % 1024 == 0 && kLoads % WAVES == 0, "whole loads for every wave");
     uint32_t off[kCount];
-    int      k[kCount];                               // of the step's k that this load has
-    uint32_t row_at[2], column_at[2];
+    uint32_t at[2];                                   // where this lane reads: see frag()
 
+    // Which k of a step load i has
+    __device__ __forceinline__ static int k_of(int i, int wave, int lane) {
+        uint32_t r, unit;
+        T::at_place((i * WAVES + wave) * 64 + lane, r, unit);
+        return ACROSS ? (int)r : (int)unit * T::kUnitElems;
+    }
     // `there`: how many of the N there are
     __device__ __forceinline__ void setup(int64_t row_bytes, int there, int wave, int lane) {
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
             uint32_t r, unit;
             T::at_place((i * WAVES + wave) * 64 + lane, r, unit);
-            const int column = (int)unit * T::kUnitElems;
-            k[i] = ACROSS ? (int)r : column;
-            off[i] = (ACROSS ? column : (int)r) < there ? r * (uint32_t)row_bytes + unit * 16u : kNowhere;
+            off[i] = (ACROSS ? (int)unit * T::kUnitElems : (int)r) < there ? r * (uint32_t)row_bytes + unit * 16u : kNowhere;
         }
         const uint32_t row = lane & 31, h = (uint32_t)lane >> 5;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            if constexpr (D::size == 2) {
-                row_at[x] = T::place(row, 2 * x + h);
-                column_at[x] = T::place(8 * h + 4 * x + ((lane >> 2) & 3), ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8u;
-            } else {
-                row_at[x] = T::place(row, 2 * h + x);
-                column_at[x] = T::place(8 * h + 4 * x, (lane & 31) >> 2) + (lane & 3) * 4u;
-            }
+            if constexpr (D::size == 2)
+                at[x] = ACROSS ? T::place(8 * h + 4 * x + ((lane >> 2) & 3), ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8u : T::place(row, 2 * x + h);
+            else
+                at[x] = ACROSS ? T::place(8 * h + 4 * x, (lane & 31) >> 2) + (lane & 3) * 4u : T::place(row, 2 * h + x);
         }
     }
-    // The step that begins at `first` and has `left` of k
-    __device__ __forceinline__ void fetch(const uint8_t* first, int left, Lds tile, int wave) const {
+    // The step that begins at `first`; PART: only `left` of its k are there
+    template <bool PART> __device__ __forceinline__ void fetch(const uint8_t* first, int left, Lds tile, int wave, int lane) const {
         const Buffer b = buffer_from(first);
 #pragma unroll
-        for (int i = 0; i < kCount; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (LSP_SHARED_AS void*)(tile + (i * WAVES + wave) * 1024u), 16, (int)(k[i] < left ? off[i] : kNowhere), 0, 0, 0);
+        for (int i = 0; i < kCount; ++i) {
+            const uint32_t o = PART && k_of(i, wave, lane) >= left ? kNowhere : off[i];
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (LSP_SHARED_AS void*)(tile + (i * WAVES + wave) * 1024u), 16, (int)o, 0, 0, 0);
+        }
     }
     // Rows (columns) 32 block + 0..31, k = 16 ks + 8 h + 0..7 for the lane's half h
     __device__ __forceinline__ Frag<D> frag(Lds tile, int block, int ks) const {
         Frag<D> f;
         if constexpr (!ACROSS) {
             const Lds t = tile + block * (32 / 4 * T::kUnits * 64);
-            if constexpr (D::size == 2) f.w = lds_read<u32x4>(t + row_at[ks & 1] + (ks >> 1) * 256);
+            if constexpr (D::size == 2) f.w = lds_read<u32x4>(t + at[ks & 1] + (ks >> 1) * 256);
             else {
-                const f32x4 a = lds_read<f32x4>(t + row_at[0] + ks * 256), b = lds_read<f32x4>(t + row_at[1] + ks * 256);
+                const f32x4 a = lds_read<f32x4>(t + at[0] + ks * 256), b = lds_read<f32x4>(t + at[1] + ks * 256);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) { f.w[j] = a[j]; f.w[4 + j] = b[j]; }
             }
@@ -70,14 +72,14 @@ template <typename D, int N, int BK, int WAVES, bool ACROSS> struct OperandTile 
             if constexpr (D::size == 2) {
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LSP_SHARED_AS s16x4*)(t + column_at[x]));
+                    const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LSP_SHARED_AS s16x4*)(t + at[x]));
                     u32x2 u;
                     __builtin_memcpy(&u, &v, 8);
                     f.w[2 * x] = u[0]; f.w[2 * x + 1] = u[1];
                 }
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) f.w[j] = lds_read<float>(t + column_at[j >> 2] + (j & 3) * 64);
+                for (int j = 0; j < 8; ++j) f.w[j] = lds_read<float>(t + at[j >> 2] + (j & 3) * 64);
             }
         }
         return f;
@@ -93,23 +95,32 @@ template <typename D, int BM_, int BN_, int WM_, int WN_, bool A_ACROSS, bool B_
 
     f32x16 acc[NI][MI];
 
-    __device__ __forceinline__ void step(const A& a, const B& b, Lds __restrict from, int wm, int wn) {
+    struct Frags { Frag<D> x[MI], y[NI]; };
+    __device__ __forceinline__ static void read(Frags& f, const A& a, const B& b, Lds from, int wm, int wn, int ks) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) f.x[i] = a.frag(from, wm * MI + i, ks);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) f.y[j] = b.frag(from + A::kBytes, wn * NI + j, ks);
+    }
+    // One step: while `from` is multiplied, `into` is filled.  The fragments of 16 k are read while those before are multiplied, and no further ahead: with the reads of a whole step
+    // ahead the accumulators would not stay in registers.
+    template <typename Fill> __device__ __forceinline__ void step(const A& a, const B& b, Lds __restrict from, Lds __restrict into, int wm, int wn, Fill&& fill) {
+        fill(into);
+        Frags f[2];
+        read(f[0], a, b, from, wm, wn, 0);
 #pragma unroll
         for (int ks = 0; ks < kSteps; ++ks) {
-            Frag<D> x[MI], y[NI];
-#pragma unroll
-            for (int i = 0; i < MI; ++i) x[i] = a.frag(from, wm * MI + i, ks);
-#pragma unroll
-            for (int j = 0; j < NI; ++j) y[j] = b.frag(from + A::kBytes, wn * NI + j, ks);
+            __builtin_amdgcn_sched_barrier(0);
+            if (ks + 1 < kSteps) read(f[(ks + 1) & 1], a, b, from, wm, wn, ks + 1);
 #pragma unroll
             for (int j = 0; j < NI; ++j)
 #pragma unroll
-                for (int i = 0; i < MI; ++i) acc[j][i] = mma<D>(x[i], y[j], acc[j][i]);
+                for (int i = 0; i < MI; ++i) acc[j][i] = mma<D>(f[ks & 1].x[i], f[ks & 1].y[j], acc[j][i]);
         }
     }
     // k from 0 to `length`; m_there, n_there: how many rows (columns) of the tile there are.  All waves are done with LDS when it returns.
-    __device__ __forceinline__ void run(const Operand& oa, const Operand& ob, int64_t length, int m_there, int n_there, Lds lds) {
-        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wm = wave % WM, wn = wave / WM;
+    __device__ __forceinline__ void run(const Operand& oa, const Operand& ob, int length, int m_there, int n_there, Lds lds) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % WM, wn = wave / WM;
         A a;
         B b;
         a.setup(oa.row_bytes, m_there, wave, lane);
@@ -121,22 +132,23 @@ template <typename D, int BM_, int BN_, int WM_, int WN_, bool A_ACROSS, bool B_
         const int64_t a_step = A_ACROSS ? oa.row_bytes * BK : BK * D::size, b_step = B_ACROSS ? ob.row_bytes * BK : BK * D::size;
         const uint8_t* pa = oa.first;
         const uint8_t* pb = ob.first;
-        int64_t left = length;
+        int left = length;
         const auto fetch = [&](Lds into) {
-            const int n = (int)min(left, (int64_t)BK);
-            a.fetch(pa, n, into, wave);
-            b.fetch(pb, n, into + A::kBytes, wave);
+            if (left >= BK) {
+                a.template fetch<false>(pa, left, into, wave, lane);
+                b.template fetch<false>(pb, left, into + A::kBytes, wave, lane);
+            } else if (left > 0) {
+                a.template fetch<true>(pa, left, into, wave, lane);
+                b.template fetch<true>(pb, left, into + A::kBytes, wave, lane);
+            }
             pa += a_step; pb += b_step; left -= BK;
         };
-        if (left > 0) fetch(lds);
-        for (int64_t k = 0; k < length; k += 2 * BK) {
+        fetch(lds);
+        const int steps = (length + BK - 1) / BK;
+        for (int t = 0; t < steps; ++t) {
+            const uint32_t now = (t & 1) * kStage;
             arrived_for_all();
-            if (left > 0) fetch(lds + kStage);
-            step(a, b, lds, wm, wn);
-            if (k + BK >= length) break;
-            arrived_for_all();
-            if (left > 0) fetch(lds);
-            step(a, b, lds + kStage, wm, wn);
+            step(a, b, lds + now, lds + (kStage - now), wm, wn, fetch);
         }
         __syncthreads();
     }

@@ -218,6 +218,7 @@ int lsp_adamw(const lsp_adamw_item* items, int32_t count, lsp_state states, doub
     lsp::AdamwGroup g{};
     g.step = {(float)(1.0 - beta1), (float)beta1, (float)(1.0 - beta2), (float)beta2, (float)(1.0 / (1.0 - std::pow(beta1, (double)step))),
               (float)(1.0 / (1.0 - std::pow(beta2, (double)step))), (float)eps, (float)rate};
+    g.one_minus_beta1 = 1.0 - beta1; g.beta1 = beta1; g.one_minus_beta2 = 1.0 - beta2; g.beta2 = beta2;
     g.grad_scale = grad_scale;
     for (int32_t first = 0; first < count; first += lsp::kMaxItems) {
         uint32_t total = 0;
