@@ -618,12 +618,12 @@ int    lsp_cross_entropy_backward(const lsp_cross_entropy_problem* problem, cons
  * LSP_STATE_F32: m and v are fp32.  LSP_STATE_8BIT: bytes; 256 elements that follow one another (the last ones of a tensor: fewer) share an fp32 scale.  m is e4m3 (4 bits
  * of exponent, 3 of mantissa, largest 448) times m_scale; v is without sign, 5 bits of exponent and 3 of mantissa: code 0 is 0 and code c otherwise
  * 2^((c >> 3) - 31) * (1 + (c & 7) / 8) (largest 1.875), times v_scale.  The step takes m and v before they are rounded (to nearest, ties to even; a v
- * that is not 0 never becomes 0, so that no small v makes a large step); a scale is the block's largest magnitude over 448 or 1.875.  State that is all zeros,
+ * that is not 0 never becomes 0 (but below 2^-149 of the largest), so that no small v makes a large step); a scale is the block's largest magnitude over 448 or 1.875.  State that is all zeros,
  * codes and scales, is where training begins.  A gradient that is not finite spoils its element and, in 8 bits, can spoil its block's states.
  *   items       HOST array of `count` descriptors, 1 <= count <= LSP_MAX_TENSORS, read during the call only; no tensor twice, no overlaps
  *   step        number of this step, from 1 on (a captured call repeats it);  0 <= beta < 1, eps >= 0
  *   grad_scale  device, one fp32 (of clipping, or of a scaled loss), or NULL: 1.  Where it is not finite the step does nothing
- * At most 2^35 elements a call, all tensors padded to 2048. */
+ * At most 2^35 elements a call, all tensors padded to 4096. */
 typedef enum { LSP_STATE_F32 = 0, LSP_STATE_8BIT = 1 } lsp_state;
 
 typedef struct {

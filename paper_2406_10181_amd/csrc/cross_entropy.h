@@ -95,56 +95,56 @@ __global__ __launch_bounds__((LossProduct<D, TILE, false, false>::kThreads)) voi
     const int64_t w_bytes = a.w_stride * D::size, h_bytes = (int64_t)a.width * D::size;
     P p;
     p.run({static_cast<const uint8_t*>(a.W) + v0 * w_bytes, w_bytes}, {a.packed + r0 * h_bytes, h_bytes}, a.width, max(a.vocab - v0, 0), P::BN, lds);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM, h = lane >> 5;
-    const int first = v0 + wm * 32 * P::MI;                                               // of the wave's piece
-    const int64_t piece = first / (32 * P::MI);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM, g = lane >> 4;
+    const int first = v0 + wm * P::kRange;                                                // of the wave's piece
+    const int64_t piece = first / P::kRange;
 #pragma unroll
     for (int j = 0; j < P::NI; ++j) {
-        const int row = r0 + 32 * (wn * P::NI + j) + (lane & 31);
-        const int want = a.target[row] - first - 4 * h;                                   // (a lane has v = first + 4 h + these)
+        const int row = r0 + 16 * (wn * P::NI + j) + (lane & 15);
+        const int want = a.target[row] - first - 4 * g;                                   // (a lane has v = first + 4 g + 16 i + 0..3)
         float hit = 0.0f, plain = 0.0f;
 #pragma unroll
         for (int i = 0; i < P::MI; ++i)
 #pragma unroll
-            for (int x = 0; x < 16; ++x) hit = want == 32 * i + 8 * (x / 4) + x % 4 ? p.acc[j][i][x] : hit;
-        if (want >= 0 && want < 32 * P::MI && !(want & 4)) a.hit[row] = hit;
+            for (int x = 0; x < 4; ++x) hit = want == 16 * i + x ? p.acc[j][i][x] : hit;
+        if (want >= 0 && want < P::kRange && (want & 12) == 0) a.hit[row] = hit;
         if (a.smoothing > 0.0f) {                                                         // (z behind the vocabulary is 0)
 #pragma unroll
             for (int i = 0; i < P::MI; ++i)
 #pragma unroll
-                for (int x = 0; x < 16; ++x) plain += p.acc[j][i][x];
-            plain = halves_sum(plain);
-            if (h == 0) a.plain[piece * a.block_rows + row] = plain;
+                for (int x = 0; x < 4; ++x) plain += p.acc[j][i][x];
+            plain = quarters_sum(plain);
+            if (g == 0) a.plain[piece * a.block_rows + row] = plain;
         }
-        if (first + 32 * P::MI > a.vocab) {
+        if (first + P::kRange > a.vocab) {
 #pragma unroll
             for (int i = 0; i < P::MI; ++i)
 #pragma unroll
-                for (int x = 0; x < 16; ++x) p.acc[j][i][x] = first + 4 * h + 32 * i + 8 * (x / 4) + x % 4 < a.vocab ? p.acc[j][i][x] : -INFINITY;
+                for (int x = 0; x < 4; ++x) p.acc[j][i][x] = first + 4 * g + 16 * i + x < a.vocab ? p.acc[j][i][x] : -INFINITY;
         }
         float top = -INFINITY, sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < P::MI; ++i)
 #pragma unroll
-            for (int x = 0; x < 16; ++x) top = fmaxf(top, p.acc[j][i][x]);
-        top = halves_max(top);
+            for (int x = 0; x < 4; ++x) top = fmaxf(top, p.acc[j][i][x]);
+        top = quarters_max(top);
         const float from = top == -INFINITY ? 0.0f : top;
 #pragma unroll
         for (int i = 0; i < P::MI; ++i)
 #pragma unroll
-            for (int x = 0; x < 16; ++x) {
+            for (int x = 0; x < 4; ++x) {
                 p.acc[j][i][x] = __builtin_amdgcn_exp2f((p.acc[j][i][x] - from) * kLossLog2e);
                 sum += p.acc[j][i][x];
             }
-        sum = halves_sum(sum);
-        if (h == 0) { a.top[piece * a.block_rows + row] = top; a.sum[piece * a.block_rows + row] = sum; }
+        sum = quarters_sum(sum);
+        if (g == 0) { a.top[piece * a.block_rows + row] = top; a.sum[piece * a.block_rows + row] = sum; }
     }
     if (!a.train) return;
-    const Lds own = lds + wave * (32 * 32 * P::MI * D::size);
 #pragma unroll
-    for (int j = 0; j < P::NI; ++j) {
-        const int row0 = r0 + 32 * (wn * P::NI + j);
-        store_wave_rows<D, 32 * P::MI>(p.acc[j], kLossTop<D>, own, 32 * P::MI, lane, [&](uint32_t r) { return a.e + ((int64_t)(row0 + (int)r) * a.padded + first) * D::size; });
+    for (int j = 0; j < P::NI; j += 2) {
+        const int row0 = r0 + 16 * (wn * P::NI + j);
+        store_two_blocks<D, P::MI>(p.acc + j, kLossTop<D>, lds + wave * (32 * P::kRange * D::size), P::kRange, lane,
+                                   [&](uint32_t r) { return a.e + ((int64_t)(row0 + (int)r) * a.padded + first) * D::size; });
     }
 }
 
@@ -166,17 +166,17 @@ __global__ __launch_bounds__((LossProduct<D, TILE, true, false>::kThreads)) void
     P p;
     p.run({static_cast<const uint8_t*>(a.W) + v0 * w_bytes + (int64_t)d0 * D::size, w_bytes}, {a.e + r0 * e_bytes + (int64_t)v0 * D::size, e_bytes}, v1 - v0, a.width - d0, P::BN, lds);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM;
-    const int first = d0 + wm * 32 * P::MI, left = a.width - first;
+    const int first = d0 + wm * P::kRange, left = a.width - first;
     const float factor = 1.0f / gradient_scale<D>(a);
 #pragma unroll
-    for (int j = 0; j < P::NI; ++j) {
-        const int row0 = r0 + 32 * (wn * P::NI + j);
+    for (int j = 0; j < P::NI; j += 2) {
+        const int row0 = r0 + 16 * (wn * P::NI + j);
         if (a.dh_splits > 1) {
             float* const to = a.dh_parts + (int64_t)split * a.block_rows * a.width + first;
-            store_wave_rows<F32, 32 * P::MI>(p.acc[j], factor, lds + wave * (32 * 32 * P::MI * 4), left, lane,
-                                             [&](uint32_t r) { return reinterpret_cast<uint8_t*>(to + (int64_t)(row0 + (int)r) * a.width); });
+            store_two_blocks<F32, P::MI>(p.acc + j, factor, lds + wave * (32 * P::kRange * 4), left, lane,
+                                         [&](uint32_t r) { return reinterpret_cast<uint8_t*>(to + (int64_t)(row0 + (int)r) * a.width); });
         } else {
-            store_wave_rows<D, 32 * P::MI>(p.acc[j], factor, lds + wave * (32 * 32 * P::MI * D::size), left, lane, [&](uint32_t r) -> uint8_t* {
+            store_two_blocks<D, P::MI>(p.acc + j, factor, lds + wave * (32 * P::kRange * D::size), left, lane, [&](uint32_t r) -> uint8_t* {
                 const int row = row0 + (int)r;
                 return row < rows ? static_cast<uint8_t*>(a.dH) + (a.index[a.block * a.block_rows + row] * a.dh_stride + first) * D::size : nullptr;
             });
@@ -201,22 +201,21 @@ __global__ __launch_bounds__((LossProduct<D, TILE, true, true>::kThreads)) void 
     // (up to whole steps: the rows behind those that count are zeros in both)
     p.run({a.packed + (int64_t)d0 * D::size, h_bytes}, {a.e + (int64_t)v0 * D::size, e_bytes}, (rows + P::BK - 1) / P::BK * P::BK, a.width - d0, P::BN, lds);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM;
-    const int first = d0 + wm * 32 * P::MI, left = a.width - first;
+    const int first = d0 + wm * P::kRange, left = a.width - first;
     const float factor = 1.0f / gradient_scale<D>(a);
 #pragma unroll
-    for (int j = 0; j < P::NI; ++j) {
-        const int row0 = v0 + 32 * (wn * P::NI + j);
+    for (int j = 0; j < P::NI; j += 2) {
+        const int row0 = v0 + 16 * (wn * P::NI + j);
         if (a.blocks > 1) {
             // the sum so far is added in registers: a lane has four d that follow one another
             float* const so_far = D::size == 4 ? static_cast<float*>(a.dW) : a.dw_sum;
             const int64_t stride = D::size == 4 ? a.dw_stride : a.width;
-            const int v = row0 + (lane & 31);
 #pragma unroll
-            for (int i = 0; i < P::MI; ++i)
+            for (int jj = j; jj < j + 2; ++jj)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int d = first + 32 * i + 8 * g + 4 * (lane >> 5);
-                    f32x4 x = {p.acc[j][i][4 * g] * factor, p.acc[j][i][4 * g + 1] * factor, p.acc[j][i][4 * g + 2] * factor, p.acc[j][i][4 * g + 3] * factor};
+                for (int i = 0; i < P::MI; ++i) {
+                    const int v = row0 + 16 * (jj - j) + (lane & 15), d = first + 16 * i + 4 * (lane >> 4);
+                    f32x4 x = p.acc[jj][i] * factor;
                     if (v < a.vocab && d < a.width) {
                         f32x4* const at = reinterpret_cast<f32x4*>(so_far + v * stride + d);
                         if (a.block > 0) x += *at;
@@ -225,7 +224,7 @@ __global__ __launch_bounds__((LossProduct<D, TILE, true, true>::kThreads)) void 
                     }
                 }
         } else {
-            store_wave_rows<D, 32 * P::MI>(p.acc[j], factor, lds + wave * (32 * 32 * P::MI * D::size), left, lane, [&](uint32_t r) -> uint8_t* {
+            store_two_blocks<D, P::MI>(p.acc + j, factor, lds + wave * (32 * P::kRange * D::size), left, lane, [&](uint32_t r) -> uint8_t* {
                 const int v = row0 + (int)r;
                 return v < a.vocab ? static_cast<uint8_t*>(a.dW) + (v * a.dw_stride + first) * D::size : nullptr;
             });
@@ -248,14 +247,18 @@ template <typename D, int TILE> static inline hipError_t launch_dh_of(const Loss
 template <typename D, int TILE> static inline hipError_t launch_dw_of(const LossArgs& a, hipStream_t st) {
     return launch_tiles<LossProduct<D, TILE, true, true>, &k_loss_dw<D, TILE>>(a, (uint32_t)((a.width + TILE - 1) / TILE * ((a.vocab + TILE - 1) / TILE)), st);
 }
+// (fp32: fragments of 256 x 256 tiles would not find room in the registers)
 template <typename D> hipError_t launch_loss_logits(const LossArgs& a, hipStream_t st) {
-    return a.tile[0] == 256 ? launch_logits_of<D, 256>(a, st) : a.tile[0] == 128 ? launch_logits_of<D, 128>(a, st) : launch_logits_of<D, 64>(a, st);
+    if constexpr (D::size == 2) if (a.tile[0] == 256) return launch_logits_of<D, 256>(a, st);
+    return a.tile[0] == 128 ? launch_logits_of<D, 128>(a, st) : launch_logits_of<D, 64>(a, st);
 }
 template <typename D> hipError_t launch_loss_dh(const LossArgs& a, hipStream_t st) {
-    return a.tile[1] == 256 ? launch_dh_of<D, 256>(a, st) : a.tile[1] == 128 ? launch_dh_of<D, 128>(a, st) : launch_dh_of<D, 64>(a, st);
+    if constexpr (D::size == 2) if (a.tile[1] == 256) return launch_dh_of<D, 256>(a, st);
+    return a.tile[1] == 128 ? launch_dh_of<D, 128>(a, st) : launch_dh_of<D, 64>(a, st);
 }
 template <typename D> hipError_t launch_loss_dw(const LossArgs& a, hipStream_t st) {
-    return a.tile[2] == 256 ? launch_dw_of<D, 256>(a, st) : a.tile[2] == 128 ? launch_dw_of<D, 128>(a, st) : launch_dw_of<D, 64>(a, st);
+    if constexpr (D::size == 2) if (a.tile[2] == 256) return launch_dw_of<D, 256>(a, st);
+    return a.tile[2] == 128 ? launch_dw_of<D, 128>(a, st) : launch_dw_of<D, 64>(a, st);
 }
 #endif
 

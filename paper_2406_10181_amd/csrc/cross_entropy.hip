@@ -190,7 +190,7 @@ static double products_us(int64_t m, int64_t n, int64_t length, int tile, int sp
     return (double)((tiles + 255) / 256) * 2.0 * tile * tile * (double)((length + splits - 1) / splits) / rate;
 }
 static int best_tile(int64_t m, int64_t n, int64_t length, bool fp32) {
-    int best = 256;
+    int best = fp32 ? 128 : 256;
     for (const int tile : {128, 64})
         if (products_us(m, n, length, tile, 1, fp32) < products_us(m, n, length, best, 1, fp32)) best = tile;
     return best;
@@ -213,6 +213,7 @@ void plan_loss(LossArgs& a, lsp_dtype dtype) {
     double least = 1e30;
     for (const int tile : {256, 128, 64})
         for (int s = 1; s <= 32; ++s) {
+            if (fp32 && tile == 256) continue;
             const double us = products_us(a.width, rows, a.vocab, tile, s, fp32) + (s > 1 ? 4.0 + 8e-6 * (double)s * (double)rows * a.width / 4.0 : 0.0);
             if (us < least) { least = us; a.tile[1] = tile; a.dh_splits = s; }
         }

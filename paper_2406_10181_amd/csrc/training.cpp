@@ -216,8 +216,8 @@ int lsp_adamw(const lsp_adamw_item* items, int32_t count, lsp_state states, doub
         if (blocks >= kMostLaunch) return LSP_ERR_SHAPE;
     }
     lsp::AdamwGroup g{};
-    g.step = {(float)(1.0 - beta1), (float)beta1, (float)(1.0 - beta2), (float)beta2, (float)(1.0 / (1.0 - std::pow(beta1, (double)step))),
-              (float)(1.0 / (1.0 - std::pow(beta2, (double)step))), (float)eps, (float)rate};
+    const double c1 = 1.0 - std::pow(beta1, (double)step), root2 = std::sqrt(1.0 - std::pow(beta2, (double)step));
+    g.step = {(float)(1.0 - beta1), (float)beta1, (float)(1.0 - beta2), (float)beta2, (float)(eps * root2), (float)(rate * root2 / c1), (float)rate, 0.0f};
     g.one_minus_beta1 = 1.0 - beta1; g.beta1 = beta1; g.one_minus_beta2 = 1.0 - beta2; g.beta2 = beta2;
     g.grad_scale = grad_scale;
     for (int32_t first = 0; first < count; first += lsp::kMaxItems) {
@@ -225,9 +225,9 @@ int lsp_adamw(const lsp_adamw_item* items, int32_t count, lsp_state states, doub
         for (int k = 0; k < lsp::kMaxItems; ++k) {
             if (first + k < count) {
                 g.item[k] = items[first + k];
-                g.first[k] = total;
+                g.first[k] = (int32_t)total;
                 total += (uint32_t)((g.item[k].elements + lsp::kAdamwElements - 1) / lsp::kAdamwElements);
-            } else g.first[k] = UINT32_MAX;
+            } else g.first[k] = INT32_MAX;
         }
         const int rc = done(lsp::launch_adamw(g, total, bits8, static_cast<hipStream_t>(stream)));
         if (rc != LSP_OK) return rc;
