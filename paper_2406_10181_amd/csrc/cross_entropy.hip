@@ -77,16 +77,61 @@ __global__ __launch_bounds__(256) void k_loss_pack(LossArgs a, int row_bytes, in
     for (int k = threadIdx.x; k < row_bytes / 16; k += 256) to[k] = u32x4{0, 0, 0, 0};
 }
 
-// L and the loss of a row from its pieces: 16 rows a workgroup, 16 threads a row, each a running maximum and sum
-__global__ __launch_bounds__(256) void k_loss_rows(LossArgs a, int fp16) {
-    __shared__ float tops[16][17], sums[16][17], plains[16][17];
+// Both of these for few rows, in one launch: a workgroup has a row (or, from `rows` on, a row of zeros behind the packed ones) and counts those before it itself.
+constexpr int kFewRows = 2048;
+__global__ __launch_bounds__(256) void k_loss_pack_few(LossArgs a, int row_bytes, int elem) {
+    __shared__ int waves[4][2];
+    const int row = (int)min((int64_t)blockIdx.x, a.rows), rows = (int)a.rows;
+    int before = 0, all = 0;
+    for (int k = threadIdx.x; k < rows; k += 256) {
+        const int64_t t = a.targets[k];
+        const bool counts = t >= 0 && t < a.vocab;
+        before += counts && k < row;
+        all += counts;
+    }
+#pragma unroll
+    for (int d = 32; d; d /= 2) { before += __shfl_xor(before, d); all += __shfl_xor(all, d); }
+    if ((threadIdx.x & 63) == 0) { waves[threadIdx.x >> 6][0] = before; waves[threadIdx.x >> 6][1] = all; }
+    __syncthreads();
+    before = waves[0][0] + waves[1][0] + waves[2][0] + waves[3][0];
+    all = waves[0][1] + waves[1][1] + waves[2][1] + waves[3][1];
+    if (blockIdx.x == 0 && threadIdx.x == 0) { a.count[0] = all; a.count[1] = 0; }
+    const u32x4* from = nullptr;
+    u32x4* to = nullptr;
+    if ((int)blockIdx.x < rows) {
+        const int64_t target = a.targets[row];
+        if (target >= 0 && target < a.vocab) {
+            from = reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.H) + row * a.h_stride * elem);
+            to = reinterpret_cast<u32x4*>(a.packed + (int64_t)before * row_bytes);
+            if (threadIdx.x == 0) { a.index[before] = row; a.target[before] = (int)target; }
+        } else {
+            if (threadIdx.x == 0) {
+                a.losses[row] = 0.0f;
+                if (a.logs) a.logs[row] = 0.0f;
+            }
+            if (a.dH) to = reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.dH) + row * a.dh_stride * elem);
+        }
+    } else {
+        const int slot = all + (int)blockIdx.x - rows;
+        if (slot >= (all + 255) / 256 * 256) return;
+        to = reinterpret_cast<u32x4*>(a.packed + (int64_t)slot * row_bytes);
+        if (threadIdx.x == 0) a.target[slot] = -1;
+    }
+    if (!to) return;
+    for (int k = threadIdx.x; k < row_bytes / 16; k += 256) to[k] = from ? from[k] : u32x4{0, 0, 0, 0};
+}
+
+// L and the loss of a row from its pieces: 16 rows a workgroup, RUNS threads a row, each a running maximum and sum
+template <int RUNS>
+__global__ __launch_bounds__(16 * RUNS) void k_loss_rows(LossArgs a, int fp16) {
+    __shared__ float tops[RUNS][17], sums[RUNS][17], plains[RUNS][17];
     const int rows = rows_of_block(a), run = threadIdx.x >> 4, r = threadIdx.x & 15, row = blockIdx.x * 16 + r;
     if ((int)blockIdx.x * 16 >= rows) return;
     float top = -INFINITY, sum = 0.0f, plain = 0.0f;
     // (rows behind the last: the pieces are there, of packed zeros or of nothing yet, and nothing is made of them)
     if (row < rows) {
 #pragma unroll 4
-        for (int p = run; p < a.pieces; p += 16) {
+        for (int p = run; p < a.pieces; p += RUNS) {
             const int64_t at = (int64_t)p * a.block_rows + row;
             const float t = a.top[at], s = a.sum[at], higher = fmaxf(top, t), from = higher == -INFINITY ? 0.0f : higher;
             sum = sum * __builtin_amdgcn_exp2f((top - from) * kLossLog2e) + s * __builtin_amdgcn_exp2f((t - from) * kLossLog2e);
@@ -98,12 +143,12 @@ __global__ __launch_bounds__(256) void k_loss_rows(LossArgs a, int fp16) {
     __syncthreads();
     float bound = 0.0f;
     if (run == 0 && row < rows) {
-#pragma unroll
-        for (int k = 1; k < 16; ++k) top = fmaxf(top, tops[k][r]);
+#pragma unroll 16
+        for (int k = 1; k < RUNS; ++k) top = fmaxf(top, tops[k][r]);
         const float from = top == -INFINITY ? 0.0f : top;
         sum = plain = 0.0f;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
+#pragma unroll 16
+        for (int k = 0; k < RUNS; ++k) {
             sum += sums[k][r] * __builtin_amdgcn_exp2f((tops[k][r] - from) * kLossLog2e);
             plain += plains[k][r];
         }
@@ -129,7 +174,7 @@ __global__ __launch_bounds__(256) void k_loss_rows(LossArgs a, int fp16) {
     if (r == 0) atomicMax(reinterpret_cast<unsigned*>(a.count) + 1, __float_as_uint(bound));
 }
 
-constexpr int kDzColumns = 1024;                                         // of a workgroup of k_loss_dz, in steps of 128
+constexpr int kDzColumns = 512;                                          // of a workgroup of k_loss_dz, in steps of 128
 
 // dz = (p (1 + 2 z_loss L) - smoothing / vocab - (1 - smoothing) [v = target]) factor in place of the exponentials: 16 rows a workgroup, so that the pieces' maxima come in
 // whole lines.  Two bytes read and two written an element: bound by memory.
@@ -176,6 +221,7 @@ __global__ __launch_bounds__(256) void k_loss_dh_sum(LossArgs a) {
     const int row = (int)(n / units), d = (int)(n - (int64_t)row * units) * 4;
     if (row >= rows) return;
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
     for (int s = 0; s < a.dh_splits; ++s) sum += *reinterpret_cast<const f32x4*>(a.dh_parts + ((int64_t)s * a.block_rows + row) * a.width + d);
     store_four<D>(static_cast<uint8_t*>(a.dH) + (a.index[a.block * a.block_rows + row] * a.dh_stride + d) * D::size, sum[0], sum[1], sum[2], sum[3]);
 }
@@ -183,17 +229,27 @@ __global__ __launch_bounds__(256) void k_loss_dh_sum(LossArgs a) {
 // ------------------------------------------------------------------ plan
 static int64_t ceil_to(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// The time of tiles_m x tiles_n products over `length`, in us, by what a CU does of them: 256 CUs, each tile's share of its rate
-static double products_us(int64_t m, int64_t n, int64_t length, int tile, int splits, bool fp32) {
-    const int64_t tiles = (m + tile - 1) / tile * ((n + tile - 1) / tile) * splits;
-    const double rate = (tile == 256 ? 4.5e6 : tile == 128 ? 3.3e6 : 1.5e6) / (fp32 ? 10.0 : 1.0);
-    return (double)((tiles + 255) / 256) * 2.0 * tile * tile * (double)((length + splits - 1) / splits) / rate;
+// The time of tiles of m x n products over `length`, in us, by a rough account: operations a us of a CU whose workgroups are few in all (fewer than half the CUs: clocks are higher then), of
+// one among many, and of as many as it holds; and what a round of them costs besides.  Measured in bf16 with tiles of 256, 128 and 64, logits: rows 1000, width 512, vocabulary 4000: 19, 12.5
+// and 12 us; 1000, 1024, 8000: 30, 25.5 and 32; 1000, 1024, 32000: 68, 92 and 121; 64, 1024, 32000: 31, 19 and 14.
+struct TileRate { int tile, at_once; double few, one, all, round; };
+constexpr TileRate kTileRates[3] = {{256, 1, 7.5e6, 4.8e6, 4.8e6, 5.0}, {128, 2, 3.3e6, 2.6e6, 3.6e6, 3.0}, {64, 4, 1.35e6, 1.0e6, 2.6e6, 2.0}};
+constexpr TileRate kTileRatesF32[2] = {{128, 2, 0.49e6, 0.49e6, 0.5e6, 3.0}, {64, 4, 0.39e6, 0.39e6, 0.52e6, 2.0}};   // (256: its fragments would not find room in the registers)
+static double products_us(int64_t m, int64_t n, int64_t length, const TileRate& r, int splits) {
+    const int64_t tiles = (m + r.tile - 1) / r.tile * ((n + r.tile - 1) / r.tile) * splits;
+    const int here = (int)std::min<int64_t>(r.at_once, (tiles + 255) / 256);
+    const double rate = tiles <= 128 ? r.few : std::min(here * r.one, r.all);
+    return (double)((tiles + 256 * here - 1) / (256 * here)) * (r.round + here * 2.0 * r.tile * r.tile * (double)((length + splits - 1) / splits) / rate);
 }
-static int best_tile(int64_t m, int64_t n, int64_t length, bool fp32) {
-    int best = fp32 ? 128 : 256;
-    for (const int tile : {128, 64})
-        if (products_us(m, n, length, tile, 1, fp32) < products_us(m, n, length, best, 1, fp32)) best = tile;
-    return best;
+// The tile and the number of parts of `length` (at most `most`) that take the least; parts' sums are written and read again, at 5 TB/s, by a launch more
+static void best_tile(int64_t m, int64_t n, int64_t length, bool fp32, int most, int32_t& tile, int32_t& splits) {
+    double least = 1e30;
+    const TileRate* const rates = fp32 ? kTileRatesF32 : kTileRates;
+    for (int k = 0; k < (fp32 ? 2 : 3); ++k)
+        for (int s = 1; s <= most; ++s) {
+            const double us = products_us(m, n, length, rates[k], s) + (s > 1 ? 4.0 + 1.6e-6 * (double)s * (double)(m * n) : 0.0);
+            if (us < least) { least = us; tile = rates[k].tile; splits = s; }
+        }
 }
 
 void plan_loss(LossArgs& a, lsp_dtype dtype) {
@@ -206,18 +262,12 @@ void plan_loss(LossArgs& a, lsp_dtype dtype) {
     a.block_rows = (int)ceil_to((a.rows + a.blocks - 1) / a.blocks, 256);
     a.blocks = (int)((a.rows + a.block_rows - 1) / a.block_rows);
     const int64_t rows = std::min<int64_t>(a.rows, a.block_rows);
-    a.tile[0] = best_tile(a.vocab, rows, a.width, fp32);
+    int32_t whole;
+    best_tile(a.vocab, rows, a.width, fp32, 1, a.tile[0], whole);
     a.piece = a.tile[0] / 2;
     a.pieces = a.padded / a.piece;
-    a.tile[1] = 256; a.dh_splits = 1;
-    double least = 1e30;
-    for (const int tile : {256, 128, 64})
-        for (int s = 1; s <= 32; ++s) {
-            if (fp32 && tile == 256) continue;
-            const double us = products_us(a.width, rows, a.vocab, tile, s, fp32) + (s > 1 ? 4.0 + 8e-6 * (double)s * (double)rows * a.width / 4.0 : 0.0);
-            if (us < least) { least = us; a.tile[1] = tile; a.dh_splits = s; }
-        }
-    a.tile[2] = best_tile(a.width, a.vocab, rows, fp32);
+    best_tile(a.width, rows, a.vocab, fp32, 32, a.tile[1], a.dh_splits);
+    best_tile(a.width, a.vocab, rows, fp32, 1, a.tile[2], whole);
 }
 
 size_t loss_workspace(LossArgs& a, lsp_dtype dtype, uint8_t* base) {
@@ -247,13 +297,16 @@ size_t loss_workspace(LossArgs& a, lsp_dtype dtype, uint8_t* base) {
 }
 
 template <typename D> static hipError_t launch_blocks(LossArgs& a, lsp_dtype dtype, hipStream_t st) {
-    hipLaunchKernelGGL(k_loss_index, dim3(1), dim3(kIndexThreads), 0, st, a);
+    const bool few = a.rows <= kFewRows && a.blocks == 1;
+    const int row_bytes = a.width * D::size;
+    if (few) hipLaunchKernelGGL(k_loss_pack_few, dim3((unsigned)(a.rows + 255)), dim3(256), 0, st, a, row_bytes, (int)D::size);
+    else hipLaunchKernelGGL(k_loss_index, dim3(1), dim3(kIndexThreads), 0, st, a);
     hipError_t e = hipGetLastError();
     for (a.block = 0; a.block < a.blocks && e == hipSuccess; ++a.block) {
-        const int row_bytes = a.width * D::size;
-        hipLaunchKernelGGL(k_loss_pack, dim3((unsigned)(a.block_rows + (a.block == 0 ? a.rows : 0))), dim3(256), 0, st, a, row_bytes, (int)D::size);
+        if (!few) hipLaunchKernelGGL(k_loss_pack, dim3((unsigned)(a.block_rows + (a.block == 0 ? a.rows : 0))), dim3(256), 0, st, a, row_bytes, (int)D::size);
         if ((e = hipGetLastError()) != hipSuccess || (e = launch_loss_logits<D>(a, st)) != hipSuccess) break;
-        hipLaunchKernelGGL(k_loss_rows, dim3((unsigned)(a.block_rows / 16)), dim3(256), 0, st, a, (int)std::is_same<D, F16>::value);
+        if (a.pieces > 64) hipLaunchKernelGGL(k_loss_rows<64>, dim3((unsigned)(a.block_rows / 16)), dim3(1024), 0, st, a, (int)std::is_same<D, F16>::value);
+        else hipLaunchKernelGGL(k_loss_rows<16>, dim3((unsigned)(a.block_rows / 16)), dim3(256), 0, st, a, (int)std::is_same<D, F16>::value);
         if ((e = hipGetLastError()) != hipSuccess || !a.train) continue;
         hipLaunchKernelGGL(k_loss_dz<D>, dim3((unsigned)(a.block_rows / 16 * ((a.padded + kDzColumns - 1) / kDzColumns))), dim3(256), 0, st, a);
         if ((e = hipGetLastError()) != hipSuccess) break;

@@ -1,5 +1,5 @@
 // The cross entropy's products in f16.
-#include "cross_entropy.h"
+#include "cross_entropy_products.h"
 
 namespace lsp {
 template hipError_t launch_loss_logits<F16>(const LossArgs& a, hipStream_t st);

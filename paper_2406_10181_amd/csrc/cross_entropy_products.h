@@ -1,0 +1,199 @@
+// The cross entropy's kernels with products in them, instantiated for each type in cross_entropy_{bf16,f16,f32}.hip.
+#pragma once
+
+#include "cross_entropy.h"
+#include "matmul.h"
+
+namespace lsp {
+
+#if defined(__HIPCC__)
+template <typename D, int TILE> struct LossTiles;
+template <typename D> struct LossTiles<D, 256> { static constexpr int M = 256, N = 256, WM = 2, WN = 4; };
+template <typename D> struct LossTiles<D, 128> { static constexpr int M = 128, N = 128, WM = 2, WN = 2; };
+template <typename D> struct LossTiles<D, 64> { static constexpr int M = 64, N = 64, WM = 2, WN = 2; };
+template <typename D, int TILE, bool A_ACROSS, bool B_ACROSS>
+using LossProduct = Product<D, LossTiles<D, TILE>::M, LossTiles<D, TILE>::N, LossTiles<D, TILE>::WM, LossTiles<D, TILE>::WN, A_ACROSS, B_ACROSS>;
+
+// z[v][row] = W[v] . H[row]
+template <typename D, int TILE>
+__global__ __launch_bounds__((LossProduct<D, TILE, false, false>::kThreads)) void k_loss_logits(LossArgs a) {
+    using P = LossProduct<D, TILE, false, false>;
+    extern __shared__ uint8_t lds_bytes[];
+    const Lds lds = (Lds)lds_bytes;
+    const int rows = rows_of_block(a);
+    const uint32_t tiles_m = a.padded / P::BM, tiles_n = (rows + P::BN - 1) / P::BN, item = item_of_block(blockIdx.x, tiles_m * tiles_n);
+    if (item == tiles_m * tiles_n) return;
+    uint32_t tm, tn;
+    tile_of_item(item, tiles_m, tiles_n, tm, tn);
+    const int v0 = tm * P::BM, r0 = tn * P::BN;
+    const int64_t w_bytes = a.w_stride * D::size, h_bytes = (int64_t)a.width * D::size;
+    P p;
+    p.run({static_cast<const uint8_t*>(a.W) + v0 * w_bytes, w_bytes}, {a.packed + r0 * h_bytes, h_bytes}, a.width, max(a.vocab - v0, 0), P::BN, lds);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM, g = lane >> 4;
+    const int first = v0 + wm * P::kRange;                                                // of the wave's piece
+    const int64_t piece = first / P::kRange;
+#pragma unroll
+    for (int j = 0; j < P::NI; ++j) {
+        const int row = r0 + 16 * (wn * P::NI + j) + (lane & 15);
+        const int want = a.target[row] - first - 4 * g;                                   // (a lane has v = first + 4 g + 16 i + 0..3)
+        float hit = 0.0f, plain = 0.0f;
+#pragma unroll
+        for (int i = 0; i < P::MI; ++i)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) hit = want == 16 * i + x ? p.acc[j][i][x] : hit;
+        if (want >= 0 && want < P::kRange && (want & 12) == 0) a.hit[row] = hit;
+        if (a.smoothing > 0.0f) {                                                         // (z behind the vocabulary is 0)
+#pragma unroll
+            for (int i = 0; i < P::MI; ++i)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) plain += p.acc[j][i][x];
+            plain = quarters_sum(plain);
+            if (g == 0) a.plain[piece * a.block_rows + row] = plain;
+        }
+        if (first + P::kRange > a.vocab) {
+#pragma unroll
+            for (int i = 0; i < P::MI; ++i)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) p.acc[j][i][x] = first + 4 * g + 16 * i + x < a.vocab ? p.acc[j][i][x] : -INFINITY;
+        }
+        float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < P::MI; ++i)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) top = fmaxf(top, p.acc[j][i][x]);
+        top = quarters_max(top);
+        const float from = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int i = 0; i < P::MI; ++i)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                p.acc[j][i][x] = __builtin_amdgcn_exp2f((p.acc[j][i][x] - from) * kLossLog2e);
+                sum += p.acc[j][i][x];
+            }
+        sum = quarters_sum(sum);
+        if (g == 0) { a.top[piece * a.block_rows + row] = top; a.sum[piece * a.block_rows + row] = sum; }
+    }
+    if (!a.train) return;
+#pragma unroll
+    for (int j = 0; j < P::NI; j += 2) {
+        const int row0 = r0 + 16 * (wn * P::NI + j);
+        store_two_blocks<D, P::MI>(p.acc + j, kLossTop<D>, lds + wave * (32 * P::kRange * D::size), P::kRange, lane,
+                                   [&](uint32_t r) { return a.e + ((int64_t)(row0 + (int)r) * a.padded + first) * D::size; });
+    }
+}
+
+// dH[row][d] = sum over v of dz[row][v] W[v][d]; with several parts of the vocabulary each has its sum in fp32
+template <typename D, int TILE>
+__global__ __launch_bounds__((LossProduct<D, TILE, true, false>::kThreads)) void k_loss_dh(LossArgs a) {
+    using P = LossProduct<D, TILE, true, false>;
+    extern __shared__ uint8_t lds_bytes[];
+    const Lds lds = (Lds)lds_bytes;
+    const int rows = rows_of_block(a);
+    const uint32_t tiles_m = (a.width + P::BM - 1) / P::BM, tiles_n = (rows + P::BN - 1) / P::BN, items = tiles_m * tiles_n * a.dh_splits, item = item_of_block(blockIdx.x, items);
+    if (item == items) return;
+    const uint32_t split = item / (tiles_m * tiles_n);
+    uint32_t tm, tn;
+    tile_of_item(item - split * tiles_m * tiles_n, tiles_m, tiles_n, tm, tn);
+    const int d0 = tm * P::BM, r0 = tn * P::BN, steps = (a.vocab + P::BK - 1) / P::BK, share = (steps + a.dh_splits - 1) / a.dh_splits;
+    const int v0 = min((int)split * share * P::BK, a.vocab), v1 = min(v0 + share * P::BK, a.vocab);
+    const int64_t w_bytes = a.w_stride * D::size, e_bytes = (int64_t)a.padded * D::size;
+    P p;
+    p.run({static_cast<const uint8_t*>(a.W) + v0 * w_bytes + (int64_t)d0 * D::size, w_bytes}, {a.e + r0 * e_bytes + (int64_t)v0 * D::size, e_bytes}, v1 - v0, a.width - d0, P::BN, lds);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM;
+    const int first = d0 + wm * P::kRange, left = a.width - first;
+    const float factor = 1.0f / gradient_scale<D>(a);
+#pragma unroll
+    for (int j = 0; j < P::NI; j += 2) {
+        const int row0 = r0 + 16 * (wn * P::NI + j);
+        if (a.dh_splits > 1) {
+            float* const to = a.dh_parts + (int64_t)split * a.block_rows * a.width + first;
+            store_two_blocks<F32, P::MI>(p.acc + j, factor, lds + wave * (32 * P::kRange * 4), left, lane,
+                                         [&](uint32_t r) { return reinterpret_cast<uint8_t*>(to + (int64_t)(row0 + (int)r) * a.width); });
+        } else {
+            store_two_blocks<D, P::MI>(p.acc + j, factor, lds + wave * (32 * P::kRange * D::size), left, lane, [&](uint32_t r) -> uint8_t* {
+                const int row = row0 + (int)r;
+                return row < rows ? static_cast<uint8_t*>(a.dH) + (a.index[a.block * a.block_rows + row] * a.dh_stride + first) * D::size : nullptr;
+            });
+        }
+    }
+}
+
+// dW[v][d] = sum over the rows of dz[row][v] H[row][d]
+template <typename D, int TILE>
+__global__ __launch_bounds__((LossProduct<D, TILE, true, true>::kThreads)) void k_loss_dw(LossArgs a) {
+    using P = LossProduct<D, TILE, true, true>;
+    extern __shared__ uint8_t lds_bytes[];
+    const Lds lds = (Lds)lds_bytes;
+    const int rows = rows_of_block(a);
+    const uint32_t tiles_m = (a.width + P::BM - 1) / P::BM, tiles_n = (a.vocab + P::BN - 1) / P::BN, item = item_of_block(blockIdx.x, tiles_m * tiles_n);
+    if (item == tiles_m * tiles_n) return;
+    uint32_t tm, tn;
+    tile_of_item(item, tiles_m, tiles_n, tm, tn);
+    const int d0 = tm * P::BM, v0 = tn * P::BN;
+    const int64_t h_bytes = (int64_t)a.width * D::size, e_bytes = (int64_t)a.padded * D::size;
+    P p;
+    // (up to whole steps: the rows behind those that count are zeros in both)
+    p.run({a.packed + (int64_t)d0 * D::size, h_bytes}, {a.e + (int64_t)v0 * D::size, e_bytes}, (rows + P::BK - 1) / P::BK * P::BK, a.width - d0, P::BN, lds);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM;
+    const int first = d0 + wm * P::kRange, left = a.width - first;
+    const float factor = 1.0f / gradient_scale<D>(a);
+#pragma unroll
+    for (int j = 0; j < P::NI; j += 2) {
+        const int row0 = v0 + 16 * (wn * P::NI + j);
+        if (a.blocks > 1) {
+            // the sum so far is added in registers: a lane has four d that follow one another
+            float* const so_far = D::size == 4 ? static_cast<float*>(a.dW) : a.dw_sum;
+            const int64_t stride = D::size == 4 ? a.dw_stride : a.width;
+#pragma unroll
+            for (int jj = j; jj < j + 2; ++jj)
+#pragma unroll
+                for (int i = 0; i < P::MI; ++i) {
+                    const int v = row0 + 16 * (jj - j) + (lane & 15), d = first + 16 * i + 4 * (lane >> 4);
+                    f32x4 x = p.acc[jj][i] * factor;
+                    if (v < a.vocab && d < a.width) {
+                        f32x4* const at = reinterpret_cast<f32x4*>(so_far + v * stride + d);
+                        if (a.block > 0) x += *at;
+                        if (D::size == 4 || a.block + 1 < a.blocks) *at = x;
+                        else store_four<D>(static_cast<uint8_t*>(a.dW) + (v * a.dw_stride + d) * D::size, x[0], x[1], x[2], x[3]);
+                    }
+                }
+        } else {
+            store_two_blocks<D, P::MI>(p.acc + j, factor, lds + wave * (32 * P::kRange * D::size), left, lane, [&](uint32_t r) -> uint8_t* {
+                const int v = row0 + (int)r;
+                return v < a.vocab ? static_cast<uint8_t*>(a.dW) + (v * a.dw_stride + first) * D::size : nullptr;
+            });
+        }
+    }
+}
+
+template <typename P, auto Kernel> static inline hipError_t launch_tiles(const LossArgs& a, uint32_t tiles, hipStream_t st) {
+    const hipError_t e = allow_dynamic_lds<Kernel, P::kLds>();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(Kernel, dim3(tiles), dim3(P::kThreads), P::kLds, st, a);
+    return hipGetLastError();
+}
+template <typename D, int TILE> static inline hipError_t launch_logits_of(const LossArgs& a, hipStream_t st) {
+    return launch_tiles<LossProduct<D, TILE, false, false>, &k_loss_logits<D, TILE>>(a, (uint32_t)(a.padded / TILE * (a.block_rows / TILE)), st);
+}
+template <typename D, int TILE> static inline hipError_t launch_dh_of(const LossArgs& a, hipStream_t st) {
+    return launch_tiles<LossProduct<D, TILE, true, false>, &k_loss_dh<D, TILE>>(a, (uint32_t)((a.width + TILE - 1) / TILE * (a.block_rows / TILE) * a.dh_splits), st);
+}
+template <typename D, int TILE> static inline hipError_t launch_dw_of(const LossArgs& a, hipStream_t st) {
+    return launch_tiles<LossProduct<D, TILE, true, true>, &k_loss_dw<D, TILE>>(a, (uint32_t)((a.width + TILE - 1) / TILE * ((a.vocab + TILE - 1) / TILE)), st);
+}
+// (fp32: fragments of 256 x 256 tiles would not find room in the registers)
+template <typename D> hipError_t launch_loss_logits(const LossArgs& a, hipStream_t st) {
+    if constexpr (D::size == 2) if (a.tile[0] == 256) return launch_logits_of<D, 256>(a, st);
+    return a.tile[0] == 128 ? launch_logits_of<D, 128>(a, st) : launch_logits_of<D, 64>(a, st);
+}
+template <typename D> hipError_t launch_loss_dh(const LossArgs& a, hipStream_t st) {
+    if constexpr (D::size == 2) if (a.tile[1] == 256) return launch_dh_of<D, 256>(a, st);
+    return a.tile[1] == 128 ? launch_dh_of<D, 128>(a, st) : launch_dh_of<D, 64>(a, st);
+}
+template <typename D> hipError_t launch_loss_dw(const LossArgs& a, hipStream_t st) {
+    if constexpr (D::size == 2) if (a.tile[2] == 256) return launch_dw_of<D, 256>(a, st);
+    return a.tile[2] == 128 ? launch_dw_of<D, 128>(a, st) : launch_dw_of<D, 64>(a, st);
+}
+#endif
+
+}  // namespace lsp
