@@ -5,18 +5,25 @@
 
 namespace lsp {
 
+constexpr int kRotaryTokens = 16;                   // most tokens of a workgroup
+// What is done head by head alike: queries, keys, and (forward) values, which are only moved
+struct RotarySegment {
+    Strided x, y;                                   // forward: from and to; backward: what was normed, and the gradient that arrives
+    Strided out;                                    // backward: the gradient that is made
+    const void *weight, *bias;
+    float *weight_sum, *bias_sum;                   // backward: gradients of these, or NULL
+    int32_t heads, placed;                          // placed: y has places of a cache, not positions of the text
+    int32_t tokens, parts;                          // of a workgroup; workgroups that share the tokens' heads
+    int32_t first, blocks;                          // its workgroups
+};
 struct RotaryArgs {
-    Strided q, k, v, qr, kr, vr;                    // backward: qr, kr are dQr, dKr and v, vr are dQ, dK
-    const void *q_w, *k_w, *q_b, *k_b;
+    RotarySegment segment[3];
     const float* frequencies;
     const int32_t *positions, *starts, *lens;
-    float* partial;                                 // backward: [workgroups][4][head_dim], sums of q_weight, k_weight, q_bias, k_bias
-    float* grads[4];                                // NULL: not asked for
-    int32_t batch, length, cache, heads, kv_heads, head_dim, rotated, neighbours, norm;
-    int32_t rows;                                   // of a token: heads of Q, of K and (forward, if there is a V) of V
-    int32_t parts;                                  // lane groups that share a token's rows
-    int32_t sums;                                   // backward: whether any of grads is asked for
-    int32_t blocks;                                 // backward: workgroups, each with a part of the sums
+    float* partial;                                 // backward: [workgroups][2][head_dim], sums for weight and bias
+    int32_t batch, length, cache, head_dim, rotated, neighbours, norm;
+    int32_t segments, blocks;
+    int32_t sums;                                   // backward: whether any gradient of a weight or bias is asked for
     float eps;
 };
 

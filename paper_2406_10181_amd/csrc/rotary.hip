@@ -2,9 +2,8 @@
 //
 // Bound by memory: a head is read and written once (backward: its gradient read, what was normed read again, a gradient written).  A group of 4, 8 or 16 lanes has a
 // head, eight elements a lane, so that the sums of a norm go through the lanes of a group by moves that need no LDS.  A lane's eight elements are four
-// whole pairs: four elements from each half of what turns, or eight neighbours; so turning needs no other lane, and the lane's four angles are the same
-// for every head of a token.  They cost an fp64 product and a sine and cosine each, some 200 instructions; a group keeps them for all rows of the token that it does.
-// Where there are few tokens their rows are dealt to many groups (`parts`), since then the angles are not what takes the time.
+// whole pairs: four elements from each half of what turns, or eight neighbours; so turning needs no other lane.  A workgroup has the queries, the keys or the values of a few tokens
+// that follow one another; its angles, an fp64 product, a sine and a cosine each, are made once for all their heads and lie in LDS.
 #include <algorithm>
 
 #include "rotary.h"
@@ -74,41 +73,67 @@ template <typename D> __device__ __forceinline__ Eight load_vector(const void* v
     return r;
 }
 
-struct Angles { float cos[4], sin[4]; };
-// Whole turns are taken off in fp64: position and frequency have 55 bits together at most, and what is left of a turn keeps at least 30 behind the point
-__device__ __forceinline__ Angles angles_of(const float (&frequency)[4], int64_t position, bool turns) {
-    Angles r;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        r.cos[j] = 1.0f; r.sin[j] = 0.0f;
-        if (!turns) continue;
-        const double whole = (double)position * ((double)frequency[j] * 0.15915494309189533577);
-        sincospif(2.0f * (float)(whole - rint(whole)), &r.sin[j], &r.cos[j]);
-    }
-    return r;
-}
-// BACK: by minus the angle
-template <bool NEIGHBOURS, bool BACK> __device__ __forceinline__ void turn(Eight& x, const Angles& t) {
+// By the angle, or (BACK) by minus the angle
+template <bool NEIGHBOURS, bool BACK> __device__ __forceinline__ void turn(Eight& x, const f32x4& cos, const f32x4& sin) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         float& a = x.x[NEIGHBOURS ? 2 * j : j];
         float& b = x.x[NEIGHBOURS ? 2 * j + 1 : 4 + j];
-        const float s = BACK ? -t.sin[j] : t.sin[j], u = a, v = b;
-        a = u * t.cos[j] - v * s;
-        b = u * s + v * t.cos[j];
+        const float s = BACK ? -sin[j] : sin[j], u = a, v = b;
+        a = u * cos[j] - v * s;
+        b = u * s + v * cos[j];
     }
 }
 
-// Whether the token counts, its position and the place of its key
-struct Token { int text, i; int64_t position, place; bool counts; };
-__device__ __forceinline__ Token token_of(const RotaryArgs& a, int token) {
-    Token t;
-    t.text = token / a.length;
-    t.i = token - t.text * a.length;
-    t.counts = t.i < valid_length(a.lens, t.text, a.length);
-    t.place = t.position = (int64_t)t.i + (a.starts ? a.starts[t.text] : 0);
-    if (a.positions && t.counts) t.position = a.positions[(int64_t)t.text * a.length + t.i];
-    return t;
+// The tokens of a workgroup, in LDS
+struct Tokens {
+    float   cos[kRotaryTokens][LSP_MAX_HEAD_DIM / 2], sin[kRotaryTokens][LSP_MAX_HEAD_DIM / 2];
+    int64_t x[kRotaryTokens], y[kRotaryTokens], out[kRotaryTokens];      // elements from the tensors' begins to the token's first head; -1: not there
+    int64_t position[kRotaryTokens];
+};
+// Whole turns are taken off in fp64: position and frequency have 55 bits together at most, and what is left of a turn keeps at least 30 behind the point.
+__device__ __forceinline__ void set_tokens(Tokens& t, const RotaryArgs& a, const RotarySegment& s, int first, int n, bool backward) {
+    if ((int)threadIdx.x < n) {
+        const int token = first + threadIdx.x, text = token / a.length, i = token - text * a.length;
+        const bool counts = i < valid_length(a.lens, text, a.length);
+        const int64_t place = (int64_t)i + (a.starts ? a.starts[text] : 0), at = s.placed ? place : i;
+        const bool there = counts && (!s.placed || (place >= 0 && place < a.cache));
+        t.position[threadIdx.x] = a.positions && counts ? a.positions[(int64_t)text * a.length + i] : place;
+        t.x[threadIdx.x] = there ? text * s.x.batch + i * s.x.position : -1;
+        t.y[threadIdx.x] = there ? text * s.y.batch + at * s.y.position : -1;
+        if (backward) t.out[threadIdx.x] = text * s.out.batch + i * s.out.position;
+    }
+    __syncthreads();
+    const int pairs = a.rotated / 2;
+    for (int k = threadIdx.x; k < n * pairs; k += kRotaryThreads) {
+        const int token = k / pairs, pair = k - token * pairs;
+        const double turns = (double)t.position[token] * ((double)a.frequencies[pair] * 0.15915494309189533577);
+        sincospif(2.0f * (float)(turns - rint(turns)), &t.sin[token][pair], &t.cos[token][pair]);
+    }
+    __syncthreads();
+}
+__device__ __forceinline__ void angles_of(const Tokens& t, int token, const Place& at, f32x4& cos, f32x4& sin) {
+    cos = f32x4{1.0f, 1.0f, 1.0f, 1.0f}; sin = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (at.pair >= 0) { cos = *reinterpret_cast<const f32x4*>(&t.cos[token][at.pair]); sin = *reinterpret_cast<const f32x4*>(&t.sin[token][at.pair]); }
+}
+// Heads of tokens that follow one another, every `step`-th from the r-th on
+struct Walk {
+    int token, head;
+    __device__ __forceinline__ Walk(int r, int heads) { token = r / heads; head = r - token * heads; }
+    __device__ __forceinline__ void advance(int by_tokens, int by_heads, int heads) {
+        token += by_tokens; head += by_heads;
+        if (head >= heads) { head -= heads; ++token; }
+    }
+};
+template <typename D> __device__ __forceinline__ uint8_t* head_at(const Strided& s, int64_t token, int head) {
+    return static_cast<uint8_t*>(const_cast<void*>(s.p)) + (token + head * s.head) * D::size;
+}
+__device__ __forceinline__ const RotarySegment& segment_of(const RotaryArgs& a, int& block, int& which) {
+    which = 0;
+    if (a.segments > 1 && block >= a.segment[1].first) which = 1;
+    if (a.segments > 2 && block >= a.segment[2].first) which = 2;
+    block -= a.segment[which].first;
+    return a.segment[which];
 }
 
 template <int NORM, int GROUP> __device__ __forceinline__ void norm_head(Eight& x, float& factor, const Place& at, int head_dim, float eps) {
@@ -126,76 +151,52 @@ template <int NORM, int GROUP> __device__ __forceinline__ void norm_head(Eight& 
         float squares = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) squares = fmaf(x.x[e], x.x[e], squares);
-        factor = 1.0f / sqrtf(fmaf(group_sum<GROUP>(squares), share, eps));
+        // (v_rsq_f32, within an ulp, takes what is below 2^-126 for zero: where eps does not keep the sum above that, the root and quotient that IEEE has)
+        const float sum = fmaf(group_sum<GROUP>(squares), share, eps);
+        factor = eps >= 0x1p-126f ? __builtin_amdgcn_rsqf(sum) : 1.0f / sqrtf(sum);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x.x[e] *= factor;
     }
 }
 
-constexpr int kAtOnce = 4;                          // rows whose loads are on their way together
-
 template <typename D, int NORM, int GROUP, bool NEIGHBOURS>
 __global__ __launch_bounds__(kRotaryThreads) void k_rotary(RotaryArgs a) {
-    const int lane = threadIdx.x % GROUP;
-    const int64_t group = (int64_t)blockIdx.x * (kRotaryThreads / GROUP) + threadIdx.x / GROUP;
-    if (group >= (int64_t)a.batch * a.length * a.parts) return;
-    const int token = (int)(group / a.parts), part = (int)(group - (int64_t)token * a.parts);
-    const Token t = token_of(a, token);
-    if (!t.counts) return;
-    const Place at(a, lane);
-    const bool inside = t.place >= 0 && t.place < a.cache;
-    // the row and its destination; NULL: nowhere
-    const auto from = [&](int row) -> const uint8_t* {
-        if (!at.there) return nullptr;
-        if (row < a.heads) return lsp::at<D>(a.q, t.text, t.i, row);
-        if (!inside) return nullptr;
-        return row < a.heads + a.kv_heads ? lsp::at<D>(a.k, t.text, t.i, row - a.heads) : lsp::at<D>(a.v, t.text, t.i, row - a.heads - a.kv_heads);
-    };
-    const auto to = [&](int row) -> uint8_t* {
-        const uint8_t* p = row < a.heads ? lsp::at<D>(a.qr, t.text, t.i, row)
-                         : row < a.heads + a.kv_heads ? lsp::at<D>(a.kr, t.text, t.place, row - a.heads) : lsp::at<D>(a.vr, t.text, t.place, row - a.heads - a.kv_heads);
-        return const_cast<uint8_t*>(p);
-    };
-    const auto fetch = [&](int row) {
+    constexpr int kGroups = kRotaryThreads / GROUP;
+    __shared__ Tokens t;
+    int block = blockIdx.x, which;
+    const RotarySegment& s = segment_of(a, block, which);
+    const int group = block / s.parts, part = block - group * s.parts, first = group * s.tokens, n = min(s.tokens, a.batch * a.length - first);
+    const Place at(a, threadIdx.x % GROUP);
+    const int heads = s.heads, step = kGroups * s.parts, by_tokens = step / heads, by_heads = step - by_tokens * heads;
+    const Eight w = load_vector<D>(which < 2 ? s.weight : nullptr, at, 1.0f), bias = load_vector<D>(which < 2 ? s.bias : nullptr, at, 0.0f);
+    set_tokens(t, a, s, first, n, false);
+    Walk now(part * kGroups + threadIdx.x / GROUP, heads);
+    const auto fetch = [&](const Walk& k) {
         Raw<D> r;
         r.a = r.b = u32x4{0, 0, 0, 0};
-        const uint8_t* p = row < a.rows ? from(row) : nullptr;
-        if (p) r = load_raw<D>(p, at);
+        if (k.token < n && at.there && t.x[k.token] >= 0) r = load_raw<D>(head_at<D>(s.x, t.x[k.token], k.head), at);
         return r;
     };
-    Raw<D> raw[kAtOnce];
+    Raw<D> raw = fetch(now);
+    while (now.token < n) {
+        Walk next = now;
+        next.advance(by_tokens, by_heads, heads);
+        const Raw<D> ahead = fetch(next);
+        Eight x = widen_raw<D>(raw);
+        if (which < 2) {
+            float factor;
+            norm_head<NORM, GROUP>(x, factor, at, a.head_dim, a.eps);
+            if constexpr (NORM != LSP_NORM_NONE) {
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) raw[k] = fetch(part + k * a.parts);
-    float frequency[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (at.pair >= 0) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) frequency[j] = a.frequencies[at.pair + j];
-    }
-    const Eight qw = load_vector<D>(a.q_w, at, 1.0f), kw = load_vector<D>(a.k_w, at, 1.0f), qb = load_vector<D>(a.q_b, at, 0.0f), kb = load_vector<D>(a.k_b, at, 0.0f);
-    const Angles angles = angles_of(frequency, t.position, at.pair >= 0);
-    for (int row0 = part; row0 < a.rows; row0 += kAtOnce * a.parts) {
-        Raw<D> next[kAtOnce];
-#pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) next[k] = fetch(row0 + (kAtOnce + k) * a.parts);
-#pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) {
-            const int row = row0 + k * a.parts;
-            if (row >= a.rows) break;                                    // (the same for a group's lanes)
-            Eight x = widen_raw<D>(raw[k]);
-            if (row < a.heads + a.kv_heads) {
-                const bool query = row < a.heads;
-                float factor;
-                norm_head<NORM, GROUP>(x, factor, at, a.head_dim, a.eps);
-                if constexpr (NORM != LSP_NORM_NONE) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x.x[e] = fmaf(x.x[e], query ? qw.x[e] : kw.x[e], query ? qb.x[e] : kb.x[e]);
-                }
-                turn<NEIGHBOURS, false>(x, angles);
+                for (int e = 0; e < 8; ++e) x.x[e] = fmaf(x.x[e], w.x[e], bias.x[e]);
             }
-            if (at.there && (row < a.heads || inside)) store_raw<D>(to(row), at, x);
+            f32x4 cos, sin;
+            angles_of(t, now.token, at, cos, sin);
+            turn<NEIGHBOURS, false>(x, cos, sin);
         }
-#pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) raw[k] = next[k];
+        if (at.there && t.y[now.token] >= 0) store_raw<D>(head_at<D>(s.y, t.y[now.token], now.head), at, x);
+        raw = ahead;
+        now = next;
     }
 }
 
@@ -204,110 +205,127 @@ __global__ __launch_bounds__(kRotaryThreads) void k_rotary(RotaryArgs a) {
 template <typename D, int NORM, int GROUP, bool NEIGHBOURS>
 __global__ __launch_bounds__(kRotaryThreads) void k_rotary_back(RotaryArgs a) {
     constexpr int kGroups = kRotaryThreads / GROUP;
-    const int lane = threadIdx.x % GROUP, own = threadIdx.x / GROUP;
-    const Place at(a, lane);
-    float frequency[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (at.pair >= 0) {
+    __shared__ Tokens t;
+    int block = blockIdx.x, which;
+    const RotarySegment& s = segment_of(a, block, which);
+    const Place at(a, threadIdx.x % GROUP);
+    const int own = threadIdx.x / GROUP, heads = s.heads, step = kGroups * s.parts, by_tokens = step / heads, by_heads = step - by_tokens * heads;
+    const int tokens = a.batch * a.length, groups = (tokens + s.tokens - 1) / s.tokens * s.parts;
+    const Eight w = load_vector<D>(s.weight, at, 1.0f);
+    Eight dw, db;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) frequency[j] = a.frequencies[at.pair + j];
-    }
-    const Eight qw = load_vector<D>(a.q_w, at, 1.0f), kw = load_vector<D>(a.k_w, at, 1.0f);
-    float sums[4][8];                                                    // of q_weight, k_weight, q_bias, k_bias
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sums[s][e] = 0.0f;
-    const int64_t items = (int64_t)a.batch * a.length * a.parts;
-    for (int64_t item = (int64_t)blockIdx.x * kGroups + own; item < items; item += (int64_t)a.blocks * kGroups) {
-        const int token = (int)(item / a.parts), part = (int)(item - (int64_t)token * a.parts);
-        const Token t = token_of(a, token);
-        const bool inside = t.place >= 0 && t.place < a.cache;
-        const Angles angles = angles_of(frequency, t.position, at.pair >= 0);
-        for (int row = part; row < a.rows; row += a.parts) {
-            const bool query = row < a.heads;
-            const int head = query ? row : row - a.heads;
-            const bool seen = t.counts && (query || inside) && at.there;
-            Eight d, x;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) d.x[e] = x.x[e] = 0.0f;
-            if (seen) {
-                d = widen_raw<D>(load_raw<D>(query ? lsp::at<D>(a.qr, t.text, t.i, head) : lsp::at<D>(a.kr, t.text, t.place, head), at));
-                if constexpr (NORM != LSP_NORM_NONE) x = widen_raw<D>(load_raw<D>(query ? lsp::at<D>(a.q, t.text, t.i, head) : lsp::at<D>(a.k, t.text, t.i, head), at));
+    for (int e = 0; e < 8; ++e) dw.x[e] = db.x[e] = 0.0f;
+    struct Both { Raw<D> d, x; };
+    for (; block < groups; block += s.blocks) {
+        const int group = block / s.parts, part = block - group * s.parts, first = group * s.tokens, n = min(s.tokens, tokens - first);
+        __syncthreads();                                                 // (the tokens before are done with)
+        set_tokens(t, a, s, first, n, true);
+        Walk now(part * kGroups + own, heads);
+        const auto fetch = [&](const Walk& k) {
+            Both r;
+            r.d.a = r.d.b = r.x.a = r.x.b = u32x4{0, 0, 0, 0};
+            if (k.token < n && at.there && t.y[k.token] >= 0) {
+                r.d = load_raw<D>(head_at<D>(s.y, t.y[k.token], k.head), at);
+                if constexpr (NORM != LSP_NORM_NONE) r.x = load_raw<D>(head_at<D>(s.x, t.x[k.token], k.head), at);
             }
-            turn<NEIGHBOURS, true>(d, angles);
-            if constexpr (NORM != LSP_NORM_NONE) {
-                float factor;
-                norm_head<NORM, GROUP>(x, factor, at, a.head_dim, a.eps);
-                float along = 0.0f, sum = 0.0f;
+            return r;
+        };
+        Both raw = fetch(now);
+        while (now.token < n) {
+            Walk next = now;
+            next.advance(by_tokens, by_heads, heads);
+            const Both ahead = fetch(next);
+            Eight d = widen_raw<D>(raw.d);
+            if (t.y[now.token] >= 0) {                                   // (the same for a group's lanes; otherwise d is zeros, and stays)
+                f32x4 cos, sin;
+                angles_of(t, now.token, at, cos, sin);
+                turn<NEIGHBOURS, true>(d, cos, sin);
+                if constexpr (NORM != LSP_NORM_NONE) {
+                    Eight x = widen_raw<D>(raw.x);
+                    float factor;
+                    norm_head<NORM, GROUP>(x, factor, at, a.head_dim, a.eps);
+                    float along = 0.0f, sum = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float dw = d.x[e] * x.x[e];
-                    sums[0][e] += query ? dw : 0.0f; sums[1][e] += query ? 0.0f : dw;
-                    sums[2][e] += query ? d.x[e] : 0.0f; sums[3][e] += query ? 0.0f : d.x[e];
-                    d.x[e] *= query ? qw.x[e] : kw.x[e];
-                    along = fmaf(d.x[e], x.x[e], along);
-                    sum += d.x[e];
+                    for (int e = 0; e < 8; ++e) {
+                        dw.x[e] = fmaf(d.x[e], x.x[e], dw.x[e]);
+                        db.x[e] += d.x[e];
+                        d.x[e] *= w.x[e];
+                        along = fmaf(d.x[e], x.x[e], along);
+                        sum += d.x[e];
+                    }
+                    const float share = 1.0f / (float)a.head_dim;
+                    along = group_sum<GROUP>(along) * share;
+                    const float mean = NORM == LSP_NORM_LAYER ? group_sum<GROUP>(sum) * share : 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) d.x[e] = factor * (d.x[e] - fmaf(x.x[e], along, mean));
                 }
-                const float share = 1.0f / (float)a.head_dim;
-                along = group_sum<GROUP>(along) * share;
-                const float mean = NORM == LSP_NORM_LAYER ? group_sum<GROUP>(sum) * share : 0.0f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d.x[e] = seen ? factor * (d.x[e] - fmaf(x.x[e], along, mean)) : 0.0f;
             }
-            if (at.there) store_raw<D>(const_cast<uint8_t*>(query ? lsp::at<D>(a.v, t.text, t.i, head) : lsp::at<D>(a.vr, t.text, t.i, head)), at, d);
+            if (at.there) store_raw<D>(head_at<D>(s.out, t.out[now.token], now.head), at, d);
+            raw = ahead;
+            now = next;
         }
     }
     if (NORM == LSP_NORM_NONE || !a.sums) return;
     __shared__ float all[kGroups][GROUP * 8 + 4];
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
+    for (int k = 0; k < 2; ++k) {
         __syncthreads();
         if (at.there) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) all[own][e < 4 ? at.first + e : at.second + e - 4] = sums[s][e];
+            for (int e = 0; e < 8; ++e) all[own][e < 4 ? at.first + e : at.second + e - 4] = k ? db.x[e] : dw.x[e];
         }
         __syncthreads();
         if ((int)threadIdx.x < a.head_dim) {
             float x = 0.0f;
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) x += all[g][threadIdx.x];
-            a.partial[((int64_t)blockIdx.x * 4 + s) * a.head_dim + threadIdx.x] = x;
+            a.partial[((int64_t)blockIdx.x * 2 + k) * a.head_dim + threadIdx.x] = x;
         }
     }
 }
 
-// The workgroups' parts of a sum, added in their order: 16 columns of one sum a workgroup, 16 runs of parts side by side
-__global__ __launch_bounds__(256) void k_rotary_sums(RotaryArgs a) {
-    const int s = blockIdx.y, column = blockIdx.x * 16 + (threadIdx.x & 15), run = threadIdx.x >> 4;
-    float* const to = a.grads[s];
+// The workgroups' parts of a sum, added in their order: 16 columns of one sum a workgroup, 64 runs of parts side by side
+__global__ __launch_bounds__(1024) void k_rotary_sums(RotaryArgs a) {
+    const RotarySegment& s = a.segment[blockIdx.y >> 1];
+    const int k = blockIdx.y & 1, column = blockIdx.x * 16 + (threadIdx.x & 15), run = threadIdx.x >> 4;
+    float* const to = k ? s.bias_sum : s.weight_sum;
     if (!to) return;
     float x = 0.0f;
     if (column < a.head_dim) {
-#pragma unroll 4
-        for (int p = run; p < a.blocks; p += 16) x += a.partial[((int64_t)p * 4 + s) * a.head_dim + column];
+#pragma unroll 8
+        for (int p = run; p < s.blocks; p += 64) x += a.partial[((int64_t)(s.first + p) * 2 + k) * a.head_dim + column];
     }
-    __shared__ float all[16][17];
+    __shared__ float all[64][17];
     all[run][threadIdx.x & 15] = x;
     __syncthreads();
     if (run == 0 && column < a.head_dim) {
         float sum = 0.0f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sum += all[r][threadIdx.x & 15];
+#pragma unroll 16
+        for (int r = 0; r < 64; ++r) sum += all[r][threadIdx.x & 15];
         to[column] = sum;
     }
 }
 
 static int group_of(int head_dim) { return head_dim <= 32 ? 4 : head_dim <= 64 ? 8 : 16; }
 
+// A workgroup has the tokens whose heads give each of its lane groups 16 of them, or as few as give 1024 workgroups; where one token each gives fewer, its heads are shared.
+// Backward with sums: at most 1024 workgroups that go on, since each leaves a part of the sums.
 void plan_rotary(RotaryArgs& a, bool backward) {
     const int64_t tokens = (int64_t)a.batch * a.length;
-    const int per_block = kRotaryThreads / group_of(a.head_dim);
-    // lane groups for 2048 workgroups, as far as there are rows
-    a.parts = (int)std::min<int64_t>(a.rows, std::max<int64_t>(1, (2048 * per_block + tokens - 1) / tokens));
-    const int64_t blocks = (tokens * a.parts + per_block - 1) / per_block;
-    a.blocks = (int)(backward && a.sums ? std::min<int64_t>(blocks, 1024) : blocks);
+    const int groups = kRotaryThreads / group_of(a.head_dim);
+    a.blocks = 0;
+    for (int k = 0; k < a.segments; ++k) {
+        RotarySegment& s = a.segment[k];
+        s.tokens = (int)std::min<int64_t>({std::max(1, 16 * groups / s.heads), kRotaryTokens, std::max<int64_t>(1, tokens / 1024)});
+        const int64_t of_tokens = (tokens + s.tokens - 1) / s.tokens;
+        s.parts = s.tokens > 1 ? 1 : (int)std::min<int64_t>((s.heads + groups - 1) / groups, std::max<int64_t>(1, 1024 / of_tokens));
+        const int64_t blocks = of_tokens * s.parts;
+        s.first = a.blocks;
+        s.blocks = (int)(backward && a.sums ? std::min<int64_t>(blocks, 1024) : blocks);
+        a.blocks += s.blocks;
+    }
 }
-size_t rotary_partial_bytes(const RotaryArgs& a) { return a.sums ? align_up((size_t)a.blocks * 4 * a.head_dim * sizeof(float), 256) : 0; }
+size_t rotary_partial_bytes(const RotaryArgs& a) { return a.sums ? align_up((size_t)a.blocks * 2 * a.head_dim * sizeof(float), 256) : 0; }
 
 template <typename D, int NORM, int GROUP> static void launch_one(const RotaryArgs& a, bool backward, hipStream_t st) {
     const dim3 grid((unsigned)a.blocks), block(kRotaryThreads);
@@ -337,7 +355,7 @@ hipError_t launch_rotary(const RotaryArgs& a, bool backward, lsp_dtype dtype, hi
     else launch_norm<BF16>(a, backward, st);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !backward || !a.sums) return e;
-    hipLaunchKernelGGL(k_rotary_sums, dim3((unsigned)((a.head_dim + 15) / 16), 4), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_rotary_sums, dim3((unsigned)((a.head_dim + 15) / 16), 4), dim3(1024), 0, st, a);
     return hipGetLastError();
 }
 

@@ -53,24 +53,26 @@ int check_rotary(const lsp_rotary_problem* p, lsp_dtype t) {
 
 lsp::RotaryArgs rotary_args(const lsp_rotary_problem* p) {
     lsp::RotaryArgs a{};
-    a.q = strided(p->Q, p->q_stride, p->batch, p->length, p->heads);
-    a.k = strided(p->K, p->k_stride, p->batch, p->length, p->kv_heads);
-    a.qr = strided(p->Qr, p->qr_stride, p->batch, p->length, p->heads);
-    a.kr = strided(p->Kr, p->kr_stride, p->batch, p->cache, p->kv_heads);
+    auto &q = a.segment[0], &k = a.segment[1], &v = a.segment[2];
+    q.x = strided(p->Q, p->q_stride, p->batch, p->length, p->heads);
+    k.x = strided(p->K, p->k_stride, p->batch, p->length, p->kv_heads);
+    q.y = strided(p->Qr, p->qr_stride, p->batch, p->length, p->heads);
+    k.y = strided(p->Kr, p->kr_stride, p->batch, p->cache, p->kv_heads);
     if (p->V) {
-        a.v = strided(p->V, p->v_stride, p->batch, p->length, p->kv_heads);
-        a.vr = strided(p->Vr, p->vr_stride, p->batch, p->cache, p->kv_heads);
+        v.x = strided(p->V, p->v_stride, p->batch, p->length, p->kv_heads);
+        v.y = strided(p->Vr, p->vr_stride, p->batch, p->cache, p->kv_heads);
     }
-    a.q_w = p->q_weight; a.k_w = p->k_weight; a.q_b = p->q_bias; a.k_b = p->k_bias;
+    q.heads = p->heads; k.heads = v.heads = p->kv_heads; k.placed = v.placed = 1;
+    q.weight = p->q_weight; k.weight = p->k_weight; q.bias = p->q_bias; k.bias = p->k_bias;
     a.frequencies = p->frequencies; a.positions = p->positions; a.starts = p->starts; a.lens = p->lens;
-    a.batch = p->batch; a.length = p->length; a.cache = p->cache; a.heads = p->heads; a.kv_heads = p->kv_heads; a.head_dim = p->head_dim;
+    a.batch = p->batch; a.length = p->length; a.cache = p->cache; a.head_dim = p->head_dim;
     a.rotated = p->rotated; a.neighbours = p->neighbours; a.norm = p->norm; a.eps = p->eps;
-    a.rows = p->heads + p->kv_heads * (p->V ? 2 : 1);
+    a.segments = p->V ? 3 : 2;
     return a;
 }
 lsp::RotaryArgs rotary_back_args(const lsp_rotary_problem* p, bool sums) {
     lsp::RotaryArgs a = rotary_args(p);
-    a.rows = p->heads + p->kv_heads;
+    a.segments = 2;
     a.sums = sums;
     lsp::plan_rotary(a, true);
     return a;
@@ -149,11 +151,12 @@ int lsp_rotary_backward(const lsp_rotary_problem* p, const lsp_rotary_gradients*
     const size_t need = lsp::rotary_partial_bytes(a);
     if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return LSP_ERR_WORKSPACE;
     a.partial = static_cast<float*>(workspace);
-    a.qr = strided(g->dQr, g->dqr_stride, p->batch, p->length, p->heads);
-    a.kr = strided(g->dKr, g->dkr_stride, p->batch, p->cache, p->kv_heads);
-    a.v = strided(g->dQ, g->dq_stride, p->batch, p->length, p->heads);
-    a.vr = strided(g->dK, g->dk_stride, p->batch, p->length, p->kv_heads);
-    a.grads[0] = g->q_weight; a.grads[1] = g->k_weight; a.grads[2] = g->q_bias; a.grads[3] = g->k_bias;
+    auto &q = a.segment[0], &k = a.segment[1];
+    q.y = strided(g->dQr, g->dqr_stride, p->batch, p->length, p->heads);
+    k.y = strided(g->dKr, g->dkr_stride, p->batch, p->cache, p->kv_heads);
+    q.out = strided(g->dQ, g->dq_stride, p->batch, p->length, p->heads);
+    k.out = strided(g->dK, g->dk_stride, p->batch, p->length, p->kv_heads);
+    q.weight_sum = g->q_weight; k.weight_sum = g->k_weight; q.bias_sum = g->q_bias; k.bias_sum = g->k_bias;
     return done(lsp::launch_rotary(a, true, dtype, static_cast<hipStream_t>(stream)));
 }
 
