@@ -78,11 +78,18 @@ class Block:
         problem.offset = offset
         return problem
 
+    def turn(self):
+        """What happens to queries and keys between their projection and attention: nothing in this block."""
+
+    def turn_back(self):
+        """The same for their gradients."""
+
     def forward(self, step=0):
         """x[0] to h[2]."""
         w, code, s = self.weights, self.code, self.stream
         lsp.lsp_residual_norm_forward(self.residual[0], code, s)
         torch.mm(self.h[0], w["qkv"].t(), out=self.qkv)
+        self.turn()
         lsp.lsp_attention_forward(self.number(self.attention, 4 * step), code, *self.forward_room, s)
         torch.mm(self.o.view(self.rows, -1), w["out"].t(), out=self.a)
         lsp.lsp_residual_norm_forward(self.number(self.residual[1], 4 * step + 1), code, s)
@@ -108,6 +115,7 @@ class Block:
         grads["out"] = self.da.t() @ self.o.view(self.rows, -1)
         torch.mm(self.da, w["out"], out=self.do.view(self.rows, -1))
         lsp.lsp_attention_backward(self.number(self.attention, 4 * step), self.attention_grads, code, *self.backward_room, s)
+        self.turn_back()
         grads["qkv"] = self.dqkv.t() @ self.h[0]
         return grads
 

@@ -712,43 +712,12 @@ class AdamwItems:
 
 def adamw_items(tensors) -> AdamwItems:
     """What lsp_adamw updates, from a list of dicts: param and grad, m and v (both float32, or both of one byte an element: states in 8 bits, with m_scale and v_scale, float32,
-    one for 256 elements), optionally master (float32), rate_factor (1) and decay (0).  Tensors are contiguous, of one size and on one device; others are a
-    ValueError.  They are kept alive by the caller, and the array serves as long as they are where they are."""
-    import torch
-    code = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
-    array, kinds, devices, seen = (lsp_adamw_item * len(tensors))(), set(), set(), set()
-
-    def need(ok, what):
-        if not ok:
-            raise ValueError(f"adamw_items: {what}")
-
-    need(len(tensors) > 0, "tensors are wanted")
-    for k, t in enumerate(tensors):
-        need(not set(t) - {"param", "grad", "m", "v", "m_scale", "v_scale", "master", "rate_factor", "decay"}, "unknown names")
-        param, grad, m, v, master = t["param"], t["grad"], t["m"], t["v"], t.get("master")
-        bits8 = m.element_size() == 1
-        kinds.add("8bit" if bits8 else "f32")
-        need(param.dtype in code and grad.dtype in code, "param and grad are float32, float16 or bfloat16")
-        need(m.element_size() == v.element_size() and (bits8 or m.dtype == v.dtype == torch.float32), "m and v are both float32 or both of one byte an element")
-        need(master is None or master.dtype == torch.float32, "master is float32")
-        n = param.numel()
-        need(n > 0 and all(x is None or x.numel() == n for x in (grad, m, v, master)), "param, grad, m, v and master are of one size")
-        scales = [t.get("m_scale"), t.get("v_scale")]
-        if bits8:
-            need(all(x is not None and x.dtype == torch.float32 and x.numel() == (n + 255) // 256 for x in scales), "m_scale and v_scale are float32, one for 256 elements")
-        else:
-            need(scales == [None, None], "scales belong to states in 8 bits")
-        there = [x for x in (param, grad, m, v, master, *scales) if x is not None]
-        need(all(x.is_contiguous() for x in there), "tensors are contiguous")
-        devices.update(x.get_device() for x in there)
-        written = [x.data_ptr() for x in there if x is not grad]
-        need(not seen & set(written) and len(set(written)) == len(written), "a tensor appears twice")
-        seen.update(written)
-        array[k] = lsp_adamw_item(param.data_ptr(), grad.data_ptr(), m.data_ptr(), v.data_ptr(), *(None if x is None else x.data_ptr() for x in (*scales, master)), n,
-                                  t.get("rate_factor", 1.0), t.get("decay", 0.0), code[param.dtype], code[grad.dtype])
-    need(len(kinds) == 1, "states are all in fp32 or all in 8 bits")
-    need(len(devices) == 1, "the tensors are on one device")
-    return AdamwItems(array, kinds.pop())
+    one for 256 elements), optionally master (float32), rate_factor (1) and decay (0).  Tensors are contiguous, of one size and on one device, and what is written overlaps
+    nothing; others are a ValueError.  They are kept alive by the caller, and the array serves as long as they are where they are."""
+    tensors = list(tensors)
+    array = (lsp_adamw_item * len(tensors))()
+    states = (_operators or _operator_calls()).adamw_items(ctypes.addressof(array), tensors)
+    return AdamwItems(array, "8bit" if states else "f32")
 
 
 def lsp_adamw(items: AdamwItems, *, rate: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step: int, grad_scale=None, stream=None, check: bool = True) -> int:

@@ -7,6 +7,10 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <algorithm>
+#include <new>
+#include <vector>
+
 #include "lsp.h"
 
 namespace {
@@ -35,6 +39,9 @@ PyObject* g_shape;
 PyObject* g_stride;
 PyObject* g_dtype;
 PyObject* g_get_device;
+PyObject* g_numel;
+PyObject* g_is_contiguous;
+PyObject* g_element_size;
 PyObject* g_types[3];         // torch's types, in the order of lsp_dtype; from the first descriptor on
 PyObject* g_int32;
 PyObject* g_int64;
@@ -458,7 +465,8 @@ PyObject* rotary_problem(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     void* n[3];
     const int64_t tokens[2] = {q.shape[0], q.shape[1]};
     for (int i = 0; i < 3; ++i) if (!whole_numbers(args[12 + i], i == 0 ? 2 : 1, tokens, g_int32, n[i], what)) return nullptr;
-    if (!on_one_device(args + 1, 14, what)) return nullptr;
+    PyObject* const elsewhere[5] = {args[1], args[11], args[12], args[13], args[14]};       // (what a program may well have on the host)
+    if (!on_one_device(elsewhere, 5, what)) return nullptr;
     Args tail(args + 15);
     const int32_t neighbours = PyObject_IsTrue(*tail.a++), norm = tail.int32();
     bool ok = tail.ok;
@@ -487,7 +495,6 @@ PyObject* rotary_gradients(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     for (const Tensor& x : t) if (type_code(x.dtype) < 0 || x.dtype != t[0].dtype) return refuse("rotary_gradients: dQr, dKr, dQ and dK are of one type, float32, float16 or bfloat16");
     void* w[4];
     for (int i = 0; i < 4; ++i) if (!vector(args[5 + i], t[0].shape[3], g_types[LSP_F32], w[i], what)) return nullptr;
-    if (!on_one_device(args + 1, 8, what)) return nullptr;
     for (int i = 0; i < 4; ++i) { d->q_shape[i] = t[2].shape[i]; d->k_shape[i] = t[3].shape[i]; d->kr_shape[i] = t[1].shape[i]; }
     d->dtype = type_code(t[0].dtype);
     d->g = lsp_rotary_gradients{t[0].data, t[1].data, t[2].data, t[3].data, static_cast<float*>(w[0]), static_cast<float*>(w[1]), static_cast<float*>(w[2]), static_cast<float*>(w[3]),
@@ -521,7 +528,8 @@ PyObject* cross_entropy_problem(PyObject*, PyObject* const* args, Py_ssize_t nar
     float *losses, *logs;
     if (args[3] == Py_None || args[4] == Py_None) return refuse("cross_entropy_problem: targets and losses are wanted");
     if (!whole_numbers(args[3], 1, h.shape, g_int64, targets, what) || !floats(args[4], h.shape[0], losses, what) || !floats(args[5], h.shape[0], logs, what)) return nullptr;
-    if (!on_one_device(args + 1, 5, what)) return nullptr;
+    PyObject* const elsewhere[2] = {args[1], args[3]};                                     // (what a program may well have on the host)
+    if (!on_one_device(elsewhere, 2, what)) return nullptr;
     bool ok = true;
     const float smoothing = number(args[6], ok), z_loss = number(args[7], ok);
     if (!ok) return nullptr;
@@ -545,7 +553,7 @@ PyObject* cross_entropy_gradients(PyObject*, PyObject* const* args, Py_ssize_t n
     float* weights;
     Tensor n;
     if (args[3] != Py_None && !n.read(args[3], 1, what)) return nullptr;
-    if (!floats(args[3], -1, weights, what) || !on_one_device(args + 1, 3, what)) return nullptr;
+    if (!floats(args[3], -1, weights, what)) return nullptr;
     bool ok = true;
     const float scale = number(args[4], ok);
     if (!ok) return nullptr;
@@ -554,6 +562,102 @@ PyObject* cross_entropy_gradients(PyObject*, PyObject* const* args, Py_ssize_t n
     d->dtype = type_code(dtype);
     d->g = lsp_cross_entropy_gradients{t[0].data, t[1].data, weights, t[0].stride[0], t[1].stride[0], scale};
     Py_RETURN_NONE;
+}
+
+// What a tensor of any shape says of itself; false with a Python exception set
+struct Flat {
+    PyObject* t = nullptr;                             // borrowed; NULL: None
+    uintptr_t data = 0;
+    int64_t   count = 0, element = 0;
+    PyObject* dtype = nullptr;
+    long      device = 0;
+    static bool number(PyObject* t, PyObject* name, int64_t& to) {
+        PyObject* x = PyObject_CallMethodNoArgs(t, name);
+        if (!x) return false;
+        to = PyLong_AsLongLong(x);
+        Py_DECREF(x);
+        return !PyErr_Occurred();
+    }
+    bool read(PyObject* x) {
+        if (!x || x == Py_None) return true;
+        t = x;
+        PyObject* type = PyObject_GetAttr(x, g_dtype);
+        PyObject* at = type ? PyObject_CallMethodNoArgs(x, g_data_ptr) : nullptr;
+        if (!at) { Py_XDECREF(type); return false; }
+        dtype = type;
+        Py_DECREF(type);
+        data = (uintptr_t)PyLong_AsUnsignedLongLongMask(at);
+        Py_DECREF(at);
+        int64_t whole = 0;
+        if (PyErr_Occurred() || !number(x, g_numel, count) || !number(x, g_is_contiguous, whole) || !device_of(x, device)) return false;
+        const int code = type_code(dtype);
+        if (code >= 0) element = code == LSP_F32 ? 4 : 2;
+        else if (!number(x, g_element_size, element)) return false;
+        if (!whole) { refuse("adamw_items: tensors are contiguous"); return false; }
+        return true;
+    }
+};
+
+PyObject* fill_adamw_items(PyObject* const* args, Py_ssize_t nargs) {
+    if (!count_is(nargs, 2)) return nullptr;
+    Args head(args);
+    auto* to = static_cast<lsp_adamw_item*>(head.pointer());
+    if (!head.ok || !know_types()) return nullptr;
+    if (!PyList_Check(args[1]) || PyList_GET_SIZE(args[1]) == 0) return refuse("adamw_items: tensors are wanted");
+    const char* names[9] = {"param", "grad", "m", "v", "m_scale", "v_scale", "master", "rate_factor", "decay"};
+    struct Range { uintptr_t begin, end; bool written; };
+    std::vector<Range> ranges;
+    int states = -1;
+    long device = 0;
+    for (Py_ssize_t i = 0; i < PyList_GET_SIZE(args[1]); ++i) {
+        PyObject* d = PyList_GET_ITEM(args[1], i);
+        if (!PyDict_Check(d)) return refuse("adamw_items: a dict for each tensor is wanted");
+        PyObject* x[9];
+        Py_ssize_t known = 0;
+        for (int k = 0; k < 9; ++k) { x[k] = PyDict_GetItemString(d, names[k]); known += x[k] != nullptr; }
+        if (known != PyDict_GET_SIZE(d)) return refuse("adamw_items: unknown names");
+        Flat f[7];
+        for (int k = 0; k < 7; ++k) if (!f[k].read(x[k])) return nullptr;
+        const Flat &param = f[0], &grad = f[1], &m = f[2], &v = f[3], &ms = f[4], &vs = f[5], &master = f[6];
+        if (!param.t || !grad.t || !m.t || !v.t) return refuse("adamw_items: param, grad, m and v are wanted");
+        if (type_code(param.dtype) < 0 || type_code(grad.dtype) < 0) return refuse("adamw_items: param and grad are float32, float16 or bfloat16");
+        const bool f32 = m.dtype == g_types[LSP_F32] && v.dtype == g_types[LSP_F32], bits8 = m.element == 1 && v.element == 1;
+        if (!f32 && !bits8) return refuse("adamw_items: m and v are both float32 or both of one byte an element");
+        if (master.t && master.dtype != g_types[LSP_F32]) return refuse("adamw_items: master is float32");
+        if (param.count <= 0 || grad.count != param.count || m.count != param.count || v.count != param.count || (master.t && master.count != param.count))
+            return refuse("adamw_items: param, grad, m, v and master are of one size, and not empty");
+        const int64_t blocks = (param.count + 255) / 256;
+        if (bits8 && (!ms.t || !vs.t || ms.dtype != g_types[LSP_F32] || vs.dtype != g_types[LSP_F32] || ms.count != blocks || vs.count != blocks))
+            return refuse("adamw_items: m_scale and v_scale are float32, one for 256 elements");
+        if (f32 && (ms.t || vs.t)) return refuse("adamw_items: scales belong to states in 8 bits");
+        if (states >= 0 && states != (int)bits8) return refuse("adamw_items: states are all in fp32 or all in 8 bits");
+        states = bits8;
+        if (i == 0) device = param.device;
+        for (int k = 0; k < 7; ++k) {
+            if (!f[k].t) continue;
+            if (f[k].device != device) return refuse("adamw_items: the tensors are on one device");
+            ranges.push_back({f[k].data, f[k].data + (uintptr_t)(f[k].count * f[k].element), k != 1});
+        }
+        bool ok = true;
+        const float factor = x[7] ? number(x[7], ok) : 1.0f, decay = x[8] && ok ? number(x[8], ok) : 0.0f;
+        if (!ok) return nullptr;
+        to[i] = lsp_adamw_item{(void*)param.data, (const void*)grad.data, (void*)m.data, (void*)v.data, (float*)ms.data, (float*)vs.data, (float*)master.data, param.count, factor, decay,
+                               type_code(param.dtype), type_code(grad.dtype)};
+    }
+    // what is written overlaps nothing (gradients may overlap one another)
+    std::sort(ranges.begin(), ranges.end(), [](const Range& a, const Range& b) { return a.begin < b.begin; });
+    uintptr_t written = 0, any = 0;
+    for (const Range& r : ranges) {
+        if (r.begin < (r.written ? any : written)) return refuse("adamw_items: tensors overlap, or one appears twice");
+        any = std::max(any, r.end);
+        if (r.written) written = std::max(written, r.end);
+    }
+    return PyLong_FromLong(states);
+}
+// (address of an array of lsp_adamw_item, list of as many dicts): fills the array, and says which states they are
+PyObject* adamw_items(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    try { return fill_adamw_items(args, nargs); }
+    catch (const std::bad_alloc&) { return PyErr_NoMemory(); }
 }
 
 // The binding's classes of descriptors: those of the C structures and, derived from these, those that are made of tensors
@@ -691,7 +795,7 @@ PyMethodDef g_methods[] = {
     method<residual_norm_forward>("residual_norm_forward"), method<residual_norm_backward>("residual_norm_backward"),
     method<rotary_problem>("rotary_problem"), method<rotary_gradients>("rotary_gradients"), method<rotary_forward>("rotary_forward"), method<rotary_backward>("rotary_backward"),
     method<cross_entropy_problem>("cross_entropy_problem"), method<cross_entropy_gradients>("cross_entropy_gradients"),
-    method<cross_entropy_forward>("cross_entropy_forward"), method<cross_entropy_backward>("cross_entropy_backward"),
+    method<cross_entropy_forward>("cross_entropy_forward"), method<cross_entropy_backward>("cross_entropy_backward"), method<adamw_items>("adamw_items"),
     method<bind_operators>("bind_operators"), {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_call", "Argument marshalling of the per-step entry points.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
@@ -707,6 +811,9 @@ PyMODINIT_FUNC PyInit__call(void) {
     g_stride = PyUnicode_InternFromString("stride");
     g_dtype = PyUnicode_InternFromString("dtype");
     g_get_device = PyUnicode_InternFromString("get_device");
+    g_numel = PyUnicode_InternFromString("numel");
+    g_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    g_element_size = PyUnicode_InternFromString("element_size");
     PyObject* ctypes = PyImport_ImportModule("ctypes");
     if (!ctypes) return nullptr;
     g_argument_error = PyObject_GetAttrString(ctypes, "ArgumentError");
