@@ -518,8 +518,8 @@ int    lsp_residual_norm_backward(const lsp_residual_norm_problem* problem, cons
  * value there in Vr, so that the caches that lsp_attention_forward reads are filled by the call that turns the keys (cache = length and starts =
  * NULL: tensors like K).  Tokens that do not count are not read, and their rows not written; nor are places outside [0, cache).
  *   Q, Qr, dQr, dQ  device, [batch][length][heads][head_dim] of `dtype`; K, V, dK  [batch][length][kv_heads][head_dim];
- *   Kr, Vr, dKr     [batch][cache][kv_heads][head_dim]; each with strides as in attention (multiples of 16 bytes, a position's below 8 MiB; in what
- *                   is written every row has a place of its own).  V and Vr may be NULL, both.
+ *   Kr, Vr, dKr     [batch][cache][kv_heads][head_dim]; each with strides as in attention (multiples of 16 bytes, a position's below 8 MiB, and here a
+ *                   head's below 256 MiB; in what is written every row has a place of its own).  V and Vr may be NULL, both.
  *   Qr may be Q and, where starts is NULL, Kr may be K and Vr V, row on row.  Otherwise what is written overlaps nothing else.
  *   q_weight, k_weight, q_bias, k_bias   device, [head_dim] of `dtype`; NULL: ones, zeros
  *   frequencies     device, [rotated / 2] fp32, radians a position; NULL only where rotated = 0
@@ -583,7 +583,7 @@ int    lsp_rotary_backward(const lsp_rotary_problem* problem, const lsp_rotary_g
  * exponentials are kept in `dtype`, each relative to the largest of its row in a piece of the vocabulary, and become the gradient of z in place: two roundings
  * in 16 bits before the second products, the largest gradient of a row being computed without them (a target's).  No atomics that add: results are the same
  * bits from run to run.  A logit that is not finite reaches its row's loss and dH, and all of dW.
- * Workspaces: 16-byte aligned, as large as the queries say; a bounded size however many rows there are. */
+ * Workspaces: 16-byte aligned, as large as the queries say: bounded but for 4 bytes a row, however many there are. */
 typedef struct {
     const void*    H;
     const void*    W;

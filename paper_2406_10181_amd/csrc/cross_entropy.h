@@ -68,7 +68,7 @@ __device__ __forceinline__ int rows_of_block(const LossArgs& a) {
 template <typename D> __device__ __forceinline__ float gradient_scale(const LossArgs& a) {
     if constexpr (!std::is_same<D, F16>::value) return 1.0f;
     const uint32_t largest = as_const<uint32_t>(a.count)[1];                              // an fp32 number's bits
-    const int exponent = min(max((int)(largest >> 23) - 127, -100), 100);
+    const int exponent = max((int)(largest >> 23) - 127, -100);
     return largest == 0 || largest >= 0x7F800000u ? 1.0f : __uint_as_float((uint32_t)(127 + 13 - exponent) << 23);
 }
 

@@ -36,12 +36,15 @@ __global__ __launch_bounds__((LossProduct<D, TILE, false, false>::kThreads)) voi
     for (int j = 0; j < P::NI; ++j) {
         const int row = r0 + 16 * (wn * P::NI + j) + (lane & 15);
         const int want = a.target[row] - first - 4 * g;                                   // (a lane has v = first + 4 g + 16 i + 0..3)
-        float hit = 0.0f, plain = 0.0f;
+        float plain = 0.0f;
+        if (__any(want >= 0 && want < P::kRange)) {                                       // (few pieces have the target of any of 16 rows)
+            float hit = 0.0f;
 #pragma unroll
-        for (int i = 0; i < P::MI; ++i)
+            for (int i = 0; i < P::MI; ++i)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) hit = want == 16 * i + x ? p.acc[j][i][x] : hit;
-        if (want >= 0 && want < P::kRange && (want & 12) == 0) a.hit[row] = hit;
+                for (int x = 0; x < 4; ++x) hit = want == 16 * i + x ? p.acc[j][i][x] : hit;
+            if (want >= 0 && want < P::kRange && (want & 12) == 0) a.hit[row] = hit;
+        }
         if (a.smoothing > 0.0f) {                                                         // (z behind the vocabulary is 0)
 #pragma unroll
             for (int i = 0; i < P::MI; ++i)

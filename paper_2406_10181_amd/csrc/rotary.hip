@@ -2,8 +2,9 @@
 //
 // Bound by memory: a head is read and written once (backward: its gradient read, what was normed read again, a gradient written).  A group of 4, 8 or 16 lanes has a
 // head, eight elements a lane, so that the sums of a norm go through the lanes of a group by moves that need no LDS.  A lane's eight elements are four
-// whole pairs: four elements from each half of what turns, or eight neighbours; so turning needs no other lane.  A workgroup has the queries, the keys or the values of a few tokens
-// that follow one another; its angles, an fp64 product, a sine and a cosine each, are made once for all their heads and lie in LDS.
+// whole pairs: four elements from each half of what turns, or eight neighbours; so turning needs no other lane.  A wave has 4, 8 or 16 heads of one token at a time, whose addresses are a scalar
+// base and what the lane adds to it once (with addresses of its own for every head a lane spent 240 instructions on one in the backward pass).  A workgroup has the queries, the keys
+// or the values of a few tokens that follow one another; its angles, an fp64 product, a sine and a cosine each, are made once for all their heads and lie in LDS.
 #include <algorithm>
 
 #include "rotary.h"
@@ -38,13 +39,15 @@ struct Place {
 };
 
 template <typename D> struct Raw { u32x4 a, b; };                        // 16 bits: the first two words of each
-template <typename D> __device__ __forceinline__ Raw<D> load_raw(const uint8_t* row, const Place& at) {
+// Bytes from a base to a lane's two fours
+struct Reach { uint32_t first, second; };
+template <typename D> __device__ __forceinline__ Raw<D> load_raw(const uint8_t* base, const Reach& at) {
     Raw<D> r;
     if constexpr (D::size == 4) {
-        r.a = *reinterpret_cast<const u32x4*>(row + at.first * 4);
-        r.b = *reinterpret_cast<const u32x4*>(row + at.second * 4);
+        r.a = *reinterpret_cast<const u32x4*>(base + at.first);
+        r.b = *reinterpret_cast<const u32x4*>(base + at.second);
     } else {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(row + at.first * 2), y = *reinterpret_cast<const u32x2*>(row + at.second * 2);
+        const u32x2 x = *reinterpret_cast<const u32x2*>(base + at.first), y = *reinterpret_cast<const u32x2*>(base + at.second);
         r.a[0] = x[0]; r.a[1] = x[1]; r.b[0] = y[0]; r.b[1] = y[1];
     }
     return r;
@@ -55,21 +58,26 @@ template <typename D> __device__ __forceinline__ Eight widen_raw(const Raw<D>& r
     for (int k = 0; k < D::size; ++k) { p.w[k] = r.a[k]; p.w[D::size + k] = r.b[k]; }
     return widen_eight<D>(p);
 }
-template <typename D> __device__ __forceinline__ void store_raw(uint8_t* row, const Place& at, const Eight& x) {
+template <typename D> __device__ __forceinline__ void store_raw(uint8_t* base, const Reach& at, const Eight& x) {
     const Packed<D> o = narrow_eight<D>(x);
     if constexpr (D::size == 4) {
-        *reinterpret_cast<u32x4*>(row + at.first * 4) = u32x4{o.w[0], o.w[1], o.w[2], o.w[3]};
-        *reinterpret_cast<u32x4*>(row + at.second * 4) = u32x4{o.w[4], o.w[5], o.w[6], o.w[7]};
+        *reinterpret_cast<u32x4*>(base + at.first) = u32x4{o.w[0], o.w[1], o.w[2], o.w[3]};
+        *reinterpret_cast<u32x4*>(base + at.second) = u32x4{o.w[4], o.w[5], o.w[6], o.w[7]};
     } else {
-        *reinterpret_cast<u32x2*>(row + at.first * 2) = u32x2{o.w[0], o.w[1]};
-        *reinterpret_cast<u32x2*>(row + at.second * 2) = u32x2{o.w[2], o.w[3]};
+        *reinterpret_cast<u32x2*>(base + at.first) = u32x2{o.w[0], o.w[1]};
+        *reinterpret_cast<u32x2*>(base + at.second) = u32x2{o.w[2], o.w[3]};
     }
+}
+// `head`: the lane's, of those that its wave has at a time
+template <typename D> __device__ __forceinline__ Reach reach_of(const Place& at, const Strided& s, int head) {
+    const uint32_t begin = (uint32_t)(head * s.head) * D::size;
+    return {begin + at.first * D::size, begin + at.second * D::size};
 }
 template <typename D> __device__ __forceinline__ Eight load_vector(const void* v, const Place& at, float otherwise) {
     Eight r;
 #pragma unroll
     for (int e = 0; e < 8; ++e) r.x[e] = otherwise;
-    if (v && at.there) r = widen_raw<D>(load_raw<D>(static_cast<const uint8_t*>(v), at));
+    if (v && at.there) r = widen_raw<D>(load_raw<D>(static_cast<const uint8_t*>(v), Reach{(uint32_t)at.first * D::size, (uint32_t)at.second * D::size}));
     return r;
 }
 
@@ -116,18 +124,23 @@ __device__ __forceinline__ void angles_of(const Tokens& t, int token, const Plac
     cos = f32x4{1.0f, 1.0f, 1.0f, 1.0f}; sin = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if (at.pair >= 0) { cos = *reinterpret_cast<const f32x4*>(&t.cos[token][at.pair]); sin = *reinterpret_cast<const f32x4*>(&t.sin[token][at.pair]); }
 }
-// Heads of tokens that follow one another, every `step`-th from the r-th on
+// A number that is the same in all lanes, in scalar registers
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+// The first of some heads of a token
+template <typename D> __device__ __forceinline__ uint8_t* heads_at(const Strided& s, int64_t token, int head) {
+    return global_pointer(static_cast<uint8_t*>(const_cast<void*>(s.p)) + (token + head * s.head) * D::size);
+}
+// What a wave does one after another: heads of tokens
 struct Walk {
-    int token, head;
-    __device__ __forceinline__ Walk(int r, int heads) { token = r / heads; head = r - token * heads; }
-    __device__ __forceinline__ void advance(int by_tokens, int by_heads, int heads) {
-        token += by_tokens; head += by_heads;
-        if (head >= heads) { head -= heads; ++token; }
+    int token, block;                                                    // of the workgroup's tokens; of a token's heads
+    __device__ __forceinline__ Walk(int u, int blocks) { token = u / blocks; block = u - token * blocks; }
+    __device__ __forceinline__ void advance(int by_tokens, int by_blocks, int blocks) {
+        token += by_tokens; block += by_blocks;
+        if (block >= blocks) { block -= blocks; ++token; }
     }
 };
-template <typename D> __device__ __forceinline__ uint8_t* head_at(const Strided& s, int64_t token, int head) {
-    return static_cast<uint8_t*>(const_cast<void*>(s.p)) + (token + head * s.head) * D::size;
-}
 __device__ __forceinline__ const RotarySegment& segment_of(const RotaryArgs& a, int& block, int& which) {
     which = 0;
     if (a.segments > 1 && block >= a.segment[1].first) which = 1;
@@ -136,7 +149,7 @@ __device__ __forceinline__ const RotarySegment& segment_of(const RotaryArgs& a, 
     return a.segment[which];
 }
 
-template <int NORM, int GROUP> __device__ __forceinline__ void norm_head(Eight& x, float& factor, const Place& at, int head_dim, float eps) {
+template <int NORM, int GROUP> __device__ __forceinline__ void norm_head(Eight& x, float& factor, bool there, int head_dim, float eps) {
     factor = 1.0f;
     if constexpr (NORM != LSP_NORM_NONE) {
         const float share = 1.0f / (float)head_dim;
@@ -146,7 +159,7 @@ template <int NORM, int GROUP> __device__ __forceinline__ void norm_head(Eight& 
             for (int e = 0; e < 8; ++e) sum += x.x[e];
             const float mean = group_sum<GROUP>(sum) * share;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x.x[e] = at.there ? x.x[e] - mean : 0.0f;
+            for (int e = 0; e < 8; ++e) x.x[e] = there ? x.x[e] - mean : 0.0f;
         }
         float squares = 0.0f;
 #pragma unroll
@@ -154,38 +167,44 @@ template <int NORM, int GROUP> __device__ __forceinline__ void norm_head(Eight& 
         // (v_rsq_f32, within an ulp, takes what is below 2^-126 for zero: where eps does not keep the sum above that, the root and quotient that IEEE has)
         const float sum = fmaf(group_sum<GROUP>(squares), share, eps);
         factor = eps >= 0x1p-126f ? __builtin_amdgcn_rsqf(sum) : 1.0f / sqrtf(sum);
+        if (!there) factor = 0.0f;                                       // (of no head: one over the root of eps may be anything)
 #pragma unroll
         for (int e = 0; e < 8; ++e) x.x[e] *= factor;
     }
 }
 
+// 4 x 1024 tokens of 32 + 32 heads of 128 in bf16, 134 MB: 24.8 us, 5.4 TB/s; 16384 tokens of 16 + 16 heads of 64 in fp32, 268 MB, 47.7 us, 5.6 TB/s.
 template <typename D, int NORM, int GROUP, bool NEIGHBOURS>
 __global__ __launch_bounds__(kRotaryThreads) void k_rotary(RotaryArgs a) {
-    constexpr int kGroups = kRotaryThreads / GROUP;
+    constexpr int kHeads = 64 / GROUP, kWaves = kRotaryThreads / 64;     // heads that a wave has at a time
     __shared__ Tokens t;
     int block = blockIdx.x, which;
     const RotarySegment& s = segment_of(a, block, which);
     const int group = block / s.parts, part = block - group * s.parts, first = group * s.tokens, n = min(s.tokens, a.batch * a.length - first);
     const Place at(a, threadIdx.x % GROUP);
-    const int heads = s.heads, step = kGroups * s.parts, by_tokens = step / heads, by_heads = step - by_tokens * heads;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), own = (threadIdx.x & 63) / GROUP;
+    const int blocks = (s.heads + kHeads - 1) / kHeads, step = kWaves * s.parts, by_tokens = step / blocks, by_blocks = step - by_tokens * blocks;
     const Eight w = load_vector<D>(which < 2 ? s.weight : nullptr, at, 1.0f), bias = load_vector<D>(which < 2 ? s.bias : nullptr, at, 0.0f);
+    const Reach from = reach_of<D>(at, s.x, own), to = reach_of<D>(at, s.y, own);
     set_tokens(t, a, s, first, n, false);
-    Walk now(part * kGroups + threadIdx.x / GROUP, heads);
+    Walk now(part * kWaves + wave, blocks);
+    const auto there = [&](const Walk& k) { return at.there && k.block * kHeads + own < s.heads; };
     const auto fetch = [&](const Walk& k) {
         Raw<D> r;
         r.a = r.b = u32x4{0, 0, 0, 0};
-        if (k.token < n && at.there && t.x[k.token] >= 0) r = load_raw<D>(head_at<D>(s.x, t.x[k.token], k.head), at);
+        if (k.token < n) {
+            const int64_t x = uniform(t.x[k.token]);
+            if (x >= 0 && there(k)) r = load_raw<D>(heads_at<D>(s.x, x, k.block * kHeads), from);
+        }
         return r;
     };
-    Raw<D> raw = fetch(now);
-    while (now.token < n) {
-        Walk next = now;
-        next.advance(by_tokens, by_heads, heads);
-        const Raw<D> ahead = fetch(next);
+    const auto work = [&](const Raw<D>& raw) {
+        const int64_t y = uniform(t.y[now.token]);
+        if (y < 0) return;                                               // (the token does not count, or its place is not in the cache)
         Eight x = widen_raw<D>(raw);
         if (which < 2) {
             float factor;
-            norm_head<NORM, GROUP>(x, factor, at, a.head_dim, a.eps);
+            norm_head<NORM, GROUP>(x, factor, there(now), a.head_dim, a.eps);
             if constexpr (NORM != LSP_NORM_NONE) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x.x[e] = fmaf(x.x[e], w.x[e], bias.x[e]);
@@ -194,24 +213,40 @@ __global__ __launch_bounds__(kRotaryThreads) void k_rotary(RotaryArgs a) {
             angles_of(t, now.token, at, cos, sin);
             turn<NEIGHBOURS, false>(x, cos, sin);
         }
-        if (at.there && t.y[now.token] >= 0) store_raw<D>(head_at<D>(s.y, t.y[now.token], now.head), at, x);
-        raw = ahead;
+        if (there(now)) store_raw<D>(heads_at<D>(s.y, y, now.block * kHeads), to, x);
+    };
+    // two sets of registers, one asked for while the other is worked on
+    Raw<D> even = fetch(now), odd;
+    while (now.token < n) {
+        Walk next = now;
+        next.advance(by_tokens, by_blocks, blocks);
+        odd = fetch(next);
+        work(even);
+        now = next;
+        if (now.token >= n) break;
+        next.advance(by_tokens, by_blocks, blocks);
+        even = fetch(next);
+        work(odd);
         now = next;
     }
 }
 
 // With y = xhat w + b turned by the angle, and d the gradient of the result turned back:  dw += d xhat, db += d, and with e = d w
 //   dx = factor (e - xhat mean(e xhat) [- mean(e), for a norm with means]).
-template <typename D, int NORM, int GROUP, bool NEIGHBOURS>
-__global__ __launch_bounds__(kRotaryThreads) void k_rotary_back(RotaryArgs a) {
-    constexpr int kGroups = kRotaryThreads / GROUP;
+// Five waves a SIMD in 16 bits, for which sums of biases are left out where nobody asks for them (BIAS): 3 x 777 padded tokens of 16 + 4 heads of 80 in fp16, with means and biases, 12.0 us, with four
+// waves 15.6; 4 x 1024 tokens of 32 + 32 heads of 128 in bf16, 39.7 us (5.1 TB/s), with four 42.1.
+template <typename D, int NORM, int GROUP, bool NEIGHBOURS, bool BIAS>
+__global__ __launch_bounds__(kRotaryThreads, D::size == 4 ? 4 : 5) void k_rotary_back(RotaryArgs a) {
+    constexpr int kHeads = 64 / GROUP, kWaves = kRotaryThreads / 64, kGroups = kRotaryThreads / GROUP;
     __shared__ Tokens t;
     int block = blockIdx.x, which;
     const RotarySegment& s = segment_of(a, block, which);
     const Place at(a, threadIdx.x % GROUP);
-    const int own = threadIdx.x / GROUP, heads = s.heads, step = kGroups * s.parts, by_tokens = step / heads, by_heads = step - by_tokens * heads;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), own = (threadIdx.x & 63) / GROUP;
+    const int blocks = (s.heads + kHeads - 1) / kHeads, step = kWaves * s.parts, by_tokens = step / blocks, by_blocks = step - by_tokens * blocks;
     const int tokens = a.batch * a.length, groups = (tokens + s.tokens - 1) / s.tokens * s.parts;
     const Eight w = load_vector<D>(s.weight, at, 1.0f);
+    const Reach of_x = reach_of<D>(at, s.x, own), of_d = reach_of<D>(at, s.y, own), of_out = reach_of<D>(at, s.out, own);
     Eight dw, db;
 #pragma unroll
     for (int e = 0; e < 8; ++e) dw.x[e] = db.x[e] = 0.0f;
@@ -220,35 +255,35 @@ __global__ __launch_bounds__(kRotaryThreads) void k_rotary_back(RotaryArgs a) {
         const int group = block / s.parts, part = block - group * s.parts, first = group * s.tokens, n = min(s.tokens, tokens - first);
         __syncthreads();                                                 // (the tokens before are done with)
         set_tokens(t, a, s, first, n, true);
-        Walk now(part * kGroups + own, heads);
+        Walk now(part * kWaves + wave, blocks);
+        const auto there = [&](const Walk& k) { return at.there && k.block * kHeads + own < s.heads; };
         const auto fetch = [&](const Walk& k) {
             Both r;
             r.d.a = r.d.b = r.x.a = r.x.b = u32x4{0, 0, 0, 0};
-            if (k.token < n && at.there && t.y[k.token] >= 0) {
-                r.d = load_raw<D>(head_at<D>(s.y, t.y[k.token], k.head), at);
-                if constexpr (NORM != LSP_NORM_NONE) r.x = load_raw<D>(head_at<D>(s.x, t.x[k.token], k.head), at);
+            if (k.token < n) {
+                const int64_t y = uniform(t.y[k.token]), x = uniform(t.x[k.token]);
+                if (y >= 0 && there(k)) {
+                    r.d = load_raw<D>(heads_at<D>(s.y, y, k.block * kHeads), of_d);
+                    if constexpr (NORM != LSP_NORM_NONE) r.x = load_raw<D>(heads_at<D>(s.x, x, k.block * kHeads), of_x);
+                }
             }
             return r;
         };
-        Both raw = fetch(now);
-        while (now.token < n) {
-            Walk next = now;
-            next.advance(by_tokens, by_heads, heads);
-            const Both ahead = fetch(next);
+        const auto work = [&](const Both& raw) {
             Eight d = widen_raw<D>(raw.d);
-            if (t.y[now.token] >= 0) {                                   // (the same for a group's lanes; otherwise d is zeros, and stays)
+            if (uniform(t.y[now.token]) >= 0) {                          // (otherwise d is zeros, and stays)
                 f32x4 cos, sin;
                 angles_of(t, now.token, at, cos, sin);
                 turn<NEIGHBOURS, true>(d, cos, sin);
                 if constexpr (NORM != LSP_NORM_NONE) {
                     Eight x = widen_raw<D>(raw.x);
                     float factor;
-                    norm_head<NORM, GROUP>(x, factor, at, a.head_dim, a.eps);
+                    norm_head<NORM, GROUP>(x, factor, there(now), a.head_dim, a.eps);
                     float along = 0.0f, sum = 0.0f;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         dw.x[e] = fmaf(d.x[e], x.x[e], dw.x[e]);
-                        db.x[e] += d.x[e];
+                        if constexpr (BIAS) db.x[e] += d.x[e];
                         d.x[e] *= w.x[e];
                         along = fmaf(d.x[e], x.x[e], along);
                         sum += d.x[e];
@@ -260,19 +295,30 @@ __global__ __launch_bounds__(kRotaryThreads) void k_rotary_back(RotaryArgs a) {
                     for (int e = 0; e < 8; ++e) d.x[e] = factor * (d.x[e] - fmaf(x.x[e], along, mean));
                 }
             }
-            if (at.there) store_raw<D>(head_at<D>(s.out, t.out[now.token], now.head), at, d);
-            raw = ahead;
+            if (there(now)) store_raw<D>(heads_at<D>(s.out, uniform(t.out[now.token]), now.block * kHeads), of_out, d);
+        };
+        Both even = fetch(now), odd;
+        while (now.token < n) {
+            Walk next = now;
+            next.advance(by_tokens, by_blocks, blocks);
+            odd = fetch(next);
+            work(even);
+            now = next;
+            if (now.token >= n) break;
+            next.advance(by_tokens, by_blocks, blocks);
+            even = fetch(next);
+            work(odd);
             now = next;
         }
     }
     if (NORM == LSP_NORM_NONE || !a.sums) return;
     __shared__ float all[kGroups][GROUP * 8 + 4];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < (BIAS ? 2 : 1); ++k) {
         __syncthreads();
         if (at.there) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) all[own][e < 4 ? at.first + e : at.second + e - 4] = k ? db.x[e] : dw.x[e];
+            for (int e = 0; e < 8; ++e) all[threadIdx.x / GROUP][e < 4 ? at.first + e : at.second + e - 4] = k ? db.x[e] : dw.x[e];
         }
         __syncthreads();
         if ((int)threadIdx.x < a.head_dim) {
@@ -289,7 +335,7 @@ __global__ __launch_bounds__(1024) void k_rotary_sums(RotaryArgs a) {
     const RotarySegment& s = a.segment[blockIdx.y >> 1];
     const int k = blockIdx.y & 1, column = blockIdx.x * 16 + (threadIdx.x & 15), run = threadIdx.x >> 4;
     float* const to = k ? s.bias_sum : s.weight_sum;
-    if (!to) return;
+    if (!to) return;                                                     // (and if nobody asks for a bias' sum there is none)
     float x = 0.0f;
     if (column < a.head_dim) {
 #pragma unroll 8
@@ -308,20 +354,21 @@ __global__ __launch_bounds__(1024) void k_rotary_sums(RotaryArgs a) {
 
 static int group_of(int head_dim) { return head_dim <= 32 ? 4 : head_dim <= 64 ? 8 : 16; }
 
-// A workgroup has the tokens whose heads give each of its lane groups 16 of them, or as few as give 1024 workgroups; where one token each gives fewer, its heads are shared.
-// Backward with sums: at most 1024 workgroups that go on, since each leaves a part of the sums.
+// A workgroup has the tokens whose heads give each of its waves 16 steps, or as few as give 1024 workgroups; where one token each gives fewer, its heads are shared.
+// Backward with sums: at most 640 workgroups of each that go on, as many as run at once, since each leaves a part of the sums.
 void plan_rotary(RotaryArgs& a, bool backward) {
     const int64_t tokens = (int64_t)a.batch * a.length;
-    const int groups = kRotaryThreads / group_of(a.head_dim);
+    const int at_a_time = 64 / group_of(a.head_dim), waves = kRotaryThreads / 64;
     a.blocks = 0;
     for (int k = 0; k < a.segments; ++k) {
         RotarySegment& s = a.segment[k];
-        s.tokens = (int)std::min<int64_t>({std::max(1, 16 * groups / s.heads), kRotaryTokens, std::max<int64_t>(1, tokens / 1024)});
+        const int steps = (s.heads + at_a_time - 1) / at_a_time;          // of a token
+        s.tokens = (int)std::min<int64_t>({std::max(1, 16 * waves / steps), kRotaryTokens, std::max<int64_t>(1, tokens / 1024)});
         const int64_t of_tokens = (tokens + s.tokens - 1) / s.tokens;
-        s.parts = s.tokens > 1 ? 1 : (int)std::min<int64_t>((s.heads + groups - 1) / groups, std::max<int64_t>(1, 1024 / of_tokens));
+        s.parts = s.tokens > 1 ? 1 : (int)std::min<int64_t>((steps + waves - 1) / waves, std::max<int64_t>(1, 1024 / of_tokens));
         const int64_t blocks = of_tokens * s.parts;
         s.first = a.blocks;
-        s.blocks = (int)(backward && a.sums ? std::min<int64_t>(blocks, 1024) : blocks);
+        s.blocks = (int)(backward && a.sums ? std::min<int64_t>(blocks, 640) : blocks);
         a.blocks += s.blocks;
     }
 }
@@ -330,8 +377,14 @@ size_t rotary_partial_bytes(const RotaryArgs& a) { return a.sums ? align_up((siz
 template <typename D, int NORM, int GROUP> static void launch_one(const RotaryArgs& a, bool backward, hipStream_t st) {
     const dim3 grid((unsigned)a.blocks), block(kRotaryThreads);
     if (backward) {
-        if (a.neighbours) hipLaunchKernelGGL((k_rotary_back<D, NORM, GROUP, true>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((k_rotary_back<D, NORM, GROUP, false>), grid, block, 0, st, a);
+        const bool bias = NORM != LSP_NORM_NONE && (a.segment[0].bias_sum || a.segment[1].bias_sum);
+        const auto with = [&](auto b) {
+            if (a.neighbours) hipLaunchKernelGGL((k_rotary_back<D, NORM, GROUP, true, decltype(b)::value>), grid, block, 0, st, a);
+            else hipLaunchKernelGGL((k_rotary_back<D, NORM, GROUP, false, decltype(b)::value>), grid, block, 0, st, a);
+        };
+        if constexpr (NORM == LSP_NORM_NONE) with(std::false_type{});
+        else if (bias) with(std::true_type{});
+        else with(std::false_type{});
     } else {
         if (a.neighbours) hipLaunchKernelGGL((k_rotary<D, NORM, GROUP, true>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((k_rotary<D, NORM, GROUP, false>), grid, block, 0, st, a);

@@ -20,6 +20,11 @@ int check_rotary_shape(const lsp_rotary_problem* p, lsp_dtype t) {
     return LSP_OK;
 }
 
+// One operand's strides: as in attention, and heads less than 256 MiB apart (16 of them are addressed with 32 bits)
+int check_heads(const int64_t (&s)[3], int64_t batch, int64_t positions, int64_t heads, int32_t dim, lsp_dtype t, bool written) {
+    const int rc = check_strides(s, batch, positions, heads, dim, t, written);
+    return rc == LSP_OK && heads > 1 && s[2] * elem_size(t) >= ((int64_t)1 << 28) ? LSP_ERR_SHAPE : rc;
+}
 bool same_strides(const int64_t (&a)[3], const int64_t (&b)[3], int64_t batch, int64_t positions, int64_t heads) {
     return (batch == 1 || a[0] == b[0]) && (positions == 1 || a[1] == b[1]) && (heads == 1 || a[2] == b[2]);
 }
@@ -33,13 +38,13 @@ int check_rotary(const lsp_rotary_problem* p, lsp_dtype t) {
     int rc = check_rotary_shape(p, t);
     if (rc != LSP_OK) return rc;
     if (!(p->eps >= 0.0f) || !std::isfinite(p->eps)) return LSP_ERR_VALUE;
-    if ((rc = check_strides(p->q_stride, p->batch, p->length, p->heads, p->head_dim, t, false)) != LSP_OK) return rc;
-    if ((rc = check_strides(p->k_stride, p->batch, p->length, p->kv_heads, p->head_dim, t, false)) != LSP_OK) return rc;
-    if ((rc = check_strides(p->qr_stride, p->batch, p->length, p->heads, p->head_dim, t, true)) != LSP_OK) return rc;
-    if ((rc = check_strides(p->kr_stride, p->batch, p->cache, p->kv_heads, p->head_dim, t, true)) != LSP_OK) return rc;
+    if ((rc = check_heads(p->q_stride, p->batch, p->length, p->heads, p->head_dim, t, false)) != LSP_OK) return rc;
+    if ((rc = check_heads(p->k_stride, p->batch, p->length, p->kv_heads, p->head_dim, t, false)) != LSP_OK) return rc;
+    if ((rc = check_heads(p->qr_stride, p->batch, p->length, p->heads, p->head_dim, t, true)) != LSP_OK) return rc;
+    if ((rc = check_heads(p->kr_stride, p->batch, p->cache, p->kv_heads, p->head_dim, t, true)) != LSP_OK) return rc;
     if (p->V) {
-        if ((rc = check_strides(p->v_stride, p->batch, p->length, p->kv_heads, p->head_dim, t, false)) != LSP_OK) return rc;
-        if ((rc = check_strides(p->vr_stride, p->batch, p->cache, p->kv_heads, p->head_dim, t, true)) != LSP_OK) return rc;
+        if ((rc = check_heads(p->v_stride, p->batch, p->length, p->kv_heads, p->head_dim, t, false)) != LSP_OK) return rc;
+        if ((rc = check_heads(p->vr_stride, p->batch, p->cache, p->kv_heads, p->head_dim, t, true)) != LSP_OK) return rc;
     }
     for (const void* q : {p->Q, p->K, p->V, static_cast<const void*>(p->Qr), static_cast<const void*>(p->Kr), static_cast<const void*>(p->Vr), p->q_weight, p->k_weight, p->q_bias, p->k_bias,
                           static_cast<const void*>(p->frequencies)})
@@ -132,10 +137,10 @@ int lsp_rotary_backward(const lsp_rotary_problem* p, const lsp_rotary_gradients*
     if (!p || !g || !g->dQr || !g->dKr || !g->dQ || !g->dK) return LSP_ERR_NULL;
     int rc = check_rotary(p, dtype);
     if (rc != LSP_OK) return rc;
-    if ((rc = check_strides(g->dqr_stride, p->batch, p->length, p->heads, p->head_dim, dtype, false)) != LSP_OK) return rc;
-    if ((rc = check_strides(g->dkr_stride, p->batch, p->cache, p->kv_heads, p->head_dim, dtype, false)) != LSP_OK) return rc;
-    if ((rc = check_strides(g->dq_stride, p->batch, p->length, p->heads, p->head_dim, dtype, true)) != LSP_OK) return rc;
-    if ((rc = check_strides(g->dk_stride, p->batch, p->length, p->kv_heads, p->head_dim, dtype, true)) != LSP_OK) return rc;
+    if ((rc = check_heads(g->dqr_stride, p->batch, p->length, p->heads, p->head_dim, dtype, false)) != LSP_OK) return rc;
+    if ((rc = check_heads(g->dkr_stride, p->batch, p->cache, p->kv_heads, p->head_dim, dtype, false)) != LSP_OK) return rc;
+    if ((rc = check_heads(g->dq_stride, p->batch, p->length, p->heads, p->head_dim, dtype, true)) != LSP_OK) return rc;
+    if ((rc = check_heads(g->dk_stride, p->batch, p->length, p->kv_heads, p->head_dim, dtype, true)) != LSP_OK) return rc;
     for (const void* q : {g->dQr, g->dKr, static_cast<const void*>(g->dQ), static_cast<const void*>(g->dK), static_cast<const void*>(g->q_weight), static_cast<const void*>(g->k_weight),
                           static_cast<const void*>(g->q_bias), static_cast<const void*>(g->k_bias)})
         if (!aligned16(q)) return LSP_ERR_ALIGN;

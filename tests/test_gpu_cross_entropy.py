@@ -189,10 +189,10 @@ def test_a_captured_call_repeats_with_other_rows():
         c.check()
 
 
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_blocks_of_rows(dtype):
     """More rows than one block of exponentials holds: dW is a sum over blocks."""
-    vocab = 400000 if dtype == "bf16" else 200000                            # 1 GiB is 1280 rows of these
+    vocab = 200000 if dtype == "f32" else 400000                            # 1 GiB is 1280 rows of these
     c = Case(dtype, 2900, 8, vocab, left_out=0.2, seed=9)
     c.backward()
     H, W, t, g = c.H.double(), c.W.double(), c.targets, c.weights.double()
@@ -212,3 +212,19 @@ def test_blocks_of_rows(dtype):
     for got, want in ((c.losses, losses), (c.dH, dH), (c.dW, dW)):
         rel = float((got.double() - want).norm() / want.norm())
         assert rel <= (2e-5 if dtype == "f32" or got is c.losses else 3 * u), rel
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-12, 1.0, 2e4, 1e30])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_scales_of_the_loss(dtype, scale):
+    """Of a scaled loss, or a mean over many tokens: gradients of z keep their digits, whatever fp16's range."""
+    c = Case(dtype, 70, 64, 300, weights=False, scale=scale, seed=11)
+    c.backward()
+    want = ref.cross_entropy(f64(c.H), f64(c.W), c.targets.cpu().numpy(), scale=scale, dtype=dtype)
+    for k in ("dH", "dW"):
+        value, bound = want[k]
+        largest = 65504.0 if dtype == "f16" else 3.38e38
+        inside = np.abs(value) + bound < largest
+        off = np.abs(f64(getattr(c, k)) - value)
+        assert np.all(off[inside] <= bound[inside]), (k, np.max(off[inside] / bound[inside]))
+        assert np.all(np.isinf(f64(getattr(c, k))[np.abs(value) - bound > largest * 1.001]))

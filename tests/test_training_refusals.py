@@ -34,7 +34,7 @@ BAD_ROTARY = [
     (dict(rotated=-8), -2), (dict(rotated=12), -2), (dict(rotated=72), -2), (dict(neighbours=2), -2), (dict(norm=3), -2), (dict(length=1 << 28), -2), (dict(batch=1 << 30), -2),
     (dict(heads=2 ** 31 - 1), -2), (dict(cache=1 << 30), -2),
     (dict(q_stride=THREE(1 << 20, -256, 64)), -2), (dict(k_stride=THREE(1 << 20, 1 << 22, 64)), -2), (dict(qr_stride=THREE(1 << 20, 0, 64)), -2), (dict(kr_stride=THREE(0, 128, 64)), -2),
-    (dict(vr_stride=THREE(1 << 20, 128, 8)), -2), (dict(v_stride=THREE(1 << 41, 128, 64)), -2),
+    (dict(vr_stride=THREE(1 << 20, 128, 8)), -2), (dict(v_stride=THREE(1 << 41, 128, 64)), -2), (dict(k_stride=THREE(1 << 20, 128, 1 << 27)), -2),
     (dict(q_stride=THREE(1 << 20, 256, 60)), -7), (dict(Q=FAKE + 8), -7), (dict(Vr=FAKE + 8), -7), (dict(q_weight=FAKE + 2), -7), (dict(k_bias=FAKE + 8), -7), (dict(frequencies=FAKE + 4), -7),
     (dict(positions=FAKE + 2), -7), (dict(starts=FAKE + 1), -7), (dict(lens=FAKE + 2), -7),
     (dict(eps=-1.0), -10), (dict(eps=NAN), -10), (dict(eps=INF), -10),
