@@ -36,14 +36,14 @@ struct LossArgs {
     float *log_sum;              // [block_rows]: L
     float *factor;               // [block_rows]: scale * weight
     uint8_t* e;                  // [block_rows][padded]
-    float* dh_parts;             // [dh_splits][block_rows][width], where there are several
+    float* dh_parts;             // [dh_splits][block_rows][width], where there are several; or more of fewer rows: parts_of_dh()
     float* dw_sum;               // [vocab][width], where there are several blocks of rows and dW is not fp32
     // plan
     int32_t block_rows, padded;  // multiples of 256
     int32_t blocks, block;       // blocks of rows, and which this is
     int32_t pieces, piece;       // pieces of the vocabulary, of so many
     int32_t tile[3];             // 256 (16 bits only), 128 or 64: of the logits, dH, dW
-    int32_t dh_splits;
+    int32_t dh_splits, dh_room;  // parts of the vocabulary that dH is made of; tiles of rows times parts
     int32_t train;
 };
 
@@ -63,6 +63,13 @@ template <typename D> constexpr float kLossTop = std::is_same<D, F16>::value ? 3
 // Rows of this block that count
 __device__ __forceinline__ int rows_of_block(const LossArgs& a) {
     return min(max(*as_const<int32_t>(a.count) - a.block * a.block_rows, 0), a.block_rows);
+}
+// Parts of the vocabulary that dH is made of, and the rows between two parts' sums: where fewer rows count than there are, their tiles get the workgroups (and the room) that the others would
+// have had.  (3001 rows of which 1800 count, width 1000, 50021 words, fp16: 183 us, with the parts planned for all rows 230.)
+struct LossParts { int splits, rows; };
+__device__ __forceinline__ LossParts parts_of_dh(const LossArgs& a, int rows) {
+    const int tile = a.tile[1], tiles = (rows + tile - 1) / tile;
+    return {a.dh_splits > 1 && tiles > 0 ? a.dh_room / tiles : 1, tiles * tile};
 }
 // fp16: what the gradient of z is multiplied by, a power of two that brings the largest that it can be to 2^14; the products of it are divided by that
 template <typename D> __device__ __forceinline__ float gradient_scale(const LossArgs& a) {

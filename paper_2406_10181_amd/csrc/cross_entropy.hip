@@ -220,9 +220,10 @@ __global__ __launch_bounds__(256) void k_loss_dh_sum(LossArgs a) {
     const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int row = (int)(n / units), d = (int)(n - (int64_t)row * units) * 4;
     if (row >= rows) return;
+    const LossParts parts = parts_of_dh(a, rows);
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 8
-    for (int s = 0; s < a.dh_splits; ++s) sum += *reinterpret_cast<const f32x4*>(a.dh_parts + ((int64_t)s * a.block_rows + row) * a.width + d);
+    for (int s = 0; s < parts.splits; ++s) sum += *reinterpret_cast<const f32x4*>(a.dh_parts + ((int64_t)s * parts.rows + row) * a.width + d);
     store_four<D>(static_cast<uint8_t*>(a.dH) + (a.index[a.block * a.block_rows + row] * a.dh_stride + d) * D::size, sum[0], sum[1], sum[2], sum[3]);
 }
 
@@ -267,6 +268,7 @@ void plan_loss(LossArgs& a, lsp_dtype dtype) {
     a.piece = a.tile[0] / 2;
     a.pieces = a.padded / a.piece;
     best_tile(a.width, rows, a.vocab, fp32, 32, a.tile[1], a.dh_splits);
+    a.dh_room = (int)((rows + a.tile[1] - 1) / a.tile[1]) * a.dh_splits;
     best_tile(a.width, a.vocab, rows, fp32, 1, a.tile[2], whole);
 }
 

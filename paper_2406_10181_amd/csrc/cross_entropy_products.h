@@ -92,12 +92,13 @@ __global__ __launch_bounds__((LossProduct<D, TILE, true, false>::kThreads)) void
     extern __shared__ uint8_t lds_bytes[];
     const Lds lds = (Lds)lds_bytes;
     const int rows = rows_of_block(a);
-    const uint32_t tiles_m = (a.width + P::BM - 1) / P::BM, tiles_n = (rows + P::BN - 1) / P::BN, items = tiles_m * tiles_n * a.dh_splits, item = item_of_block(blockIdx.x, items);
+    const LossParts parts = parts_of_dh(a, rows);
+    const uint32_t tiles_m = (a.width + P::BM - 1) / P::BM, tiles_n = (rows + P::BN - 1) / P::BN, items = tiles_m * tiles_n * parts.splits, item = item_of_block(blockIdx.x, items);
     if (item == items) return;
     const uint32_t split = item / (tiles_m * tiles_n);
     uint32_t tm, tn;
     tile_of_item(item - split * tiles_m * tiles_n, tiles_m, tiles_n, tm, tn);
-    const int d0 = tm * P::BM, r0 = tn * P::BN, steps = (a.vocab + P::BK - 1) / P::BK, share = (steps + a.dh_splits - 1) / a.dh_splits;
+    const int d0 = tm * P::BM, r0 = tn * P::BN, steps = (a.vocab + P::BK - 1) / P::BK, share = (steps + parts.splits - 1) / parts.splits;
     const int v0 = min((int)split * share * P::BK, a.vocab), v1 = min(v0 + share * P::BK, a.vocab);
     const int64_t w_bytes = a.w_stride * D::size, e_bytes = (int64_t)a.padded * D::size;
     P p;
@@ -109,7 +110,7 @@ __global__ __launch_bounds__((LossProduct<D, TILE, true, false>::kThreads)) void
     for (int j = 0; j < P::NI; j += 2) {
         const int row0 = r0 + 16 * (wn * P::NI + j);
         if (a.dh_splits > 1) {
-            float* const to = a.dh_parts + (int64_t)split * a.block_rows * a.width + first;
+            float* const to = a.dh_parts + (int64_t)split * parts.rows * a.width + first;
             store_two_blocks<F32, P::MI>(p.acc + j, factor, lds + wave * (32 * P::kRange * 4), left, lane,
                                          [&](uint32_t r) { return reinterpret_cast<uint8_t*>(to + (int64_t)(row0 + (int)r) * a.width); });
         } else {
@@ -179,7 +180,7 @@ template <typename D, int TILE> static inline hipError_t launch_logits_of(const 
     return launch_tiles<LossProduct<D, TILE, false, false>, &k_loss_logits<D, TILE>>(a, (uint32_t)(a.padded / TILE * (a.block_rows / TILE)), st);
 }
 template <typename D, int TILE> static inline hipError_t launch_dh_of(const LossArgs& a, hipStream_t st) {
-    return launch_tiles<LossProduct<D, TILE, true, false>, &k_loss_dh<D, TILE>>(a, (uint32_t)((a.width + TILE - 1) / TILE * (a.block_rows / TILE) * a.dh_splits), st);
+    return launch_tiles<LossProduct<D, TILE, true, false>, &k_loss_dh<D, TILE>>(a, (uint32_t)((a.width + TILE - 1) / TILE * a.dh_room), st);
 }
 template <typename D, int TILE> static inline hipError_t launch_dw_of(const LossArgs& a, hipStream_t st) {
     return launch_tiles<LossProduct<D, TILE, true, true>, &k_loss_dw<D, TILE>>(a, (uint32_t)((a.width + TILE - 1) / TILE * ((a.vocab + TILE - 1) / TILE)), st);
