@@ -577,7 +577,7 @@ int    lsp_rotary_backward(const lsp_rotary_problem* problem, const lsp_rotary_g
  *   width    a multiple of 8, at most 2^16;  rows at most LSP_MAX_ROWS;  vocab at most 2^20;  0 <= smoothing < 1;  0 <= z_loss <= 1
  * lsp_cross_entropy_backward gives losses and logs too (it needs no forward call before it), and the gradients of
  *   scale * sum over the rows of weights * losses
- * with respect to H (dH, rows that do not count: zeros) and W (dW), overwritten; either may be NULL.  weights: device, [rows] fp32, or NULL: ones (of rows that
+ * with respect to H (dH, rows that do not count: zeros) and W (dW), overwritten; either may be NULL.  What is written overlaps nothing else.  weights: device, [rows] fp32, or NULL: ones (of rows that
  * do not count not used); scale is finite.
  * The products run on the matrix cores in `dtype` with fp32 accumulation (fp32: in fp32).  Rows are taken in blocks; for a block the
  * exponentials are kept in `dtype`, each relative to the largest of its row in a piece of the vocabulary, and become the gradient of z in place: two roundings
@@ -621,7 +621,7 @@ int    lsp_cross_entropy_backward(const lsp_cross_entropy_problem* problem, cons
  * that is not 0 never becomes 0 (but below 2^-149 of the largest), so that no small v makes a large step); a scale is the block's largest magnitude over 448 or 1.875.  State that is all zeros,
  * codes and scales, is where training begins.  A gradient that is not finite spoils its element and, in 8 bits, can spoil its block's states.
  *   items       HOST array of `count` descriptors, 1 <= count <= LSP_MAX_TENSORS, read during the call only; no tensor twice, no overlaps
- *   step        number of this step, from 1 on (a captured call repeats it);  0 <= beta < 1, eps >= 0
+ *   step        number of this step, from 1 on (a captured call repeats it);  0 <= beta < 1, eps >= 0 (an element whose m and v are 0 gets no update but decay, whatever eps is)
  *   grad_scale  device, one fp32 (of clipping, or of a scaled loss), or NULL: 1.  Where it is not finite the step does nothing
  * At most 2^35 elements a call, all tensors padded to 4096. */
 typedef enum { LSP_STATE_F32 = 0, LSP_STATE_8BIT = 1 } lsp_state;

@@ -1,5 +1,7 @@
 // extern "C" entry points of what a training step needs around attention: rotary positions with norms of the heads, cross entropy, AdamW.  Argument checks, workspace carving,
 // launches.
+#include <cfloat>
+
 #include "adamw.h"
 #include "cross_entropy.h"
 #include "operator_checks.h"
@@ -225,7 +227,8 @@ int lsp_adamw(const lsp_adamw_item* items, int32_t count, lsp_state states, doub
     }
     lsp::AdamwGroup g{};
     const double c1 = 1.0 - std::pow(beta1, (double)step), root2 = std::sqrt(1.0 - std::pow(beta2, (double)step));
-    g.step = {(float)(1.0 - beta1), (float)beta1, (float)(1.0 - beta2), (float)beta2, (float)(eps * root2), (float)(rate * root2 / c1), (float)rate, 0.0f};
+    // (sqrt(v) is 0 or at least 2^-75: FLT_MIN beside it changes nothing, and makes 0 / 0 of an element without any gradients so far 0)
+    g.step = {(float)(1.0 - beta1), (float)beta1, (float)(1.0 - beta2), (float)beta2, std::max((float)(eps * root2), FLT_MIN), (float)(rate * root2 / c1), (float)rate, 0.0f};
     g.one_minus_beta1 = 1.0 - beta1; g.beta1 = beta1; g.one_minus_beta2 = 1.0 - beta2; g.beta2 = beta2;
     g.grad_scale = grad_scale;
     for (int32_t first = 0; first < count; first += lsp::kMaxItems) {

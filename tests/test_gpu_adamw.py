@@ -158,6 +158,24 @@ def test_tiny_blocks():
     step_and_check([d], "f32", "8bit", step=1)
 
 
+@pytest.mark.parametrize("states", ["f32", "8bit"])
+@pytest.mark.parametrize("eps", [0.0, 1e-46, 1e-8])
+def test_elements_without_gradients_only_decay(states, eps):
+    """m and v of 0: no update, also with an eps that is 0 in fp32."""
+    d, _ = tensor(900, "f32", "f32", states, False, seed=8)
+    for k in ("m", "v", "m_scale", "v_scale", "grad"):
+        if k in d:
+            d[k].zero_()
+    d["grad"][::3] = 1e-2
+    before = d["param"].clone()
+    L.lsp_adamw(L.adamw_items([d]), step=1, stream=torch.cuda.current_stream(), **dict(RATES, eps=eps))
+    without = torch.arange(900, device="cuda") % 3 != 0
+    want = f64(before) * (1 - RATES["rate"] * d["decay"])
+    assert np.all(np.abs(f64(d["param"]) - want)[without.cpu().numpy()] <= 3 * EPS * np.abs(want[without.cpu().numpy()]))
+    moved = f64(d["param"] - before)[::3]
+    assert np.all(np.abs(moved + RATES["rate"]) < 0.01 * RATES["rate"] + RATES["rate"] * d["decay"] * np.abs(f64(before)[::3]))
+
+
 @pytest.mark.parametrize("bad", [float("inf"), float("nan"), -float("inf")])
 def test_a_scale_that_is_not_finite_leaves_everything(bad):
     d, whole = tensor(3000, "bf16", "f32", "8bit", True, seed=4)
