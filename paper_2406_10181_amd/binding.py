@@ -704,10 +704,10 @@ STATE_KIND = {"f32": 0, "8bit": 1}
 
 
 class AdamwItems:
-    """HOST array of lsp_adamw_item (`array`) with what the call needs to know of all of them."""
+    """HOST array of lsp_adamw_item (`array`) with what the call needs to know of all of them: their states and their device."""
 
-    def __init__(self, array, states: str):
-        self.array, self.states = array, states
+    def __init__(self, array, states: str, device=None):
+        self.array, self.states, self.device = array, states, device
 
 
 def adamw_items(tensors) -> AdamwItems:
@@ -717,13 +717,14 @@ def adamw_items(tensors) -> AdamwItems:
     tensors = list(tensors)
     array = (lsp_adamw_item * len(tensors))()
     states = (_operators or _operator_calls()).adamw_items(ctypes.addressof(array), tensors)
-    return AdamwItems(array, "8bit" if states else "f32")
+    return AdamwItems(array, "8bit" if states else "f32", tensors[0]["param"].device)
 
 
 def lsp_adamw(items: AdamwItems, *, rate: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step: int, grad_scale=None, stream=None, check: bool = True) -> int:
-    """items: from adamw_items(); step counts from 1; grad_scale: one float32 on the device, or None."""
-    if grad_scale is not None and hasattr(grad_scale, "numel") and (grad_scale.numel() != 1 or grad_scale.element_size() != 4 or not grad_scale.is_floating_point()):
-        raise ValueError("lsp_adamw: grad_scale is one float32")
+    """items: from adamw_items(); step counts from 1; grad_scale: one float32 on the tensors' device, or None."""
+    if grad_scale is not None and hasattr(grad_scale, "numel") and \
+            (grad_scale.numel() != 1 or grad_scale.element_size() != 4 or not grad_scale.is_floating_point() or items.device not in (None, grad_scale.device)):
+        raise ValueError("lsp_adamw: grad_scale is one float32 on the tensors' device")
     rc = lib().lsp_adamw(items.array, len(items.array), STATE_KIND[items.states], rate, beta1, beta2, eps, step, _ptr(grad_scale), _stream(stream))
     if check and rc:
         _check(rc, "lsp_adamw")

@@ -465,7 +465,7 @@ PyObject* rotary_problem(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     void* n[3];
     const int64_t tokens[2] = {q.shape[0], q.shape[1]};
     for (int i = 0; i < 3; ++i) if (!whole_numbers(args[12 + i], i == 0 ? 2 : 1, tokens, g_int32, n[i], what)) return nullptr;
-    PyObject* const elsewhere[5] = {args[1], args[11], args[12], args[13], args[14]};       // (what a program may well have on the host)
+    PyObject* const elsewhere[5] = {args[1], args[11], args[12], args[13], args[14]};       // (of so many, those that a program may well have on the host)
     if (!on_one_device(elsewhere, 5, what)) return nullptr;
     Args tail(args + 15);
     const int32_t neighbours = PyObject_IsTrue(*tail.a++), norm = tail.int32();
@@ -528,8 +528,7 @@ PyObject* cross_entropy_problem(PyObject*, PyObject* const* args, Py_ssize_t nar
     float *losses, *logs;
     if (args[3] == Py_None || args[4] == Py_None) return refuse("cross_entropy_problem: targets and losses are wanted");
     if (!whole_numbers(args[3], 1, h.shape, g_int64, targets, what) || !floats(args[4], h.shape[0], losses, what) || !floats(args[5], h.shape[0], logs, what)) return nullptr;
-    PyObject* const elsewhere[2] = {args[1], args[3]};                                     // (what a program may well have on the host)
-    if (!on_one_device(elsewhere, 2, what)) return nullptr;
+    if (!on_one_device(args + 1, 5, what)) return nullptr;
     bool ok = true;
     const float smoothing = number(args[6], ok), z_loss = number(args[7], ok);
     if (!ok) return nullptr;
@@ -553,7 +552,7 @@ PyObject* cross_entropy_gradients(PyObject*, PyObject* const* args, Py_ssize_t n
     float* weights;
     Tensor n;
     if (args[3] != Py_None && !n.read(args[3], 1, what)) return nullptr;
-    if (!floats(args[3], -1, weights, what)) return nullptr;
+    if (!floats(args[3], -1, weights, what) || !on_one_device(args + 1, 3, what)) return nullptr;
     bool ok = true;
     const float scale = number(args[4], ok);
     if (!ok) return nullptr;

@@ -106,6 +106,48 @@ def test_the_tiles_of_large_problems(dtype):
     c.check()
 
 
+@pytest.mark.parametrize("rows,width,vocab,left_out", [(2900, 1032, 12100, 0.2)])
+def test_more_tiles_than_compute_units(rows, width, vocab, left_out):
+    """Over 256 tiles of 256 x 256, several of every panel ragged."""
+    c = Case("bf16", rows, width, vocab, left_out=left_out, seed=12)
+    c.backward()
+    c.check()
+
+
+@pytest.mark.parametrize("smoothing,z_loss", [(0.0, 0.0), (0.1, 1e-2)])
+def test_gradients_by_differences(smoothing, z_loss):
+    """Along directions of H and of W: (f(x + h e) - f(x - h e)) / 2h against the gradient, f = sum of weights * losses of the forward call in fp32."""
+    c = Case("f32", 40, 24, 90, smoothing=smoothing, z_loss=z_loss, seed=13)
+    h = 2.0 ** -7
+    for k in ("H", "W"):
+        x = getattr(c, k)
+        x.copy_((x * 1024).round() / 1024)                                   # (steps of 2^-7 are exact)
+    c.backward()
+    g = f64(c.weights)
+    for k in ("H", "W"):
+        x, got = getattr(c, k), f64(getattr(c, "d" + k))
+        for e in (torch.randint(0, 2, x.shape, generator=torch.Generator().manual_seed(14)).float().cuda() * 2 - 1, torch.sign(getattr(c, "d" + k))):
+            along = f64(e) @ f64(c.W).T if k == "H" else f64(c.H) @ f64(e).T # z's derivative
+            kept, f, off = x.clone(), [], 0.0
+            for sign in (1, -1):
+                x.copy_(kept + sign * h * e)
+                c.forward()
+                f.append(float((f64(c.losses) * g).sum()))
+                _, bound = ref.cross_entropy(f64(c.H), f64(c.W), c.targets.cpu().numpy(), smoothing=smoothing, z_loss=z_loss)["losses"]
+                off += float((bound * np.abs(g)).sum()) / (2 * h)
+            x.copy_(kept)
+            # What the third derivative leaves: h^2 / 6 of it.  L's is the third central moment of z' under the probabilities, at most R^3 / (6 sqrt 3) for z' within a range R; its second is
+            # at most R^2 / 4 and its first A = max |z'|, so that of z_loss L^2 is at most 2 z_loss (3 A R^2 / 4 + (|L| + 2 h A) R^3 / (6 sqrt 3)).
+            R, A = np.ptp(along, axis=1), np.abs(along).max(1)
+            third = R ** 3 / (6 * 3 ** 0.5)
+            third = third + 2 * z_loss * (0.75 * A * R ** 2 + (np.abs(f64(c.logs)) + 2 * h * A) * third)
+            right = float((got * f64(e)).sum())
+            # (and the gradient's own bound)
+            want = ref.cross_entropy(f64(c.H), f64(c.W), c.targets.cpu().numpy(), smoothing=smoothing, z_loss=z_loss, weights=g)["d" + k][1]
+            allowed = off + h * h / 6 * float((np.abs(g) * third).sum()) + float((want * np.abs(f64(e))).sum())
+            assert abs((f[0] - f[1]) / (2 * h) - right) <= allowed, (k, f, right, allowed)
+
+
 def test_rows_that_do_not_count_are_not_read():
     c = Case("bf16", 90, 64, 500, seed=2)
     c.targets[::3] = torch.tensor([-1, 500, -2 ** 63, 2 ** 62, 2 ** 32], device="cuda").repeat(6)

@@ -235,3 +235,5 @@ def test_adamw_tensors_that_belong_together():
         L.lsp_adamw(i, rate=1e-3, step=1, grad_scale=torch.zeros(2), check=False)
     with pytest.raises(ValueError):
         L.lsp_adamw(i, rate=1e-3, step=1, grad_scale=torch.zeros(1, dtype=F64), check=False)
+    with pytest.raises(ValueError):
+        L.lsp_adamw(i, rate=1e-3, step=1, grad_scale=torch.zeros(1, device="meta"), check=False)
