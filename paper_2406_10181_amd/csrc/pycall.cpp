@@ -42,6 +42,7 @@ PyObject* g_get_device;
 PyObject* g_numel;
 PyObject* g_is_contiguous;
 PyObject* g_element_size;
+PyObject* g_item_names[9];
 PyObject* g_types[3];         // torch's types, in the order of lsp_dtype; from the first descriptor on
 PyObject* g_int32;
 PyObject* g_int64;
@@ -603,7 +604,6 @@ PyObject* fill_adamw_items(PyObject* const* args, Py_ssize_t nargs) {
     auto* to = static_cast<lsp_adamw_item*>(head.pointer());
     if (!head.ok || !know_types()) return nullptr;
     if (!PyList_Check(args[1]) || PyList_GET_SIZE(args[1]) == 0) return refuse("adamw_items: tensors are wanted");
-    const char* names[9] = {"param", "grad", "m", "v", "m_scale", "v_scale", "master", "rate_factor", "decay"};
     struct Range { uintptr_t begin, end; bool written; };
     std::vector<Range> ranges;
     int states = -1;
@@ -613,7 +613,7 @@ PyObject* fill_adamw_items(PyObject* const* args, Py_ssize_t nargs) {
         if (!PyDict_Check(d)) return refuse("adamw_items: a dict for each tensor is wanted");
         PyObject* x[9];
         Py_ssize_t known = 0;
-        for (int k = 0; k < 9; ++k) { x[k] = PyDict_GetItemString(d, names[k]); known += x[k] != nullptr; }
+        for (int k = 0; k < 9; ++k) { x[k] = PyDict_GetItem(d, g_item_names[k]); known += x[k] != nullptr; }
         if (known != PyDict_GET_SIZE(d)) return refuse("adamw_items: unknown names");
         Flat f[7];
         for (int k = 0; k < 7; ++k) if (!f[k].read(x[k])) return nullptr;
@@ -813,6 +813,8 @@ PyMODINIT_FUNC PyInit__call(void) {
     g_numel = PyUnicode_InternFromString("numel");
     g_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     g_element_size = PyUnicode_InternFromString("element_size");
+    const char* const names[9] = {"param", "grad", "m", "v", "m_scale", "v_scale", "master", "rate_factor", "decay"};
+    for (int k = 0; k < 9; ++k) g_item_names[k] = PyUnicode_InternFromString(names[k]);
     PyObject* ctypes = PyImport_ImportModule("ctypes");
     if (!ctypes) return nullptr;
     g_argument_error = PyObject_GetAttrString(ctypes, "ArgumentError");
