@@ -1,13 +1,14 @@
 // Arguments of the cross-entropy kernels.  Those with products in them are in cross_entropy_products.h, the others in cross_entropy.hip.
 //
-// A block of rows goes through six kernels.  k_loss_pack copies the rows of H that count, one behind the other, so that rows that do not count cost nothing and are not
+// A block of rows goes through five kernels.  k_loss_pack copies the rows of H that count, one behind the other, so that rows that do not count cost nothing and are not
 // read.  k_loss_logits multiplies W by them; z[v][row] is in registers with the row across lanes and a piece of the vocabulary (a wave's part of the tile)
 // in the lane's registers, so that a piece's maximum and sum of exponentials take no LDS.  The exponentials, relative to the piece's maximum, are stored in the storage type: whatever
 // the size of z they keep its digits, where z itself in 16 bits would be off by a hundredth of a unit and p by a percent.  k_loss_rows makes the rows' L and losses of
-// the pieces; k_loss_dz turns the exponentials into the gradient of z in place; k_loss_dh and k_loss_dw multiply that by W and by H.
+// the pieces (k_loss_dz, where they are few); k_loss_dz turns the exponentials into the gradient of z in place; k_loss_back multiplies that by W and by H.
 //
 // 6 rows width vocab operations in all: keeping 16 bits an exponential, 2 bytes written, read, written and read twice, costs less than a second product
-// would.  The blocks are as large as kLossBytes allows, and where there are several, dW is added up in fp32.
+// would.  4096 rows, width 4096, 32000 words in bf16: logits 0.79-0.85 ms, dz 0.08 (6.5 TB/s), both gradients 1.55-1.65 ms, 2.48 ms in all, 1300 TFLOP/s, which is what the power allows of
+// products of random numbers: large plain products reach 1320 to 1580 with W's or H's rows along k, and 1100 to 1390 where an operand lies across.  The blocks are as large as kLossBytes allows, and where there are several, dW is added up in fp32.
 #pragma once
 
 #include "attention.h"
@@ -42,8 +43,10 @@ struct LossArgs {
     int32_t block_rows, padded;  // multiples of 256
     int32_t blocks, block;       // blocks of rows, and which this is
     int32_t pieces, piece;       // pieces of the vocabulary, of so many
-    int32_t tile[3];             // 256 (16 bits only), 128 or 64: of the logits, dH, dW
+    int32_t tile[2];             // 256 (16 bits only), 128 or 64: of the logits, and of dH and dW
     int32_t dh_splits, dh_room;  // parts of the vocabulary that dH is made of; tiles of rows times parts
+    int32_t dw_first;            // whether dW's workgroups come before dH's, and how many of the one come before the other
+    int32_t first_blocks;
     int32_t train;
 };
 
@@ -52,8 +55,7 @@ size_t loss_workspace(LossArgs& a, lsp_dtype dtype, uint8_t* base);     // the b
 hipError_t launch_loss(LossArgs& a, lsp_dtype dtype, hipStream_t st);
 
 template <typename D> hipError_t launch_loss_logits(const LossArgs& a, hipStream_t st);
-template <typename D> hipError_t launch_loss_dh(const LossArgs& a, hipStream_t st);
-template <typename D> hipError_t launch_loss_dw(const LossArgs& a, hipStream_t st);
+template <typename D> hipError_t launch_loss_back(const LossArgs& a, hipStream_t st);
 
 #if defined(__HIPCC__)
 constexpr float kLossLog2e = 1.44269504088896341f;
@@ -65,7 +67,7 @@ __device__ __forceinline__ int rows_of_block(const LossArgs& a) {
     return min(max(*as_const<int32_t>(a.count) - a.block * a.block_rows, 0), a.block_rows);
 }
 // Parts of the vocabulary that dH is made of, and the rows between two parts' sums: where fewer rows count than there are, their tiles get the workgroups (and the room) that the others would
-// have had.  (3001 rows of which 1800 count, width 1000, 50021 words, fp16: 183 us, with the parts planned for all rows 230.)
+// have had.  (3001 rows of which 1800 count, width 1000, 50021 words, fp16: dH in a launch of its own 183 us, with the parts planned for all rows 230.)
 struct LossParts { int splits, rows; };
 __device__ __forceinline__ LossParts parts_of_dh(const LossArgs& a, int rows) {
     const int tile = a.tile[1], tiles = (rows + tile - 1) / tile;

@@ -121,44 +121,62 @@ __global__ __launch_bounds__(256) void k_loss_pack_few(LossArgs a, int row_bytes
     for (int k = threadIdx.x; k < row_bytes / 16; k += 256) to[k] = from ? from[k] : u32x4{0, 0, 0, 0};
 }
 
-// L and the loss of a row from its pieces: 16 rows a workgroup, RUNS threads a row, each a running maximum and sum
+// What RUNS threads a row make of its pieces, each a running maximum and sum; 16 rows
+template <int RUNS> struct Runs {
+    float top[RUNS][17], sum[RUNS][17], plain[RUNS][17];
+    // r: the row's number of the 16
+    __device__ __forceinline__ void gather(const LossArgs& a, int run, int r, int row, bool there) {
+        float t = -INFINITY, s = 0.0f, x = 0.0f;
+        // (rows behind the last: the pieces are there, of packed zeros or of nothing yet, and nothing is made of them)
+        if (there) {
+#pragma unroll 4
+            for (int p = run; p < a.pieces; p += RUNS) {
+                const int64_t at = (int64_t)p * a.block_rows + row;
+                const float of_piece = a.top[at], sum_of_piece = a.sum[at], higher = fmaxf(t, of_piece), from = higher == -INFINITY ? 0.0f : higher;
+                s = s * __builtin_amdgcn_exp2f((t - from) * kLossLog2e) + sum_of_piece * __builtin_amdgcn_exp2f((of_piece - from) * kLossLog2e);
+                t = higher;
+                if (a.smoothing > 0.0f) x += a.plain[at];
+            }
+        }
+        top[run][r] = t; sum[run][r] = s; plain[run][r] = x;
+    }
+    // L, and the sum of z
+    __device__ __forceinline__ float join(int r, float& all) const {
+        float t = top[0][r], s = 0.0f;
+#pragma unroll 16
+        for (int k = 1; k < RUNS; ++k) t = fmaxf(t, top[k][r]);
+        const float from = t == -INFINITY ? 0.0f : t;
+        all = 0.0f;
+#pragma unroll 16
+        for (int k = 0; k < RUNS; ++k) {
+            s += sum[k][r] * __builtin_amdgcn_exp2f((top[k][r] - from) * kLossLog2e);
+            all += plain[k][r];
+        }
+        return t + logf(s);
+    }
+};
+__device__ __forceinline__ void store_loss(const LossArgs& a, int row, int64_t to, float L, float all) {
+    float loss = L - (1.0f - a.smoothing) * a.hit[row];
+    if (a.smoothing > 0.0f) loss -= a.smoothing * (all / (float)a.vocab);
+    if (a.z_loss > 0.0f) loss = fmaf(a.z_loss * L, L, loss);
+    a.losses[to] = loss;
+    if (a.logs) a.logs[to] = L;
+}
+
+// L and the losses: 16 rows a workgroup
 template <int RUNS>
 __global__ __launch_bounds__(16 * RUNS) void k_loss_rows(LossArgs a, int fp16) {
-    __shared__ float tops[RUNS][17], sums[RUNS][17], plains[RUNS][17];
+    __shared__ Runs<RUNS> runs;
     const int rows = rows_of_block(a), run = threadIdx.x >> 4, r = threadIdx.x & 15, row = blockIdx.x * 16 + r;
     if ((int)blockIdx.x * 16 >= rows) return;
-    float top = -INFINITY, sum = 0.0f, plain = 0.0f;
-    // (rows behind the last: the pieces are there, of packed zeros or of nothing yet, and nothing is made of them)
-    if (row < rows) {
-#pragma unroll 4
-        for (int p = run; p < a.pieces; p += RUNS) {
-            const int64_t at = (int64_t)p * a.block_rows + row;
-            const float t = a.top[at], s = a.sum[at], higher = fmaxf(top, t), from = higher == -INFINITY ? 0.0f : higher;
-            sum = sum * __builtin_amdgcn_exp2f((top - from) * kLossLog2e) + s * __builtin_amdgcn_exp2f((t - from) * kLossLog2e);
-            top = higher;
-            if (a.smoothing > 0.0f) plain += a.plain[at];
-        }
-    }
-    tops[run][r] = top; sums[run][r] = sum; plains[run][r] = plain;
+    runs.gather(a, run, r, row, row < rows);
     __syncthreads();
     float bound = 0.0f;
     if (run == 0 && row < rows) {
-#pragma unroll 16
-        for (int k = 1; k < RUNS; ++k) top = fmaxf(top, tops[k][r]);
-        const float from = top == -INFINITY ? 0.0f : top;
-        sum = plain = 0.0f;
-#pragma unroll 16
-        for (int k = 0; k < RUNS; ++k) {
-            sum += sums[k][r] * __builtin_amdgcn_exp2f((tops[k][r] - from) * kLossLog2e);
-            plain += plains[k][r];
-        }
-        const float L = top + logf(sum);
-        float loss = L - (1.0f - a.smoothing) * a.hit[row];
-        if (a.smoothing > 0.0f) loss -= a.smoothing * (plain / (float)a.vocab);
-        if (a.z_loss > 0.0f) loss = fmaf(a.z_loss * L, L, loss);
+        float all;
+        const float L = runs.join(r, all);
         const int64_t to = a.index[a.block * a.block_rows + row];
-        a.losses[to] = loss;
-        if (a.logs) a.logs[to] = L;
+        store_loss(a, row, to, L, all);
         if (a.train) {
             const float factor = a.weights ? a.scale * a.weights[to] : a.scale;
             a.log_sum[row] = L;
@@ -174,18 +192,36 @@ __global__ __launch_bounds__(16 * RUNS) void k_loss_rows(LossArgs a, int fp16) {
     if (r == 0) atomicMax(reinterpret_cast<unsigned*>(a.count) + 1, __float_as_uint(bound));
 }
 
+constexpr int kDzRuns = 16, kDzPieces = 4 * kDzRuns;                     // threads a row, and the most pieces that k_loss_dz makes L of
 constexpr int kDzColumns = 512;                                          // of a workgroup of k_loss_dz, in steps of 128
 
 // dz = (p (1 + 2 z_loss L) - smoothing / vocab - (1 - smoothing) [v = target]) factor in place of the exponentials: 16 rows a workgroup, so that the pieces' maxima come in
-// whole lines.  Two bytes read and two written an element: bound by memory.
-template <typename D>
+// whole lines.  Two bytes read and two written an element: bound by memory.  ROWS: the rows' L are made here too, by every workgroup of a row (and the losses by the first), which
+// saves a launch where the pieces are few (64 x 256 x 1000 in fp32, all of a call: 30.4 us, 32.1 with it); not in fp16, whose scale goes by all rows.
+template <typename D, bool ROWS>
 __global__ __launch_bounds__(256) void k_loss_dz(LossArgs a) {
     const int rows = rows_of_block(a), chunks = (a.padded + kDzColumns - 1) / kDzColumns;
     const int row = (int)(blockIdx.x / chunks) * 16 + (threadIdx.x >> 4), v0 = (int)(blockIdx.x % chunks) * kDzColumns + (threadIdx.x & 15) * 8;
-    if (row >= (rows + 63) / 64 * 64) return;
+    if (row >= (rows + 63) / 64 * 64) return;                              // (all sixteen rows are, or none)
     typename D::elem* const e = reinterpret_cast<typename D::elem*>(a.e) + (int64_t)row * a.padded;
     const bool there = row < rows;
-    const float L = there ? a.log_sum[row] : 0.0f, factor = there ? a.factor[row] * gradient_scale<D>(a) : 0.0f;
+    float L = 0.0f, factor = 0.0f;
+    if constexpr (ROWS) {
+        __shared__ Runs<kDzRuns> runs;
+        const int r = threadIdx.x & 15, of_r = row - (int)(threadIdx.x >> 4) + r;
+        runs.gather(a, threadIdx.x >> 4, r, of_r, of_r < rows);
+        __syncthreads();
+        if (there) {
+            float all;
+            L = runs.join(threadIdx.x >> 4, all);
+            const int64_t to = a.index[a.block * a.block_rows + row];
+            factor = a.weights ? a.scale * a.weights[to] : a.scale;
+            if (v0 == 0) store_loss(a, row, to, L, all);
+        }
+    } else if (there) {
+        L = a.log_sum[row];
+        factor = a.factor[row] * gradient_scale<D>(a);
+    }
     const float share = a.smoothing / (float)a.vocab, rise = fmaf(2.0f * a.z_loss, L, 1.0f);
     const int target = there ? a.target[row] : -1;
 #pragma unroll 4
@@ -234,23 +270,25 @@ static int64_t ceil_to(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 // one among many, and of as many as it holds; and what a round of them costs besides.  Measured in bf16 with tiles of 256, 128 and 64, logits: rows 1000, width 512, vocabulary 4000: 19, 12.5
 // and 12 us; 1000, 1024, 8000: 30, 25.5 and 32; 1000, 1024, 32000: 68, 92 and 121; 64, 1024, 32000: 31, 19 and 14.
 struct TileRate { int tile, at_once; double few, one, all, round; };
-constexpr TileRate kTileRates[3] = {{256, 1, 7.5e6, 4.8e6, 4.8e6, 5.0}, {128, 2, 3.3e6, 2.6e6, 3.6e6, 3.0}, {64, 4, 1.35e6, 1.0e6, 2.6e6, 2.0}};
-constexpr TileRate kTileRatesF32[2] = {{128, 2, 0.49e6, 0.49e6, 0.5e6, 3.0}, {64, 4, 0.39e6, 0.39e6, 0.52e6, 2.0}};   // (256: its fragments would not find room in the registers)
-static double products_us(int64_t m, int64_t n, int64_t length, const TileRate& r, int splits) {
-    const int64_t tiles = (m + r.tile - 1) / r.tile * ((n + r.tile - 1) / r.tile) * splits;
-    const int here = (int)std::min<int64_t>(r.at_once, (tiles + 255) / 256);
-    const double rate = tiles <= 128 ? r.few : std::min(here * r.one, r.all);
-    return (double)((tiles + 256 * here - 1) / (256 * here)) * (r.round + here * 2.0 * r.tile * r.tile * (double)((length + splits - 1) / splits) / rate);
+constexpr TileRate kTileRates[5] = {{256, 1, 7.5e6, 4.8e6, 4.8e6, 5.0}, {128, 2, 3.3e6, 2.6e6, 3.6e6, 3.0}, {64, 4, 1.35e6, 1.0e6, 2.6e6, 2.0},
+                                    {128, 2, 0.49e6, 0.49e6, 0.5e6, 3.0}, {64, 4, 0.39e6, 0.39e6, 0.52e6, 2.0}};   // the last two: fp32 (256: its fragments would not find room in the registers)
+static int64_t tiles_of(int64_t m, int64_t n, const TileRate& r) { return (m + r.tile - 1) / r.tile * ((n + r.tile - 1) / r.tile); }
+// `tiles`: of the whole launch
+static int at_once(int64_t tiles, const TileRate& r) { return (int)std::min<int64_t>(r.at_once, (tiles + 255) / 256); }
+static double tile_us(int64_t length, int64_t tiles, const TileRate& r) {
+    const int here = at_once(tiles, r);
+    return r.round + here * 2.0 * r.tile * r.tile * (double)length / (tiles <= 128 ? r.few : std::min(here * r.one, r.all));
 }
-// The tile and the number of parts of `length` (at most `most`) that take the least; parts' sums are written and read again, at 5 TB/s, by a launch more
-static void best_tile(int64_t m, int64_t n, int64_t length, bool fp32, int most, int32_t& tile, int32_t& splits) {
-    double least = 1e30;
-    const TileRate* const rates = fp32 ? kTileRatesF32 : kTileRates;
-    for (int k = 0; k < (fp32 ? 2 : 3); ++k)
-        for (int s = 1; s <= most; ++s) {
-            const double us = products_us(m, n, length, rates[k], s) + (s > 1 ? 4.0 + 1.6e-6 * (double)s * (double)(m * n) : 0.0);
-            if (us < least) { least = us; tile = rates[k].tile; splits = s; }
-        }
+// n tiles that take `us` each, behind m that take `first_us`, each going where there is room first
+static double two_kinds_us(int64_t m, double first_us, int64_t n, double us, int slots) {
+    const int64_t whole = m / slots, late = m % slots;
+    const double early = (double)whole * first_us, then = late ? early + first_us : early, even = std::max(early, ((double)m * first_us + (double)n * us) / slots);
+    const auto done = [&](double t) { return (double)(slots - late) * std::floor((t - early) / us + 1e-6) + (double)late * std::max(std::floor((t - then) / us + 1e-6), 0.0); };
+    double best = 1e30;
+    for (const double from : {early, then})
+        for (double k = std::max(std::ceil((even - from) / us - 1e-6), 0.0);; ++k)
+            if (done(from + k * us) >= (double)n) { best = std::min(best, from + k * us); break; }
+    return std::max(best, then);
 }
 
 void plan_loss(LossArgs& a, lsp_dtype dtype) {
@@ -263,13 +301,26 @@ void plan_loss(LossArgs& a, lsp_dtype dtype) {
     a.block_rows = (int)ceil_to((a.rows + a.blocks - 1) / a.blocks, 256);
     a.blocks = (int)((a.rows + a.block_rows - 1) / a.block_rows);
     const int64_t rows = std::min<int64_t>(a.rows, a.block_rows);
-    int32_t whole;
-    best_tile(a.vocab, rows, a.width, fp32, 1, a.tile[0], whole);
+    double least[2] = {1e30, 1e30};
+    for (int k = fp32 ? 3 : 0; k < (fp32 ? 5 : 3); ++k) {
+        const TileRate& r = kTileRates[k];
+        const int64_t n = tiles_of(a.vocab, rows, r), in_round = 256 * at_once(n, r);
+        const double us = (double)((n + in_round - 1) / in_round) * tile_us(a.width, n, r);
+        if (us < least[0]) { least[0] = us; a.tile[0] = r.tile; }
+        // both gradients, the longer products first; parts' sums are written and read again, at 5 TB/s, by a launch more
+        const int64_t dh = tiles_of(a.width, rows, r), dw = tiles_of(a.width, a.vocab, r);
+        for (int s = 1; s <= 32 && (s == 1 || (a.vocab / s >= 128 && dh * s <= 1024)); ++s) {
+            const int64_t all = dh * s + dw;
+            const double dh_us = tile_us((a.vocab + s - 1) / s, all, r), dw_us = tile_us(rows, all, r);
+            const int slots = 256 * at_once(all, r);
+            const double back = (dw_us > dh_us ? two_kinds_us(dw, dw_us, dh * s, dh_us, slots) : two_kinds_us(dh * s, dh_us, dw, dw_us, slots)) +
+                                (s > 1 ? 4.0 + 1.6e-6 * (double)s * (double)(rows * a.width) : 0.0);
+            if (back < least[1]) { least[1] = back; a.tile[1] = r.tile; a.dh_splits = s; a.dw_first = dw_us > dh_us; }
+        }
+    }
     a.piece = a.tile[0] / 2;
     a.pieces = a.padded / a.piece;
-    best_tile(a.width, rows, a.vocab, fp32, 32, a.tile[1], a.dh_splits);
     a.dh_room = (int)((rows + a.tile[1] - 1) / a.tile[1]) * a.dh_splits;
-    best_tile(a.width, a.vocab, rows, fp32, 1, a.tile[2], whole);
 }
 
 size_t loss_workspace(LossArgs& a, lsp_dtype dtype, uint8_t* base) {
@@ -307,19 +358,21 @@ template <typename D> static hipError_t launch_blocks(LossArgs& a, lsp_dtype dty
     for (a.block = 0; a.block < a.blocks && e == hipSuccess; ++a.block) {
         if (!few) hipLaunchKernelGGL(k_loss_pack, dim3((unsigned)(a.block_rows + (a.block == 0 ? a.rows : 0))), dim3(256), 0, st, a, row_bytes, (int)D::size);
         if ((e = hipGetLastError()) != hipSuccess || (e = launch_loss_logits<D>(a, st)) != hipSuccess) break;
-        if (a.pieces > 64) hipLaunchKernelGGL(k_loss_rows<64>, dim3((unsigned)(a.block_rows / 16)), dim3(1024), 0, st, a, (int)std::is_same<D, F16>::value);
-        else hipLaunchKernelGGL(k_loss_rows<16>, dim3((unsigned)(a.block_rows / 16)), dim3(256), 0, st, a, (int)std::is_same<D, F16>::value);
+        const bool fp16 = std::is_same<D, F16>::value, together = a.train && !fp16 && a.pieces <= kDzPieces;
+        if (a.pieces > kDzPieces) hipLaunchKernelGGL(k_loss_rows<64>, dim3((unsigned)(a.block_rows / 16)), dim3(1024), 0, st, a, (int)fp16);
+        else if (!together) hipLaunchKernelGGL(k_loss_rows<kDzRuns>, dim3((unsigned)(a.block_rows / 16)), dim3(16 * kDzRuns), 0, st, a, (int)fp16);
         if ((e = hipGetLastError()) != hipSuccess || !a.train) continue;
-        hipLaunchKernelGGL(k_loss_dz<D>, dim3((unsigned)(a.block_rows / 16 * ((a.padded + kDzColumns - 1) / kDzColumns))), dim3(256), 0, st, a);
-        if ((e = hipGetLastError()) != hipSuccess) break;
-        if (a.dH) {
-            if ((e = launch_loss_dh<D>(a, st)) != hipSuccess) break;
-            if (a.dh_splits > 1) {
-                hipLaunchKernelGGL(k_loss_dh_sum<D>, dim3((unsigned)(((int64_t)a.block_rows * (a.width / 4) + 255) / 256)), dim3(256), 0, st, a);
-                if ((e = hipGetLastError()) != hipSuccess) break;
-            }
+        const dim3 dz((unsigned)(a.block_rows / 16 * ((a.padded + kDzColumns - 1) / kDzColumns)));
+        if constexpr (!std::is_same<D, F16>::value) {
+            if (together) hipLaunchKernelGGL((k_loss_dz<D, true>), dz, dim3(256), 0, st, a);
         }
-        if (a.dW) e = launch_loss_dw<D>(a, st);
+        if (!together) hipLaunchKernelGGL((k_loss_dz<D, false>), dz, dim3(256), 0, st, a);
+        if ((e = hipGetLastError()) != hipSuccess) break;
+        if ((e = launch_loss_back<D>(a, st)) != hipSuccess) break;
+        if (a.dH && a.dh_splits > 1) {
+            hipLaunchKernelGGL(k_loss_dh_sum<D>, dim3((unsigned)(((int64_t)a.block_rows * (a.width / 4) + 255) / 256)), dim3(256), 0, st, a);
+            e = hipGetLastError();
+        }
     }
     return e;
 }

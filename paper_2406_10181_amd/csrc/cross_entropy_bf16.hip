@@ -3,6 +3,5 @@
 
 namespace lsp {
 template hipError_t launch_loss_logits<BF16>(const LossArgs& a, hipStream_t st);
-template hipError_t launch_loss_dh<BF16>(const LossArgs& a, hipStream_t st);
-template hipError_t launch_loss_dw<BF16>(const LossArgs& a, hipStream_t st);
+template hipError_t launch_loss_back<BF16>(const LossArgs& a, hipStream_t st);
 }  // namespace lsp

@@ -3,6 +3,5 @@
 
 namespace lsp {
 template hipError_t launch_loss_logits<F32>(const LossArgs& a, hipStream_t st);
-template hipError_t launch_loss_dh<F32>(const LossArgs& a, hipStream_t st);
-template hipError_t launch_loss_dw<F32>(const LossArgs& a, hipStream_t st);
+template hipError_t launch_loss_back<F32>(const LossArgs& a, hipStream_t st);
 }  // namespace lsp
