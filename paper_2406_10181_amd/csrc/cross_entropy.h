@@ -8,7 +8,8 @@
 //
 // 6 rows width vocab operations in all: keeping 16 bits an exponential, 2 bytes written, read, written and read twice, costs less than a second product
 // would.  4096 rows, width 4096, 32000 words in bf16: logits 0.79-0.85 ms, dz 0.08 (6.5 TB/s), both gradients 1.55-1.65 ms, 2.48 ms in all, 1300 TFLOP/s, which is what the power allows of
-// products of random numbers: large plain products reach 1320 to 1580 with W's or H's rows along k, and 1100 to 1390 where an operand lies across.  The blocks are as large as kLossBytes allows, and where there are several, dW is added up in fp32.
+// products of random numbers: large plain products reach 1320 to 1580 with W's or H's rows along k, and 1100 to 1390 where an operand lies across.
+// The blocks are as large as kLossBytes allows, and where there are several, dW is added up in fp32.
 #pragma once
 
 #include "attention.h"
@@ -43,7 +44,7 @@ struct LossArgs {
     int32_t block_rows, padded;  // multiples of 256
     int32_t blocks, block;       // blocks of rows, and which this is
     int32_t pieces, piece;       // pieces of the vocabulary, of so many
-    int32_t tile[2];             // 256 (16 bits only), 128 or 64: of the logits, and of dH and dW
+    int32_t tile[2];             // 256 (16 bits only), 128, 64 or 32: of the logits, and of dH and dW
     int32_t dh_splits, dh_room;  // parts of the vocabulary that dH is made of; tiles of rows times parts
     int32_t dw_first;            // whether dW's workgroups come before dH's, and how many of the one come before the other
     int32_t first_blocks;

@@ -266,28 +266,39 @@ __global__ __launch_bounds__(256) void k_loss_dh_sum(LossArgs a) {
 // ------------------------------------------------------------------ plan
 static int64_t ceil_to(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// The time of tiles of m x n products over `length`, in us, by a rough account: operations a us of a CU whose workgroups are few in all (fewer than half the CUs: clocks are higher then), of
-// one among many, and of as many as it holds; and what a round of them costs besides.  Measured in bf16 with tiles of 256, 128 and 64, logits: rows 1000, width 512, vocabulary 4000: 19, 12.5
-// and 12 us; 1000, 1024, 8000: 30, 25.5 and 32; 1000, 1024, 32000: 68, 92 and 121; 64, 1024, 32000: 31, 19 and 14.
+// The time of tiles of products over `length`, in us, by a rough account: operations a us of a CU whose workgroups are few in all (fewer than half the CUs: clocks are higher then), of
+// one among many, and of as many as it holds; and what a round of them costs besides.  Measured with tiles of 256, 128, 64 and 32: logits of 1000 rows, width 1024, 8000 words in bf16 30, 27, 32 and 83 us;
+// 64 x 1024 x 8000 26, 16, 8.4 and 7.2; 64 x 4096 x 1000 72, 45, 22 and 9.7, in fp32 (128 and less) 274, 80 and 27.  Of 80 calls of random sizes from 16 x 64 x 500 on, what it takes is 1 % behind
+// the best tile of the logits on average, and 3 % behind the best tile and parts of the gradients.
 struct TileRate { int tile, at_once; double few, one, all, round; };
-constexpr TileRate kTileRates[5] = {{256, 1, 7.5e6, 4.8e6, 4.8e6, 5.0}, {128, 2, 3.3e6, 2.6e6, 3.6e6, 3.0}, {64, 4, 1.35e6, 1.0e6, 2.6e6, 2.0},
-                                    {128, 2, 0.49e6, 0.49e6, 0.5e6, 3.0}, {64, 4, 0.39e6, 0.39e6, 0.52e6, 2.0}};   // the last two: fp32 (256: its fragments would not find room in the registers)
+constexpr TileRate kTileRates[7] = {{256, 1, 7.5e6, 4.8e6, 4.8e6, 5.0}, {128, 2, 3.3e6, 2.6e6, 3.6e6, 3.0}, {64, 4, 1.35e6, 1.0e6, 2.6e6, 2.0}, {32, 2, 1.4e6, 0.8e6, 1.1e6, 3.0},
+                                    {128, 2, 0.49e6, 0.49e6, 0.5e6, 3.0}, {64, 4, 0.39e6, 0.39e6, 0.52e6, 2.0}, {32, 2, 0.33e6, 0.33e6, 0.38e6, 3.0}};   // the last three: fp32
 static int64_t tiles_of(int64_t m, int64_t n, const TileRate& r) { return (m + r.tile - 1) / r.tile * ((n + r.tile - 1) / r.tile); }
-// `tiles`: of the whole launch
+// One of `tiles` in a launch, and all of them
 static int at_once(int64_t tiles, const TileRate& r) { return (int)std::min<int64_t>(r.at_once, (tiles + 255) / 256); }
-static double tile_us(int64_t length, int64_t tiles, const TileRate& r) {
+static double tile_us(int64_t tiles, int64_t length, const TileRate& r) {
     const int here = at_once(tiles, r);
     return r.round + here * 2.0 * r.tile * r.tile * (double)length / (tiles <= 128 ? r.few : std::min(here * r.one, r.all));
 }
-// n tiles that take `us` each, behind m that take `first_us`, each going where there is room first
-static double two_kinds_us(int64_t m, double first_us, int64_t n, double us, int slots) {
+static double tiles_us(int64_t tiles, int64_t length, const TileRate& r) {
+    const int in_round = 256 * at_once(tiles, r);
+    return (double)((tiles + in_round - 1) / in_round) * tile_us(tiles, length, r);
+}
+// Tiles of two kinds in a launch, m longer ones first, each going where there is room
+static double two_kinds_us(int64_t m, int64_t m_length, int64_t n, int64_t n_length, const TileRate& r) {
+    const double x = tile_us(m + n, m_length, r), y = tile_us(m + n, n_length, r);
+    const int slots = 256 * at_once(m + n, r);
+    if (m < slots) {                                                     // the others run beside them, and what is left of the longer ones then has the CUs to itself
+        const double with = (double)((n + slots - m - 1) / (slots - m)) * y, alone = m > 256 ? tile_us(m, m_length, r) : r.round + 2.0 * r.tile * r.tile * (double)m_length / r.one;
+        if (with < x) return with + (1.0 - with / x) * alone;
+    }
     const int64_t whole = m / slots, late = m % slots;
-    const double early = (double)whole * first_us, then = late ? early + first_us : early, even = std::max(early, ((double)m * first_us + (double)n * us) / slots);
-    const auto done = [&](double t) { return (double)(slots - late) * std::floor((t - early) / us + 1e-6) + (double)late * std::max(std::floor((t - then) / us + 1e-6), 0.0); };
+    const double early = (double)whole * x, then = late ? early + x : early, even = std::max(early, ((double)m * x + (double)n * y) / slots);
+    const auto done = [&](double t) { return (double)(slots - late) * std::floor((t - early) / y + 1e-6) + (double)late * std::max(std::floor((t - then) / y + 1e-6), 0.0); };
     double best = 1e30;
     for (const double from : {early, then})
-        for (double k = std::max(std::ceil((even - from) / us - 1e-6), 0.0);; ++k)
-            if (done(from + k * us) >= (double)n) { best = std::min(best, from + k * us); break; }
+        for (double k = std::max(std::ceil((even - from) / y - 1e-6), 0.0);; ++k)
+            if (done(from + k * y) >= (double)n) { best = std::min(best, from + k * y); break; }
     return std::max(best, then);
 }
 
@@ -302,23 +313,19 @@ void plan_loss(LossArgs& a, lsp_dtype dtype) {
     a.blocks = (int)((a.rows + a.block_rows - 1) / a.block_rows);
     const int64_t rows = std::min<int64_t>(a.rows, a.block_rows);
     double least[2] = {1e30, 1e30};
-    for (int k = fp32 ? 3 : 0; k < (fp32 ? 5 : 3); ++k) {
+    for (int k = fp32 ? 4 : 0; k < (fp32 ? 7 : 4); ++k) {
         const TileRate& r = kTileRates[k];
-        const int64_t n = tiles_of(a.vocab, rows, r), in_round = 256 * at_once(n, r);
-        const double us = (double)((n + in_round - 1) / in_round) * tile_us(a.width, n, r);
+        const double us = tiles_us(tiles_of(a.vocab, rows, r), a.width, r);
         if (us < least[0]) { least[0] = us; a.tile[0] = r.tile; }
-        // both gradients, the longer products first; parts' sums are written and read again, at 5 TB/s, by a launch more
+        // both gradients; parts' sums are written and read again, at 5 TB/s, by a launch more
         const int64_t dh = tiles_of(a.width, rows, r), dw = tiles_of(a.width, a.vocab, r);
         for (int s = 1; s <= 32 && (s == 1 || (a.vocab / s >= 128 && dh * s <= 1024)); ++s) {
-            const int64_t all = dh * s + dw;
-            const double dh_us = tile_us((a.vocab + s - 1) / s, all, r), dw_us = tile_us(rows, all, r);
-            const int slots = 256 * at_once(all, r);
-            const double back = (dw_us > dh_us ? two_kinds_us(dw, dw_us, dh * s, dh_us, slots) : two_kinds_us(dh * s, dh_us, dw, dw_us, slots)) +
-                                (s > 1 ? 4.0 + 1.6e-6 * (double)s * (double)(rows * a.width) : 0.0);
-            if (back < least[1]) { least[1] = back; a.tile[1] = r.tile; a.dh_splits = s; a.dw_first = dw_us > dh_us; }
+            const int64_t part = (a.vocab + s - 1) / s;
+            const double back = (rows > part ? two_kinds_us(dw, rows, dh * s, part, r) : two_kinds_us(dh * s, part, dw, rows, r)) + (s > 1 ? 4.0 + 1.6e-6 * (double)s * (double)(rows * a.width) : 0.0);
+            if (back < least[1]) { least[1] = back; a.tile[1] = r.tile; a.dh_splits = s; a.dw_first = rows > part; }
         }
     }
-    a.piece = a.tile[0] / 2;
+    a.piece = std::max(a.tile[0] / 2, 32);
     a.pieces = a.padded / a.piece;
     a.dh_room = (int)((rows + a.tile[1] - 1) / a.tile[1]) * a.dh_splits;
 }

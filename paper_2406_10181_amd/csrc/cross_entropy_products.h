@@ -7,12 +7,15 @@
 namespace lsp {
 
 #if defined(__HIPCC__)
+// 32 x 32: four groups of one wave each that share the length (64 tiles of length 4096 in bf16 9.7 us, of eight groups 8.8, but tiles that fill the CUs twice take 1.7 times as long
+// then; 16 tiles of 64 x 64 22 us, with two groups 15, with four 14).
 template <typename D, int TILE> struct LossTiles;
-template <typename D> struct LossTiles<D, 256> { static constexpr int M = 256, N = 256, WM = 2, WN = 4; };
-template <typename D> struct LossTiles<D, 128> { static constexpr int M = 128, N = 128, WM = 2, WN = 2; };
-template <typename D> struct LossTiles<D, 64> { static constexpr int M = 64, N = 64, WM = 2, WN = 2; };
+template <typename D> struct LossTiles<D, 256> { static constexpr int M = 256, N = 256, WM = 2, WN = 4, kGroups = 1; };
+template <typename D> struct LossTiles<D, 128> { static constexpr int M = 128, N = 128, WM = 2, WN = 2, kGroups = 1; };
+template <typename D> struct LossTiles<D, 64> { static constexpr int M = 64, N = 64, WM = 2, WN = 2, kGroups = 1; };
+template <typename D> struct LossTiles<D, 32> { static constexpr int M = 32, N = 32, WM = 1, WN = 1, kGroups = 4; };
 template <typename D, int TILE, bool A_ACROSS, bool B_ACROSS>
-using LossProduct = Product<D, LossTiles<D, TILE>::M, LossTiles<D, TILE>::N, LossTiles<D, TILE>::WM, LossTiles<D, TILE>::WN, A_ACROSS, B_ACROSS>;
+using LossProduct = Product<D, LossTiles<D, TILE>::M, LossTiles<D, TILE>::N, LossTiles<D, TILE>::WM, LossTiles<D, TILE>::WN, A_ACROSS, B_ACROSS, LossTiles<D, TILE>::kGroups>;
 
 // z[v][row] = W[v] . H[row]
 template <typename D, int TILE>
@@ -28,7 +31,7 @@ __global__ __launch_bounds__((LossProduct<D, TILE, false, false>::kThreads)) voi
     const int v0 = tm * P::BM, r0 = tn * P::BN;
     const int64_t w_bytes = a.w_stride * D::size, h_bytes = (int64_t)a.width * D::size;
     P p;
-    p.run({static_cast<const uint8_t*>(a.W) + v0 * w_bytes, w_bytes}, {a.packed + r0 * h_bytes, h_bytes}, a.width, max(a.vocab - v0, 0), P::BN, lds);
+    if (!p.run({static_cast<const uint8_t*>(a.W) + v0 * w_bytes, w_bytes}, {a.packed + r0 * h_bytes, h_bytes}, a.width, max(a.vocab - v0, 0), P::BN, lds)) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM, g = lane >> 4;
     const int first = v0 + wm * P::kRange;                                                // of the wave's piece
     const int64_t piece = first / P::kRange;
@@ -99,7 +102,7 @@ template <typename D, int TILE> __device__ __forceinline__ void loss_dh(const Lo
     const int v0 = min((int)split * share * P::BK, a.vocab), v1 = min(v0 + share * P::BK, a.vocab);
     const int64_t w_bytes = a.w_stride * D::size, e_bytes = (int64_t)a.padded * D::size;
     P p;
-    p.run({static_cast<const uint8_t*>(a.W) + v0 * w_bytes + (int64_t)d0 * D::size, w_bytes}, {a.e + r0 * e_bytes + (int64_t)v0 * D::size, e_bytes}, v1 - v0, a.width - d0, P::BN, lds);
+    if (!p.run({static_cast<const uint8_t*>(a.W) + v0 * w_bytes + (int64_t)d0 * D::size, w_bytes}, {a.e + r0 * e_bytes + (int64_t)v0 * D::size, e_bytes}, v1 - v0, a.width - d0, P::BN, lds)) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM;
     const int first = d0 + wm * P::kRange, left = a.width - first;
     const float factor = 1.0f / gradient_scale<D>(a);
@@ -131,7 +134,7 @@ template <typename D, int TILE> __device__ __forceinline__ void loss_dw(const Lo
     const int64_t h_bytes = (int64_t)a.width * D::size, e_bytes = (int64_t)a.padded * D::size;
     P p;
     // (up to whole steps: the rows behind those that count are zeros in both)
-    p.run({a.packed + (int64_t)d0 * D::size, h_bytes}, {a.e + (int64_t)v0 * D::size, e_bytes}, (rows + P::BK - 1) / P::BK * P::BK, a.width - d0, P::BN, lds);
+    if (!p.run({a.packed + (int64_t)d0 * D::size, h_bytes}, {a.e + (int64_t)v0 * D::size, e_bytes}, (rows + P::BK - 1) / P::BK * P::BK, a.width - d0, P::BN, lds)) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM;
     const int first = d0 + wm * P::kRange, left = a.width - first;
     const float factor = 1.0f / gradient_scale<D>(a);
@@ -192,13 +195,16 @@ template <typename D, int TILE> static inline hipError_t launch_back_of(LossArgs
     return launch_tiles<LossProduct<D, TILE, true, true>, &k_loss_back<D, TILE>>(a, (uint32_t)(dh + dw), st);
 }
 // (fp32: fragments of 256 x 256 tiles would not find room in the registers)
+template <typename D, typename Launch> static inline hipError_t with_tile(int tile, Launch&& launch) {
+    using std::integral_constant;
+    if constexpr (D::size == 2) if (tile == 256) return launch(integral_constant<int, 256>{});
+    return tile == 128 ? launch(integral_constant<int, 128>{}) : tile == 64 ? launch(integral_constant<int, 64>{}) : launch(integral_constant<int, 32>{});
+}
 template <typename D> hipError_t launch_loss_logits(const LossArgs& a, hipStream_t st) {
-    if constexpr (D::size == 2) if (a.tile[0] == 256) return launch_logits_of<D, 256>(a, st);
-    return a.tile[0] == 128 ? launch_logits_of<D, 128>(a, st) : launch_logits_of<D, 64>(a, st);
+    return with_tile<D>(a.tile[0], [&](auto tile) { return launch_logits_of<D, tile()>(a, st); });
 }
 template <typename D> hipError_t launch_loss_back(const LossArgs& a, hipStream_t st) {
-    if constexpr (D::size == 2) if (a.tile[1] == 256) return launch_back_of<D, 256>(a, st);
-    return a.tile[1] == 128 ? launch_back_of<D, 128>(a, st) : launch_back_of<D, 64>(a, st);
+    return with_tile<D>(a.tile[1], [&](auto tile) { return launch_back_of<D, tile()>(a, st); });
 }
 #endif
 

@@ -111,13 +111,17 @@ template <typename D, int N, int BK, int WAVES, bool ACROSS> struct OperandTile 
     }
 };
 
-template <typename D, int BM_, int BN_, int WM_, int WN_, bool A_ACROSS, bool B_ACROSS> struct Product {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = 128 / D::size, kWaves = WM * WN, kThreads = 64 * kWaves, MI = BM / WM / 16, NI = BN / WN / 16, kSteps = BK / 32;
+// GROUPS of waves, each with buffers of its own, take the stages of a tile by turns, and the first adds up what they have: for tiles that are few.  A stage of a wave with 2 x 2 small tiles is a chain of
+// two reads of LDS, two times four products and a barrier, 0.3 us whatever is on its way; deeper buffers do not shorten it.
+template <typename D, int BM_, int BN_, int WM_, int WN_, bool A_ACROSS, bool B_ACROSS, int GROUPS = 1> struct Product {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BK = 128 / D::size, kWaves = WM * WN, kThreads = 64 * kWaves * GROUPS, MI = BM / WM / 16, NI = BN / WN / 16, kSteps = BK / 32;
     static constexpr int kRange = 16 * MI;            // m of a wave
     using A = OperandTile<D, BM, BK, kWaves, A_ACROSS>;
     using B = OperandTile<D, BN, BK, kWaves, B_ACROSS>;
     // Three buffers for A and two for B: 160 KiB for 256 x 256 in 16 bits, all that a CU has
-    static constexpr uint32_t kBase = 3 * A::kBytes, kLds = kBase + 2 * B::kBytes;
+    static constexpr uint32_t kBase = 3 * A::kBytes, kOfGroup = kBase + 2 * B::kBytes, kLds = GROUPS * kOfGroup;
+    static constexpr uint32_t kStored = kWaves * 32 * kRange * 4, kParts = NI * MI * 1024;  // bytes that the first group stores results through, and of a wave's results
+    static_assert(GROUPS == 1 || kStored + (GROUPS - 1) * kWaves * kParts <= kLds, "room for the groups' results");
     static constexpr int kEarly = MI < 4 ? 1 : MI / 4;
     static_assert(NI % 2 == 0 && MI >= 2, "pairs of n blocks are stored, and a block of m is left when the others wait");
 
@@ -175,9 +179,12 @@ template <typename D, int BM_, int BN_, int WM_, int WN_, bool A_ACROSS, bool B_
             for (int j = 0; j < NI; ++j) y[0][j] = y[1][j];
         }
     }
-    // k from 0 to `length`; m_there, n_there: how many rows (columns) of the tile there are.  All waves are done with LDS when it returns.
-    __device__ __forceinline__ void run(const Operand& oa, const Operand& ob, int length, int m_there, int n_there, Lds lds) {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % WM, wn = wave / WM;
+    // k from 0 to `length`; m_there, n_there: how many rows (columns) of the tile there are.  All waves are done with LDS when it returns, and those of the first group have the results: false for others.
+    __device__ __forceinline__ bool run(const Operand& oa, const Operand& ob, int length, int m_there, int n_there, Lds lds) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % kWaves, group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / kWaves;
+        const int lane = threadIdx.x & 63, wm = wave % WM, wn = wave / WM;
+        const Lds whole_lds = lds;
+        lds += group * kOfGroup;
         A a;
         B b;
         a.setup(oa.row_bytes, m_there, wave, lane);
@@ -187,11 +194,11 @@ template <typename D, int BM_, int BN_, int WM_, int WN_, bool A_ACROSS, bool B_
 #pragma unroll
             for (int i = 0; i < MI; ++i) acc[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         const int64_t a_step = A_ACROSS ? oa.row_bytes * BK : BK * D::size, b_step = B_ACROSS ? ob.row_bytes * BK : BK * D::size;
-        const uint8_t* pa = oa.first;
-        const uint8_t* pb = ob.first;
-        int left_a = length, left_b = length;
-        const auto next_of_a = [&] { pa += a_step; left_a -= BK; };
-        const auto next_of_b = [&] { pb += b_step; left_b -= BK; };
+        const uint8_t* pa = oa.first + group * a_step;
+        const uint8_t* pb = ob.first + group * b_step;
+        int left_a = length - group * BK, left_b = left_a;
+        const auto next_of_a = [&] { pa += GROUPS * a_step; left_a -= GROUPS * BK; };
+        const auto next_of_b = [&] { pb += GROUPS * b_step; left_b -= GROUPS * BK; };
         // (behind the end too: what is loaded from nowhere is zeros, and the loads on their way are always as many)
         const auto fetch_a = [&](Lds into) {
 #pragma unroll
@@ -219,11 +226,29 @@ template <typename D, int BM_, int BN_, int WM_, int WN_, bool A_ACROSS, bool B_
             next_of_a(); next_of_b();
             at_a = next_a; at_b = next_b;
         };
-        const int stages = (length + BK - 1) / BK, whole = length / BK - 3;                // (what stage t asks for is of stages t + 2 and t + 3)
+        const int stages = (length + GROUPS * BK - 1) / (GROUPS * BK), whole = length / (GROUPS * BK) - 3;   // (what stage t asks for is of stages t + 2 and t + 3)
         int t = 0;
         for (; t < whole; ++t) one(std::false_type{});
         for (; t < stages; ++t) one(std::true_type{});
         arrived_for_all();
+        if constexpr (GROUPS > 1) {
+            const Lds parts = whole_lds + kStored + wave * kParts + lane * 16;
+            if (group) {
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+#pragma unroll
+                    for (int i = 0; i < MI; ++i) lds_write<f32x4>(parts + (group - 1) * (kWaves * kParts) + (j * MI + i) * 1024, acc[j][i]);
+            }
+            arrived_for_all();
+            if (group) return false;
+#pragma unroll
+            for (int g = 0; g < GROUPS - 1; ++g)
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+#pragma unroll
+                    for (int i = 0; i < MI; ++i) acc[j][i] += lds_read<f32x4>(parts + g * (kWaves * kParts) + (j * MI + i) * 1024);
+        }
+        return true;
     }
 };
 
