@@ -2,8 +2,8 @@
 //
 // Bound by memory: a bf16 element takes 22 bytes with states in fp32 (30 with an fp32 master) and 10 with states in 8 bits; nothing is read twice.  A thread
 // takes eight elements that follow one another, so that every stream goes in loads of 8 to 32 bytes a lane, and 32 lanes have the 256 elements of a scale:
-// its maximum goes through the 32 lanes without LDS.  A workgroup has 2048 elements of one tensor; the tensors' descriptors come with the launch (kMaxItems of
-// them), so that a model's many small tensors take few launches and no memory of their own.
+// its maximum goes through the 32 lanes without LDS.  A workgroup has 2048 elements of one tensor; the tensors' descriptors come with the launch (52 or
+// 64 of them), so that a model's many small tensors take few launches and no memory of their own.
 #include "adamw.h"
 #include "rows.h"
 
@@ -90,7 +90,7 @@ __device__ __forceinline__ u32x2 narrow_v(const EightWide& x, double inverse) {
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466e38f; }
 
 // m / (sqrt(v) + eps) with the bias corrections in the factors.  QUICK: by the vector unit's square root and reciprocal, each within an ulp; they take what is below 2^-126 for zero, so only
-// where eps is 2^-40 or more, which such a root (below 2^-63) does not change.  (bf16, states in 8 bits, 32000 x 4096: the quotients as IEEE has them, 70 us more of then 430.)
+// where eps is 2^-40 or more, which such a root (below 2^-63) does not change.  (bf16, states in 8 bits, 32000 x 4096: 250 us, with quotients as IEEE has them 293.)
 template <bool QUICK> __device__ __forceinline__ float updated(float p, float m, float v, const AdamwStep& s, float rate, float rate_decay) {
     p = fmaf(-rate_decay, p, p);
     if constexpr (QUICK) return fmaf(-rate * m, __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v) + s.eps), p);
@@ -183,7 +183,7 @@ template <typename P, typename G, bool MASTER, bool BITS8> struct Loaded {
 };
 
 // A workgroup's kAdamwRounds rounds of 2048 elements.  Whole ones are asked for together: more of the memory's latency is behind the arithmetic of others (states in 8 bits, 32000 x 4096
-// in bf16: 289 us, one by one 306).
+// in bf16: 250 us, one by one 269).
 template <typename P, typename G, bool MASTER, bool BITS8, bool QUICK> __device__ __forceinline__ void adamw_of(const AdamwWork& w, int elements) {
     constexpr int kRound = 8 * kAdamwThreads;
     using L = Loaded<P, G, MASTER, BITS8>;
@@ -218,19 +218,21 @@ template <typename P, bool BITS8, bool QUICK> __device__ __forceinline__ void ad
     else with(BF16{});
 }
 
+// 32000 x 4096 in bf16: states in fp32 528 us, 5.5 TB/s, with an fp32 master 684, 5.75 TB/s; states in 8 bits 250, 5.3 TB/s (moving the same five streams and doing nothing takes 238).
+// The tensor is found by a ballot: by a loop over their beginnings in scalar registers 273, for 200 tensors of 4096 elements 25 us instead of 16.
 template <bool BITS8, bool QUICK>
-__global__ __launch_bounds__(kAdamwThreads, 5) void k_adamw(AdamwGroup unused) {
-    const auto* g = group_args<AdamwGroup>();
+__global__ __launch_bounds__(kAdamwThreads, 5) void k_adamw(AdamwGroup<BITS8> unused) {
+    const auto* g = group_args<AdamwGroup<BITS8>>();
     const int block = (int)blockIdx.x;
-    int k = kMaxItems - 1;                                                                // (less one for every tensor that begins behind this workgroup: sums of signs, in scalar registers)
-#pragma unroll
-    for (int i = 1; i < kMaxItems; ++i) k += (block - g->first[i]) >> 31;
+    const int lane = threadIdx.x & 63, begin = g->first[min(lane, AdamwGroup<BITS8>::kItems - 1)];
+    const int k = __popcll(__ballot(lane < AdamwGroup<BITS8>::kItems && block >= begin)) - 1;              // (a lane has a tensor: how many begin at this workgroup or before)
     const auto& item = g->item[k];
     AdamwWork w;
     w.step = {g->step.one_minus_beta1, g->step.beta1, g->step.one_minus_beta2, g->step.beta2, g->step.eps, g->step.rate, g->step.decay_rate};
     w.grad_scale = g->grad_scale ? *as_const<float>(g->grad_scale) : 1.0f;
     const int64_t first = (int64_t)(block - g->first[k]) * kAdamwElements;
-    const int elements = (int)min(item.elements - first, (int64_t)kAdamwElements), size = item.dtype == LSP_F32 ? 4 : 2, grad_size = item.grad_dtype == LSP_F32 ? 4 : 2;
+    const int dtype = (int)(item.elements / kAdamwSizes) & 3, grad_dtype = (int)(item.elements / kAdamwSizes) >> 2;
+    const int elements = (int)min(item.elements % kAdamwSizes - first, (int64_t)kAdamwElements), size = dtype == LSP_F32 ? 4 : 2, grad_size = grad_dtype == LSP_F32 ? 4 : 2;
     w.param = global_pointer(static_cast<uint8_t*>(item.param) + first * size);
     w.grad = global_pointer(static_cast<const uint8_t*>(item.grad) + first * grad_size);
     w.m = global_pointer(static_cast<uint8_t*>(item.m) + first * (BITS8 ? 1 : 4));
@@ -243,18 +245,17 @@ __global__ __launch_bounds__(kAdamwThreads, 5) void k_adamw(AdamwGroup unused) {
     w.rate = w.step.rate * item.rate_factor; w.rate_decay = w.step.decay_rate * item.rate_factor * item.decay;
     w.beta1 = g->beta1; w.beta2 = g->beta2;
     w.m_of = g->one_minus_beta1 * (double)w.grad_scale; w.v_of = g->one_minus_beta2 * (double)w.grad_scale * (double)w.grad_scale;
-    if (item.dtype == LSP_F32) adamw_of_grad<F32, BITS8, QUICK>(w, elements, item.grad_dtype);
-    else if (item.dtype == LSP_F16) adamw_of_grad<F16, BITS8, QUICK>(w, elements, item.grad_dtype);
-    else adamw_of_grad<BF16, BITS8, QUICK>(w, elements, item.grad_dtype);
+    if (dtype == LSP_F32) adamw_of_grad<F32, BITS8, QUICK>(w, elements, grad_dtype);
+    else if (dtype == LSP_F16) adamw_of_grad<F16, BITS8, QUICK>(w, elements, grad_dtype);
+    else adamw_of_grad<BF16, BITS8, QUICK>(w, elements, grad_dtype);
 }
 
-hipError_t launch_adamw(const AdamwGroup& g, uint32_t blocks, bool bits8, hipStream_t st) {
-    const bool quick = g.step.eps >= 0x1p-40f;
-    if (bits8 && quick) hipLaunchKernelGGL((k_adamw<true, true>), dim3(blocks), dim3(kAdamwThreads), 0, st, g);
-    else if (bits8) hipLaunchKernelGGL((k_adamw<true, false>), dim3(blocks), dim3(kAdamwThreads), 0, st, g);
-    else if (quick) hipLaunchKernelGGL((k_adamw<false, true>), dim3(blocks), dim3(kAdamwThreads), 0, st, g);
-    else hipLaunchKernelGGL((k_adamw<false, false>), dim3(blocks), dim3(kAdamwThreads), 0, st, g);
+template <bool BITS8> hipError_t launch_adamw(const AdamwGroup<BITS8>& g, uint32_t blocks, hipStream_t st) {
+    if (g.step.eps >= 0x1p-40f) hipLaunchKernelGGL((k_adamw<BITS8, true>), dim3(blocks), dim3(kAdamwThreads), 0, st, g);
+    else hipLaunchKernelGGL((k_adamw<BITS8, false>), dim3(blocks), dim3(kAdamwThreads), 0, st, g);
     return hipGetLastError();
 }
+template hipError_t launch_adamw<false>(const AdamwGroup<false>& g, uint32_t blocks, hipStream_t st);
+template hipError_t launch_adamw<true>(const AdamwGroup<true>& g, uint32_t blocks, hipStream_t st);
 
 }  // namespace lsp

@@ -117,6 +117,33 @@ lsp::LossArgs loss_args(const lsp_cross_entropy_problem* p, bool train, lsp_dtyp
     return a;
 }
 
+template <bool BITS8> int adamw_launches(const lsp_adamw_item* items, int32_t count, double rate, double beta1, double beta2, double eps, int64_t step, const float* grad_scale, void* stream) {
+    using Group = lsp::AdamwGroup<BITS8>;
+    Group g{};
+    const double c1 = 1.0 - std::pow(beta1, (double)step), root2 = std::sqrt(1.0 - std::pow(beta2, (double)step));
+    // (sqrt(v) is 0 or at least 2^-75: FLT_MIN beside it changes nothing, and makes 0 / 0 of an element without any gradients so far 0)
+    g.step = {(float)(1.0 - beta1), (float)beta1, (float)(1.0 - beta2), (float)beta2, std::max((float)(eps * root2), FLT_MIN), (float)(rate * root2 / c1), (float)rate};
+    g.one_minus_beta1 = 1.0 - beta1; g.beta1 = beta1; g.one_minus_beta2 = 1.0 - beta2; g.beta2 = beta2;
+    g.grad_scale = grad_scale;
+    for (int32_t first = 0; first < count; first += Group::kItems) {
+        uint32_t total = 0;
+        for (int k = 0; k < Group::kItems; ++k) {
+            g.first[k] = first + k < count ? (int32_t)total : INT32_MAX;
+            if (first + k >= count) continue;
+            const lsp_adamw_item& i = items[first + k];
+            auto& to = g.item[k];
+            to.param = i.param; to.grad = i.grad; to.m = i.m; to.v = i.v; to.master = i.master;
+            to.elements = (i.dtype + 4 * i.grad_dtype) * lsp::kAdamwSizes + i.elements;
+            to.rate_factor = i.rate_factor; to.decay = i.decay;
+            if constexpr (BITS8) { to.m_scale = i.m_scale; to.v_scale = i.v_scale; }
+            total += (uint32_t)((i.elements + lsp::kAdamwElements - 1) / lsp::kAdamwElements);
+        }
+        const int rc = done(lsp::launch_adamw<BITS8>(g, total, static_cast<hipStream_t>(stream)));
+        if (rc != LSP_OK) return rc;
+    }
+    return LSP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -225,25 +252,7 @@ int lsp_adamw(const lsp_adamw_item* items, int32_t count, lsp_state states, doub
         blocks += (i.elements + lsp::kAdamwElements - 1) / lsp::kAdamwElements;
         if (blocks >= kMostLaunch) return LSP_ERR_SHAPE;
     }
-    lsp::AdamwGroup g{};
-    const double c1 = 1.0 - std::pow(beta1, (double)step), root2 = std::sqrt(1.0 - std::pow(beta2, (double)step));
-    // (sqrt(v) is 0 or at least 2^-75: FLT_MIN beside it changes nothing, and makes 0 / 0 of an element without any gradients so far 0)
-    g.step = {(float)(1.0 - beta1), (float)beta1, (float)(1.0 - beta2), (float)beta2, std::max((float)(eps * root2), FLT_MIN), (float)(rate * root2 / c1), (float)rate, 0.0f};
-    g.one_minus_beta1 = 1.0 - beta1; g.beta1 = beta1; g.one_minus_beta2 = 1.0 - beta2; g.beta2 = beta2;
-    g.grad_scale = grad_scale;
-    for (int32_t first = 0; first < count; first += lsp::kMaxItems) {
-        uint32_t total = 0;
-        for (int k = 0; k < lsp::kMaxItems; ++k) {
-            if (first + k < count) {
-                g.item[k] = items[first + k];
-                g.first[k] = (int32_t)total;
-                total += (uint32_t)((g.item[k].elements + lsp::kAdamwElements - 1) / lsp::kAdamwElements);
-            } else g.first[k] = INT32_MAX;
-        }
-        const int rc = done(lsp::launch_adamw(g, total, bits8, static_cast<hipStream_t>(stream)));
-        if (rc != LSP_OK) return rc;
-    }
-    return LSP_OK;
+    return bits8 ? adamw_launches<true>(items, count, rate, beta1, beta2, eps, step, grad_scale, stream) : adamw_launches<false>(items, count, rate, beta1, beta2, eps, step, grad_scale, stream);
 }
 
 }  // extern "C"
