@@ -68,14 +68,16 @@ __global__ __launch_bounds__((LossProduct<D, TILE, false, false>::kThreads)) voi
 #pragma unroll
             for (int x = 0; x < 4; ++x) top = fmaxf(top, p.acc[j][i][x]);
         top = quarters_max(top);
-        const float from = top == -INFINITY ? 0.0f : top;
+        // (the rounding of `from` is one factor for all of the piece, and of its sum: no further from 1 than a rounding of L is from L)
+        const float from = top == -INFINITY ? 0.0f : -top * kLossLog2e;
 #pragma unroll
         for (int i = 0; i < P::MI; ++i)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                p.acc[j][i][x] = __builtin_amdgcn_exp2f((p.acc[j][i][x] - from) * kLossLog2e);
-                sum += p.acc[j][i][x];
-            }
+            for (int x = 0; x < 4; ++x) p.acc[j][i][x] = __builtin_amdgcn_exp2f(fmaf(p.acc[j][i][x], kLossLog2e, from));
+#pragma unroll
+        for (int i = 0; i < P::MI; ++i)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) sum += p.acc[j][i][x];
         sum = quarters_sum(sum);
         if (g == 0) { a.top[piece * a.block_rows + row] = top; a.sum[piece * a.block_rows + row] = sum; }
     }

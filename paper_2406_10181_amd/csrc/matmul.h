@@ -10,6 +10,7 @@
 #pragma once
 
 #include "attention.h"
+#include "rows.h"
 
 namespace lsp {
 
@@ -266,8 +267,8 @@ template <typename D, int MI, typename Row> __device__ __forceinline__ void stor
             if constexpr (D::size == 4) lds_write<f32x4>(own + T::place(mine, 4 * i + g), f32x4{a, b, c, d});
             else {
                 u32x2 w;
-                w[0] = (uint32_t)narrow<D>(a) | (uint32_t)narrow<D>(b) << 16;
-                w[1] = (uint32_t)narrow<D>(c) | (uint32_t)narrow<D>(d) << 16;
+                w[0] = narrow_two<D>(a, b);
+                w[1] = narrow_two<D>(c, d);
                 lds_write<u32x2>(own + T::place(mine, 2 * i + (g >> 1)) + (g & 1) * 8u, w);
             }
         }

@@ -106,6 +106,16 @@ __device__ __forceinline__ float wave_sum(float x) {
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 
+// Two elements in a word, by one instruction (of two elements converted by themselves the compiler makes four)
+template <typename D> __device__ __forceinline__ uint32_t narrow_two(float a, float b) {
+    typedef float Two __attribute__((ext_vector_type(2)));
+    typedef std::conditional_t<std::is_same<D, BF16>::value, __bf16, _Float16> Half;
+    typedef Half Halves __attribute__((ext_vector_type(2)));
+    const Halves h = __builtin_convertvector((Two{a, b}), Halves);
+    uint32_t u;
+    __builtin_memcpy(&u, &h, 4);
+    return u;
+}
 template <typename D> __device__ __forceinline__ Packed<D> narrow_eight(const Eight& r) {
     Packed<D> o;
     if constexpr (D::size == 4) {
@@ -113,7 +123,7 @@ template <typename D> __device__ __forceinline__ Packed<D> narrow_eight(const Ei
         for (int e = 0; e < 8; ++e) o.w[e] = __float_as_uint(r.x[e]);
     } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o.w[k] = (uint32_t)narrow<D>(r.x[2 * k]) | (uint32_t)narrow<D>(r.x[2 * k + 1]) << 16;
+        for (int k = 0; k < 4; ++k) o.w[k] = narrow_two<D>(r.x[2 * k], r.x[2 * k + 1]);
     }
     return o;
 }
