@@ -7,7 +7,7 @@
 // the pieces (k_loss_dz, where they are few); k_loss_dz turns the exponentials into the gradient of z in place; k_loss_back multiplies that by W and by H.
 //
 // 6 rows width vocab operations in all: keeping 16 bits an exponential, 2 bytes written, read, written and read twice, costs less than a second product
-// would.  4096 rows, width 4096, 32000 words in bf16: logits 0.79-0.85 ms, dz 0.08 (6.5 TB/s), both gradients 1.55-1.65 ms, 2.48 ms in all, 1300 TFLOP/s, which is what the power allows of
+// would.  4096 rows, width 4096, 32000 words in bf16: logits 0.79-0.85 ms, dz 0.08 (6.5 TB/s), both gradients 1.55-1.65 ms, 2.44 ms in all, 1320 TFLOP/s, which is what the power allows of
 // products of random numbers: large plain products reach 1320 to 1580 with W's or H's rows along k, and 1100 to 1390 where an operand lies across.
 // The blocks are as large as kLossBytes allows, and where there are several, dW is added up in fp32.
 #pragma once

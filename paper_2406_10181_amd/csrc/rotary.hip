@@ -173,7 +173,7 @@ template <int NORM, int GROUP> __device__ __forceinline__ void norm_head(Eight& 
     }
 }
 
-// 4 x 1024 tokens of 32 + 32 heads of 128 in bf16, 134 MB: 24.8 us, 5.4 TB/s; 16384 tokens of 16 + 16 heads of 64 in fp32, 268 MB, 47.7 us, 5.6 TB/s.
+// 4 x 1024 tokens of 32 + 32 heads of 128 in bf16, 134 MB: 24.2 us, 5.5 TB/s; 16384 tokens of 16 + 16 heads of 64 in fp32, 268 MB, 47.6 us, 5.6 TB/s.
 template <typename D, int NORM, int GROUP, bool NEIGHBOURS>
 __global__ __launch_bounds__(kRotaryThreads) void k_rotary(RotaryArgs a) {
     constexpr int kHeads = 64 / GROUP, kWaves = kRotaryThreads / 64;     // heads that a wave has at a time
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(kRotaryThreads) void k_rotary(RotaryArgs a) {
 // With y = xhat w + b turned by the angle, and d the gradient of the result turned back:  dw += d xhat, db += d, and with e = d w
 //   dx = factor (e - xhat mean(e xhat) [- mean(e), for a norm with means]).
 // Five waves a SIMD in 16 bits, for which sums of biases are left out where nobody asks for them (BIAS): 3 x 777 padded tokens of 16 + 4 heads of 80 in fp16, with means and biases, 12.0 us, with four
-// waves 15.6; 4 x 1024 tokens of 32 + 32 heads of 128 in bf16, 39.7 us (5.1 TB/s), with four 42.1.
+// waves 15.6; 4 x 1024 tokens of 32 + 32 heads of 128 in bf16, 38.9 us (5.2 TB/s), with four 42.1.
 template <typename D, int NORM, int GROUP, bool NEIGHBOURS, bool BIAS>
 __global__ __launch_bounds__(kRotaryThreads, D::size == 4 ? 4 : 5) void k_rotary_back(RotaryArgs a) {
     constexpr int kHeads = 64 / GROUP, kWaves = kRotaryThreads / 64, kGroups = kRotaryThreads / GROUP;
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(kRotaryThreads, D::size == 4 ? 4 : 5) void k_rotary
     }
 }
 
-// The workgroups' parts of a sum, added in their order: 16 columns of one sum a workgroup, 64 runs of parts side by side
+// The workgroups' parts of a sum, added in their order: 16 columns of one sum a workgroup, 64 runs of parts side by side.  (640 parts of 128 columns: 4.5 us, a launch and two reads.)
 __global__ __launch_bounds__(1024) void k_rotary_sums(RotaryArgs a) {
     const RotarySegment& s = a.segment[blockIdx.y >> 1];
     const int k = blockIdx.y & 1, column = blockIdx.x * 16 + (threadIdx.x & 15), run = threadIdx.x >> 4;
