@@ -580,9 +580,9 @@ int    lsp_rotary_backward(const lsp_rotary_problem* problem, const lsp_rotary_g
  * with respect to H (dH, rows that do not count: zeros) and W (dW), overwritten; either may be NULL.  What is written overlaps nothing else.  weights: device, [rows] fp32, or NULL: ones (of rows that
  * do not count not used); scale is finite.
  * The products run on the matrix cores in `dtype` with fp32 accumulation (fp32: in fp32).  Rows are taken in blocks; for a block the
- * exponentials are kept in `dtype`, each relative to the largest of its row in a piece of the vocabulary, and become the gradient of z in place: two roundings
- * in 16 bits before the second products, the largest gradient of a row being computed without them (a target's).  No atomics that add: results are the same
- * bits from run to run.  A logit that is not finite reaches its row's loss and dH, and all of dW.
+ * exponentials are kept in 16 bits (fp32: in 32), each relative to the largest of its row in a piece of the vocabulary (what is below 2^-29 of that loses digits, and is 0 below
+ * 2^-40), and become the gradient of z in place, rounded to `dtype` before the second products; a target's is p - 1 of z in fp32, and dH has it without that rounding.  No atomics that add:
+ * results are the same bits from run to run.  A logit that is not finite reaches its row's loss and dH, and all of dW.
  * Workspaces: 16-byte aligned, as large as the queries say: bounded but for 4 bytes a row, however many there are. */
 typedef struct {
     const void*    H;

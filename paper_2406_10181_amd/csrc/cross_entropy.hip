@@ -7,13 +7,27 @@
 
 namespace lsp {
 
+// The largest of 64 lanes' numbers, in all of them
+__device__ __forceinline__ float top_of_wave(float x) {
+#pragma unroll
+    for (int d = 32; d; d /= 2) x = fmaxf(x, __shfl_xor(x, d));
+    return x;
+}
+// A row's part in the largest weight (of what is not finite none)
+__device__ __forceinline__ float weight_of(const LossArgs& a, int64_t row) {
+    const float w = a.weights ? fabsf(a.weights[row]) : 1.0f;
+    return w <= 3.402823466e38f ? w : 0.0f;
+}
+
 constexpr int kIndexThreads = 1024, kIndexRows = 4;                      // rows of a thread at a time
 
 // The rows that count, in order, and how many; one workgroup (the rows' targets are a few bytes each)
 __global__ __launch_bounds__(kIndexThreads) void k_loss_index(LossArgs a) {
     __shared__ int waves[kIndexThreads / 64];
+    __shared__ float tops[kIndexThreads / 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int found = 0;
+    float top = 0.0f;
     for (int64_t base = 0; base < a.rows; base += kIndexThreads * kIndexRows) {
         bool counts[kIndexRows];
         int mine = 0;
@@ -23,6 +37,7 @@ __global__ __launch_bounds__(kIndexThreads) void k_loss_index(LossArgs a) {
             const int64_t target = row < a.rows ? a.targets[row] : -1;
             counts[k] = target >= 0 && target < a.vocab;
             mine += counts[k];
+            if (counts[k]) top = fmaxf(top, weight_of(a, row));
         }
         int before = mine;                                               // of this lane and those below
 #pragma unroll
@@ -43,7 +58,12 @@ __global__ __launch_bounds__(kIndexThreads) void k_loss_index(LossArgs a) {
             if (counts[k]) a.index[at++] = (int)(base + threadIdx.x * kIndexRows + k);
         __syncthreads();
     }
-    if (threadIdx.x == 0) { a.count[0] = found; a.count[1] = 0; }
+    top = top_of_wave(top);
+    if (lane == 0) tops[wave] = top;
+    __syncthreads();
+    if (wave) return;
+    top = top_of_wave(lane < kIndexThreads / 64 ? tops[lane] : 0.0f);
+    if (lane == 0) { a.count[0] = found; a.count[1] = 0; a.count[2] = __float_as_int(top); }
 }
 
 // (4096 rows of 4096 in bf16: 15.6 us, 4.3 TB/s.)  Workgroups below block_rows: a row of the block's packed rows, zeros behind the last one up to a whole tile.  Workgroups from there on (first block only): a row
@@ -81,13 +101,20 @@ __global__ __launch_bounds__(256) void k_loss_pack(LossArgs a, int row_bytes, in
 constexpr int kFewRows = 2048;
 __global__ __launch_bounds__(256) void k_loss_pack_few(LossArgs a, int row_bytes, int elem) {
     __shared__ int waves[4][2];
+    __shared__ float tops[4];
     const int row = (int)min((int64_t)blockIdx.x, a.rows), rows = (int)a.rows;
     int before = 0, all = 0;
+    float top = 0.0f;
     for (int k = threadIdx.x; k < rows; k += 256) {
         const int64_t t = a.targets[k];
         const bool counts = t >= 0 && t < a.vocab;
         before += counts && k < row;
         all += counts;
+        if (blockIdx.x == 0 && counts) top = fmaxf(top, weight_of(a, k));
+    }
+    if (blockIdx.x == 0) {
+        top = top_of_wave(top);
+        if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
     }
 #pragma unroll
     for (int d = 32; d; d /= 2) { before += __shfl_xor(before, d); all += __shfl_xor(all, d); }
@@ -95,15 +122,20 @@ __global__ __launch_bounds__(256) void k_loss_pack_few(LossArgs a, int row_bytes
     __syncthreads();
     before = waves[0][0] + waves[1][0] + waves[2][0] + waves[3][0];
     all = waves[0][1] + waves[1][1] + waves[2][1] + waves[3][1];
-    if (blockIdx.x == 0 && threadIdx.x == 0) { a.count[0] = all; a.count[1] = 0; }
+    if (blockIdx.x == 0 && threadIdx.x == 0) { a.count[0] = all; a.count[1] = 0; a.count[2] = __float_as_int(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]))); }
     const u32x4* from = nullptr;
-    u32x4* to = nullptr;
+    u32x4 *to = nullptr, *again = nullptr;
     if ((int)blockIdx.x < rows) {
         const int64_t target = a.targets[row];
         if (target >= 0 && target < a.vocab) {
             from = reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.H) + row * a.h_stride * elem);
             to = reinterpret_cast<u32x4*>(a.packed + (int64_t)before * row_bytes);
-            if (threadIdx.x == 0) { a.index[before] = row; a.target[before] = (int)target; }
+            if (a.twice) again = reinterpret_cast<u32x4*>(a.packed + (int64_t)(all + before) * row_bytes);
+            if (threadIdx.x == 0) {
+                a.index[before] = row;
+                a.target[before] = (int)target;
+                if (a.twice) a.target[all + before] = -1;
+            }
         } else {
             if (threadIdx.x == 0) {
                 a.losses[row] = 0.0f;
@@ -112,13 +144,17 @@ __global__ __launch_bounds__(256) void k_loss_pack_few(LossArgs a, int row_bytes
             if (a.dH) to = reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.dH) + row * a.dh_stride * elem);
         }
     } else {
-        const int slot = all + (int)blockIdx.x - rows;
-        if (slot >= (all + 255) / 256 * 256) return;
+        const int there = rows_of_dw(a, all), slot = there + (int)blockIdx.x - rows;
+        if (slot >= (there + 255) / 256 * 256) return;
         to = reinterpret_cast<u32x4*>(a.packed + (int64_t)slot * row_bytes);
         if (threadIdx.x == 0) a.target[slot] = -1;
     }
     if (!to) return;
-    for (int k = threadIdx.x; k < row_bytes / 16; k += 256) to[k] = from ? from[k] : u32x4{0, 0, 0, 0};
+    for (int k = threadIdx.x; k < row_bytes / 16; k += 256) {
+        const u32x4 x = from ? from[k] : u32x4{0, 0, 0, 0};
+        to[k] = x;
+        if (again) again[k] = x;
+    }
 }
 
 // What RUNS threads a row make of its pieces, each a running maximum and sum; 16 rows
@@ -202,7 +238,8 @@ template <typename D, bool ROWS>
 __global__ __launch_bounds__(256) void k_loss_dz(LossArgs a) {
     const int rows = rows_of_block(a), chunks = (a.padded + kDzColumns - 1) / kDzColumns;
     const int row = (int)(blockIdx.x / chunks) * 16 + (threadIdx.x >> 4), v0 = (int)(blockIdx.x % chunks) * kDzColumns + (threadIdx.x & 15) * 8;
-    if (row >= (rows + 63) / 64 * 64) return;                              // (all sixteen rows are, or none)
+    const int all_rows = rows_of_dw(a, rows);
+    if ((int)(blockIdx.x / chunks) * 16 >= (all_rows + 63) / 64 * 64) return;
     typename D::elem* const e = reinterpret_cast<typename D::elem*>(a.e) + (int64_t)row * a.padded;
     const bool there = row < rows;
     float L = 0.0f, factor = 0.0f;
@@ -215,7 +252,7 @@ __global__ __launch_bounds__(256) void k_loss_dz(LossArgs a) {
             float all;
             L = runs.join(threadIdx.x >> 4, all);
             const int64_t to = a.index[a.block * a.block_rows + row];
-            factor = a.weights ? a.scale * a.weights[to] : a.scale;
+            factor = (a.weights ? a.scale * a.weights[to] : a.scale) * gradient_scale<D>(a);
             if (v0 == 0) store_loss(a, row, to, L, all);
         }
     } else if (there) {
@@ -228,9 +265,11 @@ __global__ __launch_bounds__(256) void k_loss_dz(LossArgs a) {
     for (int c = 0; c < kDzColumns; c += 128) {
         const int v = v0 + c;
         if (v >= a.padded) break;
-        Eight x;
+        Eight x, second;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) second.x[k] = 0.0f;
         if (there) {
-            x = load_eight<D>(e + v, 8);
+            x = load_eight<LossExp<D>>(reinterpret_cast<const typename LossExp<D>::elem*>(e + v), 8);
             const float of_piece = a.top[(int64_t)(v / a.piece) * a.block_rows + row];
             const float by = __builtin_amdgcn_exp2f((of_piece - L) * kLossLog2e) * (1.0f / kLossTop<D>) * rise * factor;
 #pragma unroll
@@ -238,14 +277,20 @@ __global__ __launch_bounds__(256) void k_loss_dz(LossArgs a) {
             if (target >= v && target < v + 8) {
                 // of the target z is there in fp32: p - 1 without what the rounding of p would leave of it
                 const float p_less_1 = expm1f(a.hit[row] - L), there_now = (p_less_1 * rise + (rise - 1.0f) + a.smoothing - share) * factor;
+                const float rest = D::size == 2 ? there_now - widen<D>(narrow<D>(there_now)) : 0.0f;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) x.x[k] = v + k == target ? there_now : x.x[k];
+                for (int k = 0; k < 8; ++k) {
+                    x.x[k] = v + k == target ? there_now : x.x[k];
+                    second.x[k] = v + k == target ? rest : 0.0f;
+                }
+                if (D::size == 2) a.left[row] = rest;
             }
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k) x.x[k] = 0.0f;
         }
-        store_eight<D>(e + v, x, 8);
+        if (there || row >= all_rows) store_eight<D>(e + v, x, 8);
+        if (there && a.twice) store_eight<D>(e + (int64_t)rows * a.padded + v, second, 8);
     }
 }
 
@@ -260,6 +305,8 @@ __global__ __launch_bounds__(256) void k_loss_dh_sum(LossArgs a) {
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 8
     for (int s = 0; s < parts.splits; ++s) sum += *reinterpret_cast<const f32x4*>(a.dh_parts + ((int64_t)s * parts.rows + row) * a.width + d);
+    if constexpr (D::size == 2)
+        sum += a.left[row] * (1.0f / gradient_scale<D>(a)) * four_of<D>(static_cast<const uint8_t*>(a.W) + (a.target[row] * a.w_stride + d) * D::size);
     store_four<D>(static_cast<uint8_t*>(a.dH) + (a.index[a.block * a.block_rows + row] * a.dh_stride + d) * D::size, sum[0], sum[1], sum[2], sum[3]);
 }
 
@@ -302,6 +349,7 @@ static double two_kinds_us(int64_t m, int64_t m_length, int64_t n, int64_t n_len
     return std::max(best, then);
 }
 
+constexpr int kTwiceRows = 32;
 void plan_loss(LossArgs& a, lsp_dtype dtype) {
     const bool fp32 = dtype == LSP_F32;
     const int64_t size = fp32 ? 4 : 2;
@@ -309,9 +357,11 @@ void plan_loss(LossArgs& a, lsp_dtype dtype) {
     const int64_t row = std::max<int64_t>(a.width, a.train ? a.padded : 0) * size;
     const int64_t most = std::max<int64_t>(256, std::min<int64_t>((int64_t)kLossBytes / row, a.train ? LSP_MAX_ROWS : 16384) / 256 * 256);
     a.blocks = (int)((a.rows + most - 1) / most);
-    a.block_rows = (int)ceil_to((a.rows + a.blocks - 1) / a.blocks, 256);
+    // 16 bits: the error of dW goes by the roundings of the targets' dz, of few rows by chance.  What they take off has rows of its own where those cost nothing: a stage of dW's products has 64.
+    a.twice = a.train && !fp32 && a.rows <= kTwiceRows;
+    a.block_rows = (int)ceil_to(a.twice ? 2 * a.rows : (a.rows + a.blocks - 1) / a.blocks, 256);
     a.blocks = (int)((a.rows + a.block_rows - 1) / a.block_rows);
-    const int64_t rows = std::min<int64_t>(a.rows, a.block_rows);
+    const int64_t rows = std::min<int64_t>(a.rows, a.block_rows), dw_rows = a.twice ? 2 * rows : rows;
     double least[2] = {1e30, 1e30};
     for (int k = fp32 ? 4 : 0; k < (fp32 ? 7 : 4); ++k) {
         const TileRate& r = kTileRates[k];
@@ -321,8 +371,8 @@ void plan_loss(LossArgs& a, lsp_dtype dtype) {
         const int64_t dh = tiles_of(a.width, rows, r), dw = tiles_of(a.width, a.vocab, r);
         for (int s = 1; s <= 32 && (s == 1 || (a.vocab / s >= 128 && dh * s <= 1024)); ++s) {
             const int64_t part = (a.vocab + s - 1) / s;
-            const double back = (rows > part ? two_kinds_us(dw, rows, dh * s, part, r) : two_kinds_us(dh * s, part, dw, rows, r)) + (s > 1 ? 4.0 + 1.6e-6 * (double)s * (double)(rows * a.width) : 0.0);
-            if (back < least[1]) { least[1] = back; a.tile[1] = r.tile; a.dh_splits = s; a.dw_first = rows > part; }
+            const double back = (dw_rows > part ? two_kinds_us(dw, dw_rows, dh * s, part, r) : two_kinds_us(dh * s, part, dw, dw_rows, r)) + (s > 1 ? 4.0 + 1.6e-6 * (double)s * (double)(rows * a.width) : 0.0);
+            if (back < least[1]) { least[1] = back; a.tile[1] = r.tile; a.dh_splits = s; a.dw_first = dw_rows > part; }
         }
     }
     a.piece = std::max(a.tile[0] / 2, 32);
@@ -349,6 +399,7 @@ size_t loss_workspace(LossArgs& a, lsp_dtype dtype, uint8_t* base) {
     if (a.train) {
         take(a.log_sum, (size_t)a.block_rows * 4);
         take(a.factor, (size_t)a.block_rows * 4);
+        take(a.left, size == 2 ? (size_t)a.block_rows * 4 : 0);
         take(a.e, (size_t)a.block_rows * a.padded * size);
         take(a.dh_parts, a.dh_splits > 1 ? (size_t)a.dh_splits * a.block_rows * a.width * 4 : 0);
         take(a.dw_sum, a.blocks > 1 && size == 2 ? (size_t)a.vocab * a.width * 4 : 0);

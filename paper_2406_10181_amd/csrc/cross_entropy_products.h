@@ -70,7 +70,7 @@ __global__ __launch_bounds__((LossProduct<D, TILE, false, false>::kThreads)) voi
             for (int x = 0; x < 4; ++x) top = fmaxf(top, p.acc[j][i][x]);
         top = quarters_max(top);
         // (the rounding of `from` is one factor for all of the piece, and of its sum: no further from 1 than a rounding of L is from L)
-        const float from = top == -INFINITY ? 0.0f : -top * kLossLog2e;
+        const float from = top == -INFINITY ? 0.0f : fmaf(-top, kLossLog2e, kLossTopLog2<D>);
 #pragma unroll
         for (int i = 0; i < P::MI; ++i)
 #pragma unroll
@@ -79,14 +79,14 @@ __global__ __launch_bounds__((LossProduct<D, TILE, false, false>::kThreads)) voi
         for (int i = 0; i < P::MI; ++i)
 #pragma unroll
             for (int x = 0; x < 4; ++x) sum += p.acc[j][i][x];
-        sum = quarters_sum(sum);
+        sum = quarters_sum(sum) * (1.0f / kLossTop<D>);
         if (g == 0) { a.top[piece * a.block_rows + row] = top; a.sum[piece * a.block_rows + row] = sum; }
     }
     if (!a.train) return;
 #pragma unroll
     for (int j = 0; j < P::NI; j += 2) {
         const int row0 = r0 + 16 * (wn * P::NI + j);
-        store_two_blocks<D, P::MI>(p.acc + j, kLossTop<D>, lds + wave * (32 * P::kRange * D::size), P::kRange, lane,
+        store_two_blocks<LossExp<D>, P::MI>(p.acc + j, 1.0f, lds + wave * (32 * P::kRange * D::size), P::kRange, lane,
                                    [&](uint32_t r) { return a.e + ((int64_t)(row0 + (int)r) * a.padded + first) * D::size; });
     }
 }
@@ -109,6 +109,19 @@ template <typename D, int TILE> __device__ __forceinline__ void loss_dh(const Lo
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM;
     const int first = d0 + wm * P::kRange, left = a.width - first;
     const float factor = 1.0f / gradient_scale<D>(a);
+    if constexpr (D::size == 2) {
+        // what the rounding of a target's dz took off, times its row of W; with several parts k_loss_dh_sum adds it
+        if (a.dh_splits == 1) {
+#pragma unroll
+            for (int j = 0; j < P::NI; ++j) {
+                const int row = min(r0 + 16 * (wn * P::NI + j) + (lane & 15), rows - 1), d = first + 4 * (lane >> 4);
+                const float x = a.left[row];
+                const uint8_t* const w = static_cast<const uint8_t*>(a.W) + a.target[row] * w_bytes;
+#pragma unroll
+                for (int i = 0; i < P::MI; ++i) p.acc[j][i] += x * four_of<D>(w + min(d + 16 * i, a.width - 4) * D::size);
+            }
+        }
+    }
 #pragma unroll
     for (int j = 0; j < P::NI; j += 2) {
         const int row0 = r0 + 16 * (wn * P::NI + j);
@@ -137,7 +150,7 @@ template <typename D, int TILE> __device__ __forceinline__ void loss_dw(const Lo
     const int64_t h_bytes = (int64_t)a.width * D::size, e_bytes = (int64_t)a.padded * D::size;
     P p;
     // (up to whole steps: the rows behind those that count are zeros in both)
-    if (!p.run({a.packed + (int64_t)d0 * D::size, h_bytes}, {a.e + (int64_t)v0 * D::size, e_bytes}, (rows + P::BK - 1) / P::BK * P::BK, a.width - d0, P::BN, lds)) return;
+    if (!p.run({a.packed + (int64_t)d0 * D::size, h_bytes}, {a.e + (int64_t)v0 * D::size, e_bytes}, (rows_of_dw(a, rows) + P::BK - 1) / P::BK * P::BK, a.width - d0, P::BN, lds)) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wm = wave % P::WM, wn = wave / P::WM;
     const int first = d0 + wm * P::kRange, left = a.width - first;
     const float factor = 1.0f / gradient_scale<D>(a);

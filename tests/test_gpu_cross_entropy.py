@@ -148,6 +148,20 @@ def test_gradients_by_differences(smoothing, z_loss):
             assert abs((f[0] - f[1]) / (2 * h) - right) <= allowed, (k, f, right, allowed)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows", [20, 400])
+def test_no_rounding_is_seen_beside_the_last_one(dtype, rows):
+    """Of equal weights, beside results that are rounded once.  dH: the targets' dz has no rounding, and other probabilities, a few hundredths of it, are off by u each: some percent.  dW of up to
+    32 rows too; of more the targets' dz is just below a power of two, where a rounding is off by u / 2 at most, as results are on average by about u / sqrt(6): (1 + (1 / 4 / 3) / (1 / 6)) ** 0.5 = 1.22."""
+    c = Case(dtype, rows, 512, 3000, weights=False, scale=1 / rows, seed=15)
+    c.backward()
+    want = ref.cross_entropy(f64(c.H), f64(c.W), c.targets.cpu().numpy(), scale=1 / rows, dtype=dtype)
+    for k, times in (("dH", 1.1), ("dW", 1.1 if rows <= 32 else 1.3)):
+        value = torch.from_numpy(want[k][0])
+        once = (value.to(DTYPE[dtype]).double() - value).norm()
+        assert (torch.from_numpy(f64(getattr(c, k))) - value).norm() <= times * once, k
+
+
 def test_rows_that_do_not_count_are_not_read():
     c = Case("bf16", 90, 64, 500, seed=2)
     c.targets[::3] = torch.tensor([-1, 500, -2 ** 63, 2 ** 62, 2 ** 32], device="cuda").repeat(6)

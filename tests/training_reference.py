@@ -114,8 +114,12 @@ def cross_entropy(H, W, targets, *, smoothing=0.0, z_loss=0.0, weights=None, sca
         dz = (p * rise - (1 - smoothing) * one - smoothing / V) * g
         ep = p * (es + eL + EPS * 32)                                        # of p in fp32
         edz = ((ep + u * p * (1 - one)) * np.abs(rise) + p * 2 * z_loss * eL + 4 * EPS * (p * np.abs(rise) + one + smoothing / V)) * np.abs(g) + u * np.abs(dz)
-        if dtype == "f16":                                                   # what lies below the smallest numbers: 2^-25 in units of 2^-15 and of 2^-13 of the largest
-            edz += 2.0 ** -39 * np.abs(rise * g) + 2.0 ** -37 * (np.abs(g) * (2 + 2 * z_loss * np.abs(L))).max()
+        # What lies below the smallest numbers.  Exponentials of both 16-bit types are fp16 numbers, whose steps are no smaller than 2^-24, in units of 2^-15 of the largest of their piece: off by
+        # 2^-25 2^-15 of a probability of at most 1, and as much again for its factors' roundings.
+        if dtype != "f32":
+            edz += 2.0 ** -39 * np.abs(rise * g)
+        if dtype == "f16":                                                   # dz: 2^-25 in units of 2^-13 of the largest, and the factors' roundings
+            edz += 2.0 ** -37 * (np.abs(g) * (2 + 2 * z_loss * np.abs(L))).max()
         z["dH"][rows], z["dW"] = dz @ W, dz.T @ h
         e["dH"][rows] = edz @ np.abs(W) + EPS * (V + 4) * (np.abs(dz) @ np.abs(W))
         e["dW"] = edz.T @ np.abs(h) + EPS * (len(rows) + 4) * (np.abs(dz).T @ np.abs(h))
