@@ -245,6 +245,48 @@ def test_a_captured_call_repeats_with_other_rows():
         c.check()
 
 
+@pytest.mark.parametrize("rows", [1, 24, 32, 33])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_few_rows_and_weights_that_change_between_replays(dtype, rows):
+    """Rows with second ones behind them; which count, and the largest weight, is found by each replay; weights of rows that do not count are not used, and one of infinity stays in its row and in dW."""
+    c = Case(dtype, rows, 64, 700, seed=16)
+    p = c.problem()
+    n = L.lsp_cross_entropy_backward_workspace_bytes(p, c.code)
+    ws = room(n)
+    g = L.cross_entropy_gradients(c.dH, c.dW, weights=c.weights)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        L.lsp_cross_entropy_backward(p, g, c.code, ws, n, torch.cuda.current_stream())
+    for k in range(5):
+        gen = torch.Generator().manual_seed(k)
+        targets = torch.randint(0, 700, (rows,), generator=gen)
+        targets[torch.rand(rows, generator=gen) < 0.25 * k] = -1             # (the last time no row counts)
+        weights = torch.rand(rows, generator=gen) * 10.0 ** (k - 2)
+        c.targets.copy_(targets), c.weights.copy_(weights), c.H.copy_(torch.randn(c.H.shape, generator=gen))
+        left_out = c.targets < 0
+        c.weights[left_out] = 0.0                                            # (for the oracle)
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        c.check()
+        kept = c.dH.clone(), c.dW.clone()
+        c.weights[left_out] = float("nan")
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(kept[0], c.dH) and torch.equal(kept[1], c.dW)
+        c.weights[left_out] = 0.0
+    c.targets.fill_(5)
+    c.weights.fill_(1.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    kept = c.dH.clone()
+    c.weights[0] = float("inf")
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(kept[1:], c.dH[1:]) and not torch.isfinite(c.dH[0]).any()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_blocks_of_rows(dtype):
     """More rows than one block of exponentials holds: dW is a sum over blocks."""
