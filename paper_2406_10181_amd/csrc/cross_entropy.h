@@ -3,8 +3,8 @@
 // A block of rows goes through five kernels.  k_loss_pack copies the rows of H that count, one behind the other, so that rows that do not count cost nothing and are not
 // read.  k_loss_logits multiplies W by them; z[v][row] is in registers with the row across lanes and a piece of the vocabulary (a wave's part of the tile)
 // in the lane's registers, so that a piece's maximum and sum of exponentials take no LDS.  The exponentials, relative to the piece's maximum, are stored in 16 bits (fp32: in 32): whatever
-// the size of z they keep its digits, where z itself in 16 bits would be off by a hundredth of a unit and p by a percent.  k_loss_rows makes the rows' L and losses of
-// the pieces (k_loss_dz, where they are few); k_loss_dz turns the exponentials into the gradient of z in place; k_loss_back multiplies that by W and by H.
+// the size of z they keep its digits, where z itself in 16 bits would be off by a hundredth of a unit and p by a percent.  k_loss_rows makes the rows' maxima, sums and losses of
+// the pieces (k_loss_dz, where they are few), maximum and sum apart: nothing that p is made of is rounded at the size of z; k_loss_dz turns the exponentials into the gradient of z in place; k_loss_back multiplies that by W and by H.
 //
 // Of the roundings on the way one would be seen in 16 bits, that of a target's dz, which is most of its row: dH gets what it takes off, times the target's row of W, behind the products; for
 // dW the gradient's scale keeps it small, and of up to 32 rows what is taken off has rows of its own.  dH is as far from the exact one as a result that is rounded once, dW up to 1.4 times as
@@ -40,7 +40,7 @@ struct LossArgs {
     int32_t* target;             // [block_rows]
     float *top, *sum, *plain;    // [pieces][block_rows]: a piece's maximum, sum of exponentials, sum of z (with smoothing only)
     float *hit;                  // [block_rows]: z[target]
-    float *log_sum;              // [block_rows]: L
+    float *row_top, *row_sum;    // [block_rows]: a row's maximum t and the sum of exp(z - t)
     float *factor;               // [block_rows]: scale * weight
     float *left;                 // [block_rows], 16 bits: what the rounding of dz[row][target] took off
     uint8_t* e;                  // [block_rows][padded]

@@ -157,6 +157,11 @@ __global__ __launch_bounds__(256) void k_loss_pack_few(LossArgs a, int row_bytes
     }
 }
 
+// A row's maximum t and the sum of exp(z - t).  They stay apart: in L = t + log(sum) the logarithm loses the digits that t needs, and p and the loss are made of z - t, which has none of t's size.
+struct RowSum {
+    float top, sum;
+    __device__ __forceinline__ float log_of_sum() const { return logf(sum); }
+};
 // What RUNS threads a row make of its pieces, each a running maximum and sum; 16 rows
 template <int RUNS> struct Runs {
     float top[RUNS][17], sum[RUNS][17], plain[RUNS][17];
@@ -176,8 +181,8 @@ template <int RUNS> struct Runs {
         }
         top[run][r] = t; sum[run][r] = s; plain[run][r] = x;
     }
-    // L, and the sum of z
-    __device__ __forceinline__ float join(int r, float& all) const {
+    // `all`: the sum of z
+    __device__ __forceinline__ RowSum join(int r, float& all) const {
         float t = top[0][r], s = 0.0f;
 #pragma unroll 16
         for (int k = 1; k < RUNS; ++k) t = fmaxf(t, top[k][r]);
@@ -188,12 +193,14 @@ template <int RUNS> struct Runs {
             s += sum[k][r] * __builtin_amdgcn_exp2f((top[k][r] - from) * kLossLog2e);
             all += plain[k][r];
         }
-        return t + logf(s);
+        return {t, s};
     }
 };
-__device__ __forceinline__ void store_loss(const LossArgs& a, int row, int64_t to, float L, float all) {
-    float loss = L - (1.0f - a.smoothing) * a.hit[row];
-    if (a.smoothing > 0.0f) loss -= a.smoothing * (all / (float)a.vocab);
+// (-(1 - smoothing) z[target] - smoothing mean(z) as differences from t)
+__device__ __forceinline__ void store_loss(const LossArgs& a, int row, int64_t to, const RowSum& of, float all) {
+    const float log = of.log_of_sum(), L = of.top + log;
+    float loss = fmaf(1.0f - a.smoothing, of.top - a.hit[row], log);
+    if (a.smoothing > 0.0f) loss = fmaf(a.smoothing, of.top - all / (float)a.vocab, loss);
     if (a.z_loss > 0.0f) loss = fmaf(a.z_loss * L, L, loss);
     a.losses[to] = loss;
     if (a.logs) a.logs[to] = L;
@@ -210,14 +217,15 @@ __global__ __launch_bounds__(16 * RUNS) void k_loss_rows(LossArgs a, int fp16) {
     float bound = 0.0f;
     if (run == 0 && row < rows) {
         float all;
-        const float L = runs.join(r, all);
+        const RowSum of = runs.join(r, all);
         const int64_t to = a.index[a.block * a.block_rows + row];
-        store_loss(a, row, to, L, all);
+        store_loss(a, row, to, of, all);
         if (a.train) {
             const float factor = a.weights ? a.scale * a.weights[to] : a.scale;
-            a.log_sum[row] = L;
+            a.row_top[row] = of.top;
+            a.row_sum[row] = of.sum;
             a.factor[row] = factor;
-            bound = fabsf(factor) * fmaf(2.0f * a.z_loss, fabsf(L), 2.0f);
+            bound = fabsf(factor) * fmaf(2.0f * a.z_loss, fabsf(of.top + of.log_of_sum()), 2.0f);
         }
     }
     if (!fp16 || !a.train || run) return;
@@ -242,7 +250,8 @@ __global__ __launch_bounds__(256) void k_loss_dz(LossArgs a) {
     if ((int)(blockIdx.x / chunks) * 16 >= (all_rows + 63) / 64 * 64) return;
     typename D::elem* const e = reinterpret_cast<typename D::elem*>(a.e) + (int64_t)row * a.padded;
     const bool there = row < rows;
-    float L = 0.0f, factor = 0.0f;
+    RowSum of = {0.0f, 1.0f};
+    float factor = 0.0f;
     if constexpr (ROWS) {
         __shared__ Runs<kDzRuns> runs;
         const int r = threadIdx.x & 15, of_r = row - (int)(threadIdx.x >> 4) + r;
@@ -250,16 +259,16 @@ __global__ __launch_bounds__(256) void k_loss_dz(LossArgs a) {
         __syncthreads();
         if (there) {
             float all;
-            L = runs.join(threadIdx.x >> 4, all);
+            of = runs.join(threadIdx.x >> 4, all);
             const int64_t to = a.index[a.block * a.block_rows + row];
             factor = (a.weights ? a.scale * a.weights[to] : a.scale) * gradient_scale<D>(a);
-            if (v0 == 0) store_loss(a, row, to, L, all);
+            if (v0 == 0) store_loss(a, row, to, of, all);
         }
     } else if (there) {
-        L = a.log_sum[row];
+        of = {a.row_top[row], a.row_sum[row]};
         factor = a.factor[row] * gradient_scale<D>(a);
     }
-    const float share = a.smoothing / (float)a.vocab, rise = fmaf(2.0f * a.z_loss, L, 1.0f);
+    const float log = of.log_of_sum(), share = a.smoothing / (float)a.vocab, rise = fmaf(2.0f * a.z_loss, of.top + log, 1.0f), of_sum = 1.0f / (of.sum * kLossTop<D>) * rise * factor;
     const int target = there ? a.target[row] : -1;
 #pragma unroll 4
     for (int c = 0; c < kDzColumns; c += 128) {
@@ -271,12 +280,12 @@ __global__ __launch_bounds__(256) void k_loss_dz(LossArgs a) {
         if (there) {
             x = load_eight<LossExp<D>>(reinterpret_cast<const typename LossExp<D>::elem*>(e + v), 8);
             const float of_piece = a.top[(int64_t)(v / a.piece) * a.block_rows + row];
-            const float by = __builtin_amdgcn_exp2f((of_piece - L) * kLossLog2e) * (1.0f / kLossTop<D>) * rise * factor;
+            const float by = __builtin_amdgcn_exp2f((of_piece - of.top) * kLossLog2e) * of_sum;
 #pragma unroll
             for (int k = 0; k < 8; ++k) x.x[k] = v + k < a.vocab ? fmaf(x.x[k], by, -share * factor) : 0.0f;
             if (target >= v && target < v + 8) {
                 // of the target z is there in fp32: p - 1 without what the rounding of p would leave of it
-                const float p_less_1 = expm1f(a.hit[row] - L), there_now = (p_less_1 * rise + (rise - 1.0f) + a.smoothing - share) * factor;
+                const float p_less_1 = expm1f((a.hit[row] - of.top) - log), there_now = (p_less_1 * rise + (rise - 1.0f) + a.smoothing - share) * factor;
                 const float rest = D::size == 2 ? there_now - widen<D>(narrow<D>(there_now)) : 0.0f;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
@@ -397,7 +406,8 @@ size_t loss_workspace(LossArgs& a, lsp_dtype dtype, uint8_t* base) {
     take(a.plain, a.smoothing > 0.0f ? (size_t)a.pieces * a.block_rows * 4 : 0);
     take(a.hit, (size_t)a.block_rows * 4);
     if (a.train) {
-        take(a.log_sum, (size_t)a.block_rows * 4);
+        take(a.row_top, (size_t)a.block_rows * 4);
+        take(a.row_sum, (size_t)a.block_rows * 4);
         take(a.factor, (size_t)a.block_rows * 4);
         take(a.left, size == 2 ? (size_t)a.block_rows * 4 : 0);
         take(a.e, (size_t)a.block_rows * a.padded * size);

@@ -69,12 +69,12 @@ __global__ __launch_bounds__((LossProduct<D, TILE, false, false>::kThreads)) voi
 #pragma unroll
             for (int x = 0; x < 4; ++x) top = fmaxf(top, p.acc[j][i][x]);
         top = quarters_max(top);
-        // (the rounding of `from` is one factor for all of the piece, and of its sum: no further from 1 than a rounding of L is from L)
-        const float from = top == -INFINITY ? 0.0f : fmaf(-top, kLossLog2e, kLossTopLog2<D>);
+        // (The maximum is taken off first: near it that has no rounding, however large both are.)
+        const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
         for (int i = 0; i < P::MI; ++i)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) p.acc[j][i][x] = __builtin_amdgcn_exp2f(fmaf(p.acc[j][i][x], kLossLog2e, from));
+            for (int x = 0; x < 4; ++x) p.acc[j][i][x] = __builtin_amdgcn_exp2f(fmaf(p.acc[j][i][x] - base, kLossLog2e, kLossTopLog2<D>));
 #pragma unroll
         for (int i = 0; i < P::MI; ++i)
 #pragma unroll
