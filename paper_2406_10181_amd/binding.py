@@ -97,35 +97,35 @@ _four = ctypes.c_int64 * 4
 
 
 class _AttentionOfTensors(lsp_attention_problem):
-    _fields_ = [("dtype", ctypes.c_int32)]
+    _fields_ = [("dtype", ctypes.c_int32), ("device", ctypes.c_int32)]
 
 
 class _AttentionGradientsOfTensors(lsp_attention_gradients):
-    _fields_ = [("q_shape", _four), ("k_shape", _four), ("dtype", ctypes.c_int32)]
+    _fields_ = [("q_shape", _four), ("k_shape", _four), ("dtype", ctypes.c_int32), ("device", ctypes.c_int32)]
 
 
 class _ResidualNormOfTensors(lsp_residual_norm_problem):
-    _fields_ = [("dtype", ctypes.c_int32)]
+    _fields_ = [("dtype", ctypes.c_int32), ("device", ctypes.c_int32)]
 
 
 class _ResidualNormGradientsOfTensors(lsp_residual_norm_gradients):
-    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("dtype", ctypes.c_int32), ("device", ctypes.c_int32)]
 
 
 class _RotaryOfTensors(lsp_rotary_problem):
-    _fields_ = [("dtype", ctypes.c_int32)]
+    _fields_ = [("dtype", ctypes.c_int32), ("device", ctypes.c_int32)]
 
 
 class _RotaryGradientsOfTensors(lsp_rotary_gradients):
-    _fields_ = [("q_shape", _four), ("k_shape", _four), ("kr_shape", _four), ("dtype", ctypes.c_int32)]
+    _fields_ = [("q_shape", _four), ("k_shape", _four), ("kr_shape", _four), ("dtype", ctypes.c_int32), ("device", ctypes.c_int32)]
 
 
 class _CrossEntropyOfTensors(lsp_cross_entropy_problem):
-    _fields_ = [("dtype", ctypes.c_int32)]
+    _fields_ = [("dtype", ctypes.c_int32), ("device", ctypes.c_int32)]
 
 
 class _CrossEntropyGradientsOfTensors(lsp_cross_entropy_gradients):
-    _fields_ = [("h_shape", ctypes.c_int64 * 2), ("w_shape", ctypes.c_int64 * 2), ("weights_count", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+    _fields_ = [("h_shape", ctypes.c_int64 * 2), ("w_shape", ctypes.c_int64 * 2), ("weights_count", ctypes.c_int64), ("dtype", ctypes.c_int32), ("device", ctypes.c_int32)]
 
 
 NORM_KIND = {"none": 0, "rms": 1, "layer": 2}
@@ -518,7 +518,8 @@ def _operator_calls():
         L, module = lib(), _bound()
         module.bind_operators(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
             L.lsp_dropout, L.lsp_attention_forward, L.lsp_attention_backward, L.lsp_residual_norm_forward, L.lsp_residual_norm_backward, L.lsp_rotary_forward,
-            L.lsp_rotary_backward, L.lsp_cross_entropy_forward, L.lsp_cross_entropy_backward)),
+            L.lsp_rotary_backward, L.lsp_cross_entropy_forward, L.lsp_cross_entropy_backward, L.lsp_attention_forward_workspace_bytes, L.lsp_attention_backward_workspace_bytes,
+            L.lsp_residual_norm_backward_workspace_bytes, L.lsp_rotary_backward_workspace_bytes, L.lsp_cross_entropy_forward_workspace_bytes, L.lsp_cross_entropy_backward_workspace_bytes)),
             lsp_attention_problem, lsp_attention_gradients, lsp_residual_norm_problem, lsp_residual_norm_gradients, lsp_rotary_problem, lsp_rotary_gradients,
             lsp_cross_entropy_problem, lsp_cross_entropy_gradients,
             _AttentionOfTensors, _AttentionGradientsOfTensors, _ResidualNormOfTensors, _ResidualNormGradientsOfTensors, _RotaryOfTensors, _RotaryGradientsOfTensors,
@@ -725,6 +726,8 @@ def lsp_adamw(items: AdamwItems, *, rate: float, beta1: float = 0.9, beta2: floa
     if grad_scale is not None and hasattr(grad_scale, "numel") and \
             (grad_scale.numel() != 1 or grad_scale.element_size() != 4 or not grad_scale.is_floating_point() or items.device not in (None, grad_scale.device)):
         raise ValueError("lsp_adamw: grad_scale is one float32 on the tensors' device")
+    if items.device is not None and items.device.type == "cpu":
+        raise ValueError("lsp_adamw: the tensors are on the host")
     rc = lib().lsp_adamw(items.array, len(items.array), STATE_KIND[items.states], rate, beta1, beta2, eps, step, _ptr(grad_scale), _stream(stream))
     if check and rc:
         _check(rc, "lsp_adamw")

@@ -34,6 +34,10 @@ decltype(&lsp_rotary_forward) g_rotary_forward;
 decltype(&lsp_rotary_backward) g_rotary_backward;
 decltype(&lsp_cross_entropy_forward) g_loss_forward;
 decltype(&lsp_cross_entropy_backward) g_loss_backward;
+decltype(&lsp_attention_forward_workspace_bytes) g_attention_forward_bytes, g_attention_backward_bytes;
+decltype(&lsp_residual_norm_backward_workspace_bytes) g_norm_backward_bytes;
+decltype(&lsp_rotary_backward_workspace_bytes) g_rotary_backward_bytes;
+decltype(&lsp_cross_entropy_forward_workspace_bytes) g_loss_forward_bytes, g_loss_backward_bytes;
 
 PyObject* g_shape;
 PyObject* g_stride;
@@ -181,6 +185,15 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 // residual norm's in Python, 3.7 here with three vectors; attention's 4.2, with lengths 4.5), with the checks that only the tensors allow: shapes, types and devices that belong
 // together, contiguous last axes.
 
+// The device that a tensor is on, -1: the host; false with a Python exception set
+bool device_of(PyObject* t, long& device) {
+    PyObject* where = PyObject_CallMethodNoArgs(t, g_get_device);
+    if (!where) return false;
+    device = PyLong_AsLong(where);
+    Py_DECREF(where);
+    return !PyErr_Occurred();
+}
+
 // What a tensor says of itself; false with a Python exception set
 struct Tensor {
     void* data = nullptr;
@@ -210,15 +223,6 @@ struct Tensor {
     }
     bool same_shape(const Tensor& o) const { return shape[0] == o.shape[0] && shape[1] == o.shape[1] && shape[2] == o.shape[2] && shape[3] == o.shape[3]; }
 };
-
-// The device that a tensor is on, -1: the host; false with a Python exception set
-bool device_of(PyObject* t, long& device) {
-    PyObject* where = PyObject_CallMethodNoArgs(t, g_get_device);
-    if (!where) return false;
-    device = PyLong_AsLong(where);
-    Py_DECREF(where);
-    return !PyErr_Occurred();
-}
 
 PyObject* refuse(const char* text) {
     PyErr_SetString(PyExc_ValueError, text);
@@ -252,16 +256,31 @@ float number(PyObject* x, bool& ok) {
     return (float)v;
 }
 
+// Whether all tensors of a descriptor (None: passed over) are on one device, and on which: a kernel that follows an address of the host, where caches and lists of lengths may well be, faults.
+// False with a Python exception set.  (0.08 us a tensor.)
+bool on_one_device(PyObject* const* t, int count, int32_t& device, const char* what) {
+    bool any = false;
+    for (int i = 0; i < count; ++i) {
+        if (t[i] == Py_None) continue;
+        long d;
+        if (!device_of(t[i], d)) return false;
+        if (any && d != device) { PyErr_Format(PyExc_ValueError, "%s: the tensors are on one device", what); return false; }
+        device = (int32_t)d;
+        any = true;
+    }
+    return true;
+}
+
 // What a descriptor made here remembers beside the C structure, so that the call can compare it with its other arguments: the binding's objects have these
 // fields behind the structure's own.
-struct AttentionOfTensors { lsp_attention_problem p; int32_t dtype; };
-struct AttentionGradientsOfTensors { lsp_attention_gradients g; int64_t q_shape[4], k_shape[4]; int32_t dtype; };
-struct ResidualNormOfTensors { lsp_residual_norm_problem p; int32_t dtype; };
-struct ResidualNormGradientsOfTensors { lsp_residual_norm_gradients g; int64_t rows, width; int32_t dtype; };
-struct RotaryOfTensors { lsp_rotary_problem p; int32_t dtype; };
-struct RotaryGradientsOfTensors { lsp_rotary_gradients g; int64_t q_shape[4], k_shape[4], kr_shape[4]; int32_t dtype; };
-struct CrossEntropyOfTensors { lsp_cross_entropy_problem p; int32_t dtype; };
-struct CrossEntropyGradientsOfTensors { lsp_cross_entropy_gradients g; int64_t h_shape[2], w_shape[2], weights; int32_t dtype; };
+struct AttentionOfTensors { lsp_attention_problem p; int32_t dtype, device; };
+struct AttentionGradientsOfTensors { lsp_attention_gradients g; int64_t q_shape[4], k_shape[4]; int32_t dtype, device; };
+struct ResidualNormOfTensors { lsp_residual_norm_problem p; int32_t dtype, device; };
+struct ResidualNormGradientsOfTensors { lsp_residual_norm_gradients g; int64_t rows, width; int32_t dtype, device; };
+struct RotaryOfTensors { lsp_rotary_problem p; int32_t dtype, device; };
+struct RotaryGradientsOfTensors { lsp_rotary_gradients g; int64_t q_shape[4], k_shape[4], kr_shape[4]; int32_t dtype, device; };
+struct CrossEntropyOfTensors { lsp_cross_entropy_problem p; int32_t dtype, device; };
+struct CrossEntropyGradientsOfTensors { lsp_cross_entropy_gradients g; int64_t h_shape[2], w_shape[2], weights; int32_t dtype, device; };
 
 bool matches(const AttentionOfTensors& a, const AttentionGradientsOfTensors& b) {
     const int64_t q[4] = {a.p.batch, a.p.q_len, a.p.heads, a.p.head_dim}, k[4] = {a.p.batch, a.p.k_len, a.p.kv_heads, a.p.head_dim};
@@ -299,11 +318,9 @@ PyObject* attention_problem(PyObject*, PyObject* const* args, Py_ssize_t nargs) 
         Tensor n;
         if (!n.read(args[6 + i], 1, what)) return nullptr;
         if (n.shape[0] != q.shape[0]) return refuse("attention_problem: lengths are [batch]");
-        long there, here;                              // (the one operand that a program may well have on the host, where the kernels must not read it)
-        if (!device_of(args[6 + i], there) || !device_of(args[1], here)) return nullptr;
-        if (there != here) return refuse("attention_problem: lengths are on the device of the other tensors");
         lens[i] = n.data;
     }
+    if (!on_one_device(args + 1, 7, d->device, what)) return nullptr;
     Args tail(args + 9);
     bool ok = true;
     const float scale = number(args[8], ok), dropout = number(args[10], ok);
@@ -330,6 +347,7 @@ PyObject* attention_gradients(PyObject*, PyObject* const* args, Py_ssize_t nargs
     for (int i = 0; i < 4; ++i) if (!t[i].read(args[1 + i], 4, "attention_gradients")) return nullptr;
     if (!t[0].same_shape(t[1]) || !t[2].same_shape(t[3])) return refuse("attention_gradients: dO and dQ, and dK and dV, are of one shape");
     for (const Tensor& x : t) if (type_code(x.dtype) < 0 || x.dtype != t[0].dtype) return refuse("attention_gradients: dO, dQ, dK and dV are of one type, float32, float16 or bfloat16");
+    if (!on_one_device(args + 1, 4, d->device, "attention_gradients")) return nullptr;
     for (int i = 0; i < 4; ++i) { d->q_shape[i] = t[1].shape[i]; d->k_shape[i] = t[2].shape[i]; }
     d->dtype = type_code(t[0].dtype);
     d->g = lsp_attention_gradients{t[0].data, t[1].data, t[2].data, t[3].data, {t[0].stride[0], t[0].stride[1], t[0].stride[2]}, {t[1].stride[0], t[1].stride[1], t[1].stride[2]},
@@ -363,6 +381,7 @@ PyObject* residual_norm_problem(PyObject*, PyObject* const* args, Py_ssize_t nar
         return refuse("residual_norm_problem: stats are [4][rows], float32");
     void* v[5];
     for (int i = 0; i < 5; ++i) if (!vector(args[6 + i], x.shape[1], x.dtype, v[i], what)) return nullptr;
+    if (!on_one_device(args + 1, 10, d->device, what)) return nullptr;
     Args kinds(args + 11), tail(args + 17);
     const int32_t post = kinds.int32(), pre = kinds.int32();
     bool ok = kinds.ok;
@@ -391,6 +410,7 @@ PyObject* residual_norm_gradients(PyObject*, PyObject* const* args, Py_ssize_t n
             return refuse("residual_norm_gradients: dy, dh, dx and df are of one shape and type, float32, float16 or bfloat16");
     void* v[5];
     for (int i = 0; i < 5; ++i) if (!vector(args[5 + i], t[0].shape[1], g_types[LSP_F32], v[i], what)) return nullptr;
+    if (!on_one_device(args + 1, 9, d->device, what)) return nullptr;
     d->rows = t[0].shape[0]; d->width = t[0].shape[1]; d->dtype = type_code(t[0].dtype);
     d->g = lsp_residual_norm_gradients{t[0].data, t[1].data, t[2].data, t[3].data, static_cast<float*>(v[0]), static_cast<float*>(v[1]), static_cast<float*>(v[2]), static_cast<float*>(v[3]),
                                      static_cast<float*>(v[4]), t[0].stride[0], t[1].stride[0], t[2].stride[0], t[3].stride[0]};
@@ -414,20 +434,6 @@ PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     return without_gil([&] { return g_dropout(x, y, rows, width, p, seed, offset, static_cast<lsp_dtype>(dtype), st); });
 }
 
-// Whether tensors (None: passed over) are on one device; false with a Python exception set
-bool on_one_device(PyObject* const* t, int count, const char* what) {
-    long first = 0;
-    bool any = false;
-    for (int i = 0; i < count; ++i) {
-        if (t[i] == Py_None) continue;
-        long d;
-        if (!device_of(t[i], d)) return false;
-        if (any && d != first) { PyErr_Format(PyExc_ValueError, "%s: the tensors are on one device", what); return false; }
-        first = d;
-        any = true;
-    }
-    return true;
-}
 // A contiguous tensor of integers of one type, or None
 bool whole_numbers(PyObject* t, int dims, const int64_t* shape, const PyObject* dtype, void*& to, const char* what) {
     to = nullptr;
@@ -466,8 +472,7 @@ PyObject* rotary_problem(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     void* n[3];
     const int64_t tokens[2] = {q.shape[0], q.shape[1]};
     for (int i = 0; i < 3; ++i) if (!whole_numbers(args[12 + i], i == 0 ? 2 : 1, tokens, g_int32, n[i], what)) return nullptr;
-    PyObject* const elsewhere[5] = {args[1], args[11], args[12], args[13], args[14]};       // (of so many, those that a program may well have on the host)
-    if (!on_one_device(elsewhere, 5, what)) return nullptr;
+    if (!on_one_device(args + 1, 14, d->device, what)) return nullptr;
     Args tail(args + 15);
     const int32_t neighbours = PyObject_IsTrue(*tail.a++), norm = tail.int32();
     bool ok = tail.ok;
@@ -496,6 +501,7 @@ PyObject* rotary_gradients(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     for (const Tensor& x : t) if (type_code(x.dtype) < 0 || x.dtype != t[0].dtype) return refuse("rotary_gradients: dQr, dKr, dQ and dK are of one type, float32, float16 or bfloat16");
     void* w[4];
     for (int i = 0; i < 4; ++i) if (!vector(args[5 + i], t[0].shape[3], g_types[LSP_F32], w[i], what)) return nullptr;
+    if (!on_one_device(args + 1, 8, d->device, what)) return nullptr;
     for (int i = 0; i < 4; ++i) { d->q_shape[i] = t[2].shape[i]; d->k_shape[i] = t[3].shape[i]; d->kr_shape[i] = t[1].shape[i]; }
     d->dtype = type_code(t[0].dtype);
     d->g = lsp_rotary_gradients{t[0].data, t[1].data, t[2].data, t[3].data, static_cast<float*>(w[0]), static_cast<float*>(w[1]), static_cast<float*>(w[2]), static_cast<float*>(w[3]),
@@ -529,7 +535,7 @@ PyObject* cross_entropy_problem(PyObject*, PyObject* const* args, Py_ssize_t nar
     float *losses, *logs;
     if (args[3] == Py_None || args[4] == Py_None) return refuse("cross_entropy_problem: targets and losses are wanted");
     if (!whole_numbers(args[3], 1, h.shape, g_int64, targets, what) || !floats(args[4], h.shape[0], losses, what) || !floats(args[5], h.shape[0], logs, what)) return nullptr;
-    if (!on_one_device(args + 1, 5, what)) return nullptr;
+    if (!on_one_device(args + 1, 5, d->device, what)) return nullptr;
     bool ok = true;
     const float smoothing = number(args[6], ok), z_loss = number(args[7], ok);
     if (!ok) return nullptr;
@@ -553,7 +559,7 @@ PyObject* cross_entropy_gradients(PyObject*, PyObject* const* args, Py_ssize_t n
     float* weights;
     Tensor n;
     if (args[3] != Py_None && !n.read(args[3], 1, what)) return nullptr;
-    if (!floats(args[3], -1, weights, what) || !on_one_device(args + 1, 3, what)) return nullptr;
+    if (!floats(args[3], -1, weights, what) || !on_one_device(args + 1, 3, d->device, what)) return nullptr;
     bool ok = true;
     const float scale = number(args[4], ok);
     if (!ok) return nullptr;
@@ -678,12 +684,38 @@ template <Kind KIND, typename Base, typename OfTensors> struct Given {
         PyBuffer_Release(&v);                          // (the object stays the caller's during the call)
         return true;
     }
+    bool on_host() const { return of_tensors && of_tensors->device < 0; }
     bool is_of(int32_t dtype) const {
         if (!of_tensors || of_tensors->dtype == dtype) return true;
         refuse("the descriptor's tensors are of another type than the call's");
         return false;
     }
 };
+// Whether all sizes are there: the library refuses a problem without
+bool sizes_are_there(const lsp_attention_problem& p) { return p.batch && p.q_len && p.k_len && p.heads && p.kv_heads && p.head_dim; }
+bool sizes_are_there(const lsp_residual_norm_problem& p) { return p.rows && p.width; }
+bool sizes_are_there(const lsp_rotary_problem& p) { return p.batch && p.length && p.cache && p.heads && p.kv_heads && p.head_dim; }
+bool sizes_are_there(const lsp_cross_entropy_problem& p) { return p.rows && p.width && p.vocab; }
+// Whether a call may go to the library as far as devices go: a workspace that is a tensor is where the problem's tensors are, and those are not on the host, but for a call that the library refuses for
+// its sizes or its workspace (`need`: bytes of it), with the code that it has for that.  False with a Python exception set.
+template <typename Problem> bool may_run(const Problem& p, PyObject* workspace, const void* ws, size_t bytes, size_t need) {
+    if (!p.of_tensors) return true;
+    const int32_t device = p.of_tensors->device;
+    if (device < 0) {
+        if (!sizes_are_there(*p.p) || (need && (!ws || bytes < need))) return true;
+        refuse("the descriptor's tensors are on the host");
+        return false;
+    }
+    if (!ws || PyLong_Check(workspace)) return true;
+    long there;
+    if (!device_of(workspace, there)) {
+        if (!PyErr_ExceptionMatches(PyExc_AttributeError)) return false;
+        PyErr_Clear();
+        there = -1;                                    // (numpy's)
+    }
+    if (there != device) { refuse("the workspace is on another device than the descriptor's tensors"); return false; }
+    return true;
+}
 using GivenAttention = Given<ATTENTION, lsp_attention_problem, AttentionOfTensors>;
 using GivenAttentionGradients = Given<ATTENTION_GRADIENTS, lsp_attention_gradients, AttentionGradientsOfTensors>;
 using GivenResidualNorm = Given<RESIDUAL_NORM, lsp_residual_norm_problem, ResidualNormOfTensors>;
@@ -701,7 +733,7 @@ template <typename P> bool problem_of(Args& a, P& p, int32_t& dtype) {
 }
 
 // (problem, dtype, workspace, workspace_bytes, stream)
-template <typename Problem, typename Entry> PyObject* forward(Entry entry, PyObject* const* args, Py_ssize_t nargs) {
+template <typename Problem, typename Entry, typename Query> PyObject* forward(Entry entry, Query query, PyObject* const* args, Py_ssize_t nargs) {
     if (!count_is(nargs, 5)) return nullptr;
     Args a(args);
     Problem p;
@@ -710,13 +742,13 @@ template <typename Problem, typename Entry> PyObject* forward(Entry entry, PyObj
     void* ws = a.pointer();
     const size_t bytes = a.integer();
     void* st = a.stream();
-    if (!a.ok) return nullptr;
+    if (!a.ok || !may_run(p, args[2], ws, bytes, p.on_host() ? query(p.p, static_cast<lsp_dtype>(dtype)) : 0)) return nullptr;
     return without_gil([&] { return entry(p.p, static_cast<lsp_dtype>(dtype), ws, bytes, st); });
 }
-PyObject* attention_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return forward<GivenAttention>(g_attention_forward, args, nargs); }
-PyObject* cross_entropy_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return forward<GivenCrossEntropy>(g_loss_forward, args, nargs); }
+PyObject* attention_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return forward<GivenAttention>(g_attention_forward, g_attention_forward_bytes, args, nargs); }
+PyObject* cross_entropy_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return forward<GivenCrossEntropy>(g_loss_forward, g_loss_forward_bytes, args, nargs); }
 // (problem, gradients, dtype, workspace, workspace_bytes, stream)
-template <typename Problem, typename Gradients, typename Entry> PyObject* backward(Entry entry, PyObject* const* args, Py_ssize_t nargs) {
+template <typename Problem, typename Gradients, typename Entry, typename Query> PyObject* backward(Entry entry, Query query, PyObject* const* args, Py_ssize_t nargs) {
     if (!count_is(nargs, 6)) return nullptr;
     Args a(args);
     Problem p;
@@ -728,17 +760,19 @@ template <typename Problem, typename Gradients, typename Entry> PyObject* backwa
     void* st = a.stream();
     if (!a.ok || !p.is_of(dtype) || !g.is_of(dtype)) return nullptr;
     if (p.of_tensors && g.of_tensors && !matches(*p.of_tensors, *g.of_tensors)) return refuse("the gradients are of other shapes than the problem's tensors");
+    if (p.of_tensors && g.of_tensors && p.of_tensors->device != g.of_tensors->device) return refuse("the gradients are on another device than the problem's tensors");
+    if (!may_run(p, args[3], ws, bytes, p.on_host() ? query(p.p, static_cast<lsp_dtype>(dtype)) : 0)) return nullptr;
     return without_gil([&] { return entry(p.p, g.p, static_cast<lsp_dtype>(dtype), ws, bytes, st); });
 }
 PyObject* attention_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-    return backward<GivenAttention, GivenAttentionGradients>(g_attention_backward, args, nargs);
+    return backward<GivenAttention, GivenAttentionGradients>(g_attention_backward, g_attention_backward_bytes, args, nargs);
 }
 PyObject* residual_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-    return backward<GivenResidualNorm, GivenResidualNormGradients>(g_norm_backward, args, nargs);
+    return backward<GivenResidualNorm, GivenResidualNormGradients>(g_norm_backward, g_norm_backward_bytes, args, nargs);
 }
-PyObject* rotary_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return backward<GivenRotary, GivenRotaryGradients>(g_rotary_backward, args, nargs); }
+PyObject* rotary_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return backward<GivenRotary, GivenRotaryGradients>(g_rotary_backward, g_rotary_backward_bytes, args, nargs); }
 PyObject* cross_entropy_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-    return backward<GivenCrossEntropy, GivenCrossEntropyGradients>(g_loss_backward, args, nargs);
+    return backward<GivenCrossEntropy, GivenCrossEntropyGradients>(g_loss_backward, g_loss_backward_bytes, args, nargs);
 }
 // (problem, dtype, stream)
 template <typename Problem, typename Entry> PyObject* forward_alone(Entry entry, PyObject* const* args, Py_ssize_t nargs) {
@@ -748,16 +782,16 @@ template <typename Problem, typename Entry> PyObject* forward_alone(Entry entry,
     int32_t dtype;
     if (!problem_of(a, p, dtype)) return nullptr;
     void* st = a.stream();
-    if (!a.ok) return nullptr;
+    if (!a.ok || !may_run(p, Py_None, nullptr, 0, 0)) return nullptr;
     return without_gil([&] { return entry(p.p, static_cast<lsp_dtype>(dtype), st); });
 }
 PyObject* residual_norm_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return forward_alone<GivenResidualNorm>(g_norm_forward, args, nargs); }
 PyObject* rotary_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) { return forward_alone<GivenRotary>(g_rotary_forward, args, nargs); }
 
 // (addresses of lsp_dropout, lsp_attention_forward, lsp_attention_backward, lsp_residual_norm_forward, lsp_residual_norm_backward, lsp_rotary_forward, lsp_rotary_backward,
-// lsp_cross_entropy_forward, lsp_cross_entropy_backward; the classes of the C structures, in the order of Kind, and those of descriptors made of tensors)
+// lsp_cross_entropy_forward, lsp_cross_entropy_backward, and of the workspace queries of those that have one, in the same order; the classes of the C structures, in the order of Kind, and those of descriptors made of tensors)
 PyObject* bind_operators(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-    constexpr int kCalls = 9;
+    constexpr int kCalls = 15;
     if (!count_is(nargs, kCalls + 2 * KINDS)) return nullptr;
     Args a(args);
     void* p[kCalls];
@@ -778,6 +812,12 @@ PyObject* bind_operators(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     g_rotary_backward = reinterpret_cast<decltype(g_rotary_backward)>(p[6]);
     g_loss_forward = reinterpret_cast<decltype(g_loss_forward)>(p[7]);
     g_loss_backward = reinterpret_cast<decltype(g_loss_backward)>(p[8]);
+    g_attention_forward_bytes = reinterpret_cast<decltype(g_attention_forward_bytes)>(p[9]);
+    g_attention_backward_bytes = reinterpret_cast<decltype(g_attention_backward_bytes)>(p[10]);
+    g_norm_backward_bytes = reinterpret_cast<decltype(g_norm_backward_bytes)>(p[11]);
+    g_rotary_backward_bytes = reinterpret_cast<decltype(g_rotary_backward_bytes)>(p[12]);
+    g_loss_forward_bytes = reinterpret_cast<decltype(g_loss_forward_bytes)>(p[13]);
+    g_loss_backward_bytes = reinterpret_cast<decltype(g_loss_backward_bytes)>(p[14]);
     Py_RETURN_NONE;
 }
 
