@@ -511,8 +511,8 @@ int    lsp_residual_norm_backward(const lsp_residual_norm_problem* problem, cons
  * each head of each token by itself.  norm: lsp_norm over the head_dim elements of a head, with weight [+ bias] as below (LSP_NORM_NONE: not
  * read).  rotate: pair j < rotated / 2 of a head turns by the angle position * frequencies[j],
  *   (a, b) -> (a cos - b sin, a sin + b cos);   elements from `rotated` on stay.
- * A pair is elements (j, rotated / 2 + j) or, with neighbours = 1, (2 j, 2 j + 1).  Angles are computed in fp64 (a far position keeps all
- * digits), their sines, the norms and the turning in fp32; the result is rounded once.
+ * A pair is elements (j, rotated / 2 + j) or, with neighbours = 1, (2 j, 2 j + 1).  Angles are computed in fp64 with what its roundings
+ * take off (a far position keeps all digits, as long as position * frequency is below 2^70), their sines, the norms and the turning in fp32; the result is rounded once.
  * Token i of text b counts when i < lens[b] (lengths outside [0, length] are taken as the nearer end; NULL: all count).  Its position is
  * positions[b][i] or, where that is NULL, starts[b] + i (starts NULL: i).  Its key goes to place starts[b] + i of the text's `cache` places in Kr, and its
  * value there in Vr, so that the caches that lsp_attention_forward reads are filled by the call that turns the keys (cache = length and starts =

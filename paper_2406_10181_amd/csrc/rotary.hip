@@ -4,7 +4,7 @@
 // head, eight elements a lane, so that the sums of a norm go through the lanes of a group by moves that need no LDS.  A lane's eight elements are four
 // whole pairs: four elements from each half of what turns, or eight neighbours; so turning needs no other lane.  A wave has 4, 8 or 16 heads of one token at a time, whose addresses are a scalar
 // base and what the lane adds to it once (with addresses of its own for every head a lane spent 240 instructions on one in the backward pass).  A workgroup has the queries, the keys
-// or the values of a few tokens that follow one another; its angles, an fp64 product, a sine and a cosine each, are made once for all their heads and lie in LDS.
+// or the values of a few tokens that follow one another; its angles, some products in fp64, a sine and a cosine each, are made once for all their heads and lie in LDS.
 #include <algorithm>
 
 #include "rotary.h"
@@ -99,7 +99,29 @@ struct Tokens {
     int64_t x[kRotaryTokens], y[kRotaryTokens], out[kRotaryTokens];      // elements from the tensors' begins to the token's first head; -1: not there
     int64_t position[kRotaryTokens];
 };
-// Whole turns are taken off in fp64: position and frequency have 55 bits together at most, and what is left of a turn keeps at least 30 behind the point.
+// Turns of an angle that is position * frequency.  One over 2 pi comes in two parts, and what each product's rounding takes off is added: a product of 2^31 alone would be off by 2^-23 of a turn, this is by
+// 2^-53 up to 2^51 and by 2^-35 at 2^71 radians.  (Contracted, turns - rint(turns) would have the product without its rounding, and that would count twice.)  Whole turns and then quarters are taken off in
+// fp64, so that fp32 has 1/8 of a turn at most, off by 2^-28: there Taylor's series of five and six terms leave 0.1 EPS, and sine and cosine are off by 2.8 and 1.8 EPS at most (EPS = 2^-24; the library's
+// sincospif, with quarters of its own: 2 heads of 128 over 11720 tokens 4 % longer).
+__device__ __forceinline__ void sine_and_cosine(int64_t position, float frequency, float& sin, float& cos) {
+#pragma clang fp contract(off)
+    constexpr double kPerRadian = 0.15915494309189535, kRest = -9.839338337591243e-18;
+    const double f = (double)frequency, p = (double)position;
+    const double each = f * kPerRadian, each_rest = fma(f, kPerRadian, -each) + f * kRest;
+    const double turns = p * each, rest = fma(p, each, -turns) + p * each_rest;
+    double left = (turns - rint(turns)) + rest;
+    left -= rint(left);
+    const double quarters = rint(4.0 * left);
+    const float x = (float)fma(-0.25, quarters, left), t = x * x;
+    // (coefficients: (2 pi)^k / k!, of alternating sign)
+    const float s = x * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 42.0586939f, -76.7058563f), 81.6052475f), -41.3417015f), 6.28318548f);
+    const float c = fmaf(t, fmaf(t, fmaf(t, fmaf(t, fmaf(t, -26.4262562f, 60.2446404f), -85.4568176f), 64.9393921f), -19.7392082f), 1.0f);
+    const int quarter = (int)quarters & 3;
+    sin = quarter & 1 ? c : s;
+    cos = quarter & 1 ? s : c;
+    if (quarter & 2) sin = -sin;
+    if (quarter == 1 || quarter == 2) cos = -cos;
+}
 __device__ __forceinline__ void set_tokens(Tokens& t, const RotaryArgs& a, const RotarySegment& s, int first, int n, bool backward) {
     if ((int)threadIdx.x < n) {
         const int token = first + threadIdx.x, text = token / a.length, i = token - text * a.length;
@@ -115,8 +137,7 @@ __device__ __forceinline__ void set_tokens(Tokens& t, const RotaryArgs& a, const
     const int pairs = a.rotated / 2;
     for (int k = threadIdx.x; k < n * pairs; k += kRotaryThreads) {
         const int token = k / pairs, pair = k - token * pairs;
-        const double turns = (double)t.position[token] * ((double)a.frequencies[pair] * 0.15915494309189533577);
-        sincospif(2.0f * (float)(turns - rint(turns)), &t.sin[token][pair], &t.cos[token][pair]);
+        sine_and_cosine(t.position[token], a.frequencies[pair], t.sin[token][pair], t.cos[token][pair]);
     }
     __syncthreads();
 }
