@@ -574,7 +574,7 @@ int    lsp_rotary_backward(const lsp_rotary_problem* problem, const lsp_rotary_g
  *   H        device, [rows][width] of `dtype`;  W  [vocab][width]; with row strides (elements), multiples of 16 bytes below 8 MiB
  *   targets  device, [rows] int64
  *   losses   device, [rows] fp32;  logs: the same for L, or NULL
- *   width    a multiple of 8, at most 2^16;  rows at most LSP_MAX_ROWS;  vocab at most 2^20;  0 <= smoothing < 1;  0 <= z_loss <= 1
+ *   all of them, and weights, 16-byte aligned;  width    a multiple of 8, at most 2^16;  rows at most LSP_MAX_ROWS;  vocab at most 2^20;  0 <= smoothing < 1;  0 <= z_loss <= 1
  * lsp_cross_entropy_backward gives losses and logs too (it needs no forward call before it), and the gradients of
  *   scale * sum over the rows of weights * losses
  * with respect to H (dH, rows that do not count: zeros) and W (dW), overwritten; either may be NULL.  What is written overlaps nothing else.  weights: device, [rows] fp32, or NULL: ones (of rows that
@@ -583,6 +583,7 @@ int    lsp_rotary_backward(const lsp_rotary_problem* problem, const lsp_rotary_g
  * exponentials are kept in 16 bits (fp32: in 32), each relative to the largest of its row in a piece of the vocabulary (what is below 2^-29 of that loses digits, and is 0 below
  * 2^-40), and become the gradient of z in place, rounded to `dtype` before the second products; a target's is p - 1 of z in fp32, and dH has it without that rounding.  No atomics that add:
  * results are the same bits from run to run.  A logit that is not finite reaches its row's loss and dH, and all of dW.
+ * fp16: the gradients of z have one scale, by the largest |weight|; a row whose weight is 2^-18 of that loses digits of its small probabilities' gradients, and one of 2^-38 has none of them left.
  * Workspaces: 16-byte aligned, as large as the queries say: bounded but for 4 bytes a row, however many there are. */
 typedef struct {
     const void*    H;
@@ -619,11 +620,12 @@ int    lsp_cross_entropy_backward(const lsp_cross_entropy_problem* problem, cons
  * of exponent, 3 of mantissa, largest 448) times m_scale; v is without sign, 5 bits of exponent and 3 of mantissa: code 0 is 0 and code c otherwise
  * 2^((c >> 3) - 31) * (1 + (c & 7) / 8) (largest 1.875), times v_scale.  The step takes m and v before they are rounded (to nearest, ties to even; a v
  * that is not 0 never becomes 0 (but below 2^-149 of the largest), so that no small v makes a large step); a scale is the block's largest magnitude over 448 or 1.875.  State that is all zeros,
- * codes and scales, is where training begins.  A gradient that is not finite spoils its element and, in 8 bits, can spoil its block's states.
+ * codes and scales, is where training begins.  A gradient that is not finite, or whose
+ * square is not in fp32, spoils its element and, in 8 bits, can spoil its block's states.
  *   items       HOST array of `count` descriptors, 1 <= count <= LSP_MAX_TENSORS, read during the call only; no tensor twice, no overlaps
  *   step        number of this step, from 1 on (a captured call repeats it);  0 <= beta < 1, eps >= 0 (an element whose m and v are 0 gets no update but decay, whatever eps is)
  *   grad_scale  device, one fp32 (of clipping, or of a scaled loss), or NULL: 1.  Where it is not finite the step does nothing
- * At most 2^35 elements a call, all tensors padded to 4096. */
+ * At most 2^35 elements a tensor, and in all, each tensor padded to a multiple of 4096, fewer than 2^36.  Tensors are 16-byte aligned, scales and grad_scale 4-byte. */
 typedef enum { LSP_STATE_F32 = 0, LSP_STATE_8BIT = 1 } lsp_state;
 
 typedef struct {

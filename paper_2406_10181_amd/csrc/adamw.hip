@@ -2,7 +2,7 @@
 //
 // Bound by memory: a bf16 element takes 22 bytes with states in fp32 (30 with an fp32 master) and 10 with states in 8 bits; nothing is read twice.  A thread
 // takes eight elements that follow one another, so that every stream goes in loads of 8 to 32 bytes a lane, and 32 lanes have the 256 elements of a scale:
-// its maximum goes through the 32 lanes without LDS.  A workgroup has 2048 elements of one tensor; the tensors' descriptors come with the launch (52 or
+// its maximum goes through the 32 lanes without LDS.  A workgroup has 4096 elements of one tensor, in rounds of 2048; the tensors' descriptors come with the launch (52 or
 // 64 of them), so that a model's many small tensors take few launches and no memory of their own.
 #include "adamw.h"
 #include "rows.h"

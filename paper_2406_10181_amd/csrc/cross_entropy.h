@@ -8,7 +8,7 @@
 //
 // Of the roundings on the way one would be seen in 16 bits, that of a target's dz, which is most of its row: dH gets what it takes off, times the target's row of W, behind the products; for
 // dW the gradient's scale keeps it small, and of up to 32 rows what is taken off has rows of its own.  dH is as far from the exact one as a result that is rounded once, dW up to 1.4 times as
-// far (before this both 1.4 times, and of few rows 1.6).
+// far.  Weights of fp16 that differ by 2^18 and more cost the small ones' rows digits: one scale serves all, since dW's products run over the rows.
 //
 // 6 rows width vocab operations in all: keeping 16 bits an exponential, 2 bytes written, read, written and read twice, costs less than a second product
 // would.  4096 rows, width 4096, 32000 words in bf16: logits 0.79-0.85 ms, dz 0.08 (6.5 TB/s), both gradients 1.55-1.65 ms, 2.44 ms in all, 1320 TFLOP/s, which is what the power allows of
@@ -75,10 +75,10 @@ template <typename D> constexpr float kLossTopLog2 = std::is_same<D, F32>::value
 __device__ __forceinline__ int rows_of_block(const LossArgs& a) {
     return min(max(*as_const<int32_t>(a.count) - a.block * a.block_rows, 0), a.block_rows);
 }
-// Parts of the vocabulary that dH is made of, and the rows between two parts' sums: where fewer rows count than there are, their tiles get the workgroups (and the room) that the others would
-// have had.  (3001 rows of which 1800 count, width 1000, 50021 words, fp16: dH in a launch of its own 183 us, with the parts planned for all rows 230.)
 // How many rows dW is a product of
 __device__ __forceinline__ int rows_of_dw(const LossArgs& a, int rows) { return a.twice ? 2 * rows : rows; }
+// Parts of the vocabulary that dH is made of, and the rows between two parts' sums: where fewer rows count than there are, their tiles get the workgroups (and the room) that the others would
+// have had.  (3001 rows of which 1800 count, width 1000, 50021 words, fp16: dH in a launch of its own 183 us, with the parts planned for all rows 230.)
 struct LossParts { int splits, rows; };
 __device__ __forceinline__ LossParts parts_of_dh(const LossArgs& a, int rows) {
     const int tile = a.tile[1], tiles = (rows + tile - 1) / tile;

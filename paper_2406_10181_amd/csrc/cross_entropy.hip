@@ -1,4 +1,4 @@
-// Cross entropy: which rows count, the rows' losses, the gradient of z, and the plan.  The products are in cross_entropy.h.
+// Cross entropy: which rows count, the rows' losses, the gradient of z, and the plan.  The products are in cross_entropy_products.h.
 #include <algorithm>
 #include <cmath>
 
@@ -206,7 +206,7 @@ __device__ __forceinline__ void store_loss(const LossArgs& a, int row, int64_t t
     if (a.logs) a.logs[to] = L;
 }
 
-// L and the losses: 16 rows a workgroup.  (4096 rows of 250 pieces 9 us, 8192 of 1000 25.)
+// Maxima, sums and losses: 16 rows a workgroup.  (4096 rows of 250 pieces 9 us, 8192 of 1000 25.)
 template <int RUNS>
 __global__ __launch_bounds__(16 * RUNS) void k_loss_rows(LossArgs a, int fp16) {
     __shared__ Runs<RUNS> runs;
@@ -236,11 +236,11 @@ __global__ __launch_bounds__(16 * RUNS) void k_loss_rows(LossArgs a, int fp16) {
     if (r == 0) atomicMax(reinterpret_cast<unsigned*>(a.count) + 1, __float_as_uint(bound));
 }
 
-constexpr int kDzRuns = 16, kDzPieces = 4 * kDzRuns;                     // threads a row, and the most pieces that k_loss_dz makes L of
+constexpr int kDzRuns = 16, kDzPieces = 4 * kDzRuns;                     // threads a row, and the most pieces that k_loss_dz joins
 constexpr int kDzColumns = 512;                                          // of a workgroup of k_loss_dz, in steps of 128
 
 // dz = (p (1 + 2 z_loss L) - smoothing / vocab - (1 - smoothing) [v = target]) factor in place of the exponentials: 16 rows a workgroup, so that the pieces' maxima come in
-// whole lines.  Two bytes read and two written an element: bound by memory (4096 rows of 32000 in bf16 80 us, 6.6 TB/s).  ROWS: the rows' L are made here too, by every workgroup of a row (and the losses by the first), which
+// whole lines.  Two bytes read and two written an element: bound by memory (4096 rows of 32000 in bf16 80 us, 6.6 TB/s).  ROWS: the rows' maxima and sums are made here too, by every workgroup of a row (and the losses by the first), which
 // saves a launch where the pieces are few (64 x 256 x 1000 in fp32, all of a call: 30.4 us, 32.1 with it); not in fp16, whose scale goes by all rows.
 template <typename D, bool ROWS>
 __global__ __launch_bounds__(256) void k_loss_dz(LossArgs a) {

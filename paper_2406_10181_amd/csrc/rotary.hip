@@ -194,7 +194,7 @@ template <int NORM, int GROUP> __device__ __forceinline__ void norm_head(Eight& 
     }
 }
 
-// 4 x 1024 tokens of 32 + 32 heads of 128 in bf16, 134 MB: 24.2 us, 5.5 TB/s; 16384 tokens of 16 + 16 heads of 64 in fp32, 268 MB, 47.6 us, 5.6 TB/s.
+// 4 x 1024 tokens of 32 + 32 heads of 128 in bf16, 134 MB: 24.4 us, 5.5 TB/s; 16384 tokens of 16 + 16 heads of 64 in fp32, 268 MB, 47.1 us, 5.7 TB/s.
 template <typename D, int NORM, int GROUP, bool NEIGHBOURS>
 __global__ __launch_bounds__(kRotaryThreads) void k_rotary(RotaryArgs a) {
     constexpr int kHeads = 64 / GROUP, kWaves = kRotaryThreads / 64;     // heads that a wave has at a time
